@@ -68,7 +68,8 @@ enum {
   MTPC_STATUS_BAD_TARGET = 1u,  /* a target >= v was seen; that window's log-prob is NaN               */
   MTPC_STATUS_BAD_UNIFORM = 2u, /* a uniform outside [0,1) was seen; that draw returned -1 and the log-prob
                                    (or the prefix log-marginals from that byte on) of its window is NaN */
-  MTPC_STATUS_TIMEOUT = 4u      /* a bounded barrier wait expired; the outputs of that call are invalid */
+  MTPC_STATUS_TIMEOUT = 4u,     /* a bounded barrier wait expired; the outputs of that call are invalid */
+  MTPC_STATUS_BAD_TOKEN = 8u    /* the embedding calls: a token >= v was seen; its row is NaN, it has no gradient */
 };
 
 typedef struct {
@@ -447,6 +448,103 @@ int mtpc_debug_set_draft_grouping(mtpc_head* head, int32_t mode);
 int mtpc_window_logprob_static(const mtpc_config* cfg, const void* W_emit, const void* W_sum,
                                const float* T_static, const void* hidden, const int32_t* targets, int32_t T,
                                float* out_logprob, uint32_t* out_status, void* stream);
+
+/* ------------------------------------------------------------------------------------------------------------
+ * What a training or decoding step does beside the head. These calls need no head (as mtpc_lowrank_compose). They enqueue work on `stream`,
+ * a stream of the current device, on which all their buffers lie, and do nothing else unless stated, so they may be recorded into a
+ * CUDA graph; calls that share a workspace must be ordered, as must replays of graphs that do. Matrices are rows of adjacent elements,
+ * `stride` elements from one row to the next: >= 0 for a matrix that is read (0: the same row every time), >= its width for one
+ * that is written (MTPC_ERR_SHAPE otherwise; with one row it is not looked at). Any alignment of whole elements works (MTPC_ERR_SHAPE
+ * for less); widths, strides and addresses that are multiples of eight elements are fastest. Sums are fp32 or more, in an order that
+ * sizes and alignment fix: the same call gives the same bits. Every output is rounded once.
+ * ------------------------------------------------------------------------------------------------------------ */
+
+/*
+ * Byte embeddings: out[t] = scale * table[tokens[t]], the rows a model reads for its input bytes (in decoding: those that
+ * mtpc_speculative_accept returned).
+ *   tokens  dev [T] int32; a negative one is padding, whose row is zeros. A token >= v gives a row of NaN and MTPC_STATUS_BAD_TOKEN.
+ *   table   dev [v, d] table_dtype;  out dev [T, d] out_dtype (MTPC_F32 | MTPC_BF16 each), not overlapping.
+ *   out_status dev uint32 or NULL: the call's MTPC_STATUS_* bits are or-ed into it (the caller clears it).
+ * 0 <= T <= 2^26, 1 <= v <= 2^20 and 1 <= d <= 2^20 (MTPC_ERR_UNSUPPORTED beyond).
+ */
+int mtpc_embed(const int32_t* tokens, int32_t T, const void* table, int64_t table_stride, int32_t table_dtype, int32_t v, int32_t d,
+               float scale, void* out, int64_t out_stride, int32_t out_dtype, uint32_t* out_status, void* stream);
+
+/*
+ * Their gradient: d_table[b] = scale * sum of d_out[t] over the positions t with tokens[t] = b, for every b in [0, v): OVERWRITTEN (rows
+ * of tokens that do not occur become zeros), or with accumulate != 0 added to what is there (a table that is tied to the unembeddings:
+ * W_base[0] of a factored head). Padding and tokens >= v contribute nothing; out_status as above.
+ *   d_out dev [T, d] d_out_dtype;  d_table dev [v, d] fp32, not overlapping.
+ *   workspace dev, 256-byte aligned, >= mtpc_embed_backward_workspace_bytes(T, v, d): the positions in the order of their tokens and partial
+ *             sums (10 MB at T = 8192, d = 4096).
+ */
+int mtpc_embed_backward_workspace_bytes(int32_t T, int32_t v, int32_t d, size_t* out_bytes);
+int mtpc_embed_backward(const int32_t* tokens, int32_t T, const void* d_out, int64_t d_out_stride, int32_t d_out_dtype, float scale,
+                        int32_t v, int32_t d, float* d_table, int64_t d_table_stride, int32_t accumulate, void* workspace,
+                        size_t workspace_bytes, uint32_t* out_status, void* stream);
+
+/*
+ * The residual stream's addition and the root-mean-square norm behind it, whose output the head reads as hidden states:
+ *   s = x + residual,   out = s * (mean over the row of s^2 + eps)^(-1/2) * weight
+ * s is fp32 throughout: out is formed from the sum before it is rounded to out_sum.
+ *   x, residual, out_sum, out dev [T, d] io_dtype. residual may be NULL (s = x), so may out_sum (s is not wanted). out_sum and out may
+ *           each be the buffer of x or of residual, with its stride; overlaps otherwise are not allowed.
+ *   weight  dev [d] weight_dtype, or NULL (ones).   eps > 0.
+ *   out_codes, out_scales: the output in 8 bits, both NULL if it is not wanted; out may be NULL if it is. out_codes dev [T, d] e4m3
+ *           bytes, out_scales dev [T, ceil(d / scale_group)] fp32, adjacent rows: one scale per scale_group columns (32, 64, 128; the last group
+ *           may be short) or per row (scale_group = 0). scale = the group's largest |out| / 448 (1 if that is 0), code = out / scale
+ *           rounded to nearest (ties to even, out not rounded before); code * scale stands for out. A group that holds a NaN or an infinity
+ *           has a scale that is none either.
+ * 1 <= d <= 32768 (MTPC_ERR_UNSUPPORTED beyond), 0 <= T <= 2^30. A row's squares may exceed fp32's range.
+ */
+int mtpc_residual_rmsnorm(const void* x, int64_t x_stride, const void* residual, int64_t residual_stride, const void* weight,
+                          int32_t weight_dtype, int32_t T, int32_t d, int32_t io_dtype, float eps, void* out_sum, int64_t sum_stride,
+                          void* out, int64_t out_stride, uint8_t* out_codes, int64_t codes_stride, float* out_scales,
+                          int32_t scale_group, void* stream);
+
+/*
+ * Its gradients at the sum s that the forward call left in out_sum (or x, where there was no residual):
+ *   d_x      = rstd * (weight * d_out - s * rstd^2 * mean over the row of (weight * d_out * s)) + d_sum
+ *   d_weight = sum over the rows of d_out * s * rstd
+ *   sum    dev [T, d] io_dtype;  d_out dev [T, d] d_out_dtype: the gradient of out (the head's d_hidden: MTPC_F32).
+ *   d_sum  dev [T, d] d_x_dtype or NULL: the gradient that reaches s along the residual stream.
+ *   d_x    dev [T, d] d_x_dtype: the gradient of s, which is that of x and that of residual; may be the buffer of d_sum, or of d_out or sum
+ *          where the types are the same, with its stride.
+ *   d_weight dev [d] fp32, overwritten, or NULL.
+ *   workspace dev, 256-byte aligned, >= mtpc_residual_rmsnorm_backward_workspace_bytes(T, d): parts of d_weight; not needed without it.
+ */
+int mtpc_residual_rmsnorm_backward_workspace_bytes(int32_t T, int32_t d, size_t* out_bytes);
+int mtpc_residual_rmsnorm_backward(const void* sum, int64_t sum_stride, int32_t io_dtype, const void* weight, int32_t weight_dtype,
+                                   int32_t T, int32_t d, float eps, const void* d_out, int64_t d_out_stride, int32_t d_out_dtype,
+                                   const void* d_sum, int64_t d_sum_stride, void* d_x, int64_t d_x_stride, int32_t d_x_dtype,
+                                   float* d_weight, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The norm of all gradients of a model together, and clipping: norm = sqrt(sum of g^2 over all entries) and, if norm > max_norm, every g
+ * multiplied by max_norm / norm. A list is made once of the buffers that the training calls write (they are overwritten step
+ * after step) and then serves a call per step.
+ *   entries  HOST array [count]: data dev [count] dtype, adjacent; out: where the scaled gradient goes, out_dtype: data itself (in place, the
+ *            same dtype), another buffer, or NULL (the entry counts in the norm and is not scaled). Results may not overlap
+ *            other results or other entries' data (MTPC_ERR_SHAPE). Entries may be empty, of any number and size.
+ *   workspace dev, 256-byte aligned, >= mtpc_gradient_list_workspace_bytes(entries, count); owned by the caller, used by every
+ *            call on this list, and must outlive it. Creation writes the list's chunks there and waits for `stream` (not for capture);
+ *            the entries themselves are not needed afterwards.
+ * mtpc_clip_gradients: max_norm > 0, or infinity (the norm alone; results in other buffers are then copies). out_norm dev [1] fp32: the norm
+ * before clipping (infinity if fp32 cannot hold it). Squares and sums are fp64. With a norm that is not finite (an infinity or NaN among
+ * the gradients) nothing is scaled: out_norm tells, and the caller leaves the step out. As a head, a list must not be used from two streams at once.
+ */
+typedef struct {
+  const void* data;
+  void* out;
+  int64_t count;
+  int32_t dtype, out_dtype;
+} mtpc_gradient;
+typedef struct mtpc_gradient_list mtpc_gradient_list; /* opaque; freed by mtpc_destroy_gradient_list */
+int mtpc_gradient_list_workspace_bytes(const mtpc_gradient* entries, int32_t count, size_t* out_bytes);
+int mtpc_create_gradient_list(const mtpc_gradient* entries, int32_t count, void* workspace, size_t workspace_bytes, void* stream,
+                              mtpc_gradient_list** out);
+int mtpc_clip_gradients(mtpc_gradient_list* list, float max_norm, float* out_norm, void* stream);
+int mtpc_destroy_gradient_list(mtpc_gradient_list* list);
 
 /* Frees the host-side object (the workspace and the weights stay the caller's). Synchronises nothing. */
 int mtpc_destroy(mtpc_head* head);

@@ -16,7 +16,7 @@ MTPC_F32, MTPC_BF16 = 0, 1
 MTPC_FLAG_HMM_CONTEXTUAL = 1
 MTPC_FLAG_SHORT_DRAFTS = 4
 MTPC_OK = 0
-STATUS_BAD_TARGET, STATUS_BAD_UNIFORM, STATUS_TIMEOUT = 1, 2, 4
+STATUS_BAD_TARGET, STATUS_BAD_UNIFORM, STATUS_TIMEOUT, STATUS_BAD_TOKEN = 1, 2, 4, 8
 
 EXPORTS = [
     "mtpc_workspace_bytes", "mtpc_create_head", "mtpc_window_logprob", "mtpc_draft_sample",
@@ -27,18 +27,26 @@ EXPORTS = [
     "mtpc_lowrank_compose", "mtpc_lowrank_backward", "mtpc_update_parameters", "mtpc_debug_set_wait_limit_ns",
     "mtpc_debug_set_projection_variant", "mtpc_debug_set_draft_grouping", "mtpc_lowrank_workspace_bytes",
     "mtpc_create_head_lowrank", "mtpc_lowrank_backward_workspace_bytes", "mtpc_lowrank_window_logprob_backward",
-    "mtpc_lowrank_window_loss_backward",
+    "mtpc_lowrank_window_loss_backward", "mtpc_embed", "mtpc_embed_backward", "mtpc_embed_backward_workspace_bytes",
+    "mtpc_residual_rmsnorm", "mtpc_residual_rmsnorm_backward", "mtpc_residual_rmsnorm_backward_workspace_bytes",
+    "mtpc_gradient_list_workspace_bytes", "mtpc_create_gradient_list", "mtpc_clip_gradients", "mtpc_destroy_gradient_list",
 ]
 STATIC_SCRATCH_BYTES = 16 << 20
 ERR_STATIC_SCRATCH = -7
 ERR_STATE = -8
 ERR_TIMEOUT = -6
+ERR_NULL, ERR_SHAPE, ERR_UNSUPPORTED = -1, -2, -3
 
 
 class MtpcConfig(ctypes.Structure):
     _fields_ = [("family", ctypes.c_int32), ("n", ctypes.c_int32), ("r", ctypes.c_int32), ("v", ctypes.c_int32),
                 ("d", ctypes.c_int32), ("io_dtype", ctypes.c_int32), ("max_positions", ctypes.c_int32),
                 ("max_windows_per_pos", ctypes.c_int32), ("flags", ctypes.c_uint32), ("v_valid", ctypes.c_int32)]
+
+
+class MtpcGradient(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("out", ctypes.c_void_p), ("count", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("out_dtype", ctypes.c_int32)]
 
 
 class MtpcError(RuntimeError):
@@ -91,6 +99,17 @@ def lib() -> ctypes.CDLL:
     L.mtpc_lowrank_window_loss_backward.argtypes = [vp, vp, vp, i32, i32, ctypes.c_float, vp, sz, vp, vp, vp, vp, vp, vp, vp,
                                                     vp, vp]
     L.mtpc_create_head_lowrank.argtypes = [ctypes.POINTER(MtpcConfig), i32, vp, vp, vp, vp, vp, vp, sz, vp, ctypes.POINTER(vp)]
+    i64, f32 = ctypes.c_int64, ctypes.c_float
+    L.mtpc_embed.argtypes = [vp, i32, vp, i64, i32, i32, i32, f32, vp, i64, i32, vp, vp]
+    L.mtpc_embed_backward_workspace_bytes.argtypes = [i32, i32, i32, ctypes.POINTER(sz)]
+    L.mtpc_embed_backward.argtypes = [vp, i32, vp, i64, i32, f32, i32, i32, vp, i64, i32, vp, sz, vp, vp]
+    L.mtpc_residual_rmsnorm.argtypes = [vp, i64, vp, i64, vp, i32, i32, i32, i32, f32, vp, i64, vp, i64, vp, i64, vp, i32, vp]
+    L.mtpc_residual_rmsnorm_backward_workspace_bytes.argtypes = [i32, i32, ctypes.POINTER(sz)]
+    L.mtpc_residual_rmsnorm_backward.argtypes = [vp, i64, i32, vp, i32, i32, i32, f32, vp, i64, i32, vp, i64, vp, i64, i32, vp, vp, sz, vp]
+    L.mtpc_gradient_list_workspace_bytes.argtypes = [vp, i32, ctypes.POINTER(sz)]
+    L.mtpc_create_gradient_list.argtypes = [vp, i32, vp, sz, vp, ctypes.POINTER(vp)]
+    L.mtpc_clip_gradients.argtypes = [vp, f32, vp, vp]
+    L.mtpc_destroy_gradient_list.argtypes = [vp]
     L.mtpc_status_string.argtypes = [ctypes.c_int]
     L.mtpc_status_string.restype = ctypes.c_char_p
     for name in EXPORTS:
@@ -341,5 +360,231 @@ class MtpcHead:
     def __del__(self):
         try:
             self.mtpc_destroy()
+        except Exception:
+            pass
+
+
+# -- the calls beside the head: tensors in, checked for what the C side cannot see (types, devices, strides within a row)
+def _dtype(t, what: str) -> int:
+    import torch
+    if t.dtype is torch.bfloat16:
+        return MTPC_BF16
+    if t.dtype is torch.float32:
+        return MTPC_F32
+    raise MtpcError(ERR_UNSUPPORTED, f"{what}: {t.dtype}")
+
+
+def _like(what: str, device, shape, *tensors) -> None:
+    """The tensors that are there lie on `device` and have `shape` with adjacent elements in a row."""
+    for t in tensors:
+        if t is None:
+            continue
+        if t.device != device or t.device.type != "cuda":
+            raise MtpcError(ERR_SHAPE, f"{what}: a tensor on {t.device}, another on {device}")
+        if t.shape != shape or (shape[-1] > 1 and t.stride(-1) != 1):
+            raise MtpcError(ERR_SHAPE, f"{what}: {tuple(t.shape)} with strides {t.stride()} where {tuple(shape)} is needed")
+
+
+def _same_dtype(what: str, dtype, *tensors) -> None:
+    for t in tensors:
+        if t is not None and t.dtype is not dtype:
+            raise MtpcError(ERR_UNSUPPORTED, f"{what}: {t.dtype} where {dtype} is needed")
+
+
+def _matrix(what: str, t):
+    if t.dim() != 2:
+        raise MtpcError(ERR_SHAPE, f"{what}: {tuple(t.shape)} where a matrix is needed")
+    return t.shape
+
+
+def _row_stride(t) -> int:
+    return 0 if t is None else t.stride(0)
+
+
+class _On:
+    """The device of a call's tensors as the current one, where it is not (a launch goes to the current device)."""
+
+    def __init__(self, device):
+        import torch
+        self.other = None
+        if device.type == "cuda" and torch.cuda.current_device() != device.index:
+            self.other = torch.cuda.device(device)
+
+    def __enter__(self):
+        if self.other is not None:
+            self.other.__enter__()
+
+    def __exit__(self, *exc):
+        if self.other is not None:
+            self.other.__exit__(*exc)
+
+
+class _In:
+    """The given stream as torch's current one (what torch allocates meanwhile belongs to it); None: it is already."""
+
+    def __init__(self, stream):
+        import torch
+        self.stream = None if stream is None else torch.cuda.stream(stream)
+
+    def __enter__(self):
+        if self.stream is not None:
+            self.stream.__enter__()
+
+    def __exit__(self, *exc):
+        if self.stream is not None:
+            self.stream.__exit__(*exc)
+
+
+def _scratch(what: str, workspace, need: int, device):
+    """The caller's workspace, or one from torch's allocator, which keeps it apart per stream and per captured graph."""
+    import torch
+    if workspace is None:
+        return torch.empty(need, dtype=torch.uint8, device=device)
+    if workspace.device != device or not workspace.is_contiguous() or workspace.dtype is not torch.uint8:
+        raise MtpcError(ERR_SHAPE, f"{what}: workspace of {workspace.dtype} on {workspace.device}")
+    return workspace
+
+
+def mtpc_embed(tokens, table, out, scale: float = 1.0, out_status=None, stream=None) -> None:
+    """out[t] = scale * table[tokens[t]]; a negative token is a row of zeros (include/mtpc.h). tokens [T] int32, table [v, d] and out [T, d]
+    fp32 or bf16; out_status: int32 [1], into which the status bits are or-ed."""
+    import torch
+    what = "mtpc_embed"
+    (v, d), dev, T = _matrix(what, table), table.device, tokens.numel()
+    _like(what, dev, (T,), tokens)
+    _like(what, dev, (v, d), table)
+    _like(what, dev, (T, d), out)
+    _like(what, dev, (1,), out_status)
+    _same_dtype(what, torch.int32, tokens, out_status)
+    with _On(dev):
+        _check(lib().mtpc_embed(tokens.data_ptr(), T, table.data_ptr(), table.stride(0), _dtype(table, what), v, d, scale, out.data_ptr(),
+                                out.stride(0), _dtype(out, what), _ptr(out_status), _stream(stream, dev.index)), what)
+
+
+def mtpc_embed_backward_workspace_bytes(T: int, v: int, d: int) -> int:
+    need = ctypes.c_size_t(0)
+    _check(lib().mtpc_embed_backward_workspace_bytes(T, v, d, ctypes.byref(need)), "mtpc_embed_backward_workspace_bytes")
+    return need.value
+
+
+def mtpc_embed_backward(tokens, d_out, d_table, scale: float = 1.0, accumulate: bool = False, workspace=None, out_status=None,
+                        stream=None) -> None:
+    """d_table[b] = scale * sum of d_out[t] over the positions with token b, or added to it (accumulate). tokens [T] int32, d_out [T, d]
+    fp32 or bf16, d_table [v, d] fp32. workspace None: from torch's allocator, for the call."""
+    import torch
+    what = "mtpc_embed_backward"
+    (v, d), dev, T = _matrix(what, d_table), d_table.device, tokens.numel()
+    _like(what, dev, (T,), tokens)
+    _like(what, dev, (T, d), d_out)
+    _like(what, dev, (v, d), d_table)
+    _like(what, dev, (1,), out_status)
+    _same_dtype(what, torch.int32, tokens, out_status)
+    _same_dtype(what, torch.float32, d_table)
+    with _On(dev), _In(stream):
+        ws = _scratch(what, workspace, mtpc_embed_backward_workspace_bytes(T, v, d), dev)
+        _check(lib().mtpc_embed_backward(tokens.data_ptr(), T, d_out.data_ptr(), d_out.stride(0), _dtype(d_out, what), scale, v, d,
+                                         d_table.data_ptr(), d_table.stride(0), int(bool(accumulate)), ws.data_ptr(), ws.numel(), _ptr(out_status),
+                                         _stream(stream, dev.index)), what)
+
+
+def mtpc_residual_rmsnorm(x, residual, weight, eps: float, out, out_sum=None, out_q=None, out_scale=None, scale_group: int = 0,
+                          stream=None) -> None:
+    """out_sum = x + residual (residual None: x), out = its root-mean-square norm times weight (None: ones); out_q [T, d] e4m3 (or uint8) with
+    out_scale [T, ceil(d / scale_group)] fp32 (scale_group 0: [T, 1]): the same in 8 bits. out or out_q may be None."""
+    import torch
+    what = "mtpc_residual_rmsnorm"
+    (T, d), dev = _matrix(what, x), x.device
+    _like(what, dev, (T, d), x, residual, out, out_sum, out_q)
+    _like(what, dev, (d,), weight)
+    _same_dtype(what, x.dtype, residual, out, out_sum)
+    if out_scale is not None:
+        _like(what, dev, (T, -(-d // scale_group) if scale_group > 0 else 1), out_scale)
+        _same_dtype(what, torch.float32, out_scale)
+        if not out_scale.is_contiguous():
+            raise MtpcError(ERR_SHAPE, f"{what}: out_scale with strides {out_scale.stride()}")
+    if out_q is not None and out_q.dtype not in (torch.float8_e4m3fn, torch.uint8):
+        raise MtpcError(ERR_UNSUPPORTED, f"{what}: {out_q.dtype}")
+    with _On(dev):
+        _check(lib().mtpc_residual_rmsnorm(x.data_ptr(), x.stride(0), _ptr(residual), _row_stride(residual), _ptr(weight),
+                                           MTPC_F32 if weight is None else _dtype(weight, what), T, d, _dtype(x, what), eps, _ptr(out_sum),
+                                           _row_stride(out_sum), _ptr(out), _row_stride(out), _ptr(out_q), _row_stride(out_q), _ptr(out_scale),
+                                           scale_group, _stream(stream, dev.index)), what)
+
+
+def mtpc_residual_rmsnorm_backward_workspace_bytes(T: int, d: int) -> int:
+    need = ctypes.c_size_t(0)
+    _check(lib().mtpc_residual_rmsnorm_backward_workspace_bytes(T, d, ctypes.byref(need)), "mtpc_residual_rmsnorm_backward_workspace_bytes")
+    return need.value
+
+
+def mtpc_residual_rmsnorm_backward(sum, weight, eps: float, d_out, d_sum, d_x, d_weight=None, workspace=None, stream=None) -> None:
+    """d_x: the gradient of the sum (of x and of residual alike) from d_out, the gradient of the norm's output, and d_sum, what reaches the sum along
+    the residual stream (None: nothing; d_x's dtype). d_weight [d] fp32 or None."""
+    import torch
+    what = "mtpc_residual_rmsnorm_backward"
+    (T, d), dev = _matrix(what, sum), sum.device
+    _like(what, dev, (T, d), sum, d_out, d_sum, d_x)
+    _like(what, dev, (d,), weight, d_weight)
+    _same_dtype(what, d_x.dtype, d_sum)
+    _same_dtype(what, torch.float32, d_weight)
+    with _On(dev), _In(stream):
+        ws = None
+        if d_weight is not None:
+            ws = _scratch(what, workspace, mtpc_residual_rmsnorm_backward_workspace_bytes(T, d), dev)
+        _check(lib().mtpc_residual_rmsnorm_backward(sum.data_ptr(), sum.stride(0), _dtype(sum, what), _ptr(weight),
+                                                    MTPC_F32 if weight is None else _dtype(weight, what), T, d, eps, d_out.data_ptr(),
+                                                    d_out.stride(0), _dtype(d_out, what), _ptr(d_sum), _row_stride(d_sum), d_x.data_ptr(),
+                                                    d_x.stride(0), _dtype(d_x, what), _ptr(d_weight), _ptr(ws), 0 if ws is None else ws.numel(),
+                                                    _stream(stream, dev.index)), what)
+
+
+class GradientList:
+    """The gradient buffers of a model, for mtpc_clip_gradients: made once, used every step. Keeps the tensors alive."""
+
+    def __init__(self, grads, outs=None, stream=None):
+        """grads: contiguous fp32 or bf16 tensors of one device; outs: where the scaled gradients go (None: in place; a None in it: nowhere,
+        that gradient counts in the norm alone)."""
+        import torch
+        what = "mtpc_create_gradient_list"
+        self.handle = None
+        grads = list(grads)
+        outs = grads if outs is None else list(outs)
+        if not grads or len(outs) != len(grads):
+            raise MtpcError(ERR_SHAPE, f"{what}: {len(grads)} gradients, {len(outs)} results")
+        self.device = grads[0].device
+        entries = (MtpcGradient * len(grads))()
+        for e, g, o in zip(entries, grads, outs):
+            for t in (g, o):
+                if t is not None and (t.device != self.device or t.device.type != "cuda" or not t.is_contiguous() or t.numel() != g.numel()):
+                    raise MtpcError(ERR_SHAPE, f"{what}: {tuple(t.shape)} with strides {t.stride()} on {t.device}")
+            e.data, e.out, e.count, e.dtype = g.data_ptr(), _ptr(o), g.numel(), _dtype(g, what)
+            e.out_dtype = e.dtype if o is None else _dtype(o, what)
+        need = ctypes.c_size_t(0)
+        _check(lib().mtpc_gradient_list_workspace_bytes(entries, len(grads), ctypes.byref(need)), "mtpc_gradient_list_workspace_bytes")
+        self._keep = (grads, outs)
+        handle = ctypes.c_void_p(0)
+        with _On(self.device), _In(stream):
+            self.workspace = torch.empty(need.value, dtype=torch.uint8, device=self.device)
+            _check(lib().mtpc_create_gradient_list(entries, len(grads), self.workspace.data_ptr(), need.value, _stream(stream, self.device.index),
+                                                   ctypes.byref(handle)), what)
+        self.handle = handle
+
+    def mtpc_clip_gradients(self, max_norm: float, out_norm, stream=None) -> None:
+        """out_norm [1] fp32: the norm of all gradients; where it is above max_norm (and finite) they are scaled by max_norm / norm."""
+        import torch
+        what = "mtpc_clip_gradients"
+        _like(what, self.device, (1,), out_norm)
+        _same_dtype(what, torch.float32, out_norm)
+        with _On(self.device):
+            _check(lib().mtpc_clip_gradients(self.handle, max_norm, out_norm.data_ptr(), _stream(stream, self.device.index)), what)
+
+    def mtpc_destroy_gradient_list(self) -> None:
+        if self.handle:
+            lib().mtpc_destroy_gradient_list(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.mtpc_destroy_gradient_list()
         except Exception:
             pass

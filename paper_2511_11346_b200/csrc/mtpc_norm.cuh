@@ -1,0 +1,323 @@
+// Residual addition and root-mean-square norm of the rows that the head reads as hidden states, and their gradients.
+//   s = x + residual,  rstd = (mean(s^2) + eps)^(-1/2),  out = s rstd weight
+//   d s = rstd (weight d_out - s rstd^2 mean(weight d_out s)) + d_stream,   d weight = sum over the rows of d_out s rstd
+// (d s is the gradient of x and of residual alike.) Everything between the loads and the one rounding of each output is fp32.
+//
+// Both are streams: a row is read once, into registers, and everything is formed from there. A row is a warp's up to 64 vectors of eight
+// elements, beyond that a block's with one vector a thread, so that a single row (one sequence being decoded) is spread over as
+// many warps as it can be.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp8.h>
+#include <stdint.h>
+
+#include "mtpc_ptx.cuh"
+#include "mtpc_rows.cuh"
+
+namespace mtpc {
+
+constexpr int kNormMaxWidth = 32768;     // columns: 1024 threads of 32
+constexpr int kNormMinGroup = 32;        // columns that share a scale: 32, 64 or 128 (or the row)
+constexpr float kE4m3Max = 448.f;
+// Rows whose squares overflow fp32 are formed once more from s times this. What 2^-100 takes below the range is 2^-20 of
+// the row's largest value at most.
+constexpr float kNormRescue = 0x1p-100f;
+
+struct NormArgs {
+  const void *x, *residual, *weight;      // residual, weight: may be NULL
+  void *sum, *out;                        // may be NULL
+  uint8_t* codes;                         // e4m3, may be NULL
+  float* scales;                          // [T, groups]
+  long long x_stride, residual_stride, sum_stride, out_stride, codes_stride;
+  int T, d, group, groups;                // group: columns that share a scale (0: the row)
+  bool weight_f32;
+  float eps;
+};
+
+// Largest magnitude as the bits of an fp32: compared as integers a NaN is larger than everything, so it is not lost.
+__device__ __forceinline__ unsigned magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+
+// What a code of 1 stands for where the largest magnitude is `bits`.
+__device__ __forceinline__ float code_scale(unsigned bits) {
+  const float s = __uint_as_float(bits) / kE4m3Max;
+  return s == 0.f ? 1.f : s;
+}
+
+template <typename IO, int V, int NV, int THREADS>
+__global__ void __launch_bounds__(THREADS) residual_rmsnorm_kernel(const __grid_constant__ NormArgs a) {
+  __shared__ float red[2][1][32];
+  __shared__ unsigned group_max[V == 1 ? kNormMaxWidth / kNormMinGroup : 1];
+  const int row = blockIdx.x * blockDim.y + threadIdx.y;
+  const int tid = threadIdx.x, lane = tid & 31;
+  if (V == 1 && a.codes != nullptr) {            // (rows of single elements are a block's: blockDim.y = 1)
+    for (int g = tid; g < a.groups && a.group != 0; g += blockDim.x) group_max[g] = 0;
+    __syncthreads();
+  }
+  grid_dependency_wait();
+  grid_launch_dependents();
+  if (row >= a.T) return;                                    // a whole warp, or no thread
+  const IO* x = static_cast<const IO*>(a.x) + row * a.x_stride;
+  const IO* residual = static_cast<const IO*>(a.residual) + (a.residual ? row * a.residual_stride : 0);
+  IO* sum = static_cast<IO*>(a.sum) + (a.sum ? row * a.sum_stride : 0);
+
+  float s[NV][V];
+  {
+    Pack<IO, V> px[NV], pr[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int col = (tid + j * blockDim.x) * V;
+      if (col < a.d) {
+        px[j] = load_pack<IO, V>(x + col);
+        if (a.residual) pr[j] = load_pack<IO, V>(residual + col);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int col = (tid + j * blockDim.x) * V;
+#pragma unroll
+      for (int i = 0; i < V; ++i) s[j][i] = 0.f;
+      if (col < a.d) {
+        unpack(px[j], s[j]);
+        if (a.residual) {
+          float r[V];
+          unpack(pr[j], r);
+#pragma unroll
+          for (int i = 0; i < V; ++i) s[j][i] += r[i];
+        }
+        if (a.sum) store_f32<IO, V>(sum + col, s[j]);
+      }
+    }
+  }
+  float square[1] = {0.f};
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) square[0] += s[j][i] * s[j][i];
+  }
+  row_sum(square, red[0]);
+  float rstd = rsqrtf(square[0] / a.d + a.eps);
+  if (__float_as_uint(square[0]) == 0x7f800000u) {           // the same in every thread of the row
+    square[0] = 0.f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        s[j][i] *= kNormRescue;
+        square[0] += s[j][i] * s[j][i];
+      }
+    }
+    row_sum(square, red[1]);
+    rstd = rsqrtf(square[0] / a.d);
+  }
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int col = (tid + j * blockDim.x) * V;
+    if (col < a.d) {
+      float w[V];
+      load_weight<V>(a.weight, a.weight_f32, col, w);
+#pragma unroll
+      for (int i = 0; i < V; ++i) s[j][i] = s[j][i] * rstd * w[i];
+      if (a.out) store_f32<IO, V>(static_cast<IO*>(a.out) + row * a.out_stride + col, s[j]);
+    }
+  }
+  if (a.codes == nullptr) return;
+
+  // The scale of every vector's group, then its codes.
+  unsigned largest[NV];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    largest[j] = 0;
+#pragma unroll
+    for (int i = 0; i < V; ++i) largest[j] = max(largest[j], magnitude(s[j][i]));        // (columns past the row's end are zeros)
+  }
+  uint8_t* codes = a.codes + row * a.codes_stride;
+  float* scales = a.scales + static_cast<long long>(row) * a.groups;
+  if (a.group == 0) {
+    unsigned m = 0;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) m = max(m, largest[j]);
+    m = __reduce_max_sync(0xffffffffu, m);
+    if (blockDim.x > 32) {
+      unsigned* share = reinterpret_cast<unsigned*>(red[1][0]);
+      __syncthreads();                                       // red[1] may still be read (rows whose squares overflowed)
+      if (lane == 0) share[tid >> 5] = m;
+      __syncthreads();
+      m = __reduce_max_sync(0xffffffffu, lane < static_cast<int>(blockDim.x >> 5) ? share[lane] : 0u);
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j) largest[j] = m;
+    if (tid == 0) scales[0] = code_scale(m);
+  } else if (V > 1) {
+    const int lanes = a.group / V;                           // 4 to 16 lanes hold a group
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      for (int o = 1; o < lanes; o <<= 1) largest[j] = max(largest[j], __shfl_xor_sync(0xffffffffu, largest[j], o));
+      const int col = (tid + j * blockDim.x) * V;
+      if (col < a.d && lane % lanes == 0) scales[col / a.group] = code_scale(largest[j]);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const unsigned m = __reduce_max_sync(0xffffffffu, largest[j]);       // 32 columns of one group
+      const int col = tid + j * blockDim.x;
+      if (lane == 0 && col < a.d) atomicMax(&group_max[col / a.group], m);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int col = tid + j * blockDim.x;
+      if (col < a.d) {
+        largest[j] = group_max[col / a.group];
+        if (col % a.group == 0) scales[col / a.group] = code_scale(largest[j]);
+      }
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int col = (tid + j * blockDim.x) * V;
+    if (col >= a.d) continue;
+    const float scale = code_scale(largest[j]);
+    if constexpr (V > 1) {
+      Pack<uint16_t, V / 2> o;
+#pragma unroll
+      for (int i = 0; i < V; i += 2)
+        o.e[i / 2] = __nv_cvt_float2_to_fp8x2(make_float2(s[j][i] / scale, s[j][i + 1] / scale), __NV_SATFINITE, __NV_E4M3);
+      store_pack<uint16_t, V / 2>(reinterpret_cast<uint16_t*>(codes + col), o);
+    } else {
+      codes[col] = __nv_cvt_float_to_fp8(s[j][0] / scale, __NV_SATFINITE, __NV_E4M3);
+    }
+  }
+}
+
+struct NormGradArgs {
+  const void *sum, *weight, *d_out, *d_stream;      // weight, d_stream: may be NULL
+  void* d_x;
+  float* partial;                                   // [gridDim.x, d]: the blocks' parts of d weight (NULL: not wanted)
+  long long sum_stride, d_out_stride, d_stream_stride, d_x_stride;
+  int T, d;
+  bool weight_f32;
+  float eps;
+};
+
+// Every block has every gridDim.x-th row and keeps its part of d weight in registers.
+template <typename IO, typename DY, typename DX, int V, int NV>
+__global__ void __launch_bounds__(1024) rmsnorm_grad_kernel(const __grid_constant__ NormGradArgs a) {
+  __shared__ float red[3][2][32];
+  const int tid = threadIdx.x;
+  grid_dependency_wait();
+  float w[NV][V], dw[NV][V];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int col = (tid + j * blockDim.x) * V;
+#pragma unroll
+    for (int i = 0; i < V; ++i) w[j][i] = dw[j][i] = 0.f;
+    if (col < a.d) load_weight<V>(a.weight, a.weight_f32, col, w[j]);
+  }
+  int turn = 0;
+  for (int row = blockIdx.x; row < a.T; row += gridDim.x, turn ^= 1) {
+    const IO* s_row = static_cast<const IO*>(a.sum) + row * a.sum_stride;
+    const DY* dy_row = static_cast<const DY*>(a.d_out) + row * a.d_out_stride;
+    float s[NV][V], dy[NV][V];
+    Pack<DX, V> stream[NV];
+    {
+      Pack<IO, V> ps[NV];
+      Pack<DY, V> pd[NV];
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const int col = (tid + j * blockDim.x) * V;
+        if (col < a.d) {
+          ps[j] = load_pack<IO, V>(s_row + col);
+          pd[j] = load_pack<DY, V>(dy_row + col);
+          if (a.d_stream) stream[j] = load_pack<DX, V>(static_cast<const DX*>(a.d_stream) + row * a.d_stream_stride + col);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const int col = (tid + j * blockDim.x) * V;
+#pragma unroll
+        for (int i = 0; i < V; ++i) s[j][i] = dy[j][i] = 0.f;
+        if (col < a.d) {
+          unpack(ps[j], s[j]);
+          unpack(pd[j], dy[j]);
+        }
+      }
+    }
+    float sums[2] = {0.f, 0.f};                              // of s^2 and of weight d_out s
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        sums[0] += s[j][i] * s[j][i];
+        sums[1] += dy[j][i] * w[j][i] * s[j][i];
+      }
+    }
+    row_sum(sums, red[turn]);
+    float rstd = rsqrtf(sums[0] / a.d + a.eps), step = rstd;          // step: by which d out becomes d s
+    if (__float_as_uint(sums[0]) == 0x7f800000u) {
+      sums[0] = sums[1] = 0.f;
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          s[j][i] *= kNormRescue;
+          sums[0] += s[j][i] * s[j][i];
+          sums[1] += dy[j][i] * w[j][i] * s[j][i];
+        }
+      }
+      __syncthreads();                                       // red[2] may still be read for an earlier row
+      row_sum(sums, red[2]);
+      rstd = rsqrtf(sums[0] / a.d);
+      step = rstd * kNormRescue;
+    }
+    const float mean = sums[1] * rstd / a.d;                 // of weight d_out s rstd
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int col = (tid + j * blockDim.x) * V;
+      if (col >= a.d) continue;
+      float dx[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const float unit = s[j][i] * rstd;
+        dw[j][i] += dy[j][i] * unit;
+        dx[i] = step * (dy[j][i] * w[j][i] - unit * mean);
+      }
+      if (a.d_stream) {
+        float more[V];
+        unpack(stream[j], more);
+#pragma unroll
+        for (int i = 0; i < V; ++i) dx[i] += more[i];
+      }
+      store_f32<DX, V>(static_cast<DX*>(a.d_x) + row * a.d_x_stride + col, dx);
+    }
+  }
+  if (a.partial) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int col = (tid + j * blockDim.x) * V;
+      if (col < a.d) store_f32<float, V>(a.partial + static_cast<size_t>(blockIdx.x) * a.d + col, dw[j]);
+    }
+  }
+  grid_launch_dependents();
+}
+
+// d weight from the blocks' parts: 32 columns a block, warp y adds up parts y, y + 32, ..., then the warps' sums in their order.
+__global__ void __launch_bounds__(1024) norm_weight_grad_kernel(const float* partial, int parts, int d, float* d_weight) {
+  __shared__ float share[32][33];
+  const int col = blockIdx.x * 32 + threadIdx.x;
+  grid_dependency_wait();
+  float sum = 0.f;
+  if (col < d) {
+#pragma unroll 8
+    for (int p = threadIdx.y; p < parts; p += 32) sum += partial[static_cast<size_t>(p) * d + col];
+  }
+  share[threadIdx.y][threadIdx.x] = sum;
+  __syncthreads();
+  sum = share[threadIdx.x][threadIdx.y];                     // warp y: the 32 parts of column y
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  const int mine = blockIdx.x * 32 + threadIdx.y;
+  if (threadIdx.x == 0 && mine < d) d_weight[mine] = sum;
+  grid_launch_dependents();
+}
+
+}  // namespace mtpc

@@ -1,0 +1,94 @@
+// Adjacent elements of fp32 or bf16 rows, as the streaming kernels around the head read and write them.
+#pragma once
+#include <cuda_bf16.h>
+#include <stdint.h>
+
+#include "mtpc_ptx.cuh"
+
+namespace mtpc {
+
+// V adjacent elements, at most 32 bytes, moved as one access (the address is a multiple of their size).
+template <typename T, int V>
+struct alignas(sizeof(T) * V) Pack {
+  T e[V];
+};
+template <typename T, int V>
+__device__ __forceinline__ Pack<T, V> load_pack(const T* p) {
+  static_assert(sizeof(T) * V <= 32, "a load moves 32 bytes at most");
+  if constexpr (sizeof(T) * V == 32) {
+    Pack<T, V> x;
+    uint32_t* r = reinterpret_cast<uint32_t*>(x.e);
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "l"(p));
+    return x;
+  } else {
+    return *reinterpret_cast<const Pack<T, V>*>(p);
+  }
+}
+template <typename T, int V>
+__device__ __forceinline__ void store_pack(T* p, const Pack<T, V>& x) {
+  if constexpr (sizeof(T) * V == 32) st_global_v8_b32(p, reinterpret_cast<const uint32_t*>(x.e));
+  else *reinterpret_cast<Pack<T, V>*>(p) = x;
+}
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
+template <typename T>
+__device__ __forceinline__ T from_f32(float x);
+template <>
+__device__ __forceinline__ float from_f32<float>(float x) { return x; }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+
+template <typename T, int V>
+__device__ __forceinline__ void unpack(const Pack<T, V>& p, float (&x)[V]) {
+#pragma unroll
+  for (int i = 0; i < V; ++i) x[i] = to_f32(p.e[i]);
+}
+template <typename T, int V>
+__device__ __forceinline__ void store_f32(T* p, const float (&x)[V]) {
+  Pack<T, V> o;
+#pragma unroll
+  for (int i = 0; i < V; ++i) o.e[i] = from_f32<T>(x[i]);
+  store_pack<T, V>(p, o);
+}
+
+// Sums over the threads of a row: a warp, or (blockDim.x > 32) the whole block, every thread with the same result, added up in
+// the same order. red: 32 floats per value in shared memory; a buffer may be used again after the next barrier.
+template <int N>
+__device__ __forceinline__ void row_sum(float (&x)[N], float (*red)[32]) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] += __shfl_xor_sync(0xffffffffu, x[i], o);
+  }
+  if (blockDim.x == 32) return;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+  if (lane == 0) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) red[i][warp] = x[i];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = lane < warps ? red[i][lane] : 0.f;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] += __shfl_xor_sync(0xffffffffu, x[i], o);
+  }
+}
+
+// V adjacent weights (fp32 or bf16; none: ones).
+template <int V>
+__device__ __forceinline__ void load_weight(const void* weight, bool f32, int col, float (&w)[V]) {
+  if (weight == nullptr) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) w[i] = 1.f;
+  } else if (f32) {
+    unpack(load_pack<float, V>(static_cast<const float*>(weight) + col), w);
+  } else {
+    unpack(load_pack<__nv_bfloat16, V>(static_cast<const __nv_bfloat16*>(weight) + col), w);
+  }
+}
+
+}  // namespace mtpc

@@ -1,0 +1,532 @@
+// Host side of the calls of a training or decoding step that need no head (include/mtpc.h): embeddings, the residual norm, the gradients'
+// norm. Argument checks, carving of the caller's workspace, choice of the build, launches.
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+#include <string.h>
+
+#include <algorithm>
+#include <new>
+
+#include "../../include/mtpc.h"
+#include "mtpc_clip.cuh"
+#include "mtpc_embed.cuh"
+#include "mtpc_launch.cuh"
+#include "mtpc_norm.cuh"
+
+namespace {
+
+using namespace mtpc;
+
+constexpr size_t kAlign = 256;
+constexpr int kMaxRows = 1 << 30;
+constexpr int kSms = 148;               // what grids are sized for: the results of sums that are cut by them do not depend on the device
+size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
+bool aligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+size_t element(int dtype) { return dtype == MTPC_F32 ? 4 : 2; }
+bool known(int dtype) { return dtype == MTPC_F32 || dtype == MTPC_BF16; }
+
+// The current device is one that the library is built for.
+int check_device() {
+  int dev = 0, major = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess || major != 10) {
+    cudaGetLastError();
+    return MTPC_ERR_CUDA;
+  }
+  return MTPC_OK;
+}
+
+// Rows of a matrix of the caller: every row starts where vectors of `vec` elements may. An absent matrix allows anything.
+bool rows_allow(const void* p, int64_t stride, size_t element_bytes, int vec, int rows) {
+  return p == nullptr || (aligned(p, element_bytes * vec) && (rows <= 1 || stride % vec == 0));
+}
+// Rows that are read may lie anywhere, also all in one place (stride 0); rows that are written must not overlap.
+bool input_rows(const void* p, int64_t stride, int rows) { return p == nullptr || rows <= 1 || stride >= 0; }
+bool output_rows(const void* p, int64_t stride, int rows, int d) { return p == nullptr || rows <= 1 || stride >= d; }
+
+int ceil_div(long long a, long long b) { return static_cast<int>((a + b - 1) / b); }
+int round_warp(int x) { return (x + 31) / 32 * 32; }
+
+// ---------------------------------------------------------------- residual norm
+template <typename IO>
+void launch_rmsnorm(const NormArgs& a, bool vectors, cudaStream_t st) {
+  const int packs = ceil_div(a.d, 8);
+  if (vectors && packs <= 32)
+    launch_kernel(residual_rmsnorm_kernel<IO, 8, 1, 256>, ceil_div(a.T, 8), dim3(32, 8), 0, st, true, a);
+  else if (vectors && packs <= 64)
+    launch_kernel(residual_rmsnorm_kernel<IO, 8, 2, 256>, ceil_div(a.T, 8), dim3(32, 8), 0, st, true, a);
+  else if (vectors && packs <= 1024)
+    launch_kernel(residual_rmsnorm_kernel<IO, 8, 1, 1024>, a.T, round_warp(packs), 0, st, true, a);
+  else if (vectors)
+    launch_kernel(residual_rmsnorm_kernel<IO, 8, 4, 1024>, a.T, round_warp(ceil_div(packs, 4)), 0, st, true, a);
+  else if (a.d <= 4096)
+    launch_kernel(residual_rmsnorm_kernel<IO, 1, 4, 1024>, a.T, round_warp(ceil_div(a.d, 4)), 0, st, true, a);
+  else
+    launch_kernel(residual_rmsnorm_kernel<IO, 1, 32, 1024>, a.T, round_warp(ceil_div(a.d, 32)), 0, st, true, a);
+}
+
+// Blocks of the gradient kernel: as many as give an SM 1024 threads, by what the vector build takes (the sums' order then does not depend on alignment).
+int norm_grad_blocks(int T, int d) {
+  const int threads = d <= 8192 ? round_warp(ceil_div(d, 8)) : 1024;
+  const int per_sm = std::max(1, std::min(16, 1024 / threads));
+  return std::min(T, kSms * per_sm);
+}
+template <typename IO, typename DY, typename DX>
+void launch_rmsnorm_grad(const NormGradArgs& a, int blocks, bool vectors, cudaStream_t st) {
+  const int packs = ceil_div(a.d, 8);
+  if (vectors && packs <= 1024)
+    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 8, 1>, blocks, round_warp(packs), 0, st, true, a);
+  else if (vectors)
+    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 8, 4>, blocks, round_warp(ceil_div(packs, 4)), 0, st, true, a);
+  else if (a.d <= 4096)
+    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 1, 4>, blocks, round_warp(ceil_div(a.d, 4)), 0, st, true, a);
+  else
+    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 1, 32>, blocks, round_warp(ceil_div(a.d, 32)), 0, st, true, a);
+}
+template <typename IO, typename DY>
+void launch_rmsnorm_grad(const NormGradArgs& a, int dx_dtype, int blocks, bool vectors, cudaStream_t st) {
+  if (dx_dtype == MTPC_F32) launch_rmsnorm_grad<IO, DY, float>(a, blocks, vectors, st);
+  else launch_rmsnorm_grad<IO, DY, __nv_bfloat16>(a, blocks, vectors, st);
+}
+
+// ---------------------------------------------------------------- embedding
+struct EmbedPlan {
+  int digits, tiles;                    // of the sort
+  int threads, slabs, chunk, chunks;    // of the sums
+  size_t off_key[2], off_pos[2], off_hist, off_part, total;
+};
+void plan_embed(int T, int v, int d, EmbedPlan* p) {
+  int bits = 1;
+  while ((static_cast<int64_t>(1) << bits) <= v) ++bits;                // keys run up to v
+  p->digits = (bits + kSortDigit - 1) / kSortDigit;
+  p->tiles = ceil_div(T, kSortTile);
+  // A thread has four columns; the chunks are as many as keep the device busy, of 16 positions at least.
+  p->threads = std::min(kSegmentThreads, round_warp(ceil_div(d, 4)));
+  p->slabs = ceil_div(d, 4 * p->threads);
+  p->chunk = std::max(16, ceil_div(static_cast<long long>(T) * p->slabs, kSms * 8));
+  p->chunks = ceil_div(T, p->chunk);
+  size_t off = 0;
+  auto take = [&](size_t bytes) { size_t o = off; off += align_up(bytes); return o; };
+  for (int i = 0; i < 2; ++i) {
+    p->off_key[i] = take(i < p->digits ? static_cast<size_t>(T) * 4 : 0);
+    p->off_pos[i] = take(i < p->digits ? static_cast<size_t>(T) * 4 : 0);
+  }
+  p->off_hist = take(p->tiles > 1 ? static_cast<size_t>(p->tiles) * kSortBins * 4 : 0);
+  p->off_part = take(static_cast<size_t>(p->chunks) * 2 * d * 4);
+  p->total = off;
+}
+
+int check_embed_sizes(int T, int v, int d) {
+  if (T < 0 || v < 1 || d < 1) return MTPC_ERR_SHAPE;
+  if (T > kEmbedMaxT || v > kEmbedMaxV || d > kEmbedMaxD) return MTPC_ERR_UNSUPPORTED;
+  return MTPC_OK;
+}
+
+template <typename TI, typename TO, int V>
+void launch_embed(const EmbedArgs& a, cudaStream_t st) {
+  int share = 32;                       // threads to a row
+  while (share < 256 && share * V < a.d) share <<= 1;
+  const int rows = 256 / share;
+  if (a.T >= 4 * kSms * 8) {
+    launch_kernel(embed_kernel<TI, TO, V, 4>, ceil_div(a.T, rows * 4), dim3(share, rows), 0, st, true, a);
+  } else {                              // few rows: their columns over several blocks
+    launch_kernel(embed_kernel<TI, TO, V, 1>, dim3(ceil_div(a.T, rows), ceil_div(a.d, share * V)), dim3(share, rows), 0, st, true, a);
+  }
+}
+template <typename TI, typename TO>
+void launch_embed(const EmbedArgs& a, bool vectors, cudaStream_t st) {
+  if (vectors) launch_embed<TI, TO, 8>(a, st);
+  else launch_embed<TI, TO, 1>(a, st);
+}
+
+}  // namespace
+
+struct mtpc_gradient_list {
+  const ClipChunk* chunks;              // in the workspace
+  double* partial;
+  int count, blocks;
+};
+
+namespace {
+
+// What a list of gradients needs: its chunks, and the sums of the first pass's blocks.
+struct ListPlan {
+  long long chunks;
+  int blocks;
+  size_t off_partial, total;
+};
+bool same_place(const mtpc_gradient& e) { return e.out == e.data; }
+// Elements of an entry before the first that vectors of eight may start at, for both of its addresses; -1: there is none for both.
+int wide_head(const mtpc_gradient& e) {
+  const int at = static_cast<int>(reinterpret_cast<uintptr_t>(e.data) / element(e.dtype) % 8);
+  if (e.out && static_cast<int>(reinterpret_cast<uintptr_t>(e.out) / element(e.out_dtype) % 8) != at) return -1;
+  return (8 - at) % 8;
+}
+int plan_list(const mtpc_gradient* entries, int32_t count, ListPlan* p) {
+  if (count < 0) return MTPC_ERR_SHAPE;
+  if (count > 0 && !entries) return MTPC_ERR_NULL;
+  p->chunks = 0;
+  for (int i = 0; i < count; ++i) {
+    const mtpc_gradient& e = entries[i];
+    if (e.count < 0 || e.count > (static_cast<int64_t>(1) << 40) || !known(e.dtype) || (e.out && !known(e.out_dtype))) return MTPC_ERR_SHAPE;
+    if (e.count == 0) continue;
+    if (!e.data) return MTPC_ERR_NULL;
+    if (!aligned(e.data, element(e.dtype)) || (e.out && !aligned(e.out, element(e.out_dtype)))) return MTPC_ERR_SHAPE;
+    if (e.out && same_place(e) && e.dtype != e.out_dtype) return MTPC_ERR_SHAPE;
+    p->chunks += (e.count + kClipChunk - 1) / kClipChunk;
+    if (p->chunks > (1 << 30)) return MTPC_ERR_UNSUPPORTED;
+  }
+  p->blocks = static_cast<int>(std::max<long long>(1, std::min<long long>(p->chunks, kClipMaxBlocks)));
+  p->off_partial = align_up(static_cast<size_t>(p->chunks) * sizeof(ClipChunk));
+  p->total = p->off_partial + align_up(static_cast<size_t>(p->blocks) * sizeof(double));
+  return MTPC_OK;
+}
+
+// No result may lie where another result or another entry's gradient does: the passes read and write them in no order.
+struct Span {
+  uintptr_t begin, end;
+  bool written;
+};
+int check_overlap(const mtpc_gradient* entries, int32_t count) {
+  Span* spans = new (std::nothrow) Span[2 * static_cast<size_t>(count) + 1];
+  if (!spans) return MTPC_ERR_CUDA;
+  size_t n = 0;
+  for (int i = 0; i < count; ++i) {
+    const mtpc_gradient& e = entries[i];
+    if (e.count == 0) continue;
+    const uintptr_t in = reinterpret_cast<uintptr_t>(e.data), to = reinterpret_cast<uintptr_t>(e.out);
+    if (!e.out || !same_place(e)) spans[n++] = {in, in + static_cast<size_t>(e.count) * element(e.dtype), false};
+    if (e.out) spans[n++] = {to, to + static_cast<size_t>(e.count) * element(e.out_dtype), true};
+  }
+  std::sort(spans, spans + n, [](const Span& x, const Span& y) { return x.begin < y.begin; });
+  uintptr_t any = 0, written = 0;       // where what lies before ends
+  int rc = MTPC_OK;
+  for (size_t i = 0; i < n; ++i) {
+    if (spans[i].begin < (spans[i].written ? any : written)) rc = MTPC_ERR_SHAPE;
+    any = std::max(any, spans[i].end);
+    if (spans[i].written) written = std::max(written, spans[i].end);
+  }
+  delete[] spans;
+  return rc;
+}
+
+}  // namespace
+
+extern "C" {
+
+int mtpc_embed(const int32_t* tokens, int32_t T, const void* table, int64_t table_stride, int32_t table_dtype, int32_t v, int32_t d,
+               float scale, void* out, int64_t out_stride, int32_t out_dtype, uint32_t* out_status, void* stream) {
+  int rc = check_embed_sizes(T, v, d);
+  if (rc != MTPC_OK) return rc;
+  if (!known(table_dtype) || !known(out_dtype)) return MTPC_ERR_SHAPE;
+  if (T == 0) return MTPC_OK;
+  if (!tokens || !table || !out) return MTPC_ERR_NULL;
+  if (!input_rows(table, table_stride, v) || !output_rows(out, out_stride, T, d)) return MTPC_ERR_SHAPE;
+  if (!aligned(tokens, 4) || !aligned(table, element(table_dtype)) || !aligned(out, element(out_dtype)) || !aligned(out_status, 4)) return MTPC_ERR_SHAPE;
+  if ((rc = check_device()) != MTPC_OK) return rc;
+  EmbedArgs a;
+  memset(&a, 0, sizeof(a));
+  a.tokens = tokens;
+  a.table = table;
+  a.out = out;
+  a.status = out_status;
+  a.table_stride = table_stride;
+  a.out_stride = out_stride;
+  a.T = T;
+  a.v = v;
+  a.d = d;
+  a.scale = scale;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const bool vectors = d % 8 == 0 && rows_allow(table, table_stride, element(table_dtype), 8, v) && rows_allow(out, out_stride, element(out_dtype), 8, T);
+  if (table_dtype == MTPC_F32) {
+    if (out_dtype == MTPC_F32) launch_embed<float, float>(a, vectors, st);
+    else launch_embed<float, __nv_bfloat16>(a, vectors, st);
+  } else {
+    if (out_dtype == MTPC_F32) launch_embed<__nv_bfloat16, float>(a, vectors, st);
+    else launch_embed<__nv_bfloat16, __nv_bfloat16>(a, vectors, st);
+  }
+  return check_launch();
+}
+
+int mtpc_embed_backward_workspace_bytes(int32_t T, int32_t v, int32_t d, size_t* out_bytes) {
+  if (!out_bytes) return MTPC_ERR_NULL;
+  const int rc = check_embed_sizes(T, v, d);
+  if (rc != MTPC_OK) return rc;
+  EmbedPlan p;
+  plan_embed(T > 0 ? T : 1, v, d, &p);
+  *out_bytes = p.total;
+  return MTPC_OK;
+}
+
+int mtpc_embed_backward(const int32_t* tokens, int32_t T, const void* d_out, int64_t d_out_stride, int32_t d_out_dtype, float scale,
+                        int32_t v, int32_t d, float* d_table, int64_t d_table_stride, int32_t accumulate, void* workspace,
+                        size_t workspace_bytes, uint32_t* out_status, void* stream) {
+  int rc = check_embed_sizes(T, v, d);
+  if (rc != MTPC_OK) return rc;
+  if (!known(d_out_dtype)) return MTPC_ERR_SHAPE;
+  if (!d_table || (T > 0 && (!tokens || !d_out || !workspace))) return MTPC_ERR_NULL;
+  if (!input_rows(d_out, d_out_stride, T) || !output_rows(d_table, d_table_stride, v, d)) return MTPC_ERR_SHAPE;
+  if (!aligned(tokens, 4) || !aligned(d_out, element(d_out_dtype)) || !aligned(d_table, 4) || !aligned(out_status, 4)) return MTPC_ERR_SHAPE;
+  EmbedPlan p;
+  plan_embed(T > 0 ? T : 1, v, d, &p);
+  if (T > 0 && (workspace_bytes < p.total || !aligned(workspace, kAlign))) return MTPC_ERR_WORKSPACE;
+  if (T == 0 && accumulate) return MTPC_OK;
+  if ((rc = check_device()) != MTPC_OK) return rc;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+
+  EmbedSortArgs s;
+  memset(&s, 0, sizeof(s));
+  s.tokens = tokens;
+  s.status = out_status;
+  s.d_table = accumulate ? nullptr : d_table;
+  s.d_out = d_out;
+  s.d_table_stride = d_table_stride;
+  s.d_out_stride = d_out_stride;
+  s.T = T;
+  s.v = v;
+  s.d = d;
+  s.digits = p.digits;
+  s.tiles = T > 0 ? p.tiles : 0;
+  s.d_out_bytes = static_cast<int>(element(d_out_dtype));
+  const auto allow = [](auto* kernel) {
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSortSmem)) == cudaSuccess;
+  };
+  if (!allow(embed_sort_kernel) || !allow(embed_count_kernel) || !allow(embed_scatter_kernel)) return MTPC_ERR_CUDA;
+  if (T == 0) {                         // (not accumulated: the gradient is zeros)
+    launch_kernel(embed_count_kernel, kSms, kSortThreads, kSortSmem, st, true, s, 0);
+    return check_launch();
+  }
+  s.key_a = reinterpret_cast<int*>(ws + p.off_key[0]);
+  s.pos_a = reinterpret_cast<int*>(ws + p.off_pos[0]);
+  s.key_b = reinterpret_cast<int*>(ws + p.off_key[1]);
+  s.pos_b = reinterpret_cast<int*>(ws + p.off_pos[1]);
+  s.hist = reinterpret_cast<int*>(ws + p.off_hist);
+  if (p.tiles == 1) {
+    launch_kernel(embed_sort_kernel, kSms, kSortThreads, kSortSmem, st, true, s);
+  } else {
+    for (int digit = 0; digit < p.digits; ++digit) {
+      // the first pass over the tokens also clears and prefetches
+      launch_kernel(embed_count_kernel, p.tiles + (digit == 0 ? kSms : 0), kSortThreads, kSortSmem, st, true, s, digit);
+      launch_kernel(embed_scan_kernel, 1, kSortThreads, 0, st, true, s.hist, p.tiles * kSortBins);
+      launch_kernel(embed_scatter_kernel, p.tiles, kSortThreads, kSortSmem, st, true, s, digit);
+    }
+  }
+  EmbedSegmentArgs a;
+  memset(&a, 0, sizeof(a));
+  a.key = s.key_a;
+  a.pos = s.pos_a;
+  a.d_out = d_out;
+  a.d_table = d_table;
+  a.part = reinterpret_cast<float*>(ws + p.off_part);
+  a.d_out_stride = d_out_stride;
+  a.d_table_stride = d_table_stride;
+  a.T = T;
+  a.v = v;
+  a.d = d;
+  a.chunk = p.chunk;
+  a.chunks = p.chunks;
+  a.scale = scale;
+  a.accumulate = accumulate != 0;
+  const bool vectors = d % 4 == 0 && rows_allow(d_out, d_out_stride, element(d_out_dtype), 4, T) && rows_allow(d_table, d_table_stride, 4, 4, v);
+  const int vec = vectors ? 4 : 1;
+  const dim3 grid(ceil_div(d, p.threads * vec), p.chunks);
+  if (d_out_dtype == MTPC_F32)
+    launch_kernel(vectors ? embed_segment_kernel<float, 4, 8> : embed_segment_kernel<float, 1, 8>, grid, p.threads, 0, st, true, a);
+  else
+    launch_kernel(vectors ? embed_segment_kernel<__nv_bfloat16, 4, 8> : embed_segment_kernel<__nv_bfloat16, 1, 8>, grid, p.threads, 0, st, true, a);
+  if (p.chunks > 1)
+    launch_kernel(vectors ? embed_join_kernel<4> : embed_join_kernel<1>, dim3(ceil_div(d, 32 * vec), p.chunks), 256, 0, st, true, a);
+  return check_launch();
+}
+
+int mtpc_residual_rmsnorm(const void* x, int64_t x_stride, const void* residual, int64_t residual_stride, const void* weight,
+                          int32_t weight_dtype, int32_t T, int32_t d, int32_t io_dtype, float eps, void* out_sum, int64_t sum_stride,
+                          void* out, int64_t out_stride, uint8_t* out_codes, int64_t codes_stride, float* out_scales,
+                          int32_t scale_group, void* stream) {
+  if (T < 0 || T > kMaxRows || d < 1 || !known(io_dtype) || !known(weight_dtype) || !(eps > 0.f) || isinf(eps)) return MTPC_ERR_SHAPE;
+  if (d > kNormMaxWidth) return MTPC_ERR_UNSUPPORTED;
+  if (scale_group != 0 && scale_group != 32 && scale_group != 64 && scale_group != 128) return MTPC_ERR_UNSUPPORTED;
+  if (T == 0) return MTPC_OK;
+  if (!x || (!out && !out_codes) || (out_codes != nullptr) != (out_scales != nullptr)) return MTPC_ERR_NULL;
+  if (!input_rows(x, x_stride, T) || !input_rows(residual, residual_stride, T) || !output_rows(out_sum, sum_stride, T, d) ||
+      !output_rows(out, out_stride, T, d) || !output_rows(out_codes, codes_stride, T, d))
+    return MTPC_ERR_SHAPE;
+  const size_t e = element(io_dtype);
+  if (!aligned(x, e) || !aligned(residual, e) || !aligned(weight, element(weight_dtype)) || !aligned(out_sum, e) || !aligned(out, e) ||
+      !aligned(out_scales, 4))
+    return MTPC_ERR_SHAPE;
+  int rc = check_device();
+  if (rc != MTPC_OK) return rc;
+  NormArgs a;
+  memset(&a, 0, sizeof(a));
+  a.x = x;
+  a.residual = residual;
+  a.weight = weight;
+  a.sum = out_sum;
+  a.out = out;
+  a.codes = out_codes;
+  a.scales = out_scales;
+  a.x_stride = x_stride;
+  a.residual_stride = residual_stride;
+  a.sum_stride = sum_stride;
+  a.out_stride = out_stride;
+  a.codes_stride = codes_stride;
+  a.T = T;
+  a.d = d;
+  a.group = scale_group;
+  a.groups = scale_group ? ceil_div(d, scale_group) : 1;
+  a.weight_f32 = weight_dtype == MTPC_F32;
+  a.eps = eps;
+  const bool vectors = d % 8 == 0 && rows_allow(x, x_stride, e, 8, T) && rows_allow(residual, residual_stride, e, 8, T) &&
+                       rows_allow(weight, 0, element(weight_dtype), 8, 1) && rows_allow(out_sum, sum_stride, e, 8, T) &&
+                       rows_allow(out, out_stride, e, 8, T) && rows_allow(out_codes, codes_stride, 1, 8, T);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (io_dtype == MTPC_F32) launch_rmsnorm<float>(a, vectors, st);
+  else launch_rmsnorm<__nv_bfloat16>(a, vectors, st);
+  return check_launch();
+}
+
+int mtpc_residual_rmsnorm_backward_workspace_bytes(int32_t T, int32_t d, size_t* out_bytes) {
+  if (!out_bytes) return MTPC_ERR_NULL;
+  if (T < 0 || T > kMaxRows || d < 1) return MTPC_ERR_SHAPE;
+  if (d > kNormMaxWidth) return MTPC_ERR_UNSUPPORTED;
+  *out_bytes = align_up(static_cast<size_t>(norm_grad_blocks(T > 0 ? T : 1, d)) * d * 4);
+  return MTPC_OK;
+}
+
+int mtpc_residual_rmsnorm_backward(const void* sum, int64_t sum_stride, int32_t io_dtype, const void* weight, int32_t weight_dtype,
+                                   int32_t T, int32_t d, float eps, const void* d_out, int64_t d_out_stride, int32_t d_out_dtype,
+                                   const void* d_sum, int64_t d_sum_stride, void* d_x, int64_t d_x_stride, int32_t d_x_dtype,
+                                   float* d_weight, void* workspace, size_t workspace_bytes, void* stream) {
+  if (T < 0 || T > kMaxRows || d < 1 || !known(io_dtype) || !known(weight_dtype) || !known(d_out_dtype) || !known(d_x_dtype) ||
+      !(eps > 0.f) || isinf(eps))
+    return MTPC_ERR_SHAPE;
+  if (d > kNormMaxWidth) return MTPC_ERR_UNSUPPORTED;
+  if (T > 0 && (!sum || !d_out || !d_x || (d_weight && !workspace))) return MTPC_ERR_NULL;
+  if (!input_rows(sum, sum_stride, T) || !input_rows(d_out, d_out_stride, T) || !input_rows(d_sum, d_sum_stride, T) ||
+      !output_rows(d_x, d_x_stride, T, d))
+    return MTPC_ERR_SHAPE;
+  if (!aligned(sum, element(io_dtype)) || !aligned(weight, element(weight_dtype)) || !aligned(d_out, element(d_out_dtype)) ||
+      !aligned(d_sum, element(d_x_dtype)) || !aligned(d_x, element(d_x_dtype)) || !aligned(d_weight, 4))
+    return MTPC_ERR_SHAPE;
+  const int blocks = norm_grad_blocks(T, d);
+  if (d_weight && T > 0 && (workspace_bytes < align_up(static_cast<size_t>(blocks) * d * 4) || !aligned(workspace, kAlign))) return MTPC_ERR_WORKSPACE;
+  if (T == 0 && !d_weight) return MTPC_OK;
+  int rc = check_device();
+  if (rc != MTPC_OK) return rc;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  NormGradArgs a;
+  memset(&a, 0, sizeof(a));
+  if (T > 0) {
+    a.sum = sum;
+    a.weight = weight;
+    a.d_out = d_out;
+    a.d_stream = d_sum;
+    a.d_x = d_x;
+    a.partial = d_weight ? static_cast<float*>(workspace) : nullptr;
+    a.sum_stride = sum_stride;
+    a.d_out_stride = d_out_stride;
+    a.d_stream_stride = d_sum_stride;
+    a.d_x_stride = d_x_stride;
+    a.T = T;
+    a.d = d;
+    a.weight_f32 = weight_dtype == MTPC_F32;
+    a.eps = eps;
+    const bool vectors = d % 8 == 0 && rows_allow(sum, sum_stride, element(io_dtype), 8, T) && rows_allow(weight, 0, element(weight_dtype), 8, 1) &&
+                         rows_allow(d_out, d_out_stride, element(d_out_dtype), 8, T) &&
+                         rows_allow(d_sum, d_sum_stride, element(d_x_dtype), 8, T) && rows_allow(d_x, d_x_stride, element(d_x_dtype), 8, T);
+    if (io_dtype == MTPC_F32) {
+      if (d_out_dtype == MTPC_F32) launch_rmsnorm_grad<float, float>(a, d_x_dtype, blocks, vectors, st);
+      else launch_rmsnorm_grad<float, __nv_bfloat16>(a, d_x_dtype, blocks, vectors, st);
+    } else {
+      if (d_out_dtype == MTPC_F32) launch_rmsnorm_grad<__nv_bfloat16, float>(a, d_x_dtype, blocks, vectors, st);
+      else launch_rmsnorm_grad<__nv_bfloat16, __nv_bfloat16>(a, d_x_dtype, blocks, vectors, st);
+    }
+  }
+  if (d_weight)
+    launch_kernel(norm_weight_grad_kernel, ceil_div(d, 32), dim3(32, 32), 0, st, true, static_cast<const float*>(a.partial), T > 0 ? blocks : 0, d,
+                  d_weight);
+  return check_launch();
+}
+
+int mtpc_gradient_list_workspace_bytes(const mtpc_gradient* entries, int32_t count, size_t* out_bytes) {
+  if (!out_bytes) return MTPC_ERR_NULL;
+  ListPlan p;
+  const int rc = plan_list(entries, count, &p);
+  if (rc != MTPC_OK) return rc;
+  *out_bytes = p.total;
+  return MTPC_OK;
+}
+
+int mtpc_create_gradient_list(const mtpc_gradient* entries, int32_t count, void* workspace, size_t workspace_bytes, void* stream,
+                              mtpc_gradient_list** out) {
+  if (!out) return MTPC_ERR_NULL;
+  *out = nullptr;
+  ListPlan p;
+  int rc = plan_list(entries, count, &p);
+  if (rc != MTPC_OK) return rc;
+  if (!workspace) return MTPC_ERR_NULL;
+  if (workspace_bytes < p.total || !aligned(workspace, kAlign)) return MTPC_ERR_WORKSPACE;
+  if ((rc = check_overlap(entries, count)) != MTPC_OK) return rc;
+  if ((rc = check_device()) != MTPC_OK) return rc;
+  mtpc_gradient_list* list = new (std::nothrow) mtpc_gradient_list;
+  ClipChunk* chunks = new (std::nothrow) ClipChunk[static_cast<size_t>(p.chunks) + 1];
+  if (!list || !chunks) {
+    delete list;
+    delete[] chunks;
+    return MTPC_ERR_CUDA;
+  }
+  size_t n = 0;
+  for (int i = 0; i < count; ++i) {
+    const mtpc_gradient& e = entries[i];
+    const int head = wide_head(e);
+    // Chunks of equal length, but that the first has the elements before the first vector too: the others then start on one.
+    for (int64_t at = 0; at < e.count;) {
+      ClipChunk& c = chunks[n++];
+      const int own_head = at == 0 && head > 0 ? head : 0;
+      const int64_t take = std::min<int64_t>(e.count - at, kClipChunk + own_head);
+      c.g = static_cast<const uint8_t*>(e.data) + static_cast<size_t>(at) * element(e.dtype);
+      c.out = e.out ? static_cast<uint8_t*>(e.out) + static_cast<size_t>(at) * element(e.out_dtype) : nullptr;
+      c.count = static_cast<int>(take);
+      c.kind = (e.dtype == MTPC_F32 ? kClipF32 : 0u) | (e.out && e.out_dtype == MTPC_F32 ? kClipOutF32 : 0u);
+      if (head >= 0 && own_head < take) c.kind |= kClipWide | static_cast<unsigned>(own_head) << 8;
+      at += take;
+    }
+  }
+  list->chunks = static_cast<const ClipChunk*>(workspace);
+  list->partial = reinterpret_cast<double*>(static_cast<uint8_t*>(workspace) + p.off_partial);
+  list->count = static_cast<int>(n);
+  list->blocks = p.blocks;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  bool ok = n == 0 || cudaMemcpyAsync(workspace, chunks, n * sizeof(ClipChunk), cudaMemcpyHostToDevice, st) == cudaSuccess;
+  ok = cudaStreamSynchronize(st) == cudaSuccess && ok;       // the host's copy goes away
+  delete[] chunks;
+  if (!ok) {
+    cudaGetLastError();
+    delete list;
+    return MTPC_ERR_CUDA;
+  }
+  *out = list;
+  return MTPC_OK;
+}
+
+int mtpc_clip_gradients(mtpc_gradient_list* list, float max_norm, float* out_norm, void* stream) {
+  if (!list || !out_norm) return MTPC_ERR_NULL;
+  if (!(max_norm > 0.f) || !aligned(out_norm, 4)) return MTPC_ERR_SHAPE;
+  const int rc = check_device();
+  if (rc != MTPC_OK) return rc;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  launch_kernel(gradient_square_kernel, list->blocks, kClipThreads, 0, st, true, list->chunks, list->count, list->partial);
+  launch_kernel(gradient_scale_kernel, list->blocks, kClipThreads, 0, st, true, list->chunks, list->count, static_cast<const double*>(list->partial),
+                list->blocks, max_norm, out_norm);
+  return check_launch();
+}
+
+int mtpc_destroy_gradient_list(mtpc_gradient_list* list) {
+  if (!list) return MTPC_ERR_NULL;
+  delete list;
+  return MTPC_OK;
+}
+
+}  // extern "C"
