@@ -15,6 +15,7 @@ namespace mtpc {
 
 constexpr int kClipThreads = 256;
 constexpr int kClipChunk = 8192;             // elements
+constexpr int kClipAhead = 2;                // vectors of eight in flight per thread
 constexpr int kClipMaxBlocks = 148 * 8;
 
 struct ClipChunk {
@@ -36,13 +37,13 @@ __device__ __forceinline__ double chunk_square(const ClipChunk& c) {
       const double x = to_f32(g[threadIdx.x]);
       sum += x * x;
     }
-    for (int i = threadIdx.x; i < packs; i += 4 * kClipThreads) {
-      Pack<T, 8> p[4];
+    for (int i = threadIdx.x; i < packs; i += kClipAhead * kClipThreads) {
+      Pack<T, 8> p[kClipAhead];
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
+      for (int u = 0; u < kClipAhead; ++u)
         if (i + u * kClipThreads < packs) p[u] = load_pack<T, 8>(g + head + (i + u * kClipThreads) * 8);
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
+      for (int u = 0; u < kClipAhead; ++u) {
         if (i + u * kClipThreads < packs) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
@@ -95,13 +96,13 @@ __device__ __forceinline__ void chunk_scale(const ClipChunk& c, float first, flo
   if (c.kind & kClipWide) {
     const int head = c.kind >> 8, packs = (c.count - head) / 8;
     if (static_cast<int>(threadIdx.x) < head) out[threadIdx.x] = from_f32<TO>(to_f32(g[threadIdx.x]) * first * by);
-    for (int i = threadIdx.x; i < packs; i += 4 * kClipThreads) {
-      Pack<TI, 8> p[4];
+    for (int i = threadIdx.x; i < packs; i += kClipAhead * kClipThreads) {
+      Pack<TI, 8> p[kClipAhead];
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
+      for (int u = 0; u < kClipAhead; ++u)
         if (i + u * kClipThreads < packs) p[u] = load_pack<TI, 8>(g + head + (i + u * kClipThreads) * 8);
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
+      for (int u = 0; u < kClipAhead; ++u) {
         if (i + u * kClipThreads < packs) {
           float x[8];
           unpack(p[u], x);

@@ -7,10 +7,12 @@
 // is fixed), cut into chunks of equal length, and a chunk's positions are added up row after row: each element of d_out is read once, whatever the
 // tokens are. A token whose positions lie within a chunk is written at once; of one that crosses chunks every chunk leaves its part, which are added up
 // in their order afterwards.
-//   embed_sort_kernel     one block sorts (up to kSortTile positions; beyond that embed_count / embed_scan / embed_scatter per digit), the
-//                         others meanwhile write the zeros of the rows that no position has and ask for d_out by L2 prefetch
+//   embed_order_kernel    up to kOrderMaxT positions: every block owns a range of tokens, finds their positions among all of them and sorts those;
+//                         meanwhile the device asks for d_out by L2 prefetch
+//   embed_count / embed_scan / embed_scatter_kernel   more positions: by digits of 9 bits
 //   embed_segment_kernel  the chunks
 //   embed_join_kernel     the tokens that cross chunks
+// Rows that no position has are zeros: written by further blocks of the last two, behind whose short chains of dependent loads that hides.
 #pragma once
 #include <cuda_bf16.h>
 #include <stdint.h>
@@ -69,57 +71,196 @@ __global__ void __launch_bounds__(256) embed_kernel(const __grid_constant__ Embe
 }
 
 // ---------------------------------------------------------------- the positions in the order of their tokens
-constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
-constexpr int kSortDigit = 9, kSortBins = 1 << kSortDigit;
-constexpr int kSortPerLane = 16, kSortTile = kSortThreads * kSortPerLane;      // positions a block sorts
 constexpr int kEmbedMaxT = 1 << 26, kEmbedMaxV = 1 << 20, kEmbedMaxD = 1 << 20;
-constexpr int kClearScanT = 1 << 16;              // positions up to which the blocks that clear rows look for the rows that have none
 constexpr size_t kEmbedPrefetchBytes = 32u << 20;
-constexpr size_t kSortSmem = static_cast<size_t>(kSortWarps) * kSortBins * 4;
 
 struct EmbedSortArgs {
   const int* tokens;
   int *key_a, *pos_a, *key_b, *pos_b;     // the last digit's go to key_a, pos_a
+  uint8_t* present;                       // [v + 1]: whether a token has positions
   int* hist;                              // [bins][tiles]
   unsigned* status;                       // may be NULL
-  float* d_table;                         // rows without a position are cleared (NULL: none are)
   const void* d_out;
-  long long d_table_stride, d_out_stride;
-  int T, v, d, digits, tiles;
+  long long d_out_stride;
+  int T, v, d;
+  int range;                              // embed_order_kernel: tokens of a block
+  int digits, tiles, rounds;              // else: a tile is `rounds` times kSortTile positions
   int d_out_bytes;                        // of an element
 };
 
 // The key of a position: its token, or v for padding and what is no token.
-__device__ __forceinline__ int embed_key(const EmbedSortArgs& a, int i) {
-  const int token = a.tokens[i];
-  if (token >= a.v && a.status) atomicOr(a.status, kStatusBadToken);
-  return token < 0 || token >= a.v ? a.v : token;
+__device__ __forceinline__ int embed_key(const EmbedSortArgs& a, int token) { return token < 0 || token >= a.v ? a.v : token; }
+
+// Block `part` of `parts`: its share of the first rows of d_out into L2.
+__device__ __forceinline__ void prefetch_rows(const EmbedSortArgs& a, int part, int parts) {
+  const int row_bytes = a.d * a.d_out_bytes, lines = (row_bytes + 127) / 128;           // (at most 4 MB a row)
+  const int rows = min(a.T, static_cast<int>(kEmbedPrefetchBytes / row_bytes) + 1);
+  for (int i = part * blockDim.x + threadIdx.x; i < rows * lines; i += parts * blockDim.x) {       // (at most 2^25 lines)
+    const int row = i / lines, line = i - row * lines;
+    prefetch_l2(static_cast<const uint8_t*>(a.d_out) + row * a.d_out_stride * a.d_out_bytes + line * 128);
+  }
 }
+
+// The lanes of a warp whose value has the same `bits` low bits (fewer instructions than the warp's match, which looks at all 32).
+__device__ __forceinline__ unsigned equal_lanes(unsigned x, int bits, unsigned among) {
+  for (int b = 0; b < bits; ++b) {
+    const bool one = (x >> b) & 1u;
+    const unsigned ones = __ballot_sync(0xffffffffu, one);
+    among &= one ? ones : ~ones;
+  }
+  return among;
+}
+
+// Up to kOrderMaxT positions. Every block looks through all tokens (from L2) for those of its range, lists them in order, and sorts the list by
+// counting: a warp counts its part of it per token, the counts become places, the warps write their keys and positions there. One launch of a
+// few microseconds where a sort by one block takes 18 (8192 positions): that one sorts them all while the device waits.
+constexpr int kOrderThreads = 512, kOrderWarps = kOrderThreads / 32, kOrderMaxT = 1 << 15, kOrderMaxRange = 512;
+inline size_t order_smem_bytes(int T) { return static_cast<size_t>(T) * 4; }
+__global__ void __launch_bounds__(kOrderThreads) embed_order_kernel(const __grid_constant__ EmbedSortArgs a) {
+  extern __shared__ unsigned list[];               // token's place in the range << 16 | position (below 2^15)
+  __shared__ unsigned counts[kOrderWarps][kOrderMaxRange];
+  __shared__ unsigned found[kOrderWarps], below[kOrderWarps];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int lo = blockIdx.x * a.range, tokens = min(a.range, a.v + 1 - lo);       // (key v: what is no token)
+  grid_dependency_wait();
+  grid_launch_dependents();
+  prefetch_rows(a, blockIdx.x, gridDim.x);
+
+  const int per_warp = (a.T + kOrderThreads - 1) / kOrderThreads * 32;
+  const int begin = min(warp * per_warp, a.T), end = min(begin + per_warp, a.T);
+  unsigned mine = 0, less = 0;
+  bool bad = false;
+  for (int i = begin; i < end; i += 8 * 32) {
+    int key[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) key[u] = i + u * 32 + lane < end ? a.tokens[i + u * 32 + lane] : INT32_MIN;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const bool is = i + u * 32 + lane < end;
+      bad |= key[u] >= a.v;
+      const int k = embed_key(a, key[u]);
+      mine += __popc(__ballot_sync(0xffffffffu, is && k >= lo && k < lo + tokens));
+      less += __popc(__ballot_sync(0xffffffffu, is && k < lo));
+    }
+  }
+  if (blockIdx.x == 0 && bad && a.status) atomicOr(a.status, kStatusBadToken);
+  if (lane == 0) {
+    found[warp] = mine;
+    below[warp] = less;
+  }
+  for (int b = lane; b < tokens; b += 32) counts[warp][b] = 0;
+  __syncthreads();
+  unsigned base = 0, count = 0, at = 0;            // of the range's positions: the first one's place, how many, those of the warps before
+#pragma unroll
+  for (int w = 0; w < kOrderWarps; ++w) {
+    base += below[w];
+    if (w < warp) at += found[w];
+    count += found[w];
+  }
+  if (mine > 0) {
+    for (int i = begin; i < end; i += 8 * 32) {
+      int key[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) key[u] = i + u * 32 + lane < end ? a.tokens[i + u * 32 + lane] : INT32_MIN;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int k = embed_key(a, key[u]) - lo;
+        const bool is = i + u * 32 + lane < end && k >= 0 && k < tokens;
+        const unsigned which = __ballot_sync(0xffffffffu, is);
+        if (is) list[at + __popc(which & ((1u << lane) - 1u))] = static_cast<unsigned>(k) << 16 | static_cast<unsigned>(i + u * 32 + lane);
+        at += __popc(which);
+      }
+    }
+  }
+  __syncthreads();
+
+  const int bits = 32 - __clz(tokens - 1);
+  const int share = (count + kOrderThreads - 1) / kOrderThreads * 32;
+  const int from = min(warp * share, static_cast<int>(count)), to = min(from + share, static_cast<int>(count));
+  for (int i = from; i < to; i += 32) {
+    const bool is = i + lane < to;
+    const unsigned bin = is ? list[i + lane] >> 16 : 0u;
+    const unsigned peers = equal_lanes(bin, bits, __ballot_sync(0xffffffffu, is));
+    if (is && lane == __ffs(peers) - 1) counts[warp][bin] += __popc(peers);
+    __syncwarp();
+  }
+  __syncthreads();
+  // the places: tokens in order, of each the warps in order (a thread per token)
+  unsigned sum = 0;
+  const bool has = static_cast<int>(threadIdx.x) < tokens;
+  if (has) {
+#pragma unroll
+    for (int w = 0; w < kOrderWarps; ++w) sum += counts[w][threadIdx.x];
+    a.present[lo + threadIdx.x] = sum > 0;
+  }
+  unsigned before = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const unsigned y = __shfl_up_sync(0xffffffffu, before, o);
+    if (lane >= o) before += y;
+  }
+  if (lane == 31) found[warp] = before;
+  __syncthreads();
+  before += base - sum;
+  for (int w = 0; w < warp; ++w) before += found[w];
+  if (has) {
+#pragma unroll
+    for (int w = 0; w < kOrderWarps; ++w) {
+      const unsigned c = counts[w][threadIdx.x];
+      counts[w][threadIdx.x] = before;
+      before += c;
+    }
+  }
+  __syncthreads();
+  for (int i = from; i < to; i += 32) {
+    const bool is = i + lane < to;
+    const unsigned item = is ? list[i + lane] : 0u, bin = item >> 16;
+    const unsigned peers = equal_lanes(bin, bits, __ballot_sync(0xffffffffu, is));
+    const unsigned first = is ? counts[warp][bin] : 0u;
+    __syncwarp();
+    if (is) {
+      const unsigned place = first + __popc(peers & ((1u << lane) - 1u));
+      a.key_a[place] = lo + bin;
+      a.pos_a[place] = item & 0xffffu;
+      if (lane == __ffs(peers) - 1) counts[warp][bin] = first + __popc(peers);
+    }
+    __syncwarp();
+  }
+}
+
+// More positions: a stable sort by digits, from the lowest. Every block has a tile of adjacent positions, `rounds` times kSortTile of them.
+constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
+constexpr int kSortDigit = 9, kSortBins = 1 << kSortDigit;
+constexpr int kSortPerLane = 4, kSortTile = kSortThreads * kSortPerLane;
+constexpr size_t kSortSmem = static_cast<size_t>(kSortWarps) * kSortBins * 4;
+
 // Where the keys of digit `p` are written to (alternating so that the last one writes key_a, pos_a).
 __device__ __forceinline__ int* sort_keys(const EmbedSortArgs& a, int p) { return ((a.digits - 1 - p) & 1) ? a.key_b : a.key_a; }
 __device__ __forceinline__ int* sort_positions(const EmbedSortArgs& a, int p) { return ((a.digits - 1 - p) & 1) ? a.pos_b : a.pos_a; }
 
-// A tile's keys and positions before digit p, up to 16 a lane: a warp's are adjacent.
+// The keys and positions before digit p of one round, a warp's adjacent.
 struct SortItems {
   int key[kSortPerLane], pos[kSortPerLane];
 };
-__device__ __forceinline__ void sort_load(const EmbedSortArgs& a, int p, int tile, SortItems& x) {
-  const int first = tile * kSortTile;
-  const int count = min(a.T - first, kSortTile);
-  const int per_warp = (count + kSortThreads - 1) / kSortThreads * 32;                   // at most 512
-  const int begin = (threadIdx.x >> 5) * per_warp;
-  const int end = min(begin + per_warp, count);
+__device__ __forceinline__ void sort_load(const EmbedSortArgs& a, int p, long long first, SortItems& x) {
 #pragma unroll
   for (int j = 0; j < kSortPerLane; ++j) {
-    const int i = begin + j * 32 + (threadIdx.x & 31);
+    const long long i = first + (threadIdx.x >> 5) * (32 * kSortPerLane) + j * 32 + (threadIdx.x & 31);
     x.key[j] = -1;
-    if (i < end) {
-      x.key[j] = p == 0 ? embed_key(a, first + i) : sort_keys(a, p - 1)[first + i];
-      x.pos[j] = p == 0 ? first + i : sort_positions(a, p - 1)[first + i];
+    if (i < a.T) {
+      if (p == 0) {
+        const int token = a.tokens[i];
+        if (token >= a.v && a.status) atomicOr(a.status, kStatusBadToken);
+        x.key[j] = embed_key(a, token);
+        x.pos[j] = static_cast<int>(i);
+      } else {
+        x.key[j] = sort_keys(a, p - 1)[i];
+        x.pos[j] = sort_positions(a, p - 1)[i];
+      }
     }
   }
 }
-__device__ __forceinline__ int sort_digit(int key, int p) { return (key >> (p * kSortDigit)) & (kSortBins - 1); }
+__device__ __forceinline__ unsigned sort_digit(int key, int p) { return (static_cast<unsigned>(key) >> (p * kSortDigit)) & (kSortBins - 1); }
 
 // counts[warp][bin] of the warp's keys. Equal digits of a warp's 32 keys find each other, the lowest lane counts them.
 __device__ __forceinline__ void sort_count(const SortItems& x, int p, unsigned* counts) {
@@ -129,15 +270,14 @@ __device__ __forceinline__ void sort_count(const SortItems& x, int p, unsigned* 
   __syncwarp();
 #pragma unroll
   for (int j = 0; j < kSortPerLane; ++j) {
-    if (!__any_sync(0xffffffffu, x.key[j] >= 0)) break;
-    const int digit = x.key[j] >= 0 ? sort_digit(x.key[j], p) : -1;
-    const unsigned peers = __match_any_sync(0xffffffffu, digit);
-    if (digit >= 0 && lane == __ffs(peers) - 1) mine[digit] += __popc(peers);
+    const unsigned digit = sort_digit(x.key[j], p);
+    const unsigned peers = equal_lanes(digit, kSortDigit, __ballot_sync(0xffffffffu, x.key[j] >= 0));
+    if (x.key[j] >= 0 && lane == __ffs(peers) - 1) mine[digit] += __popc(peers);
     __syncwarp();
   }
 }
-// counts -> the place of the warp's first key of each bin; base: the place of the tile's first key of bin threadIdx.x.
-__device__ __forceinline__ void sort_offsets(unsigned* counts, unsigned base) {
+// counts -> the place of the warp's first key of each bin; base: that of the block's first key of bin threadIdx.x, and behind it the next round's.
+__device__ __forceinline__ void sort_offsets(unsigned* counts, unsigned& base) {
   if (threadIdx.x < kSortBins) {
 #pragma unroll 8
     for (int w = 0; w < kSortWarps; ++w) {
@@ -154,12 +294,12 @@ __device__ __forceinline__ void sort_place(const EmbedSortArgs& a, const SortIte
   int *keys = sort_keys(a, p), *positions = sort_positions(a, p);
 #pragma unroll
   for (int j = 0; j < kSortPerLane; ++j) {
-    if (!__any_sync(0xffffffffu, x.key[j] >= 0)) break;
-    const int digit = x.key[j] >= 0 ? sort_digit(x.key[j], p) : -1;
-    const unsigned peers = __match_any_sync(0xffffffffu, digit);
-    const unsigned first = digit >= 0 ? mine[digit] : 0u;
+    const bool is = x.key[j] >= 0;
+    const unsigned digit = sort_digit(x.key[j], p);
+    const unsigned peers = equal_lanes(digit, kSortDigit, __ballot_sync(0xffffffffu, is));
+    const unsigned first = is ? mine[digit] : 0u;
     __syncwarp();
-    if (digit >= 0) {
+    if (is) {
       const unsigned at = first + __popc(peers & ((1u << lane) - 1u));
       keys[at] = x.key[j];
       positions[at] = x.pos[j];
@@ -191,90 +331,31 @@ __device__ __forceinline__ unsigned block_running_sum(unsigned x, unsigned* warp
   return (warp == 0 ? 0u : earlier) + sum - x;
 }
 
-// Block `part` of `parts`: zeros to the rows of its share of the table that no position has (where there are too many positions to look
-// through: to all of its rows), then its share of the first rows of d_out into L2.
-__device__ __forceinline__ void clear_rows(const EmbedSortArgs& a, int part, int parts, unsigned* present) {
-  if (a.d_table) {
-    const int lo = static_cast<int>(static_cast<long long>(part) * a.v / parts), hi = static_cast<int>(static_cast<long long>(part + 1) * a.v / parts);
-    for (int i = threadIdx.x; i < (hi - lo + 31) / 32; i += kSortThreads) present[i] = 0;
-    __syncthreads();
-    if (a.T <= kClearScanT) {
-      for (int i = threadIdx.x; i < a.T; i += kSortThreads) {
-        const int token = a.tokens[i];
-        if (token >= lo && token < hi) atomicOr(&present[(token - lo) >> 5], 1u << ((token - lo) & 31));
-      }
-      __syncthreads();
-    }
-    const bool wide = a.d % 4 == 0 && a.d_table_stride % 4 == 0 && (reinterpret_cast<uintptr_t>(a.d_table) & 15) == 0;
-    const int per_row = wide ? a.d / 4 : a.d;
-    int share = 32;                                    // threads to a row: as many as it has elements, up to the block
-    while (share < per_row && share < kSortThreads) share <<= 1;
-    for (int b = lo + static_cast<int>(threadIdx.x) / share; b < hi; b += kSortThreads / share) {
-      if ((present[(b - lo) >> 5] >> ((b - lo) & 31)) & 1u) continue;
-      float* row = a.d_table + b * a.d_table_stride;
-      for (int i = threadIdx.x & (share - 1); i < per_row; i += share) {
-        if (wide) reinterpret_cast<float4*>(row)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-        else row[i] = 0.f;
-      }
-    }
-  }
-  if (a.T == 0) return;
-  const long long row_bytes = static_cast<long long>(a.d) * a.d_out_bytes;
-  const int lines = static_cast<int>((row_bytes + 127) / 128);
-  const long long rows = min(static_cast<long long>(a.T), static_cast<long long>(kEmbedPrefetchBytes) / row_bytes + 1);
-  for (long long i = static_cast<long long>(part) * kSortThreads + threadIdx.x; i < rows * lines; i += static_cast<long long>(parts) * kSortThreads) {
-    const long long row = i / lines, line = i - row * lines;
-    prefetch_l2(static_cast<const uint8_t*>(a.d_out) + row * a.d_out_stride * a.d_out_bytes + line * 128);
-  }
-}
-
-// All digits of up to kSortTile positions in block 0.
-__global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const __grid_constant__ EmbedSortArgs a) {
-  extern __shared__ unsigned counts[];
-  __shared__ unsigned warp_sums[kSortWarps];
-  grid_dependency_wait();
-  grid_launch_dependents();
-  if (blockIdx.x > 0) {
-    clear_rows(a, blockIdx.x - 1, gridDim.x - 1, counts);
-    return;
-  }
-  for (int p = 0; p < a.digits; ++p) {
-    SortItems x;
-    sort_load(a, p, 0, x);
-    sort_count(x, p, counts);
-    __syncthreads();
-    unsigned mine = 0, total;
-    if (threadIdx.x < kSortBins) {
-#pragma unroll 8
-      for (int w = 0; w < kSortWarps; ++w) mine += counts[w * kSortBins + threadIdx.x];
-    }
-    const unsigned base = block_running_sum(mine, warp_sums, total);
-    sort_offsets(counts, base);
-    __syncthreads();
-    sort_place(a, x, p, counts);
-    __syncthreads();
-  }
-}
-
-// More positions, one digit: the tiles' counts, their running sums over (bin, tile), and every tile's keys to their places.
+// One digit: the tiles' counts, their running sums over (bin, tile), and every tile's keys to their places. The blocks of the first count that have no
+// tile prefetch, and clear `present`, which the last digit's placing marks.
 __global__ void __launch_bounds__(kSortThreads) embed_count_kernel(const __grid_constant__ EmbedSortArgs a, int p) {
   extern __shared__ unsigned counts[];
   grid_dependency_wait();
   grid_launch_dependents();
   if (static_cast<int>(blockIdx.x) >= a.tiles) {
-    clear_rows(a, blockIdx.x - a.tiles, gridDim.x - a.tiles, counts);
+    const int part = blockIdx.x - a.tiles, parts = gridDim.x - a.tiles;
+    for (int b = part * kSortThreads + threadIdx.x; b <= a.v; b += parts * kSortThreads) a.present[b] = 0;
+    prefetch_rows(a, part, parts);
     return;
   }
-  SortItems x;
-  sort_load(a, p, blockIdx.x, x);
-  sort_count(x, p, counts);
-  __syncthreads();
-  if (threadIdx.x < kSortBins) {
-    unsigned mine = 0;
+  unsigned sum = 0;
+  for (int r = 0; r < a.rounds; ++r) {
+    SortItems x;
+    sort_load(a, p, (static_cast<long long>(blockIdx.x) * a.rounds + r) * kSortTile, x);
+    sort_count(x, p, counts);
+    __syncthreads();
+    if (threadIdx.x < kSortBins) {
 #pragma unroll 8
-    for (int w = 0; w < kSortWarps; ++w) mine += counts[w * kSortBins + threadIdx.x];
-    a.hist[static_cast<size_t>(threadIdx.x) * a.tiles + blockIdx.x] = mine;
+      for (int w = 0; w < kSortWarps; ++w) sum += counts[w * kSortBins + threadIdx.x];
+    }
+    __syncthreads();
   }
+  if (threadIdx.x < kSortBins) a.hist[static_cast<size_t>(threadIdx.x) * a.tiles + blockIdx.x] = sum;
 }
 __global__ void __launch_bounds__(kSortThreads) embed_scan_kernel(int* hist, int count) {
   __shared__ unsigned warp_sums[kSortWarps];
@@ -294,27 +375,39 @@ __global__ void __launch_bounds__(kSortThreads) embed_scatter_kernel(const __gri
   extern __shared__ unsigned counts[];
   grid_dependency_wait();
   grid_launch_dependents();
-  SortItems x;
-  sort_load(a, p, blockIdx.x, x);
-  sort_count(x, p, counts);
-  __syncthreads();
-  sort_offsets(counts, threadIdx.x < kSortBins ? a.hist[static_cast<size_t>(threadIdx.x) * a.tiles + blockIdx.x] : 0u);
-  __syncthreads();
-  sort_place(a, x, p, counts);
+  unsigned base = threadIdx.x < kSortBins ? a.hist[static_cast<size_t>(threadIdx.x) * a.tiles + blockIdx.x] : 0u;
+  for (int r = 0; r < a.rounds; ++r) {
+    SortItems x;
+    sort_load(a, p, (static_cast<long long>(blockIdx.x) * a.rounds + r) * kSortTile, x);
+    sort_count(x, p, counts);
+    __syncthreads();
+    sort_offsets(counts, base);
+    __syncthreads();
+    sort_place(a, x, p, counts);
+    if (p == a.digits - 1) {
+#pragma unroll
+      for (int j = 0; j < kSortPerLane; ++j)
+        if (x.key[j] >= 0) a.present[x.key[j]] = 1;          // (every writer writes the same)
+    }
+    __syncthreads();
+  }
 }
 
 // ---------------------------------------------------------------- sums of the sorted positions
-constexpr int kSegmentThreads = 256;
+constexpr int kSegmentThreads = 64;
 constexpr int kSegmentStage = 256;      // positions whose keys are in shared memory at a time
+constexpr int kClearRows = 8;           // rows that a warp clears at a time
 
 struct EmbedSegmentArgs {
   const int *key, *pos;                 // sorted; key v: no token
+  const uint8_t* present;
   const void* d_out;
   float *d_table, *part;                // part [chunks][2][d]: what a chunk adds to the token it begins in / that goes on behind it
   long long d_out_stride, d_table_stride;
-  int T, v, d, chunk, chunks;
+  int T, v, d, chunk, chunks, slabs;    // slabs: of the columns
+  int clear_begin, clear_end;           // the rows that this launch's further blocks clear
   float scale;
-  bool accumulate;
+  bool accumulate, wide_rows;           // wide_rows: the table's rows allow float4
 };
 
 template <int V>
@@ -327,27 +420,54 @@ __device__ __forceinline__ void write_table(const EmbedSegmentArgs& a, int token
   store_f32<float, V>(dst, o);
 }
 
-// blockIdx.x: columns, blockIdx.y: chunk. U rows are in flight per thread.
+// Zeros to the rows without positions: warp `part` of `parts`, eight adjacent rows at a time.
+__device__ __forceinline__ void clear_rows(const EmbedSegmentArgs& a, int part, int parts) {
+  const int lane = threadIdx.x & 31;
+  const int groups = (a.clear_end - a.clear_begin + kClearRows - 1) / kClearRows;
+  for (int g = part; g < groups; g += parts) {
+    const int row0 = a.clear_begin + g * kClearRows;
+    unsigned absent = __ballot_sync(0xffffffffu, lane < kClearRows && row0 + lane < a.clear_end && !a.present[min(row0 + lane, a.v)]);
+    for (; absent; absent &= absent - 1) {
+      float* row = a.d_table + (row0 + __ffs(absent) - 1) * a.d_table_stride;
+      if (a.wide_rows) {
+        for (int i = lane; i < a.d / 4; i += 32) reinterpret_cast<float4*>(row)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      } else {
+        for (int i = lane; i < a.d; i += 32) row[i] = 0.f;
+      }
+    }
+  }
+}
+
+// A block per chunk and slab of columns (the slabs of a chunk follow each other), then those that clear. U rows are in flight per thread. Blocks of two
+// warps, so that a chunk is long: what tokens that cross chunks cost is two rows of fp32 a chunk, written and read again.
 template <typename T, int V, int U>
 __global__ void __launch_bounds__(kSegmentThreads) embed_segment_kernel(const __grid_constant__ EmbedSegmentArgs a) {
   __shared__ int key[kSegmentStage + 1], pos[kSegmentStage];
-  const int col = (blockIdx.x * blockDim.x + threadIdx.x) * V;
-  const int lo = blockIdx.y * a.chunk, hi = min(lo + a.chunk, a.T);
   grid_dependency_wait();
+  if (static_cast<int>(blockIdx.x) >= a.chunks * a.slabs) {
+    const int blocks = a.chunks * a.slabs;
+    clear_rows(a, (blockIdx.x - blocks) * (kSegmentThreads / 32) + (threadIdx.x >> 5), (gridDim.x - blocks) * (kSegmentThreads / 32));
+    grid_launch_dependents();
+    return;
+  }
+  const int chunk = blockIdx.x / a.slabs;
+  const int col = ((blockIdx.x - chunk * a.slabs) * kSegmentThreads + threadIdx.x) * V;
+  const int lo = chunk * a.chunk, hi = min(lo + a.chunk, a.T);
   float sum[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) sum[i] = 0.f;
-  float* part = a.part + static_cast<size_t>(blockIdx.y) * 2 * a.d + col;
+  float* part = a.part + static_cast<size_t>(chunk) * 2 * a.d + col;
   bool begins = true;                            // the token being added up has no position in an earlier chunk
   for (int base = lo; base < hi; base += kSegmentStage) {
     const int count = min(hi - base, kSegmentStage);
     __syncthreads();
-    for (int i = threadIdx.x; i <= count; i += blockDim.x) {
+    for (int i = threadIdx.x; i <= count; i += kSegmentThreads) {
       key[i] = base + i < a.T ? a.key[base + i] : a.v;
       if (i < count) pos[i] = a.pos[base + i];
     }
+    const int earlier = base == lo && lo > 0 ? a.key[lo - 1] : -1;
     __syncthreads();
-    if (base == lo) begins = lo == 0 || a.key[lo - 1] != key[0];
+    if (base == lo) begins = earlier != key[0];
     if (key[0] == a.v) break;                    // the rest of the positions have no token
     for (int i = 0; i < count; i += U) {
       Pack<T, V> x[U];
@@ -379,49 +499,73 @@ __global__ void __launch_bounds__(kSegmentThreads) embed_segment_kernel(const __
   grid_launch_dependents();
 }
 
-// The tokens that cross chunks: the block of the chunk in which one begins adds up its parts, warp y every eighth, then the warps' sums.
+// The tokens that cross chunks. A block has eight chunks and 32 V columns; the chunk in which such a token begins answers for it: a warp adds up its
+// parts if they are at most eight, all warps together (every eighth part each, then the warps' sums) if they are more.
+constexpr int kJoinWarps = 8;
 template <int V>
-__global__ void __launch_bounds__(256) embed_join_kernel(const __grid_constant__ EmbedSegmentArgs a) {
-  __shared__ float share[8][32][V];
-  const int c = blockIdx.y, lo = c * a.chunk, hi = min(lo + a.chunk, a.T);
+__global__ void __launch_bounds__(32 * kJoinWarps) embed_join_kernel(const __grid_constant__ EmbedSegmentArgs a) {
+  __shared__ float share[kJoinWarps][32][V];
   grid_dependency_wait();
   grid_launch_dependents();
-  if (hi >= a.T) return;
-  const int token = a.key[hi - 1];
-  if (token == a.v || a.key[hi] != token) return;                       // ends here
-  if (lo > 0 && a.key[lo - 1] == token) return;                         // began earlier
-  int last = c + 1;                                                     // the last chunk that has the token: its first key is the token
-  for (int step = 1;; step <<= 1) {                                     // (sorted: found in steps that double, then halve)
-    if (last + step >= a.chunks || a.key[static_cast<long long>(last + step) * a.chunk] != token) {
-      for (step >>= 1; step > 0; step >>= 1)
-        if (last + step < a.chunks && a.key[static_cast<long long>(last + step) * a.chunk] == token) last += step;
-      break;
-    }
-    last += step;
-  }
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int col = (blockIdx.x * 32 + lane) * V;
-  float sum[V];
+  const int slabs = (a.d + 32 * V - 1) / (32 * V), groups = (a.chunks + kJoinWarps - 1) / kJoinWarps;
+  if (static_cast<int>(blockIdx.x) >= groups * slabs) {
+    clear_rows(a, (blockIdx.x - groups * slabs) * kJoinWarps + warp, (gridDim.x - groups * slabs) * kJoinWarps);
+    return;
+  }
+  const int c0 = blockIdx.x / slabs * kJoinWarps;
+  const int col = ((blockIdx.x - blockIdx.x / slabs * slabs) * 32 + lane) * V;
+  int token = a.v, last = -1;                                           // lane q: of chunk c0 + q, and the last chunk that has the token
+  if (lane < kJoinWarps && c0 + lane < a.chunks) {
+    const int lo = (c0 + lane) * a.chunk, hi = min(lo + a.chunk, a.T);
+    const int before = lo > 0 ? a.key[lo - 1] : -1, after = hi < a.T ? a.key[hi] : a.v;
+    token = a.key[hi - 1];
+    if (token != a.v && after == token && before != token) {
+      last = c0 + lane + 1;                                             // (sorted: found in steps that double, then halve)
+      for (int step = 1;; step <<= 1) {
+        if (last + step >= a.chunks || a.key[(last + step) * a.chunk] != token) {
+          for (step >>= 1; step > 0; step >>= 1)
+            if (last + step < a.chunks && a.key[(last + step) * a.chunk] == token) last += step;
+          break;
+        }
+        last += step;
+      }
+    }
+  }
+  auto add = [&](int begin, int end, int first, int step, float (&sum)[V]) {
 #pragma unroll
-  for (int i = 0; i < V; ++i) sum[i] = 0.f;
-  if (col < a.d) {
-#pragma unroll 4
-    for (int q = c + warp; q <= last; q += 8) {
+    for (int i = 0; i < V; ++i) sum[i] = 0.f;
+    if (col >= a.d) return;
+#pragma unroll 8
+    for (int q = begin + first; q <= end; q += step) {
       float x[V];
-      unpack(load_pack<float, V>(a.part + (static_cast<size_t>(q) * 2 + (q == c ? 1 : 0)) * a.d + col), x);
+      unpack(load_pack<float, V>(a.part + (static_cast<size_t>(q) * 2 + (q == begin ? 1 : 0)) * a.d + col), x);
 #pragma unroll
       for (int i = 0; i < V; ++i) sum[i] += x[i];
     }
+  };
+  const unsigned owners = __ballot_sync(0xffffffffu, last >= 0), many = __ballot_sync(0xffffffffu, last - (c0 + lane) >= kJoinWarps);
+  const int own_token = __shfl_sync(0xffffffffu, token, warp), own_last = __shfl_sync(0xffffffffu, last, warp);
+  float sum[V];
+  if ((owners & ~many) >> warp & 1u) {
+    add(c0 + warp, own_last, 0, 1, sum);
+    if (col < a.d) write_table<V>(a, own_token, col, sum);
   }
+  for (unsigned left = many; left; left &= left - 1) {                  // (the same in every warp)
+    const int q = __ffs(left) - 1;
+    const int its_token = __shfl_sync(0xffffffffu, token, q);
+    add(c0 + q, __shfl_sync(0xffffffffu, last, q), warp, kJoinWarps, sum);
 #pragma unroll
-  for (int i = 0; i < V; ++i) share[warp][lane][i] = sum[i];
-  __syncthreads();
-  if (warp == 0 && col < a.d) {
-    for (int w = 1; w < 8; ++w) {
+    for (int i = 0; i < V; ++i) share[warp][lane][i] = sum[i];
+    __syncthreads();
+    if (warp == 0 && col < a.d) {
+      for (int w = 1; w < kJoinWarps; ++w) {
 #pragma unroll
-      for (int i = 0; i < V; ++i) sum[i] += share[w][lane][i];
+        for (int i = 0; i < V; ++i) sum[i] += share[w][lane][i];
+      }
+      write_table<V>(a, its_token, col, sum);
     }
-    write_table<V>(a, token, col, sum);
+    __syncthreads();
   }
 }
 

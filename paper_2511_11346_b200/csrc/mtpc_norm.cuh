@@ -39,12 +39,18 @@ __device__ __forceinline__ unsigned magnitude(float x) { return __float_as_uint(
 
 // What a code of 1 stands for where the largest magnitude is `bits`.
 __device__ __forceinline__ float code_scale(unsigned bits) {
-  const float s = __uint_as_float(bits) / kE4m3Max;
+  const float s = __uint_as_float(bits) * (1.f / kE4m3Max);
   return s == 0.f ? 1.f : s;
 }
+// x / scale as x * first * second (a reciprocal beside eight products, where eight divisions took longer than the row's bytes). Scales whose
+// reciprocal fp32 cannot hold go in two steps, the first a power of two.
+__device__ __forceinline__ float2 code_factors(float scale) {
+  const float first = scale < 0x1p-100f ? 0x1p64f : 1.f;
+  return make_float2(first, 1.f / (scale * first));
+}
 
-template <typename IO, int V, int NV, int THREADS>
-__global__ void __launch_bounds__(THREADS) residual_rmsnorm_kernel(const __grid_constant__ NormArgs a) {
+template <typename IO, int V, int NV, int THREADS, int CTAS>
+__global__ void __launch_bounds__(THREADS, CTAS) residual_rmsnorm_kernel(const __grid_constant__ NormArgs a) {
   __shared__ float red[2][1][32];
   __shared__ unsigned group_max[V == 1 ? kNormMaxWidth / kNormMinGroup : 1];
   const int row = blockIdx.x * blockDim.y + threadIdx.y;
@@ -176,15 +182,15 @@ __global__ void __launch_bounds__(THREADS) residual_rmsnorm_kernel(const __grid_
   for (int j = 0; j < NV; ++j) {
     const int col = (tid + j * blockDim.x) * V;
     if (col >= a.d) continue;
-    const float scale = code_scale(largest[j]);
+    const float2 by = code_factors(code_scale(largest[j]));
     if constexpr (V > 1) {
       Pack<uint16_t, V / 2> o;
 #pragma unroll
       for (int i = 0; i < V; i += 2)
-        o.e[i / 2] = __nv_cvt_float2_to_fp8x2(make_float2(s[j][i] / scale, s[j][i + 1] / scale), __NV_SATFINITE, __NV_E4M3);
+        o.e[i / 2] = __nv_cvt_float2_to_fp8x2(make_float2(s[j][i] * by.x * by.y, s[j][i + 1] * by.x * by.y), __NV_SATFINITE, __NV_E4M3);
       store_pack<uint16_t, V / 2>(reinterpret_cast<uint16_t*>(codes + col), o);
     } else {
-      codes[col] = __nv_cvt_float_to_fp8(s[j][0] / scale, __NV_SATFINITE, __NV_E4M3);
+      codes[col] = __nv_cvt_float_to_fp8(s[j][0] * by.x * by.y, __NV_SATFINITE, __NV_E4M3);
     }
   }
 }
@@ -199,91 +205,138 @@ struct NormGradArgs {
   float eps;
 };
 
-// Every block has every gridDim.x-th row and keeps its part of d weight in registers.
-template <typename IO, typename DY, typename DX, int V, int NV>
-__global__ void __launch_bounds__(1024) rmsnorm_grad_kernel(const __grid_constant__ NormGradArgs a) {
+// 16 bytes from global to shared memory without registers; they are there once the thread has waited for the group they were committed in.
+__device__ __forceinline__ void copy_async16(uint32_t dst_smem, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst_smem), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// A thread's eight elements of a row in its own places of shared memory, 16 bytes per piece, a piece's neighbours the other threads'.
+template <typename T>
+struct RingRow {
+  static constexpr int kPieces = sizeof(T) * 8 / 16;
+  static __device__ __forceinline__ void fetch(uint32_t at, const T* src) {
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) copy_async16(at + i * blockDim.x * 16, reinterpret_cast<const uint8_t*>(src) + i * 16);
+  }
+  static __device__ __forceinline__ void read(uint32_t at, float (&x)[8]) {
+    Pack<T, 8> p;
+    uint32_t* r = reinterpret_cast<uint32_t*>(p.e);
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i)
+      asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                   : "=r"(r[4 * i]), "=r"(r[4 * i + 1]), "=r"(r[4 * i + 2]), "=r"(r[4 * i + 3])
+                   : "r"(at + i * blockDim.x * 16));
+    unpack(p, x);
+  }
+};
+// Bytes of a thread's part of a stage.
+template <typename IO, typename DY, typename DX>
+__host__ __device__ constexpr int norm_grad_thread_bytes() { return 8 * (sizeof(IO) + sizeof(DY) + sizeof(DX)); }
+
+// Every block has every gridDim.x-th row and keeps its part of d weight in registers. STAGES > 0 (eight elements a thread): rows come through
+// shared memory, the next STAGES - 1 on their way while one is worked on, every thread copying and reading its own elements (no barrier of their
+// own). With one row at a time in registers two blocks of 512 threads an SM waited for memory half of the time (8192 rows of 4096, bf16, d_out
+// fp32: 88 us). Otherwise (wider rows, and rows that no vectors fit) a row is read twice, the second time from L1 or L2.
+template <typename IO, typename DY, typename DX, int V, int NV, int STAGES, int THREADS, int CTAS>
+__global__ void __launch_bounds__(THREADS, CTAS) rmsnorm_grad_kernel(const __grid_constant__ NormGradArgs a) {
+  constexpr bool kRing = STAGES > 0;
+  static_assert(!kRing || (V == 8 && NV == 1), "a thread's part of a stage is eight elements");
+  extern __shared__ uint8_t ring[];
   __shared__ float red[3][2][32];
   const int tid = threadIdx.x;
+  const uint32_t stage_bytes = norm_grad_thread_bytes<IO, DY, DX>() * blockDim.x, place = smem_u32(ring) + tid * 16;
+  const uint32_t dy_at = RingRow<IO>::kPieces * blockDim.x * 16, stream_at = dy_at + RingRow<DY>::kPieces * blockDim.x * 16;
   grid_dependency_wait();
-  float w[NV][V], dw[NV][V];
+  auto fetch = [&](int row, int stage) {
+    const int col = tid * V;
+    if (row < a.T && col < a.d) {
+      const uint32_t at = place + stage * stage_bytes;
+      RingRow<IO>::fetch(at, static_cast<const IO*>(a.sum) + row * a.sum_stride + col);
+      RingRow<DY>::fetch(at + dy_at, static_cast<const DY*>(a.d_out) + row * a.d_out_stride + col);
+      if (a.d_stream) RingRow<DX>::fetch(at + stream_at, static_cast<const DX*>(a.d_stream) + row * a.d_stream_stride + col);
+    }
+    copy_commit();
+  };
+  if constexpr (kRing) {
+#pragma unroll
+    for (int q = 0; q < STAGES - 1; ++q) fetch(blockIdx.x + q * gridDim.x, q);
+  }
+  float w[V], dw[NV][V];                                     // w: kept by the ring's threads
+  if (kRing && tid * V < a.d) load_weight<V>(a.weight, a.weight_f32, tid * V, w);
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    const int col = (tid + j * blockDim.x) * V;
 #pragma unroll
-    for (int i = 0; i < V; ++i) w[j][i] = dw[j][i] = 0.f;
-    if (col < a.d) load_weight<V>(a.weight, a.weight_f32, col, w[j]);
+    for (int i = 0; i < V; ++i) dw[j][i] = 0.f;
   }
-  int turn = 0;
+  int turn = 0, stage = 0;
   for (int row = blockIdx.x; row < a.T; row += gridDim.x, turn ^= 1) {
     const IO* s_row = static_cast<const IO*>(a.sum) + row * a.sum_stride;
     const DY* dy_row = static_cast<const DY*>(a.d_out) + row * a.d_out_stride;
-    float s[NV][V], dy[NV][V];
-    Pack<DX, V> stream[NV];
-    {
-      Pack<IO, V> ps[NV];
-      Pack<DY, V> pd[NV];
-#pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        const int col = (tid + j * blockDim.x) * V;
-        if (col < a.d) {
-          ps[j] = load_pack<IO, V>(s_row + col);
-          pd[j] = load_pack<DY, V>(dy_row + col);
-          if (a.d_stream) stream[j] = load_pack<DX, V>(static_cast<const DX*>(a.d_stream) + row * a.d_stream_stride + col);
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        const int col = (tid + j * blockDim.x) * V;
-#pragma unroll
-        for (int i = 0; i < V; ++i) s[j][i] = dy[j][i] = 0.f;
-        if (col < a.d) {
-          unpack(ps[j], s[j]);
-          unpack(pd[j], dy[j]);
-        }
-      }
+    const uint32_t at = place + stage * stage_bytes;
+    if constexpr (kRing) {
+      // (the stage that is fetched into was read by this thread alone, a turn ago)
+      fetch(row + (STAGES - 1) * gridDim.x, stage == 0 ? STAGES - 1 : stage - 1);
+      copy_wait<STAGES - 1>();
+      stage = stage + 1 == STAGES ? 0 : stage + 1;
     }
-    float sums[2] = {0.f, 0.f};                              // of s^2 and of weight d_out s
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        sums[0] += s[j][i] * s[j][i];
-        sums[1] += dy[j][i] * w[j][i] * s[j][i];
+    // s times `by`, d_out (and the weight, where it is not kept) of the thread's vector j; false past the row's end
+    auto read = [&](int j, float by, float (&s)[V], float (&dy)[V]) {
+      const int col = (tid + j * blockDim.x) * V;
+      if (col >= a.d) return false;
+      if constexpr (kRing) {
+        RingRow<IO>::read(at, s);
+        RingRow<DY>::read(at + dy_at, dy);
+      } else {
+        unpack(load_pack<IO, V>(s_row + col), s);
+        unpack(load_pack<DY, V>(dy_row + col), dy);
+        load_weight<V>(a.weight, a.weight_f32, col, w);
       }
-    }
-    row_sum(sums, red[turn]);
-    float rstd = rsqrtf(sums[0] / a.d + a.eps), step = rstd;          // step: by which d out becomes d s
-    if (__float_as_uint(sums[0]) == 0x7f800000u) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) s[i] *= by;
+      return true;
+    };
+    auto add_up = [&](float by, float (&sums)[2], float (*share)[32]) {      // s^2 and weight d_out s
       sums[0] = sums[1] = 0.f;
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
+        float s[V], dy[V];
+        if (!read(j, by, s, dy)) continue;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-          s[j][i] *= kNormRescue;
-          sums[0] += s[j][i] * s[j][i];
-          sums[1] += dy[j][i] * w[j][i] * s[j][i];
+          sums[0] += s[i] * s[i];
+          sums[1] += dy[i] * w[i] * s[i];
         }
       }
+      row_sum(sums, share);
+    };
+    float sums[2], by = 1.f;
+    add_up(by, sums, red[turn]);
+    float rstd = rsqrtf(sums[0] / a.d + a.eps);
+    if (__float_as_uint(sums[0]) == 0x7f800000u) {
+      by = kNormRescue;
       __syncthreads();                                       // red[2] may still be read for an earlier row
-      row_sum(sums, red[2]);
+      add_up(by, sums, red[2]);
       rstd = rsqrtf(sums[0] / a.d);
-      step = rstd * kNormRescue;
     }
-    const float mean = sums[1] * rstd / a.d;                 // of weight d_out s rstd
+    const float step = rstd * by, mean = sums[1] * rstd / a.d;         // by which d out becomes d s; of weight d_out s rstd
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int col = (tid + j * blockDim.x) * V;
-      if (col >= a.d) continue;
-      float dx[V];
+      float s[V], dy[V], dx[V];
+      if (!read(j, by, s, dy)) continue;
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        const float unit = s[j][i] * rstd;
-        dw[j][i] += dy[j][i] * unit;
-        dx[i] = step * (dy[j][i] * w[j][i] - unit * mean);
+        const float unit = s[i] * rstd;
+        dw[j][i] += dy[i] * unit;
+        dx[i] = step * (dy[i] * w[i] - unit * mean);
       }
       if (a.d_stream) {
         float more[V];
-        unpack(stream[j], more);
+        if constexpr (kRing) RingRow<DX>::read(at + stream_at, more);
+        else unpack(load_pack<DX, V>(static_cast<const DX*>(a.d_stream) + row * a.d_stream_stride + col), more);
 #pragma unroll
         for (int i = 0; i < V; ++i) dx[i] += more[i];
       }
@@ -297,6 +350,7 @@ __global__ void __launch_bounds__(1024) rmsnorm_grad_kernel(const __grid_constan
       if (col < a.d) store_f32<float, V>(a.partial + static_cast<size_t>(blockIdx.x) * a.d + col, dw[j]);
     }
   }
+  if constexpr (kRing) copy_wait<0>();
   grid_launch_dependents();
 }
 
@@ -307,7 +361,7 @@ __global__ void __launch_bounds__(1024) norm_weight_grad_kernel(const float* par
   grid_dependency_wait();
   float sum = 0.f;
   if (col < d) {
-#pragma unroll 8
+#pragma unroll 16
     for (int p = threadIdx.y; p < parts; p += 32) sum += partial[static_cast<size_t>(p) * d + col];
   }
   share[threadIdx.y][threadIdx.x] = sum;

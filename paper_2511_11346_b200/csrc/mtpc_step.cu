@@ -20,6 +20,7 @@ using namespace mtpc;
 
 constexpr size_t kAlign = 256;
 constexpr int kMaxRows = 1 << 30;
+constexpr long long kClearBesideJoin = 16 << 20;      // bytes
 constexpr int kSms = 148;               // what grids are sized for: the results of sums that are cut by them do not depend on the device
 size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 bool aligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
@@ -52,58 +53,73 @@ template <typename IO>
 void launch_rmsnorm(const NormArgs& a, bool vectors, cudaStream_t st) {
   const int packs = ceil_div(a.d, 8);
   if (vectors && packs <= 32)
-    launch_kernel(residual_rmsnorm_kernel<IO, 8, 1, 256>, ceil_div(a.T, 8), dim3(32, 8), 0, st, true, a);
+    launch_kernel(residual_rmsnorm_kernel<IO, 8, 1, 256, 6>, ceil_div(a.T, 8), dim3(32, 8), 0, st, true, a);
   else if (vectors && packs <= 64)
-    launch_kernel(residual_rmsnorm_kernel<IO, 8, 2, 256>, ceil_div(a.T, 8), dim3(32, 8), 0, st, true, a);
+    launch_kernel(residual_rmsnorm_kernel<IO, 8, 2, 256, 4>, ceil_div(a.T, 8), dim3(32, 8), 0, st, true, a);
   else if (vectors && packs <= 1024)
-    launch_kernel(residual_rmsnorm_kernel<IO, 8, 1, 1024>, a.T, round_warp(packs), 0, st, true, a);
+    launch_kernel(residual_rmsnorm_kernel<IO, 8, 1, 1024, 2>, a.T, round_warp(packs), 0, st, true, a);
   else if (vectors)
-    launch_kernel(residual_rmsnorm_kernel<IO, 8, 4, 1024>, a.T, round_warp(ceil_div(packs, 4)), 0, st, true, a);
+    launch_kernel(residual_rmsnorm_kernel<IO, 8, 4, 1024, 1>, a.T, round_warp(ceil_div(packs, 4)), 0, st, true, a);
   else if (a.d <= 4096)
-    launch_kernel(residual_rmsnorm_kernel<IO, 1, 4, 1024>, a.T, round_warp(ceil_div(a.d, 4)), 0, st, true, a);
+    launch_kernel(residual_rmsnorm_kernel<IO, 1, 4, 1024, 2>, a.T, round_warp(ceil_div(a.d, 4)), 0, st, true, a);
+  else if (a.d <= 8192)
+    launch_kernel(residual_rmsnorm_kernel<IO, 1, 8, 1024, 1>, a.T, round_warp(ceil_div(a.d, 8)), 0, st, true, a);
   else
-    launch_kernel(residual_rmsnorm_kernel<IO, 1, 32, 1024>, a.T, round_warp(ceil_div(a.d, 32)), 0, st, true, a);
+    launch_kernel(residual_rmsnorm_kernel<IO, 1, 32, 1024, 1>, a.T, round_warp(ceil_div(a.d, 32)), 0, st, true, a);
 }
 
-// Blocks of the gradient kernel: as many as give an SM 1024 threads, by what the vector build takes (the sums' order then does not depend on alignment).
+// Blocks of the gradient kernel: as many as give an SM 1024 threads, by what the vector build takes (the order of the sums then does not depend on
+// alignment), of two rows at least where there are rows for every SM.
 int norm_grad_blocks(int T, int d) {
   const int threads = d <= 8192 ? round_warp(ceil_div(d, 8)) : 1024;
   const int per_sm = std::max(1, std::min(16, 1024 / threads));
-  return std::min(T, kSms * per_sm);
+  return std::min(T, std::max(kSms, std::min(kSms * per_sm, T / 2)));
+}
+template <typename IO, typename DY, typename DX, int STAGES, int THREADS, int CTAS>
+bool launch_rmsnorm_grad_ring(const NormGradArgs& a, int blocks, cudaStream_t st) {
+  const int threads = round_warp(ceil_div(a.d, 8));
+  const size_t smem = static_cast<size_t>(STAGES) * norm_grad_thread_bytes<IO, DY, DX>() * threads;
+  auto* kernel = rmsnorm_grad_kernel<IO, DY, DX, 8, 1, STAGES, THREADS, CTAS>;
+  if (smem > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess) return false;
+  launch_kernel(kernel, blocks, threads, smem, st, true, a);
+  return true;
 }
 template <typename IO, typename DY, typename DX>
-void launch_rmsnorm_grad(const NormGradArgs& a, int blocks, bool vectors, cudaStream_t st) {
+bool launch_rmsnorm_grad(const NormGradArgs& a, int blocks, bool vectors, cudaStream_t st) {
   const int packs = ceil_div(a.d, 8);
-  if (vectors && packs <= 1024)
-    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 8, 1>, blocks, round_warp(packs), 0, st, true, a);
-  else if (vectors)
-    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 8, 4>, blocks, round_warp(ceil_div(packs, 4)), 0, st, true, a);
+  if (vectors && packs <= 512) return launch_rmsnorm_grad_ring<IO, DY, DX, 3, 512, 2>(a, blocks, st);
+  if (vectors && packs <= 1024) return launch_rmsnorm_grad_ring<IO, DY, DX, 2, 1024, 1>(a, blocks, st);
+  if (vectors)
+    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 8, 4, 0, 1024, 1>, blocks, round_warp(ceil_div(packs, 4)), 0, st, true, a);
   else if (a.d <= 4096)
-    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 1, 4>, blocks, round_warp(ceil_div(a.d, 4)), 0, st, true, a);
+    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 1, 4, 0, 1024, 1>, blocks, round_warp(ceil_div(a.d, 4)), 0, st, true, a);
   else
-    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 1, 32>, blocks, round_warp(ceil_div(a.d, 32)), 0, st, true, a);
+    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 1, 32, 0, 1024, 1>, blocks, round_warp(ceil_div(a.d, 32)), 0, st, true, a);
+  return true;
 }
 template <typename IO, typename DY>
-void launch_rmsnorm_grad(const NormGradArgs& a, int dx_dtype, int blocks, bool vectors, cudaStream_t st) {
-  if (dx_dtype == MTPC_F32) launch_rmsnorm_grad<IO, DY, float>(a, blocks, vectors, st);
-  else launch_rmsnorm_grad<IO, DY, __nv_bfloat16>(a, blocks, vectors, st);
+bool launch_rmsnorm_grad(const NormGradArgs& a, int dx_dtype, int blocks, bool vectors, cudaStream_t st) {
+  return dx_dtype == MTPC_F32 ? launch_rmsnorm_grad<IO, DY, float>(a, blocks, vectors, st) : launch_rmsnorm_grad<IO, DY, __nv_bfloat16>(a, blocks, vectors, st);
 }
 
 // ---------------------------------------------------------------- embedding
 struct EmbedPlan {
-  int digits, tiles;                    // of the sort
-  int threads, slabs, chunk, chunks;    // of the sums
-  size_t off_key[2], off_pos[2], off_hist, off_part, total;
+  int range;                            // tokens of a block of embed_order_kernel (0: the digits' kernels sort)
+  int digits, rounds, tiles;
+  int chunk, chunks;
+  size_t off_key[2], off_pos[2], off_present, off_hist, off_part, total;
 };
 void plan_embed(int T, int v, int d, EmbedPlan* p) {
+  memset(p, 0, sizeof(*p));
+  // Every block of the one-launch sort reads all tokens, so there are no more of them than run at once, until a block's tokens would be too many.
+  if (T <= kOrderMaxT) p->range = std::min(kOrderMaxRange, ceil_div(v + 1, 2 * kSms));
   int bits = 1;
   while ((static_cast<int64_t>(1) << bits) <= v) ++bits;                // keys run up to v
-  p->digits = (bits + kSortDigit - 1) / kSortDigit;
-  p->tiles = ceil_div(T, kSortTile);
-  // A thread has four columns; the chunks are as many as keep the device busy, of 16 positions at least.
-  p->threads = std::min(kSegmentThreads, round_warp(ceil_div(d, 4)));
-  p->slabs = ceil_div(d, 4 * p->threads);
-  p->chunk = std::max(16, ceil_div(static_cast<long long>(T) * p->slabs, kSms * 8));
+  p->digits = p->range ? 1 : (bits + kSortDigit - 1) / kSortDigit;
+  p->rounds = ceil_div(T, static_cast<long long>(kSortTile) * 1024);
+  p->tiles = ceil_div(T, static_cast<long long>(kSortTile) * p->rounds);
+  // Chunks of 16 positions at least, as many as give the SMs sixteen blocks of 256 columns each.
+  p->chunk = std::max(16, ceil_div(static_cast<long long>(T) * ceil_div(d, 4 * kSegmentThreads), kSms * 16));
   p->chunks = ceil_div(T, p->chunk);
   size_t off = 0;
   auto take = [&](size_t bytes) { size_t o = off; off += align_up(bytes); return o; };
@@ -111,9 +127,26 @@ void plan_embed(int T, int v, int d, EmbedPlan* p) {
     p->off_key[i] = take(i < p->digits ? static_cast<size_t>(T) * 4 : 0);
     p->off_pos[i] = take(i < p->digits ? static_cast<size_t>(T) * 4 : 0);
   }
-  p->off_hist = take(p->tiles > 1 ? static_cast<size_t>(p->tiles) * kSortBins * 4 : 0);
+  p->off_present = take(static_cast<size_t>(v) + 1);
+  p->off_hist = take(p->range ? 0 : static_cast<size_t>(p->tiles) * kSortBins * 4);
   p->off_part = take(static_cast<size_t>(p->chunks) * 2 * d * 4);
   p->total = off;
+}
+
+// The kernels of the sort may use the shared memory that they ask for: said once on each device.
+constexpr int kMaxDevices = 64;
+int g_sort_allowed[kMaxDevices];
+int allow_sort() {
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return MTPC_ERR_CUDA;
+  if (__atomic_load_n(&g_sort_allowed[dev], __ATOMIC_ACQUIRE)) return MTPC_OK;
+  const auto allow = [](auto* kernel, size_t bytes) {
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)) == cudaSuccess;
+  };
+  if (!allow(embed_order_kernel, order_smem_bytes(kOrderMaxT)) || !allow(embed_count_kernel, kSortSmem) || !allow(embed_scatter_kernel, kSortSmem))
+    return MTPC_ERR_CUDA;
+  __atomic_store_n(&g_sort_allowed[dev], 1, __ATOMIC_RELEASE);
+  return MTPC_OK;
 }
 
 int check_embed_sizes(int T, int v, int d) {
@@ -274,39 +307,34 @@ int mtpc_embed_backward(const int32_t* tokens, int32_t T, const void* d_out, int
   if ((rc = check_device()) != MTPC_OK) return rc;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   uint8_t* ws = static_cast<uint8_t*>(workspace);
-
+  if (T == 0)                           // (not accumulated: the gradient is zeros)
+    return cudaMemset2DAsync(d_table, static_cast<size_t>(v == 1 ? d : d_table_stride) * 4, 0, static_cast<size_t>(d) * 4, v, st) == cudaSuccess
+               ? MTPC_OK : MTPC_ERR_CUDA;
+  if ((rc = allow_sort()) != MTPC_OK) return rc;
   EmbedSortArgs s;
   memset(&s, 0, sizeof(s));
   s.tokens = tokens;
-  s.status = out_status;
-  s.d_table = accumulate ? nullptr : d_table;
-  s.d_out = d_out;
-  s.d_table_stride = d_table_stride;
-  s.d_out_stride = d_out_stride;
-  s.T = T;
-  s.v = v;
-  s.d = d;
-  s.digits = p.digits;
-  s.tiles = T > 0 ? p.tiles : 0;
-  s.d_out_bytes = static_cast<int>(element(d_out_dtype));
-  const auto allow = [](auto* kernel) {
-    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSortSmem)) == cudaSuccess;
-  };
-  if (!allow(embed_sort_kernel) || !allow(embed_count_kernel) || !allow(embed_scatter_kernel)) return MTPC_ERR_CUDA;
-  if (T == 0) {                         // (not accumulated: the gradient is zeros)
-    launch_kernel(embed_count_kernel, kSms, kSortThreads, kSortSmem, st, true, s, 0);
-    return check_launch();
-  }
   s.key_a = reinterpret_cast<int*>(ws + p.off_key[0]);
   s.pos_a = reinterpret_cast<int*>(ws + p.off_pos[0]);
   s.key_b = reinterpret_cast<int*>(ws + p.off_key[1]);
   s.pos_b = reinterpret_cast<int*>(ws + p.off_pos[1]);
+  s.present = ws + p.off_present;
   s.hist = reinterpret_cast<int*>(ws + p.off_hist);
-  if (p.tiles == 1) {
-    launch_kernel(embed_sort_kernel, kSms, kSortThreads, kSortSmem, st, true, s);
+  s.status = out_status;
+  s.d_out = d_out;
+  s.d_out_stride = d_out_stride;
+  s.T = T;
+  s.v = v;
+  s.d = d;
+  s.range = p.range;
+  s.digits = p.digits;
+  s.tiles = p.tiles;
+  s.rounds = p.rounds;
+  s.d_out_bytes = static_cast<int>(element(d_out_dtype));
+  if (p.range) {
+    launch_kernel(embed_order_kernel, ceil_div(v + 1, p.range), kOrderThreads, order_smem_bytes(T), st, true, s);
   } else {
     for (int digit = 0; digit < p.digits; ++digit) {
-      // the first pass over the tokens also clears and prefetches
       launch_kernel(embed_count_kernel, p.tiles + (digit == 0 ? kSms : 0), kSortThreads, kSortSmem, st, true, s, digit);
       launch_kernel(embed_scan_kernel, 1, kSortThreads, 0, st, true, s.hist, p.tiles * kSortBins);
       launch_kernel(embed_scatter_kernel, p.tiles, kSortThreads, kSortSmem, st, true, s, digit);
@@ -316,6 +344,7 @@ int mtpc_embed_backward(const int32_t* tokens, int32_t T, const void* d_out, int
   memset(&a, 0, sizeof(a));
   a.key = s.key_a;
   a.pos = s.pos_a;
+  a.present = s.present;
   a.d_out = d_out;
   a.d_table = d_table;
   a.part = reinterpret_cast<float*>(ws + p.off_part);
@@ -328,15 +357,34 @@ int mtpc_embed_backward(const int32_t* tokens, int32_t T, const void* d_out, int
   a.chunks = p.chunks;
   a.scale = scale;
   a.accumulate = accumulate != 0;
-  const bool vectors = d % 4 == 0 && rows_allow(d_out, d_out_stride, element(d_out_dtype), 4, T) && rows_allow(d_table, d_table_stride, 4, 4, v);
-  const int vec = vectors ? 4 : 1;
-  const dim3 grid(ceil_div(d, p.threads * vec), p.chunks);
+  a.wide_rows = d % 4 == 0 && rows_allow(d_table, d_table_stride, 4, 4, v);
+  const auto vectors = [&](int vec) {
+    return d % vec == 0 && rows_allow(d_out, d_out_stride, element(d_out_dtype), vec, T) && rows_allow(d_table, d_table_stride, 4, vec, v);
+  };
+  // Rows without positions: nearly all beside the chunks, as much as the join takes anyway (3 us of writing) beside the join.
+  const bool join = p.chunks > 1;
+  const int beside_join = join ? static_cast<int>(std::min<long long>(v / 4, kClearBesideJoin / (static_cast<long long>(d) * 4))) : 0;
+  const auto clear_blocks = [&](int warps_per_block) {
+    const int groups = ceil_div(a.clear_end - a.clear_begin, kClearRows);
+    return std::min(ceil_div(groups, warps_per_block), kSms * 64 / warps_per_block);
+  };
+  a.clear_end = accumulate ? 0 : v - beside_join;
+  const int vec = d_out_dtype == MTPC_BF16 && vectors(8) ? 8 : vectors(4) ? 4 : 1;
+  a.slabs = ceil_div(d, kSegmentThreads * vec);
+  const int blocks = p.chunks * a.slabs + clear_blocks(kSegmentThreads / 32);
   if (d_out_dtype == MTPC_F32)
-    launch_kernel(vectors ? embed_segment_kernel<float, 4, 8> : embed_segment_kernel<float, 1, 8>, grid, p.threads, 0, st, true, a);
+    launch_kernel(vec == 4 ? embed_segment_kernel<float, 4, 8> : embed_segment_kernel<float, 1, 8>, blocks, kSegmentThreads, 0, st, true, a);
   else
-    launch_kernel(vectors ? embed_segment_kernel<__nv_bfloat16, 4, 8> : embed_segment_kernel<__nv_bfloat16, 1, 8>, grid, p.threads, 0, st, true, a);
-  if (p.chunks > 1)
-    launch_kernel(vectors ? embed_join_kernel<4> : embed_join_kernel<1>, dim3(ceil_div(d, 32 * vec), p.chunks), 256, 0, st, true, a);
+    launch_kernel(vec == 8 ? embed_segment_kernel<__nv_bfloat16, 8, 4> : vec == 4 ? embed_segment_kernel<__nv_bfloat16, 4, 8>
+                                                                                   : embed_segment_kernel<__nv_bfloat16, 1, 8>,
+                  blocks, kSegmentThreads, 0, st, true, a);
+  if (join) {
+    a.clear_begin = a.clear_end;
+    a.clear_end = accumulate ? 0 : v;
+    const int join_vec = vec == 1 ? 1 : 4;
+    launch_kernel(join_vec == 4 ? embed_join_kernel<4> : embed_join_kernel<1>,
+                  ceil_div(p.chunks, kJoinWarps) * ceil_div(d, 32 * join_vec) + clear_blocks(kJoinWarps), 32 * kJoinWarps, 0, st, true, a);
+  }
   return check_launch();
 }
 
@@ -436,12 +484,16 @@ int mtpc_residual_rmsnorm_backward(const void* sum, int64_t sum_stride, int32_t 
     const bool vectors = d % 8 == 0 && rows_allow(sum, sum_stride, element(io_dtype), 8, T) && rows_allow(weight, 0, element(weight_dtype), 8, 1) &&
                          rows_allow(d_out, d_out_stride, element(d_out_dtype), 8, T) &&
                          rows_allow(d_sum, d_sum_stride, element(d_x_dtype), 8, T) && rows_allow(d_x, d_x_stride, element(d_x_dtype), 8, T);
-    if (io_dtype == MTPC_F32) {
-      if (d_out_dtype == MTPC_F32) launch_rmsnorm_grad<float, float>(a, d_x_dtype, blocks, vectors, st);
-      else launch_rmsnorm_grad<float, __nv_bfloat16>(a, d_x_dtype, blocks, vectors, st);
-    } else {
-      if (d_out_dtype == MTPC_F32) launch_rmsnorm_grad<__nv_bfloat16, float>(a, d_x_dtype, blocks, vectors, st);
-      else launch_rmsnorm_grad<__nv_bfloat16, __nv_bfloat16>(a, d_x_dtype, blocks, vectors, st);
+    bool ok;
+    if (io_dtype == MTPC_F32)
+      ok = d_out_dtype == MTPC_F32 ? launch_rmsnorm_grad<float, float>(a, d_x_dtype, blocks, vectors, st)
+                                   : launch_rmsnorm_grad<float, __nv_bfloat16>(a, d_x_dtype, blocks, vectors, st);
+    else
+      ok = d_out_dtype == MTPC_F32 ? launch_rmsnorm_grad<__nv_bfloat16, float>(a, d_x_dtype, blocks, vectors, st)
+                                   : launch_rmsnorm_grad<__nv_bfloat16, __nv_bfloat16>(a, d_x_dtype, blocks, vectors, st);
+    if (!ok) {
+      cudaGetLastError();
+      return MTPC_ERR_CUDA;
     }
   }
   if (d_weight)
