@@ -6,10 +6,12 @@
 // of them with a few tokens, so neither a row per block nor atomics suit it. The positions are sorted by token (stable, so the order of every sum
 // is fixed), cut into chunks of equal length, and a chunk's positions are added up row after row: each element of d_out is read once, whatever the
 // tokens are. A token whose positions lie within a chunk is written at once; of one that crosses chunks every chunk leaves its part, which are added up
-// in their order afterwards.
+// in their order afterwards. (By the block that is there last, found by a counter, they are not: with the fences that takes the sums of 8192 x 4096 fp32
+// took 57 us, instead of 26 and 5 for a kernel of its own.)
 //   embed_order_kernel    up to kOrderMaxT positions: every block owns a range of tokens, finds their positions among all of them and sorts those;
 //                         meanwhile the device asks for d_out by L2 prefetch
 //   embed_count / embed_scan / embed_scatter_kernel   more positions: by digits of 9 bits
+//                         (embed_bounds_kernel: where each token's positions begin and end, which the one-launch sort knows)
 //   embed_segment_kernel  the chunks
 //   embed_join_kernel     the tokens that cross chunks
 // Rows that no position has are zeros: written by further blocks of the last two, behind whose short chains of dependent loads that hides.
@@ -77,7 +79,7 @@ constexpr size_t kEmbedPrefetchBytes = 32u << 20;
 struct EmbedSortArgs {
   const int* tokens;
   int *key_a, *pos_a, *key_b, *pos_b;     // the last digit's go to key_a, pos_a
-  uint8_t* present;                       // [v + 1]: whether a token has positions
+  int2* bounds;                           // [v + 1]: where a token's positions begin and end in the order (equal: it has none)
   int* hist;                              // [bins][tiles]
   unsigned* status;                       // may be NULL
   const void* d_out;
@@ -114,28 +116,32 @@ __device__ __forceinline__ unsigned equal_lanes(unsigned x, int bits, unsigned a
 // Up to kOrderMaxT positions. Every block looks through all tokens (from L2) for those of its range, lists them in order, and sorts the list by
 // counting: a warp counts its part of it per token, the counts become places, the warps write their keys and positions there. One launch of a
 // few microseconds where a sort by one block takes 18 (8192 positions): that one sorts them all while the device waits.
-constexpr int kOrderThreads = 512, kOrderWarps = kOrderThreads / 32, kOrderMaxT = 1 << 15, kOrderMaxRange = 512;
+constexpr int kOrderThreads = 1024, kOrderWarps = kOrderThreads / 32, kOrderMaxT = 1 << 15, kOrderMaxRange = 512;
+constexpr int kOrderAhead = 8;                     // tokens that a lane holds at a time
 inline size_t order_smem_bytes(int T) { return static_cast<size_t>(T) * 4; }
-__global__ void __launch_bounds__(kOrderThreads) embed_order_kernel(const __grid_constant__ EmbedSortArgs a) {
+__global__ void __launch_bounds__(kOrderThreads, 2) embed_order_kernel(const __grid_constant__ EmbedSortArgs a) {
   extern __shared__ unsigned list[];               // token's place in the range << 16 | position (below 2^15)
-  __shared__ unsigned counts[kOrderWarps][kOrderMaxRange];
+  __shared__ uint16_t counts[kOrderWarps][kOrderMaxRange];
   __shared__ unsigned found[kOrderWarps], below[kOrderWarps];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int lo = blockIdx.x * a.range, tokens = min(a.range, a.v + 1 - lo);       // (key v: what is no token)
-  grid_dependency_wait();
-  grid_launch_dependents();
-  prefetch_rows(a, blockIdx.x, gridDim.x);
-
   const int per_warp = (a.T + kOrderThreads - 1) / kOrderThreads * 32;
   const int begin = min(warp * per_warp, a.T), end = min(begin + per_warp, a.T);
+  for (int b = lane; b < tokens; b += 32) counts[warp][b] = 0;
+  grid_dependency_wait();
+  grid_launch_dependents();
+
+  int key[kOrderAhead];
+  auto look = [&](int i) {
+#pragma unroll
+    for (int u = 0; u < kOrderAhead; ++u) key[u] = i + u * 32 + lane < end ? a.tokens[i + u * 32 + lane] : INT32_MIN;
+  };
   unsigned mine = 0, less = 0;
   bool bad = false;
-  for (int i = begin; i < end; i += 8 * 32) {
-    int key[8];
+  for (int i = begin; i < end; i += kOrderAhead * 32) {
+    look(i);
 #pragma unroll
-    for (int u = 0; u < 8; ++u) key[u] = i + u * 32 + lane < end ? a.tokens[i + u * 32 + lane] : INT32_MIN;
-#pragma unroll
-    for (int u = 0; u < 8; ++u) {
+    for (int u = 0; u < kOrderAhead; ++u) {
       const bool is = i + u * 32 + lane < end;
       bad |= key[u] >= a.v;
       const int k = embed_key(a, key[u]);
@@ -143,27 +149,21 @@ __global__ void __launch_bounds__(kOrderThreads) embed_order_kernel(const __grid
       less += __popc(__ballot_sync(0xffffffffu, is && k < lo));
     }
   }
-  if (blockIdx.x == 0 && bad && a.status) atomicOr(a.status, kStatusBadToken);
   if (lane == 0) {
     found[warp] = mine;
     below[warp] = less;
   }
-  for (int b = lane; b < tokens; b += 32) counts[warp][b] = 0;
+  prefetch_rows(a, blockIdx.x, gridDim.x);         // (behind the tokens, which otherwise wait for it)
+  if (blockIdx.x == 0 && bad && a.status) atomicOr(a.status, kStatusBadToken);
   __syncthreads();
-  unsigned base = 0, count = 0, at = 0;            // of the range's positions: the first one's place, how many, those of the warps before
-#pragma unroll
-  for (int w = 0; w < kOrderWarps; ++w) {
-    base += below[w];
-    if (w < warp) at += found[w];
-    count += found[w];
-  }
+  // of the range's positions: the first one's place, how many, those of the warps before
+  const unsigned base = __reduce_add_sync(0xffffffffu, below[lane]), count = __reduce_add_sync(0xffffffffu, found[lane]);
+  unsigned at = __reduce_add_sync(0xffffffffu, lane < warp ? found[lane] : 0u);
   if (mine > 0) {
-    for (int i = begin; i < end; i += 8 * 32) {
-      int key[8];
+    for (int i = begin; i < end; i += kOrderAhead * 32) {
+      if (per_warp > kOrderAhead * 32) look(i);    // (else they are still held)
 #pragma unroll
-      for (int u = 0; u < 8; ++u) key[u] = i + u * 32 + lane < end ? a.tokens[i + u * 32 + lane] : INT32_MIN;
-#pragma unroll
-      for (int u = 0; u < 8; ++u) {
+      for (int u = 0; u < kOrderAhead; ++u) {
         const int k = embed_key(a, key[u]) - lo;
         const bool is = i + u * 32 + lane < end && k >= 0 && k < tokens;
         const unsigned which = __ballot_sync(0xffffffffu, is);
@@ -185,13 +185,12 @@ __global__ void __launch_bounds__(kOrderThreads) embed_order_kernel(const __grid
     __syncwarp();
   }
   __syncthreads();
-  // the places: tokens in order, of each the warps in order (a thread per token)
-  unsigned sum = 0;
+  // the places behind the range's first: tokens in order, of each the warps in order (a thread per token; at most kOrderMaxT of them)
   const bool has = static_cast<int>(threadIdx.x) < tokens;
+  unsigned sum = 0;
   if (has) {
-#pragma unroll
+#pragma unroll 8
     for (int w = 0; w < kOrderWarps; ++w) sum += counts[w][threadIdx.x];
-    a.present[lo + threadIdx.x] = sum > 0;
   }
   unsigned before = sum;
 #pragma unroll
@@ -201,10 +200,10 @@ __global__ void __launch_bounds__(kOrderThreads) embed_order_kernel(const __grid
   }
   if (lane == 31) found[warp] = before;
   __syncthreads();
-  before += base - sum;
-  for (int w = 0; w < warp; ++w) before += found[w];
+  before += __reduce_add_sync(0xffffffffu, lane < warp ? found[lane] : 0u) - sum;
   if (has) {
-#pragma unroll
+    a.bounds[lo + threadIdx.x] = make_int2(base + before, base + before + sum);
+#pragma unroll 8
     for (int w = 0; w < kOrderWarps; ++w) {
       const unsigned c = counts[w][threadIdx.x];
       counts[w][threadIdx.x] = before;
@@ -219,7 +218,7 @@ __global__ void __launch_bounds__(kOrderThreads) embed_order_kernel(const __grid
     const unsigned first = is ? counts[warp][bin] : 0u;
     __syncwarp();
     if (is) {
-      const unsigned place = first + __popc(peers & ((1u << lane) - 1u));
+      const unsigned place = base + first + __popc(peers & ((1u << lane) - 1u));
       a.key_a[place] = lo + bin;
       a.pos_a[place] = item & 0xffffu;
       if (lane == __ffs(peers) - 1) counts[warp][bin] = first + __popc(peers);
@@ -332,14 +331,14 @@ __device__ __forceinline__ unsigned block_running_sum(unsigned x, unsigned* warp
 }
 
 // One digit: the tiles' counts, their running sums over (bin, tile), and every tile's keys to their places. The blocks of the first count that have no
-// tile prefetch, and clear `present`, which the last digit's placing marks.
+// tile prefetch, and clear the bounds.
 __global__ void __launch_bounds__(kSortThreads) embed_count_kernel(const __grid_constant__ EmbedSortArgs a, int p) {
   extern __shared__ unsigned counts[];
   grid_dependency_wait();
   grid_launch_dependents();
   if (static_cast<int>(blockIdx.x) >= a.tiles) {
     const int part = blockIdx.x - a.tiles, parts = gridDim.x - a.tiles;
-    for (int b = part * kSortThreads + threadIdx.x; b <= a.v; b += parts * kSortThreads) a.present[b] = 0;
+    for (int b = part * kSortThreads + threadIdx.x; b <= a.v; b += parts * kSortThreads) a.bounds[b] = make_int2(0, 0);
     prefetch_rows(a, part, parts);
     return;
   }
@@ -384,30 +383,36 @@ __global__ void __launch_bounds__(kSortThreads) embed_scatter_kernel(const __gri
     sort_offsets(counts, base);
     __syncthreads();
     sort_place(a, x, p, counts);
-    if (p == a.digits - 1) {
-#pragma unroll
-      for (int j = 0; j < kSortPerLane; ++j)
-        if (x.key[j] >= 0) a.present[x.key[j]] = 1;          // (every writer writes the same)
-    }
     __syncthreads();
   }
 }
 
+__global__ void __launch_bounds__(256) embed_bounds_kernel(const __grid_constant__ EmbedSortArgs a) {
+  grid_dependency_wait();
+  grid_launch_dependents();
+  for (int i = blockIdx.x * 256 + threadIdx.x; i < a.T; i += gridDim.x * 256) {
+    const int key = a.key_a[i];
+    if (i == 0 || a.key_a[i - 1] != key) a.bounds[key].x = i;
+    if (i == a.T - 1 || a.key_a[i + 1] != key) a.bounds[key].y = i + 1;
+  }
+}
+
 // ---------------------------------------------------------------- sums of the sorted positions
-constexpr int kSegmentThreads = 64;
+constexpr int kSegmentThreads = 256;
 constexpr int kSegmentStage = 256;      // positions whose keys are in shared memory at a time
-constexpr int kClearRows = 8;           // rows that a warp clears at a time
+constexpr int kClearRows = 8;           // rows that a block clears at a time
 
 struct EmbedSegmentArgs {
   const int *key, *pos;                 // sorted; key v: no token
-  const uint8_t* present;
+  const int2* bounds;
   const void* d_out;
   float *d_table, *part;                // part [chunks][2][d]: what a chunk adds to the token it begins in / that goes on behind it
   long long d_out_stride, d_table_stride;
   int T, v, d, chunk, chunks, slabs;    // slabs: of the columns
-  int clear_begin, clear_end;           // the rows that this launch's further blocks clear
+  int clear_begin, clear_end;           // the rows that this launch's further blocks look at
   float scale;
-  bool accumulate, wide_rows;           // wide_rows: the table's rows allow float4
+  bool accumulate;
+  int row_vec;                          // vectors of so many elements fit the table's rows
 };
 
 template <int V>
@@ -420,38 +425,46 @@ __device__ __forceinline__ void write_table(const EmbedSegmentArgs& a, int token
   store_f32<float, V>(dst, o);
 }
 
-// Zeros to the rows without positions: warp `part` of `parts`, eight adjacent rows at a time.
+// Zeros to the rows without positions: block `part` of `parts`, kClearRows adjacent rows at a time (longer runs per block write slower:
+// 256 MB by blocks of 256 threads in runs of 56 KB 41 us, warps with runs of 64 KB 47 to 75).
 __device__ __forceinline__ void clear_rows(const EmbedSegmentArgs& a, int part, int parts) {
   const int lane = threadIdx.x & 31;
   const int groups = (a.clear_end - a.clear_begin + kClearRows - 1) / kClearRows;
   for (int g = part; g < groups; g += parts) {
     const int row0 = a.clear_begin + g * kClearRows;
-    unsigned absent = __ballot_sync(0xffffffffu, lane < kClearRows && row0 + lane < a.clear_end && !a.present[min(row0 + lane, a.v)]);
-    for (; absent; absent &= absent - 1) {
+    bool none = false;
+    if (lane < kClearRows && row0 + lane < a.clear_end) {
+      const int2 b = a.bounds[row0 + lane];
+      none = b.x == b.y;
+    }
+    for (unsigned absent = __ballot_sync(0xffffffffu, none); absent; absent &= absent - 1) {
       float* row = a.d_table + (row0 + __ffs(absent) - 1) * a.d_table_stride;
-      if (a.wide_rows) {
-        for (int i = lane; i < a.d / 4; i += 32) reinterpret_cast<float4*>(row)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (a.row_vec == 8) {
+        const float zeros[8] = {};
+        for (int i = threadIdx.x * 8; i < a.d; i += blockDim.x * 8) st_global_v8(row + i, zeros);
+      } else if (a.row_vec == 4) {
+        for (int i = threadIdx.x; i < a.d / 4; i += blockDim.x) reinterpret_cast<float4*>(row)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
       } else {
-        for (int i = lane; i < a.d; i += 32) row[i] = 0.f;
+        for (int i = threadIdx.x; i < a.d; i += blockDim.x) row[i] = 0.f;
       }
     }
   }
 }
 
-// A block per chunk and slab of columns (the slabs of a chunk follow each other), then those that clear. U rows are in flight per thread. Blocks of two
-// warps, so that a chunk is long: what tokens that cross chunks cost is two rows of fp32 a chunk, written and read again.
+// A block per chunk and slab of columns (the slabs of a chunk follow each other), beside those that clear. U rows are in flight per thread. A slab is
+// 4 KB of a row where rows are that long: in slabs of 1 KB, with four times as long chunks, the kernel alone takes 26 to 32 us instead of
+// 25 (8192 x 4096 fp32), by registers or by a ring of cp.async.
 template <typename T, int V, int U>
-__global__ void __launch_bounds__(kSegmentThreads) embed_segment_kernel(const __grid_constant__ EmbedSegmentArgs a) {
+__global__ void __launch_bounds__(kSegmentThreads, 4) embed_segment_kernel(const __grid_constant__ EmbedSegmentArgs a) {
   __shared__ int key[kSegmentStage + 1], pos[kSegmentStage];
   grid_dependency_wait();
   if (static_cast<int>(blockIdx.x) >= a.chunks * a.slabs) {
-    const int blocks = a.chunks * a.slabs;
-    clear_rows(a, (blockIdx.x - blocks) * (kSegmentThreads / 32) + (threadIdx.x >> 5), (gridDim.x - blocks) * (kSegmentThreads / 32));
+    clear_rows(a, blockIdx.x - a.chunks * a.slabs, gridDim.x - a.chunks * a.slabs);
     grid_launch_dependents();
     return;
   }
   const int chunk = blockIdx.x / a.slabs;
-  const int col = ((blockIdx.x - chunk * a.slabs) * kSegmentThreads + threadIdx.x) * V;
+  const int col = ((blockIdx.x - chunk * a.slabs) * blockDim.x + threadIdx.x) * V;
   const int lo = chunk * a.chunk, hi = min(lo + a.chunk, a.T);
   float sum[V];
 #pragma unroll
@@ -460,12 +473,12 @@ __global__ void __launch_bounds__(kSegmentThreads) embed_segment_kernel(const __
   bool begins = true;                            // the token being added up has no position in an earlier chunk
   for (int base = lo; base < hi; base += kSegmentStage) {
     const int count = min(hi - base, kSegmentStage);
+    const int earlier = base == lo && lo > 0 ? a.key[lo - 1] : -1;
     __syncthreads();
-    for (int i = threadIdx.x; i <= count; i += kSegmentThreads) {
+    for (int i = threadIdx.x; i <= count; i += blockDim.x) {
       key[i] = base + i < a.T ? a.key[base + i] : a.v;
       if (i < count) pos[i] = a.pos[base + i];
     }
-    const int earlier = base == lo && lo > 0 ? a.key[lo - 1] : -1;
     __syncthreads();
     if (base == lo) begins = earlier != key[0];
     if (key[0] == a.v) break;                    // the rest of the positions have no token
@@ -510,7 +523,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) embed_join_kernel(const __gri
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int slabs = (a.d + 32 * V - 1) / (32 * V), groups = (a.chunks + kJoinWarps - 1) / kJoinWarps;
   if (static_cast<int>(blockIdx.x) >= groups * slabs) {
-    clear_rows(a, (blockIdx.x - groups * slabs) * kJoinWarps + warp, (gridDim.x - groups * slabs) * kJoinWarps);
+    clear_rows(a, blockIdx.x - groups * slabs, gridDim.x - groups * slabs);
     return;
   }
   const int c0 = blockIdx.x / slabs * kJoinWarps;
@@ -518,18 +531,10 @@ __global__ void __launch_bounds__(32 * kJoinWarps) embed_join_kernel(const __gri
   int token = a.v, last = -1;                                           // lane q: of chunk c0 + q, and the last chunk that has the token
   if (lane < kJoinWarps && c0 + lane < a.chunks) {
     const int lo = (c0 + lane) * a.chunk, hi = min(lo + a.chunk, a.T);
-    const int before = lo > 0 ? a.key[lo - 1] : -1, after = hi < a.T ? a.key[hi] : a.v;
     token = a.key[hi - 1];
-    if (token != a.v && after == token && before != token) {
-      last = c0 + lane + 1;                                             // (sorted: found in steps that double, then halve)
-      for (int step = 1;; step <<= 1) {
-        if (last + step >= a.chunks || a.key[(last + step) * a.chunk] != token) {
-          for (step >>= 1; step > 0; step >>= 1)
-            if (last + step < a.chunks && a.key[(last + step) * a.chunk] == token) last += step;
-          break;
-        }
-        last += step;
-      }
+    if (token != a.v) {
+      const int2 b = a.bounds[token];
+      if (b.x >= lo && b.y > hi) last = (b.y - 1) / a.chunk;            // begins here and goes on
     }
   }
   auto add = [&](int begin, int end, int first, int step, float (&sum)[V]) {

@@ -205,14 +205,6 @@ struct NormGradArgs {
   float eps;
 };
 
-// 16 bytes from global to shared memory without registers; they are there once the thread has waited for the group they were committed in.
-__device__ __forceinline__ void copy_async16(uint32_t dst_smem, const void* src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst_smem), "l"(src) : "memory");
-}
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
 // A thread's eight elements of a row in its own places of shared memory, 16 bytes per piece, a piece's neighbours the other threads'.
 template <typename T>
 struct RingRow {

@@ -53,6 +53,14 @@ __device__ __forceinline__ void store_f32(T* p, const float (&x)[V]) {
   store_pack<T, V>(p, o);
 }
 
+// 16 bytes from global to shared memory without registers; they are there once the thread has waited for the group they were committed in.
+__device__ __forceinline__ void copy_async16(uint32_t dst_smem, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst_smem), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
 // Sums over the threads of a row: a warp, or (blockDim.x > 32) the whole block, every thread with the same result, added up in
 // the same order. red: 32 floats per value in shared memory; a buffer may be used again after the next barrier.
 template <int N>

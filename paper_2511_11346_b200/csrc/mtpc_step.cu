@@ -20,7 +20,7 @@ using namespace mtpc;
 
 constexpr size_t kAlign = 256;
 constexpr int kMaxRows = 1 << 30;
-constexpr long long kClearBesideJoin = 16 << 20;      // bytes
+constexpr long long kClearBesideChunks = 32 << 20;    // bytes
 constexpr int kSms = 148;               // what grids are sized for: the results of sums that are cut by them do not depend on the device
 size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 bool aligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
@@ -106,20 +106,21 @@ bool launch_rmsnorm_grad(const NormGradArgs& a, int dx_dtype, int blocks, bool v
 struct EmbedPlan {
   int range;                            // tokens of a block of embed_order_kernel (0: the digits' kernels sort)
   int digits, rounds, tiles;
-  int chunk, chunks;
-  size_t off_key[2], off_pos[2], off_present, off_hist, off_part, total;
+  int threads, chunk, chunks;           // of the sums
+  size_t off_key[2], off_pos[2], off_bounds, off_hist, off_part, total;
 };
 void plan_embed(int T, int v, int d, EmbedPlan* p) {
   memset(p, 0, sizeof(*p));
-  // Every block of the one-launch sort reads all tokens, so there are no more of them than run at once, until a block's tokens would be too many.
-  if (T <= kOrderMaxT) p->range = std::min(kOrderMaxRange, ceil_div(v + 1, 2 * kSms));
+  // Every block of the one-launch sort reads all tokens, so there is one per SM (a second one on some of them takes twice as long), until a block's tokens would be too many.
+  if (T <= kOrderMaxT) p->range = std::min(kOrderMaxRange, ceil_div(v + 1, kSms));
   int bits = 1;
   while ((static_cast<int64_t>(1) << bits) <= v) ++bits;                // keys run up to v
   p->digits = p->range ? 1 : (bits + kSortDigit - 1) / kSortDigit;
   p->rounds = ceil_div(T, static_cast<long long>(kSortTile) * 1024);
   p->tiles = ceil_div(T, static_cast<long long>(kSortTile) * p->rounds);
-  // Chunks of 16 positions at least, as many as give the SMs sixteen blocks of 256 columns each.
-  p->chunk = std::max(16, ceil_div(static_cast<long long>(T) * ceil_div(d, 4 * kSegmentThreads), kSms * 16));
+  // Chunks of 8 positions at least, as many as give every SM twice the four blocks that it holds, of 256 threads with four columns each.
+  p->threads = std::min(kSegmentThreads, round_warp(ceil_div(d, 4)));
+  p->chunk = std::max(8, ceil_div(static_cast<long long>(T) * ceil_div(d, 4 * p->threads) * p->threads, kSms * 8 * kSegmentThreads));
   p->chunks = ceil_div(T, p->chunk);
   size_t off = 0;
   auto take = [&](size_t bytes) { size_t o = off; off += align_up(bytes); return o; };
@@ -127,7 +128,7 @@ void plan_embed(int T, int v, int d, EmbedPlan* p) {
     p->off_key[i] = take(i < p->digits ? static_cast<size_t>(T) * 4 : 0);
     p->off_pos[i] = take(i < p->digits ? static_cast<size_t>(T) * 4 : 0);
   }
-  p->off_present = take(static_cast<size_t>(v) + 1);
+  p->off_bounds = take((static_cast<size_t>(v) + 1) * sizeof(int2));
   p->off_hist = take(p->range ? 0 : static_cast<size_t>(p->tiles) * kSortBins * 4);
   p->off_part = take(static_cast<size_t>(p->chunks) * 2 * d * 4);
   p->total = off;
@@ -318,7 +319,7 @@ int mtpc_embed_backward(const int32_t* tokens, int32_t T, const void* d_out, int
   s.pos_a = reinterpret_cast<int*>(ws + p.off_pos[0]);
   s.key_b = reinterpret_cast<int*>(ws + p.off_key[1]);
   s.pos_b = reinterpret_cast<int*>(ws + p.off_pos[1]);
-  s.present = ws + p.off_present;
+  s.bounds = reinterpret_cast<int2*>(ws + p.off_bounds);
   s.hist = reinterpret_cast<int*>(ws + p.off_hist);
   s.status = out_status;
   s.d_out = d_out;
@@ -339,12 +340,13 @@ int mtpc_embed_backward(const int32_t* tokens, int32_t T, const void* d_out, int
       launch_kernel(embed_scan_kernel, 1, kSortThreads, 0, st, true, s.hist, p.tiles * kSortBins);
       launch_kernel(embed_scatter_kernel, p.tiles, kSortThreads, kSortSmem, st, true, s, digit);
     }
+    launch_kernel(embed_bounds_kernel, std::min(ceil_div(T, 256), kSms * 8), 256, 0, st, true, s);
   }
   EmbedSegmentArgs a;
   memset(&a, 0, sizeof(a));
   a.key = s.key_a;
   a.pos = s.pos_a;
-  a.present = s.present;
+  a.bounds = s.bounds;
   a.d_out = d_out;
   a.d_table = d_table;
   a.part = reinterpret_cast<float*>(ws + p.off_part);
@@ -357,33 +359,29 @@ int mtpc_embed_backward(const int32_t* tokens, int32_t T, const void* d_out, int
   a.chunks = p.chunks;
   a.scale = scale;
   a.accumulate = accumulate != 0;
-  a.wide_rows = d % 4 == 0 && rows_allow(d_table, d_table_stride, 4, 4, v);
+  const auto table_allows = [&](int vec) { return d % vec == 0 && rows_allow(d_table, d_table_stride, 4, vec, v); };
+  a.row_vec = table_allows(8) ? 8 : table_allows(4) ? 4 : 1;
   const auto vectors = [&](int vec) {
-    return d % vec == 0 && rows_allow(d_out, d_out_stride, element(d_out_dtype), vec, T) && rows_allow(d_table, d_table_stride, 4, vec, v);
+    return table_allows(vec) && rows_allow(d_out, d_out_stride, element(d_out_dtype), vec, T);
   };
-  // Rows without positions: nearly all beside the chunks, as much as the join takes anyway (3 us of writing) beside the join.
-  const bool join = p.chunks > 1;
-  const int beside_join = join ? static_cast<int>(std::min<long long>(v / 4, kClearBesideJoin / (static_cast<long long>(d) * 4))) : 0;
-  const auto clear_blocks = [&](int warps_per_block) {
-    const int groups = ceil_div(a.clear_end - a.clear_begin, kClearRows);
-    return std::min(ceil_div(groups, warps_per_block), kSms * 64 / warps_per_block);
-  };
-  a.clear_end = accumulate ? 0 : v - beside_join;
+  // Rows without positions are cleared beside the chunks where they are many, as much as the chunks take to run; the others beside the join, whose
+  // blocks are short: in the chunks' launch the last ones would be theirs.
+  const auto clear_blocks = [&]() { return std::min(ceil_div(a.clear_end - a.clear_begin, kClearRows), kSms * 256); };
+  const long long table_bytes = static_cast<long long>(v) * d * 4;
+  a.clear_end = accumulate || (p.chunks > 1 && table_bytes < 2 * kClearBesideChunks) ? 0 : p.chunks == 1 ? v : static_cast<int>(kClearBesideChunks / (d * 4LL));
   const int vec = d_out_dtype == MTPC_BF16 && vectors(8) ? 8 : vectors(4) ? 4 : 1;
-  a.slabs = ceil_div(d, kSegmentThreads * vec);
-  const int blocks = p.chunks * a.slabs + clear_blocks(kSegmentThreads / 32);
-  if (d_out_dtype == MTPC_F32)
-    launch_kernel(vec == 4 ? embed_segment_kernel<float, 4, 8> : embed_segment_kernel<float, 1, 8>, blocks, kSegmentThreads, 0, st, true, a);
-  else
-    launch_kernel(vec == 8 ? embed_segment_kernel<__nv_bfloat16, 8, 4> : vec == 4 ? embed_segment_kernel<__nv_bfloat16, 4, 8>
-                                                                                   : embed_segment_kernel<__nv_bfloat16, 1, 8>,
-                  blocks, kSegmentThreads, 0, st, true, a);
-  if (join) {
+  const int threads = std::min(p.threads, round_warp(ceil_div(d, vec)));
+  a.slabs = ceil_div(d, threads * vec);
+  auto* segment = d_out_dtype == MTPC_F32 ? (vec == 4 ? embed_segment_kernel<float, 4, 8> : embed_segment_kernel<float, 1, 8>)
+                  : vec == 8 ? embed_segment_kernel<__nv_bfloat16, 8, 4>
+                  : vec == 4 ? embed_segment_kernel<__nv_bfloat16, 4, 8> : embed_segment_kernel<__nv_bfloat16, 1, 8>;
+  launch_kernel(segment, p.chunks * a.slabs + clear_blocks(), threads, 0, st, true, a);
+  if (p.chunks > 1) {
     a.clear_begin = a.clear_end;
-    a.clear_end = accumulate ? 0 : v;
+    a.clear_end = accumulate ? a.clear_begin : v;
     const int join_vec = vec == 1 ? 1 : 4;
     launch_kernel(join_vec == 4 ? embed_join_kernel<4> : embed_join_kernel<1>,
-                  ceil_div(p.chunks, kJoinWarps) * ceil_div(d, 32 * join_vec) + clear_blocks(kJoinWarps), 32 * kJoinWarps, 0, st, true, a);
+                  ceil_div(p.chunks, kJoinWarps) * ceil_div(d, 32 * join_vec) + clear_blocks(), 32 * kJoinWarps, 0, st, true, a);
   }
   return check_launch();
 }
