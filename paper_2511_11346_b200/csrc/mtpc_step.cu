@@ -118,9 +118,9 @@ void plan_embed(int T, int v, int d, EmbedPlan* p) {
   p->digits = p->range ? 1 : (bits + kSortDigit - 1) / kSortDigit;
   p->rounds = ceil_div(T, static_cast<long long>(kSortTile) * 1024);
   p->tiles = ceil_div(T, static_cast<long long>(kSortTile) * p->rounds);
-  // Chunks of 8 positions at least, as many as give every SM twice the four blocks that it holds, of 256 threads with four columns each.
+  // Chunks of 8 positions at least, as many as give every SM the four blocks that it holds, of 256 threads with four columns each.
   p->threads = std::min(kSegmentThreads, round_warp(ceil_div(d, 4)));
-  p->chunk = std::max(8, ceil_div(static_cast<long long>(T) * ceil_div(d, 4 * p->threads) * p->threads, kSms * 8 * kSegmentThreads));
+  p->chunk = std::max(8, ceil_div(static_cast<long long>(T) * ceil_div(d, 4 * p->threads) * p->threads, kSms * 4 * kSegmentThreads));
   p->chunks = ceil_div(T, p->chunk);
   size_t off = 0;
   auto take = [&](size_t bytes) { size_t o = off; off += align_up(bytes); return o; };
@@ -134,19 +134,19 @@ void plan_embed(int T, int v, int d, EmbedPlan* p) {
   p->total = off;
 }
 
-// The kernels of the sort may use the shared memory that they ask for: said once on each device.
+// The embedding gradient's kernels may use the shared memory that they ask for: said once on each device.
 constexpr int kMaxDevices = 64;
-int g_sort_allowed[kMaxDevices];
-int allow_sort() {
+int g_embed_allowed[kMaxDevices];
+int allow_embed_gradient() {
   int dev = -1;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return MTPC_ERR_CUDA;
-  if (__atomic_load_n(&g_sort_allowed[dev], __ATOMIC_ACQUIRE)) return MTPC_OK;
+  if (__atomic_load_n(&g_embed_allowed[dev], __ATOMIC_ACQUIRE)) return MTPC_OK;
   const auto allow = [](auto* kernel, size_t bytes) {
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)) == cudaSuccess;
   };
   if (!allow(embed_order_kernel, order_smem_bytes(kOrderMaxT)) || !allow(embed_count_kernel, kSortSmem) || !allow(embed_scatter_kernel, kSortSmem))
     return MTPC_ERR_CUDA;
-  __atomic_store_n(&g_sort_allowed[dev], 1, __ATOMIC_RELEASE);
+  __atomic_store_n(&g_embed_allowed[dev], 1, __ATOMIC_RELEASE);
   return MTPC_OK;
 }
 
@@ -311,7 +311,7 @@ int mtpc_embed_backward(const int32_t* tokens, int32_t T, const void* d_out, int
   if (T == 0)                           // (not accumulated: the gradient is zeros)
     return cudaMemset2DAsync(d_table, static_cast<size_t>(v == 1 ? d : d_table_stride) * 4, 0, static_cast<size_t>(d) * 4, v, st) == cudaSuccess
                ? MTPC_OK : MTPC_ERR_CUDA;
-  if ((rc = allow_sort()) != MTPC_OK) return rc;
+  if ((rc = allow_embed_gradient()) != MTPC_OK) return rc;
   EmbedSortArgs s;
   memset(&s, 0, sizeof(s));
   s.tokens = tokens;
