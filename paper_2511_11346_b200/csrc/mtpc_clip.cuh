@@ -1,8 +1,10 @@
 // The 2-norm of many gradient tensors together, and the gradients scaled to a largest norm.
 //   norm = sqrt(sum over all tensors of g^2),   out = g min(1, max_norm / norm)
-// Two passes over the data, since no element can be scaled before the last one is squared. The tensors are cut into chunks when the list is made, so
-// that a list of one large tensor and one of thousands of small ones are the same work, dealt evenly. The second pass walks the chunks
-// backwards: what the first one read last is still in L2 (126 MB).
+// Two passes over the data, since no element can be scaled before the last one is squared. The tensors are cut into chunks of 2048 elements when the
+// list is made, eight to a thread, so that a list of one large tensor and one of thousands of small ones are the same work; the chunks are dealt
+// round-robin to the blocks, as many as take the same number of rounds, and a thread has its elements of the next three chunks on their way at
+// once. (Chunks of 8192 left up to a third of the last round empty: 78 MB of fp32 48 us. A run of its own for every block writes a tenth
+// slower than chunks dealt out.) The second pass walks the chunks backwards: what the first one read last is still in L2 (126 MB).
 // Squares and their sums are fp64, so that no fp32 gradient overflows or vanishes in them; the order of every sum is fixed.
 #pragma once
 #include <cuda_bf16.h>
@@ -14,53 +16,87 @@
 namespace mtpc {
 
 constexpr int kClipThreads = 256;
-constexpr int kClipChunk = 8192;             // elements
-constexpr int kClipAhead = 2;                // vectors of eight in flight per thread
-constexpr int kClipMaxBlocks = 148 * 8;
+constexpr int kClipChunk = 8 * kClipThreads;   // elements (the first chunk of a tensor: and those before its first vector)
+constexpr int kClipAhead = 3;                  // chunks in flight
+constexpr int kClipBlocks = 148 * 4;           // of a wave
+constexpr int kClipWaves = 8;                  // at most
+constexpr int kClipStage = 64;                 // chunks of a block that are known ahead
 
-struct ClipChunk {
+struct alignas(16) ClipChunk {
   const void* g;
-  void* out;                                 // NULL: the norm alone is wanted
+  void* out;                                   // NULL: the norm alone is wanted
   int count;
-  unsigned kind;                             // kClip* bits, and from bit 8 on the elements before the first that vectors may start at
+  unsigned kind;                               // kClip* bits, and from bit 8 on the elements before the first that vectors may start at
+  unsigned pad[2];
 };
 constexpr unsigned kClipF32 = 1u, kClipOutF32 = 2u, kClipWide = 4u;     // Wide: behind those, both addresses allow vectors of eight elements
+constexpr unsigned kClipFull = 8u;             // Wide, nothing before the first vector, kClipChunk elements
 
+// What a thread has of a chunk: a vector and perhaps one of the up to fourteen elements beside the vectors, or (not Wide) eight elements apart.
+struct ClipItem {
+  uint32_t x[8], beside;
+};
+struct ClipPlace {
+  bool wide, has;                              // has: a vector, at `at`
+  int at, beside;                              // beside: -1: none
+};
+__device__ __forceinline__ ClipPlace clip_place(const ClipChunk& c) {
+  ClipPlace p;
+  const int tid = threadIdx.x, head = c.kind >> 8, packs = (c.count - head) / 8, rest = c.count - head - packs * 8;
+  p.wide = (c.kind & kClipWide) != 0;
+  p.has = p.wide && tid < packs;
+  p.at = head + tid * 8;
+  p.beside = !p.wide ? -1 : tid < head ? tid : tid >= 8 && tid - 8 < rest ? head + packs * 8 + tid - 8 : -1;
+  return p;
+}
 template <typename T>
-__device__ __forceinline__ double chunk_square(const ClipChunk& c) {
+__device__ __forceinline__ uint32_t raw_element(const T* p) {
+  if constexpr (sizeof(T) == 4) return *reinterpret_cast<const uint32_t*>(p);
+  else return *reinterpret_cast<const uint16_t*>(p);
+}
+template <typename T>
+__device__ __forceinline__ void clip_load(const ClipChunk& c, ClipItem& item) {
   const T* g = static_cast<const T*>(c.g);
-  double sum = 0.0;
-  int done = 0;
-  if (c.kind & kClipWide) {
-    const int head = c.kind >> 8, packs = (c.count - head) / 8;
-    if (static_cast<int>(threadIdx.x) < head) {
-      const double x = to_f32(g[threadIdx.x]);
-      sum += x * x;
+  const ClipPlace p = clip_place(c);
+  if (p.wide) {
+    if (p.has) {
+      const Pack<T, 8> pack = load_pack<T, 8>(g + p.at);
+      const uint32_t* words = reinterpret_cast<const uint32_t*>(pack.e);
+#pragma unroll
+      for (int i = 0; i < static_cast<int>(2 * sizeof(T)); ++i) item.x[i] = words[i];
     }
-    for (int i = threadIdx.x; i < packs; i += kClipAhead * kClipThreads) {
-      Pack<T, 8> p[kClipAhead];
+    if (p.beside >= 0) item.beside = raw_element(g + p.beside);
+  } else {
 #pragma unroll
-      for (int u = 0; u < kClipAhead; ++u)
-        if (i + u * kClipThreads < packs) p[u] = load_pack<T, 8>(g + head + (i + u * kClipThreads) * 8);
-#pragma unroll
-      for (int u = 0; u < kClipAhead; ++u) {
-        if (i + u * kClipThreads < packs) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const double x = to_f32(p[u].e[e]);
-            sum += x * x;
-          }
-        }
-      }
+    for (int i = 0; i < 8; ++i) {
+      const int at = threadIdx.x + i * kClipThreads;
+      if (at < c.count) item.x[i] = raw_element(g + at);
     }
-    done = head + packs * 8;
   }
-#pragma unroll 4
-  for (int i = done + threadIdx.x; i < c.count; i += kClipThreads) {
-    const double x = to_f32(g[i]);
-    sum += x * x;
+}
+__device__ __forceinline__ void clip_load(const ClipChunk& c, ClipItem& item) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) item.x[i] = 0;
+  item.beside = 0;
+  if (c.kind & kClipF32) clip_load<float>(c, item);
+  else clip_load<__nv_bfloat16>(c, item);
+}
+// The elements as fp32 (zeros where there is none).
+__device__ __forceinline__ void clip_values(const ClipChunk& c, const ClipItem& item, float (&x)[8], float& beside) {
+  if (c.kind & kClipF32) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(item.x[i]);
+    beside = __uint_as_float(item.beside);
+  } else {
+    beside = __uint_as_float(item.beside << 16);
+    if (c.kind & kClipWide) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(item.x[i] << 16), x[2 * i + 1] = __uint_as_float(item.x[i] & 0xffff0000u);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(item.x[i] << 16);
+    }
   }
-  return sum;
 }
 
 // Sum over the block; every thread has it.
@@ -75,53 +111,91 @@ __device__ __forceinline__ double block_sum(double x, double* share) {
   return x;
 }
 
-__global__ void __launch_bounds__(kClipThreads) gradient_square_kernel(const ClipChunk* chunks, int count, double* partial) {
+// The block's chunks, in the order of `walk` (its i-th is chunks[walk(i)], of `mine` in all), kClipAhead at a time. Where all of those are full and fp32,
+// as most are of most lists, whole(chunks) does them, at half of the instructions; else part(chunk, item) each that skip(chunk) does not leave out.
+template <typename Walk, typename Skip, typename Whole, typename Part>
+__device__ __forceinline__ void clip_walk(const ClipChunk* chunks, int mine, ClipChunk* stage, Walk walk, Skip skip, Whole whole, Part part) {
+  ClipChunk next;
+  const int tid = threadIdx.x;
+  if (tid < kClipStage && tid < mine) next = chunks[walk(tid)];
+  for (int first = 0; first < mine; first += kClipStage) {
+    const int here = min(kClipStage, mine - first);
+    __syncthreads();
+    if (tid < here) stage[tid] = next;
+    __syncthreads();
+    if (tid < kClipStage && first + kClipStage + tid < mine) next = chunks[walk(first + kClipStage + tid)];
+    for (int i = 0; i < here; i += kClipAhead) {
+      unsigned all = i + kClipAhead <= here ? kClipFull | kClipF32 | kClipOutF32 : 0u;
+#pragma unroll
+      for (int u = 0; u < kClipAhead; ++u)
+        if (all && skip(stage[i + u])) all = 0;
+        else if (all) all &= stage[i + u].kind;
+      if (all == (kClipFull | kClipF32 | kClipOutF32)) {
+        whole(stage + i);
+      } else {
+#pragma unroll 1
+        for (int u = 0; u < min(kClipAhead, here - i); ++u) {
+          if (skip(stage[i + u])) continue;
+          ClipItem item;
+          clip_load(stage[i + u], item);
+          part(stage[i + u], item);
+        }
+      }
+    }
+  }
+}
+
+__global__ void __launch_bounds__(kClipThreads, 4) gradient_square_kernel(const ClipChunk* chunks, int count, double* partial) {
   __shared__ double share[kClipThreads / 32];
+  __shared__ ClipChunk stage[kClipStage];
   grid_dependency_wait();
   double sum = 0.0;
-  for (int c = blockIdx.x; c < count; c += gridDim.x) {
-    const ClipChunk chunk = chunks[c];
-    sum += (chunk.kind & kClipF32) ? chunk_square<float>(chunk) : chunk_square<__nv_bfloat16>(chunk);
-  }
+  const int block = blockIdx.x, blocks = gridDim.x;
+  clip_walk(chunks, block < count ? (count - block + blocks - 1) / blocks : 0, stage, [&](int i) { return block + i * blocks; },
+            [](const ClipChunk&) { return false; },
+            [&](const ClipChunk* c) {
+              Pack<float, 8> x[kClipAhead];
+#pragma unroll
+              for (int u = 0; u < kClipAhead; ++u) x[u] = load_pack<float, 8>(static_cast<const float*>(c[u].g) + threadIdx.x * 8);
+#pragma unroll
+              for (int u = 0; u < kClipAhead; ++u) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum += static_cast<double>(x[u].e[i]) * x[u].e[i];
+              }
+            },
+            [&](const ClipChunk& c, const ClipItem& item) {
+              float x[8], beside;
+              clip_values(c, item, x, beside);
+#pragma unroll
+              for (int i = 0; i < 8; ++i) sum += static_cast<double>(x[i]) * x[i];
+              sum += static_cast<double>(beside) * beside;
+            });
   sum = block_sum(sum, share);
   if (threadIdx.x == 0) partial[blockIdx.x] = sum;
   grid_launch_dependents();
 }
 
-template <typename TI, typename TO>
-__device__ __forceinline__ void chunk_scale(const ClipChunk& c, float first, float by) {
-  const TI* g = static_cast<const TI*>(c.g);
-  TO* out = static_cast<TO*>(c.out);
-  int done = 0;
-  if (c.kind & kClipWide) {
-    const int head = c.kind >> 8, packs = (c.count - head) / 8;
-    if (static_cast<int>(threadIdx.x) < head) out[threadIdx.x] = from_f32<TO>(to_f32(g[threadIdx.x]) * first * by);
-    for (int i = threadIdx.x; i < packs; i += kClipAhead * kClipThreads) {
-      Pack<TI, 8> p[kClipAhead];
+template <typename T>
+__device__ __forceinline__ void clip_store(const ClipChunk& c, const float (&x)[8], float beside) {
+  T* out = static_cast<T*>(c.out);
+  const ClipPlace p = clip_place(c);
+  if (p.wide) {
+    if (p.has) store_f32<T, 8>(out + p.at, x);
+    if (p.beside >= 0) out[p.beside] = from_f32<T>(beside);
+  } else {
 #pragma unroll
-      for (int u = 0; u < kClipAhead; ++u)
-        if (i + u * kClipThreads < packs) p[u] = load_pack<TI, 8>(g + head + (i + u * kClipThreads) * 8);
-#pragma unroll
-      for (int u = 0; u < kClipAhead; ++u) {
-        if (i + u * kClipThreads < packs) {
-          float x[8];
-          unpack(p[u], x);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] = x[e] * first * by;
-          store_f32<TO, 8>(out + head + (i + u * kClipThreads) * 8, x);
-        }
-      }
+    for (int i = 0; i < 8; ++i) {
+      const int at = threadIdx.x + i * kClipThreads;
+      if (at < c.count) out[at] = from_f32<T>(x[i]);
     }
-    done = head + packs * 8;
   }
-#pragma unroll 4
-  for (int i = done + threadIdx.x; i < c.count; i += kClipThreads) out[i] = from_f32<TO>(to_f32(g[i]) * first * by);
 }
 
-// blocks: of the kernel before.
-__global__ void __launch_bounds__(kClipThreads) gradient_scale_kernel(const ClipChunk* chunks, int count, const double* partial, int blocks,
-                                                                      float max_norm, float* out_norm) {
+// blocks: of both kernels.
+__global__ void __launch_bounds__(kClipThreads, 4) gradient_scale_kernel(const ClipChunk* chunks, int count, const double* partial, int blocks,
+                                                                         float max_norm, float* out_norm) {
   __shared__ double share[kClipThreads / 32];
+  __shared__ ClipChunk stage[kClipStage];
   grid_dependency_wait();
   double sum = 0.0;
   for (int i = threadIdx.x; i < blocks; i += kClipThreads) sum += partial[i];
@@ -131,17 +205,29 @@ __global__ void __launch_bounds__(kClipThreads) gradient_scale_kernel(const Clip
   const double ratio = norm > max_norm && norm <= 1.7976931348623157e308 ? max_norm / norm : 1.0;
   // A ratio near the end of fp32's range is multiplied in two steps, the first a power of two.
   const float first = ratio < 0x1p-100 ? 0x1p-64f : 1.f, by = static_cast<float>(ratio / first);
-  for (int c = count - 1 - static_cast<int>(blockIdx.x); c >= 0; c -= gridDim.x) {
-    const ClipChunk chunk = chunks[c];
-    if (chunk.out == nullptr || (chunk.out == chunk.g && ratio == 1.0)) continue;
-    if (chunk.kind & kClipF32) {
-      if (chunk.kind & kClipOutF32) chunk_scale<float, float>(chunk, first, by);
-      else chunk_scale<float, __nv_bfloat16>(chunk, first, by);
-    } else {
-      if (chunk.kind & kClipOutF32) chunk_scale<__nv_bfloat16, float>(chunk, first, by);
-      else chunk_scale<__nv_bfloat16, __nv_bfloat16>(chunk, first, by);
-    }
-  }
+  const int block = blockIdx.x;
+  clip_walk(chunks, block < count ? (count - block + blocks - 1) / blocks : 0, stage, [&](int i) { return count - 1 - block - i * blocks; },
+            [&](const ClipChunk& c) { return c.out == nullptr || (c.out == c.g && ratio == 1.0); },
+            [&](const ClipChunk* c) {
+              Pack<float, 8> x[kClipAhead];
+#pragma unroll
+              for (int u = 0; u < kClipAhead; ++u) x[u] = load_pack<float, 8>(static_cast<const float*>(c[u].g) + threadIdx.x * 8);
+#pragma unroll
+              for (int u = 0; u < kClipAhead; ++u) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[u].e[i] = x[u].e[i] * first * by;
+                store_pack<float, 8>(static_cast<float*>(c[u].out) + threadIdx.x * 8, x[u]);
+              }
+            },
+            [&](const ClipChunk& c, const ClipItem& item) {
+              float x[8], beside;
+              clip_values(c, item, x, beside);
+#pragma unroll
+              for (int i = 0; i < 8; ++i) x[i] = x[i] * first * by;
+              beside = beside * first * by;
+              if (c.kind & kClipOutF32) clip_store<float>(c, x, beside);
+              else clip_store<__nv_bfloat16>(c, x, beside);
+            });
   grid_launch_dependents();
 }
 

@@ -210,7 +210,11 @@ int plan_list(const mtpc_gradient* entries, int32_t count, ListPlan* p) {
     p->chunks += (e.count + kClipChunk - 1) / kClipChunk;
     if (p->chunks > (1 << 30)) return MTPC_ERR_UNSUPPORTED;
   }
-  p->blocks = static_cast<int>(std::max<long long>(1, std::min<long long>(p->chunks, kClipMaxBlocks)));
+  // One wave of blocks, or up to kClipWaves of them with 16 chunks each (the waves follow each other through the list, so that the second pass finds
+  // more of what the first one left in L2: 671 MB 306 us in eight waves, 327 in one; 78 MB, where each block's sum of the others' counts, 47 and 41).
+  const long long waves = std::max<long long>(1, std::min<long long>(kClipWaves, p->chunks / (16 * kClipBlocks)));
+  const long long rounds = std::max<long long>(1, (p->chunks + waves * kClipBlocks - 1) / (waves * kClipBlocks));
+  p->blocks = static_cast<int>(std::max<long long>(1, (p->chunks + rounds - 1) / rounds));      // every block as many chunks, but for one
   p->off_partial = align_up(static_cast<size_t>(p->chunks) * sizeof(ClipChunk));
   p->total = p->off_partial + align_up(static_cast<size_t>(p->blocks) * sizeof(double));
   return MTPC_OK;
@@ -539,8 +543,9 @@ int mtpc_create_gradient_list(const mtpc_gradient* entries, int32_t count, void*
       c.g = static_cast<const uint8_t*>(e.data) + static_cast<size_t>(at) * element(e.dtype);
       c.out = e.out ? static_cast<uint8_t*>(e.out) + static_cast<size_t>(at) * element(e.out_dtype) : nullptr;
       c.count = static_cast<int>(take);
-      c.kind = (e.dtype == MTPC_F32 ? kClipF32 : 0u) | (e.out && e.out_dtype == MTPC_F32 ? kClipOutF32 : 0u);
-      if (head >= 0 && own_head < take) c.kind |= kClipWide | static_cast<unsigned>(own_head) << 8;
+      c.pad[0] = c.pad[1] = 0;
+      c.kind = (e.dtype == MTPC_F32 ? kClipF32 : 0u) | ((e.out ? e.out_dtype : e.dtype) == MTPC_F32 ? kClipOutF32 : 0u);
+      if (head >= 0 && own_head < take) c.kind |= kClipWide | (own_head == 0 && take == kClipChunk ? kClipFull : 0u) | static_cast<unsigned>(own_head) << 8;
       at += take;
     }
   }
