@@ -7,6 +7,7 @@ be loaded, importing a symbol from it raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 from . import build as _build
@@ -364,84 +365,89 @@ class MtpcHead:
             pass
 
 
-# -- the calls beside the head: tensors in, checked for what the C side cannot see (types, devices, strides within a row)
-def _dtype(t, what: str) -> int:
-    import torch
-    if t.dtype is torch.bfloat16:
-        return MTPC_BF16
-    if t.dtype is torch.float32:
-        return MTPC_F32
-    raise MtpcError(ERR_UNSUPPORTED, f"{what}: {t.dtype}")
+# -- the calls beside the head: tensors in, checked for what the C side cannot see (types, devices, strides within a row). A decoding step makes some of
+# them per layer on a single row, so the checks look at each tensor once, through the calls of torch that make no objects.
+def _refuse(what: str, why: str, code: int = ERR_SHAPE):
+    raise MtpcError(code, f"{what}: {why}")
 
 
-def _like(what: str, device, shape, *tensors) -> None:
-    """The tensors that are there lie on `device` and have `shape` with adjacent elements in a row."""
-    for t in tensors:
-        if t is None:
-            continue
-        if t.device != device or t.device.type != "cuda":
-            raise MtpcError(ERR_SHAPE, f"{what}: a tensor on {t.device}, another on {device}")
-        if t.shape != shape or (shape[-1] > 1 and t.stride(-1) != 1):
-            raise MtpcError(ERR_SHAPE, f"{what}: {tuple(t.shape)} with strides {t.stride()} where {tuple(shape)} is needed")
+def _dtypes() -> dict:
+    global _dtype_codes
+    if _dtype_codes is None:
+        import torch
+        _dtype_codes = {torch.float32: MTPC_F32, torch.bfloat16: MTPC_BF16}
+    return _dtype_codes
 
 
-def _same_dtype(what: str, dtype, *tensors) -> None:
-    for t in tensors:
-        if t is not None and t.dtype is not dtype:
-            raise MtpcError(ERR_UNSUPPORTED, f"{what}: {t.dtype} where {dtype} is needed")
+_dtype_codes = None
+
+
+def _dtype(what: str, t) -> int:
+    code = _dtypes().get(t.dtype)
+    if code is None:
+        _refuse(what, f"{t.dtype}", ERR_UNSUPPORTED)
+    return code
 
 
 def _matrix(what: str, t):
-    if t.dim() != 2:
-        raise MtpcError(ERR_SHAPE, f"{what}: {tuple(t.shape)} where a matrix is needed")
-    return t.shape
+    """(rows, columns, device) of a matrix on a device."""
+    if t.dim() != 2 or not t.is_cuda:
+        _refuse(what, f"{tuple(t.shape)} on {t.device} where a matrix on a device is needed")
+    rows, columns = t.shape
+    return rows, columns, t.get_device()
 
 
-def _row_stride(t) -> int:
-    return 0 if t is None else t.stride(0)
+def _rows(what: str, t, rows: int, columns: int, device: int, dtype=None) -> int:
+    """The stride of a [rows, columns] matrix on `device` (and of a dtype) whose rows are adjacent elements."""
+    if t.shape == (rows, columns) and t.get_device() == device and (dtype is None or t.dtype is dtype):
+        stride, inner = t.stride()
+        if inner == 1 or columns == 1:
+            return stride
+    elif dtype is not None and t.dtype is not dtype:
+        _refuse(what, f"{t.dtype} where {dtype} is needed", ERR_UNSUPPORTED)
+    _refuse(what, f"{tuple(t.shape)} with strides {t.stride()} on {t.device} where ({rows}, {columns}) on device {device} is needed")
 
 
-class _On:
-    """The device of a call's tensors as the current one, where it is not (a launch goes to the current device)."""
-
-    def __init__(self, device):
-        import torch
-        self.other = None
-        if device.type == "cuda" and torch.cuda.current_device() != device.index:
-            self.other = torch.cuda.device(device)
-
-    def __enter__(self):
-        if self.other is not None:
-            self.other.__enter__()
-
-    def __exit__(self, *exc):
-        if self.other is not None:
-            self.other.__exit__(*exc)
+def _vector(what: str, t, count: int, device: int, dtype=None) -> int:
+    """The address of a [count] vector of adjacent elements on `device`; 0 for None."""
+    if t is None:
+        return 0
+    if t.shape != (count,) or (count > 1 and t.stride(0) != 1) or t.get_device() != device:
+        _refuse(what, f"{tuple(t.shape)} with strides {t.stride()} on {t.device} where ({count},) on device {device} is needed")
+    if dtype is not None and t.dtype is not dtype:
+        _refuse(what, f"{t.dtype} where {dtype} is needed", ERR_UNSUPPORTED)
+    return t.data_ptr()
 
 
-class _In:
-    """The given stream as torch's current one (what torch allocates meanwhile belongs to it); None: it is already."""
-
-    def __init__(self, stream):
-        import torch
-        self.stream = None if stream is None else torch.cuda.stream(stream)
-
-    def __enter__(self):
-        if self.stream is not None:
-            self.stream.__enter__()
-
-    def __exit__(self, *exc):
-        if self.stream is not None:
-            self.stream.__exit__(*exc)
+def _call(what: str, function, device: int, stream, *args) -> None:
+    """The call on `stream` (None: torch's current one of the device), with the tensors' device as the current one: a launch goes there."""
+    import torch
+    if torch._C._cuda_getDevice() == device:
+        code = function(*args, _stream(stream, device))
+    else:
+        with torch.cuda.device(device):
+            code = function(*args, _stream(stream, device))
+    if code != MTPC_OK:
+        raise MtpcError(code, what)
 
 
-def _scratch(what: str, workspace, need: int, device):
+@functools.lru_cache(maxsize=256)
+def _scratch_bytes(name: str, *sizes) -> int:
+    need = ctypes.c_size_t(0)
+    _check(getattr(lib(), name)(*sizes, ctypes.byref(need)), name)
+    return need.value
+
+
+def _scratch(what: str, workspace, need: int, device: int, stream):
     """The caller's workspace, or one from torch's allocator, which keeps it apart per stream and per captured graph."""
     import torch
     if workspace is None:
-        return torch.empty(need, dtype=torch.uint8, device=device)
-    if workspace.device != device or not workspace.is_contiguous() or workspace.dtype is not torch.uint8:
-        raise MtpcError(ERR_SHAPE, f"{what}: workspace of {workspace.dtype} on {workspace.device}")
+        if stream is None:
+            return torch.empty(need, dtype=torch.uint8, device=device)
+        with torch.cuda.stream(stream):
+            return torch.empty(need, dtype=torch.uint8, device=device)
+    if workspace.get_device() != device or not workspace.is_contiguous() or workspace.dtype is not torch.uint8:
+        _refuse(what, f"workspace of {workspace.dtype} on {workspace.device}")
     return workspace
 
 
@@ -450,21 +456,15 @@ def mtpc_embed(tokens, table, out, scale: float = 1.0, out_status=None, stream=N
     fp32 or bf16; out_status: int32 [1], into which the status bits are or-ed."""
     import torch
     what = "mtpc_embed"
-    (v, d), dev, T = _matrix(what, table), table.device, tokens.numel()
-    _like(what, dev, (T,), tokens)
-    _like(what, dev, (v, d), table)
-    _like(what, dev, (T, d), out)
-    _like(what, dev, (1,), out_status)
-    _same_dtype(what, torch.int32, tokens, out_status)
-    with _On(dev):
-        _check(lib().mtpc_embed(tokens.data_ptr(), T, table.data_ptr(), table.stride(0), _dtype(table, what), v, d, scale, out.data_ptr(),
-                                out.stride(0), _dtype(out, what), _ptr(out_status), _stream(stream, dev.index)), what)
+    v, d, dev = _matrix(what, table)
+    T = tokens.numel()
+    _call(what, lib().mtpc_embed, dev, stream, _vector(what, tokens, T, dev, torch.int32), T, table.data_ptr(), _rows(what, table, v, d, dev),
+          _dtype(what, table), v, d, scale, out.data_ptr(), _rows(what, out, T, d, dev), _dtype(what, out),
+          _vector(what, out_status, 1, dev, torch.int32))
 
 
 def mtpc_embed_backward_workspace_bytes(T: int, v: int, d: int) -> int:
-    need = ctypes.c_size_t(0)
-    _check(lib().mtpc_embed_backward_workspace_bytes(T, v, d, ctypes.byref(need)), "mtpc_embed_backward_workspace_bytes")
-    return need.value
+    return _scratch_bytes("mtpc_embed_backward_workspace_bytes", T, v, d)
 
 
 def mtpc_embed_backward(tokens, d_out, d_table, scale: float = 1.0, accumulate: bool = False, workspace=None, out_status=None,
@@ -473,18 +473,12 @@ def mtpc_embed_backward(tokens, d_out, d_table, scale: float = 1.0, accumulate: 
     fp32 or bf16, d_table [v, d] fp32. workspace None: from torch's allocator, for the call."""
     import torch
     what = "mtpc_embed_backward"
-    (v, d), dev, T = _matrix(what, d_table), d_table.device, tokens.numel()
-    _like(what, dev, (T,), tokens)
-    _like(what, dev, (T, d), d_out)
-    _like(what, dev, (v, d), d_table)
-    _like(what, dev, (1,), out_status)
-    _same_dtype(what, torch.int32, tokens, out_status)
-    _same_dtype(what, torch.float32, d_table)
-    with _On(dev), _In(stream):
-        ws = _scratch(what, workspace, mtpc_embed_backward_workspace_bytes(T, v, d), dev)
-        _check(lib().mtpc_embed_backward(tokens.data_ptr(), T, d_out.data_ptr(), d_out.stride(0), _dtype(d_out, what), scale, v, d,
-                                         d_table.data_ptr(), d_table.stride(0), int(bool(accumulate)), ws.data_ptr(), ws.numel(), _ptr(out_status),
-                                         _stream(stream, dev.index)), what)
+    v, d, dev = _matrix(what, d_table)
+    T = tokens.numel()
+    ws = _scratch(what, workspace, _scratch_bytes("mtpc_embed_backward_workspace_bytes", T, v, d), dev, stream)
+    _call(what, lib().mtpc_embed_backward, dev, stream, _vector(what, tokens, T, dev, torch.int32), T, d_out.data_ptr(),
+          _rows(what, d_out, T, d, dev), _dtype(what, d_out), scale, v, d, d_table.data_ptr(), _rows(what, d_table, v, d, dev, torch.float32),
+          1 if accumulate else 0, ws.data_ptr(), ws.numel(), _vector(what, out_status, 1, dev, torch.int32))
 
 
 def mtpc_residual_rmsnorm(x, residual, weight, eps: float, out, out_sum=None, out_q=None, out_scale=None, scale_group: int = 0,
@@ -493,49 +487,43 @@ def mtpc_residual_rmsnorm(x, residual, weight, eps: float, out, out_sum=None, ou
     out_scale [T, ceil(d / scale_group)] fp32 (scale_group 0: [T, 1]): the same in 8 bits. out or out_q may be None."""
     import torch
     what = "mtpc_residual_rmsnorm"
-    (T, d), dev = _matrix(what, x), x.device
-    _like(what, dev, (T, d), x, residual, out, out_sum, out_q)
-    _like(what, dev, (d,), weight)
-    _same_dtype(what, x.dtype, residual, out, out_sum)
+    T, d, dev = _matrix(what, x)
+    io = x.dtype
+    r_stride = 0 if residual is None else _rows(what, residual, T, d, dev, io)
+    s_stride = 0 if out_sum is None else _rows(what, out_sum, T, d, dev, io)
+    o_stride = 0 if out is None else _rows(what, out, T, d, dev, io)
+    q_stride = 0
+    if out_q is not None:
+        q_stride = _rows(what, out_q, T, d, dev)
+        if out_q.dtype not in (torch.float8_e4m3fn, torch.uint8):
+            _refuse(what, f"{out_q.dtype}", ERR_UNSUPPORTED)
     if out_scale is not None:
-        _like(what, dev, (T, -(-d // scale_group) if scale_group > 0 else 1), out_scale)
-        _same_dtype(what, torch.float32, out_scale)
+        _rows(what, out_scale, T, -(-d // scale_group) if scale_group > 0 else 1, dev, torch.float32)
         if not out_scale.is_contiguous():
-            raise MtpcError(ERR_SHAPE, f"{what}: out_scale with strides {out_scale.stride()}")
-    if out_q is not None and out_q.dtype not in (torch.float8_e4m3fn, torch.uint8):
-        raise MtpcError(ERR_UNSUPPORTED, f"{what}: {out_q.dtype}")
-    with _On(dev):
-        _check(lib().mtpc_residual_rmsnorm(x.data_ptr(), x.stride(0), _ptr(residual), _row_stride(residual), _ptr(weight),
-                                           MTPC_F32 if weight is None else _dtype(weight, what), T, d, _dtype(x, what), eps, _ptr(out_sum),
-                                           _row_stride(out_sum), _ptr(out), _row_stride(out), _ptr(out_q), _row_stride(out_q), _ptr(out_scale),
-                                           scale_group, _stream(stream, dev.index)), what)
+            _refuse(what, f"out_scale with strides {out_scale.stride()}")
+    _call(what, lib().mtpc_residual_rmsnorm, dev, stream, x.data_ptr(), _rows(what, x, T, d, dev), _ptr(residual), r_stride,
+          _vector(what, weight, d, dev), MTPC_F32 if weight is None else _dtype(what, weight), T, d, _dtype(what, x), eps, _ptr(out_sum), s_stride,
+          _ptr(out), o_stride, _ptr(out_q), q_stride, _ptr(out_scale), scale_group)
 
 
 def mtpc_residual_rmsnorm_backward_workspace_bytes(T: int, d: int) -> int:
-    need = ctypes.c_size_t(0)
-    _check(lib().mtpc_residual_rmsnorm_backward_workspace_bytes(T, d, ctypes.byref(need)), "mtpc_residual_rmsnorm_backward_workspace_bytes")
-    return need.value
+    return _scratch_bytes("mtpc_residual_rmsnorm_backward_workspace_bytes", T, d)
 
 
 def mtpc_residual_rmsnorm_backward(sum, weight, eps: float, d_out, d_sum, d_x, d_weight=None, workspace=None, stream=None) -> None:
     """d_x: the gradient of the sum (of x and of residual alike) from d_out, the gradient of the norm's output, and d_sum, what reaches the sum along
-    the residual stream (None: nothing; d_x's dtype). d_weight [d] fp32 or None."""
+    the residual stream (None: nothing; d_x's dtype). d_weight [d] fp32 or None. workspace as in mtpc_embed_backward."""
     import torch
     what = "mtpc_residual_rmsnorm_backward"
-    (T, d), dev = _matrix(what, sum), sum.device
-    _like(what, dev, (T, d), sum, d_out, d_sum, d_x)
-    _like(what, dev, (d,), weight, d_weight)
-    _same_dtype(what, d_x.dtype, d_sum)
-    _same_dtype(what, torch.float32, d_weight)
-    with _On(dev), _In(stream):
-        ws = None
-        if d_weight is not None:
-            ws = _scratch(what, workspace, mtpc_residual_rmsnorm_backward_workspace_bytes(T, d), dev)
-        _check(lib().mtpc_residual_rmsnorm_backward(sum.data_ptr(), sum.stride(0), _dtype(sum, what), _ptr(weight),
-                                                    MTPC_F32 if weight is None else _dtype(weight, what), T, d, eps, d_out.data_ptr(),
-                                                    d_out.stride(0), _dtype(d_out, what), _ptr(d_sum), _row_stride(d_sum), d_x.data_ptr(),
-                                                    d_x.stride(0), _dtype(d_x, what), _ptr(d_weight), _ptr(ws), 0 if ws is None else ws.numel(),
-                                                    _stream(stream, dev.index)), what)
+    T, d, dev = _matrix(what, sum)
+    ws, ws_ptr, ws_bytes = None, 0, 0
+    if d_weight is not None:
+        ws = _scratch(what, workspace, _scratch_bytes("mtpc_residual_rmsnorm_backward_workspace_bytes", T, d), dev, stream)
+        ws_ptr, ws_bytes = ws.data_ptr(), ws.numel()
+    _call(what, lib().mtpc_residual_rmsnorm_backward, dev, stream, sum.data_ptr(), _rows(what, sum, T, d, dev), _dtype(what, sum),
+          _vector(what, weight, d, dev), MTPC_F32 if weight is None else _dtype(what, weight), T, d, eps, d_out.data_ptr(),
+          _rows(what, d_out, T, d, dev), _dtype(what, d_out), _ptr(d_sum), 0 if d_sum is None else _rows(what, d_sum, T, d, dev, d_x.dtype),
+          d_x.data_ptr(), _rows(what, d_x, T, d, dev), _dtype(what, d_x), _vector(what, d_weight, d, dev, torch.float32), ws_ptr, ws_bytes)
 
 
 class GradientList:
@@ -551,32 +539,30 @@ class GradientList:
         outs = grads if outs is None else list(outs)
         if not grads or len(outs) != len(grads):
             raise MtpcError(ERR_SHAPE, f"{what}: {len(grads)} gradients, {len(outs)} results")
-        self.device = grads[0].device
+        self.device = grads[0].get_device()
         entries = (MtpcGradient * len(grads))()
         for e, g, o in zip(entries, grads, outs):
             for t in (g, o):
-                if t is not None and (t.device != self.device or t.device.type != "cuda" or not t.is_contiguous() or t.numel() != g.numel()):
-                    raise MtpcError(ERR_SHAPE, f"{what}: {tuple(t.shape)} with strides {t.stride()} on {t.device}")
-            e.data, e.out, e.count, e.dtype = g.data_ptr(), _ptr(o), g.numel(), _dtype(g, what)
-            e.out_dtype = e.dtype if o is None else _dtype(o, what)
+                if t is not None and (not t.is_cuda or t.get_device() != self.device or not t.is_contiguous() or t.numel() != g.numel()):
+                    _refuse(what, f"{tuple(t.shape)} with strides {t.stride()} on {t.device}")
+            e.data, e.out, e.count, e.dtype = g.data_ptr(), _ptr(o), g.numel(), _dtype(what, g)
+            e.out_dtype = e.dtype if o is None else _dtype(what, o)
         need = ctypes.c_size_t(0)
         _check(lib().mtpc_gradient_list_workspace_bytes(entries, len(grads), ctypes.byref(need)), "mtpc_gradient_list_workspace_bytes")
         self._keep = (grads, outs)
         handle = ctypes.c_void_p(0)
-        with _On(self.device), _In(stream):
-            self.workspace = torch.empty(need.value, dtype=torch.uint8, device=self.device)
-            _check(lib().mtpc_create_gradient_list(entries, len(grads), self.workspace.data_ptr(), need.value, _stream(stream, self.device.index),
-                                                   ctypes.byref(handle)), what)
+        self.workspace = _scratch(what, None, need.value, self.device, stream)
+
+        def create(raw):
+            return lib().mtpc_create_gradient_list(entries, len(grads), self.workspace.data_ptr(), need.value, raw, ctypes.byref(handle))
+        _call(what, create, self.device, stream)
         self.handle = handle
 
     def mtpc_clip_gradients(self, max_norm: float, out_norm, stream=None) -> None:
         """out_norm [1] fp32: the norm of all gradients; where it is above max_norm (and finite) they are scaled by max_norm / norm."""
         import torch
         what = "mtpc_clip_gradients"
-        _like(what, self.device, (1,), out_norm)
-        _same_dtype(what, torch.float32, out_norm)
-        with _On(self.device):
-            _check(lib().mtpc_clip_gradients(self.handle, max_norm, out_norm.data_ptr(), _stream(stream, self.device.index)), what)
+        _call(what, lib().mtpc_clip_gradients, self.device, stream, self.handle, max_norm, _vector(what, out_norm, 1, self.device, torch.float32))
 
     def mtpc_destroy_gradient_list(self) -> None:
         if self.handle:
