@@ -30,8 +30,9 @@ struct NormArgs {
   float* scales;                          // [T, groups]
   long long x_stride, residual_stride, sum_stride, out_stride, codes_stride;
   int T, d, group, groups;                // group: columns that share a scale (0: the row)
+  int group_shift;                        // its logarithm
   bool weight_f32;
-  float eps;
+  float eps, inv_d;
 };
 
 // Largest magnitude as the bits of an fp32: compared as integers a NaN is larger than everything, so it is not lost.
@@ -46,12 +47,12 @@ __device__ __forceinline__ float code_scale(unsigned bits) {
 // reciprocal fp32 cannot hold go in two steps, the first a power of two.
 __device__ __forceinline__ float2 code_factors(float scale) {
   const float first = scale < 0x1p-100f ? 0x1p64f : 1.f;
-  return make_float2(first, 1.f / (scale * first));
+  return make_float2(first, __fdividef(1.f, scale * first));          // (scale * first is between 2^-100 and 2^120)
 }
 
 template <typename IO, int V, int NV, int THREADS, int CTAS>
 __global__ void __launch_bounds__(THREADS, CTAS) residual_rmsnorm_kernel(const __grid_constant__ NormArgs a) {
-  __shared__ float red[2][1][32];
+  __shared__ float red[2][32];
   __shared__ unsigned group_max[V == 1 ? kNormMaxWidth / kNormMinGroup : 1];
   const int row = blockIdx.x * blockDim.y + threadIdx.y;
   const int tid = threadIdx.x, lane = tid & 31;
@@ -94,26 +95,26 @@ __global__ void __launch_bounds__(THREADS, CTAS) residual_rmsnorm_kernel(const _
       }
     }
   }
-  float square[1] = {0.f};
+  float square = 0.f;
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) square[0] += s[j][i] * s[j][i];
+    for (int i = 0; i < V; ++i) square += s[j][i] * s[j][i];
   }
-  row_sum(square, red[0]);
-  float rstd = rsqrtf(square[0] / a.d + a.eps);
-  if (__float_as_uint(square[0]) == 0x7f800000u) {           // the same in every thread of the row
-    square[0] = 0.f;
+  square = row_sum(square, red[0]);
+  float rstd = rsqrtf(square * a.inv_d + a.eps);
+  if (__float_as_uint(square) == 0x7f800000u) {              // the same in every thread of the row
+    square = 0.f;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         s[j][i] *= kNormRescue;
-        square[0] += s[j][i] * s[j][i];
+        square += s[j][i] * s[j][i];
       }
     }
-    row_sum(square, red[1]);
-    rstd = rsqrtf(square[0] / a.d);
+    square = row_sum(square, red[1]);
+    rstd = rsqrtf(square * a.inv_d);
   }
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
@@ -144,7 +145,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) residual_rmsnorm_kernel(const _
     for (int j = 0; j < NV; ++j) m = max(m, largest[j]);
     m = __reduce_max_sync(0xffffffffu, m);
     if (blockDim.x > 32) {
-      unsigned* share = reinterpret_cast<unsigned*>(red[1][0]);
+      unsigned* share = reinterpret_cast<unsigned*>(red[1]);
       __syncthreads();                                       // red[1] may still be read (rows whose squares overflowed)
       if (lane == 0) share[tid >> 5] = m;
       __syncthreads();
@@ -157,24 +158,26 @@ __global__ void __launch_bounds__(THREADS, CTAS) residual_rmsnorm_kernel(const _
     const int lanes = a.group / V;                           // 4 to 16 lanes hold a group
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      for (int o = 1; o < lanes; o <<= 1) largest[j] = max(largest[j], __shfl_xor_sync(0xffffffffu, largest[j], o));
+#pragma unroll
+      for (int o = 1; o < 16; o <<= 1)
+        if (o < lanes) largest[j] = max(largest[j], __shfl_xor_sync(0xffffffffu, largest[j], o));
       const int col = (tid + j * blockDim.x) * V;
-      if (col < a.d && lane % lanes == 0) scales[col / a.group] = code_scale(largest[j]);
+      if (col < a.d && (lane & (lanes - 1)) == 0) scales[col >> a.group_shift] = code_scale(largest[j]);
     }
   } else {
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const unsigned m = __reduce_max_sync(0xffffffffu, largest[j]);       // 32 columns of one group
       const int col = tid + j * blockDim.x;
-      if (lane == 0 && col < a.d) atomicMax(&group_max[col / a.group], m);
+      if (lane == 0 && col < a.d) atomicMax(&group_max[col >> a.group_shift], m);
     }
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int col = tid + j * blockDim.x;
       if (col < a.d) {
-        largest[j] = group_max[col / a.group];
-        if (col % a.group == 0) scales[col / a.group] = code_scale(largest[j]);
+        largest[j] = group_max[col >> a.group_shift];
+        if ((col & (a.group - 1)) == 0) scales[col >> a.group_shift] = code_scale(largest[j]);
       }
     }
   }
@@ -202,144 +205,178 @@ struct NormGradArgs {
   long long sum_stride, d_out_stride, d_stream_stride, d_x_stride;
   int T, d;
   bool weight_f32;
-  float eps;
+  float eps, inv_d;
 };
 
-// A thread's eight elements of a row in its own places of shared memory, 16 bytes per piece, a piece's neighbours the other threads'.
+// A thread's eight elements of a row in its own places of shared memory, in pieces of 16 bytes `pitch` apart, a piece's neighbours the other threads'.
 template <typename T>
 struct RingRow {
   static constexpr int kPieces = sizeof(T) * 8 / 16;
-  static __device__ __forceinline__ void fetch(uint32_t at, const T* src) {
+  static __device__ __forceinline__ void fetch(uint32_t at, const T* src, uint32_t pitch) {
 #pragma unroll
-    for (int i = 0; i < kPieces; ++i) copy_async16(at + i * blockDim.x * 16, reinterpret_cast<const uint8_t*>(src) + i * 16);
+    for (int i = 0; i < kPieces; ++i) copy_async16(at + i * pitch, reinterpret_cast<const uint8_t*>(src) + i * 16);
   }
-  static __device__ __forceinline__ void read(uint32_t at, float (&x)[8]) {
+  static __device__ __forceinline__ void read(uint32_t at, uint32_t pitch, float (&x)[8]) {
     Pack<T, 8> p;
     uint32_t* r = reinterpret_cast<uint32_t*>(p.e);
 #pragma unroll
     for (int i = 0; i < kPieces; ++i)
       asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
                    : "=r"(r[4 * i]), "=r"(r[4 * i + 1]), "=r"(r[4 * i + 2]), "=r"(r[4 * i + 3])
-                   : "r"(at + i * blockDim.x * 16));
+                   : "r"(at + i * pitch));
     unpack(p, x);
   }
 };
-// Bytes of a thread's part of a stage.
+// Bytes of a thread's part of a row.
 template <typename IO, typename DY, typename DX>
 __host__ __device__ constexpr int norm_grad_thread_bytes() { return 8 * (sizeof(IO) + sizeof(DY) + sizeof(DX)); }
 
-// Every block has every gridDim.x-th row and keeps its part of d weight in registers. STAGES > 0 (eight elements a thread): rows come through
-// shared memory, the next STAGES - 1 on their way while one is worked on, every thread copying and reading its own elements (no barrier of their
-// own). With one row at a time in registers two blocks of 512 threads an SM waited for memory half of the time (8192 rows of 4096, bf16, d_out
-// fp32: 88 us). Otherwise (wider rows, and rows that no vectors fit) a row is read twice, the second time from L1 or L2.
+// Every block has every gridDim.x-th row and keeps its part of d weight in registers. STAGES > 0: rows come through shared memory, the next
+// STAGES - 1 on their way while one is worked on, every thread copying and reading its own elements (no barrier of their own). With one row at a
+// time in registers two blocks of 512 threads an SM waited for memory half of the time (8192 rows of 4096, bf16, d_out fp32: 88 us); with eight
+// elements a thread and the row read from the ring twice, shared memory and shuffles were the bound (74 us). Otherwise (wider rows, and rows that no
+// vectors fit) a row is read twice, the second time from L1 or L2.
 template <typename IO, typename DY, typename DX, int V, int NV, int STAGES, int THREADS, int CTAS>
 __global__ void __launch_bounds__(THREADS, CTAS) rmsnorm_grad_kernel(const __grid_constant__ NormGradArgs a) {
   constexpr bool kRing = STAGES > 0;
-  static_assert(!kRing || (V == 8 && NV == 1), "a thread's part of a stage is eight elements");
-  extern __shared__ uint8_t ring[];
-  __shared__ float red[3][2][32];
+  static_assert(!kRing || V == 8, "a piece of the ring is 16 bytes of eight elements");
+  constexpr int kHeld = kRing ? NV : 1;                      // vectors of s, d_out and the weight that a thread holds at a time
+  // (a ring of two vectors a thread is for rows that fill the first ones: its block is THREADS wide, and addresses are offsets known to the compiler)
+  constexpr bool kFixed = kRing && NV > 1;
+  const uint32_t threads = kFixed ? THREADS : blockDim.x;
+  extern __shared__ __align__(16) uint8_t ring[];
+  __shared__ __align__(16) float red[3][2][32];
   const int tid = threadIdx.x;
-  const uint32_t stage_bytes = norm_grad_thread_bytes<IO, DY, DX>() * blockDim.x, place = smem_u32(ring) + tid * 16;
-  const uint32_t dy_at = RingRow<IO>::kPieces * blockDim.x * 16, stream_at = dy_at + RingRow<DY>::kPieces * blockDim.x * 16;
+  const uint32_t pitch = threads * 16, vector_bytes = norm_grad_thread_bytes<IO, DY, DX>() * threads, stage_bytes = NV * vector_bytes;
+  const uint32_t place = smem_u32(ring) + tid * 16, dy_at = RingRow<IO>::kPieces * pitch, stream_at = dy_at + RingRow<DY>::kPieces * pitch;
+  bool inside[NV];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) inside[j] = (kFixed && j + 1 < NV) || (tid + j * threads) * V < a.d;
+  clear_row_sums(&red[0][0][0], 3 * 2 * 32);
   grid_dependency_wait();
-  auto fetch = [&](int row, int stage) {
-    const int col = tid * V;
-    if (row < a.T && col < a.d) {
+  int next_row = blockIdx.x;                                 // the next to be fetched, and where the thread's first vector of it is
+  const IO* next_s = static_cast<const IO*>(a.sum) + next_row * a.sum_stride + tid * V;
+  const DY* next_dy = static_cast<const DY*>(a.d_out) + next_row * a.d_out_stride + tid * V;
+  const DX* next_stream = static_cast<const DX*>(a.d_stream) + next_row * a.d_stream_stride + tid * V;
+  auto fetch = [&](int stage) {
+    if (next_row < a.T) {
       const uint32_t at = place + stage * stage_bytes;
-      RingRow<IO>::fetch(at, static_cast<const IO*>(a.sum) + row * a.sum_stride + col);
-      RingRow<DY>::fetch(at + dy_at, static_cast<const DY*>(a.d_out) + row * a.d_out_stride + col);
-      if (a.d_stream) RingRow<DX>::fetch(at + stream_at, static_cast<const DX*>(a.d_stream) + row * a.d_stream_stride + col);
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        if (inside[j]) {
+          RingRow<IO>::fetch(at + j * vector_bytes, next_s + j * threads * V, pitch);
+          RingRow<DY>::fetch(at + j * vector_bytes + dy_at, next_dy + j * threads * V, pitch);
+          if (a.d_stream) RingRow<DX>::fetch(at + j * vector_bytes + stream_at, next_stream + j * threads * V, pitch);
+        }
+      }
+      next_row += gridDim.x;
+      next_s += gridDim.x * a.sum_stride;
+      next_dy += gridDim.x * a.d_out_stride;
+      next_stream += gridDim.x * a.d_stream_stride;
     }
     copy_commit();
   };
   if constexpr (kRing) {
 #pragma unroll
-    for (int q = 0; q < STAGES - 1; ++q) fetch(blockIdx.x + q * gridDim.x, q);
+    for (int q = 0; q < STAGES - 1; ++q) fetch(q);
   }
-  float w[V], dw[NV][V];                                     // w: kept by the ring's threads
-  if (kRing && tid * V < a.d) load_weight<V>(a.weight, a.weight_f32, tid * V, w);
+  float s[kHeld][V], dy[kHeld][V], w[kHeld][V], dw[NV][V];
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
+    if constexpr (kRing) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) w[j][i] = 0.f;
+      if (inside[j]) load_weight<V>(a.weight, a.weight_f32, (tid + j * threads) * V, w[j]);
+    }
 #pragma unroll
     for (int i = 0; i < V; ++i) dw[j][i] = 0.f;
   }
   int turn = 0, stage = 0;
-  for (int row = blockIdx.x; row < a.T; row += gridDim.x, turn ^= 1) {
+  DX* out_row = static_cast<DX*>(a.d_x) + blockIdx.x * a.d_x_stride;
+  for (int row = blockIdx.x; row < a.T; row += gridDim.x, turn ^= 1, out_row += gridDim.x * a.d_x_stride) {
     const IO* s_row = static_cast<const IO*>(a.sum) + row * a.sum_stride;
     const DY* dy_row = static_cast<const DY*>(a.d_out) + row * a.d_out_stride;
     const uint32_t at = place + stage * stage_bytes;
     if constexpr (kRing) {
       // (the stage that is fetched into was read by this thread alone, a turn ago)
-      fetch(row + (STAGES - 1) * gridDim.x, stage == 0 ? STAGES - 1 : stage - 1);
+      fetch(stage == 0 ? STAGES - 1 : stage - 1);
       copy_wait<STAGES - 1>();
       stage = stage + 1 == STAGES ? 0 : stage + 1;
-    }
-    // s times `by`, d_out (and the weight, where it is not kept) of the thread's vector j; false past the row's end
-    auto read = [&](int j, float by, float (&s)[V], float (&dy)[V]) {
-      const int col = (tid + j * blockDim.x) * V;
-      if (col >= a.d) return false;
-      if constexpr (kRing) {
-        RingRow<IO>::read(at, s);
-        RingRow<DY>::read(at + dy_at, dy);
-      } else {
-        unpack(load_pack<IO, V>(s_row + col), s);
-        unpack(load_pack<DY, V>(dy_row + col), dy);
-        load_weight<V>(a.weight, a.weight_f32, col, w);
-      }
 #pragma unroll
-      for (int i = 0; i < V; ++i) s[i] *= by;
+      for (int j = 0; j < NV; ++j) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) s[j][i] = dy[j][i] = 0.f;
+        if (inside[j]) {
+          RingRow<IO>::read(at + j * vector_bytes, pitch, s[j]);
+          RingRow<DY>::read(at + j * vector_bytes + dy_at, pitch, dy[j]);
+        }
+      }
+    }
+    // vector j of s times `by`, d_out and the weight into the one place held (those of the ring are there); false past the row's end
+    auto read = [&](int j, float by) {
+      const int col = (tid + j * threads) * V;
+      if (!inside[j]) return false;
+      unpack(load_pack<IO, V>(s_row + col), s[0]);
+      unpack(load_pack<DY, V>(dy_row + col), dy[0]);
+      load_weight<V>(a.weight, a.weight_f32, col, w[0]);
+#pragma unroll
+      for (int i = 0; i < V; ++i) s[0][i] *= by;
       return true;
     };
     auto add_up = [&](float by, float (&sums)[2], float (*share)[32]) {      // s^2 and weight d_out s
       sums[0] = sums[1] = 0.f;
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
-        float s[V], dy[V];
-        if (!read(j, by, s, dy)) continue;
+        const int h = kRing ? j : 0;
+        if (!kRing && !read(j, by)) continue;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-          sums[0] += s[i] * s[i];
-          sums[1] += dy[i] * w[i] * s[i];
+          sums[0] += s[h][i] * s[h][i];
+          sums[1] += dy[h][i] * w[h][i] * s[h][i];
         }
       }
       row_sum(sums, share);
     };
     float sums[2], by = 1.f;
     add_up(by, sums, red[turn]);
-    float rstd = rsqrtf(sums[0] / a.d + a.eps);
+    float rstd = rsqrtf(sums[0] * a.inv_d + a.eps);
     if (__float_as_uint(sums[0]) == 0x7f800000u) {
       by = kNormRescue;
+#pragma unroll
+      for (int j = 0; j < kHeld; ++j) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) s[j][i] *= by;
+      }
       __syncthreads();                                       // red[2] may still be read for an earlier row
       add_up(by, sums, red[2]);
-      rstd = rsqrtf(sums[0] / a.d);
+      rstd = rsqrtf(sums[0] * a.inv_d);
     }
-    const float step = rstd * by, mean = sums[1] * rstd / a.d;         // by which d out becomes d s; of weight d_out s rstd
+    // with unit = s rstd: d s = step (weight d_out) - back unit + d_stream
+    const float step = rstd * by, back = step * (sums[1] * rstd * a.inv_d);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int col = (tid + j * blockDim.x) * V;
-      float s[V], dy[V], dx[V];
-      if (!read(j, by, s, dy)) continue;
+      const int col = (tid + j * threads) * V, h = kRing ? j : 0;
+      float dx[V];
+      if (kRing ? !inside[j] : !read(j, by)) continue;
+#pragma unroll
+      for (int i = 0; i < V; ++i) dx[i] = 0.f;
+      if (a.d_stream) {
+        if constexpr (kRing) RingRow<DX>::read(at + j * vector_bytes + stream_at, pitch, dx);
+        else unpack(load_pack<DX, V>(static_cast<const DX*>(a.d_stream) + row * a.d_stream_stride + col), dx);
+      }
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        const float unit = s[i] * rstd;
-        dw[j][i] += dy[i] * unit;
-        dx[i] = step * (dy[i] * w[i] - unit * mean);
+        const float unit = s[h][i] * rstd;
+        dx[i] = (dx[i] - back * unit) + step * (dy[h][i] * w[h][i]);
+        dw[j][i] += dy[h][i] * unit;
       }
-      if (a.d_stream) {
-        float more[V];
-        if constexpr (kRing) RingRow<DX>::read(at + stream_at, more);
-        else unpack(load_pack<DX, V>(static_cast<const DX*>(a.d_stream) + row * a.d_stream_stride + col), more);
-#pragma unroll
-        for (int i = 0; i < V; ++i) dx[i] += more[i];
-      }
-      store_f32<DX, V>(static_cast<DX*>(a.d_x) + row * a.d_x_stride + col, dx);
+      store_f32<DX, V>(out_row + col, dx);
     }
   }
   if (a.partial) {
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int col = (tid + j * blockDim.x) * V;
-      if (col < a.d) store_f32<float, V>(a.partial + static_cast<size_t>(blockIdx.x) * a.d + col, dw[j]);
+      if (inside[j]) store_f32<float, V>(a.partial + static_cast<size_t>(blockIdx.x) * a.d + (tid + j * threads) * V, dw[j]);
     }
   }
   if constexpr (kRing) copy_wait<0>();

@@ -61,29 +61,50 @@ __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_gr
 template <int N>
 __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// Sums over the threads of a row: a warp, or (blockDim.x > 32) the whole block, every thread with the same result, added up in
-// the same order. red: 32 floats per value in shared memory; a buffer may be used again after the next barrier.
-template <int N>
-__device__ __forceinline__ void row_sum(float (&x)[N], float (*red)[32]) {
+// The sum over the threads of a row: a warp, or (blockDim.x > 32) the whole block, every thread with the same result, added up in the same order.
+// red: 32 floats in shared memory; a buffer may be used again after the next barrier.
+__device__ __forceinline__ float row_sum(float x, float* red) {
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[i] += __shfl_xor_sync(0xffffffffu, x[i], o);
-  }
-  if (blockDim.x == 32) return;
+  for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  if (blockDim.x == 32) return x;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-  if (lane == 0) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) red[i][warp] = x[i];
-  }
+  if (lane == 0) red[warp] = x;
   __syncthreads();
+  x = lane < warps ? red[lane] : 0.f;
 #pragma unroll
-  for (int i = 0; i < N; ++i) x[i] = lane < warps ? red[i][lane] : 0.f;
+  for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  return x;
+}
+// Two sums at once, for blocks that take many rows: within a warp they take the shuffles of one and another (half of the lanes carry each), the warps'
+// sums are read as vectors. red: 32 floats each, zero from the row's number of warps on.
+__device__ __forceinline__ void row_sum(float (&x)[2], float (*red)[32]) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+  const bool upper = lane & 16;
+  float mine = (upper ? x[1] : x[0]) + __shfl_xor_sync(0xffffffffu, upper ? x[0] : x[1], 16);
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[i] += __shfl_xor_sync(0xffffffffu, x[i], o);
+  for (int o = 8; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+  if (blockDim.x == 32) {
+    x[0] = __shfl_sync(0xffffffffu, mine, 0);
+    x[1] = __shfl_sync(0xffffffffu, mine, 16);
+    return;
   }
+  if ((lane & 15) == 0) red[lane >> 4][warp] = mine;
+  __syncthreads();
+  x[0] = x[1] = 0.f;
+  for (int w = 0; w < warps; w += 4) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float4 y = *reinterpret_cast<const float4*>(&red[i][w]);
+      x[i] += (y.x + y.y) + (y.z + y.w);
+    }
+  }
+}
+
+// Before the first such sums on a block's buffers (`count` floats): the words of warps that are not there.
+__device__ __forceinline__ void clear_row_sums(float* red, int count) {
+  if (blockDim.x == 32) return;
+  for (int i = threadIdx.x; i < count; i += blockDim.x) red[i] = 0.f;
+  __syncthreads();
 }
 
 // V adjacent weights (fp32 or bf16; none: ones).

@@ -68,27 +68,28 @@ void launch_rmsnorm(const NormArgs& a, bool vectors, cudaStream_t st) {
     launch_kernel(residual_rmsnorm_kernel<IO, 1, 32, 1024, 1>, a.T, round_warp(ceil_div(a.d, 32)), 0, st, true, a);
 }
 
-// Blocks of the gradient kernel: as many as give an SM 1024 threads, by what the vector build takes (the order of the sums then does not depend on
-// alignment), of two rows at least where there are rows for every SM.
+// Blocks of the gradient kernel: as many as an SM takes of the vector build (the order of the sums then does not depend on alignment), of two rows at
+// least where there are rows for every SM.
 int norm_grad_blocks(int T, int d) {
-  const int threads = d <= 8192 ? round_warp(ceil_div(d, 8)) : 1024;
+  const int threads = d <= 2048 ? round_warp(ceil_div(d, 8)) : 512;
   const int per_sm = std::max(1, std::min(16, 1024 / threads));
-  return std::min(T, std::max(kSms, std::min(kSms * per_sm, T / 2)));
+  return std::min(T, std::max(kSms, std::min(kSms * (d <= 4096 ? per_sm : 1), T / 2)));
 }
-template <typename IO, typename DY, typename DX, int STAGES, int THREADS, int CTAS>
+template <typename IO, typename DY, typename DX, int NV, int STAGES, int THREADS, int CTAS>
 bool launch_rmsnorm_grad_ring(const NormGradArgs& a, int blocks, cudaStream_t st) {
-  const int threads = round_warp(ceil_div(a.d, 8));
-  const size_t smem = static_cast<size_t>(STAGES) * norm_grad_thread_bytes<IO, DY, DX>() * threads;
-  auto* kernel = rmsnorm_grad_kernel<IO, DY, DX, 8, 1, STAGES, THREADS, CTAS>;
-  if (smem > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess) return false;
+  const int threads = NV > 1 ? THREADS : round_warp(ceil_div(a.d, 8));
+  const size_t smem = static_cast<size_t>(STAGES) * NV * norm_grad_thread_bytes<IO, DY, DX>() * threads;
+  auto* kernel = rmsnorm_grad_kernel<IO, DY, DX, 8, NV, STAGES, THREADS, CTAS>;
+  if (smem > 46 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess) return false;
   launch_kernel(kernel, blocks, threads, smem, st, true, a);
   return true;
 }
 template <typename IO, typename DY, typename DX>
 bool launch_rmsnorm_grad(const NormGradArgs& a, int blocks, bool vectors, cudaStream_t st) {
   const int packs = ceil_div(a.d, 8);
-  if (vectors && packs <= 512) return launch_rmsnorm_grad_ring<IO, DY, DX, 3, 512, 2>(a, blocks, st);
-  if (vectors && packs <= 1024) return launch_rmsnorm_grad_ring<IO, DY, DX, 2, 1024, 1>(a, blocks, st);
+  if (vectors && packs <= 256) return launch_rmsnorm_grad_ring<IO, DY, DX, 1, 3, 256, 4>(a, blocks, st);
+  if (vectors && packs <= 512) return launch_rmsnorm_grad_ring<IO, DY, DX, 2, 3, 256, 2>(a, blocks, st);
+  if (vectors && packs <= 1024) return launch_rmsnorm_grad_ring<IO, DY, DX, 2, 2, 512, 1>(a, blocks, st);
   if (vectors)
     launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 8, 4, 0, 1024, 1>, blocks, round_warp(ceil_div(packs, 4)), 0, st, true, a);
   else if (a.d <= 4096)
@@ -426,8 +427,10 @@ int mtpc_residual_rmsnorm(const void* x, int64_t x_stride, const void* residual,
   a.d = d;
   a.group = scale_group;
   a.groups = scale_group ? ceil_div(d, scale_group) : 1;
+  while ((1 << a.group_shift) < scale_group) ++a.group_shift;
   a.weight_f32 = weight_dtype == MTPC_F32;
   a.eps = eps;
+  a.inv_d = 1.f / d;
   const bool vectors = d % 8 == 0 && rows_allow(x, x_stride, e, 8, T) && rows_allow(residual, residual_stride, e, 8, T) &&
                        rows_allow(weight, 0, element(weight_dtype), 8, 1) && rows_allow(out_sum, sum_stride, e, 8, T) &&
                        rows_allow(out, out_stride, e, 8, T) && rows_allow(out_codes, codes_stride, 1, 8, T);
@@ -483,6 +486,7 @@ int mtpc_residual_rmsnorm_backward(const void* sum, int64_t sum_stride, int32_t 
     a.d = d;
     a.weight_f32 = weight_dtype == MTPC_F32;
     a.eps = eps;
+    a.inv_d = 1.f / d;
     const bool vectors = d % 8 == 0 && rows_allow(sum, sum_stride, element(io_dtype), 8, T) && rows_allow(weight, 0, element(weight_dtype), 8, 1) &&
                          rows_allow(d_out, d_out_stride, element(d_out_dtype), 8, T) &&
                          rows_allow(d_sum, d_sum_stride, element(d_x_dtype), 8, T) && rows_allow(d_x, d_x_stride, element(d_x_dtype), 8, T);
