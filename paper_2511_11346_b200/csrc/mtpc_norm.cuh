@@ -208,178 +208,215 @@ struct NormGradArgs {
   float eps, inv_d;
 };
 
-// A thread's eight elements of a row in its own places of shared memory, in pieces of 16 bytes `pitch` apart, a piece's neighbours the other threads'.
-template <typename T>
-struct RingRow {
-  static constexpr int kPieces = sizeof(T) * 8 / 16;
-  static __device__ __forceinline__ void fetch(uint32_t at, const T* src, uint32_t pitch) {
-#pragma unroll
-    for (int i = 0; i < kPieces; ++i) copy_async16(at + i * pitch, reinterpret_cast<const uint8_t*>(src) + i * 16);
-  }
-  static __device__ __forceinline__ void read(uint32_t at, uint32_t pitch, float (&x)[8]) {
-    Pack<T, 8> p;
-    uint32_t* r = reinterpret_cast<uint32_t*>(p.e);
-#pragma unroll
-    for (int i = 0; i < kPieces; ++i)
-      asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                   : "=r"(r[4 * i]), "=r"(r[4 * i + 1]), "=r"(r[4 * i + 2]), "=r"(r[4 * i + 3])
-                   : "r"(at + i * pitch));
-    unpack(p, x);
-  }
-};
-// Bytes of a thread's part of a row.
-template <typename IO, typename DY, typename DX>
-__host__ __device__ constexpr int norm_grad_thread_bytes() { return 8 * (sizeof(IO) + sizeof(DY) + sizeof(DX)); }
-
-// Every block has every gridDim.x-th row and keeps its part of d weight in registers. STAGES > 0: rows come through shared memory, the next
-// STAGES - 1 on their way while one is worked on, every thread copying and reading its own elements (no barrier of their own). With one row at a
-// time in registers two blocks of 512 threads an SM waited for memory half of the time (8192 rows of 4096, bf16, d_out fp32: 88 us); with eight
-// elements a thread and the row read from the ring twice, shared memory and shuffles were the bound (74 us). Otherwise (wider rows, and rows that no
-// vectors fit) a row is read twice, the second time from L1 or L2.
-template <typename IO, typename DY, typename DX, int V, int NV, int STAGES, int THREADS, int CTAS>
+// Every block has every gridDim.x-th row and keeps its part of d weight in registers, NV vectors of eight elements a thread; its vectors of the next AHEAD
+// rows are on their way to registers. What bounds it is what the SM issues for a row beside its bytes, so the arithmetic goes by packed pairs: 8192 rows
+// of 4096 (bf16, d_out fp32) one by one 88 to 104 us, with rows fetched by cp.async through shared memory, where issuing the copies took 1000 of 3500
+// cycles a row, 65 to 78.
+template <typename IO, typename DY, typename DX, int NV, int AHEAD, int THREADS, int CTAS>
 __global__ void __launch_bounds__(THREADS, CTAS) rmsnorm_grad_kernel(const __grid_constant__ NormGradArgs a) {
-  constexpr bool kRing = STAGES > 0;
-  static_assert(!kRing || V == 8, "a piece of the ring is 16 bytes of eight elements");
-  constexpr int kHeld = kRing ? NV : 1;                      // vectors of s, d_out and the weight that a thread holds at a time
-  // (a ring of two vectors a thread is for rows that fill the first ones: its block is THREADS wide, and addresses are offsets known to the compiler)
-  constexpr bool kFixed = kRing && NV > 1;
-  const uint32_t threads = kFixed ? THREADS : blockDim.x;
-  extern __shared__ __align__(16) uint8_t ring[];
-  __shared__ __align__(16) float red[3][2][32];
-  const int tid = threadIdx.x;
-  const uint32_t pitch = threads * 16, vector_bytes = norm_grad_thread_bytes<IO, DY, DX>() * threads, stage_bytes = NV * vector_bytes;
-  const uint32_t place = smem_u32(ring) + tid * 16, dy_at = RingRow<IO>::kPieces * pitch, stream_at = dy_at + RingRow<DY>::kPieces * pitch;
+  __shared__ float red[3][32];
+  const int tid = threadIdx.x, threads = blockDim.x;
   bool inside[NV];
 #pragma unroll
-  for (int j = 0; j < NV; ++j) inside[j] = (kFixed && j + 1 < NV) || (tid + j * threads) * V < a.d;
-  clear_row_sums(&red[0][0][0], 3 * 2 * 32);
+  for (int j = 0; j < NV; ++j) inside[j] = (tid + j * threads) * 8 < a.d;
+  for (int i = tid; i < 96; i += threads) red[i >> 5][i & 31] = 0.f;
+  __syncthreads();
   grid_dependency_wait();
-  int next_row = blockIdx.x;                                 // the next to be fetched, and where the thread's first vector of it is
-  const IO* next_s = static_cast<const IO*>(a.sum) + next_row * a.sum_stride + tid * V;
-  const DY* next_dy = static_cast<const DY*>(a.d_out) + next_row * a.d_out_stride + tid * V;
-  const DX* next_stream = static_cast<const DX*>(a.d_stream) + next_row * a.d_stream_stride + tid * V;
-  auto fetch = [&](int stage) {
-    if (next_row < a.T) {
-      const uint32_t at = place + stage * stage_bytes;
+  struct Row {
+    Raw8<IO> s[NV];
+    Raw8<DY> dy[NV];
+    Raw8<DX> stream[NV];
+  } ahead[AHEAD];
+  const IO* next_s = static_cast<const IO*>(a.sum) + blockIdx.x * a.sum_stride + tid * 8;          // the thread's first vector of the row to be fetched next
+  const DY* next_dy = static_cast<const DY*>(a.d_out) + blockIdx.x * a.d_out_stride + tid * 8;
+  const DX* next_stream = static_cast<const DX*>(a.d_stream) + blockIdx.x * a.d_stream_stride + tid * 8;
+  int next = blockIdx.x;
+  auto fetch = [&](Row& x) {
+    if (next < a.T) {
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
         if (inside[j]) {
-          RingRow<IO>::fetch(at + j * vector_bytes, next_s + j * threads * V, pitch);
-          RingRow<DY>::fetch(at + j * vector_bytes + dy_at, next_dy + j * threads * V, pitch);
-          if (a.d_stream) RingRow<DX>::fetch(at + j * vector_bytes + stream_at, next_stream + j * threads * V, pitch);
+          x.s[j].load(next_s + j * threads * 8);
+          x.dy[j].load(next_dy + j * threads * 8);
+          if (a.d_stream) x.stream[j].load(next_stream + j * threads * 8);
         }
       }
-      next_row += gridDim.x;
+      next += gridDim.x;
       next_s += gridDim.x * a.sum_stride;
       next_dy += gridDim.x * a.d_out_stride;
       next_stream += gridDim.x * a.d_stream_stride;
     }
-    copy_commit();
   };
-  if constexpr (kRing) {
 #pragma unroll
-    for (int q = 0; q < STAGES - 1; ++q) fetch(q);
+  for (int q = 0; q < AHEAD; ++q) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {             // (what lies past the row's end stays zero, and so does d_stream if there is none)
+      ahead[q].s[j].clear();
+      ahead[q].dy[j].clear();
+      ahead[q].stream[j].clear();
+    }
+    fetch(ahead[q]);
   }
-  float s[kHeld][V], dy[kHeld][V], w[kHeld][V], dw[NV][V];
+  uint64_t w[NV][4], dw[NV][4];
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    if constexpr (kRing) {
+    float x[8] = {};
+    if (inside[j]) load_weight<8>(a.weight, a.weight_f32, (tid + j * threads) * 8, x);
 #pragma unroll
-      for (int i = 0; i < V; ++i) w[j][i] = 0.f;
-      if (inside[j]) load_weight<V>(a.weight, a.weight_f32, (tid + j * threads) * V, w[j]);
+    for (int i = 0; i < 4; ++i) {
+      w[j][i] = pack2(x[2 * i], x[2 * i + 1]);
+      dw[j][i] = 0;
     }
-#pragma unroll
-    for (int i = 0; i < V; ++i) dw[j][i] = 0.f;
   }
-  int turn = 0, stage = 0;
-  DX* out_row = static_cast<DX*>(a.d_x) + blockIdx.x * a.d_x_stride;
-  for (int row = blockIdx.x; row < a.T; row += gridDim.x, turn ^= 1, out_row += gridDim.x * a.d_x_stride) {
-    const IO* s_row = static_cast<const IO*>(a.sum) + row * a.sum_stride;
-    const DY* dy_row = static_cast<const DY*>(a.d_out) + row * a.d_out_stride;
-    const uint32_t at = place + stage * stage_bytes;
-    if constexpr (kRing) {
-      // (the stage that is fetched into was read by this thread alone, a turn ago)
-      fetch(stage == 0 ? STAGES - 1 : stage - 1);
-      copy_wait<STAGES - 1>();
-      stage = stage + 1 == STAGES ? 0 : stage + 1;
+  int turn = 0;
+  DX* out = static_cast<DX*>(a.d_x) + blockIdx.x * a.d_x_stride + tid * 8;
+  auto work = [&](Row& mine) {
+    uint64_t s[NV][4], dy[NV][4];
+    Raw8<DX> stream[NV];
 #pragma unroll
-      for (int j = 0; j < NV; ++j) {
+    for (int j = 0; j < NV; ++j) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) s[j][i] = dy[j][i] = 0.f;
-        if (inside[j]) {
-          RingRow<IO>::read(at + j * vector_bytes, pitch, s[j]);
-          RingRow<DY>::read(at + j * vector_bytes + dy_at, pitch, dy[j]);
-        }
+      for (int i = 0; i < 4; ++i) {
+        s[j][i] = mine.s[j].pair(i);
+        dy[j][i] = mine.dy[j].pair(i);
       }
+      stream[j] = mine.stream[j];
     }
-    // vector j of s times `by`, d_out and the weight into the one place held (those of the ring are there); false past the row's end
-    auto read = [&](int j, float by) {
-      const int col = (tid + j * threads) * V;
-      if (!inside[j]) return false;
-      unpack(load_pack<IO, V>(s_row + col), s[0]);
-      unpack(load_pack<DY, V>(dy_row + col), dy[0]);
-      load_weight<V>(a.weight, a.weight_f32, col, w[0]);
-#pragma unroll
-      for (int i = 0; i < V; ++i) s[0][i] *= by;
-      return true;
-    };
-    auto add_up = [&](float by, float (&sums)[2], float (*share)[32]) {      // s^2 and weight d_out s
-      sums[0] = sums[1] = 0.f;
+    fetch(mine);
+    auto add_up = [&](float (&sums)[2], float* share) {        // s^2 and weight d_out s
+      uint64_t squares = 0, products = 0;
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
-        const int h = kRing ? j : 0;
-        if (!kRing && !read(j, by)) continue;
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-          sums[0] += s[h][i] * s[h][i];
-          sums[1] += dy[h][i] * w[h][i] * s[h][i];
+        for (int i = 0; i < 4; ++i) {
+          squares = fma2(s[j][i], s[j][i], squares);
+          products = fma2(mul2(dy[j][i], w[j][i]), s[j][i], products);
         }
       }
-      row_sum(sums, share);
+      const float2 x = unpack2(squares), y = unpack2(products);
+      sums[0] = x.x + x.y;
+      sums[1] = y.x + y.y;
+      row_sums(sums, share);
     };
     float sums[2], by = 1.f;
-    add_up(by, sums, red[turn]);
+    add_up(sums, red[turn]);
     float rstd = rsqrtf(sums[0] * a.inv_d + a.eps);
     if (__float_as_uint(sums[0]) == 0x7f800000u) {
       by = kNormRescue;
 #pragma unroll
-      for (int j = 0; j < kHeld; ++j) {
+      for (int j = 0; j < NV; ++j) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) s[j][i] *= by;
+        for (int i = 0; i < 4; ++i) s[j][i] = mul2(s[j][i], pack2(by, by));
       }
       __syncthreads();                                       // red[2] may still be read for an earlier row
-      add_up(by, sums, red[2]);
+      add_up(sums, red[2]);
       rstd = rsqrtf(sums[0] * a.inv_d);
     }
     // with unit = s rstd: d s = step (weight d_out) - back unit + d_stream
+    const float step = rstd * by, back = -step * (sums[1] * rstd * a.inv_d);
+    const uint64_t rstd2 = pack2(rstd, rstd), step2 = pack2(step, step), back2 = pack2(back, back);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      uint64_t dx[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint64_t unit = mul2(s[j][i], rstd2);
+        dx[i] = fma2(step2, mul2(dy[j][i], w[j][i]), fma2(back2, unit, stream[j].pair(i)));
+        dw[j][i] = fma2(dy[j][i], unit, dw[j][i]);
+      }
+      if (inside[j]) store_pairs<DX>(out + j * threads * 8, dx);
+    }
+    out += gridDim.x * a.d_x_stride;
+    turn ^= 1;
+  };
+  for (int row = blockIdx.x; row < a.T; row += AHEAD * gridDim.x) {
+#pragma unroll
+    for (int q = 0; q < AHEAD; ++q)
+      if (row + q * static_cast<int>(gridDim.x) < a.T) work(ahead[q]);
+  }
+  if (a.partial) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (inside[j]) store_pairs<float>(a.partial + static_cast<size_t>(blockIdx.x) * a.d + (tid + j * threads) * 8, dw[j]);
+  }
+  grid_launch_dependents();
+}
+
+// The same of rows that no vectors fit, or that are wider than the registers of a block: element after element of a thread, read twice, the second time
+// from L1 or L2.
+template <typename IO, typename DY, typename DX, int V, int NV>
+__global__ void __launch_bounds__(1024) rmsnorm_grad_plain_kernel(const __grid_constant__ NormGradArgs a) {
+  __shared__ float red[2][32];
+  const int tid = threadIdx.x;
+  grid_dependency_wait();
+  float dw[NV][V];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) dw[j][i] = 0.f;
+  }
+  for (int row = blockIdx.x; row < a.T; row += gridDim.x) {
+    const IO* s_row = static_cast<const IO*>(a.sum) + row * a.sum_stride;
+    const DY* dy_row = static_cast<const DY*>(a.d_out) + row * a.d_out_stride;
+    float s[V], dy[V], w[V];
+    auto read = [&](int j, float by) {                       // vector j of s times `by`, d_out and the weight; false past the row's end
+      const int col = (tid + j * blockDim.x) * V;
+      if (col >= a.d) return false;
+      unpack(load_pack<IO, V>(s_row + col), s);
+      unpack(load_pack<DY, V>(dy_row + col), dy);
+      load_weight<V>(a.weight, a.weight_f32, col, w);
+#pragma unroll
+      for (int i = 0; i < V; ++i) s[i] *= by;
+      return true;
+    };
+    auto add_up = [&](float by, float (&sums)[2]) {           // s^2 and weight d_out s
+      sums[0] = sums[1] = 0.f;
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        if (!read(j, by)) continue;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          sums[0] += s[i] * s[i];
+          sums[1] += dy[i] * w[i] * s[i];
+        }
+      }
+      __syncthreads();                                       // the last sums have been read
+      sums[0] = row_sum(sums[0], red[0]);
+      sums[1] = row_sum(sums[1], red[1]);
+    };
+    float sums[2], by = 1.f;
+    add_up(by, sums);
+    float rstd = rsqrtf(sums[0] * a.inv_d + a.eps);
+    if (__float_as_uint(sums[0]) == 0x7f800000u) {
+      by = kNormRescue;
+      add_up(by, sums);
+      rstd = rsqrtf(sums[0] * a.inv_d);
+    }
     const float step = rstd * by, back = step * (sums[1] * rstd * a.inv_d);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int col = (tid + j * threads) * V, h = kRing ? j : 0;
+      const int col = (tid + j * blockDim.x) * V;
       float dx[V];
-      if (kRing ? !inside[j] : !read(j, by)) continue;
+      if (!read(j, by)) continue;
 #pragma unroll
       for (int i = 0; i < V; ++i) dx[i] = 0.f;
-      if (a.d_stream) {
-        if constexpr (kRing) RingRow<DX>::read(at + j * vector_bytes + stream_at, pitch, dx);
-        else unpack(load_pack<DX, V>(static_cast<const DX*>(a.d_stream) + row * a.d_stream_stride + col), dx);
-      }
+      if (a.d_stream) unpack(load_pack<DX, V>(static_cast<const DX*>(a.d_stream) + row * a.d_stream_stride + col), dx);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        const float unit = s[h][i] * rstd;
-        dx[i] = (dx[i] - back * unit) + step * (dy[h][i] * w[h][i]);
-        dw[j][i] += dy[h][i] * unit;
+        const float unit = s[i] * rstd;
+        dx[i] = (dx[i] - back * unit) + step * (dy[i] * w[i]);
+        dw[j][i] += dy[i] * unit;
       }
-      store_f32<DX, V>(out_row + col, dx);
+      store_f32<DX, V>(static_cast<DX*>(a.d_x) + row * a.d_x_stride + col, dx);
     }
   }
   if (a.partial) {
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      if (inside[j]) store_f32<float, V>(a.partial + static_cast<size_t>(blockIdx.x) * a.d + (tid + j * threads) * V, dw[j]);
+      const int col = (tid + j * blockDim.x) * V;
+      if (col < a.d) store_f32<float, V>(a.partial + static_cast<size_t>(blockIdx.x) * a.d + col, dw[j]);
     }
   }
-  if constexpr (kRing) copy_wait<0>();
   grid_launch_dependents();
 }
 

@@ -53,14 +53,6 @@ __device__ __forceinline__ void store_f32(T* p, const float (&x)[V]) {
   store_pack<T, V>(p, o);
 }
 
-// 16 bytes from global to shared memory without registers; they are there once the thread has waited for the group they were committed in.
-__device__ __forceinline__ void copy_async16(uint32_t dst_smem, const void* src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst_smem), "l"(src) : "memory");
-}
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
 // The sum over the threads of a row: a warp, or (blockDim.x > 32) the whole block, every thread with the same result, added up in the same order.
 // red: 32 floats in shared memory; a buffer may be used again after the next barrier.
 __device__ __forceinline__ float row_sum(float x, float* red) {
@@ -75,36 +67,76 @@ __device__ __forceinline__ float row_sum(float x, float* red) {
   for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
   return x;
 }
-// Two sums at once, for blocks that take many rows: within a warp they take the shuffles of one and another (half of the lanes carry each), the warps'
-// sums are read as vectors. red: 32 floats each, zero from the row's number of warps on.
-__device__ __forceinline__ void row_sum(float (&x)[2], float (*red)[32]) {
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+// Two sums at once, of a block of at most sixteen warps: half of the lanes carry each. red: 32 floats, zero from the number of warps on (and from 16 and it on).
+__device__ __forceinline__ void row_sums(float (&x)[2], float* red) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const bool upper = lane & 16;
   float mine = (upper ? x[1] : x[0]) + __shfl_xor_sync(0xffffffffu, upper ? x[0] : x[1], 16);
 #pragma unroll
   for (int o = 8; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
-  if (blockDim.x == 32) {
-    x[0] = __shfl_sync(0xffffffffu, mine, 0);
-    x[1] = __shfl_sync(0xffffffffu, mine, 16);
-    return;
-  }
-  if ((lane & 15) == 0) red[lane >> 4][warp] = mine;
-  __syncthreads();
-  x[0] = x[1] = 0.f;
-  for (int w = 0; w < warps; w += 4) {
+  if (blockDim.x > 32) {
+    if ((lane & 15) == 0) red[lane + warp] = mine;
+    __syncthreads();
+    mine = red[lane];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const float4 y = *reinterpret_cast<const float4*>(&red[i][w]);
-      x[i] += (y.x + y.y) + (y.z + y.w);
-    }
+    for (int o = 8; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
   }
+  x[0] = __shfl_sync(0xffffffffu, mine, 0);
+  x[1] = __shfl_sync(0xffffffffu, mine, 16);
 }
 
-// Before the first such sums on a block's buffers (`count` floats): the words of warps that are not there.
-__device__ __forceinline__ void clear_row_sums(float* red, int count) {
-  if (blockDim.x == 32) return;
-  for (int i = threadIdx.x; i < count; i += blockDim.x) red[i] = 0.f;
-  __syncthreads();
+// Two fp32 values as one operand: the packed multiply-adds do both in one instruction.
+__device__ __forceinline__ uint64_t pack2(float lo, float hi) {
+  uint64_t d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
+  return d;
+}
+__device__ __forceinline__ float2 unpack2(uint64_t x) {
+  float2 d;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(d.x), "=f"(d.y) : "l"(x));
+  return d;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+
+// Eight adjacent elements as they were read, by a load that stays where it is written; and as four pairs of fp32.
+template <typename T>
+struct Raw8 {
+  uint32_t r[2 * sizeof(T)];
+  __device__ __forceinline__ void load(const T* p) {
+    if constexpr (sizeof(T) == 4)
+      asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                   : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                   : "l"(p));
+    else
+      asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "l"(p));
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < static_cast<int>(2 * sizeof(T)); ++i) r[i] = 0;
+  }
+  __device__ __forceinline__ uint64_t pair(int i) const {
+    if constexpr (sizeof(T) == 4) return pack2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1]));
+    else return pack2(__uint_as_float(r[i] << 16), __uint_as_float(r[i] & 0xffff0000u));
+  }
+};
+template <typename T>
+__device__ __forceinline__ void store_pairs(T* p, const uint64_t (&x)[4]) {
+  float y[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 v = unpack2(x[i]);
+    y[2 * i] = v.x, y[2 * i + 1] = v.y;
+  }
+  store_f32<T, 8>(p, y);
 }
 
 // V adjacent weights (fp32 or bf16; none: ones).

@@ -71,36 +71,29 @@ void launch_rmsnorm(const NormArgs& a, bool vectors, cudaStream_t st) {
 // Blocks of the gradient kernel: as many as an SM takes of the vector build (the order of the sums then does not depend on alignment), of two rows at
 // least where there are rows for every SM.
 int norm_grad_blocks(int T, int d) {
-  const int threads = d <= 2048 ? round_warp(ceil_div(d, 8)) : 512;
-  const int per_sm = std::max(1, std::min(16, 1024 / threads));
-  return std::min(T, std::max(kSms, std::min(kSms * (d <= 4096 ? per_sm : 1), T / 2)));
-}
-template <typename IO, typename DY, typename DX, int NV, int STAGES, int THREADS, int CTAS>
-bool launch_rmsnorm_grad_ring(const NormGradArgs& a, int blocks, cudaStream_t st) {
-  const int threads = NV > 1 ? THREADS : round_warp(ceil_div(a.d, 8));
-  const size_t smem = static_cast<size_t>(STAGES) * NV * norm_grad_thread_bytes<IO, DY, DX>() * threads;
-  auto* kernel = rmsnorm_grad_kernel<IO, DY, DX, 8, NV, STAGES, THREADS, CTAS>;
-  if (smem > 46 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess) return false;
-  launch_kernel(kernel, blocks, threads, smem, st, true, a);
-  return true;
+  const int per_sm = d > 4096 ? 1 : d > 2048 ? 2 : std::min(16, 512 / round_warp(ceil_div(d, 8)));
+  return std::min(T, std::max(kSms, std::min(kSms * per_sm, T / 2)));
 }
 template <typename IO, typename DY, typename DX>
-bool launch_rmsnorm_grad(const NormGradArgs& a, int blocks, bool vectors, cudaStream_t st) {
+void launch_rmsnorm_grad(const NormGradArgs& a, int blocks, bool vectors, cudaStream_t st) {
   const int packs = ceil_div(a.d, 8);
-  if (vectors && packs <= 256) return launch_rmsnorm_grad_ring<IO, DY, DX, 1, 3, 256, 4>(a, blocks, st);
-  if (vectors && packs <= 512) return launch_rmsnorm_grad_ring<IO, DY, DX, 2, 3, 256, 2>(a, blocks, st);
-  if (vectors && packs <= 1024) return launch_rmsnorm_grad_ring<IO, DY, DX, 2, 2, 512, 1>(a, blocks, st);
-  if (vectors)
-    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 8, 4, 0, 1024, 1>, blocks, round_warp(ceil_div(packs, 4)), 0, st, true, a);
+  if (vectors && packs <= 256)
+    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 1, 1, 256, 2>, blocks, round_warp(packs), 0, st, true, a);
+  else if (vectors && packs <= 512)
+    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 2, 1, 256, 2>, blocks, round_warp(ceil_div(packs, 2)), 0, st, true, a);
+  else if (vectors && packs <= 1024)
+    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 2, 1, 512, 1>, blocks, round_warp(ceil_div(packs, 2)), 0, st, true, a);
+  else if (vectors)
+    launch_kernel(rmsnorm_grad_plain_kernel<IO, DY, DX, 8, 4>, blocks, round_warp(ceil_div(packs, 4)), 0, st, true, a);
   else if (a.d <= 4096)
-    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 1, 4, 0, 1024, 1>, blocks, round_warp(ceil_div(a.d, 4)), 0, st, true, a);
+    launch_kernel(rmsnorm_grad_plain_kernel<IO, DY, DX, 1, 4>, blocks, round_warp(ceil_div(a.d, 4)), 0, st, true, a);
   else
-    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 1, 32, 0, 1024, 1>, blocks, round_warp(ceil_div(a.d, 32)), 0, st, true, a);
-  return true;
+    launch_kernel(rmsnorm_grad_plain_kernel<IO, DY, DX, 1, 32>, blocks, round_warp(ceil_div(a.d, 32)), 0, st, true, a);
 }
 template <typename IO, typename DY>
-bool launch_rmsnorm_grad(const NormGradArgs& a, int dx_dtype, int blocks, bool vectors, cudaStream_t st) {
-  return dx_dtype == MTPC_F32 ? launch_rmsnorm_grad<IO, DY, float>(a, blocks, vectors, st) : launch_rmsnorm_grad<IO, DY, __nv_bfloat16>(a, blocks, vectors, st);
+void launch_rmsnorm_grad(const NormGradArgs& a, int dx_dtype, int blocks, bool vectors, cudaStream_t st) {
+  if (dx_dtype == MTPC_F32) launch_rmsnorm_grad<IO, DY, float>(a, blocks, vectors, st);
+  else launch_rmsnorm_grad<IO, DY, __nv_bfloat16>(a, blocks, vectors, st);
 }
 
 // ---------------------------------------------------------------- embedding
@@ -490,16 +483,12 @@ int mtpc_residual_rmsnorm_backward(const void* sum, int64_t sum_stride, int32_t 
     const bool vectors = d % 8 == 0 && rows_allow(sum, sum_stride, element(io_dtype), 8, T) && rows_allow(weight, 0, element(weight_dtype), 8, 1) &&
                          rows_allow(d_out, d_out_stride, element(d_out_dtype), 8, T) &&
                          rows_allow(d_sum, d_sum_stride, element(d_x_dtype), 8, T) && rows_allow(d_x, d_x_stride, element(d_x_dtype), 8, T);
-    bool ok;
-    if (io_dtype == MTPC_F32)
-      ok = d_out_dtype == MTPC_F32 ? launch_rmsnorm_grad<float, float>(a, d_x_dtype, blocks, vectors, st)
-                                   : launch_rmsnorm_grad<float, __nv_bfloat16>(a, d_x_dtype, blocks, vectors, st);
-    else
-      ok = d_out_dtype == MTPC_F32 ? launch_rmsnorm_grad<__nv_bfloat16, float>(a, d_x_dtype, blocks, vectors, st)
-                                   : launch_rmsnorm_grad<__nv_bfloat16, __nv_bfloat16>(a, d_x_dtype, blocks, vectors, st);
-    if (!ok) {
-      cudaGetLastError();
-      return MTPC_ERR_CUDA;
+    if (io_dtype == MTPC_F32) {
+      if (d_out_dtype == MTPC_F32) launch_rmsnorm_grad<float, float>(a, d_x_dtype, blocks, vectors, st);
+      else launch_rmsnorm_grad<float, __nv_bfloat16>(a, d_x_dtype, blocks, vectors, st);
+    } else {
+      if (d_out_dtype == MTPC_F32) launch_rmsnorm_grad<__nv_bfloat16, float>(a, d_x_dtype, blocks, vectors, st);
+      else launch_rmsnorm_grad<__nv_bfloat16, __nv_bfloat16>(a, d_x_dtype, blocks, vectors, st);
     }
   }
   if (d_weight)
