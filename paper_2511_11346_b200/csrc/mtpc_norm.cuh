@@ -4,8 +4,7 @@
 // (d s is the gradient of x and of residual alike.) Everything between the loads and the one rounding of each output is fp32.
 //
 // Both are streams: a row is read once, into registers, and everything is formed from there. A row is a warp's up to 64 vectors of eight
-// elements, beyond that a block's with one vector a thread, so that a single row (one sequence being decoded) is spread over as
-// many warps as it can be.
+// elements, beyond that a block's with two vectors a thread.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp8.h>
@@ -37,6 +36,12 @@ struct NormArgs {
 
 // Largest magnitude as the bits of an fp32: compared as integers a NaN is larger than everything, so it is not lost.
 __device__ __forceinline__ unsigned magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+// The larger magnitude of two values (of either sign), NaN if one is.
+__device__ __forceinline__ float larger(float x, float y) {
+  float d;
+  asm("max.NaN.xorsign.abs.f32 %0, %1, %2;" : "=f"(d) : "f"(x), "f"(y));
+  return d;
+}
 
 // What a code of 1 stands for where the largest magnitude is `bits`.
 __device__ __forceinline__ float code_scale(unsigned bits) {
@@ -50,56 +55,166 @@ __device__ __forceinline__ float2 code_factors(float scale) {
   return make_float2(first, __fdividef(1.f, scale * first));          // (scale * first is between 2^-100 and 2^120)
 }
 
-template <typename IO, int V, int NV, int THREADS, int CTAS>
+// The largest magnitude of the row's columns, every thread with the same.
+__device__ __forceinline__ unsigned row_max(unsigned m, unsigned* share) {
+  m = __reduce_max_sync(0xffffffffu, m);
+  if (blockDim.x > 32) {
+    const int lane = threadIdx.x & 31;
+    __syncthreads();                                         // `share` may still be read
+    if (lane == 0) share[threadIdx.x >> 5] = m;
+    __syncthreads();
+    m = __reduce_max_sync(0xffffffffu, lane < static_cast<int>(blockDim.x >> 5) ? share[lane] : 0u);
+  }
+  return m;
+}
+
+// NV vectors of eight elements a thread. Beside its bytes a row costs what an SM issues for it, so the arithmetic goes by packed pairs: with 8-bit
+// output, 2005 rows of 4096, element by element 16.6 to 24 us.
+template <typename IO, int NV, int THREADS, int CTAS>
 __global__ void __launch_bounds__(THREADS, CTAS) residual_rmsnorm_kernel(const __grid_constant__ NormArgs a) {
   __shared__ float red[2][32];
-  __shared__ unsigned group_max[V == 1 ? kNormMaxWidth / kNormMinGroup : 1];
   const int row = blockIdx.x * blockDim.y + threadIdx.y;
-  const int tid = threadIdx.x, lane = tid & 31;
-  if (V == 1 && a.codes != nullptr) {            // (rows of single elements are a block's: blockDim.y = 1)
-    for (int g = tid; g < a.groups && a.group != 0; g += blockDim.x) group_max[g] = 0;
+  const int tid = threadIdx.x, lane = tid & 31, threads = blockDim.x;
+  grid_dependency_wait();
+  grid_launch_dependents();
+  if (row >= a.T) return;                                    // a whole warp, or no thread
+  uint64_t s[NV][4];
+  {
+    Raw8<IO> x[NV], r[NV];
+    const IO* x_row = static_cast<const IO*>(a.x) + row * a.x_stride + tid * 8;
+    const IO* r_row = static_cast<const IO*>(a.residual) + row * a.residual_stride + tid * 8;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      x[j].clear();
+      if ((tid + j * threads) * 8 < a.d) {
+        x[j].load(x_row + j * threads * 8);
+        if (a.residual) r[j].load(r_row + j * threads * 8);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[j][i] = x[j].pair(i);
+      if ((tid + j * threads) * 8 < a.d) {
+        if (a.residual) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[j][i] = add2(s[j][i], r[j].pair(i));
+        }
+        if (a.sum) store_pairs<IO>(static_cast<IO*>(a.sum) + row * a.sum_stride + (tid + j * threads) * 8, s[j]);
+      }
+    }
+  }
+  auto squares = [&]() {
+    uint64_t sum = 0;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum = fma2(s[j][i], s[j][i], sum);
+    }
+    const float2 x = unpack2(sum);
+    return x.x + x.y;
+  };
+  float square = row_sum(squares(), red[0]);
+  float rstd = rsqrtf(square * a.inv_d + a.eps);
+  if (__float_as_uint(square) == 0x7f800000u) {              // the same in every thread of the row
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[j][i] = mul2(s[j][i], pack2(kNormRescue, kNormRescue));
+    }
+    square = row_sum(squares(), red[1]);
+    rstd = rsqrtf(square * a.inv_d);
+  }
+  const uint64_t rstd2 = pack2(rstd, rstd);
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int col = (tid + j * threads) * 8;
+    if (col < a.d) {
+      float w[8];
+      load_weight<8>(a.weight, a.weight_f32, col, w);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[j][i] = mul2(mul2(s[j][i], rstd2), pack2(w[2 * i], w[2 * i + 1]));
+      if (a.out) store_pairs<IO>(static_cast<IO*>(a.out) + row * a.out_stride + col, s[j]);
+    }
+  }
+  if (a.codes == nullptr) return;
+
+  // The scale of every vector's group, then its codes. (Columns past the row's end are zeros.)
+  unsigned largest[NV];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    float m = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 x = unpack2(s[j][i]);
+      m = larger(larger(m, x.x), x.y);
+    }
+    largest[j] = magnitude(m);
+  }
+  float* scales = a.scales + static_cast<long long>(row) * a.groups;
+  if (a.group == 0) {
+    unsigned m = largest[0];
+#pragma unroll
+    for (int j = 1; j < NV; ++j) m = max(m, largest[j]);
+    m = row_max(m, reinterpret_cast<unsigned*>(red[1]));
+#pragma unroll
+    for (int j = 0; j < NV; ++j) largest[j] = m;
+    if (tid == 0) scales[0] = code_scale(m);
+  } else {
+    const int lanes = a.group / 8;                           // 4 to 16 lanes hold a group
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+#pragma unroll
+      for (int o = 1; o < 16; o <<= 1)
+        if (o < lanes) largest[j] = max(largest[j], __shfl_xor_sync(0xffffffffu, largest[j], o));
+      const int col = (tid + j * threads) * 8;
+      if (col < a.d && (lane & (lanes - 1)) == 0) scales[col >> a.group_shift] = code_scale(largest[j]);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int col = (tid + j * threads) * 8;
+    if (col >= a.d) continue;
+    const float2 by = code_factors(code_scale(largest[j]));
+    Pack<uint16_t, 4> o;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint64_t q = s[j][i];
+      if (by.x != 1.f) q = mul2(q, pack2(by.x, by.x));
+      const float2 x = unpack2(mul2(q, pack2(by.y, by.y)));
+      o.e[i] = __nv_cvt_float2_to_fp8x2(x, __NV_SATFINITE, __NV_E4M3);
+    }
+    store_pack<uint16_t, 4>(reinterpret_cast<uint16_t*>(a.codes + row * a.codes_stride + col), o);
+  }
+}
+
+// The same of rows that no vectors fit: a block per row, NV single elements a thread, 32 adjacent ones to a warp.
+template <typename IO, int NV>
+__global__ void __launch_bounds__(1024) residual_rmsnorm_plain_kernel(const __grid_constant__ NormArgs a) {
+  __shared__ float red[2][32];
+  __shared__ unsigned group_max[kNormMaxWidth / kNormMinGroup];
+  const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 31;
+  if (a.codes != nullptr && a.group != 0) {
+    for (int g = tid; g < a.groups; g += blockDim.x) group_max[g] = 0;
     __syncthreads();
   }
   grid_dependency_wait();
   grid_launch_dependents();
-  if (row >= a.T) return;                                    // a whole warp, or no thread
   const IO* x = static_cast<const IO*>(a.x) + row * a.x_stride;
-  const IO* residual = static_cast<const IO*>(a.residual) + (a.residual ? row * a.residual_stride : 0);
-  IO* sum = static_cast<IO*>(a.sum) + (a.sum ? row * a.sum_stride : 0);
-
-  float s[NV][V];
-  {
-    Pack<IO, V> px[NV], pr[NV];
+  const IO* residual = static_cast<const IO*>(a.residual) + row * a.residual_stride;
+  float s[NV];
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const int col = (tid + j * blockDim.x) * V;
-      if (col < a.d) {
-        px[j] = load_pack<IO, V>(x + col);
-        if (a.residual) pr[j] = load_pack<IO, V>(residual + col);
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const int col = (tid + j * blockDim.x) * V;
-#pragma unroll
-      for (int i = 0; i < V; ++i) s[j][i] = 0.f;
-      if (col < a.d) {
-        unpack(px[j], s[j]);
-        if (a.residual) {
-          float r[V];
-          unpack(pr[j], r);
-#pragma unroll
-          for (int i = 0; i < V; ++i) s[j][i] += r[i];
-        }
-        if (a.sum) store_f32<IO, V>(sum + col, s[j]);
-      }
-    }
+  for (int j = 0; j < NV; ++j) {
+    const int col = tid + j * blockDim.x;
+    s[j] = 0.f;
+    if (col < a.d) s[j] = a.residual ? to_f32(x[col]) + to_f32(residual[col]) : to_f32(x[col]);
   }
   float square = 0.f;
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-#pragma unroll
-    for (int i = 0; i < V; ++i) square += s[j][i] * s[j][i];
+    const int col = tid + j * blockDim.x;
+    if (a.sum && col < a.d) static_cast<IO*>(a.sum)[row * a.sum_stride + col] = from_f32<IO>(s[j]);
+    square += s[j] * s[j];
   }
   square = row_sum(square, red[0]);
   float rstd = rsqrtf(square * a.inv_d + a.eps);
@@ -107,94 +222,46 @@ __global__ void __launch_bounds__(THREADS, CTAS) residual_rmsnorm_kernel(const _
     square = 0.f;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        s[j][i] *= kNormRescue;
-        square += s[j][i] * s[j][i];
-      }
+      s[j] *= kNormRescue;
+      square += s[j] * s[j];
     }
     square = row_sum(square, red[1]);
     rstd = rsqrtf(square * a.inv_d);
   }
+  unsigned m = 0;
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    const int col = (tid + j * blockDim.x) * V;
+    const int col = tid + j * blockDim.x;
     if (col < a.d) {
-      float w[V];
-      load_weight<V>(a.weight, a.weight_f32, col, w);
-#pragma unroll
-      for (int i = 0; i < V; ++i) s[j][i] = s[j][i] * rstd * w[i];
-      if (a.out) store_f32<IO, V>(static_cast<IO*>(a.out) + row * a.out_stride + col, s[j]);
+      float w[1];
+      load_weight<1>(a.weight, a.weight_f32, col, w);
+      s[j] = s[j] * rstd * w[0];
+      if (a.out) static_cast<IO*>(a.out)[row * a.out_stride + col] = from_f32<IO>(s[j]);
+    }
+    m = max(m, magnitude(s[j]));                             // (columns past the row's end are zeros)
+    if (a.codes && a.group != 0) {
+      const unsigned here = __reduce_max_sync(0xffffffffu, magnitude(s[j]));       // 32 columns of one group
+      if (lane == 0 && col < a.d) atomicMax(&group_max[col >> a.group_shift], here);
     }
   }
   if (a.codes == nullptr) return;
-
-  // The scale of every vector's group, then its codes.
-  unsigned largest[NV];
-#pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    largest[j] = 0;
-#pragma unroll
-    for (int i = 0; i < V; ++i) largest[j] = max(largest[j], magnitude(s[j][i]));        // (columns past the row's end are zeros)
-  }
-  uint8_t* codes = a.codes + row * a.codes_stride;
   float* scales = a.scales + static_cast<long long>(row) * a.groups;
   if (a.group == 0) {
-    unsigned m = 0;
-#pragma unroll
-    for (int j = 0; j < NV; ++j) m = max(m, largest[j]);
-    m = __reduce_max_sync(0xffffffffu, m);
-    if (blockDim.x > 32) {
-      unsigned* share = reinterpret_cast<unsigned*>(red[1]);
-      __syncthreads();                                       // red[1] may still be read (rows whose squares overflowed)
-      if (lane == 0) share[tid >> 5] = m;
-      __syncthreads();
-      m = __reduce_max_sync(0xffffffffu, lane < static_cast<int>(blockDim.x >> 5) ? share[lane] : 0u);
-    }
-#pragma unroll
-    for (int j = 0; j < NV; ++j) largest[j] = m;
+    m = row_max(m, reinterpret_cast<unsigned*>(red[1]));
     if (tid == 0) scales[0] = code_scale(m);
-  } else if (V > 1) {
-    const int lanes = a.group / V;                           // 4 to 16 lanes hold a group
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-#pragma unroll
-      for (int o = 1; o < 16; o <<= 1)
-        if (o < lanes) largest[j] = max(largest[j], __shfl_xor_sync(0xffffffffu, largest[j], o));
-      const int col = (tid + j * blockDim.x) * V;
-      if (col < a.d && (lane & (lanes - 1)) == 0) scales[col >> a.group_shift] = code_scale(largest[j]);
-    }
   } else {
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const unsigned m = __reduce_max_sync(0xffffffffu, largest[j]);       // 32 columns of one group
-      const int col = tid + j * blockDim.x;
-      if (lane == 0 && col < a.d) atomicMax(&group_max[col >> a.group_shift], m);
-    }
     __syncthreads();
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const int col = tid + j * blockDim.x;
-      if (col < a.d) {
-        largest[j] = group_max[col >> a.group_shift];
-        if ((col & (a.group - 1)) == 0) scales[col >> a.group_shift] = code_scale(largest[j]);
-      }
-    }
   }
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    const int col = (tid + j * blockDim.x) * V;
+    const int col = tid + j * blockDim.x;
     if (col >= a.d) continue;
-    const float2 by = code_factors(code_scale(largest[j]));
-    if constexpr (V > 1) {
-      Pack<uint16_t, V / 2> o;
-#pragma unroll
-      for (int i = 0; i < V; i += 2)
-        o.e[i / 2] = __nv_cvt_float2_to_fp8x2(make_float2(s[j][i] * by.x * by.y, s[j][i + 1] * by.x * by.y), __NV_SATFINITE, __NV_E4M3);
-      store_pack<uint16_t, V / 2>(reinterpret_cast<uint16_t*>(codes + col), o);
-    } else {
-      codes[col] = __nv_cvt_float_to_fp8(s[j][0] * by.x * by.y, __NV_SATFINITE, __NV_E4M3);
+    if (a.group != 0) {
+      m = group_max[col >> a.group_shift];
+      if ((col & (a.group - 1)) == 0) scales[col >> a.group_shift] = code_scale(m);
     }
+    const float2 by = code_factors(code_scale(m));
+    a.codes[row * a.codes_stride + col] = __nv_cvt_float_to_fp8(s[j] * by.x * by.y, __NV_SATFINITE, __NV_E4M3);
   }
 }
 

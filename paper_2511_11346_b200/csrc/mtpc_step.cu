@@ -53,19 +53,17 @@ template <typename IO>
 void launch_rmsnorm(const NormArgs& a, bool vectors, cudaStream_t st) {
   const int packs = ceil_div(a.d, 8);
   if (vectors && packs <= 32)
-    launch_kernel(residual_rmsnorm_kernel<IO, 8, 1, 256, 6>, ceil_div(a.T, 8), dim3(32, 8), 0, st, true, a);
+    launch_kernel(residual_rmsnorm_kernel<IO, 1, 256, 6>, ceil_div(a.T, 8), dim3(32, 8), 0, st, true, a);
   else if (vectors && packs <= 64)
-    launch_kernel(residual_rmsnorm_kernel<IO, 8, 2, 256, 4>, ceil_div(a.T, 8), dim3(32, 8), 0, st, true, a);
+    launch_kernel(residual_rmsnorm_kernel<IO, 2, 256, 4>, ceil_div(a.T, 8), dim3(32, 8), 0, st, true, a);
   else if (vectors && packs <= 1024)
-    launch_kernel(residual_rmsnorm_kernel<IO, 8, 1, 1024, 2>, a.T, round_warp(packs), 0, st, true, a);
+    launch_kernel(residual_rmsnorm_kernel<IO, 2, 512, 2>, a.T, round_warp(ceil_div(packs, 2)), 0, st, true, a);
   else if (vectors)
-    launch_kernel(residual_rmsnorm_kernel<IO, 8, 4, 1024, 1>, a.T, round_warp(ceil_div(packs, 4)), 0, st, true, a);
+    launch_kernel(residual_rmsnorm_kernel<IO, 4, 1024, 1>, a.T, round_warp(ceil_div(packs, 4)), 0, st, true, a);
   else if (a.d <= 4096)
-    launch_kernel(residual_rmsnorm_kernel<IO, 1, 4, 1024, 2>, a.T, round_warp(ceil_div(a.d, 4)), 0, st, true, a);
-  else if (a.d <= 8192)
-    launch_kernel(residual_rmsnorm_kernel<IO, 1, 8, 1024, 1>, a.T, round_warp(ceil_div(a.d, 8)), 0, st, true, a);
+    launch_kernel(residual_rmsnorm_plain_kernel<IO, 4>, a.T, round_warp(ceil_div(a.d, 4)), 0, st, true, a);
   else
-    launch_kernel(residual_rmsnorm_kernel<IO, 1, 32, 1024, 1>, a.T, round_warp(ceil_div(a.d, 32)), 0, st, true, a);
+    launch_kernel(residual_rmsnorm_plain_kernel<IO, 32>, a.T, round_warp(ceil_div(a.d, 32)), 0, st, true, a);
 }
 
 // Blocks of the gradient kernel: as many as an SM takes of the vector build (the order of the sums then does not depend on alignment), of two rows at
@@ -74,13 +72,20 @@ int norm_grad_blocks(int T, int d) {
   const int per_sm = d > 4096 ? 1 : d > 2048 ? 2 : std::min(16, 512 / round_warp(ceil_div(d, 8)));
   return std::min(T, std::max(kSms, std::min(kSms * per_sm, T / 2)));
 }
+// Returns the blocks launched, each of which leaves its part of d weight.
 template <typename IO, typename DY, typename DX>
-void launch_rmsnorm_grad(const NormGradArgs& a, int blocks, bool vectors, cudaStream_t st) {
+int launch_rmsnorm_grad(const NormGradArgs& a, int blocks, bool vectors, cudaStream_t st) {
   const int packs = ceil_div(a.d, 8);
+  // Two blocks with two vectors a thread where a row ahead of them fits the registers, else one with one vector: 8192 rows of 4096, d_out fp32, two blocks /
+  // one, us: all else bf16 57 / 64, fp32 sum 94 / 70, fp32 d_x 107 / 80, all fp32 124 / 86.
+  constexpr bool kNarrow = sizeof(IO) + sizeof(DY) + sizeof(DX) <= 8;
+  if (vectors && packs > 256 && packs <= 512 && !kNarrow) blocks = std::min(blocks, kSms);
   if (vectors && packs <= 256)
     launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 1, 1, 256, 2>, blocks, round_warp(packs), 0, st, true, a);
-  else if (vectors && packs <= 512)
+  else if (vectors && packs <= 512 && kNarrow)
     launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 2, 1, 256, 2>, blocks, round_warp(ceil_div(packs, 2)), 0, st, true, a);
+  else if (vectors && packs <= 512)
+    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 1, 1, 512, 1>, blocks, round_warp(packs), 0, st, true, a);
   else if (vectors && packs <= 1024)
     launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 2, 1, 512, 1>, blocks, round_warp(ceil_div(packs, 2)), 0, st, true, a);
   else if (vectors)
@@ -89,11 +94,11 @@ void launch_rmsnorm_grad(const NormGradArgs& a, int blocks, bool vectors, cudaSt
     launch_kernel(rmsnorm_grad_plain_kernel<IO, DY, DX, 1, 4>, blocks, round_warp(ceil_div(a.d, 4)), 0, st, true, a);
   else
     launch_kernel(rmsnorm_grad_plain_kernel<IO, DY, DX, 1, 32>, blocks, round_warp(ceil_div(a.d, 32)), 0, st, true, a);
+  return blocks;
 }
 template <typename IO, typename DY>
-void launch_rmsnorm_grad(const NormGradArgs& a, int dx_dtype, int blocks, bool vectors, cudaStream_t st) {
-  if (dx_dtype == MTPC_F32) launch_rmsnorm_grad<IO, DY, float>(a, blocks, vectors, st);
-  else launch_rmsnorm_grad<IO, DY, __nv_bfloat16>(a, blocks, vectors, st);
+int launch_rmsnorm_grad(const NormGradArgs& a, int dx_dtype, int blocks, bool vectors, cudaStream_t st) {
+  return dx_dtype == MTPC_F32 ? launch_rmsnorm_grad<IO, DY, float>(a, blocks, vectors, st) : launch_rmsnorm_grad<IO, DY, __nv_bfloat16>(a, blocks, vectors, st);
 }
 
 // ---------------------------------------------------------------- embedding
@@ -464,6 +469,7 @@ int mtpc_residual_rmsnorm_backward(const void* sum, int64_t sum_stride, int32_t 
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   NormGradArgs a;
   memset(&a, 0, sizeof(a));
+  int parts = 0;                        // of d weight
   if (T > 0) {
     a.sum = sum;
     a.weight = weight;
@@ -483,17 +489,15 @@ int mtpc_residual_rmsnorm_backward(const void* sum, int64_t sum_stride, int32_t 
     const bool vectors = d % 8 == 0 && rows_allow(sum, sum_stride, element(io_dtype), 8, T) && rows_allow(weight, 0, element(weight_dtype), 8, 1) &&
                          rows_allow(d_out, d_out_stride, element(d_out_dtype), 8, T) &&
                          rows_allow(d_sum, d_sum_stride, element(d_x_dtype), 8, T) && rows_allow(d_x, d_x_stride, element(d_x_dtype), 8, T);
-    if (io_dtype == MTPC_F32) {
-      if (d_out_dtype == MTPC_F32) launch_rmsnorm_grad<float, float>(a, d_x_dtype, blocks, vectors, st);
-      else launch_rmsnorm_grad<float, __nv_bfloat16>(a, d_x_dtype, blocks, vectors, st);
-    } else {
-      if (d_out_dtype == MTPC_F32) launch_rmsnorm_grad<__nv_bfloat16, float>(a, d_x_dtype, blocks, vectors, st);
-      else launch_rmsnorm_grad<__nv_bfloat16, __nv_bfloat16>(a, d_x_dtype, blocks, vectors, st);
-    }
+    if (io_dtype == MTPC_F32)
+      parts = d_out_dtype == MTPC_F32 ? launch_rmsnorm_grad<float, float>(a, d_x_dtype, blocks, vectors, st)
+                                      : launch_rmsnorm_grad<float, __nv_bfloat16>(a, d_x_dtype, blocks, vectors, st);
+    else
+      parts = d_out_dtype == MTPC_F32 ? launch_rmsnorm_grad<__nv_bfloat16, float>(a, d_x_dtype, blocks, vectors, st)
+                                      : launch_rmsnorm_grad<__nv_bfloat16, __nv_bfloat16>(a, d_x_dtype, blocks, vectors, st);
   }
   if (d_weight)
-    launch_kernel(norm_weight_grad_kernel, ceil_div(d, 32), dim3(32, 32), 0, st, true, static_cast<const float*>(a.partial), T > 0 ? blocks : 0, d,
-                  d_weight);
+    launch_kernel(norm_weight_grad_kernel, ceil_div(d, 32), dim3(32, 32), 0, st, true, static_cast<const float*>(a.partial), parts, d, d_weight);
   return check_launch();
 }
 
