@@ -43,6 +43,43 @@ def lowrank_backward(lora_A, lora_B, dW_emit):
     return dW, dA, dB
 
 
+def embed(tokens, table, scale: float = 1.0, dtype=None):
+    """Device tensors tokens [T] int32 (negative: padding) and table [v, d] (fp32 or bf16) -> rows scale * table[token] [T, d]
+    (dtype: the table's)."""
+    import torch
+    out = torch.empty((tokens.shape[0], table.shape[1]), dtype=dtype or table.dtype, device=table.device)
+    B.mtpc_embed(tokens, table, out, scale=scale)
+    return out
+
+
+def embed_backward(tokens, d_out, v: int, scale: float = 1.0, into=None):
+    """Gradient of `embed` with respect to the table [v, d] (fp32). into: added to that tensor (a table tied to the unembeddings: the gradient
+    dW_base[0] of a factored head)."""
+    import torch
+    d_table = torch.empty((v, d_out.shape[1]), dtype=torch.float32, device=d_out.device) if into is None else into
+    B.mtpc_embed_backward(tokens, d_out, d_table, scale=scale, accumulate=into is not None)
+    return d_table
+
+
+def residual_rmsnorm(x, residual, weight, eps: float = 1e-5):
+    """Device tensors x, residual (or None) [T, d] -> (hidden states, x + residual): the residual stream's last addition and the norm whose output a
+    head reads."""
+    import torch
+    hidden, total = torch.empty_like(x), torch.empty_like(x)
+    B.mtpc_residual_rmsnorm(x, residual, weight, eps, hidden, out_sum=total)
+    return hidden, total
+
+
+def residual_rmsnorm_backward(total, weight, d_hidden, d_total=None, eps: float = 1e-5, dtype=None):
+    """-> (gradient of x and of residual [T, d] (dtype: total's), gradient of weight [d] fp32) from the head's d_hidden and what reaches the sum along
+    the residual stream."""
+    import torch
+    d_x = torch.empty(total.shape, dtype=dtype or total.dtype, device=total.device)
+    d_weight = torch.empty(total.shape[1], dtype=torch.float32, device=total.device)
+    B.mtpc_residual_rmsnorm_backward(total, weight, eps, d_hidden, d_total, d_x, d_weight)
+    return d_x, d_weight
+
+
 class DeviceHead:
     """Weights of a workload resident in HBM plus a head created on them."""
 
@@ -160,19 +197,28 @@ class DeviceHead:
                                                out["dT_static"])
         return out
 
-    def window_loss_backward(self, num_sequences, sequence_length, gamma, hidden=None, targets=None):
-        """-> dict(slot_loss [n], loss [1], dh, dW_emit, dW_sum, dT_static or None) as fp32 device tensors."""
+    def window_loss_backward(self, num_sequences, sequence_length, gamma, hidden=None, targets=None, out=None, max_norm=None):
+        """-> dict(slot_loss [n], loss [1], dh, dW_emit, dW_sum, dT_static or None) as fp32 device tensors. out: the dict of an earlier call, whose
+        buffers are written again. max_norm: the parameters' gradients together are clipped to that norm, in place, and
+        `grad_norm` [1] is what it was before."""
         import torch
         s = self.wl.shape
         h = self.hidden_device() if hidden is None else hidden
         t = torch.from_numpy(self.wl.targets).to(self.device) if targets is None else targets
         T = h.shape[0]
         f32 = dict(dtype=torch.float32, device=self.device)
-        out = dict(slot_loss=torch.empty(s.n, **f32), loss=torch.empty(1, **f32), dh=torch.empty((T, s.d), **f32),
-                   dW_emit=torch.empty((s.n, s.r, s.v, s.d), **f32), dW_sum=torch.empty((s.sum_rows, s.d), **f32),
-                   dT_static=torch.empty((max(s.n - 1, 1), s.r, s.r), **f32) if s.family == I.HMM else None)
+        if out is None:
+            out = dict(slot_loss=torch.empty(s.n, **f32), loss=torch.empty(1, **f32), dh=torch.empty((T, s.d), **f32),
+                       dW_emit=torch.empty((s.n, s.r, s.v, s.d), **f32), dW_sum=torch.empty((s.sum_rows, s.d), **f32),
+                       dT_static=torch.empty((max(s.n - 1, 1), s.r, s.r), **f32) if s.family == I.HMM else None)
         self.head.mtpc_window_loss_backward(h, t, num_sequences, sequence_length, gamma, out["slot_loss"], out["loss"],
                                             out["dh"], out["dW_emit"], out["dW_sum"], out["dT_static"])
+        if max_norm is not None:
+            if "gradients" not in out:
+                out["grad_norm"] = torch.empty(1, **f32)
+                out["gradients"] = B.GradientList([out["dW_emit"], out["dW_sum"]] +
+                                                  ([out["dT_static"]] if s.family == I.HMM and s.n > 1 else []))
+            out["gradients"].mtpc_clip_gradients(max_norm, out["grad_norm"])
         return out
 
     def close(self):
