@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
+import struct
 
 from . import build as _build
 
@@ -540,13 +541,17 @@ class GradientList:
         if not grads or len(outs) != len(grads):
             raise MtpcError(ERR_SHAPE, f"{what}: {len(grads)} gradients, {len(outs)} results")
         self.device = grads[0].get_device()
-        entries = (MtpcGradient * len(grads))()
-        for e, g, o in zip(entries, grads, outs):
-            for t in (g, o):
-                if t is not None and (not t.is_cuda or t.get_device() != self.device or not t.is_contiguous() or t.numel() != g.numel()):
+        codes, table = _dtypes(), bytearray(32 * len(grads))
+        for i, (g, o) in enumerate(zip(grads, outs)):
+            count = g.numel()
+            for t in (g,) if o is None or o is g else (g, o):
+                if not t.is_cuda or t.get_device() != self.device or not t.is_contiguous() or t.numel() != count:
                     _refuse(what, f"{tuple(t.shape)} with strides {t.stride()} on {t.device}")
-            e.data, e.out, e.count, e.dtype = g.data_ptr(), _ptr(o), g.numel(), _dtype(what, g)
-            e.out_dtype = e.dtype if o is None else _dtype(what, o)
+                if t.dtype not in codes:
+                    _refuse(what, f"{t.dtype}", ERR_UNSUPPORTED)
+            struct.pack_into("=QQqii", table, 32 * i, g.data_ptr(), 0 if o is None else o.data_ptr(), count, codes[g.dtype],
+                             codes[g.dtype if o is None else o.dtype])          # an mtpc_gradient
+        entries = (MtpcGradient * len(grads)).from_buffer(table)
         need = ctypes.c_size_t(0)
         _check(lib().mtpc_gradient_list_workspace_bytes(entries, len(grads), ctypes.byref(need)), "mtpc_gradient_list_workspace_bytes")
         self._keep = (grads, outs)
