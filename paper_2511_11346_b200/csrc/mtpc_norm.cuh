@@ -30,6 +30,7 @@ struct NormArgs {
   long long x_stride, residual_stride, sum_stride, out_stride, codes_stride;
   int T, d, group, groups;                // group: columns that share a scale (0: the row)
   int group_shift;                        // its logarithm
+  int shift, pitch;                       // of split rows (SplitRow)
   bool weight_f32;
   float eps, inv_d;
 };
@@ -69,8 +70,8 @@ __device__ __forceinline__ unsigned row_max(unsigned m, unsigned* share) {
 }
 
 // NV vectors of eight elements a thread. Beside its bytes a row costs what an SM issues for it, so the arithmetic goes by packed pairs: with 8-bit
-// output, 2005 rows of 4096, element by element 16.6 to 24 us.
-template <typename IO, int NV, int THREADS, int CTAS>
+// output, 2005 rows of 4096, element by element 16.6 to 24 us. SPLIT: rows that start off their vectors (no groups of columns with scales of their own).
+template <typename IO, int NV, int THREADS, int CTAS, bool SPLIT>
 __global__ void __launch_bounds__(THREADS, CTAS) residual_rmsnorm_kernel(const __grid_constant__ NormArgs a) {
   __shared__ float red[2][32];
   const int row = blockIdx.x * blockDim.y + threadIdx.y;
@@ -78,29 +79,39 @@ __global__ void __launch_bounds__(THREADS, CTAS) residual_rmsnorm_kernel(const _
   grid_dependency_wait();
   grid_launch_dependents();
   if (row >= a.T) return;                                    // a whole warp, or no thread
+  const SplitRow split(SPLIT ? a.shift : 0, SPLIT ? a.pitch : 0, row, a.d);
+  const int begin = (SPLIT ? split.head : 0) + tid * 8, beside = SPLIT ? split.beside(tid) : -1;       // the thread's first column, and a single one
+  bool inside[NV];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) inside[j] = SPLIT ? tid + j * threads < split.packs : begin + j * threads * 8 < a.d;
   uint64_t s[NV][4];
+  float single = 0.f;
   {
     Raw8<IO> x[NV], r[NV];
-    const IO* x_row = static_cast<const IO*>(a.x) + row * a.x_stride + tid * 8;
-    const IO* r_row = static_cast<const IO*>(a.residual) + row * a.residual_stride + tid * 8;
+    const IO* x_row = static_cast<const IO*>(a.x) + row * a.x_stride;
+    const IO* r_row = static_cast<const IO*>(a.residual) + row * a.residual_stride;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       x[j].clear();
-      if ((tid + j * threads) * 8 < a.d) {
-        x[j].load(x_row + j * threads * 8);
-        if (a.residual) r[j].load(r_row + j * threads * 8);
+      if (inside[j]) {
+        x[j].load(x_row + begin + j * threads * 8);
+        if (a.residual) r[j].load(r_row + begin + j * threads * 8);
       }
+    }
+    if (SPLIT && beside >= 0) {
+      single = a.residual ? to_f32(x_row[beside]) + to_f32(r_row[beside]) : to_f32(x_row[beside]);
+      if (a.sum) static_cast<IO*>(a.sum)[row * a.sum_stride + beside] = from_f32<IO>(single);
     }
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) s[j][i] = x[j].pair(i);
-      if ((tid + j * threads) * 8 < a.d) {
+      if (inside[j]) {
         if (a.residual) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) s[j][i] = add2(s[j][i], r[j].pair(i));
         }
-        if (a.sum) store_pairs<IO>(static_cast<IO*>(a.sum) + row * a.sum_stride + (tid + j * threads) * 8, s[j]);
+        if (a.sum) store_pairs<IO>(static_cast<IO*>(a.sum) + row * a.sum_stride + begin + j * threads * 8, s[j]);
       }
     }
   }
@@ -112,7 +123,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) residual_rmsnorm_kernel(const _
       for (int i = 0; i < 4; ++i) sum = fma2(s[j][i], s[j][i], sum);
     }
     const float2 x = unpack2(sum);
-    return x.x + x.y;
+    return SPLIT ? x.x + x.y + single * single : x.x + x.y;
   };
   float square = row_sum(squares(), red[0]);
   float rstd = rsqrtf(square * a.inv_d + a.eps);
@@ -122,20 +133,26 @@ __global__ void __launch_bounds__(THREADS, CTAS) residual_rmsnorm_kernel(const _
 #pragma unroll
       for (int i = 0; i < 4; ++i) s[j][i] = mul2(s[j][i], pack2(kNormRescue, kNormRescue));
     }
+    single *= kNormRescue;
     square = row_sum(squares(), red[1]);
     rstd = rsqrtf(square * a.inv_d);
   }
   const uint64_t rstd2 = pack2(rstd, rstd);
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    const int col = (tid + j * threads) * 8;
-    if (col < a.d) {
+    const int col = begin + j * threads * 8;
+    if (inside[j]) {
       float w[8];
-      load_weight<8>(a.weight, a.weight_f32, col, w);
+      if constexpr (SPLIT) load_weight8(a.weight, a.weight_f32, col, w);
+      else load_weight<8>(a.weight, a.weight_f32, col, w);
 #pragma unroll
       for (int i = 0; i < 4; ++i) s[j][i] = mul2(mul2(s[j][i], rstd2), pack2(w[2 * i], w[2 * i + 1]));
       if (a.out) store_pairs<IO>(static_cast<IO*>(a.out) + row * a.out_stride + col, s[j]);
     }
+  }
+  if (SPLIT && beside >= 0) {
+    single = single * rstd * load_weight1(a.weight, a.weight_f32, beside);
+    if (a.out) static_cast<IO*>(a.out)[row * a.out_stride + beside] = from_f32<IO>(single);
   }
   if (a.codes == nullptr) return;
 
@@ -153,7 +170,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) residual_rmsnorm_kernel(const _
   }
   float* scales = a.scales + static_cast<long long>(row) * a.groups;
   if (a.group == 0) {
-    unsigned m = largest[0];
+    unsigned m = SPLIT ? max(largest[0], magnitude(single)) : largest[0];
 #pragma unroll
     for (int j = 1; j < NV; ++j) m = max(m, largest[j]);
     m = row_max(m, reinterpret_cast<unsigned*>(red[1]));
@@ -167,14 +184,14 @@ __global__ void __launch_bounds__(THREADS, CTAS) residual_rmsnorm_kernel(const _
 #pragma unroll
       for (int o = 1; o < 16; o <<= 1)
         if (o < lanes) largest[j] = max(largest[j], __shfl_xor_sync(0xffffffffu, largest[j], o));
-      const int col = (tid + j * threads) * 8;
-      if (col < a.d && (lane & (lanes - 1)) == 0) scales[col >> a.group_shift] = code_scale(largest[j]);
+      const int col = begin + j * threads * 8;
+      if (inside[j] && (lane & (lanes - 1)) == 0) scales[col >> a.group_shift] = code_scale(largest[j]);
     }
   }
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    const int col = (tid + j * threads) * 8;
-    if (col >= a.d) continue;
+    const int col = begin + j * threads * 8;
+    if (!inside[j]) continue;
     const float2 by = code_factors(code_scale(largest[j]));
     Pack<uint16_t, 4> o;
 #pragma unroll
@@ -185,6 +202,10 @@ __global__ void __launch_bounds__(THREADS, CTAS) residual_rmsnorm_kernel(const _
       o.e[i] = __nv_cvt_float2_to_fp8x2(x, __NV_SATFINITE, __NV_E4M3);
     }
     store_pack<uint16_t, 4>(reinterpret_cast<uint16_t*>(a.codes + row * a.codes_stride + col), o);
+  }
+  if (SPLIT && beside >= 0) {
+    const float2 by = code_factors(code_scale(largest[0]));
+    a.codes[row * a.codes_stride + beside] = __nv_cvt_float_to_fp8(single * by.x * by.y, __NV_SATFINITE, __NV_E4M3);
   }
 }
 
@@ -271,6 +292,7 @@ struct NormGradArgs {
   float* partial;                                   // [gridDim.x, d]: the blocks' parts of d weight (NULL: not wanted)
   long long sum_stride, d_out_stride, d_stream_stride, d_x_stride;
   int T, d;
+  int shift, pitch;                                 // of split rows (SplitRow)
   bool weight_f32;
   float eps, inv_d;
 };
@@ -278,14 +300,16 @@ struct NormGradArgs {
 // Every block has every gridDim.x-th row and keeps its part of d weight in registers, NV vectors of eight elements a thread; its vectors of the next AHEAD
 // rows are on their way to registers. What bounds it is what the SM issues for a row beside its bytes, so the arithmetic goes by packed pairs: 8192 rows
 // of 4096 (bf16, d_out fp32) one by one 88 to 104 us, with rows fetched by cp.async through shared memory, where issuing the copies took 1000 of 3500
-// cycles a row, 65 to 78.
-template <typename IO, typename DY, typename DX, int NV, int AHEAD, int THREADS, int CTAS>
+// cycles a row, 65 to 78. SPLIT: rows that start off their vectors, at the same columns in all rows of a block.
+template <typename IO, typename DY, typename DX, int NV, int AHEAD, int THREADS, int CTAS, bool SPLIT>
 __global__ void __launch_bounds__(THREADS, CTAS) rmsnorm_grad_kernel(const __grid_constant__ NormGradArgs a) {
   __shared__ float red[3][32];
   const int tid = threadIdx.x, threads = blockDim.x;
+  const SplitRow split(SPLIT ? a.shift : 0, SPLIT ? a.pitch : 0, blockIdx.x, a.d);          // (gridDim.x: a multiple of eight, or one row a block)
+  const int begin = (SPLIT ? split.head : 0) + tid * 8, beside = SPLIT ? split.beside(tid) : -1;       // the thread's first column, and a single one
   bool inside[NV];
 #pragma unroll
-  for (int j = 0; j < NV; ++j) inside[j] = (tid + j * threads) * 8 < a.d;
+  for (int j = 0; j < NV; ++j) inside[j] = SPLIT ? tid + j * threads < split.packs : begin + j * threads * 8 < a.d;
   for (int i = tid; i < 96; i += threads) red[i >> 5][i & 31] = 0.f;
   __syncthreads();
   grid_dependency_wait();
@@ -293,20 +317,26 @@ __global__ void __launch_bounds__(THREADS, CTAS) rmsnorm_grad_kernel(const __gri
     Raw8<IO> s[NV];
     Raw8<DY> dy[NV];
     Raw8<DX> stream[NV];
+    float s1 = 0.f, dy1 = 0.f, stream1 = 0.f;                // the single column's
   } ahead[AHEAD];
-  const IO* next_s = static_cast<const IO*>(a.sum) + blockIdx.x * a.sum_stride + tid * 8;          // the thread's first vector of the row to be fetched next
-  const DY* next_dy = static_cast<const DY*>(a.d_out) + blockIdx.x * a.d_out_stride + tid * 8;
-  const DX* next_stream = static_cast<const DX*>(a.d_stream) + blockIdx.x * a.d_stream_stride + tid * 8;
+  const IO* next_s = static_cast<const IO*>(a.sum) + blockIdx.x * a.sum_stride;          // the row to be fetched next
+  const DY* next_dy = static_cast<const DY*>(a.d_out) + blockIdx.x * a.d_out_stride;
+  const DX* next_stream = static_cast<const DX*>(a.d_stream) + blockIdx.x * a.d_stream_stride;
   int next = blockIdx.x;
   auto fetch = [&](Row& x) {
     if (next < a.T) {
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
         if (inside[j]) {
-          x.s[j].load(next_s + j * threads * 8);
-          x.dy[j].load(next_dy + j * threads * 8);
-          if (a.d_stream) x.stream[j].load(next_stream + j * threads * 8);
+          x.s[j].load(next_s + begin + j * threads * 8);
+          x.dy[j].load(next_dy + begin + j * threads * 8);
+          if (a.d_stream) x.stream[j].load(next_stream + begin + j * threads * 8);
         }
+      }
+      if (SPLIT && beside >= 0) {
+        x.s1 = to_f32(next_s[beside]);
+        x.dy1 = to_f32(next_dy[beside]);
+        if (a.d_stream) x.stream1 = to_f32(next_stream[beside]);
       }
       next += gridDim.x;
       next_s += gridDim.x * a.sum_stride;
@@ -328,15 +358,20 @@ __global__ void __launch_bounds__(THREADS, CTAS) rmsnorm_grad_kernel(const __gri
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     float x[8] = {};
-    if (inside[j]) load_weight<8>(a.weight, a.weight_f32, (tid + j * threads) * 8, x);
+    if (inside[j]) {
+      if constexpr (SPLIT) load_weight8(a.weight, a.weight_f32, begin + j * threads * 8, x);
+      else load_weight<8>(a.weight, a.weight_f32, begin + j * threads * 8, x);
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       w[j][i] = pack2(x[2 * i], x[2 * i + 1]);
       dw[j][i] = 0;
     }
   }
+  const float w1 = SPLIT && beside >= 0 ? load_weight1(a.weight, a.weight_f32, beside) : 0.f;
+  float dw1 = 0.f;
   int turn = 0;
-  DX* out = static_cast<DX*>(a.d_x) + blockIdx.x * a.d_x_stride + tid * 8;
+  DX* out = static_cast<DX*>(a.d_x) + blockIdx.x * a.d_x_stride;
   auto work = [&](Row& mine) {
     uint64_t s[NV][4], dy[NV][4];
     Raw8<DX> stream[NV];
@@ -349,6 +384,8 @@ __global__ void __launch_bounds__(THREADS, CTAS) rmsnorm_grad_kernel(const __gri
       }
       stream[j] = mine.stream[j];
     }
+    float s1 = mine.s1;
+    const float dy1 = mine.dy1, stream1 = mine.stream1;
     fetch(mine);
     auto add_up = [&](float (&sums)[2], float* share) {        // s^2 and weight d_out s
       uint64_t squares = 0, products = 0;
@@ -361,8 +398,8 @@ __global__ void __launch_bounds__(THREADS, CTAS) rmsnorm_grad_kernel(const __gri
         }
       }
       const float2 x = unpack2(squares), y = unpack2(products);
-      sums[0] = x.x + x.y;
-      sums[1] = y.x + y.y;
+      sums[0] = SPLIT ? x.x + x.y + s1 * s1 : x.x + x.y;
+      sums[1] = SPLIT ? y.x + y.y + dy1 * w1 * s1 : y.x + y.y;
       row_sums(sums, share);
     };
     float sums[2], by = 1.f;
@@ -375,6 +412,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) rmsnorm_grad_kernel(const __gri
 #pragma unroll
         for (int i = 0; i < 4; ++i) s[j][i] = mul2(s[j][i], pack2(by, by));
       }
+      s1 *= by;
       __syncthreads();                                       // red[2] may still be read for an earlier row
       add_up(sums, red[2]);
       rstd = rsqrtf(sums[0] * a.inv_d);
@@ -391,7 +429,12 @@ __global__ void __launch_bounds__(THREADS, CTAS) rmsnorm_grad_kernel(const __gri
         dx[i] = fma2(step2, mul2(dy[j][i], w[j][i]), fma2(back2, unit, stream[j].pair(i)));
         dw[j][i] = fma2(dy[j][i], unit, dw[j][i]);
       }
-      if (inside[j]) store_pairs<DX>(out + j * threads * 8, dx);
+      if (inside[j]) store_pairs<DX>(out + begin + j * threads * 8, dx);
+    }
+    if (SPLIT && beside >= 0) {
+      const float unit = s1 * rstd;
+      out[beside] = from_f32<DX>((stream1 + back * unit) + step * (dy1 * w1));
+      dw1 += dy1 * unit;
     }
     out += gridDim.x * a.d_x_stride;
     turn ^= 1;
@@ -402,9 +445,22 @@ __global__ void __launch_bounds__(THREADS, CTAS) rmsnorm_grad_kernel(const __gri
       if (row + q * static_cast<int>(gridDim.x) < a.T) work(ahead[q]);
   }
   if (a.partial) {
+    float* part = a.partial + static_cast<size_t>(blockIdx.x) * a.d;
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
-      if (inside[j]) store_pairs<float>(a.partial + static_cast<size_t>(blockIdx.x) * a.d + (tid + j * threads) * 8, dw[j]);
+    for (int j = 0; j < NV; ++j) {
+      if (!inside[j]) continue;
+      if constexpr (SPLIT) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float2 x = unpack2(dw[j][i]);
+          part[begin + j * threads * 8 + 2 * i] = x.x;
+          part[begin + j * threads * 8 + 2 * i + 1] = x.y;
+        }
+      } else {
+        store_pairs<float>(part + begin + j * threads * 8, dw[j]);
+      }
+    }
+    if (SPLIT && beside >= 0) part[beside] = dw1;
   }
   grid_launch_dependents();
 }

@@ -144,6 +144,19 @@ __device__ __forceinline__ void store_pairs(T* p, const uint64_t (&x)[4]) {
   store_f32<T, 8>(p, y);
 }
 
+// A row of d elements whose first vector of eight elements does not start it: `head` elements, `packs` vectors, `rest` elements. The elements beside the
+// vectors, at most fourteen, go one to a thread (beside: its column, -1: none). Rows at a pitch that is no multiple of eight start at
+// different places; those of several matrices do so alike if their addresses and pitches are alike modulo eight elements (`shift`, `pitch`).
+struct SplitRow {
+  int head, packs, rest;
+  __device__ __forceinline__ SplitRow(int shift, int pitch, int row, int d) {
+    head = min((8 - ((shift + (row & 7) * pitch) & 7)) & 7, d);
+    packs = (d - head) / 8;
+    rest = d - head - packs * 8;
+  }
+  __device__ __forceinline__ int beside(int tid) const { return tid < head ? tid : tid < head + rest ? packs * 8 + tid : -1; }
+};
+
 // V adjacent weights (fp32 or bf16; none: ones).
 template <int V>
 __device__ __forceinline__ void load_weight(const void* weight, bool f32, int col, float (&w)[V]) {
@@ -155,6 +168,16 @@ __device__ __forceinline__ void load_weight(const void* weight, bool f32, int co
   } else {
     unpack(load_pack<__nv_bfloat16, V>(static_cast<const __nv_bfloat16*>(weight) + col), w);
   }
+}
+
+// One weight, and eight that lie anywhere.
+__device__ __forceinline__ float load_weight1(const void* weight, bool f32, int col) {
+  if (weight == nullptr) return 1.f;
+  return f32 ? static_cast<const float*>(weight)[col] : to_f32(static_cast<const __nv_bfloat16*>(weight)[col]);
+}
+__device__ __forceinline__ void load_weight8(const void* weight, bool f32, int col, float (&w)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w[i] = load_weight1(weight, f32, col + i);
 }
 
 }  // namespace mtpc

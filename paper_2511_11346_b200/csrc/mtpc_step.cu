@@ -6,6 +6,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <initializer_list>
 #include <new>
 
 #include "../../include/mtpc.h"
@@ -41,6 +42,24 @@ int check_device() {
 bool rows_allow(const void* p, int64_t stride, size_t element_bytes, int vec, int rows) {
   return p == nullptr || (aligned(p, element_bytes * vec) && (rows <= 1 || stride % vec == 0));
 }
+// Whether rows start off their vectors of eight elements alike in all of some matrices: then *shift and *pitch say how (SplitRow). Absent ones are left out.
+struct RowsOf {
+  const void* p;
+  int64_t stride;
+  size_t element_bytes;
+};
+bool rows_alike(std::initializer_list<RowsOf> all, int* shift, int* pitch) {
+  bool first = true;
+  for (const RowsOf& m : all) {
+    if (m.p == nullptr) continue;
+    const int s = static_cast<int>(reinterpret_cast<uintptr_t>(m.p) / m.element_bytes % 8), q = static_cast<int>(((m.stride % 8) + 8) % 8);
+    if (!first && (s != *shift || q != *pitch)) return false;
+    *shift = s;
+    *pitch = q;
+    first = false;
+  }
+  return true;
+}
 // Rows that are read may lie anywhere, also all in one place (stride 0); rows that are written must not overlap.
 bool input_rows(const void* p, int64_t stride, int rows) { return p == nullptr || rows <= 1 || stride >= 0; }
 bool output_rows(const void* p, int64_t stride, int rows, int d) { return p == nullptr || rows <= 1 || stride >= d; }
@@ -49,21 +68,26 @@ int ceil_div(long long a, long long b) { return static_cast<int>((a + b - 1) / b
 int round_warp(int x) { return (x + 31) / 32 * 32; }
 
 // ---------------------------------------------------------------- residual norm
-template <typename IO>
-void launch_rmsnorm(const NormArgs& a, bool vectors, cudaStream_t st) {
+// How the rows of a call are read: as vectors, as vectors between single elements, or element by element.
+enum RowPath { kRowVectors, kRowSplit, kRowElements };
+template <typename IO, bool SPLIT>
+void launch_rmsnorm_vectors(const NormArgs& a, cudaStream_t st) {
   const int packs = ceil_div(a.d, 8);
-  if (vectors && packs <= 32)
-    launch_kernel(residual_rmsnorm_kernel<IO, 1, 256, 6>, ceil_div(a.T, 8), dim3(32, 8), 0, st, true, a);
-  else if (vectors && packs <= 64)
-    launch_kernel(residual_rmsnorm_kernel<IO, 2, 256, 4>, ceil_div(a.T, 8), dim3(32, 8), 0, st, true, a);
-  else if (vectors && packs <= 1024)
-    launch_kernel(residual_rmsnorm_kernel<IO, 2, 512, 2>, a.T, round_warp(ceil_div(packs, 2)), 0, st, true, a);
-  else if (vectors)
-    launch_kernel(residual_rmsnorm_kernel<IO, 4, 1024, 1>, a.T, round_warp(ceil_div(packs, 4)), 0, st, true, a);
-  else if (a.d <= 4096)
-    launch_kernel(residual_rmsnorm_plain_kernel<IO, 4>, a.T, round_warp(ceil_div(a.d, 4)), 0, st, true, a);
+  if (packs <= 32)
+    launch_kernel(residual_rmsnorm_kernel<IO, 1, 256, 6, SPLIT>, ceil_div(a.T, 8), dim3(32, 8), 0, st, true, a);
+  else if (packs <= 64)
+    launch_kernel(residual_rmsnorm_kernel<IO, 2, 256, 4, SPLIT>, ceil_div(a.T, 8), dim3(32, 8), 0, st, true, a);
+  else if (packs <= 1024)
+    launch_kernel(residual_rmsnorm_kernel<IO, 2, 512, 2, SPLIT>, a.T, round_warp(ceil_div(packs, 2)), 0, st, true, a);
   else
-    launch_kernel(residual_rmsnorm_plain_kernel<IO, 32>, a.T, round_warp(ceil_div(a.d, 32)), 0, st, true, a);
+    launch_kernel(residual_rmsnorm_kernel<IO, 4, 1024, 1, SPLIT>, a.T, round_warp(ceil_div(packs, 4)), 0, st, true, a);
+}
+template <typename IO>
+void launch_rmsnorm(const NormArgs& a, RowPath path, cudaStream_t st) {
+  if (path == kRowVectors) launch_rmsnorm_vectors<IO, false>(a, st);
+  else if (path == kRowSplit) launch_rmsnorm_vectors<IO, true>(a, st);
+  else if (a.d <= 4096) launch_kernel(residual_rmsnorm_plain_kernel<IO, 4>, a.T, round_warp(ceil_div(a.d, 4)), 0, st, true, a);
+  else launch_kernel(residual_rmsnorm_plain_kernel<IO, 32>, a.T, round_warp(ceil_div(a.d, 32)), 0, st, true, a);
 }
 
 // Blocks of the gradient kernel: as many as an SM takes of the vector build (the order of the sums then does not depend on alignment), of two rows at
@@ -72,23 +96,31 @@ int norm_grad_blocks(int T, int d) {
   const int per_sm = d > 4096 ? 1 : d > 2048 ? 2 : std::min(16, 512 / round_warp(ceil_div(d, 8)));
   return std::min(T, std::max(kSms, std::min(kSms * per_sm, T / 2)));
 }
-// Returns the blocks launched, each of which leaves its part of d weight.
-template <typename IO, typename DY, typename DX>
-int launch_rmsnorm_grad(const NormGradArgs& a, int blocks, bool vectors, cudaStream_t st) {
+// Returns the blocks launched, each of which leaves its part of d weight (at most `blocks`).
+template <typename IO, typename DY, typename DX, bool SPLIT>
+int launch_rmsnorm_grad_vectors(const NormGradArgs& a, int blocks, cudaStream_t st) {
   const int packs = ceil_div(a.d, 8);
   // Two blocks with two vectors a thread where a row ahead of them fits the registers, else one with one vector: 8192 rows of 4096, d_out fp32, two blocks /
   // one, us: all else bf16 57 / 64, fp32 sum 94 / 70, fp32 d_x 107 / 80, all fp32 124 / 86.
   constexpr bool kNarrow = sizeof(IO) + sizeof(DY) + sizeof(DX) <= 8;
-  if (vectors && packs > 256 && packs <= 512 && !kNarrow) blocks = std::min(blocks, kSms);
-  if (vectors && packs <= 256)
-    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 1, 1, 256, 2>, blocks, round_warp(packs), 0, st, true, a);
-  else if (vectors && packs <= 512 && kNarrow)
-    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 2, 1, 256, 2>, blocks, round_warp(ceil_div(packs, 2)), 0, st, true, a);
-  else if (vectors && packs <= 512)
-    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 1, 1, 512, 1>, blocks, round_warp(packs), 0, st, true, a);
-  else if (vectors && packs <= 1024)
-    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 2, 1, 512, 1>, blocks, round_warp(ceil_div(packs, 2)), 0, st, true, a);
-  else if (vectors)
+  if (packs > 256 && packs <= 512 && !kNarrow) blocks = std::min(blocks, kSms);
+  if (SPLIT && blocks < a.T) blocks = std::max(8, blocks / 8 * 8);        // a block's rows start alike
+  if (packs <= 256)
+    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 1, 1, 256, 2, SPLIT>, blocks, round_warp(packs), 0, st, true, a);
+  else if (packs <= 512 && kNarrow)
+    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 2, 1, 256, 2, SPLIT>, blocks, round_warp(ceil_div(packs, 2)), 0, st, true, a);
+  else if (packs <= 512)
+    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 1, 1, 512, 1, SPLIT>, blocks, round_warp(packs), 0, st, true, a);
+  else
+    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 2, 1, 512, 1, SPLIT>, blocks, round_warp(ceil_div(packs, 2)), 0, st, true, a);
+  return blocks;
+}
+template <typename IO, typename DY, typename DX>
+int launch_rmsnorm_grad(const NormGradArgs& a, int blocks, RowPath path, cudaStream_t st) {
+  const int packs = ceil_div(a.d, 8);
+  if (packs <= 1024 && path != kRowElements)
+    return path == kRowVectors ? launch_rmsnorm_grad_vectors<IO, DY, DX, false>(a, blocks, st) : launch_rmsnorm_grad_vectors<IO, DY, DX, true>(a, blocks, st);
+  if (path == kRowVectors)
     launch_kernel(rmsnorm_grad_plain_kernel<IO, DY, DX, 8, 4>, blocks, round_warp(ceil_div(packs, 4)), 0, st, true, a);
   else if (a.d <= 4096)
     launch_kernel(rmsnorm_grad_plain_kernel<IO, DY, DX, 1, 4>, blocks, round_warp(ceil_div(a.d, 4)), 0, st, true, a);
@@ -97,8 +129,8 @@ int launch_rmsnorm_grad(const NormGradArgs& a, int blocks, bool vectors, cudaStr
   return blocks;
 }
 template <typename IO, typename DY>
-int launch_rmsnorm_grad(const NormGradArgs& a, int dx_dtype, int blocks, bool vectors, cudaStream_t st) {
-  return dx_dtype == MTPC_F32 ? launch_rmsnorm_grad<IO, DY, float>(a, blocks, vectors, st) : launch_rmsnorm_grad<IO, DY, __nv_bfloat16>(a, blocks, vectors, st);
+int launch_rmsnorm_grad(const NormGradArgs& a, int dx_dtype, int blocks, RowPath path, cudaStream_t st) {
+  return dx_dtype == MTPC_F32 ? launch_rmsnorm_grad<IO, DY, float>(a, blocks, path, st) : launch_rmsnorm_grad<IO, DY, __nv_bfloat16>(a, blocks, path, st);
 }
 
 // ---------------------------------------------------------------- embedding
@@ -155,21 +187,17 @@ int check_embed_sizes(int T, int v, int d) {
   return MTPC_OK;
 }
 
-template <typename TI, typename TO, int V>
-void launch_embed(const EmbedArgs& a, cudaStream_t st) {
-  int share = 32;                       // threads to a row
-  while (share < 256 && share * V < a.d) share <<= 1;
-  const int rows = 256 / share;
-  if (a.T >= 4 * kSms * 8) {
-    launch_kernel(embed_kernel<TI, TO, V, 4>, ceil_div(a.T, rows * 4), dim3(share, rows), 0, st, true, a);
-  } else {                              // few rows: their columns over several blocks
-    launch_kernel(embed_kernel<TI, TO, V, 1>, dim3(ceil_div(a.T, rows), ceil_div(a.d, share * V)), dim3(share, rows), 0, st, true, a);
-  }
-}
 template <typename TI, typename TO>
 void launch_embed(const EmbedArgs& a, bool vectors, cudaStream_t st) {
-  if (vectors) launch_embed<TI, TO, 8>(a, st);
-  else launch_embed<TI, TO, 1>(a, st);
+  int share = 32;                       // threads to a row
+  while (share < 256 && share * 8 < a.d) share <<= 1;
+  const int rows = 256 / share;
+  if (!vectors)
+    launch_kernel(embed_split_kernel<TI, TO>, ceil_div(a.T, rows), dim3(share, rows), 0, st, true, a);
+  else if (a.T >= 4 * kSms * 8)
+    launch_kernel(embed_kernel<TI, TO, 8, 4>, ceil_div(a.T, rows * 4), dim3(share, rows), 0, st, true, a);
+  else                                  // few rows: their columns over several blocks
+    launch_kernel(embed_kernel<TI, TO, 8, 1>, dim3(ceil_div(a.T, rows), ceil_div(a.d, share * 8)), dim3(share, rows), 0, st, true, a);
 }
 
 }  // namespace
@@ -273,6 +301,7 @@ int mtpc_embed(const int32_t* tokens, int32_t T, const void* table, int64_t tabl
   a.v = v;
   a.d = d;
   a.scale = scale;
+  rows_alike({{out, T > 1 ? out_stride : 0, element(out_dtype)}}, &a.shift, &a.pitch);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool vectors = d % 8 == 0 && rows_allow(table, table_stride, element(table_dtype), 8, v) && rows_allow(out, out_stride, element(out_dtype), 8, T);
   if (table_dtype == MTPC_F32) {
@@ -314,6 +343,39 @@ int mtpc_embed_backward(const int32_t* tokens, int32_t T, const void* d_out, int
   if (T == 0)                           // (not accumulated: the gradient is zeros)
     return cudaMemset2DAsync(d_table, static_cast<size_t>(v == 1 ? d : d_table_stride) * 4, 0, static_cast<size_t>(d) * 4, v, st) == cudaSuccess
                ? MTPC_OK : MTPC_ERR_CUDA;
+  EmbedSegmentArgs a;
+  memset(&a, 0, sizeof(a));
+  a.key = reinterpret_cast<int*>(ws + p.off_key[0]);
+  a.pos = reinterpret_cast<int*>(ws + p.off_pos[0]);
+  a.bounds = reinterpret_cast<int2*>(ws + p.off_bounds);
+  a.d_out = d_out;
+  a.d_table = d_table;
+  a.part = reinterpret_cast<float*>(ws + p.off_part);
+  a.d_out_stride = d_out_stride;
+  a.d_table_stride = d_table_stride;
+  a.T = T;
+  a.v = v;
+  a.d = d;
+  a.chunk = p.chunk;
+  a.chunks = p.chunks;
+  a.scale = scale;
+  a.accumulate = accumulate != 0;
+  const auto table_allows = [&](int vec) { return d % vec == 0 && rows_allow(d_table, d_table_stride, 4, vec, v); };
+  a.row_vec = table_allows(8) ? 8 : table_allows(4) ? 4 : 1;
+  const auto vectors = [&](int vec) {
+    return table_allows(vec) && rows_allow(d_out, d_out_stride, element(d_out_dtype), vec, T);
+  };
+  const int vec = vectors(4) ? 4 : 1;
+  if (T <= kFewT) {
+    const int threads = std::min(kFewThreads, round_warp(ceil_div(d, vec)));
+    const dim3 grid(std::min(v, kSms * 16), ceil_div(d, threads * vec));
+    if (d_out_dtype == MTPC_F32)
+      launch_kernel(vec == 4 ? embed_few_kernel<float, 4, 8> : embed_few_kernel<float, 1, 8>, grid, threads, 0, st, true, tokens, a, out_status);
+    else
+      launch_kernel(vec == 4 ? embed_few_kernel<__nv_bfloat16, 4, 8> : embed_few_kernel<__nv_bfloat16, 1, 8>, grid, threads, 0, st, true, tokens, a,
+                    out_status);
+    return check_launch();
+  }
   if ((rc = allow_embed_gradient()) != MTPC_OK) return rc;
   EmbedSortArgs s;
   memset(&s, 0, sizeof(s));
@@ -345,39 +407,15 @@ int mtpc_embed_backward(const int32_t* tokens, int32_t T, const void* d_out, int
     }
     launch_kernel(embed_bounds_kernel, std::min(ceil_div(T, 256), kSms * 8), 256, 0, st, true, s);
   }
-  EmbedSegmentArgs a;
-  memset(&a, 0, sizeof(a));
-  a.key = s.key_a;
-  a.pos = s.pos_a;
-  a.bounds = s.bounds;
-  a.d_out = d_out;
-  a.d_table = d_table;
-  a.part = reinterpret_cast<float*>(ws + p.off_part);
-  a.d_out_stride = d_out_stride;
-  a.d_table_stride = d_table_stride;
-  a.T = T;
-  a.v = v;
-  a.d = d;
-  a.chunk = p.chunk;
-  a.chunks = p.chunks;
-  a.scale = scale;
-  a.accumulate = accumulate != 0;
-  const auto table_allows = [&](int vec) { return d % vec == 0 && rows_allow(d_table, d_table_stride, 4, vec, v); };
-  a.row_vec = table_allows(8) ? 8 : table_allows(4) ? 4 : 1;
-  const auto vectors = [&](int vec) {
-    return table_allows(vec) && rows_allow(d_out, d_out_stride, element(d_out_dtype), vec, T);
-  };
   // Rows without positions are cleared beside the chunks where they are many, as much as the chunks take to run; the others beside the join, whose
   // blocks are short: in the chunks' launch the last ones would be theirs.
   const auto clear_blocks = [&]() { return std::min(ceil_div(a.clear_end - a.clear_begin, kClearRows), kSms * 256); };
   const long long table_bytes = static_cast<long long>(v) * d * 4;
   a.clear_end = accumulate || (p.chunks > 1 && table_bytes < 2 * kClearBesideChunks) ? 0 : p.chunks == 1 ? v : static_cast<int>(kClearBesideChunks / (d * 4LL));
-  const int vec = d_out_dtype == MTPC_BF16 && vectors(8) ? 8 : vectors(4) ? 4 : 1;
   const int threads = std::min(p.threads, round_warp(ceil_div(d, vec)));
   a.slabs = ceil_div(d, threads * vec);
   auto* segment = d_out_dtype == MTPC_F32 ? (vec == 4 ? embed_segment_kernel<float, 4, 8> : embed_segment_kernel<float, 1, 8>)
-                  : vec == 8 ? embed_segment_kernel<__nv_bfloat16, 8, 4>
-                  : vec == 4 ? embed_segment_kernel<__nv_bfloat16, 4, 8> : embed_segment_kernel<__nv_bfloat16, 1, 8>;
+                                          : (vec == 4 ? embed_segment_kernel<__nv_bfloat16, 4, 8> : embed_segment_kernel<__nv_bfloat16, 1, 8>);
   launch_kernel(segment, p.chunks * a.slabs + clear_blocks(), threads, 0, st, true, a);
   if (p.chunks > 1) {
     a.clear_begin = a.clear_end;
@@ -432,9 +470,12 @@ int mtpc_residual_rmsnorm(const void* x, int64_t x_stride, const void* residual,
   const bool vectors = d % 8 == 0 && rows_allow(x, x_stride, e, 8, T) && rows_allow(residual, residual_stride, e, 8, T) &&
                        rows_allow(weight, 0, element(weight_dtype), 8, 1) && rows_allow(out_sum, sum_stride, e, 8, T) &&
                        rows_allow(out, out_stride, e, 8, T) && rows_allow(out_codes, codes_stride, 1, 8, T);
+  const bool alike = (!out_codes || scale_group == 0) && rows_alike({{x, T > 1 ? x_stride : 0, e}, {residual, T > 1 ? residual_stride : 0, e},
+      {out_sum, T > 1 ? sum_stride : 0, e}, {out, T > 1 ? out_stride : 0, e}, {out_codes, T > 1 ? codes_stride : 0, 1}}, &a.shift, &a.pitch);
+  const RowPath path = vectors ? kRowVectors : alike ? kRowSplit : kRowElements;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (io_dtype == MTPC_F32) launch_rmsnorm<float>(a, vectors, st);
-  else launch_rmsnorm<__nv_bfloat16>(a, vectors, st);
+  if (io_dtype == MTPC_F32) launch_rmsnorm<float>(a, path, st);
+  else launch_rmsnorm<__nv_bfloat16>(a, path, st);
   return check_launch();
 }
 
@@ -489,12 +530,16 @@ int mtpc_residual_rmsnorm_backward(const void* sum, int64_t sum_stride, int32_t 
     const bool vectors = d % 8 == 0 && rows_allow(sum, sum_stride, element(io_dtype), 8, T) && rows_allow(weight, 0, element(weight_dtype), 8, 1) &&
                          rows_allow(d_out, d_out_stride, element(d_out_dtype), 8, T) &&
                          rows_allow(d_sum, d_sum_stride, element(d_x_dtype), 8, T) && rows_allow(d_x, d_x_stride, element(d_x_dtype), 8, T);
+    const auto rows = [&](const void* p, int64_t stride, int dtype) { return RowsOf{p, T > 1 ? stride : 0, element(dtype)}; };
+    const bool alike = rows_alike({rows(sum, sum_stride, io_dtype), rows(d_out, d_out_stride, d_out_dtype), rows(d_sum, d_sum_stride, d_x_dtype),
+                                   rows(d_x, d_x_stride, d_x_dtype)}, &a.shift, &a.pitch);
+    const RowPath path = vectors ? kRowVectors : alike ? kRowSplit : kRowElements;
     if (io_dtype == MTPC_F32)
-      parts = d_out_dtype == MTPC_F32 ? launch_rmsnorm_grad<float, float>(a, d_x_dtype, blocks, vectors, st)
-                                      : launch_rmsnorm_grad<float, __nv_bfloat16>(a, d_x_dtype, blocks, vectors, st);
+      parts = d_out_dtype == MTPC_F32 ? launch_rmsnorm_grad<float, float>(a, d_x_dtype, blocks, path, st)
+                                      : launch_rmsnorm_grad<float, __nv_bfloat16>(a, d_x_dtype, blocks, path, st);
     else
-      parts = d_out_dtype == MTPC_F32 ? launch_rmsnorm_grad<__nv_bfloat16, float>(a, d_x_dtype, blocks, vectors, st)
-                                      : launch_rmsnorm_grad<__nv_bfloat16, __nv_bfloat16>(a, d_x_dtype, blocks, vectors, st);
+      parts = d_out_dtype == MTPC_F32 ? launch_rmsnorm_grad<__nv_bfloat16, float>(a, d_x_dtype, blocks, path, st)
+                                      : launch_rmsnorm_grad<__nv_bfloat16, __nv_bfloat16>(a, d_x_dtype, blocks, path, st);
   }
   if (d_weight)
     launch_kernel(norm_weight_grad_kernel, ceil_div(d, 32), dim3(32, 32), 0, st, true, static_cast<const float*>(a.partial), parts, d, d_weight);

@@ -124,6 +124,36 @@ def test_gradient_of_strided_rows(off, pad):
     check_gradient(tokens_of("any", T, v, rng), one.expand(T, d), v, torch.empty(v, d, device="cuda"), 1.0)      # the same row at every position
 
 
+# The one launch of few positions, the sort in one, the digits' sort: on both sides of where one takes over.
+@pytest.mark.parametrize("T", [127, 128, 129, 32767, 32768, 32769])
+@pytest.mark.parametrize("kind,v,d", [("any", 1, 1), ("bad", 300, 37), ("zipf", 320, 64), ("padding", 7, 260)])
+def test_gradient_where_the_kernels_change(kind, T, v, d):
+    rng = np.random.default_rng(T)
+    tokens = tokens_of(kind, T, v, rng)
+    for t in (torch.float32, torch.bfloat16):
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        d_out, start = torch.randn(T, d, device="cuda").to(t), torch.randn(v, d, device="cuda")
+        check_gradient(tokens, d_out, v, torch.full((v, d), float("nan"), device="cuda"), 0.7, status=status)
+        assert status.item() == (B.STATUS_BAD_TOKEN if kind == "bad" else 0)
+        check_gradient(tokens, d_out, v, start.clone(), 0.7, start=start)
+
+
+def test_few_positions_keep_infinities_in_their_rows_and_the_same_bits():
+    rng = np.random.default_rng(3)
+    tokens = tokens_of("zipf", 128, 20, rng)
+    d_out = torch.randn(128, 300, device="cuda")
+    d_out[5, 7], d_out[90] = float("inf"), float("nan")
+    first, again = torch.empty(20, 300, device="cuda"), torch.empty(20, 300, device="cuda")
+    where = torch.from_numpy(tokens).cuda()
+    B.mtpc_embed_backward(where, d_out, first)
+    for _ in range(20):
+        B.mtpc_embed_backward(where, d_out, again)
+        assert torch.equal(first.view(torch.int32), again.view(torch.int32))
+    touched = {int(tokens[5]), int(tokens[90])}
+    bad = set(torch.nonzero(~torch.isfinite(first).all(1)).flatten().tolist())
+    assert bad == {b for b in touched if 0 <= b < 20}
+
+
 def test_gradient_without_positions():
     table = torch.ones(300, 50, device="cuda")
     none = torch.zeros(0, dtype=torch.int32, device="cuda")

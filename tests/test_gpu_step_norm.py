@@ -170,6 +170,37 @@ def test_backward_of_strided_rows_and_in_place(off, pad):
     check_backward(s, w, up[:1].expand(T, d), more[:1].expand(T, d), out[:, :d], dw)
 
 
+# Rows that start off their vectors, alike in all matrices and not; more of them than blocks, of which 144 at least take part in d weight here.
+@pytest.mark.parametrize("T,d,off,pad", [(700, 1001, 0, 0), (400, 2047, 3, 0), (310, 4099, 5, 4), (20, 8191, 0, 0), (500, 5, 1, 0), (500, 13, 0, 1), (300, 520, 3, 8),
+                                         (9, 9, 0, 0)])
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+def test_rows_off_their_vectors(io, T, d, off, pad):
+    torch.manual_seed(T + d)
+    t, other = TYPES[io], torch.bfloat16 if io == "f32" else torch.float32
+    x, res, weight = rows(T, d, t, off, pad), rows(T, d, t, off + 8, pad, 2.0), 1 + 0.2 * torch.randn(d, device="cuda")
+    whole = torch.full((T * (d + pad) + off,), 5.0, dtype=t, device="cuda")
+    out = whole[off:].view(T, d + pad)
+    codes = torch.full((T * (d + pad) + off,), 1, dtype=torch.uint8, device="cuda")
+    q, scale = codes[off:].view(T, d + pad), torch.empty(T, 1, device="cuda")
+    check_forward(x, res, weight.to(t), out[:, :d], None, q[:, :d], scale)
+    kept = out.clone(), q.clone()
+    assert (out[:, d:] == 5).all() and (whole[:off] == 5).all() and (q[:, d:] == 1).all() and (codes[:off] == 1).all()
+    check_forward(x.clone(), res, weight.to(t), out[:, :d], torch.empty(T, d, dtype=t, device="cuda"), q[:, :d], scale)       # a sum elsewhere, one kernel or the other
+    check_forward(x, res, weight, out[:, :d], res, q[:, :d], scale)                                                          # over its term
+    check_forward(x, None, None, out[:, :d], None)
+    assert torch.equal(kept[1][:, d:], q[:, d:])
+    up, more = rows(T, d, other, off, pad), rows(T, d, t, off, pad)
+    dw = torch.empty(d, device="cuda")
+    for grads in ((up, more), (up, None), (rows(T, d, other, off + 1, pad), more)):
+        check_backward(x, weight, grads[0], grads[1], out[:, :d], dw)
+        assert (out[:, d:] == 5).all() and (whole[:off] == 5).all()
+    check_backward(x, weight.to(t), up, more, more, dw)
+    big = x.clone()
+    big[0] = torch.randn(d, device="cuda") * 3e37                              # squares beyond fp32
+    check_backward(big, weight, up, None, out[:, :d], dw)
+    check_forward(big, None, weight, out[:, :d], None, q[:, :d], scale)
+
+
 def test_gradients_are_the_norms_differences():
     """Directional derivatives of the forward call (fp32) by central differences. With h the step, each difference quotient is off by its curvature, below
     50 h^2 of the terms' magnitudes here, and by the outputs' roundings, 32 u of theirs divided by h: h = 2^-8 keeps both below 1.5e-3."""
