@@ -87,7 +87,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) residual_rmsnorm_kernel(const _
   uint64_t s[NV][4];
   float single = 0.f;
   {
-    Raw8<IO> x[NV], r[NV];
+    Raw<IO, 8> x[NV], r[NV];
     const IO* x_row = static_cast<const IO*>(a.x) + row * a.x_stride;
     const IO* r_row = static_cast<const IO*>(a.residual) + row * a.residual_stride;
 #pragma unroll
@@ -314,9 +314,9 @@ __global__ void __launch_bounds__(THREADS, CTAS) rmsnorm_grad_kernel(const __gri
   __syncthreads();
   grid_dependency_wait();
   struct Row {
-    Raw8<IO> s[NV];
-    Raw8<DY> dy[NV];
-    Raw8<DX> stream[NV];
+    Raw<IO, 8> s[NV];
+    Raw<DY, 8> dy[NV];
+    Raw<DX, 8> stream[NV];
     float s1 = 0.f, dy1 = 0.f, stream1 = 0.f;                // the single column's
   } ahead[AHEAD];
   const IO* next_s = static_cast<const IO*>(a.sum) + blockIdx.x * a.sum_stride;          // the row to be fetched next
@@ -374,7 +374,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) rmsnorm_grad_kernel(const __gri
   DX* out = static_cast<DX*>(a.d_x) + blockIdx.x * a.d_x_stride;
   auto work = [&](Row& mine) {
     uint64_t s[NV][4], dy[NV][4];
-    Raw8<DX> stream[NV];
+    Raw<DX, 8> stream[NV];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
 #pragma unroll

@@ -112,26 +112,35 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
   return d;
 }
 
-// Eight adjacent elements as they were read, by a load that stays where it is written; and as four pairs of fp32.
-template <typename T>
-struct Raw8 {
-  uint32_t r[2 * sizeof(T)];
+// V adjacent elements as they were read, by a load that stays where it is written (of a Pack's bf16 elements a conditional load is taken apart at once, so
+// that each waits for its own data); and as fp32, one by one or in pairs.
+template <typename T, int V>
+struct Raw {
+  static constexpr int kBytes = sizeof(T) * V;
+  uint32_t r[kBytes < 4 ? 1 : kBytes / 4];
   __device__ __forceinline__ void load(const T* p) {
-    if constexpr (sizeof(T) == 4)
+    if constexpr (kBytes == 32)
       asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                    : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
                    : "l"(p));
-    else
+    else if constexpr (kBytes == 16)
       asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "l"(p));
+    else if constexpr (kBytes == 8)
+      asm volatile("ld.global.v2.b32 {%0, %1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "l"(p));
+    else if constexpr (kBytes == 4)
+      asm volatile("ld.global.b32 %0, [%1];" : "=r"(r[0]) : "l"(p));
+    else
+      asm volatile("ld.global.u16 %0, [%1];" : "=r"(r[0]) : "l"(p));
   }
   __device__ __forceinline__ void clear() {
 #pragma unroll
-    for (int i = 0; i < static_cast<int>(2 * sizeof(T)); ++i) r[i] = 0;
+    for (uint32_t& x : r) x = 0;
   }
-  __device__ __forceinline__ uint64_t pair(int i) const {
-    if constexpr (sizeof(T) == 4) return pack2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1]));
-    else return pack2(__uint_as_float(r[i] << 16), __uint_as_float(r[i] & 0xffff0000u));
+  __device__ __forceinline__ float value(int i) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(r[i]);
+    else return __uint_as_float(i & 1 ? r[i / 2] & 0xffff0000u : r[i / 2] << 16);
   }
+  __device__ __forceinline__ uint64_t pair(int i) const { return pack2(value(2 * i), value(2 * i + 1)); }
 };
 template <typename T>
 __device__ __forceinline__ void store_pairs(T* p, const uint64_t (&x)[4]) {

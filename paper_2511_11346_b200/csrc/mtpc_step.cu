@@ -189,7 +189,7 @@ int check_embed_sizes(int T, int v, int d) {
 
 template <typename TI, typename TO>
 void launch_embed(const EmbedArgs& a, bool vectors, cudaStream_t st) {
-  int share = 32;                       // threads to a row
+  int share = 8;                        // threads to a row
   while (share < 256 && share * 8 < a.d) share <<= 1;
   const int rows = 256 / share;
   if (!vectors)
