@@ -8,10 +8,11 @@
 // tokens are. A token whose positions lie within a chunk is written at once; of one that crosses chunks every chunk leaves its part, which are added up
 // in their order afterwards. (By the block that is there last, found by a counter, they are not: with the fences that takes the sums of 8192 x 4096 fp32
 // took 57 us, instead of 26 and 5 for a kernel of its own.)
-//   embed_order_kernel    up to kOrderMaxT positions: every block owns a range of tokens, finds their positions among all of them and sorts those;
+//   embed_order_kernel    up to kOrderMaxT positions (or half as many): every block owns a range of tokens, finds their positions among
+//                         all of them and sorts those;
 //                         meanwhile the device asks for d_out by L2 prefetch
-//   embed_count / embed_scan / embed_scatter_kernel   more positions: by digits of 9 bits
-//                         (embed_bounds_kernel: where each token's positions begin and end, which the one-launch sort knows)
+//   embed_count / embed_scatter_kernel   more positions: by digits of 9 bits
+//                         (embed_bounds_kernel: where each token's positions begin and end, which the one-launch sort and a single digit's know)
 //   embed_segment_kernel  the chunks
 //   embed_join_kernel     the tokens that cross chunks
 // A step of a few positions is all launches: up to kFewT of them embed_few_kernel does it alone, row of the table after row.
@@ -137,7 +138,7 @@ struct EmbedSortArgs {
   const int* tokens;
   int *key_a, *pos_a, *key_b, *pos_b;     // the last digit's go to key_a, pos_a
   int2* bounds;                           // [v + 1]: where a token's positions begin and end in the order (equal: it has none)
-  int* hist;                              // [bins][tiles]
+  uint2* hist;                            // [tiles][bins], two bins each
   unsigned* status;                       // may be NULL
   const void* d_out;
   long long d_out_stride;
@@ -284,11 +285,13 @@ __global__ void __launch_bounds__(kOrderThreads, 2) embed_order_kernel(const __g
   }
 }
 
-// More positions: a stable sort by digits, from the lowest. Every block has a tile of adjacent positions, `rounds` times kSortTile of them.
-constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
+// More positions: a stable sort by digits, from the lowest. Every block has a tile of adjacent positions, `rounds` times kSortTile of them: small ones, so
+// that the usual batches are many tiles.
+constexpr int kSortThreads = 256, kSortWarps = kSortThreads / 32;
 constexpr int kSortDigit = 9, kSortBins = 1 << kSortDigit;
 constexpr int kSortPerLane = 4, kSortTile = kSortThreads * kSortPerLane;
-constexpr size_t kSortSmem = static_cast<size_t>(kSortWarps) * kSortBins * 4;
+constexpr int kSortMaxTiles = 296;      // (two blocks an SM; every block of the second kernel reads all tiles' counts)
+static_assert(kSortBins == 2 * kSortThreads, "a thread has two bins");
 
 // Where the keys of digit `p` are written to (alternating so that the last one writes key_a, pos_a).
 __device__ __forceinline__ int* sort_keys(const EmbedSortArgs& a, int p) { return ((a.digits - 1 - p) & 1) ? a.key_b : a.key_a; }
@@ -332,14 +335,15 @@ __device__ __forceinline__ void sort_count(const SortItems& x, int p, unsigned* 
     __syncwarp();
   }
 }
-// counts -> the place of the warp's first key of each bin; base: that of the block's first key of bin threadIdx.x, and behind it the next round's.
-__device__ __forceinline__ void sort_offsets(unsigned* counts, unsigned& base) {
-  if (threadIdx.x < kSortBins) {
-#pragma unroll 8
-    for (int w = 0; w < kSortWarps; ++w) {
-      const unsigned c = counts[w * kSortBins + threadIdx.x];
-      counts[w * kSortBins + threadIdx.x] = base;
-      base += c;
+// counts -> the place of the warp's first key of each bin; base: that of the block's first keys of the thread's two bins, and behind it the next round's.
+__device__ __forceinline__ void sort_offsets(unsigned* counts, unsigned (&base)[2]) {
+#pragma unroll
+  for (int w = 0; w < kSortWarps; ++w) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const unsigned c = counts[w * kSortBins + 2 * threadIdx.x + i];
+      counts[w * kSortBins + 2 * threadIdx.x + i] = base[i];
+      base[i] += c;
     }
   }
 }
@@ -364,8 +368,8 @@ __device__ __forceinline__ void sort_place(const EmbedSortArgs& a, const SortIte
     __syncwarp();
   }
 }
-// Exclusive running sum of one value a thread over the block; total: of all.
-__device__ __forceinline__ unsigned block_running_sum(unsigned x, unsigned* warp_sums, unsigned& total) {
+// Exclusive running sum of one value a thread over the block.
+__device__ __forceinline__ unsigned block_running_sum(unsigned x, unsigned* warp_sums) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   unsigned sum = x;
 #pragma unroll
@@ -375,66 +379,61 @@ __device__ __forceinline__ unsigned block_running_sum(unsigned x, unsigned* warp
   }
   if (lane == 31) warp_sums[warp] = sum;
   __syncthreads();
-  unsigned before = warp_sums[lane];                   // (32 warps)
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const unsigned y = __shfl_up_sync(0xffffffffu, before, o);
-    if (lane >= o) before += y;
-  }
-  total = __shfl_sync(0xffffffffu, before, kSortWarps - 1);
-  const unsigned earlier = __shfl_sync(0xffffffffu, before, warp == 0 ? 0 : warp - 1);
-  __syncthreads();                                     // warp_sums may be written again
-  return (warp == 0 ? 0u : earlier) + sum - x;
+  return __reduce_add_sync(0xffffffffu, lane < warp ? warp_sums[lane] : 0u) + sum - x;
 }
 
-// One digit: the tiles' counts, their running sums over (bin, tile), and every tile's keys to their places. The blocks of the first count that have no
-// tile prefetch, and clear the bounds.
+// One digit: the tiles' counts, hist[tile][bin]; and every tile's keys to their places. Where those begin, over the bins and of each the tiles, every block adds
+// up for itself (with a launch of one block between the two that did so, and tiles of 4096: the gradient of 65536 positions of 512 55 us, now 44.5). The
+// blocks of the first count that have no tile prefetch, and clear the bounds if a later kernel finds them.
 __global__ void __launch_bounds__(kSortThreads) embed_count_kernel(const __grid_constant__ EmbedSortArgs a, int p) {
-  extern __shared__ unsigned counts[];
+  __shared__ unsigned counts[kSortWarps * kSortBins];
   grid_dependency_wait();
   grid_launch_dependents();
   if (static_cast<int>(blockIdx.x) >= a.tiles) {
     const int part = blockIdx.x - a.tiles, parts = gridDim.x - a.tiles;
-    for (int b = part * kSortThreads + threadIdx.x; b <= a.v; b += parts * kSortThreads) a.bounds[b] = make_int2(0, 0);
+    if (a.digits > 1)
+      for (int b = part * kSortThreads + threadIdx.x; b <= a.v; b += parts * kSortThreads) a.bounds[b] = make_int2(0, 0);
     prefetch_rows(a, part, parts);
     return;
   }
-  unsigned sum = 0;
+  uint2 sum = make_uint2(0, 0);
   for (int r = 0; r < a.rounds; ++r) {
     SortItems x;
     sort_load(a, p, (static_cast<long long>(blockIdx.x) * a.rounds + r) * kSortTile, x);
     sort_count(x, p, counts);
     __syncthreads();
-    if (threadIdx.x < kSortBins) {
-#pragma unroll 8
-      for (int w = 0; w < kSortWarps; ++w) sum += counts[w * kSortBins + threadIdx.x];
+#pragma unroll
+    for (int w = 0; w < kSortWarps; ++w) {
+      sum.x += counts[w * kSortBins + 2 * threadIdx.x];
+      sum.y += counts[w * kSortBins + 2 * threadIdx.x + 1];
     }
     __syncthreads();
   }
-  if (threadIdx.x < kSortBins) a.hist[static_cast<size_t>(threadIdx.x) * a.tiles + blockIdx.x] = sum;
+  a.hist[blockIdx.x * kSortThreads + threadIdx.x] = sum;
 }
-__global__ void __launch_bounds__(kSortThreads) embed_scan_kernel(int* hist, int count) {
+__global__ void __launch_bounds__(kSortThreads) embed_scatter_kernel(const __grid_constant__ EmbedSortArgs a, int p) {
+  __shared__ unsigned counts[kSortWarps * kSortBins];
   __shared__ unsigned warp_sums[kSortWarps];
   grid_dependency_wait();
   grid_launch_dependents();
-  unsigned before = 0;
-  for (int i = 0; i < count; i += kSortThreads) {
-    const int at = i + threadIdx.x;
-    const unsigned x = at < count ? hist[at] : 0u;
-    unsigned total;
-    const unsigned sum = block_running_sum(x, warp_sums, total);
-    if (at < count) hist[at] = before + sum;
-    before += total;
+  SortItems x;
+  sort_load(a, p, static_cast<long long>(blockIdx.x) * a.rounds * kSortTile, x);
+  uint2 all = make_uint2(0, 0), before = make_uint2(0, 0);
+#pragma unroll 16
+  for (int t = 0; t < a.tiles; ++t) {
+    const uint2 c = a.hist[t * kSortThreads + threadIdx.x];
+    all.x += c.x, all.y += c.y;
+    if (t < static_cast<int>(blockIdx.x)) before.x += c.x, before.y += c.y;
   }
-}
-__global__ void __launch_bounds__(kSortThreads) embed_scatter_kernel(const __grid_constant__ EmbedSortArgs a, int p) {
-  extern __shared__ unsigned counts[];
-  grid_dependency_wait();
-  grid_launch_dependents();
-  unsigned base = threadIdx.x < kSortBins ? a.hist[static_cast<size_t>(threadIdx.x) * a.tiles + blockIdx.x] : 0u;
+  const unsigned first = block_running_sum(all.x + all.y, warp_sums), second = first + all.x;
+  if (a.digits == 1 && blockIdx.x == 0) {
+    const int b = 2 * threadIdx.x;
+    if (b <= a.v) a.bounds[b] = make_int2(first, second);
+    if (b < a.v) a.bounds[b + 1] = make_int2(second, second + all.y);
+  }
+  unsigned base[2] = {first + before.x, second + before.y};
   for (int r = 0; r < a.rounds; ++r) {
-    SortItems x;
-    sort_load(a, p, (static_cast<long long>(blockIdx.x) * a.rounds + r) * kSortTile, x);
+    if (r > 0) sort_load(a, p, (static_cast<long long>(blockIdx.x) * a.rounds + r) * kSortTile, x);
     sort_count(x, p, counts);
     __syncthreads();
     sort_offsets(counts, base);

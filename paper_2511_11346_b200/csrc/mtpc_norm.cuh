@@ -297,15 +297,16 @@ struct NormGradArgs {
   float eps, inv_d;
 };
 
-// Every block has every gridDim.x-th row and keeps its part of d weight in registers, NV vectors of eight elements a thread; its vectors of the next AHEAD
+// Every block has every gridDim.x-th row (of ROWS > 1 threadIdx.y each, rows of a warp: 16384 rows of 64 11 instead of 15 us) and keeps its part of d weight in registers, NV vectors of eight elements a thread; its vectors of the next AHEAD
 // rows are on their way to registers. What bounds it is what the SM issues for a row beside its bytes, so the arithmetic goes by packed pairs: 8192 rows
 // of 4096 (bf16, d_out fp32) one by one 88 to 104 us, with rows fetched by cp.async through shared memory, where issuing the copies took 1000 of 3500
 // cycles a row, 65 to 78. SPLIT: rows that start off their vectors, at the same columns in all rows of a block.
-template <typename IO, typename DY, typename DX, int NV, int AHEAD, int THREADS, int CTAS, bool SPLIT>
+template <typename IO, typename DY, typename DX, int NV, int AHEAD, int THREADS, int CTAS, bool SPLIT, int ROWS>
 __global__ void __launch_bounds__(THREADS, CTAS) rmsnorm_grad_kernel(const __grid_constant__ NormGradArgs a) {
   __shared__ float red[3][32];
   const int tid = threadIdx.x, threads = blockDim.x;
-  const SplitRow split(SPLIT ? a.shift : 0, SPLIT ? a.pitch : 0, blockIdx.x, a.d);          // (gridDim.x: a multiple of eight, or one row a block)
+  const int first_row = ROWS > 1 ? blockIdx.x * ROWS + threadIdx.y : blockIdx.x, row_step = gridDim.x * ROWS;
+  const SplitRow split(SPLIT ? a.shift : 0, SPLIT ? a.pitch : 0, first_row, a.d);          // (row_step: a multiple of eight, or one row a block)
   const int begin = (SPLIT ? split.head : 0) + tid * 8, beside = SPLIT ? split.beside(tid) : -1;       // the thread's first column, and a single one
   bool inside[NV];
 #pragma unroll
@@ -317,12 +318,14 @@ __global__ void __launch_bounds__(THREADS, CTAS) rmsnorm_grad_kernel(const __gri
     Raw<IO, 8> s[NV];
     Raw<DY, 8> dy[NV];
     Raw<DX, 8> stream[NV];
-    float s1 = 0.f, dy1 = 0.f, stream1 = 0.f;                // the single column's
+    Raw<IO, 1> s1;                                           // the single column's
+    Raw<DY, 1> dy1;
+    Raw<DX, 1> stream1;
   } ahead[AHEAD];
-  const IO* next_s = static_cast<const IO*>(a.sum) + blockIdx.x * a.sum_stride;          // the row to be fetched next
-  const DY* next_dy = static_cast<const DY*>(a.d_out) + blockIdx.x * a.d_out_stride;
-  const DX* next_stream = static_cast<const DX*>(a.d_stream) + blockIdx.x * a.d_stream_stride;
-  int next = blockIdx.x;
+  const IO* next_s = static_cast<const IO*>(a.sum) + first_row * a.sum_stride;          // the row to be fetched next
+  const DY* next_dy = static_cast<const DY*>(a.d_out) + first_row * a.d_out_stride;
+  const DX* next_stream = static_cast<const DX*>(a.d_stream) + first_row * a.d_stream_stride;
+  int next = first_row;
   auto fetch = [&](Row& x) {
     if (next < a.T) {
 #pragma unroll
@@ -334,14 +337,14 @@ __global__ void __launch_bounds__(THREADS, CTAS) rmsnorm_grad_kernel(const __gri
         }
       }
       if (SPLIT && beside >= 0) {
-        x.s1 = to_f32(next_s[beside]);
-        x.dy1 = to_f32(next_dy[beside]);
-        if (a.d_stream) x.stream1 = to_f32(next_stream[beside]);
+        x.s1.load(next_s + beside);
+        x.dy1.load(next_dy + beside);
+        if (a.d_stream) x.stream1.load(next_stream + beside);
       }
-      next += gridDim.x;
-      next_s += gridDim.x * a.sum_stride;
-      next_dy += gridDim.x * a.d_out_stride;
-      next_stream += gridDim.x * a.d_stream_stride;
+      next += row_step;
+      next_s += row_step * a.sum_stride;
+      next_dy += row_step * a.d_out_stride;
+      next_stream += row_step * a.d_stream_stride;
     }
   };
 #pragma unroll
@@ -352,6 +355,9 @@ __global__ void __launch_bounds__(THREADS, CTAS) rmsnorm_grad_kernel(const __gri
       ahead[q].dy[j].clear();
       ahead[q].stream[j].clear();
     }
+    ahead[q].s1.clear();
+    ahead[q].dy1.clear();
+    ahead[q].stream1.clear();
     fetch(ahead[q]);
   }
   uint64_t w[NV][4], dw[NV][4];
@@ -371,7 +377,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) rmsnorm_grad_kernel(const __gri
   const float w1 = SPLIT && beside >= 0 ? load_weight1(a.weight, a.weight_f32, beside) : 0.f;
   float dw1 = 0.f;
   int turn = 0;
-  DX* out = static_cast<DX*>(a.d_x) + blockIdx.x * a.d_x_stride;
+  DX* out = static_cast<DX*>(a.d_x) + first_row * a.d_x_stride;
   auto work = [&](Row& mine) {
     uint64_t s[NV][4], dy[NV][4];
     Raw<DX, 8> stream[NV];
@@ -384,8 +390,8 @@ __global__ void __launch_bounds__(THREADS, CTAS) rmsnorm_grad_kernel(const __gri
       }
       stream[j] = mine.stream[j];
     }
-    float s1 = mine.s1;
-    const float dy1 = mine.dy1, stream1 = mine.stream1;
+    float s1 = mine.s1.value(0);
+    const float dy1 = mine.dy1.value(0), stream1 = mine.stream1.value(0);
     fetch(mine);
     auto add_up = [&](float (&sums)[2], float* share) {        // s^2 and weight d_out s
       uint64_t squares = 0, products = 0;
@@ -413,7 +419,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) rmsnorm_grad_kernel(const __gri
         for (int i = 0; i < 4; ++i) s[j][i] = mul2(s[j][i], pack2(by, by));
       }
       s1 *= by;
-      __syncthreads();                                       // red[2] may still be read for an earlier row
+      if constexpr (ROWS == 1) __syncthreads();              // red[2] may still be read for an earlier row
       add_up(sums, red[2]);
       rstd = rsqrtf(sums[0] * a.inv_d);
     }
@@ -436,16 +442,18 @@ __global__ void __launch_bounds__(THREADS, CTAS) rmsnorm_grad_kernel(const __gri
       out[beside] = from_f32<DX>((stream1 + back * unit) + step * (dy1 * w1));
       dw1 += dy1 * unit;
     }
-    out += gridDim.x * a.d_x_stride;
+    out += row_step * a.d_x_stride;
     turn ^= 1;
   };
-  for (int row = blockIdx.x; row < a.T; row += AHEAD * gridDim.x) {
+  for (int row = first_row; row < a.T; row += AHEAD * row_step) {
 #pragma unroll
     for (int q = 0; q < AHEAD; ++q)
-      if (row + q * static_cast<int>(gridDim.x) < a.T) work(ahead[q]);
+      if (row + q * row_step < a.T) work(ahead[q]);
   }
   if (a.partial) {
     float* part = a.partial + static_cast<size_t>(blockIdx.x) * a.d;
+    __shared__ alignas(16) float share[ROWS > 1 ? ROWS : 1][ROWS > 1 ? 32 * 8 * NV : 1];
+    float* mine = ROWS > 1 ? share[threadIdx.y] : part;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       if (!inside[j]) continue;
@@ -453,14 +461,26 @@ __global__ void __launch_bounds__(THREADS, CTAS) rmsnorm_grad_kernel(const __gri
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float2 x = unpack2(dw[j][i]);
-          part[begin + j * threads * 8 + 2 * i] = x.x;
-          part[begin + j * threads * 8 + 2 * i + 1] = x.y;
+          mine[begin + j * threads * 8 + 2 * i] = x.x;
+          mine[begin + j * threads * 8 + 2 * i + 1] = x.y;
         }
+      } else if constexpr (ROWS > 1) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) *reinterpret_cast<uint64_t*>(mine + begin + j * threads * 8 + 2 * i) = dw[j][i];
       } else {
         store_pairs<float>(part + begin + j * threads * 8, dw[j]);
       }
     }
-    if (SPLIT && beside >= 0) part[beside] = dw1;
+    if (SPLIT && beside >= 0) mine[beside] = dw1;
+    if constexpr (ROWS > 1) {
+      __syncthreads();
+      for (int col = threadIdx.y * 32 + tid; col < a.d; col += 32 * ROWS) {
+        float sum = 0.f;
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) sum += share[r][col];
+        part[col] = sum;
+      }
+    }
   }
   grid_launch_dependents();
 }

@@ -90,9 +90,10 @@ void launch_rmsnorm(const NormArgs& a, RowPath path, cudaStream_t st) {
   else launch_kernel(residual_rmsnorm_plain_kernel<IO, 32>, a.T, round_warp(ceil_div(a.d, 32)), 0, st, true, a);
 }
 
-// Blocks of the gradient kernel: as many as an SM takes of the vector build (the order of the sums then does not depend on alignment), of two rows at
-// least where there are rows for every SM.
+// Blocks of the gradient kernel: as many as an SM takes, of two rows (a warp) at least where there are rows for every SM.
+constexpr int kGradRows = 8;            // rows of a block whose warps have one each, d <= 256
 int norm_grad_blocks(int T, int d) {
+  if (d <= 256) return std::min(ceil_div(T, kGradRows), 2 * kSms);
   const int per_sm = d > 4096 ? 1 : d > 2048 ? 2 : std::min(16, 512 / round_warp(ceil_div(d, 8)));
   return std::min(T, std::max(kSms, std::min(kSms * per_sm, T / 2)));
 }
@@ -104,15 +105,17 @@ int launch_rmsnorm_grad_vectors(const NormGradArgs& a, int blocks, cudaStream_t 
   // one, us: all else bf16 57 / 64, fp32 sum 94 / 70, fp32 d_x 107 / 80, all fp32 124 / 86.
   constexpr bool kNarrow = sizeof(IO) + sizeof(DY) + sizeof(DX) <= 8;
   if (packs > 256 && packs <= 512 && !kNarrow) blocks = std::min(blocks, kSms);
-  if (SPLIT && blocks < a.T) blocks = std::max(8, blocks / 8 * 8);        // a block's rows start alike
-  if (packs <= 256)
-    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 1, 1, 256, 2, SPLIT>, blocks, round_warp(packs), 0, st, true, a);
+  if (SPLIT && packs > 32 && blocks < a.T) blocks = std::max(8, blocks / 8 * 8);        // a block's rows start alike
+  if (packs <= 32)
+    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 1, 1, 256, 2, SPLIT, kGradRows>, blocks, dim3(32, kGradRows), 0, st, true, a);
+  else if (packs <= 256)
+    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 1, 1, 256, 2, SPLIT, 1>, blocks, round_warp(packs), 0, st, true, a);
   else if (packs <= 512 && kNarrow)
-    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 2, 1, 256, 2, SPLIT>, blocks, round_warp(ceil_div(packs, 2)), 0, st, true, a);
+    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 2, 1, 256, 2, SPLIT, 1>, blocks, round_warp(ceil_div(packs, 2)), 0, st, true, a);
   else if (packs <= 512)
-    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 1, 1, 512, 1, SPLIT>, blocks, round_warp(packs), 0, st, true, a);
+    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 1, 1, 512, 1, SPLIT, 1>, blocks, round_warp(packs), 0, st, true, a);
   else
-    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 2, 1, 512, 1, SPLIT>, blocks, round_warp(ceil_div(packs, 2)), 0, st, true, a);
+    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 2, 1, 512, 1, SPLIT, 1>, blocks, round_warp(ceil_div(packs, 2)), 0, st, true, a);
   return blocks;
 }
 template <typename IO, typename DY, typename DX>
@@ -142,12 +145,14 @@ struct EmbedPlan {
 };
 void plan_embed(int T, int v, int d, EmbedPlan* p) {
   memset(p, 0, sizeof(*p));
-  // Every block of the one-launch sort reads all tokens, so there is one per SM (a second one on some of them takes twice as long), until a block's tokens would be too many.
-  if (T <= kOrderMaxT) p->range = std::min(kOrderMaxRange, ceil_div(v + 1, kSms));
   int bits = 1;
   while ((static_cast<int64_t>(1) << bits) <= v) ++bits;                // keys run up to v
+  // Every block of the one-launch sort reads all tokens, so there is one per SM (a second one on some of them takes twice as long), until a block's tokens
+  // would be too many. One digit / the one launch, the whole gradient, 320 tokens: 8192 positions of 4096 41 / 37 us, 16384 of 1024 30.4 / 30.1,
+  // 32768 of 1024 36.9 / 41.2; two digits, 30000 tokens: 16000 of 512 39 / 32, 32768 of 512 47 / 46.
+  if (T <= (bits <= kSortDigit ? kOrderMaxT / 2 : kOrderMaxT)) p->range = std::min(kOrderMaxRange, ceil_div(v + 1, kSms));
   p->digits = p->range ? 1 : (bits + kSortDigit - 1) / kSortDigit;
-  p->rounds = ceil_div(T, static_cast<long long>(kSortTile) * 1024);
+  p->rounds = ceil_div(T, static_cast<long long>(kSortTile) * kSortMaxTiles);
   p->tiles = ceil_div(T, static_cast<long long>(kSortTile) * p->rounds);
   // Chunks of 8 positions at least, as many as give every SM the four blocks that it holds, of 256 threads with four columns each.
   p->threads = std::min(kSegmentThreads, round_warp(ceil_div(d, 4)));
@@ -175,8 +180,7 @@ int allow_embed_gradient() {
   const auto allow = [](auto* kernel, size_t bytes) {
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)) == cudaSuccess;
   };
-  if (!allow(embed_order_kernel, order_smem_bytes(kOrderMaxT)) || !allow(embed_count_kernel, kSortSmem) || !allow(embed_scatter_kernel, kSortSmem))
-    return MTPC_ERR_CUDA;
+  if (!allow(embed_order_kernel, order_smem_bytes(kOrderMaxT))) return MTPC_ERR_CUDA;
   __atomic_store_n(&g_embed_allowed[dev], 1, __ATOMIC_RELEASE);
   return MTPC_OK;
 }
@@ -385,7 +389,7 @@ int mtpc_embed_backward(const int32_t* tokens, int32_t T, const void* d_out, int
   s.key_b = reinterpret_cast<int*>(ws + p.off_key[1]);
   s.pos_b = reinterpret_cast<int*>(ws + p.off_pos[1]);
   s.bounds = reinterpret_cast<int2*>(ws + p.off_bounds);
-  s.hist = reinterpret_cast<int*>(ws + p.off_hist);
+  s.hist = reinterpret_cast<uint2*>(ws + p.off_hist);
   s.status = out_status;
   s.d_out = d_out;
   s.d_out_stride = d_out_stride;
@@ -401,11 +405,10 @@ int mtpc_embed_backward(const int32_t* tokens, int32_t T, const void* d_out, int
     launch_kernel(embed_order_kernel, ceil_div(v + 1, p.range), kOrderThreads, order_smem_bytes(T), st, true, s);
   } else {
     for (int digit = 0; digit < p.digits; ++digit) {
-      launch_kernel(embed_count_kernel, p.tiles + (digit == 0 ? kSms : 0), kSortThreads, kSortSmem, st, true, s, digit);
-      launch_kernel(embed_scan_kernel, 1, kSortThreads, 0, st, true, s.hist, p.tiles * kSortBins);
-      launch_kernel(embed_scatter_kernel, p.tiles, kSortThreads, kSortSmem, st, true, s, digit);
+      launch_kernel(embed_count_kernel, p.tiles + (digit == 0 ? kSms : 0), kSortThreads, 0, st, true, s, digit);
+      launch_kernel(embed_scatter_kernel, p.tiles, kSortThreads, 0, st, true, s, digit);
     }
-    launch_kernel(embed_bounds_kernel, std::min(ceil_div(T, 256), kSms * 8), 256, 0, st, true, s);
+    if (p.digits > 1) launch_kernel(embed_bounds_kernel, std::min(ceil_div(T, 256), kSms * 8), 256, 0, st, true, s);
   }
   // Rows without positions are cleared beside the chunks where they are many, as much as the chunks take to run; the others beside the join, whose
   // blocks are short: in the chunks' launch the last ones would be theirs.

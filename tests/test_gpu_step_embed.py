@@ -125,8 +125,8 @@ def test_gradient_of_strided_rows(off, pad):
 
 
 # The one launch of few positions, the sort in one, the digits' sort: on both sides of where one takes over.
-@pytest.mark.parametrize("T", [127, 128, 129, 32767, 32768, 32769])
-@pytest.mark.parametrize("kind,v,d", [("any", 1, 1), ("bad", 300, 37), ("zipf", 320, 64), ("padding", 7, 260)])
+@pytest.mark.parametrize("T", [127, 128, 129, 16384, 16385, 32768, 32769, 310000])
+@pytest.mark.parametrize("kind,v,d", [("any", 1, 1), ("bad", 300, 37), ("bad", 511, 4), ("zipf", 512, 3), ("any", 300000, 2), ("zipf", 320, 64), ("padding", 7, 260)])
 def test_gradient_where_the_kernels_change(kind, T, v, d):
     rng = np.random.default_rng(T)
     tokens = tokens_of(kind, T, v, rng)
