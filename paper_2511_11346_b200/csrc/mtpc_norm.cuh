@@ -297,10 +297,11 @@ struct NormGradArgs {
   float eps, inv_d;
 };
 
-// Every block has every gridDim.x-th row (of ROWS > 1 threadIdx.y each, rows of a warp: 16384 rows of 64 11 instead of 15 us) and keeps its part of d weight in registers, NV vectors of eight elements a thread; its vectors of the next AHEAD
-// rows are on their way to registers. What bounds it is what the SM issues for a row beside its bytes, so the arithmetic goes by packed pairs: 8192 rows
-// of 4096 (bf16, d_out fp32) one by one 88 to 104 us, with rows fetched by cp.async through shared memory, where issuing the copies took 1000 of 3500
-// cycles a row, 65 to 78. SPLIT: rows that start off their vectors, at the same columns in all rows of a block.
+// Every block has every gridDim.x-th row (of ROWS > 1 threadIdx.y each, rows of a warp: 16384 rows of 64 11 instead of 15 us) and keeps its part of
+// d weight in registers, NV vectors of eight elements a thread; its vectors of the next AHEAD rows are on their way to registers. What bounds it is what the
+// SM issues for a row beside its bytes, so the arithmetic goes by packed pairs: 8192 rows of 4096 (bf16, d_out fp32) one by one 88 to 104 us, with rows
+// fetched by cp.async through shared memory, where issuing the copies took 1000 of 3500 cycles a row, 65 to 78. SPLIT: rows that start off their
+// vectors, at the same columns in all rows of a block.
 template <typename IO, typename DY, typename DX, int NV, int AHEAD, int THREADS, int CTAS, bool SPLIT, int ROWS>
 __global__ void __launch_bounds__(THREADS, CTAS) rmsnorm_grad_kernel(const __grid_constant__ NormGradArgs a) {
   __shared__ float red[3][32];

@@ -92,37 +92,41 @@ void launch_rmsnorm(const NormArgs& a, RowPath path, cudaStream_t st) {
 
 // Blocks of the gradient kernel: as many as an SM takes, of two rows (a warp) at least where there are rows for every SM.
 constexpr int kGradRows = 8;            // rows of a block whose warps have one each, d <= 256
-int norm_grad_blocks(int T, int d) {
+int norm_grad_blocks(int T, int d, int vectors_a_thread = 2) {
   if (d <= 256) return std::min(ceil_div(T, kGradRows), 2 * kSms);
-  const int per_sm = d > 4096 ? 1 : d > 2048 ? 2 : std::min(16, 512 / round_warp(ceil_div(d, 8)));
+  const int per_sm = d > 4096 ? 1 : std::max(1, std::min(16, 512 / round_warp(ceil_div(d, 8 * vectors_a_thread))));
   return std::min(T, std::max(kSms, std::min(kSms * per_sm, T / 2)));
 }
-// Returns the blocks launched, each of which leaves its part of d weight (at most `blocks`).
+// Returns the blocks launched, each of which leaves its part of d weight.
 template <typename IO, typename DY, typename DX, bool SPLIT>
-int launch_rmsnorm_grad_vectors(const NormGradArgs& a, int blocks, cudaStream_t st) {
+int launch_rmsnorm_grad_vectors(const NormGradArgs& a, cudaStream_t st) {
   const int packs = ceil_div(a.d, 8);
-  // Two blocks with two vectors a thread where a row ahead of them fits the registers, else one with one vector: 8192 rows of 4096, d_out fp32, two blocks /
-  // one, us: all else bf16 57 / 64, fp32 sum 94 / 70, fp32 d_x 107 / 80, all fp32 124 / 86.
-  constexpr bool kNarrow = sizeof(IO) + sizeof(DY) + sizeof(DX) <= 8;
-  if (packs > 256 && packs <= 512 && !kNarrow) blocks = std::min(blocks, kSms);
+  // Two vectors a thread where a row ahead of them fits the registers and a warp has that many, else one; us, two / one: 8192 rows of 4096, d_out fp32,
+  // all else bf16 57 / 64, fp32 sum 94 / 70, fp32 d_x 107 / 80, all fp32 124 / 86; 16384 rows, all bf16: of 2048 57 / 67, of 1024 34.6 / 36.9, of
+  // 512 24.7 / 23.9; of 2047, in split rows, 68 / 64.
+  constexpr bool kNarrow = !SPLIT && sizeof(IO) + sizeof(DY) + sizeof(DX) <= 8;
+  const int nv = packs > 512 || (kNarrow && packs > 64) ? 2 : 1, threads = round_warp(ceil_div(packs, nv));
+  int blocks = norm_grad_blocks(a.T, a.d, nv);
   if (SPLIT && packs > 32 && blocks < a.T) blocks = std::max(8, blocks / 8 * 8);        // a block's rows start alike
   if (packs <= 32)
     launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 1, 1, 256, 2, SPLIT, kGradRows>, blocks, dim3(32, kGradRows), 0, st, true, a);
-  else if (packs <= 256)
-    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 1, 1, 256, 2, SPLIT, 1>, blocks, round_warp(packs), 0, st, true, a);
-  else if (packs <= 512 && kNarrow)
-    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 2, 1, 256, 2, SPLIT, 1>, blocks, round_warp(ceil_div(packs, 2)), 0, st, true, a);
-  else if (packs <= 512)
-    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 1, 1, 512, 1, SPLIT, 1>, blocks, round_warp(packs), 0, st, true, a);
-  else
-    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 2, 1, 512, 1, SPLIT, 1>, blocks, round_warp(ceil_div(packs, 2)), 0, st, true, a);
+  else if (threads <= 256 && nv == 1)
+    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 1, 1, 256, 2, SPLIT, 1>, blocks, threads, 0, st, true, a);
+  else if (nv == 1)
+    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 1, 1, 512, 1, SPLIT, 1>, blocks, threads, 0, st, true, a);
+  else if constexpr (kNarrow) {
+    if (threads <= 256) launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 2, 1, 256, 2, SPLIT, 1>, blocks, threads, 0, st, true, a);
+    else launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 2, 1, 512, 1, SPLIT, 1>, blocks, threads, 0, st, true, a);
+  } else
+    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 2, 1, 512, 1, SPLIT, 1>, blocks, threads, 0, st, true, a);
   return blocks;
 }
 template <typename IO, typename DY, typename DX>
-int launch_rmsnorm_grad(const NormGradArgs& a, int blocks, RowPath path, cudaStream_t st) {
+int launch_rmsnorm_grad(const NormGradArgs& a, RowPath path, cudaStream_t st) {
   const int packs = ceil_div(a.d, 8);
   if (packs <= 1024 && path != kRowElements)
-    return path == kRowVectors ? launch_rmsnorm_grad_vectors<IO, DY, DX, false>(a, blocks, st) : launch_rmsnorm_grad_vectors<IO, DY, DX, true>(a, blocks, st);
+    return path == kRowVectors ? launch_rmsnorm_grad_vectors<IO, DY, DX, false>(a, st) : launch_rmsnorm_grad_vectors<IO, DY, DX, true>(a, st);
+  const int blocks = norm_grad_blocks(a.T, a.d);
   if (path == kRowVectors)
     launch_kernel(rmsnorm_grad_plain_kernel<IO, DY, DX, 8, 4>, blocks, round_warp(ceil_div(packs, 4)), 0, st, true, a);
   else if (a.d <= 4096)
@@ -132,8 +136,8 @@ int launch_rmsnorm_grad(const NormGradArgs& a, int blocks, RowPath path, cudaStr
   return blocks;
 }
 template <typename IO, typename DY>
-int launch_rmsnorm_grad(const NormGradArgs& a, int dx_dtype, int blocks, RowPath path, cudaStream_t st) {
-  return dx_dtype == MTPC_F32 ? launch_rmsnorm_grad<IO, DY, float>(a, blocks, path, st) : launch_rmsnorm_grad<IO, DY, __nv_bfloat16>(a, blocks, path, st);
+int launch_rmsnorm_grad(const NormGradArgs& a, int dx_dtype, RowPath path, cudaStream_t st) {
+  return dx_dtype == MTPC_F32 ? launch_rmsnorm_grad<IO, DY, float>(a, path, st) : launch_rmsnorm_grad<IO, DY, __nv_bfloat16>(a, path, st);
 }
 
 // ---------------------------------------------------------------- embedding
@@ -538,11 +542,11 @@ int mtpc_residual_rmsnorm_backward(const void* sum, int64_t sum_stride, int32_t 
                                    rows(d_x, d_x_stride, d_x_dtype)}, &a.shift, &a.pitch);
     const RowPath path = vectors ? kRowVectors : alike ? kRowSplit : kRowElements;
     if (io_dtype == MTPC_F32)
-      parts = d_out_dtype == MTPC_F32 ? launch_rmsnorm_grad<float, float>(a, d_x_dtype, blocks, path, st)
-                                      : launch_rmsnorm_grad<float, __nv_bfloat16>(a, d_x_dtype, blocks, path, st);
+      parts = d_out_dtype == MTPC_F32 ? launch_rmsnorm_grad<float, float>(a, d_x_dtype, path, st)
+                                      : launch_rmsnorm_grad<float, __nv_bfloat16>(a, d_x_dtype, path, st);
     else
-      parts = d_out_dtype == MTPC_F32 ? launch_rmsnorm_grad<__nv_bfloat16, float>(a, d_x_dtype, blocks, path, st)
-                                      : launch_rmsnorm_grad<__nv_bfloat16, __nv_bfloat16>(a, d_x_dtype, blocks, path, st);
+      parts = d_out_dtype == MTPC_F32 ? launch_rmsnorm_grad<__nv_bfloat16, float>(a, d_x_dtype, path, st)
+                                      : launch_rmsnorm_grad<__nv_bfloat16, __nv_bfloat16>(a, d_x_dtype, path, st);
   }
   if (d_weight)
     launch_kernel(norm_weight_grad_kernel, ceil_div(d, 32), dim3(32, 32), 0, st, true, static_cast<const float*>(a.partial), parts, d, d_weight);
