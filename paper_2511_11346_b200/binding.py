@@ -528,7 +528,8 @@ def mtpc_residual_rmsnorm_backward(sum, weight, eps: float, d_out, d_sum, d_x, d
 
 
 class GradientList:
-    """The gradient buffers of a model, for mtpc_clip_gradients: made once, used every step. Keeps the tensors alive."""
+    """The gradient buffers of a model, for mtpc_clip_gradients: made once, used every step. Keeps the tensors alive; its workspace belongs to the stream
+    that it is made on, so work with it on other streams, and graphs that hold such work, are done before it is dropped."""
 
     def __init__(self, grads, outs=None, stream=None):
         """grads: contiguous fp32 or bf16 tensors of one device; outs: where the scaled gradients go (None: in place; a None in it: nowhere,

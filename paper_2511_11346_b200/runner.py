@@ -207,10 +207,12 @@ class DeviceHead:
         t = torch.from_numpy(self.wl.targets).to(self.device) if targets is None else targets
         T = h.shape[0]
         f32 = dict(dtype=torch.float32, device=self.device)
+        shapes = dict(slot_loss=(s.n,), loss=(1,), dh=(T, s.d), dW_emit=(s.n, s.r, s.v, s.d), dW_sum=(s.sum_rows, s.d),
+                      dT_static=(max(s.n - 1, 1), s.r, s.r) if s.family == I.HMM else None)
         if out is None:
-            out = dict(slot_loss=torch.empty(s.n, **f32), loss=torch.empty(1, **f32), dh=torch.empty((T, s.d), **f32),
-                       dW_emit=torch.empty((s.n, s.r, s.v, s.d), **f32), dW_sum=torch.empty((s.sum_rows, s.d), **f32),
-                       dT_static=torch.empty((max(s.n - 1, 1), s.r, s.r), **f32) if s.family == I.HMM else None)
+            out = {k: None if shape is None else torch.empty(shape, **f32) for k, shape in shapes.items()}
+        elif any((out[k] is None) != (shape is None) or (shape is not None and out[k].shape != shape) for k, shape in shapes.items()):
+            raise B.MtpcError(B.ERR_SHAPE, "window_loss_backward: out is of a call with other sizes")
         self.head.mtpc_window_loss_backward(h, t, num_sequences, sequence_length, gamma, out["slot_loss"], out["loss"],
                                             out["dh"], out["dW_emit"], out["dW_sum"], out["dT_static"])
         if max_norm is not None:

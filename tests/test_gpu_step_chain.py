@@ -70,6 +70,18 @@ def test_training_step(family, n, r, v, d, N, L):
     dh.close()
 
 
+def test_buffers_of_a_call_with_other_sizes_are_refused():
+    wl = I.make_workload("chain", I.HeadShape(I.CP, 4, 8, 256, 256), 24, seed=3, weight_std=0.1)
+    dh = R.DeviceHead(wl)
+    hidden, targets = dh.hidden_device(), torch.from_numpy(wl.targets).cuda()
+    out = dh.window_loss_backward(2, 8, 0.9, hidden=hidden[:16], targets=targets[:16], max_norm=1.0)
+    with pytest.raises(B.MtpcError):
+        dh.window_loss_backward(3, 8, 0.9, hidden=hidden, targets=targets, out=out, max_norm=1.0)
+    again = dh.window_loss_backward(2, 8, 0.9, hidden=hidden[8:], targets=targets[8:], out=out, max_norm=1.0)
+    assert again is out
+    dh.close()
+
+
 def test_training_step_of_a_factored_head_with_a_tied_table():
     n, r, v, d, k, N, L = 3, 4, 320, 128, 16, 2, 60
     T = N * L

@@ -170,6 +170,20 @@ def test_backward_of_strided_rows_and_in_place(off, pad):
     check_backward(s, w, up[:1].expand(T, d), more[:1].expand(T, d), out[:, :d], dw)
 
 
+@pytest.mark.parametrize("T,d,off", [(300, 520, 1), (300, 2048, 3), (5, 8200, 0), (3, 20001, 0), (300, 64, 5)])
+def test_backward_in_place_of_rows_that_are_not_alike_or_wide(T, d, off):
+    torch.manual_seed(T + d)
+    s, more, w, dw = rows(T, d, torch.float32), rows(T, d, torch.float32), torch.randn(d, device="cuda"), torch.empty(d, device="cuda")
+    up = rows(T, d, torch.float32, off)
+    for which in range(3):
+        a = [s.clone(), torch.cat([torch.zeros(off, device="cuda"), up.flatten()])[off:].view(T, d), more.clone()]
+        check_backward(a[0], w, a[1], a[2], a[which], dw)
+    x, res = rows(T, d, torch.bfloat16), rows(T, d, torch.bfloat16, off)
+    for which in range(2):
+        a = [x.clone(), torch.cat([torch.zeros(off, device="cuda").bfloat16(), res.flatten()])[off:].view(T, d)]
+        check_forward(a[0], a[1], w, torch.empty_like(x), a[which])
+
+
 # Rows that start off their vectors, alike in all matrices and not; more of them than blocks, of which 144 at least take part in d weight here.
 @pytest.mark.parametrize("T,d,off,pad", [(700, 1001, 0, 0), (400, 2047, 3, 0), (310, 4099, 5, 4), (20, 8191, 0, 0), (500, 5, 1, 0), (500, 13, 0, 1), (300, 520, 3, 8),
                                          (9, 9, 0, 0)])
