@@ -9,7 +9,6 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
-import struct
 
 from . import build as _build
 
@@ -534,7 +533,7 @@ class GradientList:
     def __init__(self, grads, outs=None, stream=None):
         """grads: contiguous fp32 or bf16 tensors of one device; outs: where the scaled gradients go (None: in place; a None in it: nowhere,
         that gradient counts in the norm alone)."""
-        import torch
+        import numpy as np
         what = "mtpc_create_gradient_list"
         self.handle = None
         grads = list(grads)
@@ -542,25 +541,36 @@ class GradientList:
         if not grads or len(outs) != len(grads):
             raise MtpcError(ERR_SHAPE, f"{what}: {len(grads)} gradients, {len(outs)} results")
         self.device = grads[0].get_device()
-        codes, table = _dtypes(), bytearray(32 * len(grads))
-        for i, (g, o) in enumerate(zip(grads, outs)):
-            count = g.numel()
-            for t in (g,) if o is None or o is g else (g, o):
-                if not t.is_cuda or t.get_device() != self.device or not t.is_contiguous() or t.numel() != count:
-                    _refuse(what, f"{tuple(t.shape)} with strides {t.stride()} on {t.device}")
-                if t.dtype not in codes:
-                    _refuse(what, f"{t.dtype}", ERR_UNSUPPORTED)
-            struct.pack_into("=QQqii", table, 32 * i, g.data_ptr(), 0 if o is None else o.data_ptr(), count, codes[g.dtype],
-                             codes[g.dtype if o is None else o.dtype])          # an mtpc_gradient
-        entries = (MtpcGradient * len(grads)).from_buffer(table)
+        codes = _dtypes()
+
+        def columns(tensors):                                # one quantity after the other: a list may have thousands
+            if self.device < 0 or any(t.get_device() != self.device for t in tensors) or not all([t.is_contiguous() for t in tensors]):
+                t = next(t for t in tensors if not t.is_cuda or t.get_device() != self.device or not t.is_contiguous())
+                _refuse(what, f"{tuple(t.shape)} with strides {t.stride()} on {t.device}")
+            kinds = [codes.get(t.dtype) for t in tensors]
+            if None in kinds:
+                _refuse(what, f"{tensors[kinds.index(None)].dtype}", ERR_UNSUPPORTED)
+            return [t.data_ptr() for t in tensors], [t.numel() for t in tensors], kinds
+
+        entries = np.zeros(len(grads), dtype=MtpcGradient)
+        entries["data"], entries["count"], entries["dtype"] = columns(grads)
+        entries["out"], entries["out_dtype"] = entries["data"], entries["dtype"]
+        if outs is not grads:
+            to = [g if o is None else o for g, o in zip(grads, outs)]
+            entries["out"], counts, entries["out_dtype"] = columns(to)
+            wrong = next((i for i, g in enumerate(grads) if counts[i] != g.numel()), None)
+            if wrong is not None:
+                _refuse(what, f"a result of {counts[wrong]} elements for a gradient of {grads[wrong].numel()}")
+            entries["out"][[i for i, o in enumerate(outs) if o is None]] = 0
+        raw_entries = entries.ctypes.data
         need = ctypes.c_size_t(0)
-        _check(lib().mtpc_gradient_list_workspace_bytes(entries, len(grads), ctypes.byref(need)), "mtpc_gradient_list_workspace_bytes")
+        _check(lib().mtpc_gradient_list_workspace_bytes(raw_entries, len(grads), ctypes.byref(need)), "mtpc_gradient_list_workspace_bytes")
         self._keep = (grads, outs)
         handle = ctypes.c_void_p(0)
         self.workspace = _scratch(what, None, need.value, self.device, stream)
 
         def create(raw):
-            return lib().mtpc_create_gradient_list(entries, len(grads), self.workspace.data_ptr(), need.value, raw, ctypes.byref(handle))
+            return lib().mtpc_create_gradient_list(raw_entries, len(grads), self.workspace.data_ptr(), need.value, raw, ctypes.byref(handle))
         _call(what, create, self.device, stream)
         self.handle = handle
 
