@@ -371,30 +371,35 @@ def _refuse(what: str, why: str, code: int = ERR_SHAPE):
     raise MtpcError(code, f"{what}: {why}")
 
 
+_dtype_codes = None
+
+
 def _dtypes() -> dict:
-    global _dtype_codes
+    """What the calls look up in torch, once (an import statement in every call costs a tenth of a small one)."""
+    global _dtype_codes, _current_device, _raw_stream, _int32, _float32
     if _dtype_codes is None:
         import torch
+        _current_device, _int32, _float32 = torch._C._cuda_getDevice, torch.int32, torch.float32
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
         _dtype_codes = {torch.float32: MTPC_F32, torch.bfloat16: MTPC_BF16}
     return _dtype_codes
 
 
-_dtype_codes = None
-
-
 def _dtype(what: str, t) -> int:
-    code = _dtypes().get(t.dtype)
+    code = _dtype_codes.get(t.dtype)
     if code is None:
         _refuse(what, f"{t.dtype}", ERR_UNSUPPORTED)
     return code
 
 
 def _matrix(what: str, t):
-    """(rows, columns, device) of a matrix on a device."""
-    if t.dim() != 2 or not t.is_cuda:
-        _refuse(what, f"{tuple(t.shape)} on {t.device} where a matrix on a device is needed")
-    rows, columns = t.shape
-    return rows, columns, t.get_device()
+    """(rows, columns, stride, device) of a matrix on a device whose rows are adjacent elements."""
+    shape, device = t.shape, t.get_device()
+    if len(shape) == 2 and device >= 0:
+        stride, inner = t.stride()
+        if inner == 1 or shape[1] == 1:
+            return shape[0], shape[1], stride, device
+    _refuse(what, f"{tuple(t.shape)} with strides {t.stride()} on {t.device} where a matrix of adjacent rows on a device is needed")
 
 
 def _rows(what: str, t, rows: int, columns: int, device: int, dtype=None) -> int:
@@ -421,10 +426,10 @@ def _vector(what: str, t, count: int, device: int, dtype=None) -> int:
 
 def _call(what: str, function, device: int, stream, *args) -> None:
     """The call on `stream` (None: torch's current one of the device), with the tensors' device as the current one: a launch goes there."""
-    import torch
-    if torch._C._cuda_getDevice() == device:
-        code = function(*args, _stream(stream, device))
+    if _current_device() == device:
+        code = function(*args, _stream(stream, device) if stream is not None else _raw_stream(device))
     else:
+        import torch
         with torch.cuda.device(device):
             code = function(*args, _stream(stream, device))
     if code != MTPC_OK:
@@ -454,13 +459,13 @@ def _scratch(what: str, workspace, need: int, device: int, stream):
 def mtpc_embed(tokens, table, out, scale: float = 1.0, out_status=None, stream=None) -> None:
     """out[t] = scale * table[tokens[t]]; a negative token is a row of zeros (include/mtpc.h). tokens [T] int32, table [v, d] and out [T, d]
     fp32 or bf16; out_status: int32 [1], into which the status bits are or-ed."""
-    import torch
+    _dtypes()
     what = "mtpc_embed"
-    v, d, dev = _matrix(what, table)
+    v, d, stride, dev = _matrix(what, table)
     T = tokens.numel()
-    _call(what, lib().mtpc_embed, dev, stream, _vector(what, tokens, T, dev, torch.int32), T, table.data_ptr(), _rows(what, table, v, d, dev),
+    _call(what, lib().mtpc_embed, dev, stream, _vector(what, tokens, T, dev, _int32), T, table.data_ptr(), stride,
           _dtype(what, table), v, d, scale, out.data_ptr(), _rows(what, out, T, d, dev), _dtype(what, out),
-          _vector(what, out_status, 1, dev, torch.int32))
+          _vector(what, out_status, 1, dev, _int32))
 
 
 def mtpc_embed_backward_workspace_bytes(T: int, v: int, d: int) -> int:
@@ -471,37 +476,40 @@ def mtpc_embed_backward(tokens, d_out, d_table, scale: float = 1.0, accumulate: 
                         stream=None) -> None:
     """d_table[b] = scale * sum of d_out[t] over the positions with token b, or added to it (accumulate). tokens [T] int32, d_out [T, d]
     fp32 or bf16, d_table [v, d] fp32. workspace None: from torch's allocator, for the call."""
-    import torch
+    _dtypes()
     what = "mtpc_embed_backward"
-    v, d, dev = _matrix(what, d_table)
+    v, d, stride, dev = _matrix(what, d_table)
+    if d_table.dtype is not _float32:
+        _refuse(what, f"{d_table.dtype} where {_float32} is needed", ERR_UNSUPPORTED)
     T = tokens.numel()
     ws = _scratch(what, workspace, _scratch_bytes("mtpc_embed_backward_workspace_bytes", T, v, d), dev, stream)
-    _call(what, lib().mtpc_embed_backward, dev, stream, _vector(what, tokens, T, dev, torch.int32), T, d_out.data_ptr(),
-          _rows(what, d_out, T, d, dev), _dtype(what, d_out), scale, v, d, d_table.data_ptr(), _rows(what, d_table, v, d, dev, torch.float32),
-          1 if accumulate else 0, ws.data_ptr(), ws.numel(), _vector(what, out_status, 1, dev, torch.int32))
+    _call(what, lib().mtpc_embed_backward, dev, stream, _vector(what, tokens, T, dev, _int32), T, d_out.data_ptr(),
+          _rows(what, d_out, T, d, dev), _dtype(what, d_out), scale, v, d, d_table.data_ptr(), stride,
+          1 if accumulate else 0, ws.data_ptr(), ws.numel(), _vector(what, out_status, 1, dev, _int32))
 
 
 def mtpc_residual_rmsnorm(x, residual, weight, eps: float, out, out_sum=None, out_q=None, out_scale=None, scale_group: int = 0,
                           stream=None) -> None:
     """out_sum = x + residual (residual None: x), out = its root-mean-square norm times weight (None: ones); out_q [T, d] e4m3 (or uint8) with
     out_scale [T, ceil(d / scale_group)] fp32 (scale_group 0: [T, 1]): the same in 8 bits. out or out_q may be None."""
-    import torch
+    _dtypes()
     what = "mtpc_residual_rmsnorm"
-    T, d, dev = _matrix(what, x)
+    T, d, stride, dev = _matrix(what, x)
     io = x.dtype
     r_stride = 0 if residual is None else _rows(what, residual, T, d, dev, io)
     s_stride = 0 if out_sum is None else _rows(what, out_sum, T, d, dev, io)
     o_stride = 0 if out is None else _rows(what, out, T, d, dev, io)
     q_stride = 0
     if out_q is not None:
+        import torch
         q_stride = _rows(what, out_q, T, d, dev)
         if out_q.dtype not in (torch.float8_e4m3fn, torch.uint8):
             _refuse(what, f"{out_q.dtype}", ERR_UNSUPPORTED)
     if out_scale is not None:
-        _rows(what, out_scale, T, -(-d // scale_group) if scale_group > 0 else 1, dev, torch.float32)
+        _rows(what, out_scale, T, -(-d // scale_group) if scale_group > 0 else 1, dev, _float32)
         if not out_scale.is_contiguous():
             _refuse(what, f"out_scale with strides {out_scale.stride()}")
-    _call(what, lib().mtpc_residual_rmsnorm, dev, stream, x.data_ptr(), _rows(what, x, T, d, dev), _ptr(residual), r_stride,
+    _call(what, lib().mtpc_residual_rmsnorm, dev, stream, x.data_ptr(), stride, _ptr(residual), r_stride,
           _vector(what, weight, d, dev), MTPC_F32 if weight is None else _dtype(what, weight), T, d, _dtype(what, x), eps, _ptr(out_sum), s_stride,
           _ptr(out), o_stride, _ptr(out_q), q_stride, _ptr(out_scale), scale_group)
 
@@ -513,17 +521,17 @@ def mtpc_residual_rmsnorm_backward_workspace_bytes(T: int, d: int) -> int:
 def mtpc_residual_rmsnorm_backward(sum, weight, eps: float, d_out, d_sum, d_x, d_weight=None, workspace=None, stream=None) -> None:
     """d_x: the gradient of the sum (of x and of residual alike) from d_out, the gradient of the norm's output, and d_sum, what reaches the sum along
     the residual stream (None: nothing; d_x's dtype). d_weight [d] fp32 or None. workspace as in mtpc_embed_backward."""
-    import torch
+    _dtypes()
     what = "mtpc_residual_rmsnorm_backward"
-    T, d, dev = _matrix(what, sum)
+    T, d, stride, dev = _matrix(what, sum)
     ws, ws_ptr, ws_bytes = None, 0, 0
     if d_weight is not None:
         ws = _scratch(what, workspace, _scratch_bytes("mtpc_residual_rmsnorm_backward_workspace_bytes", T, d), dev, stream)
         ws_ptr, ws_bytes = ws.data_ptr(), ws.numel()
-    _call(what, lib().mtpc_residual_rmsnorm_backward, dev, stream, sum.data_ptr(), _rows(what, sum, T, d, dev), _dtype(what, sum),
+    _call(what, lib().mtpc_residual_rmsnorm_backward, dev, stream, sum.data_ptr(), stride, _dtype(what, sum),
           _vector(what, weight, d, dev), MTPC_F32 if weight is None else _dtype(what, weight), T, d, eps, d_out.data_ptr(),
           _rows(what, d_out, T, d, dev), _dtype(what, d_out), _ptr(d_sum), 0 if d_sum is None else _rows(what, d_sum, T, d, dev, d_x.dtype),
-          d_x.data_ptr(), _rows(what, d_x, T, d, dev), _dtype(what, d_x), _vector(what, d_weight, d, dev, torch.float32), ws_ptr, ws_bytes)
+          d_x.data_ptr(), _rows(what, d_x, T, d, dev), _dtype(what, d_x), _vector(what, d_weight, d, dev, _float32), ws_ptr, ws_bytes)
 
 
 class GradientList:
@@ -576,9 +584,8 @@ class GradientList:
 
     def mtpc_clip_gradients(self, max_norm: float, out_norm, stream=None) -> None:
         """out_norm [1] fp32: the norm of all gradients; where it is above max_norm (and finite) they are scaled by max_norm / norm."""
-        import torch
         what = "mtpc_clip_gradients"
-        _call(what, lib().mtpc_clip_gradients, self.device, stream, self.handle, max_norm, _vector(what, out_norm, 1, self.device, torch.float32))
+        _call(what, lib().mtpc_clip_gradients, self.device, stream, self.handle, max_norm, _vector(what, out_norm, 1, self.device, _float32))
 
     def mtpc_destroy_gradient_list(self) -> None:
         if self.handle:
