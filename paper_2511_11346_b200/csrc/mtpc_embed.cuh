@@ -507,57 +507,107 @@ __device__ __forceinline__ void clear_rows(const EmbedSegmentArgs& a, int part, 
   }
 }
 
+// V adjacent sums, in pairs where they are several.
+template <typename T, int V>
+struct RowSum {
+  uint64_t pairs[V / 2 > 0 ? V / 2 : 1];
+  float one;
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (uint64_t& x : pairs) x = 0;
+    one = 0.f;
+  }
+  __device__ __forceinline__ void add(const Raw<T, V>& x) {
+    if constexpr (V == 1) {
+      one += x.value(0);
+    } else {
+#pragma unroll
+      for (int i = 0; i < V / 2; ++i) pairs[i] = add2(pairs[i], x.pair(i));
+    }
+  }
+  __device__ __forceinline__ void get(float (&x)[V]) const {
+    if constexpr (V == 1) {
+      x[0] = one;
+    } else {
+#pragma unroll
+      for (int i = 0; i < V / 2; ++i) {
+        const float2 y = unpack2(pairs[i]);
+        x[2 * i] = y.x, x[2 * i + 1] = y.y;
+      }
+    }
+  }
+};
+
 // A block per chunk and slab of columns (the slabs of a chunk follow each other), beside those that clear. U rows are in flight per thread. A slab is
 // 4 KB of a row where rows are that long: in slabs of 1 KB, with four times as long chunks, the kernel alone takes 26 to 32 us instead of
 // 25 (8192 x 4096 fp32), by registers or by a ring of cp.async.
 template <typename T, int V, int U>
 __global__ void __launch_bounds__(kSegmentThreads, 4) embed_segment_kernel(const __grid_constant__ EmbedSegmentArgs a) {
-  __shared__ int key[kSegmentStage + 1], pos[kSegmentStage];
+  static_assert(32 % U == 0 && kSegmentStage == 256, "a group's bits lie in one of eight words");
+  __shared__ alignas(16) const T* row[kSegmentStage];
+  __shared__ int key[kSegmentStage + 1];
+  __shared__ alignas(16) unsigned valid[kSegmentStage / 32], ends[kSegmentStage / 32];      // bits: has a token; the last one of it or of the chunk
   grid_dependency_wait();
   if (static_cast<int>(blockIdx.x) >= a.chunks * a.slabs) {
     clear_rows(a, blockIdx.x - a.chunks * a.slabs, gridDim.x - a.chunks * a.slabs);
     grid_launch_dependents();
     return;
   }
-  const int chunk = blockIdx.x / a.slabs;
+  const int chunk = blockIdx.x / a.slabs, lane = threadIdx.x & 31;
   const int col = ((blockIdx.x - chunk * a.slabs) * blockDim.x + threadIdx.x) * V;
   const int lo = chunk * a.chunk, hi = min(lo + a.chunk, a.T);
-  float sum[V];
-#pragma unroll
-  for (int i = 0; i < V; ++i) sum[i] = 0.f;
+  RowSum<T, V> sum;
+  sum.clear();
   float* part = a.part + static_cast<size_t>(chunk) * 2 * a.d + col;
   bool begins = true;                            // the token being added up has no position in an earlier chunk
   for (int base = lo; base < hi; base += kSegmentStage) {
-    const int count = min(hi - base, kSegmentStage);
+    const int here = min(hi - base, kSegmentStage);
     const int earlier = base == lo && lo > 0 ? a.key[lo - 1] : -1;
     __syncthreads();
-    for (int i = threadIdx.x; i <= count; i += blockDim.x) {
+    for (int i = threadIdx.x; i <= here; i += blockDim.x) {
       key[i] = base + i < a.T ? a.key[base + i] : a.v;
-      if (i < count) pos[i] = a.pos[base + i];
+      if (i < here) row[i] = static_cast<const T*>(a.d_out) + a.pos[base + i] * a.d_out_stride;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < kSegmentStage; i += blockDim.x) {
+      const bool is = i < here && key[i] != a.v;
+      const unsigned some = __ballot_sync(0xffffffffu, is), last = __ballot_sync(0xffffffffu, is && (key[i + 1] != key[i] || base + i + 1 == hi));
+      if (lane == 0) valid[i / 32] = some, ends[i / 32] = last;
     }
     __syncthreads();
     if (base == lo) begins = earlier != key[0];
-    if (key[0] == a.v) break;                    // the rest of the positions have no token
+    int count = 0;                               // the positions that have a token come first
+#pragma unroll
+    for (int w = 0; w < kSegmentStage / 32; ++w) count += __popc(valid[w]);
+    if (count == 0) break;
+    if (col >= a.d) continue;
     for (int i = 0; i < count; i += U) {
       Raw<T, V> x[U];
+      const unsigned stops = ends[i / 32] >> (i % 32);
+      if (i + U <= count) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (i + u < count && key[i + u] != a.v && col < a.d)
-          x[u].load(static_cast<const T*>(a.d_out) + pos[i + u] * a.d_out_stride + col);
+        for (int u = 0; u < U; ++u) x[u].load(row[i + u] + col);
+      } else {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (i + u < count) x[u].load(row[i + u] + col);
+      }
+      if (i + U <= count && (stops & ((1u << U) - 1u)) == 0u) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) sum.add(x[u]);
+        continue;
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        if (i + u >= count || key[i + u] == a.v) break;
-#pragma unroll
-        for (int e = 0; e < V; ++e) sum[e] += x[u].value(e);
-        const bool ends = key[i + u + 1] != key[i + u];
-        if (ends || base + i + u + 1 == hi) {
-          if (col < a.d) {
-            if (begins && ends) write_table<V>(a, key[i + u], col, sum);
-            else store_f32<float, V>(part + (begins ? a.d : 0), sum);
-          }
-#pragma unroll
-          for (int e = 0; e < V; ++e) sum[e] = 0.f;
+        if (i + u >= count) break;
+        sum.add(x[u]);
+        if ((stops >> u) & 1u) {
+          float total[V];
+          sum.get(total);
+          const bool over = key[i + u + 1] != key[i + u];                // the token's last position, not only the chunk's
+          if (begins && over) write_table<V>(a, key[i + u], col, total);
+          else store_f32<float, V>(part + (begins ? a.d : 0), total);
+          sum.clear();
           begins = true;
         }
       }
