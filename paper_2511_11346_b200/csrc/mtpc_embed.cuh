@@ -15,7 +15,8 @@
 //                         (embed_bounds_kernel: where each token's positions begin and end, which the one-launch sort and a single digit's know)
 //   embed_segment_kernel  the chunks
 //   embed_join_kernel     the tokens that cross chunks
-// A step of a few positions is all launches: up to kFewT of them embed_few_kernel does it alone, row of the table after row.
+// A step of a few positions is all launches: up to kFewT of them embed_few_kernel does it alone, row of the table after row, where the table is
+// not a large one.
 // Rows that no position has are zeros: written by further blocks of the last two, behind whose short chains of dependent loads that hides.
 #pragma once
 #include <cuda_bf16.h>
@@ -679,7 +680,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) embed_join_kernel(const __gri
 }
 
 // Few positions: a block has its columns of every gridDim.x-th row of the table and adds up the positions that have the row's token, U on their way at a
-// time, or writes zeros. (T = 128, d = 1024, bf16: the other kernels 14 us, this one 4.)
+// time, or writes zeros. (T = 128, d = 1024, bf16, 268 rows: the other kernels 14 us, this one 6.)
 constexpr int kFewT = 128, kFewThreads = 256;
 template <typename T, int V, int U>
 __global__ void __launch_bounds__(kFewThreads) embed_few_kernel(const int* tokens, const __grid_constant__ EmbedSegmentArgs a, unsigned* status) {

@@ -22,6 +22,7 @@ using namespace mtpc;
 constexpr size_t kAlign = 256;
 constexpr int kMaxRows = 1 << 30;
 constexpr long long kClearBesideChunks = 32 << 20;    // bytes
+constexpr long long kFewBytes = 32 << 20;
 constexpr int kSms = 148;               // what grids are sized for: the results of sums that are cut by them do not depend on the device
 size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 bool aligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
@@ -97,7 +98,6 @@ void launch_rmsnorm(const NormArgs& a, RowPath path, cudaStream_t st) {
 // Blocks of the gradient kernel: as many as an SM takes, of two rows (a warp) at least where there are rows for every SM.
 constexpr int kGradRows = 8;            // rows of a block whose warps have one each, d <= 256
 int norm_grad_blocks(int T, int d, int vectors_a_thread = 2) {
-  if (d <= 256) return std::min(ceil_div(T, kGradRows), 2 * kSms);
   const int per_sm = d > 4096 ? 1 : std::max(1, std::min(16, 512 / round_warp(ceil_div(d, 8 * vectors_a_thread))));
   return std::min(T, std::max(kSms, std::min(kSms * per_sm, T / 2)));
 }
@@ -110,7 +110,7 @@ int launch_rmsnorm_grad_vectors(const NormGradArgs& a, cudaStream_t st) {
   // 512 24.7 / 23.9; of 2047, in split rows, 68 / 64.
   constexpr bool kNarrow = !SPLIT && sizeof(IO) + sizeof(DY) + sizeof(DX) <= 8;
   const int nv = packs > 512 || (kNarrow && packs > 64) ? 2 : 1, threads = round_warp(ceil_div(packs, nv));
-  int blocks = norm_grad_blocks(a.T, a.d, nv);
+  int blocks = packs <= 32 ? std::min(ceil_div(a.T, kGradRows), 2 * kSms) : norm_grad_blocks(a.T, a.d, nv);
   if (SPLIT && packs > 32 && blocks < a.T) blocks = std::max(8, blocks / 8 * 8);        // a block's rows start alike
   if (packs <= 32)
     launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 1, 1, 256, 2, SPLIT, kGradRows>, blocks, dim3(32, kGradRows), 0, st, true, a);
@@ -378,7 +378,9 @@ int mtpc_embed_backward(const int32_t* tokens, int32_t T, const void* d_out, int
     return table_allows(vec) && rows_allow(d_out, d_out_stride, element(d_out_dtype), vec, T);
   };
   const int vec = vectors(4) ? 4 : 1;
-  if (T <= kFewT) {
+  // One launch for few positions, but where most of its time would be clearing (one launch / three, us: 128 positions, 5000 rows of 512 6.5 / 12.4,
+  // 32768 rows 24 / 18.6), which it does row after row.
+  if (T <= kFewT && (accumulate ? v <= 32768 : static_cast<long long>(v) * d * 4 <= kFewBytes)) {
     const int threads = std::min(kFewThreads, round_warp(ceil_div(d, vec)));
     const dim3 grid(std::min(v, kSms * 16), ceil_div(d, threads * vec));
     if (d_out_dtype == MTPC_F32)

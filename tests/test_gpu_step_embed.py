@@ -92,7 +92,7 @@ def check_gradient(tokens, d_out, v, d_table, scale, start=None, status=None):
     ("any", 1, 320, 4096), ("zipf", 8192, 320, 512), ("zipf", 8192, 320, 1000), ("one", 5000, 320, 256), ("one", 16385, 3, 64), ("runs", 3000, 400, 96),
     ("runs", 16384, 511, 40), ("runs", 4097, 512, 1001), ("padding", 100, 10, 64), ("bad", 2000, 77, 64), ("any", 2005, 32768, 128), ("any", 17, 300000, 8),
     ("zipf", 40000, 320, 72), ("any", 33000, 5000, 33), ("any", 20000, 300000, 4), ("one", 70001, 1, 16), ("runs", 70000, 900, 12), ("any", 16, 4, 20000),
-    ("any", 2, 2, 1), ("runs", 300000, 700, 3),
+    ("any", 2, 2, 1), ("runs", 300000, 700, 3), ("any", 100, 32768, 300), ("bad", 128, 33000, 257), ("any", 1, 40000, 256),
 ])
 def test_gradient(grad, kind, T, v, d):
     rng = np.random.default_rng(T + v)
@@ -103,7 +103,8 @@ def test_gradient(grad, kind, T, v, d):
     assert status.item() == (B.STATUS_BAD_TOKEN if kind == "bad" else 0)
 
 
-@pytest.mark.parametrize("kind,T,v,d", [("zipf", 3000, 320, 256), ("any", 5, 40, 33), ("one", 400, 3, 64), ("zipf", 20000, 320, 24)])
+@pytest.mark.parametrize("kind,T,v,d", [("zipf", 3000, 320, 256), ("any", 5, 40, 33), ("one", 400, 3, 64), ("zipf", 20000, 320, 24),
+                                        ("any", 100, 32769, 12), ("any", 100, 32768, 12)])
 def test_gradient_added_to_a_tied_table(kind, T, v, d):
     rng = np.random.default_rng(9 + T)
     start = torch.randn(v, d, device="cuda")
