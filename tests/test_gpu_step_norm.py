@@ -129,6 +129,25 @@ def test_rows_of_zeros_of_extremes_and_of_what_is_no_number():
         check_backward(x, w, dy, None, dx, dw)
 
 
+@pytest.mark.parametrize("d,where", [(77, 0), (77, 76), (77, 40), (5, 2), (1003, 1002), (4099, 0)])
+def test_what_is_no_number_beside_the_vectors(d, where):
+    for t in (torch.float32, torch.bfloat16):
+        x = torch.randn(9, d, device="cuda").to(t)
+        clean = torch.empty(9, d, dtype=t, device="cuda")
+        q, scale, q2, scale2 = (f(9) for f in (lambda n: torch.empty(n, d, dtype=torch.uint8, device="cuda"), lambda n: torch.empty(n, 1, device="cuda")) * 2)
+        check_forward(x, None, None, clean, None, q, scale)
+        x[3, where], x[6, where] = float("nan"), float("-inf")
+        out = torch.empty_like(clean)
+        B.mtpc_residual_rmsnorm(x, None, None, EPS, out, out_q=q2, out_scale=scale2)
+        others = [0, 1, 2, 4, 5, 7, 8]
+        assert torch.equal(out[others], clean[others]) and torch.equal(q2[others], q[others]) and torch.equal(scale2[others], scale[others])
+        assert torch.isnan(out[3]).all() and torch.isnan(scale2[3]) and torch.isnan(q2[3].view(torch.float8_e4m3fn).float()).all()
+        assert torch.isnan(out[6, where]) and torch.isnan(scale2[6])
+        x[3, where], x[6, where] = 0, 0
+        x[3, where] = torch.finfo(t).max                                    # a single element beyond what fp32 can square
+        check_forward(x, None, None, out, None, q2, scale2)
+
+
 def check_backward(s, weight, dy, more, dx, dw, eps=EPS):
     given = host(s), host(weight), host(dy), host(more)
     B.mtpc_residual_rmsnorm_backward(s, weight, eps, dy, more, dx, dw)
