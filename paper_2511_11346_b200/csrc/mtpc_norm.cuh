@@ -44,16 +44,47 @@ __device__ __forceinline__ float larger(float x, float y) {
   return d;
 }
 
-// What a code of 1 stands for where the largest magnitude is `bits`.
-__device__ __forceinline__ float code_scale(unsigned bits) {
-  const float s = __uint_as_float(bits) * (1.f / kE4m3Max);
-  return s == 0.f ? 1.f : s;
+// 1 / x to 23 digits, for x well within the range.
+__device__ __forceinline__ float reciprocal_near(float x) {
+  float d;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(d) : "f"(x));
+  return d;
 }
-// x / scale as x * first * second (a reciprocal beside eight products, where eight divisions took longer than the row's bytes). Scales whose
-// reciprocal fp32 cannot hold go in two steps, the first a power of two.
-__device__ __forceinline__ float2 code_factors(float scale) {
-  const float first = scale < 0x1p-100f ? 0x1p64f : 1.f;
-  return make_float2(first, __fdividef(1.f, scale * first));          // (scale * first is between 2^-100 and 2^120)
+// How the elements of a group become codes whose largest magnitude is `bits`: scale, what a code of 1 stands for, is the quotient by 448 rounded once (the
+// product with the reciprocal and one step of Newton's iteration, whose remainder is exact in a fused multiply-add), and x / scale is x first hi + x first lo,
+// where hi + lo is the reciprocal to twice the digits by the same step: rounded once, to the nearest fp32 but for 2^-46 of it. (The products with reciprocals of
+// 24 digits move codes that lie near the middle of two; eight divisions beside a vector's loads take longer than the row's bytes.)
+// Magnitudes far from one take the division for the scale, below whose digits a remainder may fall, and go to the middle of the range first, by
+// a power of two, where no digit of lo is lost. A scale that is not finite has hi = 0: what is finite gives 0.
+struct alignas(16) CodeFactors {
+  float scale, first, hi, lo;
+};
+__device__ __forceinline__ CodeFactors code_factors(unsigned bits) {
+  const float x = __uint_as_float(bits);
+  CodeFactors f;
+  if (bits - 0x26800000u < 0x61000000u - 0x26800000u) {      // 2^-50 to 2^67
+    const float q = x * (1.f / kE4m3Max);
+    f.scale = fmaf(fmaf(q, -kE4m3Max, x), 1.f / kE4m3Max, q);
+    f.first = 1.f;
+    f.hi = reciprocal_near(f.scale);
+    f.lo = fmaf(-f.hi, f.scale, 1.f) * f.hi;
+  } else {
+    f.scale = x / kE4m3Max;
+    if (f.scale == 0.f) f.scale = 1.f;
+    f.first = f.scale < 0x1p-59f ? 0x1p64f : f.scale > 0x1p58f ? 0x1p-64f : 1.f;
+    const float s = f.scale * f.first;                       // (between 2^-85 and 2^60, or not finite)
+    f.hi = s < 0x1p100f ? reciprocal_near(s) : isnan(s) ? s : 0.f;
+    f.lo = s < 0x1p100f ? fmaf(-f.hi, s, 1.f) * f.hi : 0.f;
+  }
+  return f;
+}
+__device__ __forceinline__ float code_quotient(float x, const CodeFactors& f) {
+  x *= f.first;
+  return fmaf(x, f.hi, x * f.lo);
+}
+__device__ __forceinline__ uint64_t code_quotients(uint64_t x, const CodeFactors& f) {
+  if (f.first != 1.f) x = mul2(x, pack2(f.first, f.first));
+  return fma2(x, pack2(f.hi, f.hi), mul2(x, pack2(f.lo, f.lo)));
 }
 
 // The largest magnitude of the row's columns, every thread with the same.
@@ -158,6 +189,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) residual_rmsnorm_kernel(const _
 
   // The scale of every vector's group, then its codes. (Columns past the row's end are zeros.)
   unsigned largest[NV];
+  CodeFactors by[NV];
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     float m = 0.f;
@@ -174,9 +206,10 @@ __global__ void __launch_bounds__(THREADS, CTAS) residual_rmsnorm_kernel(const _
 #pragma unroll
     for (int j = 1; j < NV; ++j) m = max(m, largest[j]);
     m = row_max(m, reinterpret_cast<unsigned*>(red[1]));
+    by[0] = code_factors(m);
 #pragma unroll
-    for (int j = 0; j < NV; ++j) largest[j] = m;
-    if (tid == 0) scales[0] = code_scale(m);
+    for (int j = 1; j < NV; ++j) by[j] = by[0];
+    if (tid == 0) scales[0] = by[0].scale;
   } else {
     const int lanes = a.group / 8;                           // 4 to 16 lanes hold a group
 #pragma unroll
@@ -185,27 +218,22 @@ __global__ void __launch_bounds__(THREADS, CTAS) residual_rmsnorm_kernel(const _
       for (int o = 1; o < 16; o <<= 1)
         if (o < lanes) largest[j] = max(largest[j], __shfl_xor_sync(0xffffffffu, largest[j], o));
       const int col = begin + j * threads * 8;
-      if (inside[j] && (lane & (lanes - 1)) == 0) scales[col >> a.group_shift] = code_scale(largest[j]);
+      by[j] = code_factors(largest[j]);
+      if (inside[j] && (lane & (lanes - 1)) == 0) scales[col >> a.group_shift] = by[j].scale;
     }
   }
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     const int col = begin + j * threads * 8;
     if (!inside[j]) continue;
-    const float2 by = code_factors(code_scale(largest[j]));
     Pack<uint16_t, 4> o;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      uint64_t q = s[j][i];
-      if (by.x != 1.f) q = mul2(q, pack2(by.x, by.x));
-      const float2 x = unpack2(mul2(q, pack2(by.y, by.y)));
-      o.e[i] = __nv_cvt_float2_to_fp8x2(x, __NV_SATFINITE, __NV_E4M3);
-    }
+    for (int i = 0; i < 4; ++i) o.e[i] = __nv_cvt_float2_to_fp8x2(unpack2(code_quotients(s[j][i], by[j])), __NV_SATFINITE, __NV_E4M3);
     store_pack<uint16_t, 4>(reinterpret_cast<uint16_t*>(a.codes + row * a.codes_stride + col), o);
   }
   if (SPLIT && beside >= 0) {
-    const float2 by = code_factors(code_scale(largest[0]));
-    a.codes[row * a.codes_stride + beside] = __nv_cvt_float_to_fp8(single * by.x * by.y, __NV_SATFINITE, __NV_E4M3);
+    a.codes[row * a.codes_stride + beside] =
+        __nv_cvt_float_to_fp8(code_quotient(single, by[0]), __NV_SATFINITE, __NV_E4M3);
   }
 }
 
@@ -214,6 +242,7 @@ template <typename IO, int NV>
 __global__ void __launch_bounds__(1024) residual_rmsnorm_plain_kernel(const __grid_constant__ NormArgs a) {
   __shared__ float red[2][32];
   __shared__ unsigned group_max[kNormMaxWidth / kNormMinGroup];
+  __shared__ CodeFactors group_factors[kNormMaxWidth / kNormMinGroup];
   const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 31;
   if (a.codes != nullptr && a.group != 0) {
     for (int g = tid; g < a.groups; g += blockDim.x) group_max[g] = 0;
@@ -267,22 +296,26 @@ __global__ void __launch_bounds__(1024) residual_rmsnorm_plain_kernel(const __gr
   }
   if (a.codes == nullptr) return;
   float* scales = a.scales + static_cast<long long>(row) * a.groups;
+  CodeFactors by;
   if (a.group == 0) {
     m = row_max(m, reinterpret_cast<unsigned*>(red[1]));
-    if (tid == 0) scales[0] = code_scale(m);
-  } else {
+    by = code_factors(m);
+    if (tid == 0) scales[0] = by.scale;
+  } else {                                                   // (formed once per group: per element they cost more than the rest)
+    __syncthreads();
+    for (int g = tid; g < a.groups; g += blockDim.x) {
+      const CodeFactors f = code_factors(group_max[g]);
+      group_factors[g] = f;
+      scales[g] = f.scale;
+    }
     __syncthreads();
   }
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     const int col = tid + j * blockDim.x;
     if (col >= a.d) continue;
-    if (a.group != 0) {
-      m = group_max[col >> a.group_shift];
-      if ((col & (a.group - 1)) == 0) scales[col >> a.group_shift] = code_scale(m);
-    }
-    const float2 by = code_factors(code_scale(m));
-    a.codes[row * a.codes_stride + col] = __nv_cvt_float_to_fp8(s[j] * by.x * by.y, __NV_SATFINITE, __NV_E4M3);
+    if (a.group != 0) by = group_factors[col >> a.group_shift];
+    a.codes[row * a.codes_stride + col] = __nv_cvt_float_to_fp8(code_quotient(s[j], by), __NV_SATFINITE, __NV_E4M3);
   }
 }
 
