@@ -32,9 +32,16 @@ struct NormArgs {
   int group_shift;                        // its logarithm
   int shift, pitch;                       // of split rows (SplitRow)
   bool weight_f32;
-  float eps, inv_d;
+  float eps, width, inv_width;            // d and 1 / d
 };
 
+// A row's sum divided by its width: the product with the reciprocal and one step of Newton's iteration, rounded once (the remainder is exact in a fused
+// multiply-add; a division in its place costs registers that the gradients do not have). The product alone has the reciprocal's rounding in every row alike.
+template <typename Args>
+__device__ __forceinline__ float row_mean(const Args& a, float sum) {
+  const float q = sum * a.inv_width;
+  return fabsf(sum) < INFINITY ? fmaf(fmaf(-q, a.width, sum), a.inv_width, q) : q;
+}
 // Largest magnitude as the bits of an fp32: compared as integers a NaN is larger than everything, so it is not lost.
 __device__ __forceinline__ unsigned magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 // The larger magnitude of two values (of either sign), NaN if one is.
@@ -157,7 +164,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) residual_rmsnorm_kernel(const _
     return SPLIT ? x.x + x.y + single * single : x.x + x.y;
   };
   float square = row_sum(squares(), red[0]);
-  float rstd = rsqrtf(square * a.inv_d + a.eps);
+  float rstd = rsqrtf(row_mean(a, square) + a.eps);
   if (__float_as_uint(square) == 0x7f800000u) {              // the same in every thread of the row
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
@@ -166,7 +173,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) residual_rmsnorm_kernel(const _
     }
     single *= kNormRescue;
     square = row_sum(squares(), red[1]);
-    rstd = rsqrtf(square * a.inv_d);
+    rstd = rsqrtf(row_mean(a, square));
   }
   const uint64_t rstd2 = pack2(rstd, rstd);
 #pragma unroll
@@ -267,7 +274,7 @@ __global__ void __launch_bounds__(1024) residual_rmsnorm_plain_kernel(const __gr
     square += s[j] * s[j];
   }
   square = row_sum(square, red[0]);
-  float rstd = rsqrtf(square * a.inv_d + a.eps);
+  float rstd = rsqrtf(row_mean(a, square) + a.eps);
   if (__float_as_uint(square) == 0x7f800000u) {              // the same in every thread of the row
     square = 0.f;
 #pragma unroll
@@ -276,7 +283,7 @@ __global__ void __launch_bounds__(1024) residual_rmsnorm_plain_kernel(const __gr
       square += s[j] * s[j];
     }
     square = row_sum(square, red[1]);
-    rstd = rsqrtf(square * a.inv_d);
+    rstd = rsqrtf(row_mean(a, square));
   }
   unsigned m = 0;
 #pragma unroll
@@ -327,7 +334,7 @@ struct NormGradArgs {
   int T, d;
   int shift, pitch;                                 // of split rows (SplitRow)
   bool weight_f32;
-  float eps, inv_d;
+  float eps, width, inv_width;                      // d and 1 / d
 };
 
 // Every block has every gridDim.x-th row (of ROWS > 1 threadIdx.y each, rows of a warp: 16384 rows of 64 11 instead of 15 us) and keeps its part of
@@ -444,7 +451,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) rmsnorm_grad_kernel(const __gri
     };
     float sums[2], by = 1.f;
     add_up(sums, red[turn]);
-    float rstd = rsqrtf(sums[0] * a.inv_d + a.eps);
+    float rstd = rsqrtf(row_mean(a, sums[0]) + a.eps);
     if (__float_as_uint(sums[0]) == 0x7f800000u) {
       by = kNormRescue;
 #pragma unroll
@@ -455,10 +462,10 @@ __global__ void __launch_bounds__(THREADS, CTAS) rmsnorm_grad_kernel(const __gri
       s1 *= by;
       if constexpr (ROWS == 1) __syncthreads();              // red[2] may still be read for an earlier row
       add_up(sums, red[2]);
-      rstd = rsqrtf(sums[0] * a.inv_d);
+      rstd = rsqrtf(row_mean(a, sums[0]));
     }
     // with unit = s rstd: d s = step (weight d_out) - back unit + d_stream
-    const float step = rstd * by, back = -step * (sums[1] * rstd * a.inv_d);
+    const float step = rstd * by, back = -step * (row_mean(a, sums[1]) * rstd);
     const uint64_t rstd2 = pack2(rstd, rstd), step2 = pack2(step, step), back2 = pack2(back, back);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
@@ -563,13 +570,13 @@ __global__ void __launch_bounds__(1024) rmsnorm_grad_plain_kernel(const __grid_c
     };
     float sums[2], by = 1.f;
     add_up(by, sums);
-    float rstd = rsqrtf(sums[0] * a.inv_d + a.eps);
+    float rstd = rsqrtf(row_mean(a, sums[0]) + a.eps);
     if (__float_as_uint(sums[0]) == 0x7f800000u) {
       by = kNormRescue;
       add_up(by, sums);
-      rstd = rsqrtf(sums[0] * a.inv_d);
+      rstd = rsqrtf(row_mean(a, sums[0]));
     }
-    const float step = rstd * by, back = step * (sums[1] * rstd * a.inv_d);
+    const float step = rstd * by, back = step * (row_mean(a, sums[1]) * rstd);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int col = (tid + j * blockDim.x) * V;

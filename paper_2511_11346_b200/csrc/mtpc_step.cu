@@ -479,7 +479,8 @@ int mtpc_residual_rmsnorm(const void* x, int64_t x_stride, const void* residual,
   while ((1 << a.group_shift) < scale_group) ++a.group_shift;
   a.weight_f32 = weight_dtype == MTPC_F32;
   a.eps = eps;
-  a.inv_d = 1.f / d;
+  a.width = static_cast<float>(d);
+  a.inv_width = 1.f / a.width;
   const bool vectors = d % 8 == 0 && rows_allow(x, x_stride, e, 8, T) && rows_allow(residual, residual_stride, e, 8, T) &&
                        rows_allow(weight, 0, element(weight_dtype), 8, 1) && rows_allow(out_sum, sum_stride, e, 8, T) &&
                        rows_allow(out, out_stride, e, 8, T) && rows_allow(out_codes, codes_stride, 1, 8, T);
@@ -539,7 +540,8 @@ int mtpc_residual_rmsnorm_backward(const void* sum, int64_t sum_stride, int32_t 
     a.d = d;
     a.weight_f32 = weight_dtype == MTPC_F32;
     a.eps = eps;
-    a.inv_d = 1.f / d;
+    a.width = static_cast<float>(d);
+    a.inv_width = 1.f / a.width;
     const bool vectors = d % 8 == 0 && rows_allow(sum, sum_stride, element(io_dtype), 8, T) && rows_allow(weight, 0, element(weight_dtype), 8, 1) &&
                          rows_allow(d_out, d_out_stride, element(d_out_dtype), 8, T) &&
                          rows_allow(d_sum, d_sum_stride, element(d_x_dtype), 8, T) && rows_allow(d_x, d_x_stride, element(d_x_dtype), 8, T);
