@@ -18,7 +18,7 @@ namespace mtpc {
 constexpr int kNormMaxWidth = 32768;     // columns: 1024 threads of 32
 constexpr int kNormMinGroup = 32;        // columns that share a scale: 32, 64 or 128 (or the row)
 constexpr float kE4m3Max = 448.f;
-// Rows whose squares overflow fp32 are formed once more from s times this. What 2^-100 takes below the range is 2^-20 of
+// Rows whose squares (or their mean with eps) overflow fp32 are formed once more from s times this. What 2^-100 takes below the range is 2^-20 of
 // the row's largest value at most.
 constexpr float kNormRescue = 0x1p-100f;
 
@@ -164,8 +164,9 @@ __global__ void __launch_bounds__(THREADS, CTAS) residual_rmsnorm_kernel(const _
     return SPLIT ? x.x + x.y + single * single : x.x + x.y;
   };
   float square = row_sum(squares(), red[0]);
-  float rstd = rsqrtf(row_mean(a, square) + a.eps);
-  if (__float_as_uint(square) == 0x7f800000u) {              // the same in every thread of the row
+  const float mean = row_mean(a, square) + a.eps;
+  float rstd = rsqrtf(mean);
+  if (mean == INFINITY) {                                    // the same in every thread of the row
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
 #pragma unroll
@@ -173,7 +174,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) residual_rmsnorm_kernel(const _
     }
     single *= kNormRescue;
     square = row_sum(squares(), red[1]);
-    rstd = rsqrtf(row_mean(a, square));
+    rstd = rsqrtf(row_mean(a, square) + a.eps * kNormRescue * kNormRescue);
   }
   const uint64_t rstd2 = pack2(rstd, rstd);
 #pragma unroll
@@ -274,8 +275,9 @@ __global__ void __launch_bounds__(1024) residual_rmsnorm_plain_kernel(const __gr
     square += s[j] * s[j];
   }
   square = row_sum(square, red[0]);
-  float rstd = rsqrtf(row_mean(a, square) + a.eps);
-  if (__float_as_uint(square) == 0x7f800000u) {              // the same in every thread of the row
+  const float mean = row_mean(a, square) + a.eps;
+  float rstd = rsqrtf(mean);
+  if (mean == INFINITY) {                                    // the same in every thread of the row
     square = 0.f;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
@@ -283,7 +285,7 @@ __global__ void __launch_bounds__(1024) residual_rmsnorm_plain_kernel(const __gr
       square += s[j] * s[j];
     }
     square = row_sum(square, red[1]);
-    rstd = rsqrtf(row_mean(a, square));
+    rstd = rsqrtf(row_mean(a, square) + a.eps * kNormRescue * kNormRescue);
   }
   unsigned m = 0;
 #pragma unroll
@@ -451,8 +453,9 @@ __global__ void __launch_bounds__(THREADS, CTAS) rmsnorm_grad_kernel(const __gri
     };
     float sums[2], by = 1.f;
     add_up(sums, red[turn]);
-    float rstd = rsqrtf(row_mean(a, sums[0]) + a.eps);
-    if (__float_as_uint(sums[0]) == 0x7f800000u) {
+    const float mean = row_mean(a, sums[0]) + a.eps;
+    float rstd = rsqrtf(mean);
+    if (mean == INFINITY) {
       by = kNormRescue;
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
@@ -462,7 +465,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) rmsnorm_grad_kernel(const __gri
       s1 *= by;
       if constexpr (ROWS == 1) __syncthreads();              // red[2] may still be read for an earlier row
       add_up(sums, red[2]);
-      rstd = rsqrtf(row_mean(a, sums[0]));
+      rstd = rsqrtf(row_mean(a, sums[0]) + a.eps * by * by);
     }
     // with unit = s rstd: d s = step (weight d_out) - back unit + d_stream
     const float step = rstd * by, back = -step * (row_mean(a, sums[1]) * rstd);
@@ -570,11 +573,12 @@ __global__ void __launch_bounds__(1024) rmsnorm_grad_plain_kernel(const __grid_c
     };
     float sums[2], by = 1.f;
     add_up(by, sums);
-    float rstd = rsqrtf(row_mean(a, sums[0]) + a.eps);
-    if (__float_as_uint(sums[0]) == 0x7f800000u) {
+    const float mean = row_mean(a, sums[0]) + a.eps;
+    float rstd = rsqrtf(mean);
+    if (mean == INFINITY) {
       by = kNormRescue;
       add_up(by, sums);
-      rstd = rsqrtf(row_mean(a, sums[0]));
+      rstd = rsqrtf(row_mean(a, sums[0]) + a.eps * by * by);
     }
     const float step = rstd * by, back = step * (row_mean(a, sums[1]) * rstd);
 #pragma unroll
