@@ -18,9 +18,10 @@ namespace mtpc {
 constexpr int kNormMaxWidth = 32768;     // columns: 1024 threads of 32
 constexpr int kNormMinGroup = 32;        // columns that share a scale: 32, 64 or 128 (or the row)
 constexpr float kE4m3Max = 448.f;
-// Rows whose squares (or their mean with eps) overflow fp32 are formed once more from s times this. What 2^-100 takes below the range is 2^-20 of
-// the row's largest value at most.
-constexpr float kNormRescue = 0x1p-100f;
+// Rows whose squares (or their mean with eps) overflow fp32 are formed once more from s times this: 32768 squares of it times fp32's largest value still
+// fit. What it takes below the range leaves an output off by 2^-134 of its weight at most, half the smallest step times rstd: the roots of such
+// rows' means are above 2^56.
+constexpr float kNormRescue = 0x1p-72f;
 
 struct NormArgs {
   const void *x, *residual, *weight;      // residual, weight: may be NULL

@@ -46,3 +46,11 @@ def normal(T, d, *stds):
 @pytest.mark.parametrize("eps", [1e-5, 1e34, 1e36, 1e38, 3e38])
 def test_eps_beside_squares_beyond_the_range(d, eps):
     check(normal(6, d, 1e17, 1e18, 1e19), eps)
+
+
+@pytest.mark.parametrize("d", [64, 520, 4096, 9000])
+def test_small_elements_beside_squares_beyond_the_range(d):
+    """(what the largest element's square does to the rest)"""
+    x = normal(6, d, 1e-6, 1e-12, 1e-18)
+    x[:3, d // 3], x[3:, d // 2] = 1e20, -3e38
+    check(x, 1e-5, backward=False)
