@@ -22,6 +22,10 @@ constexpr float kE4m3Max = 448.f;
 // fit. What it takes below the range leaves an output off by 2^-134 of its weight at most, half the smallest step times rstd: the roots of such
 // rows' means are above 2^56.
 constexpr float kNormRescue = 0x1p-72f;
+// Rows whose mean with eps is below this, whose squares lose digits below the range, from s times 2^60.
+constexpr float kNormLowMean = 0x1p-96f, kNormRaise = 0x1p60f;
+__device__ __forceinline__ bool norm_far(float mean) { return mean == INFINITY || mean < kNormLowMean; }
+__device__ __forceinline__ float norm_factor(float mean) { return mean < kNormLowMean ? kNormRaise : kNormRescue; }
 
 struct NormArgs {
   const void *x, *residual, *weight;      // residual, weight: may be NULL
@@ -167,15 +171,16 @@ __global__ void __launch_bounds__(THREADS, CTAS) residual_rmsnorm_kernel(const _
   float square = row_sum(squares(), red[0]);
   const float mean = row_mean(a, square) + a.eps;
   float rstd = rsqrtf(mean);
-  if (mean == INFINITY) {                                    // the same in every thread of the row
+  if (norm_far(mean)) {                                      // the same in every thread of the row
+    const float by = norm_factor(mean);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[j][i] = mul2(s[j][i], pack2(kNormRescue, kNormRescue));
+      for (int i = 0; i < 4; ++i) s[j][i] = mul2(s[j][i], pack2(by, by));
     }
-    single *= kNormRescue;
+    single *= by;
     square = row_sum(squares(), red[1]);
-    rstd = rsqrtf(row_mean(a, square) + a.eps * kNormRescue * kNormRescue);
+    rstd = rsqrtf(row_mean(a, square) + a.eps * by * by);
   }
   const uint64_t rstd2 = pack2(rstd, rstd);
 #pragma unroll
@@ -278,15 +283,16 @@ __global__ void __launch_bounds__(1024) residual_rmsnorm_plain_kernel(const __gr
   square = row_sum(square, red[0]);
   const float mean = row_mean(a, square) + a.eps;
   float rstd = rsqrtf(mean);
-  if (mean == INFINITY) {                                    // the same in every thread of the row
+  if (norm_far(mean)) {                                      // the same in every thread of the row
+    const float by = norm_factor(mean);
     square = 0.f;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      s[j] *= kNormRescue;
+      s[j] *= by;
       square += s[j] * s[j];
     }
     square = row_sum(square, red[1]);
-    rstd = rsqrtf(row_mean(a, square) + a.eps * kNormRescue * kNormRescue);
+    rstd = rsqrtf(row_mean(a, square) + a.eps * by * by);
   }
   unsigned m = 0;
 #pragma unroll
@@ -456,8 +462,8 @@ __global__ void __launch_bounds__(THREADS, CTAS) rmsnorm_grad_kernel(const __gri
     add_up(sums, red[turn]);
     const float mean = row_mean(a, sums[0]) + a.eps;
     float rstd = rsqrtf(mean);
-    if (mean == INFINITY) {
-      by = kNormRescue;
+    if (norm_far(mean)) {
+      by = norm_factor(mean);
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
 #pragma unroll
@@ -576,8 +582,8 @@ __global__ void __launch_bounds__(1024) rmsnorm_grad_plain_kernel(const __grid_c
     add_up(by, sums);
     const float mean = row_mean(a, sums[0]) + a.eps;
     float rstd = rsqrtf(mean);
-    if (mean == INFINITY) {
-      by = kNormRescue;
+    if (norm_far(mean)) {
+      by = norm_factor(mean);
       add_up(by, sums);
       rstd = rsqrtf(row_mean(a, sums[0]) + a.eps * by * by);
     }

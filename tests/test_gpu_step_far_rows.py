@@ -54,3 +54,9 @@ def test_small_elements_beside_squares_beyond_the_range(d):
     x = normal(6, d, 1e-6, 1e-12, 1e-18)
     x[:3, d // 3], x[3:, d // 2] = 1e20, -3e38
     check(x, 1e-5, backward=False)
+
+
+@pytest.mark.parametrize("d", [64, 520, 4096, 9000])
+@pytest.mark.parametrize("eps", [1e-45, 1e-42, 1e-39, 1e-36, 1e-30])
+def test_squares_below_the_range_beside_as_small_an_eps(d, eps):
+    check(normal(6, d, 1e-17, 1e-20, 1e-22), eps)
