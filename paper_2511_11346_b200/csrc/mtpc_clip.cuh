@@ -203,8 +203,9 @@ __global__ void __launch_bounds__(kClipThreads, 4) gradient_scale_kernel(const C
   if (blockIdx.x == 0 && threadIdx.x == 0) out_norm[0] = static_cast<float>(norm);
   // A norm that is not finite scales nothing: the gradients stay as they are.
   const double ratio = norm > max_norm && norm <= 1.7976931348623157e308 ? max_norm / norm : 1.0;
-  // A ratio near the end of fp32's range is multiplied in two steps, the first a power of two.
-  const float first = ratio < 0x1p-100 ? 0x1p-64f : 1.f, by = static_cast<float>(ratio / first);
+  // A ratio below fp32's normal range is multiplied in two steps, the first a power of two that leaves the least normal number to the second: what the first step
+  // takes below the range is nothing after the second.
+  const float first = ratio < 0x1p-126 ? ldexpf(1.f, max(ilogb(ratio) + 126, -149)) : 1.f, by = static_cast<float>(ratio / first);
   const int block = blockIdx.x;
   clip_walk(chunks, block < count ? (count - block + blocks - 1) / blocks : 0, stage, [&](int i) { return count - 1 - block - i * blocks; },
             [&](const ClipChunk& c) { return c.out == nullptr || (c.out == c.g && ratio == 1.0); },
