@@ -80,6 +80,20 @@ def residual_rmsnorm_backward(total, weight, d_hidden, d_total=None, eps: float 
     return d_x, d_weight
 
 
+def _written_again(what, shapes, device, out):
+    """The dict of an earlier call, if its tensors are what the call writes: adjacent fp32 elements of these shapes (None: absent) on that device."""
+    import torch
+    for key, shape in shapes.items():
+        t = out.get(key)
+        if shape is None and t is None:
+            continue
+        if (not isinstance(t, torch.Tensor) or shape is None or t.shape != shape or t.dtype is not torch.float32 or t.device != device or
+                not t.is_contiguous()):
+            is_now = f"{t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}" if isinstance(t, torch.Tensor) else repr(t)
+            raise B.MtpcError(B.ERR_SHAPE, f"{what}: out[{key!r}] is {is_now} where fp32 {shape} on {device} is written")
+    return out
+
+
 class DeviceHead:
     """Weights of a workload resident in HBM plus a head created on them."""
 
@@ -206,13 +220,13 @@ class DeviceHead:
         h = self.hidden_device() if hidden is None else hidden
         t = torch.from_numpy(self.wl.targets).to(self.device) if targets is None else targets
         T = h.shape[0]
-        f32 = dict(dtype=torch.float32, device=self.device)
+        f32 = dict(dtype=torch.float32, device=h.device)
         shapes = dict(slot_loss=(s.n,), loss=(1,), dh=(T, s.d), dW_emit=(s.n, s.r, s.v, s.d), dW_sum=(s.sum_rows, s.d),
                       dT_static=(max(s.n - 1, 1), s.r, s.r) if s.family == I.HMM else None)
         if out is None:
             out = {k: None if shape is None else torch.empty(shape, **f32) for k, shape in shapes.items()}
-        elif any((out[k] is None) != (shape is None) or (shape is not None and out[k].shape != shape) for k, shape in shapes.items()):
-            raise B.MtpcError(B.ERR_SHAPE, "window_loss_backward: out is of a call with other sizes")
+        else:
+            _written_again("window_loss_backward", shapes, h.device, out)
         self.head.mtpc_window_loss_backward(h, t, num_sequences, sequence_length, gamma, out["slot_loss"], out["loss"],
                                             out["dh"], out["dW_emit"], out["dW_sum"], out["dT_static"])
         if max_norm is not None:
