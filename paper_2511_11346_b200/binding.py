@@ -561,7 +561,8 @@ class GradientList:
             return [t.data_ptr() for t in tensors], [t.numel() for t in tensors], kinds
 
         entries = np.zeros(len(grads), dtype=MtpcGradient)
-        entries["data"], entries["count"], entries["dtype"] = columns(grads)
+        self._addresses, counts, kinds = columns(grads)
+        entries["data"], entries["count"], entries["dtype"] = self._addresses, counts, kinds
         entries["out"], entries["out_dtype"] = entries["data"], entries["dtype"]
         if outs is not grads:
             to = [g if o is None else o for g, o in zip(grads, outs)]
@@ -581,6 +582,10 @@ class GradientList:
             return lib().mtpc_create_gradient_list(raw_entries, len(grads), self.workspace.data_ptr(), need.value, raw, ctypes.byref(handle))
         _call(what, create, self.device, stream)
         self.handle = handle
+
+    def is_of(self, grads) -> bool:
+        """Whether these tensors lie where those lay that the list was made of: it holds their addresses."""
+        return [t.data_ptr() for t in grads] == self._addresses
 
     def mtpc_clip_gradients(self, max_norm: float, out_norm, stream=None) -> None:
         """out_norm [1] fp32: the norm of all gradients; where it is above max_norm (and finite) they are scaled by max_norm / norm."""

@@ -227,13 +227,15 @@ class DeviceHead:
             out = {k: None if shape is None else torch.empty(shape, **f32) for k, shape in shapes.items()}
         else:
             _written_again("window_loss_backward", shapes, h.device, out)
+        grads = [out["dW_emit"], out["dW_sum"]] + ([out["dT_static"]] if s.family == I.HMM and s.n > 1 else [])
+        if max_norm is not None and "gradients" in out and not out["gradients"].is_of(grads):
+            raise B.MtpcError(B.ERR_SHAPE, "window_loss_backward: out['gradients'] is a list of other buffers (without it, a call makes one of these)")
         self.head.mtpc_window_loss_backward(h, t, num_sequences, sequence_length, gamma, out["slot_loss"], out["loss"],
                                             out["dh"], out["dW_emit"], out["dW_sum"], out["dT_static"])
         if max_norm is not None:
             if "gradients" not in out:
                 out["grad_norm"] = torch.empty(1, **f32)
-                out["gradients"] = B.GradientList([out["dW_emit"], out["dW_sum"]] +
-                                                  ([out["dT_static"]] if s.family == I.HMM and s.n > 1 else []))
+                out["gradients"] = B.GradientList(grads)
             out["gradients"].mtpc_clip_gradients(max_norm, out["grad_norm"])
         return out
 
