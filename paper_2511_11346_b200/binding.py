@@ -544,6 +544,7 @@ class GradientList:
         import numpy as np
         what = "mtpc_create_gradient_list"
         self.handle = None
+        self.norm = None                                     # for whoever keeps the norm's buffer with the list
         grads = list(grads)
         outs = grads if outs is None else list(outs)
         if not grads or len(outs) != len(grads):

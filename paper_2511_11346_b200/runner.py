@@ -213,8 +213,9 @@ class DeviceHead:
 
     def window_loss_backward(self, num_sequences, sequence_length, gamma, hidden=None, targets=None, out=None, max_norm=None):
         """-> dict(slot_loss [n], loss [1], dh, dW_emit, dW_sum, dT_static or None) as fp32 device tensors. out: the dict of an earlier call, whose
-        buffers are written again. max_norm: the parameters' gradients together are clipped to that norm, in place, and
-        `grad_norm` [1] is what it was before."""
+        buffers are written again. max_norm: the gradients of the head's parameters together are clipped to that norm, in place, and
+        `grad_norm` [1] is what it was before; `gradients` is the list for that, of these very buffers, made by the first such call (not while a graph is
+        captured). dh is not scaled: what is behind the head gets the gradient of the loss itself (for a norm over a whole model: `GradientList`)."""
         import torch
         s = self.wl.shape
         h = self.hidden_device() if hidden is None else hidden
@@ -232,11 +233,16 @@ class DeviceHead:
             raise B.MtpcError(B.ERR_SHAPE, "window_loss_backward: out['gradients'] is a list of other buffers (without it, a call makes one of these)")
         self.head.mtpc_window_loss_backward(h, t, num_sequences, sequence_length, gamma, out["slot_loss"], out["loss"],
                                             out["dh"], out["dW_emit"], out["dW_sum"], out["dT_static"])
-        if max_norm is not None:
-            if "gradients" not in out:
-                out["grad_norm"] = torch.empty(1, **f32)
-                out["gradients"] = B.GradientList(grads)
-            out["gradients"].mtpc_clip_gradients(max_norm, out["grad_norm"])
+        if max_norm is None:
+            out.pop("grad_norm", None)                       # (an earlier step's)
+            return out
+        if "gradients" not in out:
+            out["gradients"] = B.GradientList(grads)
+        clip = out["gradients"]
+        if "grad_norm" not in out:                           # where the list's calls write it: kept with the list, for graphs that hold them
+            clip.norm = torch.empty(1, **f32) if clip.norm is None else clip.norm
+            out["grad_norm"] = clip.norm
+        clip.mtpc_clip_gradients(max_norm, out["grad_norm"])
         return out
 
     def close(self):

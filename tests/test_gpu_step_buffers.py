@@ -49,3 +49,16 @@ def test_a_buffer_that_is_not_the_lists_is_refused(key):
     out[key] = old.view(old.shape)
     assert call(0.5, out=out, max_norm=1e-3) is out and torch.equal(out[key], want[key]) and torch.equal(out["grad_norm"], want["grad_norm"])
     dh.close()
+
+
+def test_the_norm_of_an_earlier_step_does_not_stay():
+    dh, call = head(I.CP)
+    out = call(max_norm=1e-3)
+    norm = out["grad_norm"]
+    assert norm.item() > 1e-3
+    assert call(0.5, out=out) is out and "grad_norm" not in out
+    want = call(0.5, max_norm=1e-3)
+    plain = call(0.5)
+    assert all(torch.equal(out[k], plain[k]) for k in ("dW_emit", "dW_sum", "dh", "loss"))
+    assert call(0.5, out=out, max_norm=1e-3)["grad_norm"] is norm and torch.equal(norm, want["grad_norm"])       # (a graph that writes it still does)
+    dh.close()
