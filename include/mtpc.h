@@ -488,7 +488,8 @@ int mtpc_embed_backward(const int32_t* tokens, int32_t T, const void* d_out, int
  *   s = x + residual,   out = s * (mean over the row of s^2 + eps)^(-1/2) * weight
  * s is fp32 throughout: out is formed from the sum before it is rounded to out_sum.
  *   x, residual, out_sum, out dev [T, d] io_dtype. residual may be NULL (s = x), so may out_sum (s is not wanted). out_sum and out may
- *           each be the buffer of x or of residual, with its stride; overlaps otherwise are not allowed.
+ *           each be the buffer of x or of residual, with its stride, but not both the same one (MTPC_ERR_SHAPE); overlaps otherwise are
+ *           not allowed.
  *   weight  dev [d] weight_dtype, or NULL (ones).   eps > 0.
  *   out_codes, out_scales: the output in 8 bits, both NULL if it is not wanted; out may be NULL if it is. out_codes dev [T, d] e4m3
  *           bytes, out_scales dev [T, ceil(d / scale_group)] fp32, adjacent rows: one scale per scale_group columns (32, 64, 128; the last group

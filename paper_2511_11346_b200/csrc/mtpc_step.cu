@@ -458,6 +458,7 @@ int mtpc_residual_rmsnorm(const void* x, int64_t x_stride, const void* residual,
     return MTPC_ERR_SHAPE;
   int rc = check_device();
   if (rc != MTPC_OK) return rc;
+  if (out && out == out_sum) return MTPC_ERR_SHAPE;          // one would be written over the other
   NormArgs a;
   memset(&a, 0, sizeof(a));
   a.x = x;
