@@ -347,11 +347,11 @@ struct NormGradArgs {
 };
 
 // Every block has every gridDim.x-th row (of ROWS > 1 threadIdx.y each, rows of a warp: 16384 rows of 64 11 instead of 15 us) and keeps its part of
-// d weight in registers, NV vectors of eight elements a thread; its vectors of the next AHEAD rows are on their way to registers. What bounds it is what the
+// d weight in registers, NV vectors of eight elements a thread; its vectors of the next row are on their way to registers. What bounds it is what the
 // SM issues for a row beside its bytes, so the arithmetic goes by packed pairs: 8192 rows of 4096 (bf16, d_out fp32) one by one 88 to 104 us, with rows
 // fetched by cp.async through shared memory, where issuing the copies took 1000 of 3500 cycles a row, 65 to 78. SPLIT: rows that start off their
 // vectors, at the same columns in all rows of a block.
-template <typename IO, typename DY, typename DX, int NV, int AHEAD, int THREADS, int CTAS, bool SPLIT, int ROWS>
+template <typename IO, typename DY, typename DX, int NV, int THREADS, int CTAS, bool SPLIT, int ROWS>
 __global__ void __launch_bounds__(THREADS, CTAS) rmsnorm_grad_kernel(const __grid_constant__ NormGradArgs a) {
   __shared__ float red[3][32];
   const int tid = threadIdx.x, threads = blockDim.x;
@@ -371,7 +371,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) rmsnorm_grad_kernel(const __gri
     Raw<IO, 1> s1;                                           // the single column's
     Raw<DY, 1> dy1;
     Raw<DX, 1> stream1;
-  } ahead[AHEAD];
+  } ahead;
   const IO* next_s = static_cast<const IO*>(a.sum) + first_row * a.sum_stride;          // the row to be fetched next
   const DY* next_dy = static_cast<const DY*>(a.d_out) + first_row * a.d_out_stride;
   const DX* next_stream = static_cast<const DX*>(a.d_stream) + first_row * a.d_stream_stride;
@@ -398,18 +398,15 @@ __global__ void __launch_bounds__(THREADS, CTAS) rmsnorm_grad_kernel(const __gri
     }
   };
 #pragma unroll
-  for (int q = 0; q < AHEAD; ++q) {
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {             // (what lies past the row's end stays zero, and so does d_stream if there is none)
-      ahead[q].s[j].clear();
-      ahead[q].dy[j].clear();
-      ahead[q].stream[j].clear();
-    }
-    ahead[q].s1.clear();
-    ahead[q].dy1.clear();
-    ahead[q].stream1.clear();
-    fetch(ahead[q]);
+  for (int j = 0; j < NV; ++j) {               // (what lies past the row's end stays zero, and so does d_stream if there is none)
+    ahead.s[j].clear();
+    ahead.dy[j].clear();
+    ahead.stream[j].clear();
   }
+  ahead.s1.clear();
+  ahead.dy1.clear();
+  ahead.stream1.clear();
+  fetch(ahead);
   uint64_t w[NV][4], dw[NV][4];
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
@@ -428,21 +425,21 @@ __global__ void __launch_bounds__(THREADS, CTAS) rmsnorm_grad_kernel(const __gri
   float dw1 = 0.f;
   int turn = 0;
   DX* out = static_cast<DX*>(a.d_x) + first_row * a.d_x_stride;
-  auto work = [&](Row& mine) {
+  for (int row = first_row; row < a.T; row += row_step) {
     uint64_t s[NV][4], dy[NV][4];
     Raw<DX, 8> stream[NV];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        s[j][i] = mine.s[j].pair(i);
-        dy[j][i] = mine.dy[j].pair(i);
+        s[j][i] = ahead.s[j].pair(i);
+        dy[j][i] = ahead.dy[j].pair(i);
       }
-      stream[j] = mine.stream[j];
+      stream[j] = ahead.stream[j];
     }
-    float s1 = mine.s1.value(0);
-    const float dy1 = mine.dy1.value(0), stream1 = mine.stream1.value(0);
-    fetch(mine);
+    float s1 = ahead.s1.value(0);
+    const float dy1 = ahead.dy1.value(0), stream1 = ahead.stream1.value(0);
+    fetch(ahead);
     auto add_up = [&](float (&sums)[2], float* share) {        // s^2 and weight d_out s
       uint64_t squares = 0, products = 0;
 #pragma unroll
@@ -495,11 +492,6 @@ __global__ void __launch_bounds__(THREADS, CTAS) rmsnorm_grad_kernel(const __gri
     }
     out += row_step * a.d_x_stride;
     turn ^= 1;
-  };
-  for (int row = first_row; row < a.T; row += AHEAD * row_step) {
-#pragma unroll
-    for (int q = 0; q < AHEAD; ++q)
-      if (row + q * row_step < a.T) work(ahead[q]);
   }
   if (a.partial) {
     float* part = a.partial + static_cast<size_t>(blockIdx.x) * a.d;

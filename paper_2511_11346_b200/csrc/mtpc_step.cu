@@ -113,16 +113,16 @@ int launch_rmsnorm_grad_vectors(const NormGradArgs& a, cudaStream_t st) {
   int blocks = packs <= 32 ? std::min(ceil_div(a.T, kGradRows), 2 * kSms) : norm_grad_blocks(a.T, a.d, nv);
   if (SPLIT && packs > 32 && blocks < a.T) blocks = std::max(8, blocks / 8 * 8);        // a block's rows start alike
   if (packs <= 32)
-    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 1, 1, 256, 2, SPLIT, kGradRows>, blocks, dim3(32, kGradRows), 0, st, true, a);
+    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 1, 256, 2, SPLIT, kGradRows>, blocks, dim3(32, kGradRows), 0, st, true, a);
   else if (threads <= 256 && nv == 1)
-    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 1, 1, 256, 2, SPLIT, 1>, blocks, threads, 0, st, true, a);
+    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 1, 256, 2, SPLIT, 1>, blocks, threads, 0, st, true, a);
   else if (nv == 1)
-    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 1, 1, 512, 1, SPLIT, 1>, blocks, threads, 0, st, true, a);
+    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 1, 512, 1, SPLIT, 1>, blocks, threads, 0, st, true, a);
   else if constexpr (kNarrow) {
-    if (threads <= 256) launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 2, 1, 256, 2, SPLIT, 1>, blocks, threads, 0, st, true, a);
-    else launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 2, 1, 512, 1, SPLIT, 1>, blocks, threads, 0, st, true, a);
+    if (threads <= 256) launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 2, 256, 2, SPLIT, 1>, blocks, threads, 0, st, true, a);
+    else launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 2, 512, 1, SPLIT, 1>, blocks, threads, 0, st, true, a);
   } else
-    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 2, 1, 512, 1, SPLIT, 1>, blocks, threads, 0, st, true, a);
+    launch_kernel(rmsnorm_grad_kernel<IO, DY, DX, 2, 512, 1, SPLIT, 1>, blocks, threads, 0, st, true, a);
   return blocks;
 }
 template <typename IO, typename DY, typename DX>
