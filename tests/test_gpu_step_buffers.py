@@ -62,3 +62,31 @@ def test_the_norm_of_an_earlier_step_does_not_stay():
     assert all(torch.equal(out[k], plain[k]) for k in ("dW_emit", "dW_sum", "dh", "loss"))
     assert call(0.5, out=out, max_norm=1e-3)["grad_norm"] is norm and torch.equal(norm, want["grad_norm"])       # (a graph that writes it still does)
     dh.close()
+
+
+def test_a_captured_step_with_clipping():
+    """The list is made by an eager step; a graph of the next one serves every step after it, whatever eager steps do to the dict in between."""
+    dh, _ = head()
+    g = torch.Generator(device="cuda").manual_seed(1)
+    hidden, targets = torch.randn(N * L, 64, device="cuda", generator=g).bfloat16(), torch.randint(0, 64, (N * L, 4), device="cuda", generator=g, dtype=torch.int32)
+    hidden = hidden.to(dh.hidden_device().dtype)
+    call = lambda **kw: dh.window_loss_backward(N, L, 0.9, hidden=hidden, targets=targets, **kw)  # noqa: E731
+    out = call(max_norm=1e-3)
+    norm = out["grad_norm"]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(out=out, max_norm=1e-3)
+    call(out=out)
+    spare = [torch.full((1,), 5.0, device="cuda") for _ in range(64)]      # where a buffer that was let go would lie
+    for turn in range(3):
+        hidden.copy_(torch.randn(N * L, 64, device="cuda", generator=g))
+        for k in ("dW_emit", "dW_sum", "dT_static", "dh"):
+            out[k].fill_(7.0)
+        norm.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = {k: t.clone() for k, t in out.items() if isinstance(t, torch.Tensor)}
+        want = call(max_norm=1e-3)
+        assert all(torch.equal(got[k], want[k]) for k in got) and torch.equal(norm, want["grad_norm"]) and norm.item() > 1e-3
+    assert all(s.item() == 5.0 for s in spare)
+    dh.close()
