@@ -494,9 +494,9 @@ int mtpc_embed_backward(const int32_t* tokens, int32_t T, const void* d_out, int
  *   out_codes, out_scales: the output in 8 bits, both NULL if it is not wanted; out may be NULL if it is. out_codes dev [T, d] e4m3
  *           bytes, out_scales dev [T, ceil(d / scale_group)] fp32, adjacent rows: one scale per scale_group columns (32, 64, 128; the last group
  *           may be short) or per row (scale_group = 0). scale = the group's largest |out| / 448 (1 if that is 0), code = out / scale
- *           rounded to nearest (ties to even, out not rounded before); code * scale stands for out. A group that holds a NaN or an infinity
- *           has a scale that is none either.
- * 1 <= d <= 32768 (MTPC_ERR_UNSUPPORTED beyond), 0 <= T <= 2^30. A row's squares may exceed fp32's range.
+ *           rounded to nearest (ties to even; out is not rounded before, either quotient is to fp32); code * scale stands for out. A
+ *           group that holds a NaN or an infinity has a scale that is not finite either.
+ * 1 <= d <= 32768 (MTPC_ERR_UNSUPPORTED beyond), 0 <= T <= 2^30. A row's squares may leave fp32's range on either side.
  */
 int mtpc_residual_rmsnorm(const void* x, int64_t x_stride, const void* residual, int64_t residual_stride, const void* weight,
                           int32_t weight_dtype, int32_t T, int32_t d, int32_t io_dtype, float eps, void* out_sum, int64_t sum_stride,
@@ -512,6 +512,8 @@ int mtpc_residual_rmsnorm(const void* x, int64_t x_stride, const void* residual,
  *   d_x    dev [T, d] d_x_dtype: the gradient of s, which is that of x and that of residual; may be the buffer of d_sum, or of d_out or sum
  *          where the types are the same, with its stride.
  *   d_weight dev [d] fp32, overwritten, or NULL.
+ * A row's squares may leave fp32's range here too, its sum of weight * d_out * s may not (in a row whose squares fit, that takes a weight * d_out
+ * of 2^64).
  *   workspace dev, 256-byte aligned, >= mtpc_residual_rmsnorm_backward_workspace_bytes(T, d): parts of d_weight; not needed without it.
  */
 int mtpc_residual_rmsnorm_backward_workspace_bytes(int32_t T, int32_t d, size_t* out_bytes);
@@ -531,7 +533,7 @@ int mtpc_residual_rmsnorm_backward(const void* sum, int64_t sum_stride, int32_t 
  *            call on this list, and must outlive it. Creation writes the list's chunks there and waits for `stream` (not for capture);
  *            the entries themselves are not needed afterwards.
  * mtpc_clip_gradients: max_norm > 0, or infinity (the norm alone; results in other buffers are then copies). out_norm dev [1] fp32: the norm
- * before clipping (infinity if fp32 cannot hold it). Squares and sums are fp64. With a norm that is not finite (an infinity or NaN among
+ * before clipping (infinity if fp32 cannot hold it, scaled by all the same). Squares and sums are fp64. With a norm that is not finite (an infinity or NaN among
  * the gradients) nothing is scaled: out_norm tells, and the caller leaves the step out. As a head, a list must not be used from two streams at once.
  */
 typedef struct {

@@ -6,8 +6,8 @@
 // of them with a few tokens, so neither a row per block nor atomics suit it. The positions are sorted by token (stable, so the order of every sum
 // is fixed), cut into chunks of equal length, and a chunk's positions are added up row after row: each element of d_out is read once, whatever the
 // tokens are. A token whose positions lie within a chunk is written at once; of one that crosses chunks every chunk leaves its part, which are added up
-// in their order afterwards. (By the block that is there last, found by a counter, they are not: with the fences that takes the sums of 8192 x 4096 fp32
-// took 57 us, instead of 26 and 5 for a kernel of its own.)
+// in their order afterwards, by a kernel of its own. (Left to whichever block comes last, found by a counter, the sums of 8192 x 4096 fp32 took 57 us, fences
+// included, instead of 26 and 5 for the join.)
 //   embed_order_kernel    up to kOrderMaxT positions (or half as many): every block owns a range of tokens, finds their positions among
 //                         all of them and sorts those;
 //                         meanwhile the device asks for d_out by L2 prefetch

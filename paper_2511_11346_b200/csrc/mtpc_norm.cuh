@@ -3,8 +3,10 @@
 //   d s = rstd (weight d_out - s rstd^2 mean(weight d_out s)) + d_stream,   d weight = sum over the rows of d_out s rstd
 // (d s is the gradient of x and of residual alike.) Everything between the loads and the one rounding of each output is fp32.
 //
-// Both are streams: a row is read once, into registers, and everything is formed from there. A row is a warp's up to 64 vectors of eight
-// elements, beyond that a block's with two vectors a thread.
+// Both are streams: a row is read once, into registers, and everything is formed from there. Forward, a row is a warp's up to 64 vectors of eight elements (one or
+// two a lane), beyond that a block's with two vectors a thread, from 8192 columns on four. Gradient: a warp's up to 32 vectors, beyond that a block's with one
+// or two vectors a thread, by what a row ahead leaves of the registers. Rows that no vectors fit go element by element; the gradient
+// reads those, and rows of more than 8192 columns, twice, the second time from L1 or L2.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp8.h>

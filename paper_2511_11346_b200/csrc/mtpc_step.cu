@@ -74,7 +74,7 @@ enum RowPath { kRowVectors, kRowSplit, kRowElements };
 template <typename IO, bool SPLIT>
 void launch_rmsnorm_vectors(const NormArgs& a, cudaStream_t st) {
   const int packs = ceil_div(a.d, 8);
-  // Blocks of 256 threads on an SM: bf16 six instead of five (2005 rows of 4096 to 8 bits 15.4 for 16.3 us), where fp32 would spill (8192 rows 85 for 82).
+  // Blocks of 256 threads on an SM: bf16 six instead of five (2005 rows of 4096 to 8 bits 14.1 for 14.4 us), where fp32 would spill (8192 rows 87 for 80).
   constexpr int kCtas = sizeof(IO) == 2 && !SPLIT ? 6 : 4;
   if (packs <= 32)
     launch_kernel(residual_rmsnorm_kernel<IO, 1, 256, 6, SPLIT>, ceil_div(a.T, 8), dim3(32, 8), 0, st, true, a);
