@@ -258,7 +258,6 @@ template <typename IO, int NV>
 __global__ void __launch_bounds__(1024) residual_rmsnorm_plain_kernel(const __grid_constant__ NormArgs a) {
   __shared__ float red[2][32];
   __shared__ unsigned group_max[kNormMaxWidth / kNormMinGroup];
-  __shared__ CodeFactors group_factors[kNormMaxWidth / kNormMinGroup];
   const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 31;
   if (a.codes != nullptr && a.group != 0) {
     for (int g = tid; g < a.groups; g += blockDim.x) group_max[g] = 0;
@@ -319,20 +318,17 @@ __global__ void __launch_bounds__(1024) residual_rmsnorm_plain_kernel(const __gr
     m = row_max(m, reinterpret_cast<unsigned*>(red[1]));
     by = code_factors(m);
     if (tid == 0) scales[0] = by.scale;
-  } else {                                                   // (formed once per group: per element they cost more than the rest)
-    __syncthreads();
-    for (int g = tid; g < a.groups; g += blockDim.x) {
-      const CodeFactors f = code_factors(group_max[g]);
-      group_factors[g] = f;
-      scales[g] = f.scale;
-    }
+  } else {
     __syncthreads();
   }
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     const int col = tid + j * blockDim.x;
     if (col >= a.d) continue;
-    if (a.group != 0) by = group_factors[col >> a.group_shift];
+    if (a.group != 0) {
+      by = code_factors(group_max[col >> a.group_shift]);
+      if ((col & (a.group - 1)) == 0) scales[col >> a.group_shift] = by.scale;
+    }
     a.codes[row * a.codes_stride + col] = __nv_cvt_float_to_fp8(code_quotient(s[j], by), __NV_SATFINITE, __NV_E4M3);
   }
 }
