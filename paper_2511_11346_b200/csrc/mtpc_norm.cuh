@@ -70,7 +70,7 @@ __device__ __forceinline__ float reciprocal_near(float x) {
 // 24 digits move codes that lie near the middle of two; eight divisions beside a vector's loads take longer than the row's bytes.)
 // Magnitudes far from one take the division for the scale, below whose digits a remainder may fall, and go to the middle of the range first, by
 // a power of two, where no digit of lo is lost. A scale that is not finite has hi = 0: what is finite gives 0.
-struct alignas(16) CodeFactors {
+struct CodeFactors {
   float scale, first, hi, lo;
 };
 __device__ __forceinline__ CodeFactors code_factors(unsigned bits) {
