@@ -69,7 +69,8 @@ enum {
   MTPC_STATUS_BAD_UNIFORM = 2u, /* a uniform outside [0,1) was seen; that draw returned -1 and the log-prob
                                    (or the prefix log-marginals from that byte on) of its window is NaN */
   MTPC_STATUS_TIMEOUT = 4u,     /* a bounded barrier wait expired; the outputs of that call are invalid */
-  MTPC_STATUS_BAD_TOKEN = 8u    /* the embedding calls: a token >= v was seen; its row is NaN, it has no gradient */
+  MTPC_STATUS_BAD_TOKEN = 8u,   /* the embedding calls: a token >= v was seen; its row is NaN, it has no gradient */
+  MTPC_STATUS_BAD_OFFSET = 16u  /* the losses of sequences: offsets that decrease or leave [0, T] were seen; the loss is NaN */
 };
 
 typedef struct {
@@ -548,6 +549,52 @@ int mtpc_create_gradient_list(const mtpc_gradient* entries, int32_t count, void*
                               mtpc_gradient_list** out);
 int mtpc_clip_gradients(mtpc_gradient_list* list, float max_norm, float* out_norm, void* stream);
 int mtpc_destroy_gradient_list(mtpc_gradient_list* list);
+
+/*
+ * Dropout: out = residual + x * scale where an element is kept, residual alone (or zero) where it is dropped. The gradient with respect to x is the same
+ * call on the gradient of out, without residual: it draws the same mask again, which is nowhere stored.
+ *   An element e = row * d + column (whatever the strides) is kept if part e % 8 of Philox4x32-10 of the counter (e / 8, step) under the key `seed` is
+ *   at least p in steps of 2^-16 (rounded to nearest, at most 65535 of them); parts are 16 bits, the lower half of a word first. scale = 1 / (1 - that p).
+ *   x    dev [T, d] x_dtype;  residual dev [T, d] out_dtype or NULL;  out dev [T, d] out_dtype: may be the buffer of x (of the same type) or of
+ *        residual, with its stride.
+ *   rng  dev int64 [2]: seed and step, read when the work runs, so that a replayed graph draws anew once the caller has counted the step up in between;
+ *        it has to hold the same values in the gradient's call. offset is added to the step: another one for every call of a step that must not share
+ *        its mask (a layer's number, with steps further apart than there are layers).
+ * 0 <= p < 1, 0 <= T <= 2^30, 1 <= d <= 2^30, T * d <= 2^40 (MTPC_ERR_UNSUPPORTED beyond).
+ */
+int mtpc_dropout(const void* x, int64_t x_stride, int32_t x_dtype, const void* residual, int64_t residual_stride, int32_t T, int32_t d,
+                 float p, const int64_t* rng, int64_t offset, void* out, int64_t out_stride, int32_t out_dtype, void* stream);
+
+/*
+ * Losses of log-likelihoods (of windows: mtpc_window_logprob) over packed sequences, and their gradients in logp: what
+ * mtpc_window_logprob_backward takes as `weight`. Sequence s has the positions offsets[s] .. offsets[s + 1] - 1.
+ *   logp, old_logp, ref_logp dev [T] fp32;  d_logp dev [T] fp32, overwritten at the positions of sequences (0 where the mask is 0) and left as it
+ *           was outside of them; not overlapping an input.
+ *   offsets dev int32 [S + 1], not decreasing, within [0, T]; otherwise MTPC_STATUS_BAD_OFFSET is or-ed into out_status (dev uint32 or NULL), the loss is NaN,
+ *           and what d_logp holds is not defined. A sequence may be empty.
+ *   mask    dev [T] bytes or NULL: positions with 0 count nowhere, whatever their values are (infinities and NaN too).
+ *   workspace dev, 256-byte aligned, >= mtpc_objective_workspace_bytes(T, S).
+ * 0 <= T <= 2^30, 1 <= S <= 2^20 (MTPC_ERR_UNSUPPORTED beyond). Differences of log-likelihoods and sums are fp64.
+ *
+ * mtpc_policy_loss: the average over the valid positions (by_sequence != 0: over every sequence's valid positions and then over the S sequences, those
+ * without any among them with 0) of -min(r a, clip(r, 1 - clip_low, 1 + clip_high) a) + beta (exp(q) - q - 1), r = exp(logp - old_logp),
+ * q = ref_logp - logp, a = advantage[s], or advantage[t] if advantage_by_position != 0. The gradient is that of r a where that is the smaller one or both are
+ * equal, zero in it where the clipped one is smaller. ref_logp is not read (and may be NULL) if beta is 0.
+ *   out_loss dev [1]; out_stats dev [3] or NULL: the averages of the first term, of exp(q) - q - 1 (0 if beta is 0) and of the clipped positions.
+ *   clip_low, clip_high, beta >= 0 and finite.
+ *
+ * mtpc_preference_loss: sequences 2p (preferred) and 2p + 1 are a pair, S even. h = beta (sum of logp - ref_logp over the one's valid positions - over
+ * the other's); the loss is the mean over the pairs of -(1 - smoothing) log sigmoid(h) - smoothing log sigmoid(-h).
+ *   out_loss dev [1]; out_h dev [S / 2] or NULL.  beta >= 0 and finite, 0 <= smoothing <= 1.
+ */
+int mtpc_objective_workspace_bytes(int32_t T, int32_t S, size_t* out_bytes);
+int mtpc_policy_loss(const float* logp, const float* old_logp, const float* ref_logp, const float* advantage, int32_t advantage_by_position,
+                     const uint8_t* mask, const int32_t* offsets, int32_t T, int32_t S, float clip_low, float clip_high, float beta,
+                     int32_t by_sequence, float* out_loss, float* out_stats, float* d_logp, void* workspace, size_t workspace_bytes,
+                     uint32_t* out_status, void* stream);
+int mtpc_preference_loss(const float* logp, const float* ref_logp, const uint8_t* mask, const int32_t* offsets, int32_t T, int32_t S, float beta,
+                         float smoothing, float* out_loss, float* out_h, float* d_logp, void* workspace, size_t workspace_bytes,
+                         uint32_t* out_status, void* stream);
 
 /* Frees the host-side object (the workspace and the weights stay the caller's). Synchronises nothing. */
 int mtpc_destroy(mtpc_head* head);

@@ -17,7 +17,7 @@ MTPC_F32, MTPC_BF16 = 0, 1
 MTPC_FLAG_HMM_CONTEXTUAL = 1
 MTPC_FLAG_SHORT_DRAFTS = 4
 MTPC_OK = 0
-STATUS_BAD_TARGET, STATUS_BAD_UNIFORM, STATUS_TIMEOUT, STATUS_BAD_TOKEN = 1, 2, 4, 8
+STATUS_BAD_TARGET, STATUS_BAD_UNIFORM, STATUS_TIMEOUT, STATUS_BAD_TOKEN, STATUS_BAD_OFFSET = 1, 2, 4, 8, 16
 
 EXPORTS = [
     "mtpc_workspace_bytes", "mtpc_create_head", "mtpc_window_logprob", "mtpc_draft_sample",
@@ -31,6 +31,7 @@ EXPORTS = [
     "mtpc_lowrank_window_loss_backward", "mtpc_embed", "mtpc_embed_backward", "mtpc_embed_backward_workspace_bytes",
     "mtpc_residual_rmsnorm", "mtpc_residual_rmsnorm_backward", "mtpc_residual_rmsnorm_backward_workspace_bytes",
     "mtpc_gradient_list_workspace_bytes", "mtpc_create_gradient_list", "mtpc_clip_gradients", "mtpc_destroy_gradient_list",
+    "mtpc_dropout", "mtpc_objective_workspace_bytes", "mtpc_policy_loss", "mtpc_preference_loss",
 ]
 STATIC_SCRATCH_BYTES = 16 << 20
 ERR_STATIC_SCRATCH = -7
@@ -111,6 +112,10 @@ def lib() -> ctypes.CDLL:
     L.mtpc_create_gradient_list.argtypes = [vp, i32, vp, sz, vp, ctypes.POINTER(vp)]
     L.mtpc_clip_gradients.argtypes = [vp, f32, vp, vp]
     L.mtpc_destroy_gradient_list.argtypes = [vp]
+    L.mtpc_dropout.argtypes = [vp, i64, i32, vp, i64, i32, i32, f32, vp, i64, vp, i64, i32, vp]
+    L.mtpc_objective_workspace_bytes.argtypes = [i32, i32, ctypes.POINTER(sz)]
+    L.mtpc_policy_loss.argtypes = [vp, vp, vp, vp, i32, vp, vp, i32, i32, f32, f32, f32, i32, vp, vp, vp, vp, sz, vp, vp]
+    L.mtpc_preference_loss.argtypes = [vp, vp, vp, vp, i32, i32, f32, f32, vp, vp, vp, vp, sz, vp, vp]
     L.mtpc_status_string.argtypes = [ctypes.c_int]
     L.mtpc_status_string.restype = ctypes.c_char_p
     for name in EXPORTS:
@@ -376,10 +381,11 @@ _dtype_codes = None
 
 def _dtypes() -> dict:
     """What the calls look up in torch, once (an import statement in every call costs a tenth of a small one)."""
-    global _dtype_codes, _current_device, _raw_stream, _int32, _float32
+    global _dtype_codes, _current_device, _raw_stream, _int32, _int64, _float32, _bool, _uint8
     if _dtype_codes is None:
         import torch
         _current_device, _int32, _float32 = torch._C._cuda_getDevice, torch.int32, torch.float32
+        _int64, _bool, _uint8 = torch.int64, torch.bool, torch.uint8
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
         _dtype_codes = {torch.float32: MTPC_F32, torch.bfloat16: MTPC_BF16}
     return _dtype_codes
@@ -532,6 +538,64 @@ def mtpc_residual_rmsnorm_backward(sum, weight, eps: float, d_out, d_sum, d_x, d
           _vector(what, weight, d, dev), MTPC_F32 if weight is None else _dtype(what, weight), T, d, eps, d_out.data_ptr(),
           _rows(what, d_out, T, d, dev), _dtype(what, d_out), _ptr(d_sum), 0 if d_sum is None else _rows(what, d_sum, T, d, dev, d_x.dtype),
           d_x.data_ptr(), _rows(what, d_x, T, d, dev), _dtype(what, d_x), _vector(what, d_weight, d, dev, _float32), ws_ptr, ws_bytes)
+
+
+def mtpc_dropout(x, out, p: float, rng, offset: int = 0, residual=None, stream=None) -> None:
+    """out = residual + x / (1 - p) where an element is kept, residual (None: 0) where it is dropped (include/mtpc.h). x, out [T, d] fp32 or bf16, residual of
+    out's dtype; rng int64 [2] on the device: seed and step. On the gradient of out, without residual, the same call gives the gradient of x."""
+    _dtypes()
+    what = "mtpc_dropout"
+    T, d, stride, dev = _matrix(what, x)
+    if rng.dtype is not _int64:
+        _refuse(what, f"{rng.dtype} where {_int64} is needed", ERR_UNSUPPORTED)
+    _call(what, lib().mtpc_dropout, dev, stream, x.data_ptr(), stride, _dtype(what, x), _ptr(residual),
+          0 if residual is None else _rows(what, residual, T, d, dev, out.dtype), T, d, p, _vector(what, rng, 2, dev), offset, out.data_ptr(),
+          _rows(what, out, T, d, dev), _dtype(what, out))
+
+
+def mtpc_objective_workspace_bytes(T: int, S: int) -> int:
+    return _scratch_bytes("mtpc_objective_workspace_bytes", T, S)
+
+
+def _positions(what: str, logp, offsets, mask):
+    """(T, S, device, address of the mask) of packed sequences."""
+    T, S, dev = logp.numel(), offsets.numel() - 1, logp.get_device()
+    if dev < 0:
+        _refuse(what, f"logp on {logp.device}")
+    if mask is None:
+        return T, S, dev, 0
+    if mask.dtype is not _bool and mask.dtype is not _uint8:
+        _refuse(what, f"a mask of {mask.dtype}", ERR_UNSUPPORTED)
+    return T, S, dev, _vector(what, mask, T, dev)
+
+
+def mtpc_policy_loss(logp, old_logp, ref_logp, advantage, offsets, clip_low: float, clip_high: float, beta: float, out_loss, d_logp, mask=None,
+                     by_sequence: bool = False, by_position: bool = False, out_stats=None, workspace=None, out_status=None, stream=None) -> None:
+    """The clipped policy loss with a KL term and its gradient in logp (include/mtpc.h). logp, old_logp, ref_logp (None with beta 0) and d_logp [T] fp32,
+    offsets [S + 1] int32, advantage [S] fp32 (by_position: [T]), mask [T] bool or uint8 or None, out_loss [1], out_stats [3] or None."""
+    _dtypes()
+    what = "mtpc_policy_loss"
+    T, S, dev, mask_at = _positions(what, logp, offsets, mask)
+    ws = _scratch(what, workspace, _scratch_bytes("mtpc_objective_workspace_bytes", T, S), dev, stream)
+    _call(what, lib().mtpc_policy_loss, dev, stream, _vector(what, logp, T, dev, _float32), _vector(what, old_logp, T, dev, _float32),
+          _vector(what, ref_logp, T, dev, _float32), _vector(what, advantage, T if by_position else S, dev, _float32), 1 if by_position else 0, mask_at,
+          _vector(what, offsets, S + 1, dev, _int32), T, S, clip_low, clip_high, beta, 1 if by_sequence else 0, _vector(what, out_loss, 1, dev, _float32),
+          _vector(what, out_stats, 3, dev, _float32), _vector(what, d_logp, T, dev, _float32), ws.data_ptr(), ws.numel(),
+          _vector(what, out_status, 1, dev, _int32))
+
+
+def mtpc_preference_loss(logp, ref_logp, offsets, beta: float, out_loss, d_logp, mask=None, smoothing: float = 0.0, out_h=None, workspace=None,
+                         out_status=None, stream=None) -> None:
+    """The loss of pairs of sequences (2p preferred to 2p + 1) and its gradient in logp (include/mtpc.h). Arguments as for mtpc_policy_loss;
+    out_h [S / 2] fp32 or None."""
+    _dtypes()
+    what = "mtpc_preference_loss"
+    T, S, dev, mask_at = _positions(what, logp, offsets, mask)
+    ws = _scratch(what, workspace, _scratch_bytes("mtpc_objective_workspace_bytes", T, S), dev, stream)
+    _call(what, lib().mtpc_preference_loss, dev, stream, _vector(what, logp, T, dev, _float32), _vector(what, ref_logp, T, dev, _float32), mask_at,
+          _vector(what, offsets, S + 1, dev, _int32), T, S, beta, smoothing, _vector(what, out_loss, 1, dev, _float32),
+          _vector(what, out_h, S // 2, dev, _float32), _vector(what, d_logp, T, dev, _float32), ws.data_ptr(), ws.numel(),
+          _vector(what, out_status, 1, dev, _int32))
 
 
 class GradientList:

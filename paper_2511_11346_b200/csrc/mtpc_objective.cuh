@@ -1,0 +1,400 @@
+// Losses of log-likelihoods in packed sequences, and their gradients.
+//
+// Policy: per valid position t of sequence s, ratio r = exp(logp - old), advantage a of the sequence:
+//   value = -min(r a, clip(r, 1 - low, 1 + high) a) + beta (e^q - 1 - q),   q = ref - logp
+//   slope = -(r a, or 0 where the clipped one is smaller) + beta (1 - e^q)
+// weighted by 1 / (all valid positions), or by 1 / (S * the sequence's valid positions).
+// Preference: sequences 2p and 2p + 1, h = beta (sum of logp - ref over the one's valid positions - over the other's),
+//   loss = mean of -(1 - s) log sigmoid(h) - s log sigmoid(-h),   slope = +- beta (s - sigmoid(-h)) / pairs.
+//
+// Differences of log-likelihoods are formed in fp64, where none is lost, and rounded for the exponentials; whether a ratio is clipped is decided on the fp64
+// difference, against the logarithms of the ends, since a position beside an end would else change sides by a rounding. All sums are fp64, in an
+// order that sizes fix.
+//
+// Work is dealt in items: a warp has one of P equal slices of one sequence, so that long sequences among short ones spread over the device and no
+// position has to look for its sequence. Weights need the counts of valid positions first, so the call goes over the data twice (the mask alone
+// for the counts; logp and ref for the sums of pairs). Few positions: all phases in one launch of one cluster, with its barrier between
+// them (a chain of four kernels of 2 us each otherwise); many: a launch for each phase. Bound by launches, and by HBM from a million positions on.
+#pragma once
+#include <math_constants.h>
+#include <stdint.h>
+
+#include "mtpc_ptx.cuh"
+
+namespace mtpc {
+
+constexpr uint32_t kStatusBadOffset = 16u;
+constexpr int kObjectiveThreads = 512, kObjectiveWarps = kObjectiveThreads / 32;
+constexpr int kObjectiveCtas = 8;                  // of the cluster that does a small call alone
+
+struct ObjectiveArgs {
+  const float *logp, *old, *ref, *advantage;       // ref: NULL without the KL term; advantage [S], or [T] with by_position (policy)
+  const uint8_t* mask;                             // [T] or NULL
+  const int* offsets;                              // [S + 1]
+  int T, S, parts;                                 // parts: slices of a sequence
+  int by_sequence, by_position;
+  double log_low, log_high;                        // logarithms of the ends
+  float low, high;                                 // the ends: 1 - clip_low, 1 + clip_high
+  double beta, smoothing;
+  float *loss, *stats, *d_logp, *h;                // stats [3] or NULL; h [S / 2] or NULL
+  uint32_t* status;
+  // workspace
+  int* count;                                      // [S * parts] valid positions of every slice
+  double* sum;                                     // [S * parts][3] (policy) or [S * parts] (preference)
+  double* term;                                    // [S / 2] a pair's loss
+  float* slope;                                    // [S / 2]
+};
+
+// Where sequence s lies; offsets that decrease or leave [0, T] are brought into it and refused at the end.
+struct Span {
+  int begin, end;
+  bool refused;
+};
+__device__ __forceinline__ Span span_of(const ObjectiveArgs& a, int s) {
+  const int lo = a.offsets[s], hi = a.offsets[s + 1];
+  Span x;
+  x.refused = lo < 0 || hi < lo || hi > a.T;
+  x.begin = min(max(lo, 0), a.T);
+  x.end = max(x.begin, min(max(hi, 0), a.T));
+  return x;
+}
+// Item `item`: slice `item % parts` of sequence `item / parts`, cut at multiples of four positions.
+struct Slice {
+  int s, begin, end;
+};
+__device__ __forceinline__ Slice slice_of(const ObjectiveArgs& a, int item) {
+  Slice c;
+  c.s = item / a.parts;
+  const int part = item - c.s * a.parts;
+  const Span x = span_of(a, c.s);
+  auto cut = [&](int q) {
+    if (q == 0) return x.begin;
+    if (q == a.parts) return x.end;
+    return max(x.begin, (x.begin + static_cast<int>(static_cast<long long>(x.end - x.begin) * q / a.parts)) & ~3);
+  };
+  c.begin = cut(part);
+  c.end = cut(part + 1);
+  return c;
+}
+
+template <typename F>
+__device__ __forceinline__ F warp_total(F x) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  return x;
+}
+
+// body(first position, four flags) for every group of four positions that a warp's lanes have of [begin, end): the flags say which are inside and valid.
+template <bool WIDE, typename Body>
+__device__ __forceinline__ void over_slice(const ObjectiveArgs& a, const Slice& c, int lane, Body body) {
+#pragma unroll 2
+  for (int q = (c.begin >> 2) + lane; q * 4ll < c.end; q += 32) {
+    const int t = q * 4;
+    uint32_t valid = 0;
+    const bool inside = t >= c.begin && t + 4 <= c.end;
+    if (WIDE && inside && a.mask != nullptr) {
+      const uint32_t m = *reinterpret_cast<const uint32_t*>(a.mask + t);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) valid |= ((m >> (8 * i)) & 0xffu) ? 1u << i : 0u;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (t + i >= c.begin && t + i < c.end && (a.mask == nullptr || a.mask[t + i] != 0)) valid |= 1u << i;
+    }
+    body(t, valid, inside);
+  }
+}
+template <bool WIDE>
+__device__ __forceinline__ void load4(const float* p, int t, bool inside, uint32_t valid, float (&x)[4]) {
+  if (WIDE && inside) {
+    const float4 v = *reinterpret_cast<const float4*>(p + t);
+    x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = valid >> i & 1 ? p[t + i] : 0.f;
+  }
+}
+template <bool WIDE>
+__device__ __forceinline__ void store4(float* p, const Slice& c, int t, bool inside, const float (&x)[4]) {
+  if (WIDE && inside) {
+    *reinterpret_cast<float4*>(p + t) = make_float4(x[0], x[1], x[2], x[3]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (t + i >= c.begin && t + i < c.end) p[t + i] = x[i];
+  }
+}
+
+// ---- phases, each over items first, first + step, ... of a warp
+template <bool WIDE>
+__device__ __forceinline__ void count_phase(const ObjectiveArgs& a, int first, int step, int lane) {
+  for (int item = first; item < a.S * a.parts; item += step) {
+    const Slice c = slice_of(a, item);
+    int n = 0;
+    over_slice<WIDE>(a, c, lane, [&](int, uint32_t valid, bool) { n += __popc(valid); });
+    n = warp_total(n);
+    if (lane == 0) a.count[item] = n;
+  }
+}
+
+// e^q - 1 - q, and e^q - 1: near zero by the series, whose next term is below 2^-28 of the first; the function less q is off by q's rounding.
+__device__ __forceinline__ void exp_beyond(float q, float& beyond, float& m1) {
+  m1 = expm1f(q);
+  if (fabsf(q) < 0.5f) {
+    float s = 1.f / 40320.f;
+    s = fmaf(s, q, 1.f / 5040.f);
+    s = fmaf(s, q, 1.f / 720.f);
+    s = fmaf(s, q, 1.f / 120.f);
+    s = fmaf(s, q, 1.f / 24.f);
+    s = fmaf(s, q, 1.f / 6.f);
+    s = fmaf(s, q, 0.5f);
+    beyond = q * q * s;
+  } else {
+    beyond = m1 - q;
+  }
+}
+
+// total: all valid positions.
+template <bool WIDE>
+__device__ __forceinline__ void policy_phase(const ObjectiveArgs& a, int first, int step, int lane, long long total) {
+  for (int item = first; item < a.S * a.parts; item += step) {
+    const Slice c = slice_of(a, item);
+    long long n = total;
+    if (a.by_sequence) {
+      const Span x = span_of(a, c.s);
+      int mine = a.mask == nullptr && lane == 0 ? x.end - x.begin : 0;
+      if (a.mask != nullptr)
+        for (int q = lane; q < a.parts; q += 32) mine += a.count[c.s * a.parts + q];
+      n = static_cast<long long>(warp_total(mine)) * a.S;
+    }
+    const double weight = n > 0 ? 1.0 / static_cast<double>(n) : 0.0;
+    const float w = static_cast<float>(weight), beta = static_cast<float>(a.beta);
+    float adv4[4];
+    adv4[0] = adv4[1] = adv4[2] = adv4[3] = a.by_position ? 0.f : a.advantage[c.s];
+    double value = 0.0, kl = 0.0;
+    int clipped = 0;
+    over_slice<WIDE>(a, c, lane, [&](int t, uint32_t valid, bool inside) {
+      float lp[4], old[4], ref[4], g[4];
+      load4<WIDE>(a.logp, t, inside, valid, lp);
+      load4<WIDE>(a.old, t, inside, valid, old);
+      if (a.ref != nullptr) load4<WIDE>(a.ref, t, inside, valid, ref);
+      if (a.by_position) load4<WIDE>(a.advantage, t, inside, valid, adv4);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float adv = adv4[i];
+        const double diff = static_cast<double>(lp[i]) - static_cast<double>(old[i]);
+        const float r = expf(static_cast<float>(diff));
+        const bool up = adv > 0.f && diff > a.log_high, down = adv < 0.f && diff < a.log_low, out = up || down;
+        const float gain = adv == 0.f ? 0.f : (up ? a.high : down ? a.low : r) * adv;
+        float slope = out || adv == 0.f ? 0.f : -gain, beyond = 0.f, m1 = 0.f;
+        if (a.ref != nullptr) {
+          exp_beyond(static_cast<float>(static_cast<double>(ref[i]) - static_cast<double>(lp[i])), beyond, m1);
+          slope = fmaf(-beta, m1, slope);
+        }
+        const bool counts = valid >> i & 1;
+        g[i] = counts ? w * slope : 0.f;
+        if (counts) {
+          value -= static_cast<double>(gain);
+          kl += static_cast<double>(beyond);
+          clipped += out ? 1 : 0;
+        }
+      }
+      store4<WIDE>(a.d_logp, c, t, inside, g);
+    });
+    value = warp_total(value);
+    kl = warp_total(kl);
+    clipped = warp_total(clipped);
+    if (lane == 0) {
+      a.sum[3 * static_cast<size_t>(item)] = value * weight;
+      a.sum[3 * static_cast<size_t>(item) + 1] = kl * weight;
+      a.sum[3 * static_cast<size_t>(item) + 2] = clipped * weight;
+    }
+  }
+}
+
+// N sums of n values each that the threads of a block have in turn, in an order that n fixes; every thread gets them. red: N * kObjectiveWarps values.
+template <int N, typename F, typename Get>
+__device__ __forceinline__ void block_totals(int n, F (&x)[N], F* red, Get get) {
+#pragma unroll
+  for (int k = 0; k < N; ++k) x[k] = 0;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < n; i += kObjectiveThreads) get(i, x);
+#pragma unroll
+  for (int k = 0; k < N; ++k) x[k] = warp_total(x[k]);
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) red[k * kObjectiveWarps + (threadIdx.x >> 5)] = x[k];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    x[k] = 0;
+#pragma unroll
+    for (int i = 0; i < kObjectiveWarps; ++i) x[k] += red[k * kObjectiveWarps + i];
+  }
+}
+// All valid positions (whole numbers: any order gives the same).
+__device__ __forceinline__ long long all_valid(const ObjectiveArgs& a, long long* red) {
+  long long n[1];
+  if (a.mask != nullptr) {
+    block_totals<1>(a.S * a.parts, n, red, [&](int i, long long (&x)[1]) { x[0] += a.count[i]; });
+  } else {
+    block_totals<1>(a.S, n, red, [&](int s, long long (&x)[1]) {
+      const Span c = span_of(a, s);
+      x[0] += c.end - c.begin;
+    });
+  }
+  return n[0];
+}
+// Whether offsets were refused: the loss has no value then.
+__device__ __forceinline__ bool any_refused(const ObjectiveArgs& a, long long* red) {
+  long long n[1];
+  block_totals<1>(a.S, n, red, [&](int s, long long (&x)[1]) { x[0] += span_of(a, s).refused ? 1 : 0; });
+  if (n[0] > 0 && threadIdx.x == 0 && a.status != nullptr) atomicOr(a.status, kStatusBadOffset);
+  return n[0] > 0;
+}
+__device__ __forceinline__ void policy_final(const ObjectiveArgs& a, double* red) {
+  const bool refused = any_refused(a, reinterpret_cast<long long*>(red));
+  double s[3];
+  block_totals<3>(a.S * a.parts, s, red, [&](int item, double (&x)[3]) {
+#pragma unroll
+    for (int i = 0; i < 3; ++i) x[i] += a.sum[3 * static_cast<size_t>(item) + i];
+  });
+  if (threadIdx.x == 0) {
+    a.loss[0] = refused ? CUDART_NAN_F : static_cast<float>(s[0] + a.beta * s[1]);
+    if (a.stats != nullptr)
+      for (int i = 0; i < 3; ++i) a.stats[i] = refused ? CUDART_NAN_F : static_cast<float>(s[i]);
+  }
+}
+
+template <bool WIDE>
+__device__ __forceinline__ void ratio_phase(const ObjectiveArgs& a, int first, int step, int lane) {
+  for (int item = first; item < a.S * a.parts; item += step) {
+    const Slice c = slice_of(a, item);
+    double sum = 0.0;
+    over_slice<WIDE>(a, c, lane, [&](int t, uint32_t valid, bool inside) {
+      float lp[4], ref[4];
+      load4<WIDE>(a.logp, t, inside, valid, lp);
+      load4<WIDE>(a.ref, t, inside, valid, ref);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (valid >> i & 1) sum += static_cast<double>(lp[i]) - static_cast<double>(ref[i]);
+    });
+    sum = warp_total(sum);
+    if (lane == 0) a.sum[item] = sum;
+  }
+}
+// Pairs first, first + step, ... of a warp.
+__device__ __forceinline__ void pairs_phase(const ObjectiveArgs& a, int first, int step, int lane) {
+  const int pairs = a.S / 2;
+  for (int p = first; p < pairs; p += step) {
+    double h = 0.0;
+    for (int q = lane; q < 2 * a.parts; q += 32) {
+      const double x = a.sum[static_cast<size_t>(2 * p) * a.parts + q];
+      h += q < a.parts ? x : -x;
+    }
+    h = a.beta * warp_total(h);
+    const double e = exp(-fabs(h));
+    const double low = e / (1.0 + e), of_other = h > 0.0 ? low : 1.0 - low;      // sigmoid(-h)
+    if (lane == 0) {
+      a.term[p] = log1p(e) + (1.0 - a.smoothing) * fmax(-h, 0.0) + a.smoothing * fmax(h, 0.0);      // log sigmoid(h) = min(h, 0) - log1p(e)
+      a.slope[p] = static_cast<float>(a.beta * (a.smoothing - of_other) / pairs);
+      if (a.h != nullptr) a.h[p] = static_cast<float>(h);
+    }
+  }
+}
+__device__ __forceinline__ void preference_final(const ObjectiveArgs& a, double* red) {
+  const bool refused = any_refused(a, reinterpret_cast<long long*>(red));
+  double s[1];
+  block_totals<1>(a.S / 2, s, red, [&](int p, double (&x)[1]) { x[0] += a.term[p]; });
+  if (threadIdx.x == 0) a.loss[0] = refused ? CUDART_NAN_F : static_cast<float>(s[0] / (a.S / 2));
+}
+template <bool WIDE>
+__device__ __forceinline__ void spread_phase(const ObjectiveArgs& a, int first, int step, int lane) {
+  for (int item = first; item < a.S * a.parts; item += step) {
+    const Slice c = slice_of(a, item);
+    const float slope = c.s & 1 ? -a.slope[c.s >> 1] : a.slope[c.s >> 1];
+    over_slice<WIDE>(a, c, lane, [&](int t, uint32_t valid, bool inside) {
+      float g[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) g[i] = valid >> i & 1 ? slope : 0.f;
+      store4<WIDE>(a.d_logp, c, t, inside, g);
+    });
+  }
+}
+
+// ---- one cluster does the whole call
+template <bool WIDE>
+__global__ void __launch_bounds__(kObjectiveThreads) policy_cluster_kernel(const ObjectiveArgs a) {
+  __shared__ double red[3 * kObjectiveWarps];
+  grid_launch_dependents();
+  grid_dependency_wait();
+  const int rank = static_cast<int>(cluster_cta_rank()), lane = threadIdx.x & 31;
+  const int first = rank * kObjectiveWarps + (threadIdx.x >> 5), step = kObjectiveCtas * kObjectiveWarps;
+  if (a.mask != nullptr) {
+    count_phase<WIDE>(a, first, step, lane);
+    cluster_sync_all();
+  }
+  policy_phase<WIDE>(a, first, step, lane, a.by_sequence ? 0 : all_valid(a, reinterpret_cast<long long*>(red)));
+  cluster_sync_all();
+  if (rank == 0) policy_final(a, red);
+}
+template <bool WIDE>
+__global__ void __launch_bounds__(kObjectiveThreads) preference_cluster_kernel(const ObjectiveArgs a) {
+  __shared__ double red[kObjectiveWarps];
+  grid_launch_dependents();
+  grid_dependency_wait();
+  const int rank = static_cast<int>(cluster_cta_rank()), lane = threadIdx.x & 31;
+  const int first = rank * kObjectiveWarps + (threadIdx.x >> 5), step = kObjectiveCtas * kObjectiveWarps;
+  ratio_phase<WIDE>(a, first, step, lane);
+  cluster_sync_all();
+  pairs_phase(a, first, step, lane);
+  cluster_sync_all();
+  spread_phase<WIDE>(a, first, step, lane);
+  if (rank == 0) preference_final(a, red);
+}
+
+// ---- a launch for each phase
+template <bool WIDE>
+__global__ void __launch_bounds__(kObjectiveThreads) count_kernel(const ObjectiveArgs a) {
+  grid_launch_dependents();
+  grid_dependency_wait();
+  count_phase<WIDE>(a, blockIdx.x * kObjectiveWarps + (threadIdx.x >> 5), gridDim.x * kObjectiveWarps, threadIdx.x & 31);
+}
+template <bool WIDE>
+__global__ void __launch_bounds__(kObjectiveThreads) policy_kernel(const ObjectiveArgs a) {
+  __shared__ long long red[kObjectiveWarps];
+  grid_launch_dependents();
+  grid_dependency_wait();
+  policy_phase<WIDE>(a, blockIdx.x * kObjectiveWarps + (threadIdx.x >> 5), gridDim.x * kObjectiveWarps, threadIdx.x & 31,
+                     a.by_sequence ? 0 : all_valid(a, red));
+}
+__global__ void __launch_bounds__(kObjectiveThreads) policy_final_kernel(const ObjectiveArgs a) {
+  __shared__ double red[3 * kObjectiveWarps];
+  grid_launch_dependents();
+  grid_dependency_wait();
+  policy_final(a, red);
+}
+template <bool WIDE>
+__global__ void __launch_bounds__(kObjectiveThreads) ratio_kernel(const ObjectiveArgs a) {
+  grid_launch_dependents();
+  grid_dependency_wait();
+  ratio_phase<WIDE>(a, blockIdx.x * kObjectiveWarps + (threadIdx.x >> 5), gridDim.x * kObjectiveWarps, threadIdx.x & 31);
+}
+__global__ void __launch_bounds__(kObjectiveThreads) pairs_kernel(const ObjectiveArgs a) {
+  grid_launch_dependents();
+  grid_dependency_wait();
+  pairs_phase(a, blockIdx.x * kObjectiveWarps + (threadIdx.x >> 5), gridDim.x * kObjectiveWarps, threadIdx.x & 31);
+}
+// The last block adds up the loss.
+template <bool WIDE>
+__global__ void __launch_bounds__(kObjectiveThreads) spread_kernel(const ObjectiveArgs a) {
+  __shared__ double red[kObjectiveWarps];
+  grid_launch_dependents();
+  grid_dependency_wait();
+  if (blockIdx.x + 1 == gridDim.x) preference_final(a, red);
+  else spread_phase<WIDE>(a, blockIdx.x * kObjectiveWarps + (threadIdx.x >> 5), (gridDim.x - 1) * kObjectiveWarps, threadIdx.x & 31);
+}
+
+}  // namespace mtpc

@@ -12,6 +12,7 @@
 #include "../../include/mtpc.h"
 #include "mtpc_clip.cuh"
 #include "mtpc_embed.cuh"
+#include "mtpc_host.cuh"
 #include "mtpc_launch.cuh"
 #include "mtpc_norm.cuh"
 
@@ -19,30 +20,9 @@ namespace {
 
 using namespace mtpc;
 
-constexpr size_t kAlign = 256;
-constexpr int kMaxRows = 1 << 30;
 constexpr long long kClearBesideChunks = 32 << 20;    // bytes
 constexpr long long kFewBytes = 32 << 20;
-constexpr int kSms = 148;               // what grids are sized for: the results of sums that are cut by them do not depend on the device
-size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
-bool aligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
-size_t element(int dtype) { return dtype == MTPC_F32 ? 4 : 2; }
-bool known(int dtype) { return dtype == MTPC_F32 || dtype == MTPC_BF16; }
 
-// The current device is one that the library is built for.
-int check_device() {
-  int dev = 0, major = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess || major != 10) {
-    cudaGetLastError();
-    return MTPC_ERR_CUDA;
-  }
-  return MTPC_OK;
-}
-
-// Rows of a matrix of the caller: every row starts where vectors of `vec` elements may. An absent matrix allows anything.
-bool rows_allow(const void* p, int64_t stride, size_t element_bytes, int vec, int rows) {
-  return p == nullptr || (aligned(p, element_bytes * vec) && (rows <= 1 || stride % vec == 0));
-}
 // Whether rows start off their vectors of eight elements alike in all of some matrices: then *shift and *pitch say how (SplitRow). Absent ones are left out.
 struct RowsOf {
   const void* p;
@@ -61,12 +41,6 @@ bool rows_alike(std::initializer_list<RowsOf> all, int* shift, int* pitch) {
   }
   return true;
 }
-// Rows that are read may lie anywhere, also all in one place (stride 0); rows that are written must not overlap.
-bool input_rows(const void* p, int64_t stride, int rows) { return p == nullptr || rows <= 1 || stride >= 0; }
-bool output_rows(const void* p, int64_t stride, int rows, int d) { return p == nullptr || rows <= 1 || stride >= d; }
-
-int ceil_div(long long a, long long b) { return static_cast<int>((a + b - 1) / b); }
-int round_warp(int x) { return (x + 31) / 32 * 32; }
 
 // ---------------------------------------------------------------- residual norm
 // How the rows of a call are read: as vectors, as vectors between single elements, or element by element.

@@ -80,6 +80,35 @@ def residual_rmsnorm_backward(total, weight, d_hidden, d_total=None, eps: float 
     return d_x, d_weight
 
 
+def dropout(x, p: float, rng, offset: int = 0, residual=None, dtype=None):
+    """Device tensors x, residual (or None) [T, d] -> residual + dropout of x (dtype: the residual's, or x's). On the gradient of that, without residual:
+    the gradient of x, while rng [2] int64 (seed, step) holds the same values."""
+    import torch
+    out = torch.empty(x.shape, dtype=dtype or (x if residual is None else residual).dtype, device=x.device)
+    B.mtpc_dropout(x, out, p, rng, offset=offset, residual=residual)
+    return out
+
+
+def policy_loss(logp, old_logp, ref_logp, advantage, offsets, clip_low: float = 0.2, clip_high: float = 0.2, beta: float = 0.0, mask=None, by_sequence=False,
+                by_position=False):
+    """-> dict(loss [1], stats [3], d_logp [T]) of packed sequences; d_logp is the `weight` of DeviceHead.window_logprob_backward."""
+    import torch
+    f32 = dict(dtype=torch.float32, device=logp.device)
+    out = dict(loss=torch.empty(1, **f32), stats=torch.empty(3, **f32), d_logp=torch.zeros(logp.shape, **f32))
+    B.mtpc_policy_loss(logp, old_logp, ref_logp, advantage, offsets, clip_low, clip_high, beta, out["loss"], out["d_logp"], mask=mask,
+                       by_sequence=by_sequence, by_position=by_position, out_stats=out["stats"])
+    return out
+
+
+def preference_loss(logp, ref_logp, offsets, beta: float = 0.1, smoothing: float = 0.0, mask=None):
+    """-> dict(loss [1], h [S / 2], d_logp [T]) of packed pairs of sequences; d_logp as for policy_loss."""
+    import torch
+    f32 = dict(dtype=torch.float32, device=logp.device)
+    out = dict(loss=torch.empty(1, **f32), h=torch.empty((offsets.numel() - 1) // 2, **f32), d_logp=torch.zeros(logp.shape, **f32))
+    B.mtpc_preference_loss(logp, ref_logp, offsets, beta, out["loss"], out["d_logp"], mask=mask, smoothing=smoothing, out_h=out["h"])
+    return out
+
+
 def _written_again(what, shapes, device, out):
     """The dict of an earlier call, if its tensors are what the call writes: adjacent fp32 elements of these shapes (None: absent) on that device."""
     import torch

@@ -1,0 +1,73 @@
+"""The calls that fit a model to tasks, without a device: what they refuse, the workspaces they ask for."""
+import ctypes
+
+import pytest
+
+from paper_2511_11346_b200 import binding as B
+
+P, ODD = ctypes.c_void_p(4096), ctypes.c_void_p(4098)           # never dereferenced: the argument checks come first
+F32, BF16 = B.MTPC_F32, B.MTPC_BF16
+NULL, SHAPE, UNSUPPORTED, WORKSPACE, CUDA = -1, -2, -3, -4, -5
+BIG, NAN, INF = 1 << 40, float("nan"), float("inf")
+
+
+def dropout(x=P, xs=64, xd=BF16, r=None, rs=64, T=4, d=64, p=0.1, rng=P, offset=0, out=P, os=64, od=BF16):
+    return B.lib().mtpc_dropout(x, xs, xd, r, rs, T, d, p, rng, offset, out, os, od, None)
+
+
+def policy(lp=P, old=P, ref=P, adv=P, per=0, mask=None, off=P, T=64, S=4, lo=0.2, hi=0.2, beta=0.1, seq=0, loss=P, stats=P, d=P, ws=P, wb=BIG, status=None):
+    return B.lib().mtpc_policy_loss(lp, old, ref, adv, per, mask, off, T, S, lo, hi, beta, seq, loss, stats, d, ws, wb, status, None)
+
+
+def preference(lp=P, ref=P, mask=None, off=P, T=64, S=4, beta=0.1, sm=0.0, loss=P, h=P, d=P, ws=P, wb=BIG, status=None):
+    return B.lib().mtpc_preference_loss(lp, ref, mask, off, T, S, beta, sm, loss, h, d, ws, wb, status, None)
+
+
+@pytest.mark.parametrize("call,kw,code", [
+    (dropout, dict(x=None), NULL), (dropout, dict(out=None), NULL), (dropout, dict(rng=None), NULL), (dropout, dict(T=-1), SHAPE), (dropout, dict(d=0), SHAPE),
+    (dropout, dict(T=(1 << 30) + 1), SHAPE), (dropout, dict(d=(1 << 30) + 1), SHAPE), (dropout, dict(T=1 << 20, d=(1 << 20) + 1, os=1 << 21), UNSUPPORTED), (dropout, dict(p=1.0), SHAPE), (dropout, dict(p=-0.1), SHAPE),
+    (dropout, dict(p=NAN), SHAPE), (dropout, dict(xd=2), SHAPE), (dropout, dict(od=-1), SHAPE), (dropout, dict(xs=-64), SHAPE), (dropout, dict(os=63), SHAPE),
+    (dropout, dict(os=0), SHAPE), (dropout, dict(r=P, rs=-1), SHAPE), (dropout, dict(rng=ctypes.c_void_p(4100)), SHAPE), (dropout, dict(x=ODD, xd=F32), SHAPE),
+    (dropout, dict(out=ODD, od=F32), SHAPE), (dropout, dict(r=ODD, od=F32), SHAPE),
+    (policy, dict(lp=None), NULL), (policy, dict(old=None), NULL), (policy, dict(ref=None), NULL), (policy, dict(adv=None), NULL), (policy, dict(off=None), NULL),
+    (policy, dict(loss=None), NULL), (policy, dict(d=None), NULL), (policy, dict(ws=None), NULL), (policy, dict(wb=16), WORKSPACE), (policy, dict(ws=ODD), WORKSPACE),
+    (policy, dict(T=-1), SHAPE), (policy, dict(S=0), SHAPE), (policy, dict(S=(1 << 20) + 1), UNSUPPORTED), (policy, dict(T=(1 << 30) + 1), UNSUPPORTED),
+    (policy, dict(lo=-0.1), SHAPE), (policy, dict(hi=NAN), SHAPE), (policy, dict(hi=INF), SHAPE), (policy, dict(beta=-1.0), SHAPE), (policy, dict(beta=NAN), SHAPE),
+    (policy, dict(lp=ODD), SHAPE), (policy, dict(d=ODD), SHAPE), (policy, dict(off=ODD), SHAPE), (policy, dict(stats=ODD), SHAPE), (policy, dict(status=ODD), SHAPE),
+    (preference, dict(lp=None), NULL), (preference, dict(ref=None), NULL), (preference, dict(off=None), NULL), (preference, dict(loss=None), NULL),
+    (preference, dict(d=None), NULL), (preference, dict(ws=None), NULL), (preference, dict(wb=16), WORKSPACE), (preference, dict(S=3), SHAPE),
+    (preference, dict(S=0), SHAPE), (preference, dict(beta=-0.1), SHAPE), (preference, dict(sm=1.5), SHAPE), (preference, dict(sm=NAN), SHAPE),
+    (preference, dict(h=ODD), SHAPE), (preference, dict(ref=ODD), SHAPE),
+])
+def test_refusals(call, kw, code):
+    assert call(**kw) == code
+
+
+def test_what_is_allowed_reaches_the_check_for_a_device():
+    import torch
+    assert dropout(T=0, x=None, out=None, rng=None) == 0
+    if torch.cuda.is_available():
+        pytest.skip("a device is present")
+    assert dropout() == dropout(T=1, xs=-1, os=0) == dropout(x=ODD, out=ODD, p=0.0) == dropout(r=P, rs=0, od=F32) == CUDA
+    assert policy() == policy(ref=None, beta=0.0, stats=None) == policy(lo=5.0, mask=ODD) == policy(T=0, lp=None, old=None, ref=None, d=None) == CUDA
+    assert preference() == preference(h=None, sm=1.0) == preference(T=0, lp=None, ref=None, d=None) == CUDA
+
+
+def test_workspaces():
+    need, L = ctypes.c_size_t(0), B.lib()
+    assert L.mtpc_objective_workspace_bytes(8, 8, None) == NULL and L.mtpc_objective_workspace_bytes(-1, 8, ctypes.byref(need)) == SHAPE
+    assert L.mtpc_objective_workspace_bytes(8, 0, ctypes.byref(need)) == SHAPE and L.mtpc_objective_workspace_bytes(8, 1 << 21, ctypes.byref(need)) == UNSUPPORTED
+    for T in (0, 1, 511, 65536, 65537, 1 << 20, 1 << 30):
+        for S in (1, 2, 1000, 1 << 20):
+            n = B.mtpc_objective_workspace_bytes(T, S)
+            assert n % 256 == 0 and n >= 28 * S
+    assert B.mtpc_objective_workspace_bytes(1 << 21, 256) < 1 << 20
+
+
+def test_tensors_that_do_not_fit_are_refused():
+    import torch
+    x, i = torch.zeros(4, 8), torch.zeros(5, dtype=torch.int32)
+    for call in (lambda: B.mtpc_dropout(x, x, 0.1, torch.zeros(2, dtype=torch.int64)), lambda: B.mtpc_policy_loss(x[0], x[0], x[0], x[1], i, 0.2, 0.2, 0.1, x[0], x[0]),
+                 lambda: B.mtpc_preference_loss(x[0], x[0], i, 0.1, x[0], x[0])):
+        with pytest.raises(B.MtpcError):
+            call()                                        # no tensor of a device
