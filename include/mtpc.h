@@ -70,7 +70,8 @@ enum {
                                    (or the prefix log-marginals from that byte on) of its window is NaN */
   MTPC_STATUS_TIMEOUT = 4u,     /* a bounded barrier wait expired; the outputs of that call are invalid */
   MTPC_STATUS_BAD_TOKEN = 8u,   /* the embedding calls: a token >= v was seen; its row is NaN, it has no gradient */
-  MTPC_STATUS_BAD_OFFSET = 16u  /* the losses of sequences: offsets that decrease or leave [0, T] were seen; the loss is NaN */
+  MTPC_STATUS_BAD_OFFSET = 16u, /* the losses of sequences: offsets that decrease or leave [0, T] were seen; the loss is NaN */
+  MTPC_STATUS_BAD_ADAPTOR = 32u /* the adapted projection: an adaptor >= S was seen; its row is NaN, it has no gradient */
 };
 
 typedef struct {
@@ -549,6 +550,42 @@ int mtpc_create_gradient_list(const mtpc_gradient* entries, int32_t count, void*
                               mtpc_gradient_list** out);
 int mtpc_clip_gradients(mtpc_gradient_list* list, float max_norm, float* out_norm, void* stream);
 int mtpc_destroy_gradient_list(mtpc_gradient_list* list);
+
+/*
+ * A projection with low-rank adaptors of many requests beside it (as U = W + A B of the factored head, one W for all):
+ *   out[t] = W x[t] + A[i] low[t],   low[t] = scale[i] * (B[i] x_low[t]),   i = row_adaptor[t]; without an adaptor (i < 0) out[t] = W x[t]
+ *   x, x_low dev [T, d] bf16: x_low is what the adaptors read, where that is not x itself (dropped-out activations: mtpc_dropout), or NULL.
+ *   W    dev [m, d] bf16;  A dev [S, m, k], B dev [S, k, d] bf16, adjacent;  scale dev [S] fp32 or NULL (ones).
+ *   row_adaptor dev [T] int32, or NULL: adaptor 0 for all rows. An adaptor >= S gives a row of NaN and MTPC_STATUS_BAD_ADAPTOR. Rows of one
+ *        adaptor are fastest beside each other, as those of a request are; any order works. What one adaptor's factors hold does not
+ *        reach rows of another, infinities and NaN included.
+ *   out  dev [T, m] bf16, not overlapping an input;  out_low dev [T, k] fp32, adjacent, or NULL: low, which the gradient of A needs (0 without adaptor).
+ *   workspace dev, 256-byte aligned, >= mtpc_adapted_projection_workspace_bytes(T, d, m, k, S, aligned_rows). aligned_rows != 0: every operand starts on 16
+ *        bytes, with strides, k and d that are multiples of eight elements and strides >= d; 0: any, of which the call makes copies.
+ *   out_status as for mtpc_embed.
+ * Products accumulate in fp32; low is held to 16 bits or more for its product with A, and out is rounded once.
+ * 0 <= T <= 2^24, 1 <= d, m <= 2^17, 1 <= k <= 64, 1 <= S <= 4096, S k max(d, m) <= 2^34 (MTPC_ERR_UNSUPPORTED beyond).
+ */
+int mtpc_adapted_projection_workspace_bytes(int32_t T, int32_t d, int32_t m, int32_t k, int32_t S, int32_t aligned_rows, size_t* out_bytes);
+int mtpc_adapted_projection(const void* x, int64_t x_stride, const void* x_low, int64_t x_low_stride, const void* W, int64_t W_stride, const void* A,
+                            const void* B, const float* scale, const int32_t* row_adaptor, int32_t T, int32_t d, int32_t m, int32_t k, int32_t S, void* out,
+                            int64_t out_stride, float* out_low, void* workspace, size_t workspace_bytes, uint32_t* out_status, void* stream);
+
+/*
+ * Its gradients but for that of W, which is shared and stays as it is:
+ *   v[t] = scale[i] * (A[i]^T d_out[t]),   d_x[t] = W^T d_out[t] + B[i]^T v[t],   dA[i] = sum of d_out[t] low[t]^T,   dB[i] = sum of v[t] x_low[t]^T
+ * over the rows t with adaptor i; adaptors without rows get zeros. Every output may be NULL.
+ *   x_low  dev [T, d] bf16: what the adaptors read (x, where the forward call had no x_low); needed for dB.   low: the forward call's out_low; for dA.
+ *   d_out  dev [T, m] bf16 (the norm's gradient in front of the head writes that type);  d_x dev [T, d] bf16.
+ *   d_x_low dev [T, d] bf16 or NULL: takes B[i]^T v[t] apart from d_x (for the gradient of the dropout in front of the adaptors, whose call adds it to d_x).
+ *   dA dev [S, m, k] fp32, dB dev [S, k, d] fp32, adjacent, overwritten.
+ *   Rows with an adaptor >= S: as above, in d_x (d_x_low, where that is given). Other arguments and limits as above; aligned_rows speaks of d_out and m too.
+ */
+int mtpc_adapted_projection_backward_workspace_bytes(int32_t T, int32_t d, int32_t m, int32_t k, int32_t S, int32_t aligned_rows, size_t* out_bytes);
+int mtpc_adapted_projection_backward(const void* x_low, int64_t x_low_stride, const void* W, int64_t W_stride, const void* A, const void* B,
+                                     const float* scale, const int32_t* row_adaptor, const float* low, int32_t T, int32_t d, int32_t m, int32_t k, int32_t S,
+                                     const void* d_out, int64_t d_out_stride, void* d_x, int64_t d_x_stride, void* d_x_low, int64_t d_x_low_stride,
+                                     float* dA, float* dB, void* workspace, size_t workspace_bytes, uint32_t* out_status, void* stream);
 
 /*
  * Dropout: out = residual + x * scale where an element is kept, residual alone (or zero) where it is dropped. The gradient with respect to x is the same

@@ -1,4 +1,4 @@
-"""fp64 CPU oracle of what fits a model to tasks beside its head: dropout, and the policy and preference losses. TEST INFRASTRUCTURE, not a
+"""fp64 CPU oracle of what fits a model to tasks beside its head: adaptors beside a projection, dropout, and the policy and preference losses. TEST INFRASTRUCTURE, not a
 product path: plain numpy from the definitions in include/mtpc.h, position by position, sharing no code with the CUDA library.
 
 Pins (tests/test_oracle_tune.py): Philox4x32-10 equals the published known answers; every gradient equals central finite differences of its loss.
@@ -86,3 +86,46 @@ def preference_loss(logp, ref, offsets, beta, smoothing=0.0, mask=None):
             for t in range(offsets[s], offsets[s + 1]):
                 grad[t] = sign * slope if valid[t] else 0.0
     return loss, np.array(hs), grad
+
+
+def adapted_projection(x, W, A, B, scale, which, x_low=None):
+    """(out, low, sums of the magnitudes of out's terms [T, m], of low's [T, k]); which None: adaptor 0, negative: none, >= S: NaN"""
+    f = lambda a: np.asarray(a, dtype=np.float64)  # noqa: E731
+    x, W, A, B = f(x), f(W), f(A), f(B)
+    x_low = x if x_low is None else f(x_low)
+    S, _, k = A.shape
+    out, size = x @ W.T, np.abs(x) @ np.abs(W).T
+    low, low_size = np.zeros((len(x), k)), np.zeros((len(x), k))
+    for t in range(len(x)):
+        i = 0 if which is None else int(which[t])
+        if i >= S:
+            out[t], low[t] = np.nan, np.nan
+        elif i >= 0:
+            s = 1.0 if scale is None else float(scale[i])
+            low[t], low_size[t] = s * (B[i] @ x_low[t]), abs(s) * (np.abs(B[i]) @ np.abs(x_low[t]))
+            out[t] += A[i] @ low[t]
+            size[t] += np.abs(A[i]) @ low_size[t]
+    return out, low, size, low_size
+
+
+def adapted_projection_grad(x_low, W, A, B, scale, which, low, d_out):
+    """dict of d_x, d_x_low (its adaptors' part), dA, dB and, by the same names with _size, the sums of their terms' magnitudes"""
+    f = lambda a: np.asarray(a, dtype=np.float64)  # noqa: E731
+    x_low, W, A, B, low, g = f(x_low), f(W), f(A), f(B), f(low), f(d_out)
+    S = len(A)
+    base, base_size = g @ W, np.abs(g) @ np.abs(W)
+    part, part_size = np.zeros_like(base), np.zeros_like(base)
+    r = {key: np.zeros_like(v) for key, v in (("dA", A), ("dA_size", A), ("dB", B), ("dB_size", B))}
+    for t in range(len(g)):
+        i = 0 if which is None else int(which[t])
+        if i >= S:
+            base[t], part[t] = np.nan, np.nan
+        elif i >= 0:
+            s = 1.0 if scale is None else float(scale[i])
+            v, v_size = s * (A[i].T @ g[t]), abs(s) * (np.abs(A[i]).T @ np.abs(g[t]))
+            part[t], part_size[t] = B[i].T @ v, np.abs(B[i]).T @ v_size
+            r["dA"][i] += np.outer(g[t], low[t])
+            r["dA_size"][i] += np.abs(np.outer(g[t], low[t]))
+            r["dB"][i] += np.outer(v, x_low[t])
+            r["dB_size"][i] += np.outer(v_size, np.abs(x_low[t]))
+    return dict(r, d_x=base + part, d_x_size=base_size + part_size, d_x_base=base, d_x_base_size=base_size, d_x_low=part, d_x_low_size=part_size)

@@ -17,7 +17,7 @@ MTPC_F32, MTPC_BF16 = 0, 1
 MTPC_FLAG_HMM_CONTEXTUAL = 1
 MTPC_FLAG_SHORT_DRAFTS = 4
 MTPC_OK = 0
-STATUS_BAD_TARGET, STATUS_BAD_UNIFORM, STATUS_TIMEOUT, STATUS_BAD_TOKEN, STATUS_BAD_OFFSET = 1, 2, 4, 8, 16
+STATUS_BAD_TARGET, STATUS_BAD_UNIFORM, STATUS_TIMEOUT, STATUS_BAD_TOKEN, STATUS_BAD_OFFSET, STATUS_BAD_ADAPTOR = 1, 2, 4, 8, 16, 32
 
 EXPORTS = [
     "mtpc_workspace_bytes", "mtpc_create_head", "mtpc_window_logprob", "mtpc_draft_sample",
@@ -31,7 +31,8 @@ EXPORTS = [
     "mtpc_lowrank_window_loss_backward", "mtpc_embed", "mtpc_embed_backward", "mtpc_embed_backward_workspace_bytes",
     "mtpc_residual_rmsnorm", "mtpc_residual_rmsnorm_backward", "mtpc_residual_rmsnorm_backward_workspace_bytes",
     "mtpc_gradient_list_workspace_bytes", "mtpc_create_gradient_list", "mtpc_clip_gradients", "mtpc_destroy_gradient_list",
-    "mtpc_dropout", "mtpc_objective_workspace_bytes", "mtpc_policy_loss", "mtpc_preference_loss",
+    "mtpc_adapted_projection_workspace_bytes", "mtpc_adapted_projection", "mtpc_adapted_projection_backward_workspace_bytes",
+    "mtpc_adapted_projection_backward", "mtpc_dropout", "mtpc_objective_workspace_bytes", "mtpc_policy_loss", "mtpc_preference_loss",
 ]
 STATIC_SCRATCH_BYTES = 16 << 20
 ERR_STATIC_SCRATCH = -7
@@ -112,6 +113,11 @@ def lib() -> ctypes.CDLL:
     L.mtpc_create_gradient_list.argtypes = [vp, i32, vp, sz, vp, ctypes.POINTER(vp)]
     L.mtpc_clip_gradients.argtypes = [vp, f32, vp, vp]
     L.mtpc_destroy_gradient_list.argtypes = [vp]
+    L.mtpc_adapted_projection_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, i32, ctypes.POINTER(sz)]
+    L.mtpc_adapted_projection.argtypes = [vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp, i64, vp, vp, sz, vp, vp]
+    L.mtpc_adapted_projection_backward_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, i32, ctypes.POINTER(sz)]
+    L.mtpc_adapted_projection_backward.argtypes = [vp, i64, vp, i64, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, vp, vp, sz, vp,
+                                                   vp]
     L.mtpc_dropout.argtypes = [vp, i64, i32, vp, i64, i32, i32, f32, vp, i64, vp, i64, i32, vp]
     L.mtpc_objective_workspace_bytes.argtypes = [i32, i32, ctypes.POINTER(sz)]
     L.mtpc_policy_loss.argtypes = [vp, vp, vp, vp, i32, vp, vp, i32, i32, f32, f32, f32, i32, vp, vp, vp, vp, sz, vp, vp]
@@ -381,11 +387,11 @@ _dtype_codes = None
 
 def _dtypes() -> dict:
     """What the calls look up in torch, once (an import statement in every call costs a tenth of a small one)."""
-    global _dtype_codes, _current_device, _raw_stream, _int32, _int64, _float32, _bool, _uint8
+    global _dtype_codes, _current_device, _raw_stream, _int32, _int64, _float32, _bfloat16, _bool, _uint8
     if _dtype_codes is None:
         import torch
         _current_device, _int32, _float32 = torch._C._cuda_getDevice, torch.int32, torch.float32
-        _int64, _bool, _uint8 = torch.int64, torch.bool, torch.uint8
+        _int64, _bfloat16, _bool, _uint8 = torch.int64, torch.bfloat16, torch.bool, torch.uint8
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
         _dtype_codes = {torch.float32: MTPC_F32, torch.bfloat16: MTPC_BF16}
     return _dtype_codes
@@ -538,6 +544,78 @@ def mtpc_residual_rmsnorm_backward(sum, weight, eps: float, d_out, d_sum, d_x, d
           _vector(what, weight, d, dev), MTPC_F32 if weight is None else _dtype(what, weight), T, d, eps, d_out.data_ptr(),
           _rows(what, d_out, T, d, dev), _dtype(what, d_out), _ptr(d_sum), 0 if d_sum is None else _rows(what, d_sum, T, d, dev, d_x.dtype),
           d_x.data_ptr(), _rows(what, d_x, T, d, dev), _dtype(what, d_x), _vector(what, d_weight, d, dev, _float32), ws_ptr, ws_bytes)
+
+
+def _factors(what: str, A, B, m: int, d: int, dev: int):
+    """(S, k) of the adaptors' factors A [S, m, k] and B [S, k, d]."""
+    shape = A.shape
+    if len(shape) != 3 or shape[1] != m or B.shape != (shape[0], shape[2], d):
+        _refuse(what, f"adaptors {tuple(A.shape)} and {tuple(B.shape)} where (S, {m}, k) and (S, k, {d}) are needed")
+    for t in (A, B):
+        if t.dtype is not _bfloat16:
+            _refuse(what, f"{t.dtype} where {_bfloat16} is needed", ERR_UNSUPPORTED)
+        if t.get_device() != dev or not t.is_contiguous():
+            _refuse(what, f"adaptors {tuple(t.shape)} with strides {t.stride()} on {t.device}")
+    return shape[0], shape[2]
+
+
+def _plain_rows(*rows) -> int:
+    """Whether tensor maps address matrices as they lie: (address, stride) each, and what else has to be a multiple of eight."""
+    return 0 if any(at % 16 or stride % 8 for at, stride in rows) else 1
+
+
+def mtpc_adapted_projection(x, W, A, B, scale, row_adaptor, out, out_low=None, x_low=None, workspace=None, out_status=None, stream=None) -> None:
+    """out[t] = W x[t] + A[i] low[t], low[t] = scale[i] B[i] x_low[t], i = row_adaptor[t] (include/mtpc.h). x, x_low (None: x) [T, d], W [m, d],
+    A [S, m, k], B [S, k, d], out [T, m] bf16; scale [S] fp32 or None, row_adaptor [T] int32 (negative: none) or None (0 for all), out_low [T, k] fp32 or None."""
+    _dtypes()
+    what = "mtpc_adapted_projection"
+    T, d, stride, dev = _matrix(what, x)
+    m = W.shape[0]
+    W_stride = _rows(what, W, m, d, dev, _bfloat16)
+    if x.dtype is not _bfloat16:
+        _refuse(what, f"{x.dtype} where {_bfloat16} is needed", ERR_UNSUPPORTED)
+    S, k = _factors(what, A, B, m, d, dev)
+    low_stride = 0 if x_low is None else _rows(what, x_low, T, d, dev, _bfloat16)
+    out_stride = _rows(what, out, T, m, dev, _bfloat16)
+    if out_low is not None and (out_low.shape != (T, k) or out_low.dtype is not _float32 or not out_low.is_contiguous() or out_low.get_device() != dev):
+        _refuse(what, f"out_low {tuple(out_low.shape)} of {out_low.dtype}")
+    plain = _plain_rows((x.data_ptr(), stride if T > 1 else 0), (W.data_ptr(), W_stride if m > 1 else 0), (A.data_ptr(), k), (B.data_ptr(), d),
+                        (0 if x_low is None else x_low.data_ptr(), low_stride if T > 1 else 0))
+    if (T > 1 and (stride < d or (x_low is not None and low_stride < d))) or (m > 1 and W_stride < d):
+        plain = 0
+    ws = _scratch(what, workspace, _scratch_bytes("mtpc_adapted_projection_workspace_bytes", T, d, m, k, S, plain), dev, stream)
+    _call(what, lib().mtpc_adapted_projection, dev, stream, x.data_ptr(), stride, _ptr(x_low), low_stride, W.data_ptr(), W_stride, A.data_ptr(),
+          B.data_ptr(), _vector(what, scale, S, dev, _float32), _vector(what, row_adaptor, T, dev, _int32), T, d, m, k, S, out.data_ptr(), out_stride,
+          _ptr(out_low), ws.data_ptr(), ws.numel(), _vector(what, out_status, 1, dev, _int32))
+
+
+def mtpc_adapted_projection_backward(x_low, W, A, B, scale, row_adaptor, low, d_out, d_x, dA=None, dB=None, d_x_low=None, workspace=None, out_status=None,
+                                     stream=None) -> None:
+    """Gradients of the adapted projection from d_out [T, m] bf16 (include/mtpc.h): d_x [T, d] bf16, dA [S, m, k], dB [S, k, d] fp32, each None where it is
+    not wanted. x_low: the rows that the adaptors read (x, unless the forward call had others); low: the forward call's out_low (None without dA); d_x_low
+    [T, d] bf16: takes the adaptors' part of d_x apart."""
+    _dtypes()
+    what = "mtpc_adapted_projection_backward"
+    T, m, g_stride, dev = _matrix(what, d_out)
+    d = W.shape[1]
+    if d_out.dtype is not _bfloat16:
+        _refuse(what, f"{d_out.dtype} where {_bfloat16} is needed", ERR_UNSUPPORTED)
+    W_stride = _rows(what, W, m, d, dev, _bfloat16)
+    S, k = _factors(what, A, B, m, d, dev)
+    x_stride = 0 if x_low is None else _rows(what, x_low, T, d, dev, _bfloat16)
+    for name, t, shape in (("low", low, (T, k)), ("dA", dA, (S, m, k)), ("dB", dB, (S, k, d))):
+        if t is not None and (t.shape != shape or t.dtype is not _float32 or not t.is_contiguous() or t.get_device() != dev):
+            _refuse(what, f"{name} {tuple(t.shape)} of {t.dtype} where adjacent fp32 {shape} is needed")
+    plain = _plain_rows((d_out.data_ptr(), g_stride if T > 1 else 0), (W.data_ptr(), W_stride if m > 1 else 0), (A.data_ptr(), k), (B.data_ptr(), d),
+                        (0 if x_low is None else x_low.data_ptr(), x_stride if T > 1 else 0))
+    if (T > 1 and (g_stride < m or (x_low is not None and x_stride < d))) or (m > 1 and W_stride < d):
+        plain = 0
+    ws = _scratch(what, workspace, _scratch_bytes("mtpc_adapted_projection_backward_workspace_bytes", T, d, m, k, S, plain), dev, stream)
+    _call(what, lib().mtpc_adapted_projection_backward, dev, stream, _ptr(x_low), x_stride, W.data_ptr(), W_stride, A.data_ptr(), B.data_ptr(),
+          _vector(what, scale, S, dev, _float32), _vector(what, row_adaptor, T, dev, _int32), _ptr(low), T, d, m, k, S, d_out.data_ptr(), g_stride,
+          _ptr(d_x), 0 if d_x is None else _rows(what, d_x, T, d, dev, _bfloat16), _ptr(d_x_low),
+          0 if d_x_low is None else _rows(what, d_x_low, T, d, dev, _bfloat16), _ptr(dA), _ptr(dB), ws.data_ptr(), ws.numel(),
+          _vector(what, out_status, 1, dev, _int32))
 
 
 def mtpc_dropout(x, out, p: float, rng, offset: int = 0, residual=None, stream=None) -> None:

@@ -9,7 +9,7 @@ import sys
 PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libmtpc.so")
-SOURCES = ["mtpc_api.cu", "mtpc_step.cu", "mtpc_tune.cu"]
+SOURCES = ["mtpc_api.cu", "mtpc_step.cu", "mtpc_tune.cu", "mtpc_adapted.cu"]
 HEADERS = sorted(f for f in os.listdir(CSRC) if f.endswith(".cuh")) + [os.path.join("..", "..", "include", "mtpc.h")]
 
 

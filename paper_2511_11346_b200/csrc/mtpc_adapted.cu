@@ -1,0 +1,496 @@
+// Host side of the projection with low-rank adaptors (include/mtpc.h): argument checks, tensor maps, carving of the caller's workspace, choice of
+// the build, launches.
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+#include <string.h>
+
+#include <algorithm>
+#include <initializer_list>
+
+#include "../../include/mtpc.h"
+#include "mtpc_adapted.cuh"
+#include "mtpc_host.cuh"
+#include "mtpc_launch.cuh"
+
+namespace {
+
+using namespace mtpc;
+
+constexpr int kSmemLimit = 232448;      // 227 KB of dynamic shared memory per CTA on sm_100
+constexpr int kFewRows = 128;
+constexpr int kMaxAdaptors = 4096, kMaxWidth = 1 << 17, kMaxBatch = 1 << 24;
+constexpr size_t kControl = 1024 + sizeof(GemmControl);
+
+// ---------------------------------------------------------------- tensor maps
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiledFn encode_fn() {
+  static EncodeTiledFn fn = []() -> EncodeTiledFn {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess) return nullptr;
+    return reinterpret_cast<EncodeTiledFn>(p);
+  }();
+  return fn;
+}
+// bf16 rows of `cols` adjacent elements, `pitch` apart, of `matrices` matrices one behind the other (0: a map of two axes): boxes of 64 columns x box_rows,
+// 128-byte swizzle, zeros outside.
+int map_rows(CUtensorMap* tm, const void* base, uint64_t rows, uint64_t cols, uint64_t pitch, uint32_t box_rows, uint64_t matrices = 0) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return MTPC_ERR_CUDA;
+  const cuuint64_t dims[3] = {cols, rows, matrices}, strides[2] = {pitch * 2, rows * pitch * 2};
+  const cuuint32_t box[3] = {64, box_rows, 1}, each[3] = {1, 1, 1};
+  const CUresult r = fn(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, matrices ? 3 : 2, const_cast<void*>(base), dims, strides, box, each,
+                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? MTPC_OK : MTPC_ERR_CUDA;
+}
+
+// ---------------------------------------------------------------- sizes
+int check_sizes(int T, int d, int m, int k, int S) {
+  if (T < 0 || d < 1 || m < 1 || k < 1 || S < 1) return MTPC_ERR_SHAPE;
+  if (T > kMaxBatch || d > kMaxWidth || m > kMaxWidth || k > kMaxRank || S > kMaxAdaptors) return MTPC_ERR_UNSUPPORTED;
+  if (static_cast<int64_t>(S) * k * std::max(d, m) > (static_cast<int64_t>(1) << 34)) return MTPC_ERR_UNSUPPORTED;
+  return MTPC_OK;
+}
+int up8(int x) { return (x + 7) / 8 * 8; }
+int rank16(int k) { return (k + 15) / 16 * 16; }
+int pieces_of(int k) { return (k + kPieceRank - 1) / kPieceRank; }
+int chunks_of(int K) { return ceil_div(K, kChunkBlocks * kBlockK); }
+
+struct ForwardPlan {
+  size_t off_status, off_low, off_part, off_two, off_x, off_x_low, off_W, off_A, off_B, total;
+};
+void plan_forward(int T, int d, int m, int k, int S, bool copies, ForwardPlan* p) {
+  size_t off = 0;
+  auto take = [&](size_t bytes) { size_t o = off; off += align_up(bytes); return o; };
+  const size_t rows = T, dp = up8(d);
+  const bool few = T <= kFewRows;
+  p->off_status = take(4);
+  p->off_low = take(few ? rows * k * 4 : 0);
+  p->off_part = take(few ? 0 : rows * chunks_of(d) * rank16(k) * 4);
+  p->off_two = take(few ? 0 : rows * pieces_of(k) * 128);
+  p->off_x = take(copies ? rows * dp * 2 : 0);
+  p->off_x_low = take(copies && !few ? rows * dp * 2 : 0);
+  p->off_W = take(copies ? m * dp * 2 : 0);
+  p->off_A = take(copies && !few ? static_cast<size_t>(S) * m * up8(k) * 2 : 0);
+  p->off_B = take(copies && !few ? static_cast<size_t>(S) * k * dp * 2 : 0);
+  p->total = off;
+}
+
+// Runs of row blocks that the adaptors' gradients are cut into: what takes least, a run being its blocks and about four more for its start and end. An adaptor's
+// rows lie beside each other, so that up to S runs cut few adaptors' rows (n: runs that have rows).
+int grad_splits(int tiles, int S, int blocks) {
+  int best = 1;
+  double least = 0.0;
+  for (int s = 1; s <= 32 && s <= std::max(1, blocks / 4); ++s) {
+    const int n = std::max(s, S);
+    const double cost = static_cast<double>(ceil_div(static_cast<long long>(tiles) * n, kSms)) * (static_cast<double>(blocks) / n + 4.0);
+    if (s == 1 || cost < least * 0.97) best = s, least = cost;
+  }
+  return best;
+}
+struct BackwardPlan {
+  int splits;
+  size_t off_status, off_part, off_two, off_low3, off_v3, off_present, off_grad, off_x, off_W, off_A, off_B, off_g, total;
+};
+void plan_backward(int T, int d, int m, int k, int S, bool copies, BackwardPlan* p) {
+  size_t off = 0;
+  auto take = [&](size_t bytes) { size_t o = off; off += align_up(bytes); return o; };
+  const size_t rows = T, dp = up8(d), k16 = rank16(k);
+  const int blocks = ceil_div(T, 64), tiles = ceil_div(d, kBlockM) + ceil_div(m, kBlockM);
+  p->splits = grad_splits(tiles, S, blocks);
+  p->off_status = take(4);
+  p->off_part = take(rows * chunks_of(m) * k16 * 4);
+  p->off_two = take(rows * pieces_of(k) * 128);
+  p->off_low3 = take(rows * 3 * k16 * 2);
+  p->off_v3 = take(rows * 3 * k16 * 2);
+  p->off_present = take(static_cast<size_t>(ceil_div(blocks, 32)) * S * 4);
+  p->off_grad = take(p->splits > 1 ? static_cast<size_t>(p->splits) * S * tiles * kBlockM * k16 * 4 : 0);
+  p->off_x = take(copies ? rows * dp * 2 : 0);
+  p->off_W = take(copies ? m * dp * 2 : 0);
+  p->off_A = take(copies ? static_cast<size_t>(S) * m * up8(k) * 2 : 0);
+  p->off_B = take(copies ? static_cast<size_t>(S) * k * dp * 2 : 0);
+  p->off_g = take(copies ? rows * up8(m) * 2 : 0);
+  p->total = off;
+}
+
+// ---------------------------------------------------------------- operands
+struct Rows {
+  const __nv_bfloat16* p;
+  int64_t stride;
+};
+// Whether tensor maps can address rows as they lie.
+bool mappable(const void* p, int64_t stride, int64_t rows, int cols) { return aligned(p, 16) && (rows <= 1 || (stride % 8 == 0 && stride >= cols)); }
+
+// Copies of what is not mappable, in one launch; `fine`: all of it was.
+struct Copier {
+  CopyParams c;
+  int n = 0;
+  Copier() { memset(&c, 0, sizeof(c)); }
+  Rows rows(const void* p, int64_t stride, int64_t rows, int cols, void* to) {
+    Rows r{static_cast<const __nv_bfloat16*>(p), rows > 1 ? stride : up8(cols)};
+    if (p == nullptr || mappable(p, stride, rows, cols)) return r;
+    CopyRows& m = c.m[n];
+    m.src = r.p;
+    m.dst = static_cast<__nv_bfloat16*>(to);
+    m.stride = stride;
+    m.rows = rows;
+    m.cols = cols;
+    m.pitch = up8(cols);
+    ++n;
+    c.begin[n] = c.begin[n - 1] + rows * (m.pitch / 8);
+    if (n == 4) launch_now();
+    return Rows{m.dst, m.pitch};
+  }
+  void launch_now() {
+    if (n == 0) return;
+    for (int i = n + 1; i <= 4; ++i) c.begin[i] = c.begin[n];
+    launch_kernel(copy_rows_kernel, ceil_div(c.begin[4], 256), 256, 0, st, true, c);
+    memset(&c, 0, sizeof(c));
+    n = 0;
+  }
+  cudaStream_t st = nullptr;
+};
+
+constexpr int kMaxDevices = 64;
+int g_allowed[kMaxDevices];
+// The kernels may use the shared memory that they ask for: said once on each device.
+int allow_shared_memory() {
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return MTPC_ERR_CUDA;
+  if (__atomic_load_n(&g_allowed[dev], __ATOMIC_ACQUIRE)) return MTPC_OK;
+  const auto allow = [](auto* kernel, int bytes) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess; };
+  bool ok = allow(adaptor_low_kernel<false>, kSmemLimit) && allow(adaptor_low_kernel<true>, kSmemLimit) && allow(adapted_rows_kernel, kSmemLimit);
+  ok = ok && allow(adapted_gemm_kernel<false, 256, 2>, kSmemLimit) && allow(adapted_gemm_kernel<true, 256, 2>, kSmemLimit);
+  ok = ok && allow(adapted_gemm_kernel<false, 128, 1>, kSmemLimit) && allow(adapted_gemm_kernel<true, 128, 1>, kSmemLimit);
+  ok = ok && allow(adapted_gemm_kernel<false, 64, 1>, kSmemLimit) && allow(adapted_gemm_kernel<true, 64, 1>, kSmemLimit);
+  ok = ok && allow(adaptor_grad_kernel<16>, kSmemLimit) && allow(adaptor_grad_kernel<32>, kSmemLimit) && allow(adaptor_grad_kernel<48>, kSmemLimit) &&
+       allow(adaptor_grad_kernel<64>, kSmemLimit);
+  if (!ok) return MTPC_ERR_CUDA;
+  __atomic_store_n(&g_allowed[dev], 1, __ATOMIC_RELEASE);
+  return MTPC_OK;
+}
+int stages_of(int stage_bytes, int ctas_per_sm = 1) {
+  return std::min(kMaxStages, static_cast<int>((kSmemLimit / ctas_per_sm - (ctas_per_sm > 1 ? 1024 : 0) - kControl) / stage_bytes));
+}
+
+// ---------------------------------------------------------------- launches
+// low or v: rows [T, K] times the factors; parts of every chunk of K.
+int launch_low(const Rows& rows, const Rows& factors, bool mn, const int* which, int T, int K, int k, int S, float* part, unsigned* status, cudaStream_t st) {
+  LowParams p;
+  memset(&p, 0, sizeof(p));
+  int rc = map_rows(&p.tm_a, rows.p, T, K, rows.stride, kBlockM);
+  if (rc == MTPC_OK) rc = mn ? map_rows(&p.tm_f, factors.p, K, k, factors.stride, 64, S) : map_rows(&p.tm_f, factors.p, k, K, factors.stride, rank16(k), S);
+  if (rc != MTPC_OK) return rc;
+  p.which = which;
+  p.part = part;
+  p.status = status;
+  p.wait_limit_ns = kWaitLimitNs;
+  p.T = T;
+  p.S = S;
+  p.k16 = rank16(k);
+  p.kblocks = ceil_div(K, kBlockK);
+  p.chunks = chunks_of(K);
+  p.tiles = ceil_div(T, kBlockM);
+  p.stages = stages_of(kLowStageBytes, 2);
+  const size_t smem = kControl + static_cast<size_t>(p.stages) * kLowStageBytes;
+  launch_kernel(mn ? adaptor_low_kernel<true> : adaptor_low_kernel<false>, std::min(p.tiles * p.chunks, 2 * kSms), kLowThreads, smem, st, true, p);
+  return check_launch();
+}
+int launch_join(const LowJoinParams& p, cudaStream_t st) {
+  launch_kernel(adaptor_join_kernel, ceil_div(static_cast<long long>(p.T) * (p.k16 / 4), 256), 256, 0, st, true, p);
+  return check_launch();
+}
+
+template <bool B_MN, int TN, int CTAS>
+int launch_gemm(AdaptedParams& p, const Rows& a, const Rows& b, const __nv_bfloat16* two, const Rows& f, int K, cudaStream_t st) {
+  constexpr int kBCols = TN / CTAS;
+  int rc = map_rows(&p.tm_a, a.p, p.T, K, a.stride, kBlockM);
+  if (rc == MTPC_OK) rc = B_MN ? map_rows(&p.tm_b, b.p, K, p.N, b.stride, 64) : map_rows(&p.tm_b, b.p, p.N, K, b.stride, kBCols);
+  if (rc == MTPC_OK && p.pieces > 0) {
+    rc = map_rows(&p.tm_u, two, p.T, p.pieces * 64, p.pieces * 64, kBlockM);
+    if (rc == MTPC_OK) rc = B_MN ? map_rows(&p.tm_f, f.p, p.k, p.N, f.stride, 64, p.S) : map_rows(&p.tm_f, f.p, p.N, p.k, f.stride, kBCols, p.S);
+  }
+  if (rc != MTPC_OK) return rc;
+  p.m_units = ceil_div(p.T, kBlockM * CTAS);
+  p.n_tiles = ceil_div(p.N, TN);
+  p.stage_bytes = kABytes + kBCols * kBlockK * 2;
+  p.stages = stages_of(p.stage_bytes);
+  const size_t smem = kControl + static_cast<size_t>(p.stages) * p.stage_bytes;
+  const int workers = std::min(p.m_units * p.n_tiles, kSms / CTAS);
+  launch_clusters(adapted_gemm_kernel<B_MN, TN, CTAS>, CTAS, workers * CTAS, kAdaptedThreads, smem, st, true, p);
+  return check_launch();
+}
+// rows [T, K] times W (N rows of K, or with b_mn K rows of N), plus two terms of low times the factors; kblocks 0: these alone.
+int launch_product(const Rows& a, const Rows& b, const __nv_bfloat16* two, const Rows& f, bool b_mn, const int* which, int T, int K, int N, int k, int S,
+                   bool shared, bool adaptors, void* out, int64_t out_stride, unsigned* status, cudaStream_t st) {
+  AdaptedParams p;
+  memset(&p, 0, sizeof(p));
+  p.which = which;
+  p.out = static_cast<__nv_bfloat16*>(out);
+  p.out_stride = out_stride;
+  p.status = status;
+  p.wait_limit_ns = kWaitLimitNs;
+  p.T = T;
+  p.S = S;
+  p.N = N;
+  p.k = k;
+  p.pieces = adaptors ? pieces_of(k) : 0;
+  p.kblocks = shared ? ceil_div(K, kBlockK) : 0;
+  p.store = rows_allow(out, out_stride, 2, 16, T) ? 32 : rows_allow(out, out_stride, 2, 8, T) ? 16 : 2;
+  // Cycles that a K block of a tile takes and that its rest does, by the bytes that an SM gets from L2 and its MMAs' time, whichever is longer.
+  const double kb = p.kblocks + 2.0 * p.pieces;
+  const double pair = ceil_div(static_cast<long long>(ceil_div(T, 256)) * ceil_div(N, 256), kSms / 2) * (kb * 560 + 2000);
+  const double wide = ceil_div(static_cast<long long>(ceil_div(T, 128)) * ceil_div(N, 128), kSms) * (kb * 450 + 1500);
+  const double narrow = ceil_div(static_cast<long long>(ceil_div(T, 128)) * ceil_div(N, 64), kSms) * (kb * 350 + 1200);
+  if (pair <= wide && pair <= narrow)
+    return b_mn ? launch_gemm<true, 256, 2>(p, a, b, two, f, K, st) : launch_gemm<false, 256, 2>(p, a, b, two, f, K, st);
+  if (wide <= narrow) return b_mn ? launch_gemm<true, 128, 1>(p, a, b, two, f, K, st) : launch_gemm<false, 128, 1>(p, a, b, two, f, K, st);
+  return b_mn ? launch_gemm<true, 64, 1>(p, a, b, two, f, K, st) : launch_gemm<false, 64, 1>(p, a, b, two, f, K, st);
+}
+
+int launch_few_rows(const Rows& x, const Rows& W, const void* x_low, int64_t x_low_stride, const void* A, const void* B, const float* scale, const int* which,
+                    int T, int d, int m, int k, int S, void* out, int64_t out_stride, float* low, unsigned* status, unsigned* user_status, cudaStream_t st) {
+  LowRowsParams l;
+  memset(&l, 0, sizeof(l));
+  l.x = static_cast<const __nv_bfloat16*>(x_low);
+  l.B = static_cast<const __nv_bfloat16*>(B);
+  l.x_stride = T > 1 ? x_low_stride : 0;
+  l.which = which;
+  l.scale = scale;
+  l.low = low;
+  l.status = user_status;
+  l.T = T;
+  l.d = d;
+  l.k = k;
+  l.S = S;
+  l.wide = d % 8 == 0 && rows_allow(x_low, x_low_stride, 2, 8, T) && aligned(B, 16);
+  launch_kernel(low_rows_kernel, dim3(T, ceil_div(k, 4)), 128, 0, st, true, l);
+
+  RowsParams p;
+  memset(&p, 0, sizeof(p));
+  p.tokens = (T + 15) / 16 * 16;
+  int rc = map_rows(&p.tm_w, W.p, m, d, W.stride, kBlockM);
+  if (rc == MTPC_OK) rc = map_rows(&p.tm_x, x.p, T, d, x.stride, p.tokens);
+  if (rc != MTPC_OK) return rc;
+  p.A = static_cast<const __nv_bfloat16*>(A);
+  p.low = low;
+  p.which = which;
+  p.out = static_cast<__nv_bfloat16*>(out);
+  p.out_stride = out_stride;
+  p.status = status;
+  p.wait_limit_ns = kWaitLimitNs;
+  p.T = T;
+  p.S = S;
+  p.N = m;
+  p.k = k;
+  p.kblocks = ceil_div(d, kBlockK);
+  const int tiles = ceil_div(m, kBlockM);
+  p.split = 1;
+  while (p.split < 8 && p.split * 2 <= p.kblocks && tiles * p.split < 2 * kSms - 64) p.split *= 2;
+  p.stage_bytes = kABytes + p.tokens * kBlockK * 2;
+  p.stages = stages_of(p.stage_bytes, 2);
+  p.wide = k % 8 == 0 && aligned(A, 16);
+  const size_t smem = kControl + static_cast<size_t>(p.stages) * p.stage_bytes;
+  launch_clusters(adapted_rows_kernel, p.split, tiles * p.split, kRowsThreads, smem, st, true, p);
+  return check_launch();
+}
+
+}  // namespace
+
+extern "C" {
+
+int mtpc_adapted_projection_workspace_bytes(int32_t T, int32_t d, int32_t m, int32_t k, int32_t S, int32_t aligned_rows, size_t* out_bytes) {
+  if (!out_bytes) return MTPC_ERR_NULL;
+  const int rc = check_sizes(T, d, m, k, S);
+  if (rc != MTPC_OK) return rc;
+  ForwardPlan p;
+  plan_forward(T, d, m, k, S, aligned_rows == 0, &p);
+  *out_bytes = p.total;
+  return MTPC_OK;
+}
+
+int mtpc_adapted_projection(const void* x, int64_t x_stride, const void* x_low, int64_t x_low_stride, const void* W, int64_t W_stride, const void* A,
+                            const void* B, const float* scale, const int32_t* row_adaptor, int32_t T, int32_t d, int32_t m, int32_t k, int32_t S, void* out,
+                            int64_t out_stride, float* out_low, void* workspace, size_t workspace_bytes, uint32_t* out_status, void* stream) {
+  int rc = check_sizes(T, d, m, k, S);
+  if (rc != MTPC_OK) return rc;
+  if (T == 0) return MTPC_OK;
+  if (!x || !W || !A || !B || !out || !workspace) return MTPC_ERR_NULL;
+  if (!x_low) {
+    x_low = x;
+    x_low_stride = x_stride;
+  }
+  if (!input_rows(x, x_stride, T) || !input_rows(x_low, x_low_stride, T) || !input_rows(W, W_stride, m) || !output_rows(out, out_stride, T, m)) return MTPC_ERR_SHAPE;
+  for (const void* q : {x, x_low, W, A, B, static_cast<const void*>(out)})
+    if (!aligned(q, 2)) return MTPC_ERR_SHAPE;
+  for (const void* q : {static_cast<const void*>(scale), static_cast<const void*>(row_adaptor), static_cast<const void*>(out_low), static_cast<const void*>(out_status)})
+    if (!aligned(q, 4)) return MTPC_ERR_SHAPE;
+  const bool few = T <= kFewRows;
+  const bool copies = !mappable(x, x_stride, T, d) || !mappable(W, W_stride, m, d) ||
+                      (!few && (!mappable(x_low, x_low_stride, T, d) || !mappable(A, k, 2, k) || !mappable(B, d, 2, d)));
+  ForwardPlan plan;
+  plan_forward(T, d, m, k, S, copies, &plan);
+  if (workspace_bytes < plan.total || !aligned(workspace, kAlign)) return MTPC_ERR_WORKSPACE;
+  if ((rc = check_device()) != MTPC_OK || (rc = allow_shared_memory()) != MTPC_OK) return rc;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  unsigned* status = out_status ? out_status : reinterpret_cast<unsigned*>(ws + plan.off_status);
+  Copier copy;
+  copy.st = st;
+  const Rows xr = copy.rows(x, x_stride, T, d, ws + plan.off_x), Wr = copy.rows(W, W_stride, m, d, ws + plan.off_W);
+  if (few) {
+    copy.launch_now();
+    float* low = out_low ? out_low : reinterpret_cast<float*>(ws + plan.off_low);
+    return launch_few_rows(xr, Wr, x_low, x_low_stride, A, B, scale, row_adaptor, T, d, m, k, S, out, out_stride, low, status, out_status, st);
+  }
+  const Rows Ar = copy.rows(A, k, static_cast<int64_t>(S) * m, k, ws + plan.off_A), Br = copy.rows(B, d, static_cast<int64_t>(S) * k, d, ws + plan.off_B);
+  const Rows lr = x_low == x && x_low_stride == x_stride ? xr : copy.rows(x_low, x_low_stride, T, d, ws + plan.off_x_low);
+  copy.launch_now();
+  float* part = reinterpret_cast<float*>(ws + plan.off_part);
+  if ((rc = launch_low(lr, Br, false, row_adaptor, T, d, k, S, part, status, st)) != MTPC_OK) return rc;
+  LowJoinParams j;
+  memset(&j, 0, sizeof(j));
+  j.which = row_adaptor;
+  j.scale = scale;
+  j.part = part;
+  j.low = out_low;
+  j.two = reinterpret_cast<__nv_bfloat16*>(ws + plan.off_two);
+  j.status = out_status;
+  j.T = T;
+  j.S = S;
+  j.k = k;
+  j.k16 = rank16(k);
+  j.chunks = chunks_of(d);
+  j.pieces = pieces_of(k);
+  if ((rc = launch_join(j, st)) != MTPC_OK) return rc;
+  return launch_product(xr, Wr, j.two, Ar, false, row_adaptor, T, d, m, k, S, true, true, out, out_stride, status, st);
+}
+
+int mtpc_adapted_projection_backward_workspace_bytes(int32_t T, int32_t d, int32_t m, int32_t k, int32_t S, int32_t aligned_rows, size_t* out_bytes) {
+  if (!out_bytes) return MTPC_ERR_NULL;
+  const int rc = check_sizes(T, d, m, k, S);
+  if (rc != MTPC_OK) return rc;
+  BackwardPlan p;
+  plan_backward(T, d, m, k, S, aligned_rows == 0, &p);
+  *out_bytes = p.total;
+  return MTPC_OK;
+}
+
+int mtpc_adapted_projection_backward(const void* x_low, int64_t x_low_stride, const void* W, int64_t W_stride, const void* A, const void* B,
+                                     const float* scale, const int32_t* row_adaptor, const float* low, int32_t T, int32_t d, int32_t m, int32_t k, int32_t S,
+                                     const void* d_out, int64_t d_out_stride, void* d_x, int64_t d_x_stride, void* d_x_low, int64_t d_x_low_stride,
+                                     float* dA, float* dB, void* workspace, size_t workspace_bytes, uint32_t* out_status, void* stream) {
+  int rc = check_sizes(T, d, m, k, S);
+  if (rc != MTPC_OK) return rc;
+  if (!workspace || (T > 0 && (!d_out || !A || !B || (d_x && !W) || (dA && !low) || (dB && !x_low)))) return MTPC_ERR_NULL;
+  if (!input_rows(x_low, x_low_stride, T) || !input_rows(W, W_stride, m) || !input_rows(d_out, d_out_stride, T) || !output_rows(d_x, d_x_stride, T, d) ||
+      !output_rows(d_x_low, d_x_low_stride, T, d))
+    return MTPC_ERR_SHAPE;
+  for (const void* q : {x_low, W, A, B, d_out, static_cast<const void*>(d_x), static_cast<const void*>(d_x_low)})
+    if (!aligned(q, 2)) return MTPC_ERR_SHAPE;
+  for (const void* q : {static_cast<const void*>(scale), static_cast<const void*>(row_adaptor), static_cast<const void*>(low), static_cast<const void*>(dA),
+                        static_cast<const void*>(dB), static_cast<const void*>(out_status)})
+    if (!aligned(q, 4)) return MTPC_ERR_SHAPE;
+  const bool copies = (dB && !mappable(x_low, x_low_stride, T, d)) || (d_x && !mappable(W, W_stride, m, d)) || !mappable(A, k, 2, k) || !mappable(B, d, 2, d) ||
+                      !mappable(d_out, d_out_stride, T, m);
+  BackwardPlan plan;
+  plan_backward(T, d, m, k, S, copies, &plan);
+  if (workspace_bytes < plan.total || !aligned(workspace, kAlign)) return MTPC_ERR_WORKSPACE;
+  if ((rc = check_device()) != MTPC_OK || (rc = allow_shared_memory()) != MTPC_OK) return rc;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (T == 0) {
+    if ((dA && cudaMemsetAsync(dA, 0, static_cast<size_t>(S) * m * k * 4, st) != cudaSuccess) ||
+        (dB && cudaMemsetAsync(dB, 0, static_cast<size_t>(S) * k * d * 4, st) != cudaSuccess))
+      return MTPC_ERR_CUDA;
+    return MTPC_OK;
+  }
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  unsigned* status = out_status ? out_status : reinterpret_cast<unsigned*>(ws + plan.off_status);
+  Copier copy;
+  copy.st = st;
+  const Rows gr = copy.rows(d_out, d_out_stride, T, m, ws + plan.off_g);
+  const Rows Ar = copy.rows(A, k, static_cast<int64_t>(S) * m, k, ws + plan.off_A), Br = copy.rows(B, d, static_cast<int64_t>(S) * k, d, ws + plan.off_B);
+  const Rows Wr = d_x ? copy.rows(W, W_stride, m, d, ws + plan.off_W) : Rows{nullptr, 0};
+  const Rows xr = dB ? copy.rows(x_low, x_low_stride, T, d, ws + plan.off_x) : Rows{nullptr, 0};
+  copy.launch_now();
+
+  LowJoinParams j;
+  memset(&j, 0, sizeof(j));
+  j.which = row_adaptor;
+  j.status = out_status;
+  j.T = T;
+  j.S = S;
+  j.k = k;
+  j.k16 = rank16(k);
+  j.pieces = pieces_of(k);
+  __nv_bfloat16* two = reinterpret_cast<__nv_bfloat16*>(ws + plan.off_two);
+  __nv_bfloat16* low3 = reinterpret_cast<__nv_bfloat16*>(ws + plan.off_low3);
+  __nv_bfloat16* v3 = reinterpret_cast<__nv_bfloat16*>(ws + plan.off_v3);
+  if (d_x || d_x_low || dB) {
+    float* part = reinterpret_cast<float*>(ws + plan.off_part);
+    if ((rc = launch_low(gr, Ar, true, row_adaptor, T, m, k, S, part, status, st)) != MTPC_OK) return rc;
+    j.scale = scale;
+    j.part = part;
+    j.two = d_x || d_x_low ? two : nullptr;
+    j.three = dB ? v3 : nullptr;
+    j.chunks = chunks_of(m);
+    if ((rc = launch_join(j, st)) != MTPC_OK) return rc;
+  }
+  if (d_x && (rc = launch_product(gr, Wr, two, Br, true, row_adaptor, T, m, d, k, S, true, d_x_low == nullptr, d_x, d_x_stride, status, st)) != MTPC_OK) return rc;
+  if (d_x_low && (rc = launch_product(gr, Rows{gr.p, gr.stride}, two, Br, true, row_adaptor, T, m, d, k, S, false, true, d_x_low, d_x_low_stride, status, st)) != MTPC_OK)
+    return rc;
+  if (!dA && !dB) return MTPC_OK;
+  if (dA) {
+    j.scale = nullptr;
+    j.part = nullptr;
+    j.given = low;
+    j.two = nullptr;
+    j.three = low3;
+    if ((rc = launch_join(j, st)) != MTPC_OK) return rc;
+  }
+  uint32_t* present = reinterpret_cast<uint32_t*>(ws + plan.off_present);
+  GradParams p;
+  memset(&p, 0, sizeof(p));
+  p.which = row_adaptor;
+  p.present = present;
+  p.out[0] = dA;
+  p.out[1] = dB;
+  p.part = reinterpret_cast<float*>(ws + plan.off_grad);
+  p.status = status;
+  p.wait_limit_ns = kWaitLimitNs;
+  p.T = T;
+  p.S = S;
+  p.k = k;
+  p.cols[0] = m;
+  p.cols[1] = d;
+  p.tiles[0] = dA ? ceil_div(m, kBlockM) : 0;
+  p.tiles[1] = dB ? ceil_div(d, kBlockM) : 0;
+  p.blocks = ceil_div(T, 64);
+  p.splits = plan.splits;
+  const int k16 = rank16(k);
+  for (int q = 0; q < 2; ++q) {
+    if (!p.tiles[q]) continue;
+    const Rows& r = q ? xr : gr;
+    const __nv_bfloat16* terms = q ? v3 : low3;
+    if ((rc = map_rows(&p.tm_rows[q], r.p, T, p.cols[q], r.stride, 64)) != MTPC_OK || (rc = map_rows(&p.tm_rows_each[q], r.p, T, p.cols[q], r.stride, 1)) != MTPC_OK ||
+        (rc = map_rows(&p.tm_terms[q], terms, T, 3 * k16, 3 * k16, 64)) != MTPC_OK || (rc = map_rows(&p.tm_terms_each[q], terms, T, 3 * k16, 3 * k16, 1)) != MTPC_OK)
+      return rc;
+  }
+  p.stage_bytes = kABytes + ceil_div(3 * k16, 64) * static_cast<int>(kMnBoxBytes);
+  p.stages = stages_of(p.stage_bytes);
+  const size_t smem = kControl + static_cast<size_t>(p.stages) * p.stage_bytes;
+  launch_kernel(adaptor_present_kernel, ceil_div(p.blocks, 32), kPresentThreads, static_cast<size_t>(S) * 4, st, true, row_adaptor, T, S, present);
+  auto* kernel = k16 == 16 ? adaptor_grad_kernel<16> : k16 == 32 ? adaptor_grad_kernel<32> : k16 == 48 ? adaptor_grad_kernel<48> : adaptor_grad_kernel<64>;
+  const long long items = static_cast<long long>(p.tiles[0] + p.tiles[1]) * S * p.splits;
+  launch_kernel(kernel, static_cast<int>(std::min<long long>(items, kSms)), kGradThreads, smem, st, true, p);
+  if (p.splits > 1) {
+    const long long quads = static_cast<long long>(S) * (p.tiles[0] + p.tiles[1]) * kBlockM * (k16 / 4);
+    launch_kernel(adaptor_grad_join_kernel, ceil_div(quads, 256), 256, 0, st, true, p, k16);
+  }
+  return check_launch();
+}
+
+}  // extern "C"

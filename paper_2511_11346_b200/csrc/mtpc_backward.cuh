@@ -1075,7 +1075,6 @@ struct PlainGemmParams {
   uint64_t wait_limit_ns;   // limit of every pipeline wait
 };
 constexpr int kPlainTileN = 256;
-constexpr uint32_t kMnBoxBytes = 64 * kBlockK * 2;   // one 64 x 64 bf16 box: 8 KB
 // Scratch of a split launch: parts of at most kSplitParts 128 x 256 tiles (three rounds of a 148-SM device).
 constexpr int kSplitParts = 444;
 constexpr size_t kSplitPartBytes = static_cast<size_t>(kBlockM) * kPlainTileN * sizeof(float);

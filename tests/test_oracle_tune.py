@@ -65,3 +65,35 @@ def test_preference_gradient_by_differences(smoothing):
         down[t] -= 1e-6
         assert abs((call(up)[0] - call(down)[0]) / 2e-6 - grad[t]) < 1e-8
     assert np.allclose(tu.preference_loss(logp, logp, offsets, 0.7)[0], np.log(2))
+
+
+def test_adapted_projection_is_the_composed_matrix():
+    rng = np.random.default_rng(7)
+    T, d, m, k, S = 6, 5, 4, 2, 3
+    x, W, A, B = (rng.standard_normal(s) for s in ((T, d), (m, d), (S, m, k), (S, k, d)))
+    scale, which = rng.random(S), np.array([0, 2, -1, 2, 1, 3])
+    out, low, size, _ = tu.adapted_projection(x, W, A, B, scale, which)
+    for t in (0, 1, 3, 4):
+        i = which[t]
+        assert np.allclose(out[t], (W + scale[i] * A[i] @ B[i]) @ x[t]) and np.allclose(A[i] @ low[t], out[t] - W @ x[t])
+    assert np.allclose(out[2], W @ x[2]) and not low[2].any() and np.isnan(out[5]).all() and (np.abs(out[:5]) <= size[:5]).all()
+    other = rng.standard_normal((T, d))
+    assert np.allclose(tu.adapted_projection(x, W, A, B, None, None, other)[0], x @ W.T + other @ (A[0] @ B[0]).T)
+
+
+def test_adapted_projection_gradients_by_differences():
+    rng = np.random.default_rng(8)
+    T, d, m, k, S = 5, 4, 3, 2, 2
+    given = dict(x=rng.standard_normal((T, d)), x_low=rng.standard_normal((T, d)), A=rng.standard_normal((S, m, k)), B=rng.standard_normal((S, k, d)))
+    W, scale, which, g = rng.standard_normal((m, d)), rng.random(S), np.array([1, -1, 0, 1, 1]), rng.standard_normal((T, m))
+    value = lambda v: float((tu.adapted_projection(v["x"], W, v["A"], v["B"], scale, which, v["x_low"])[0] * g).sum())  # noqa: E731
+    low = tu.adapted_projection(given["x"], W, given["A"], given["B"], scale, which, given["x_low"])[1]
+    got = tu.adapted_projection_grad(given["x_low"], W, given["A"], given["B"], scale, which, low, g)
+    assert np.allclose(got["d_x"], got["d_x_base"] + got["d_x_low"])
+    for name, grad in (("x", "d_x_base"), ("x_low", "d_x_low"), ("A", "dA"), ("B", "dB")):
+        for at in np.ndindex(given[name].shape):
+            up, down = dict(given), dict(given)
+            up[name], down[name] = given[name].copy(), given[name].copy()
+            up[name][at] += 1e-6
+            down[name][at] -= 1e-6
+            assert abs((value(up) - value(down)) / 2e-6 - got[grad][at]) < 1e-7
