@@ -124,11 +124,12 @@ struct Rows {
 // Whether tensor maps can address rows as they lie.
 bool mappable(const void* p, int64_t stride, int64_t rows, int cols) { return aligned(p, 16) && (rows <= 1 || (stride % 8 == 0 && stride >= cols)); }
 
-// Copies of what is not mappable, in one launch; `fine`: all of it was.
+// Copies of what is not mappable, up to four of them in one launch.
 struct Copier {
   CopyParams c;
   int n = 0;
-  Copier() { memset(&c, 0, sizeof(c)); }
+  cudaStream_t st;
+  explicit Copier(cudaStream_t stream) : st(stream) { memset(&c, 0, sizeof(c)); }
   Rows rows(const void* p, int64_t stride, int64_t rows, int cols, void* to) {
     Rows r{static_cast<const __nv_bfloat16*>(p), rows > 1 ? stride : up8(cols)};
     if (p == nullptr || mappable(p, stride, rows, cols)) return r;
@@ -141,8 +142,9 @@ struct Copier {
     m.pitch = up8(cols);
     ++n;
     c.begin[n] = c.begin[n - 1] + rows * (m.pitch / 8);
-    if (n == 4) launch_now();
-    return Rows{m.dst, m.pitch};
+    r = Rows{m.dst, m.pitch};
+    if (n == 4) launch_now();           // (which clears m)
+    return r;
   }
   void launch_now() {
     if (n == 0) return;
@@ -151,7 +153,6 @@ struct Copier {
     memset(&c, 0, sizeof(c));
     n = 0;
   }
-  cudaStream_t st = nullptr;
 };
 
 constexpr int kMaxDevices = 64;
@@ -338,8 +339,7 @@ int mtpc_adapted_projection(const void* x, int64_t x_stride, const void* x_low, 
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   unsigned* status = out_status ? out_status : reinterpret_cast<unsigned*>(ws + plan.off_status);
-  Copier copy;
-  copy.st = st;
+  Copier copy(st);
   const Rows xr = copy.rows(x, x_stride, T, d, ws + plan.off_x), Wr = copy.rows(W, W_stride, m, d, ws + plan.off_W);
   if (few) {
     copy.launch_now();
@@ -409,8 +409,7 @@ int mtpc_adapted_projection_backward(const void* x_low, int64_t x_low_stride, co
   }
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   unsigned* status = out_status ? out_status : reinterpret_cast<unsigned*>(ws + plan.off_status);
-  Copier copy;
-  copy.st = st;
+  Copier copy(st);
   const Rows gr = copy.rows(d_out, d_out_stride, T, m, ws + plan.off_g);
   const Rows Ar = copy.rows(A, k, static_cast<int64_t>(S) * m, k, ws + plan.off_A), Br = copy.rows(B, d, static_cast<int64_t>(S) * k, d, ws + plan.off_B);
   const Rows Wr = d_x ? copy.rows(W, W_stride, m, d, ws + plan.off_W) : Rows{nullptr, 0};
