@@ -106,7 +106,7 @@ void plan_backward(int T, int d, int m, int k, int S, bool copies, BackwardPlan*
   p->off_two = take(rows * pieces_of(k) * 128);
   p->off_low3 = take(rows * 3 * k16 * 2);
   p->off_v3 = take(rows * 3 * k16 * 2);
-  p->off_present = take(static_cast<size_t>(ceil_div(blocks, 32)) * S * 4);
+  p->off_present = take(static_cast<size_t>(ceil_div(blocks, 32)) * S * 8);
   p->off_grad = take(p->splits > 1 ? static_cast<size_t>(p->splits) * S * tiles * kBlockM * k16 * 4 : 0);
   p->off_x = take(copies ? rows * dp * 2 : 0);
   p->off_W = take(copies ? m * dp * 2 : 0);
@@ -173,8 +173,8 @@ int allow_shared_memory() {
   __atomic_store_n(&g_allowed[dev], 1, __ATOMIC_RELEASE);
   return MTPC_OK;
 }
-int stages_of(int stage_bytes, int ctas_per_sm = 1) {
-  return std::min(kMaxStages, static_cast<int>((kSmemLimit / ctas_per_sm - (ctas_per_sm > 1 ? 1024 : 0) - kControl) / stage_bytes));
+int stages_of(int stage_bytes, int ctas_per_sm = 1, int beside = 0) {
+  return std::min(kMaxStages, static_cast<int>((kSmemLimit / ctas_per_sm - (ctas_per_sm > 1 ? 1024 : 0) - kControl - beside) / stage_bytes));
 }
 
 // ---------------------------------------------------------------- launches
@@ -200,8 +200,12 @@ int launch_low(const Rows& rows, const Rows& factors, bool mn, const int* which,
   launch_kernel(mn ? adaptor_low_kernel<true> : adaptor_low_kernel<false>, std::min(p.tiles * p.chunks, 2 * kSms), kLowThreads, smem, st, true, p);
   return check_launch();
 }
-int launch_join(const LowJoinParams& p, cudaStream_t st) {
-  launch_kernel(adaptor_join_kernel, ceil_div(static_cast<long long>(p.T) * (p.k16 / 4), 256), 256, 0, st, true, p);
+int launch_join(LowJoinParams& p, cudaStream_t st) {
+  const int blocks = ceil_div(static_cast<long long>(p.T) * (p.k16 / 4), kJoinThreads);
+  p.sum_blocks = p.part ? blocks : 0;
+  p.given_blocks = p.given ? blocks : 0;
+  const int present_blocks = p.present ? ceil_div(p.T, 32 * 64) : 0;
+  launch_kernel(adaptor_join_kernel, p.sum_blocks + p.given_blocks + present_blocks, kJoinThreads, p.present ? static_cast<size_t>(p.S) * 4 : 0, st, true, p);
   return check_launch();
 }
 
@@ -218,8 +222,9 @@ int launch_gemm(AdaptedParams& p, const Rows& a, const Rows& b, const __nv_bfloa
   p.m_units = ceil_div(p.T, kBlockM * CTAS);
   p.n_tiles = ceil_div(p.N, TN);
   p.stage_bytes = kABytes + kBCols * kBlockK * 2;
-  p.stages = stages_of(p.stage_bytes);
-  const size_t smem = kControl + static_cast<size_t>(p.stages) * p.stage_bytes;
+  const int staging = p.store == 2 ? kStoreBytes : 0;
+  p.stages = stages_of(p.stage_bytes, 1, staging);
+  const size_t smem = kControl + staging + static_cast<size_t>(p.stages) * p.stage_bytes;
   const int workers = std::min(p.m_units * p.n_tiles, kSms / CTAS);
   launch_clusters(adapted_gemm_kernel<B_MN, TN, CTAS>, CTAS, workers * CTAS, kAdaptedThreads, smem, st, true, p);
   return check_launch();
@@ -293,7 +298,7 @@ int launch_few_rows(const Rows& x, const Rows& W, const void* x_low, int64_t x_l
   while (p.split < 8 && p.split * 2 <= p.kblocks && tiles * p.split < 2 * kSms - 64) p.split *= 2;
   p.stage_bytes = kABytes + p.tokens * kBlockK * 2;
   p.stages = stages_of(p.stage_bytes, 2);
-  p.wide = k % 8 == 0 && aligned(A, 16);
+  p.wide = k % 8 == 0 && aligned(A, 16) && aligned(low, 16);
   const size_t smem = kControl + static_cast<size_t>(p.stages) * p.stage_bytes;
   launch_clusters(adapted_rows_kernel, p.split, tiles * p.split, kRowsThreads, smem, st, true, p);
   return check_launch();
@@ -429,32 +434,34 @@ int mtpc_adapted_projection_backward(const void* x_low, int64_t x_low_stride, co
   __nv_bfloat16* low3 = reinterpret_cast<__nv_bfloat16*>(ws + plan.off_low3);
   __nv_bfloat16* v3 = reinterpret_cast<__nv_bfloat16*>(ws + plan.off_v3);
   if (d_x || d_x_low || dB) {
-    float* part = reinterpret_cast<float*>(ws + plan.off_part);
-    if ((rc = launch_low(gr, Ar, true, row_adaptor, T, m, k, S, part, status, st)) != MTPC_OK) return rc;
+    j.part = reinterpret_cast<float*>(ws + plan.off_part);
+    if ((rc = launch_low(gr, Ar, true, row_adaptor, T, m, k, S, reinterpret_cast<float*>(ws + plan.off_part), status, st)) != MTPC_OK) return rc;
     j.scale = scale;
-    j.part = part;
     j.two = d_x || d_x_low ? two : nullptr;
     j.three = dB ? v3 : nullptr;
     j.chunks = chunks_of(m);
+  }
+  if (dA) {
+    j.given = low;
+    j.given_three = low3;
+  }
+  if (dA || dB) {
+    j.present = reinterpret_cast<uint32_t*>(ws + plan.off_present);
+    j.whole = j.present + static_cast<size_t>(ceil_div(T, 32 * 64)) * S;
+  }
+  if (j.part || j.given) {
     if ((rc = launch_join(j, st)) != MTPC_OK) return rc;
   }
   if (d_x && (rc = launch_product(gr, Wr, two, Br, true, row_adaptor, T, m, d, k, S, true, d_x_low == nullptr, d_x, d_x_stride, status, st)) != MTPC_OK) return rc;
   if (d_x_low && (rc = launch_product(gr, Rows{gr.p, gr.stride}, two, Br, true, row_adaptor, T, m, d, k, S, false, true, d_x_low, d_x_low_stride, status, st)) != MTPC_OK)
     return rc;
   if (!dA && !dB) return MTPC_OK;
-  if (dA) {
-    j.scale = nullptr;
-    j.part = nullptr;
-    j.given = low;
-    j.two = nullptr;
-    j.three = low3;
-    if ((rc = launch_join(j, st)) != MTPC_OK) return rc;
-  }
-  uint32_t* present = reinterpret_cast<uint32_t*>(ws + plan.off_present);
   GradParams p;
   memset(&p, 0, sizeof(p));
   p.which = row_adaptor;
-  p.present = present;
+  p.present = j.present;
+  p.whole = j.whole;
+  p.after_join = !d_x && !d_x_low;
   p.out[0] = dA;
   p.out[1] = dB;
   p.part = reinterpret_cast<float*>(ws + plan.off_grad);
@@ -481,7 +488,6 @@ int mtpc_adapted_projection_backward(const void* x_low, int64_t x_low_stride, co
   p.stage_bytes = kABytes + ceil_div(3 * k16, 64) * static_cast<int>(kMnBoxBytes);
   p.stages = stages_of(p.stage_bytes);
   const size_t smem = kControl + static_cast<size_t>(p.stages) * p.stage_bytes;
-  launch_kernel(adaptor_present_kernel, ceil_div(p.blocks, 32), kPresentThreads, static_cast<size_t>(S) * 4, st, true, row_adaptor, T, S, present);
   auto* kernel = k16 == 16 ? adaptor_grad_kernel<16> : k16 == 32 ? adaptor_grad_kernel<32> : k16 == 48 ? adaptor_grad_kernel<48> : adaptor_grad_kernel<64>;
   const long long items = static_cast<long long>(p.tiles[0] + p.tiles[1]) * S * p.splits;
   launch_kernel(kernel, static_cast<int>(std::min<long long>(items, kSms)), kGradThreads, smem, st, true, p);

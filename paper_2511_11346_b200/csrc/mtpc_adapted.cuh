@@ -303,32 +303,63 @@ __device__ __forceinline__ void split_terms(float x, __nv_bfloat16& hi, __nv_bfl
   lo = __float2bfloat16_rn(r - __bfloat162float(mid));
 }
 
+// Sums of chunks, scaled, as low or v and its terms; the terms of values that are given; and which blocks of 64 rows have an adaptor's rows. One launch: blocks
+// [0, sum_blocks), then given_blocks, then a block for every 32 blocks of rows.
 struct LowJoinParams {
   const int* which;
   const float* scale;                   // [S] or NULL: ones
-  const float* part;                    // [chunks][T][k16], or NULL: the values are given
-  const float* given;                   // [T, k]: used instead of the chunks' sums, not scaled
+  const float* part;                    // [chunks][T][k16]
   float* low;                           // [T, k] or NULL
   __nv_bfloat16* two;                   // [T][pieces][64] or NULL
   __nv_bfloat16* three;                 // [T][3][k16] or NULL
+  const float* given;                   // [T, k]
+  __nv_bfloat16* given_three;           // [T][3][k16]
+  uint32_t *present, *whole;            // bit b % 32 of [(b / 32) S + i]: block b has rows of i, and no others
   unsigned* status;                     // or NULL
   int T, S, k, k16, chunks, pieces;
+  int sum_blocks, given_blocks;
 };
-__global__ void __launch_bounds__(256) adaptor_join_kernel(const LowJoinParams p) {
+constexpr int kJoinThreads = 256;
+__device__ __forceinline__ void present_blocks(const LowJoinParams& p, int group, uint32_t* words) {
+  __shared__ uint32_t mixed;
+  for (int i = threadIdx.x; i < p.S; i += kJoinThreads) words[i] = 0;
+  if (threadIdx.x == 0) mixed = 0;
+  __syncthreads();
+  for (int r = threadIdx.x; r < 32 * 64; r += kJoinThreads) {
+    const long long t = static_cast<long long>(group) * (32 * 64) + r;
+    if (t >= p.T) continue;
+    const int i = adaptor_of(p.which, p.S, static_cast<int>(t), p.T), head = adaptor_of(p.which, p.S, static_cast<int>(t) - r % 64, p.T);
+    if (i >= 0) atomicOr(&words[i], 1u << (r / 64));
+    if (i != head) atomicOr(&mixed, 1u << (r / 64));
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < p.S; i += kJoinThreads) {
+    p.present[static_cast<size_t>(group) * p.S + i] = words[i];
+    p.whole[static_cast<size_t>(group) * p.S + i] = words[i] & ~mixed;
+  }
+}
+__global__ void __launch_bounds__(kJoinThreads) adaptor_join_kernel(const LowJoinParams p) {
+  extern __shared__ uint32_t words[];
+  grid_launch_dependents();             // (no gate: what is behind waits before it reads what is written here)
   grid_dependency_wait();
-  grid_launch_dependents();
-  const long long at = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
+  const int block = blockIdx.x;
+  if (block >= p.sum_blocks + p.given_blocks) {
+    present_blocks(p, block - p.sum_blocks - p.given_blocks, words);
+    return;
+  }
+  const bool given = block >= p.sum_blocks;
+  const long long at = static_cast<long long>(given ? block - p.sum_blocks : block) * kJoinThreads + threadIdx.x;
   const int quads = p.k16 / 4;
   const int t = static_cast<int>(at / quads), j0 = static_cast<int>(at - static_cast<long long>(t) * quads) * 4;
   if (t >= p.T) return;
   const int i = adaptor_of(p.which, p.S, t, p.T);
   float x[4] = {0.f, 0.f, 0.f, 0.f};
-  if (p.given != nullptr) {
+  if (given) {
 #pragma unroll
     for (int q = 0; q < 4; ++q)
       if (i >= 0 && j0 + q < p.k) x[q] = p.given[static_cast<size_t>(t) * p.k + j0 + q];
   } else if (i >= 0) {
-#pragma unroll 4
+#pragma unroll 8
     for (int c = 0; c < p.chunks; ++c) {
       const float4 y = *reinterpret_cast<const float4*>(p.part + (static_cast<size_t>(c) * p.T + t) * p.k16 + j0);
       x[0] += y.x, x[1] += y.y, x[2] += y.z, x[3] += y.w;
@@ -339,7 +370,7 @@ __global__ void __launch_bounds__(256) adaptor_join_kernel(const LowJoinParams p
   }
   const bool refused = adaptor_refused(p.which, p.S, t);
   if (refused && p.status != nullptr && j0 == 0) atomicOr(p.status, kStatusBadAdaptor);
-  if (p.low != nullptr) {
+  if (!given && p.low != nullptr) {
     float* dst = p.low + static_cast<size_t>(t) * p.k + j0;
 #pragma unroll
     for (int q = 0; q < 4; ++q)
@@ -349,13 +380,14 @@ __global__ void __launch_bounds__(256) adaptor_join_kernel(const LowJoinParams p
 #pragma unroll
   for (int q = 0; q < 4; ++q) split_terms(j0 + q < p.k ? x[q] : 0.f, h[q], m[q], l[q]);
   const uint2 hv = *reinterpret_cast<const uint2*>(h), mv = *reinterpret_cast<const uint2*>(m), lv = *reinterpret_cast<const uint2*>(l);
-  if (p.two != nullptr) {
+  if (!given && p.two != nullptr) {
     __nv_bfloat16* dst = p.two + (static_cast<size_t>(t) * p.pieces + j0 / kPieceRank) * 64 + j0 % kPieceRank;
     *reinterpret_cast<uint2*>(dst) = hv;
     *reinterpret_cast<uint2*>(dst + kPieceRank) = mv;
   }
-  if (p.three != nullptr) {
-    __nv_bfloat16* dst = p.three + static_cast<size_t>(t) * 3 * p.k16 + j0;
+  __nv_bfloat16* three = given ? p.given_three : p.three;
+  if (three != nullptr) {
+    __nv_bfloat16* dst = three + static_cast<size_t>(t) * 3 * p.k16 + j0;
     *reinterpret_cast<uint2*>(dst) = hv;
     *reinterpret_cast<uint2*>(dst + p.k16) = mv;
     *reinterpret_cast<uint2*>(dst + 2 * p.k16) = lv;
@@ -380,19 +412,25 @@ struct AdaptedParams {
 };
 constexpr int kAdaptedThreads = 320;
 
-// Columns [col, col + 32) of a row of out, x in fp32.
-__device__ __forceinline__ void store_row32(const AdaptedParams& p, __nv_bfloat16* row, int col, const uint32_t (&x)[32]) {
+// Thirty-two columns of 32 rows from `col` on, a row a lane (`rows` of them exist), x in fp32. Rows that allow no vectors are written a row at a time, its columns
+// side by side, by way of `stage` (2005 x 2003: each lane its own row, two bytes at a time, the kernel took 51 us, so 11).
+constexpr int kStorePitch = 17;                   // words of a staged row: 32 columns and one over, so that lanes meet no bank twice
+constexpr int kStoreBytes = 8 * 32 * kStorePitch * 4;
+__device__ __forceinline__ void store_rows32(const AdaptedParams& p, __nv_bfloat16* first, int lane, int rows, int col, const uint32_t (&x)[32], uint32_t* stage) {
   uint32_t y[16];
 #pragma unroll
   for (int q = 0; q < 16; ++q) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(__uint_as_float(x[2 * q]), __uint_as_float(x[2 * q + 1]));
     y[q] = *reinterpret_cast<const uint32_t*>(&v);
   }
-  __nv_bfloat16* dst = row + col;
-  if (col + 32 <= p.N && p.store == 32) {
-    st_global_v8_b32(dst, y);
-    st_global_v8_b32(dst + 16, y + 8);
-  } else if (p.store >= 16) {
+  if (p.store >= 16) {
+    if (lane >= rows) return;
+    __nv_bfloat16* dst = first + lane * p.out_stride + col;
+    if (col + 32 <= p.N && p.store == 32) {
+      st_global_v8_b32(dst, y);
+      st_global_v8_b32(dst + 16, y + 8);
+      return;
+    }
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       if (col + 8 * q + 8 <= p.N) {
@@ -403,11 +441,18 @@ __device__ __forceinline__ void store_row32(const AdaptedParams& p, __nv_bfloat1
           if (col + 8 * q + e < p.N) dst[8 * q + e] = __ushort_as_bfloat16(static_cast<unsigned short>(y[4 * q + e / 2] >> (16 * (e & 1))));
       }
     }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 32; ++e)
-      if (col + e < p.N) dst[e] = __ushort_as_bfloat16(static_cast<unsigned short>(y[e / 2] >> (16 * (e & 1))));
+    return;
   }
+#pragma unroll
+  for (int q = 0; q < 16; ++q) stage[lane * kStorePitch + q] = y[q];
+  __syncwarp();
+  if (col + lane < p.N) {
+    __nv_bfloat16* dst = first + col + lane;
+#pragma unroll 8
+    for (int r = 0; r < rows; ++r)
+      dst[r * p.out_stride] = __ushort_as_bfloat16(static_cast<unsigned short>(stage[r * kStorePitch + lane / 2] >> (16 * (lane & 1))));
+  }
+  __syncwarp();
 }
 
 template <bool B_MN, int TN, int CTAS>
@@ -458,8 +503,8 @@ __global__ void __launch_bounds__(kAdaptedThreads, 1) adapted_gemm_kernel(const 
   if (CTAS == 2) cluster_sync_all();   // the peer's barriers are initialised before anything arrives on them
   tc_fence_after();
   const uint32_t tmem_base = warp_uniform(ctl->tmem_base);
-  grid_dependency_wait();
-  grid_launch_dependents();
+  // Ahead of this kernel are adaptor_low_kernel, a gate, and adaptor_join_kernel, which is none: rows and W are there, the terms of low are waited for where they
+  // are read. This kernel is a gate again: what is behind it starts when the epilogue warps have waited.
   TileAdaptors<kWords> ta;
   int adaptor = 0;
   uint32_t off[kWords];
@@ -471,6 +516,7 @@ __global__ void __launch_bounds__(kAdaptedThreads, 1) adapted_gemm_kernel(const 
     const uint32_t own_full = smem_u32(&ctl->full[0]), empty0 = smem_u32(&ctl->empty[0]);
     const uint32_t full0 = CTAS == 2 ? warp_uniform(cluster_map_shared(own_full, 0)) : own_full;   // the leader's barriers
     uint32_t full = 0, a_dst = 0;
+    bool waited = false;
     auto begin = [&]() {
       ok = bounded_wait_all(empty0 + 8 * stage, phase ^ 1u, ctl, p);
       if (!ok) return false;
@@ -504,6 +550,8 @@ __global__ void __launch_bounds__(kAdaptedThreads, 1) adapted_gemm_kernel(const 
       }
       if (p.pieces == 0) continue;
       ta.load(p.which, p.S, mt * CTAS * kBlockM, p.T, lane);
+      if (!waited) grid_dependency_wait();
+      waited = true;
       while (ok && ta.next(adaptor, off)) {
         for (int q = 0; q < p.pieces; ++q) {
           if (!begin()) break;
@@ -588,7 +636,10 @@ __global__ void __launch_bounds__(kAdaptedThreads, 1) adapted_gemm_kernel(const 
   } else {
     const int quarter = warp & 3, sub = (warp - 2) >> 2;
     const uint32_t lane_base = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16);
+    uint32_t* stage = reinterpret_cast<uint32_t*>(ctl + 1) + (warp - 2) * (32 * kStorePitch);        // (there with p.store == 2 only)
     uint32_t use = 0;
+    grid_dependency_wait();
+    grid_launch_dependents();
     for (int item = first_item; item < items; item += item_step, ++use) {
       const int mt = item / p.n_tiles, nt = item - mt * p.n_tiles;
       const uint32_t slot = use % kSlots;
@@ -599,7 +650,7 @@ __global__ void __launch_bounds__(kAdaptedThreads, 1) adapted_gemm_kernel(const 
       if (!bounded_wait_warp(smem_u32(&ctl->tfull[slot]), (use / kSlots) & 1u, ctl, p.status, lane)) break;
       tc_fence_after();
       const uint32_t tcol = lane_base + slot * TN;
-      __nv_bfloat16* out = p.out + (inside ? row : 0) * p.out_stride;
+      __nv_bfloat16* out = p.out + (row - lane) * p.out_stride;
       const int batches = (min(TN, p.N - nt * TN) + 31) / 32;
       for (int b = sub; b < batches; b += 2) {
         uint32_t x[32];
@@ -609,7 +660,8 @@ __global__ void __launch_bounds__(kAdaptedThreads, 1) adapted_gemm_kernel(const 
 #pragma unroll
           for (int q = 0; q < 32; ++q) x[q] = refused ? 0x7fffffffu : 0u;
         }
-        if (inside) store_row32(p, out, nt * TN + b * 32, x);
+        store_rows32(p, out, lane, min(32, p.T - (row - lane)), nt * TN + b * 32, x, stage);
+        __syncwarp();
       }
       tc_fence_before();
       __syncwarp();
@@ -704,9 +756,46 @@ struct RowsParams {
   uint64_t wait_limit_ns;
   int T, S, N, k, tokens;               // tokens: T rounded up to 16
   int kblocks, split, stages, stage_bytes;
-  int wide;                             // rows of A are vectors of eight elements
+  int wide;                             // rows of A and of low are vectors of eight elements
 };
 constexpr int kRowsThreads = 192;
+constexpr int kRowsAhead = 16;                    // rows of a CTA whose adaptors' part is formed while W is on its way
+// The adaptors' part of column n of rows t, t + split, t + 2 split, t + 3 split (those that exist).
+__device__ __forceinline__ void rows_adaptors(const RowsParams& p, int t, int n, float* y) {
+  int i[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    i[q] = n < p.N ? adaptor_of(p.which, p.S, t + q * p.split, p.T) : -1;
+    y[q] = 0.f;
+  }
+  if (p.wide) {
+    for (int j = 0; j < p.k; j += 8) {
+      Raw<__nv_bfloat16, 8> a[4];
+      float4 l[4][2];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        if (i[q] < 0) continue;
+        a[q].load(p.A + (static_cast<size_t>(i[q]) * p.N + n) * p.k + j);
+        const float4* low = reinterpret_cast<const float4*>(p.low + static_cast<size_t>(t + q * p.split) * p.k + j);
+        l[q][0] = low[0], l[q][1] = low[1];
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        if (i[q] < 0) continue;
+        const float v[8] = {l[q][0].x, l[q][0].y, l[q][0].z, l[q][0].w, l[q][1].x, l[q][1].y, l[q][1].z, l[q][1].w};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[q] = fmaf(a[q].value(e), v[e], y[q]);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if (i[q] < 0) continue;
+      const __nv_bfloat16* a = p.A + (static_cast<size_t>(i[q]) * p.N + n) * p.k;
+      for (int j = 0; j < p.k; ++j) y[q] = fmaf(to_f32(a[j]), p.low[static_cast<size_t>(t + q * p.split) * p.k + j], y[q]);
+    }
+  }
+}
 __global__ void __launch_bounds__(kRowsThreads) adapted_rows_kernel(const __grid_constant__ RowsParams p) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw_addr = smem_u32(smem_raw);
@@ -739,6 +828,7 @@ __global__ void __launch_bounds__(kRowsThreads) adapted_rows_kernel(const __grid
   tc_fence_after();
   const uint32_t tmem_base = warp_uniform(ctl->tmem_base);
   const uint32_t full0 = smem_u32(&ctl->full[0]), empty0 = smem_u32(&ctl->empty[0]);
+  float part[kRowsAhead];               // the adaptors' part of this CTA's rows
   // sums [tokens][128] fp32, over the stages once these have been multiplied
   float* sums = reinterpret_cast<float*>(smem_raw + (tiles_addr - raw_addr));
 
@@ -780,6 +870,8 @@ __global__ void __launch_bounds__(kRowsThreads) adapted_rows_kernel(const __grid
     const uint32_t lane_base = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16);
     grid_dependency_wait();
     grid_launch_dependents();
+#pragma unroll
+    for (int q = 0; q < kRowsAhead; q += 4) rows_adaptors(p, rank + q * p.split, tile * kBlockM + quarter * 32 + lane, part + q);
     if (bounded_wait_warp(smem_u32(&ctl->tfull[0]), 0, ctl, p.status, lane)) {
       tc_fence_after();
       for (int b = 0; b < p.tokens / 16; ++b) {
@@ -796,27 +888,19 @@ __global__ void __launch_bounds__(kRowsThreads) adapted_rows_kernel(const __grid
   if (warp >= 2) {
     const int m = (warp & 3) * 32 + lane, n = tile * kBlockM + m;
     const uint32_t own = smem_u32(sums) + 4u * m;
-    for (int t = rank; t < p.T; t += p.split) {
-      float y = 0.f;
-      for (int r = 0; r < p.split; ++r) y += ld_cluster_f32(cluster_map_shared(own + 4u * kBlockM * t, r));
-      const int i = adaptor_of(p.which, p.S, t, p.T);
-      if (n < p.N) {
-        if (i >= 0) {
-          const __nv_bfloat16* a = p.A + (static_cast<size_t>(i) * p.N + n) * p.k;
-          const float* low = p.low + static_cast<size_t>(t) * p.k;
-          if (p.wide) {
-            for (int j = 0; j < p.k; j += 8) {
-              Raw<__nv_bfloat16, 8> av;
-              av.load(a + j);
+    auto finish = [&](int t, float y) {
+      if (t >= p.T) return;
+      float sum = 0.f;
+      for (int r = 0; r < p.split; ++r) sum += ld_cluster_f32(cluster_map_shared(own + 4u * kBlockM * t, r));
+      if (n < p.N) p.out[t * p.out_stride + n] = __float2bfloat16_rn(adaptor_refused(p.which, p.S, t) ? CUDART_NAN_F : sum + y);
+    };
 #pragma unroll
-              for (int e = 0; e < 8; ++e) y = fmaf(av.value(e), low[j + e], y);
-            }
-          } else {
-            for (int j = 0; j < p.k; ++j) y = fmaf(to_f32(a[j]), low[j], y);
-          }
-        }
-        p.out[t * p.out_stride + n] = adaptor_refused(p.which, p.S, t) ? __float2bfloat16_rn(CUDART_NAN_F) : __float2bfloat16_rn(y);
-      }
+    for (int q = 0; q < kRowsAhead; ++q) finish(rank + q * p.split, part[q]);
+    for (int t = rank + kRowsAhead * p.split; t < p.T; t += 4 * p.split) {
+      float more[4];
+      rows_adaptors(p, t, n, more);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) finish(t + q * p.split, more[q]);
     }
   }
   tc_fence_before();
@@ -831,36 +915,20 @@ __global__ void __launch_bounds__(kRowsThreads) adapted_rows_kernel(const __grid
 }
 
 // ---- gradients of the adaptors
-// Which blocks of 64 rows have a row of an adaptor: bit b % 32 of present[(b / 32) S + i].
-constexpr int kPresentThreads = 256;
-__global__ void __launch_bounds__(kPresentThreads) adaptor_present_kernel(const int* which, int T, int S, uint32_t* present) {
-  extern __shared__ uint32_t words[];
-  grid_dependency_wait();
-  grid_launch_dependents();
-  for (int i = threadIdx.x; i < S; i += kPresentThreads) words[i] = 0;
-  __syncthreads();
-  for (int r = threadIdx.x; r < 32 * 64; r += kPresentThreads) {
-    const long long t = static_cast<long long>(blockIdx.x) * (32 * 64) + r;
-    const int i = t < T ? adaptor_of(which, S, static_cast<int>(t), T) : -1;
-    if (i >= 0) atomicOr(&words[i], 1u << (r / 64));
-  }
-  __syncthreads();
-  for (int i = threadIdx.x; i < S; i += kPresentThreads) present[static_cast<size_t>(blockIdx.x) * S + i] = words[i];
-}
-
 // dA (product 0: rows g, terms of low) and dB (product 1: rows x', terms of v): 128 columns of the rows are the MMA's M, the 3 k16 terms its N, rows its K. An item is
 // one tile of columns of one adaptor over one of `splits` runs of row blocks; every eight blocks the accumulators are added to fp32 registers.
 struct GradParams {
   CUtensorMap tm_rows[2], tm_rows_each[2];       // [T, cols]    box 64 x 64, and 64 x 1
   CUtensorMap tm_terms[2], tm_terms_each[2];     // [T, 3 k16]   box 64 x 64, and 64 x 1
   const int* which;
-  const uint32_t* present;
+  const uint32_t *present, *whole;               // LowJoinParams
   float* out[2];                                 // dA [S, m, k], dB [S, k, d]; either may be NULL
   float* part;                                   // [splits][S][columns of both, whole tiles][k16], splits > 1
   unsigned* status;
   uint64_t wait_limit_ns;
   int T, S, k, cols[2], tiles[2];                // tiles of an absent product: 0
   int blocks, splits, stages, stage_bytes;
+  int after_join;
 };
 constexpr int kGradThreads = 192;
 
@@ -881,16 +949,22 @@ __device__ __forceinline__ GradItem grad_item(const GradParams& p, int item) {
 // The row blocks of an item that have rows of its adaptor, in order; a warp walks over them as a whole.
 struct BlockWalk {
   int block, end;
-  uint32_t word;
+  uint32_t word, alone;
+  __device__ __forceinline__ void look(const GradParams& p, const GradItem& g, int b) {
+    const size_t at = static_cast<size_t>(b >> 5) * p.S + g.adaptor;
+    word = p.present[at];
+    alone = p.whole[at];
+  }
   __device__ __forceinline__ void start(const GradParams& p, const GradItem& g) {
     block = static_cast<int>(static_cast<long long>(g.split) * p.blocks / p.splits) - 1;
     end = static_cast<int>(static_cast<long long>(g.split + 1) * p.blocks / p.splits);
-    word = block + 1 < end ? p.present[static_cast<size_t>((block + 1) >> 5) * p.S + g.adaptor] : 0;
+    word = alone = 0;
+    if (block + 1 < end) look(p, g, block + 1);
   }
   __device__ __forceinline__ bool next(const GradParams& p, const GradItem& g) {
     while (true) {
       if (++block >= end) return false;
-      if ((block & 31) == 0) word = p.present[static_cast<size_t>(block >> 5) * p.S + g.adaptor];
+      if ((block & 31) == 0) look(p, g, block);
       const uint32_t ahead = word >> (block & 31);
       if (ahead != 0) {
         block += __ffs(ahead) - 1;
@@ -899,6 +973,8 @@ struct BlockWalk {
       block |= 31;
     }
   }
+  // Whether all rows of the block are the adaptor's.
+  __device__ __forceinline__ bool whole() const { return alone >> (block & 31) & 1; }
 };
 
 template <int K16>
@@ -934,7 +1010,8 @@ __global__ void __launch_bounds__(kGradThreads, 1) adaptor_grad_kernel(const __g
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = warp_uniform(ctl->tmem_base);
-  grid_dependency_wait();
+  // The kernel ahead is a gate whatever was asked for, or the join itself (after_join): what the join wrote is there, and nothing here needs the product.
+  if (p.after_join) grid_dependency_wait();
   grid_launch_dependents();
   const uint32_t full0 = smem_u32(&ctl->full[0]), empty0 = smem_u32(&ctl->empty[0]);
 
@@ -949,21 +1026,20 @@ __global__ void __launch_bounds__(kGradThreads, 1) adaptor_grad_kernel(const __g
       walk.start(p, g);
       while (walk.next(p, g)) {
         const int t0 = walk.block * 64;
-        // lanes below 16 have four rows each; a row of another adaptor (or none) is read past the last: zeros
-        int at[4];
-        bool foreign = false;
+        const bool whole = walk.whole();
+        int at[4] = {0, 0, 0, 0};
+        if (!whole) {                   // lanes below 16 have four rows each; a row of another adaptor (or none) is read past the last: zeros
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int t = t0 + 4 * (lane & 15) + q;
-          at[q] = adaptor_of(p.which, p.S, t, p.T) == g.adaptor ? t : p.T;
-          foreign |= at[q] == p.T && t < p.T;
+          for (int q = 0; q < 4; ++q) {
+            const int t = t0 + 4 * (lane & 15) + q;
+            at[q] = adaptor_of(p.which, p.S, t, p.T) == g.adaptor ? t : p.T;
+          }
         }
-        foreign = __any_sync(0xffffffffu, foreign);
         if (!bounded_wait_all(empty0 + 8 * stage, phase ^ 1u, ctl, p)) { ok = false; break; }
         const uint32_t full = full0 + 8 * stage, dst = tiles_addr + stage * p.stage_bytes;
         mbar_arrive_expect_tx(lead, full, kABytes + kTermBoxes * kMnBoxBytes);
         __syncwarp();
-        if (!foreign) {
+        if (whole) {
 #pragma unroll
           for (int q = 0; q < 2; ++q) tma_load_2d(lead, dst + q * kMnBoxBytes, rows, full, g.tile * kBlockM + q * 64, t0);
 #pragma unroll
@@ -1070,6 +1146,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) adaptor_grad_kernel(const __g
       }
     }
   }
+  grid_dependency_wait();               // so that the end of this grid is that of all before it
   tc_fence_before();
   __syncthreads();
   if (warp == 1) {
