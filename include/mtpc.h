@@ -560,7 +560,7 @@ int mtpc_destroy_gradient_list(mtpc_gradient_list* list);
  *        adaptor are fastest beside each other, as those of a request are; any order works. What one adaptor's factors hold does not
  *        reach rows of another, infinities and NaN included.
  *   out  dev [T, m] bf16, not overlapping an input;  out_low dev [T, k] fp32, adjacent, or NULL: low, which the gradient of A needs (0 without adaptor).
- *   workspace dev, 256-byte aligned, >= mtpc_adapted_projection_workspace_bytes(T, d, m, k, S, aligned_rows). aligned_rows != 0: every operand starts on 16
+ *   workspace dev, 256-byte aligned, >= mtpc_adapted_projection_workspace_bytes(T, d, m, k, S, aligned_rows) (0 bytes: it may be NULL). aligned_rows != 0: every operand starts on 16
  *        bytes, with strides, k and d that are multiples of eight elements and strides >= d; 0: any, of which the call makes copies.
  *   out_status as for mtpc_embed.
  * Products accumulate in fp32; low is held to 16 bits or more for its product with A, and out is rounded once.
@@ -610,7 +610,7 @@ int mtpc_dropout(const void* x, int64_t x_stride, int32_t x_dtype, const void* r
  *   offsets dev int32 [S + 1], not decreasing, within [0, T]; otherwise MTPC_STATUS_BAD_OFFSET is or-ed into out_status (dev uint32 or NULL), the loss is NaN,
  *           and what d_logp holds is not defined. A sequence may be empty.
  *   mask    dev [T] bytes or NULL: positions with 0 count nowhere, whatever their values are (infinities and NaN too).
- *   workspace dev, 256-byte aligned, >= mtpc_objective_workspace_bytes(T, S).
+ *   workspace dev, 256-byte aligned, >= mtpc_objective_workspace_bytes(T, S); small calls need none (0 bytes: it may be NULL).
  * 0 <= T <= 2^30, 1 <= S <= 2^20 (MTPC_ERR_UNSUPPORTED beyond). Differences of log-likelihoods and sums are fp64.
  *
  * mtpc_policy_loss: the average over the valid positions (by_sequence != 0: over every sequence's valid positions and then over the S sequences, those

@@ -387,11 +387,12 @@ _dtype_codes = None
 
 def _dtypes() -> dict:
     """What the calls look up in torch, once (an import statement in every call costs a tenth of a small one)."""
-    global _dtype_codes, _current_device, _raw_stream, _int32, _int64, _float32, _bfloat16, _bool, _uint8
+    global _dtype_codes, _current_device, _raw_stream, _int32, _int64, _float32, _bfloat16, _bool, _uint8, _empty
     if _dtype_codes is None:
         import torch
         _current_device, _int32, _float32 = torch._C._cuda_getDevice, torch.int32, torch.float32
         _int64, _bfloat16, _bool, _uint8 = torch.int64, torch.bfloat16, torch.bool, torch.uint8
+        _empty = torch.empty
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
         _dtype_codes = {torch.float32: MTPC_F32, torch.bfloat16: MTPC_BF16}
     return _dtype_codes
@@ -466,6 +467,28 @@ def _scratch(what: str, workspace, need: int, device: int, stream):
     if workspace.get_device() != device or not workspace.is_contiguous() or workspace.dtype is not torch.uint8:
         _refuse(what, f"workspace of {workspace.dtype} on {workspace.device}")
     return workspace
+
+
+def _flat(what: str, t, count: int, device: int, dtype) -> int:
+    """The address of `count` adjacent elements of a dtype on `device`; 0 for None."""
+    if t is None:
+        return 0
+    if t.numel() == count and t.dtype is dtype and t.get_device() == device and t.is_contiguous():
+        return t.data_ptr()
+    if t.dtype is not dtype:
+        _refuse(what, f"{t.dtype} where {dtype} is needed", ERR_UNSUPPORTED)
+    _refuse(what, f"{tuple(t.shape)} with strides {t.stride()} on {t.device} where {count} adjacent elements on device {device} are needed")
+
+
+def _workspace(what: str, workspace, need: int, device: int, stream):
+    """(address, bytes) of _scratch, and what keeps it alive; a call that needs none makes none."""
+    if need == 0:
+        return 0, 0, None
+    if workspace is None and stream is None:
+        ws = _empty(need, dtype=_uint8, device=device)
+    else:
+        ws = _scratch(what, workspace, need, device, stream)
+    return ws.data_ptr(), ws.numel(), ws
 
 
 def mtpc_embed(tokens, table, out, scale: float = 1.0, out_status=None, stream=None) -> None:
@@ -549,19 +572,13 @@ def mtpc_residual_rmsnorm_backward(sum, weight, eps: float, d_out, d_sum, d_x, d
 def _factors(what: str, A, B, m: int, d: int, dev: int):
     """(S, k) of the adaptors' factors A [S, m, k] and B [S, k, d]."""
     shape = A.shape
-    if len(shape) != 3 or shape[1] != m or B.shape != (shape[0], shape[2], d):
-        _refuse(what, f"adaptors {tuple(A.shape)} and {tuple(B.shape)} where (S, {m}, k) and (S, k, {d}) are needed")
+    if (len(shape) == 3 and shape[1] == m and B.shape == (shape[0], shape[2], d) and A.dtype is _bfloat16 and B.dtype is _bfloat16 and A.is_contiguous() and
+            B.is_contiguous() and A.get_device() == dev and B.get_device() == dev):
+        return shape[0], shape[2]
     for t in (A, B):
         if t.dtype is not _bfloat16:
             _refuse(what, f"{t.dtype} where {_bfloat16} is needed", ERR_UNSUPPORTED)
-        if t.get_device() != dev or not t.is_contiguous():
-            _refuse(what, f"adaptors {tuple(t.shape)} with strides {t.stride()} on {t.device}")
-    return shape[0], shape[2]
-
-
-def _plain_rows(*rows) -> int:
-    """Whether tensor maps address matrices as they lie: (address, stride) each, and what else has to be a multiple of eight."""
-    return 0 if any(at % 16 or stride % 8 for at, stride in rows) else 1
+    _refuse(what, f"adaptors {tuple(A.shape)} on {A.device} and {tuple(B.shape)} on {B.device} where adjacent (S, {m}, k) and (S, k, {d}) are needed")
 
 
 def mtpc_adapted_projection(x, W, A, B, scale, row_adaptor, out, out_low=None, x_low=None, workspace=None, out_status=None, stream=None) -> None:
@@ -579,14 +596,14 @@ def mtpc_adapted_projection(x, W, A, B, scale, row_adaptor, out, out_low=None, x
     out_stride = _rows(what, out, T, m, dev, _bfloat16)
     if out_low is not None and (out_low.shape != (T, k) or out_low.dtype is not _float32 or not out_low.is_contiguous() or out_low.get_device() != dev):
         _refuse(what, f"out_low {tuple(out_low.shape)} of {out_low.dtype}")
-    plain = _plain_rows((x.data_ptr(), stride if T > 1 else 0), (W.data_ptr(), W_stride if m > 1 else 0), (A.data_ptr(), k), (B.data_ptr(), d),
-                        (0 if x_low is None else x_low.data_ptr(), low_stride if T > 1 else 0))
-    if (T > 1 and (stride < d or (x_low is not None and low_stride < d))) or (m > 1 and W_stride < d):
-        plain = 0
-    ws = _scratch(what, workspace, _scratch_bytes("mtpc_adapted_projection_workspace_bytes", T, d, m, k, S, plain), dev, stream)
-    _call(what, lib().mtpc_adapted_projection, dev, stream, x.data_ptr(), stride, _ptr(x_low), low_stride, W.data_ptr(), W_stride, A.data_ptr(),
-          B.data_ptr(), _vector(what, scale, S, dev, _float32), _vector(what, row_adaptor, T, dev, _int32), T, d, m, k, S, out.data_ptr(), out_stride,
-          _ptr(out_low), ws.data_ptr(), ws.numel(), _vector(what, out_status, 1, dev, _int32))
+    x_at, W_at, A_at, B_at, low_at = x.data_ptr(), W.data_ptr(), A.data_ptr(), B.data_ptr(), 0 if x_low is None else x_low.data_ptr()
+    # whether tensor maps address the operands as they lie
+    plain = (x_at | W_at | A_at | B_at | low_at) % 16 == 0 and (d | k) % 8 == 0 and (T <= 1 or (stride % 8 == 0 and stride >= d)) and (
+        m <= 1 or (W_stride % 8 == 0 and W_stride >= d)) and (x_low is None or T <= 1 or (low_stride % 8 == 0 and low_stride >= d))
+    ws_at, ws_bytes, ws = _workspace(what, workspace, _scratch_bytes("mtpc_adapted_projection_workspace_bytes", T, d, m, k, S, 1 if plain else 0), dev, stream)
+    _call(what, lib().mtpc_adapted_projection, dev, stream, x_at, stride, low_at, low_stride, W_at, W_stride, A_at, B_at, _flat(what, scale, S, dev, _float32),
+          _flat(what, row_adaptor, T, dev, _int32), T, d, m, k, S, out.data_ptr(), out_stride, _ptr(out_low), ws_at, ws_bytes,
+          _flat(what, out_status, 1, dev, _int32))
 
 
 def mtpc_adapted_projection_backward(x_low, W, A, B, scale, row_adaptor, low, d_out, d_x, dA=None, dB=None, d_x_low=None, workspace=None, out_status=None,
@@ -606,16 +623,15 @@ def mtpc_adapted_projection_backward(x_low, W, A, B, scale, row_adaptor, low, d_
     for name, t, shape in (("low", low, (T, k)), ("dA", dA, (S, m, k)), ("dB", dB, (S, k, d))):
         if t is not None and (t.shape != shape or t.dtype is not _float32 or not t.is_contiguous() or t.get_device() != dev):
             _refuse(what, f"{name} {tuple(t.shape)} of {t.dtype} where adjacent fp32 {shape} is needed")
-    plain = _plain_rows((d_out.data_ptr(), g_stride if T > 1 else 0), (W.data_ptr(), W_stride if m > 1 else 0), (A.data_ptr(), k), (B.data_ptr(), d),
-                        (0 if x_low is None else x_low.data_ptr(), x_stride if T > 1 else 0))
-    if (T > 1 and (g_stride < m or (x_low is not None and x_stride < d))) or (m > 1 and W_stride < d):
-        plain = 0
-    ws = _scratch(what, workspace, _scratch_bytes("mtpc_adapted_projection_backward_workspace_bytes", T, d, m, k, S, plain), dev, stream)
-    _call(what, lib().mtpc_adapted_projection_backward, dev, stream, _ptr(x_low), x_stride, W.data_ptr(), W_stride, A.data_ptr(), B.data_ptr(),
-          _vector(what, scale, S, dev, _float32), _vector(what, row_adaptor, T, dev, _int32), _ptr(low), T, d, m, k, S, d_out.data_ptr(), g_stride,
-          _ptr(d_x), 0 if d_x is None else _rows(what, d_x, T, d, dev, _bfloat16), _ptr(d_x_low),
-          0 if d_x_low is None else _rows(what, d_x_low, T, d, dev, _bfloat16), _ptr(dA), _ptr(dB), ws.data_ptr(), ws.numel(),
-          _vector(what, out_status, 1, dev, _int32))
+    g_at, W_at, A_at, B_at, x_at = d_out.data_ptr(), W.data_ptr(), A.data_ptr(), B.data_ptr(), 0 if x_low is None else x_low.data_ptr()
+    plain = (g_at | W_at | A_at | B_at | x_at) % 16 == 0 and (d | k) % 8 == 0 and (T <= 1 or (g_stride % 8 == 0 and g_stride >= m)) and (
+        m <= 1 or (W_stride % 8 == 0 and W_stride >= d)) and (x_low is None or T <= 1 or (x_stride % 8 == 0 and x_stride >= d))
+    ws_at, ws_bytes, ws = _workspace(what, workspace, _scratch_bytes("mtpc_adapted_projection_backward_workspace_bytes", T, d, m, k, S, 1 if plain else 0), dev,
+                                     stream)
+    _call(what, lib().mtpc_adapted_projection_backward, dev, stream, x_at, x_stride, W_at, W_stride, A_at, B_at, _flat(what, scale, S, dev, _float32),
+          _flat(what, row_adaptor, T, dev, _int32), _ptr(low), T, d, m, k, S, g_at, g_stride, _ptr(d_x),
+          0 if d_x is None else _rows(what, d_x, T, d, dev, _bfloat16), _ptr(d_x_low), 0 if d_x_low is None else _rows(what, d_x_low, T, d, dev, _bfloat16),
+          _ptr(dA), _ptr(dB), ws_at, ws_bytes, _flat(what, out_status, 1, dev, _int32))
 
 
 def mtpc_dropout(x, out, p: float, rng, offset: int = 0, residual=None, stream=None) -> None:
@@ -624,10 +640,8 @@ def mtpc_dropout(x, out, p: float, rng, offset: int = 0, residual=None, stream=N
     _dtypes()
     what = "mtpc_dropout"
     T, d, stride, dev = _matrix(what, x)
-    if rng.dtype is not _int64:
-        _refuse(what, f"{rng.dtype} where {_int64} is needed", ERR_UNSUPPORTED)
     _call(what, lib().mtpc_dropout, dev, stream, x.data_ptr(), stride, _dtype(what, x), _ptr(residual),
-          0 if residual is None else _rows(what, residual, T, d, dev, out.dtype), T, d, p, _vector(what, rng, 2, dev), offset, out.data_ptr(),
+          0 if residual is None else _rows(what, residual, T, d, dev, out.dtype), T, d, p, _flat(what, rng, 2, dev, _int64), offset, out.data_ptr(),
           _rows(what, out, T, d, dev), _dtype(what, out))
 
 
@@ -644,7 +658,7 @@ def _positions(what: str, logp, offsets, mask):
         return T, S, dev, 0
     if mask.dtype is not _bool and mask.dtype is not _uint8:
         _refuse(what, f"a mask of {mask.dtype}", ERR_UNSUPPORTED)
-    return T, S, dev, _vector(what, mask, T, dev)
+    return T, S, dev, _flat(what, mask, T, dev, mask.dtype)
 
 
 def mtpc_policy_loss(logp, old_logp, ref_logp, advantage, offsets, clip_low: float, clip_high: float, beta: float, out_loss, d_logp, mask=None,
@@ -654,12 +668,12 @@ def mtpc_policy_loss(logp, old_logp, ref_logp, advantage, offsets, clip_low: flo
     _dtypes()
     what = "mtpc_policy_loss"
     T, S, dev, mask_at = _positions(what, logp, offsets, mask)
-    ws = _scratch(what, workspace, _scratch_bytes("mtpc_objective_workspace_bytes", T, S), dev, stream)
-    _call(what, lib().mtpc_policy_loss, dev, stream, _vector(what, logp, T, dev, _float32), _vector(what, old_logp, T, dev, _float32),
-          _vector(what, ref_logp, T, dev, _float32), _vector(what, advantage, T if by_position else S, dev, _float32), 1 if by_position else 0, mask_at,
-          _vector(what, offsets, S + 1, dev, _int32), T, S, clip_low, clip_high, beta, 1 if by_sequence else 0, _vector(what, out_loss, 1, dev, _float32),
-          _vector(what, out_stats, 3, dev, _float32), _vector(what, d_logp, T, dev, _float32), ws.data_ptr(), ws.numel(),
-          _vector(what, out_status, 1, dev, _int32))
+    ws_at, ws_bytes, ws = _workspace(what, workspace, _scratch_bytes("mtpc_objective_workspace_bytes", T, S), dev, stream)
+    _call(what, lib().mtpc_policy_loss, dev, stream, _flat(what, logp, T, dev, _float32), _flat(what, old_logp, T, dev, _float32),
+          _flat(what, ref_logp, T, dev, _float32), _flat(what, advantage, T if by_position else S, dev, _float32), 1 if by_position else 0, mask_at,
+          _flat(what, offsets, S + 1, dev, _int32), T, S, clip_low, clip_high, beta, 1 if by_sequence else 0, _flat(what, out_loss, 1, dev, _float32),
+          _flat(what, out_stats, 3, dev, _float32), _flat(what, d_logp, T, dev, _float32), ws_at, ws_bytes,
+          _flat(what, out_status, 1, dev, _int32))
 
 
 def mtpc_preference_loss(logp, ref_logp, offsets, beta: float, out_loss, d_logp, mask=None, smoothing: float = 0.0, out_h=None, workspace=None,
@@ -669,11 +683,11 @@ def mtpc_preference_loss(logp, ref_logp, offsets, beta: float, out_loss, d_logp,
     _dtypes()
     what = "mtpc_preference_loss"
     T, S, dev, mask_at = _positions(what, logp, offsets, mask)
-    ws = _scratch(what, workspace, _scratch_bytes("mtpc_objective_workspace_bytes", T, S), dev, stream)
-    _call(what, lib().mtpc_preference_loss, dev, stream, _vector(what, logp, T, dev, _float32), _vector(what, ref_logp, T, dev, _float32), mask_at,
-          _vector(what, offsets, S + 1, dev, _int32), T, S, beta, smoothing, _vector(what, out_loss, 1, dev, _float32),
-          _vector(what, out_h, S // 2, dev, _float32), _vector(what, d_logp, T, dev, _float32), ws.data_ptr(), ws.numel(),
-          _vector(what, out_status, 1, dev, _int32))
+    ws_at, ws_bytes, ws = _workspace(what, workspace, _scratch_bytes("mtpc_objective_workspace_bytes", T, S), dev, stream)
+    _call(what, lib().mtpc_preference_loss, dev, stream, _flat(what, logp, T, dev, _float32), _flat(what, ref_logp, T, dev, _float32), mask_at,
+          _flat(what, offsets, S + 1, dev, _int32), T, S, beta, smoothing, _flat(what, out_loss, 1, dev, _float32),
+          _flat(what, out_h, S // 2, dev, _float32), _flat(what, d_logp, T, dev, _float32), ws_at, ws_bytes,
+          _flat(what, out_status, 1, dev, _int32))
 
 
 class GradientList:

@@ -21,6 +21,7 @@ constexpr int kSmemLimit = 232448;      // 227 KB of dynamic shared memory per C
 constexpr int kFewRows = 128;
 constexpr int kMaxAdaptors = 4096, kMaxWidth = 1 << 17, kMaxBatch = 1 << 24;
 constexpr size_t kControl = 1024 + sizeof(GemmControl);
+constexpr int kRowsShared = sizeof(RowsShared) + 16;
 
 // ---------------------------------------------------------------- tensor maps
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
@@ -60,15 +61,14 @@ int pieces_of(int k) { return (k + kPieceRank - 1) / kPieceRank; }
 int chunks_of(int K) { return ceil_div(K, kChunkBlocks * kBlockK); }
 
 struct ForwardPlan {
-  size_t off_status, off_low, off_part, off_two, off_x, off_x_low, off_W, off_A, off_B, total;
+  size_t off_low, off_part, off_two, off_x, off_x_low, off_W, off_A, off_B, total;
 };
 void plan_forward(int T, int d, int m, int k, int S, bool copies, ForwardPlan* p) {
   size_t off = 0;
   auto take = [&](size_t bytes) { size_t o = off; off += align_up(bytes); return o; };
   const size_t rows = T, dp = up8(d);
-  const bool few = T <= kFewRows;
-  p->off_status = take(4);
-  p->off_low = take(few ? rows * k * 4 : 0);
+  const bool few = T <= kFewRows, own_low = static_cast<int64_t>(T) * k <= kOwnLow;
+  p->off_low = take(few && !own_low ? rows * k * 4 : 0);
   p->off_part = take(few ? 0 : rows * chunks_of(d) * rank16(k) * 4);
   p->off_two = take(few ? 0 : rows * pieces_of(k) * 128);
   p->off_x = take(copies ? rows * dp * 2 : 0);
@@ -93,7 +93,7 @@ int grad_splits(int tiles, int S, int blocks) {
 }
 struct BackwardPlan {
   int splits;
-  size_t off_status, off_part, off_two, off_low3, off_v3, off_present, off_grad, off_x, off_W, off_A, off_B, off_g, total;
+  size_t off_part, off_two, off_low3, off_v3, off_present, off_grad, off_x, off_W, off_A, off_B, off_g, total;
 };
 void plan_backward(int T, int d, int m, int k, int S, bool copies, BackwardPlan* p) {
   size_t off = 0;
@@ -101,7 +101,6 @@ void plan_backward(int T, int d, int m, int k, int S, bool copies, BackwardPlan*
   const size_t rows = T, dp = up8(d), k16 = rank16(k);
   const int blocks = ceil_div(T, 64), tiles = ceil_div(d, kBlockM) + ceil_div(m, kBlockM);
   p->splits = grad_splits(tiles, S, blocks);
-  p->off_status = take(4);
   p->off_part = take(rows * chunks_of(m) * k16 * 4);
   p->off_two = take(rows * pieces_of(k) * 128);
   p->off_low3 = take(rows * 3 * k16 * 2);
@@ -163,7 +162,10 @@ int allow_shared_memory() {
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return MTPC_ERR_CUDA;
   if (__atomic_load_n(&g_allowed[dev], __ATOMIC_ACQUIRE)) return MTPC_OK;
   const auto allow = [](auto* kernel, int bytes) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess; };
-  bool ok = allow(adaptor_low_kernel<false>, kSmemLimit) && allow(adaptor_low_kernel<true>, kSmemLimit) && allow(adapted_rows_kernel, kSmemLimit);
+  bool ok = allow(adaptor_low_kernel<false>, kSmemLimit) && allow(adaptor_low_kernel<true>, kSmemLimit) && allow(adapted_rows_kernel<1, false>, kSmemLimit);
+  ok = ok && allow(adapted_rows_kernel<1, true>, kSmemLimit) && allow(adapted_rows_kernel<2, true>, kSmemLimit);
+  ok = ok && allow(adapted_rows_kernel<4, true>, kSmemLimit) && allow(adapted_rows_kernel<8, true>, kSmemLimit);
+  ok = ok && allow(adapted_rows_kernel<2, false>, kSmemLimit) && allow(adapted_rows_kernel<4, false>, kSmemLimit) && allow(adapted_rows_kernel<8, false>, kSmemLimit);
   ok = ok && allow(adapted_gemm_kernel<false, 256, 2>, kSmemLimit) && allow(adapted_gemm_kernel<true, 256, 2>, kSmemLimit);
   ok = ok && allow(adapted_gemm_kernel<false, 128, 1>, kSmemLimit) && allow(adapted_gemm_kernel<true, 128, 1>, kSmemLimit);
   ok = ok && allow(adapted_gemm_kernel<false, 64, 1>, kSmemLimit) && allow(adapted_gemm_kernel<true, 64, 1>, kSmemLimit);
@@ -258,7 +260,7 @@ int launch_product(const Rows& a, const Rows& b, const __nv_bfloat16* two, const
 }
 
 int launch_few_rows(const Rows& x, const Rows& W, const void* x_low, int64_t x_low_stride, const void* A, const void* B, const float* scale, const int* which,
-                    int T, int d, int m, int k, int S, void* out, int64_t out_stride, float* low, unsigned* status, unsigned* user_status, cudaStream_t st) {
+                    int T, int d, int m, int k, int S, void* out, int64_t out_stride, float* low, float* user_low, unsigned* status, cudaStream_t st) {
   LowRowsParams l;
   memset(&l, 0, sizeof(l));
   l.x = static_cast<const __nv_bfloat16*>(x_low);
@@ -267,13 +269,14 @@ int launch_few_rows(const Rows& x, const Rows& W, const void* x_low, int64_t x_l
   l.which = which;
   l.scale = scale;
   l.low = low;
-  l.status = user_status;
+  l.status = status;
   l.T = T;
   l.d = d;
   l.k = k;
   l.S = S;
   l.wide = d % 8 == 0 && rows_allow(x_low, x_low_stride, 2, 8, T) && aligned(B, 16);
-  launch_kernel(low_rows_kernel, dim3(T, ceil_div(k, 4)), 128, 0, st, true, l);
+  const bool own_low = T * k <= kOwnLow;
+  if (!own_low) launch_kernel(low_rows_kernel, dim3(T, ceil_div(k, 4)), 128, 0, st, true, l);
 
   RowsParams p;
   memset(&p, 0, sizeof(p));
@@ -294,13 +297,26 @@ int launch_few_rows(const Rows& x, const Rows& W, const void* x_low, int64_t x_l
   p.k = k;
   p.kblocks = ceil_div(d, kBlockK);
   const int tiles = ceil_div(m, kBlockM);
-  p.split = 1;
-  while (p.split < 8 && p.split * 2 <= p.kblocks && tiles * p.split < 2 * kSms - 64) p.split *= 2;
+  // K is cut until the CTAs are as many as the device holds at once, two on an SM; behind low_rows_kernel and for few rows no further than into four (4096 x 4096, k = 16,
+  // two / four / eight parts, us: 5 rows 10.7 / 10.6 / 14, 16 rows 12.3 / 11.5 / 12.9, 64 rows 24 / 18.5 / 17.5; one row by itself 17.5 / 13.2 / 10.3).
+  const int most = own_low || T > 32 ? 8 : 4;
+  int split = 1;
+  while (split < most && split * 2 <= p.kblocks && tiles * split <= kSms) split *= 2;
   p.stage_bytes = kABytes + p.tokens * kBlockK * 2;
-  p.stages = stages_of(p.stage_bytes, 2);
-  p.wide = k % 8 == 0 && aligned(A, 16) && aligned(low, 16);
-  const size_t smem = kControl + static_cast<size_t>(p.stages) * p.stage_bytes;
-  launch_clusters(adapted_rows_kernel, p.split, tiles * p.split, kRowsThreads, smem, st, true, p);
+  p.stages = stages_of(p.stage_bytes, 2, kRowsShared);
+  p.wide = k % 8 == 0 && aligned(A, 16) && (own_low || aligned(low, 16));
+  p.own = l;
+  p.own.low = user_low;
+  const size_t smem = kControl + kRowsShared + static_cast<size_t>(p.stages) * p.stage_bytes;
+  auto* kernel = own_low ? (split == 8   ? adapted_rows_kernel<8, true>
+                            : split == 4 ? adapted_rows_kernel<4, true>
+                            : split == 2 ? adapted_rows_kernel<2, true>
+                                         : adapted_rows_kernel<1, true>)
+                         : (split == 8   ? adapted_rows_kernel<8, false>
+                            : split == 4 ? adapted_rows_kernel<4, false>
+                            : split == 2 ? adapted_rows_kernel<2, false>
+                                         : adapted_rows_kernel<1, false>);
+  launch_clusters(kernel, split, tiles * split, kRowsThreads, smem, st, true, p);
   return check_launch();
 }
 
@@ -324,7 +340,7 @@ int mtpc_adapted_projection(const void* x, int64_t x_stride, const void* x_low, 
   int rc = check_sizes(T, d, m, k, S);
   if (rc != MTPC_OK) return rc;
   if (T == 0) return MTPC_OK;
-  if (!x || !W || !A || !B || !out || !workspace) return MTPC_ERR_NULL;
+  if (!x || !W || !A || !B || !out) return MTPC_ERR_NULL;
   if (!x_low) {
     x_low = x;
     x_low_stride = x_stride;
@@ -339,23 +355,23 @@ int mtpc_adapted_projection(const void* x, int64_t x_stride, const void* x_low, 
                       (!few && (!mappable(x_low, x_low_stride, T, d) || !mappable(A, k, 2, k) || !mappable(B, d, 2, d)));
   ForwardPlan plan;
   plan_forward(T, d, m, k, S, copies, &plan);
+  if (plan.total > 0 && !workspace) return MTPC_ERR_NULL;
   if (workspace_bytes < plan.total || !aligned(workspace, kAlign)) return MTPC_ERR_WORKSPACE;
   if ((rc = check_device()) != MTPC_OK || (rc = allow_shared_memory()) != MTPC_OK) return rc;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   uint8_t* ws = static_cast<uint8_t*>(workspace);
-  unsigned* status = out_status ? out_status : reinterpret_cast<unsigned*>(ws + plan.off_status);
   Copier copy(st);
   const Rows xr = copy.rows(x, x_stride, T, d, ws + plan.off_x), Wr = copy.rows(W, W_stride, m, d, ws + plan.off_W);
   if (few) {
     copy.launch_now();
     float* low = out_low ? out_low : reinterpret_cast<float*>(ws + plan.off_low);
-    return launch_few_rows(xr, Wr, x_low, x_low_stride, A, B, scale, row_adaptor, T, d, m, k, S, out, out_stride, low, status, out_status, st);
+    return launch_few_rows(xr, Wr, x_low, x_low_stride, A, B, scale, row_adaptor, T, d, m, k, S, out, out_stride, low, out_low, out_status, st);
   }
   const Rows Ar = copy.rows(A, k, static_cast<int64_t>(S) * m, k, ws + plan.off_A), Br = copy.rows(B, d, static_cast<int64_t>(S) * k, d, ws + plan.off_B);
   const Rows lr = x_low == x && x_low_stride == x_stride ? xr : copy.rows(x_low, x_low_stride, T, d, ws + plan.off_x_low);
   copy.launch_now();
   float* part = reinterpret_cast<float*>(ws + plan.off_part);
-  if ((rc = launch_low(lr, Br, false, row_adaptor, T, d, k, S, part, status, st)) != MTPC_OK) return rc;
+  if ((rc = launch_low(lr, Br, false, row_adaptor, T, d, k, S, part, out_status, st)) != MTPC_OK) return rc;
   LowJoinParams j;
   memset(&j, 0, sizeof(j));
   j.which = row_adaptor;
@@ -371,7 +387,7 @@ int mtpc_adapted_projection(const void* x, int64_t x_stride, const void* x_low, 
   j.chunks = chunks_of(d);
   j.pieces = pieces_of(k);
   if ((rc = launch_join(j, st)) != MTPC_OK) return rc;
-  return launch_product(xr, Wr, j.two, Ar, false, row_adaptor, T, d, m, k, S, true, true, out, out_stride, status, st);
+  return launch_product(xr, Wr, j.two, Ar, false, row_adaptor, T, d, m, k, S, true, true, out, out_stride, out_status, st);
 }
 
 int mtpc_adapted_projection_backward_workspace_bytes(int32_t T, int32_t d, int32_t m, int32_t k, int32_t S, int32_t aligned_rows, size_t* out_bytes) {
@@ -390,7 +406,7 @@ int mtpc_adapted_projection_backward(const void* x_low, int64_t x_low_stride, co
                                      float* dA, float* dB, void* workspace, size_t workspace_bytes, uint32_t* out_status, void* stream) {
   int rc = check_sizes(T, d, m, k, S);
   if (rc != MTPC_OK) return rc;
-  if (!workspace || (T > 0 && (!d_out || !A || !B || (d_x && !W) || (dA && !low) || (dB && !x_low)))) return MTPC_ERR_NULL;
+  if (T > 0 && (!workspace || !d_out || !A || !B || (d_x && !W) || (dA && !low) || (dB && !x_low))) return MTPC_ERR_NULL;
   if (!input_rows(x_low, x_low_stride, T) || !input_rows(W, W_stride, m) || !input_rows(d_out, d_out_stride, T) || !output_rows(d_x, d_x_stride, T, d) ||
       !output_rows(d_x_low, d_x_low_stride, T, d))
     return MTPC_ERR_SHAPE;
@@ -413,7 +429,6 @@ int mtpc_adapted_projection_backward(const void* x_low, int64_t x_low_stride, co
     return MTPC_OK;
   }
   uint8_t* ws = static_cast<uint8_t*>(workspace);
-  unsigned* status = out_status ? out_status : reinterpret_cast<unsigned*>(ws + plan.off_status);
   Copier copy(st);
   const Rows gr = copy.rows(d_out, d_out_stride, T, m, ws + plan.off_g);
   const Rows Ar = copy.rows(A, k, static_cast<int64_t>(S) * m, k, ws + plan.off_A), Br = copy.rows(B, d, static_cast<int64_t>(S) * k, d, ws + plan.off_B);
@@ -435,7 +450,7 @@ int mtpc_adapted_projection_backward(const void* x_low, int64_t x_low_stride, co
   __nv_bfloat16* v3 = reinterpret_cast<__nv_bfloat16*>(ws + plan.off_v3);
   if (d_x || d_x_low || dB) {
     j.part = reinterpret_cast<float*>(ws + plan.off_part);
-    if ((rc = launch_low(gr, Ar, true, row_adaptor, T, m, k, S, reinterpret_cast<float*>(ws + plan.off_part), status, st)) != MTPC_OK) return rc;
+    if ((rc = launch_low(gr, Ar, true, row_adaptor, T, m, k, S, reinterpret_cast<float*>(ws + plan.off_part), out_status, st)) != MTPC_OK) return rc;
     j.scale = scale;
     j.two = d_x || d_x_low ? two : nullptr;
     j.three = dB ? v3 : nullptr;
@@ -452,8 +467,8 @@ int mtpc_adapted_projection_backward(const void* x_low, int64_t x_low_stride, co
   if (j.part || j.given) {
     if ((rc = launch_join(j, st)) != MTPC_OK) return rc;
   }
-  if (d_x && (rc = launch_product(gr, Wr, two, Br, true, row_adaptor, T, m, d, k, S, true, d_x_low == nullptr, d_x, d_x_stride, status, st)) != MTPC_OK) return rc;
-  if (d_x_low && (rc = launch_product(gr, Rows{gr.p, gr.stride}, two, Br, true, row_adaptor, T, m, d, k, S, false, true, d_x_low, d_x_low_stride, status, st)) != MTPC_OK)
+  if (d_x && (rc = launch_product(gr, Wr, two, Br, true, row_adaptor, T, m, d, k, S, true, d_x_low == nullptr, d_x, d_x_stride, out_status, st)) != MTPC_OK) return rc;
+  if (d_x_low && (rc = launch_product(gr, Rows{gr.p, gr.stride}, two, Br, true, row_adaptor, T, m, d, k, S, false, true, d_x_low, d_x_low_stride, out_status, st)) != MTPC_OK)
     return rc;
   if (!dA && !dB) return MTPC_OK;
   GradParams p;
@@ -465,7 +480,7 @@ int mtpc_adapted_projection_backward(const void* x_low, int64_t x_low_stride, co
   p.out[0] = dA;
   p.out[1] = dB;
   p.part = reinterpret_cast<float*>(ws + plan.off_grad);
-  p.status = status;
+  p.status = out_status;
   p.wait_limit_ns = kWaitLimitNs;
   p.T = T;
   p.S = S;

@@ -700,7 +700,7 @@ struct LowRowsParams {
 __global__ void __launch_bounds__(128) low_rows_kernel(const LowRowsParams p) {
   __shared__ float4 red[4];
   grid_dependency_wait();
-  grid_launch_dependents();             // (a gate: what follows may read the call's inputs before it waits)
+  grid_launch_dependents();             // (a gate: what is behind may read all but low before it waits)
   const int t = blockIdx.x, j0 = blockIdx.y * 4, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int i = adaptor_of(p.which, p.S, t, p.T);
   float s[4] = {0.f, 0.f, 0.f, 0.f};
@@ -709,6 +709,7 @@ __global__ void __launch_bounds__(128) low_rows_kernel(const LowRowsParams p) {
     const __nv_bfloat16* f = p.B + (static_cast<size_t>(i) * p.k + j0) * p.d;
     const int js = min(4, p.k - j0);
     if (p.wide) {
+#pragma unroll 4
       for (int c = threadIdx.x * 8; c < p.d; c += 1024) {
         Raw<__nv_bfloat16, 8> xv, fv[4];
         xv.load(x + c);
@@ -743,68 +744,121 @@ __global__ void __launch_bounds__(128) low_rows_kernel(const LowRowsParams p) {
 }
 
 // out of few rows: W's rows are the MMA's M (128 of them a cluster), the tokens its N. The CTAs of a cluster share K; their sums meet in shared memory, every CTA
-// adds up its share of the tokens and the adaptors' part, which is read where it is needed only.
+// adds up its share of the tokens and the adaptors' part. W, which is all but a few of the bytes, is asked into L2 while the kernels ahead still run.
+// A few rank values in all (T k <= kOwnLow): every cluster forms low itself, each CTA over its share of K, one launch less.
 struct RowsParams {
   CUtensorMap tm_w;                     // W [N, K]   box 64 x 128
   CUtensorMap tm_x;                     // x [T, K]   box 64 x tokens
   const __nv_bfloat16* A;               // [S, N, k]
-  const float* low;                     // [T, k]
+  const float* low;                     // [T, k] (low_rows_kernel's)
   const int* which;
   __nv_bfloat16* out;
   int64_t out_stride;
   unsigned* status;
   uint64_t wait_limit_ns;
   int T, S, N, k, tokens;               // tokens: T rounded up to 16
-  int kblocks, split, stages, stage_bytes;
+  int kblocks, stages, stage_bytes;
   int wide;                             // rows of A and of low are vectors of eight elements
+  // where low is formed here
+  LowRowsParams own;                    // low: NULL or where it is wanted
 };
-constexpr int kRowsThreads = 192;
-constexpr int kRowsAhead = 16;                    // rows of a CTA whose adaptors' part is formed while W is on its way
-// The adaptors' part of column n of rows t, t + split, t + 2 split, t + 3 split (those that exist).
-__device__ __forceinline__ void rows_adaptors(const RowsParams& p, int t, int n, float* y) {
+constexpr int kOwnLow = 32;
+struct RowsShared {
+  float part[kOwnLow], low[kOwnLow];
+};
+constexpr int kRowsThreads = 320;
+constexpr int kRowsAhead = 8;                     // rows of a thread whose adaptors' part is formed while W is on its way
+// The adaptors' part of column n of rows t, t + step, t + 2 step, t + 3 step (those that exist): begin() asks for A, finish() needs low.
+struct RowsAdaptors {
   int i[4];
+  Raw<__nv_bfloat16, 8> a[4][2];        // the first sixteen of A's row, where rows are vectors
+  __device__ __forceinline__ void begin(const RowsParams& p, int step, int t, int n) {
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    i[q] = n < p.N ? adaptor_of(p.which, p.S, t + q * p.split, p.T) : -1;
-    y[q] = 0.f;
-  }
-  if (p.wide) {
-    for (int j = 0; j < p.k; j += 8) {
-      Raw<__nv_bfloat16, 8> a[4];
-      float4 l[4][2];
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        if (i[q] < 0) continue;
-        a[q].load(p.A + (static_cast<size_t>(i[q]) * p.N + n) * p.k + j);
-        const float4* low = reinterpret_cast<const float4*>(p.low + static_cast<size_t>(t + q * p.split) * p.k + j);
-        l[q][0] = low[0], l[q][1] = low[1];
-      }
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        if (i[q] < 0) continue;
-        const float v[8] = {l[q][0].x, l[q][0].y, l[q][0].z, l[q][0].w, l[q][1].x, l[q][1].y, l[q][1].z, l[q][1].w};
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[q] = fmaf(a[q].value(e), v[e], y[q]);
-      }
-    }
-  } else {
+    for (int q = 0; q < 4; ++q) i[q] = n < p.N ? adaptor_of(p.which, p.S, t + q * step, p.T) : -1;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       if (i[q] < 0) continue;
-      const __nv_bfloat16* a = p.A + (static_cast<size_t>(i[q]) * p.N + n) * p.k;
-      for (int j = 0; j < p.k; ++j) y[q] = fmaf(to_f32(a[j]), p.low[static_cast<size_t>(t + q * p.split) * p.k + j], y[q]);
+      const __nv_bfloat16* row = p.A + (static_cast<size_t>(i[q]) * p.N + n) * p.k;
+      if (p.wide) {
+        a[q][0].load(row);
+        if (p.k > 8) a[q][1].load(row + 8);
+      }
+      if (!p.wide || p.k > 16) prefetch_l2(row + p.k - 1);
+    }
+  }
+  __device__ __forceinline__ void finish(const RowsParams& p, const float* low_rows, int step, int t, int n, float* y) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      y[q] = 0.f;
+      if (i[q] < 0) continue;
+      const __nv_bfloat16* row = p.A + (static_cast<size_t>(i[q]) * p.N + n) * p.k;
+      const float* low = low_rows + static_cast<size_t>(t + q * step) * p.k;
+      if (p.wide) {
+        for (int j = 0; j < p.k; j += 8) {
+          const float4 l0 = reinterpret_cast<const float4*>(low + j)[0], l1 = reinterpret_cast<const float4*>(low + j)[1];
+          Raw<__nv_bfloat16, 8> v = j == 0 ? a[q][0] : a[q][1];
+          if (j >= 16) v.load(row + j);
+          const float l[8] = {l0.x, l0.y, l0.z, l0.w, l1.x, l1.y, l1.z, l1.w};
+#pragma unroll
+          for (int e = 0; e < 8; ++e) y[q] = fmaf(v.value(e), l[e], y[q]);
+        }
+      } else {
+        for (int j = 0; j < p.k; ++j) y[q] = fmaf(to_f32(row[j]), low[j], y[q]);
+      }
+    }
+  }
+};
+// This CTA's share [c0, c1) of K of the T k dot products, four at a time a warp.
+__device__ __forceinline__ void own_low_parts(const LowRowsParams& p, int c0, int c1, int warp, int lane, float* part) {
+  for (int base = warp * 4; base < p.T * p.k; base += 32) {
+    const __nv_bfloat16 *x[4], *f[4];
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int id = min(base + q, p.T * p.k - 1), t = id / p.k, i = max(adaptor_of(p.which, p.S, t, p.T), 0);       // (what a row without adaptor gives is not used)
+      x[q] = p.x + t * p.x_stride;
+      f[q] = p.B + (static_cast<size_t>(i) * p.k + (id - t * p.k)) * p.d;
+    }
+    if (p.wide) {
+#pragma unroll 2
+      for (int c = c0 + lane * 8; c < c1; c += 256) {
+        Raw<__nv_bfloat16, 8> xv[4], fv[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          xv[q].load(x[q] + c);
+          fv[q].load(f[q] + c);
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) s[q] = fmaf(xv[q].value(e), fv[q].value(e), s[q]);
+      }
+    } else {
+      for (int c = c0 + lane; c < c1; c += 32)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) s[q] = fmaf(to_f32(x[q][c]), to_f32(f[q][c]), s[q]);
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) s[q] += __shfl_xor_sync(0xffffffffu, s[q], o);
+      if (lane == 0 && base + q < p.T * p.k) part[base + q] = s[q];
     }
   }
 }
+__device__ __forceinline__ void rows_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }      // warps 2 to 9
+
+template <int SPLIT, bool OWN_LOW>
 __global__ void __launch_bounds__(kRowsThreads) adapted_rows_kernel(const __grid_constant__ RowsParams p) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw_addr = smem_u32(smem_raw);
   const uint32_t tiles_addr = (raw_addr + 1023u) & ~1023u;
   GemmControl* ctl = reinterpret_cast<GemmControl*>(smem_raw + (tiles_addr - raw_addr) + static_cast<size_t>(p.stages) * p.stage_bytes);
+  RowsShared* shared = reinterpret_cast<RowsShared*>((reinterpret_cast<uintptr_t>(ctl + 1) + 15) & ~static_cast<uintptr_t>(15));
   const int warp = static_cast<int>(warp_uniform(threadIdx.x >> 5));
   const int lane = threadIdx.x & 31;
-  const int rank = static_cast<int>(blockIdx.x % p.split), tile = blockIdx.x / p.split;
-  const int kb0 = static_cast<int>(static_cast<long long>(rank) * p.kblocks / p.split), kb1 = static_cast<int>(static_cast<long long>(rank + 1) * p.kblocks / p.split);
+  const int rank = static_cast<int>(blockIdx.x % SPLIT), tile = blockIdx.x / SPLIT;
+  const int kb0 = rank * p.kblocks / SPLIT, kb1 = (rank + 1) * p.kblocks / SPLIT;
   const uint32_t tmem_cols = p.tokens <= 32 ? 32u : p.tokens <= 64 ? 64u : 128u;
   if (threadIdx.x == 0) {
     for (int s = 0; s < p.stages; ++s) {
@@ -833,8 +887,12 @@ __global__ void __launch_bounds__(kRowsThreads) adapted_rows_kernel(const __grid
   float* sums = reinterpret_cast<float*>(smem_raw + (tiles_addr - raw_addr));
 
   if (warp == 0) {
-    // The kernel ahead is low_rows_kernel, a gate (or this grid was launched plainly): x and W are what the caller made them.
     const uint32_t lead = elect_one();
+    // low_rows_kernel ahead is a gate: x and W are there. Without it W is asked into L2 while the kernel ahead still runs.
+    if (OWN_LOW) {
+      for (int kb = kb0; kb < kb1; ++kb) tma_prefetch_2d(lead, &p.tm_w, kb * kBlockK, tile * kBlockM);
+      grid_dependency_wait();
+    }
     const uint32_t bytes = kABytes + static_cast<uint32_t>(p.tokens) * (kBlockK * 2);
     uint32_t stage = 0, phase = 0, issued = 0;
     for (int kb = kb0; kb < kb1; ++kb) {
@@ -866,15 +924,33 @@ __global__ void __launch_bounds__(kRowsThreads) adapted_rows_kernel(const __grid
     if (ok) umma_commit(lead, smem_u32(&ctl->tfull[0]));
     __syncwarp();
   } else {
-    const int quarter = warp & 3;
+    const int quarter = warp & 3, sub = (warp - 2) >> 2, n = tile * kBlockM + quarter * 32 + lane;
     const uint32_t lane_base = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16);
-    grid_dependency_wait();
-    grid_launch_dependents();
+    const int first = rank + SPLIT * sub;
+    if (OWN_LOW) {
+      grid_dependency_wait();
+      grid_launch_dependents();
+      for (int t = first; t < p.T; t += 2 * SPLIT) {
+        const int i = adaptor_of(p.which, p.S, t, p.T);
+        if (i >= 0 && n < p.N) prefetch_l2(p.A + (static_cast<size_t>(i) * p.N + n) * p.k);
+      }
+      own_low_parts(p.own, kb0 * kBlockK, min(kb1 * kBlockK, p.own.d), warp - 2, lane, shared->part);
+    } else {
+      RowsAdaptors ra;
+      ra.begin(p, 2 * SPLIT, first, n);
+      grid_dependency_wait();
+      grid_launch_dependents();
+      ra.finish(p, p.low, 2 * SPLIT, first, n, part);
 #pragma unroll
-    for (int q = 0; q < kRowsAhead; q += 4) rows_adaptors(p, rank + q * p.split, tile * kBlockM + quarter * 32 + lane, part + q);
+      for (int q = 4; q < kRowsAhead; q += 4) {
+        if (first + q * 2 * SPLIT >= p.T) break;
+        ra.begin(p, 2 * SPLIT, first + q * 2 * SPLIT, n);
+        ra.finish(p, p.low, 2 * SPLIT, first + q * 2 * SPLIT, n, part + q);
+      }
+    }
     if (bounded_wait_warp(smem_u32(&ctl->tfull[0]), 0, ctl, p.status, lane)) {
       tc_fence_after();
-      for (int b = 0; b < p.tokens / 16; ++b) {
+      for (int b = sub; b < p.tokens / 16; b += 2) {
         float x[16];
         tmem_ld16(lane_base + b * 16, x);
 #pragma unroll
@@ -886,21 +962,53 @@ __global__ void __launch_bounds__(kRowsThreads) adapted_rows_kernel(const __grid
   __syncthreads();
   cluster_sync_all();                                                // the other CTAs' sums
   if (warp >= 2) {
-    const int m = (warp & 3) * 32 + lane, n = tile * kBlockM + m;
+    const int m = (warp & 3) * 32 + lane, n = tile * kBlockM + m, first = rank + SPLIT * ((warp - 2) >> 2);
     const uint32_t own = smem_u32(sums) + 4u * m;
-    auto finish = [&](int t, float y) {
-      if (t >= p.T) return;
-      float sum = 0.f;
-      for (int r = 0; r < p.split; ++r) sum += ld_cluster_f32(cluster_map_shared(own + 4u * kBlockM * t, r));
-      if (n < p.N) p.out[t * p.out_stride + n] = __float2bfloat16_rn(adaptor_refused(p.which, p.S, t) ? CUDART_NAN_F : sum + y);
+    if (OWN_LOW) {
+      const int id = threadIdx.x - 64;
+      if (id < p.T * p.k) {
+        float v[SPLIT], all = 0.f;
+#pragma unroll
+        for (int r = 0; r < SPLIT; ++r) v[r] = ld_cluster_f32(cluster_map_shared(smem_u32(shared->part + id), r));
+#pragma unroll
+        for (int r = 0; r < SPLIT; ++r) all += v[r];
+        const int t = id / p.k, i = adaptor_of(p.which, p.S, t, p.T);
+        const bool refused = adaptor_refused(p.which, p.S, t);
+        all = i < 0 ? 0.f : all * (p.own.scale == nullptr ? 1.f : p.own.scale[i]);
+        shared->low[id] = all;
+        if (blockIdx.x == 0) {
+          if (p.own.low != nullptr) p.own.low[id] = refused ? CUDART_NAN_F : all;
+          if (refused && p.own.status != nullptr) atomicOr(p.own.status, kStatusBadAdaptor);
+        }
+      }
+      rows_sync();
+    }
+    auto finish = [&](int t, const float* y) {                        // four rows: all loads in flight together
+      float sum[4][SPLIT];
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int r = 0; r < SPLIT; ++r)
+          sum[q][r] = t + q * 2 * SPLIT < p.T ? ld_cluster_f32(cluster_map_shared(own + 4u * kBlockM * (t + q * 2 * SPLIT), r)) : 0.f;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int at = t + q * 2 * SPLIT;
+        if (at >= p.T || n >= p.N) continue;
+        float all = y[q];
+#pragma unroll
+        for (int r = 0; r < SPLIT; ++r) all += sum[q][r];
+        p.out[at * p.out_stride + n] = __float2bfloat16_rn(adaptor_refused(p.which, p.S, at) ? CUDART_NAN_F : all);
+      }
     };
 #pragma unroll
-    for (int q = 0; q < kRowsAhead; ++q) finish(rank + q * p.split, part[q]);
-    for (int t = rank + kRowsAhead * p.split; t < p.T; t += 4 * p.split) {
+    for (int q = 0; q < (OWN_LOW ? 0 : kRowsAhead); q += 4)
+      if (first + q * 2 * SPLIT < p.T) finish(first + q * 2 * SPLIT, part + q);
+    for (int t = first + (OWN_LOW ? 0 : kRowsAhead * 2 * SPLIT); t < p.T; t += 8 * SPLIT) {
       float more[4];
-      rows_adaptors(p, t, n, more);
-#pragma unroll
-      for (int q = 0; q < 4; ++q) finish(t + q * p.split, more[q]);
+      RowsAdaptors ra;
+      ra.begin(p, 2 * SPLIT, t, n);
+      ra.finish(p, OWN_LOW ? shared->low : p.low, 2 * SPLIT, t, n, more);
+      finish(t, more);
     }
   }
   tc_fence_before();

@@ -26,6 +26,8 @@ namespace mtpc {
 constexpr uint32_t kStatusBadOffset = 16u;
 constexpr int kObjectiveThreads = 512, kObjectiveWarps = kObjectiveThreads / 32;
 constexpr int kObjectiveCtas = 8;                  // of the cluster that does a small call alone
+constexpr int kSmallItems = 1024;                  // that such a call has at most
+constexpr int kMostBlocks = 148 * 4;               // of a launch for one phase
 
 struct ObjectiveArgs {
   const float *logp, *old, *ref, *advantage;       // ref: NULL without the KL term; advantage [S], or [T] with by_position (policy)
@@ -40,7 +42,8 @@ struct ObjectiveArgs {
   uint32_t* status;
   // workspace
   int* count;                                      // [S * parts] valid positions of every slice
-  double* sum;                                     // [S * parts][3] (policy) or [S * parts] (preference)
+  long long* block_count;                          // [kMostBlocks] of all slices of a block
+  double* sum;                                     // [kMostBlocks][3] of all slices of a block (policy), or [S * parts] (preference)
   double* term;                                    // [S / 2] a pair's loss
   float* slope;                                    // [S / 2]
 };
@@ -126,15 +129,38 @@ __device__ __forceinline__ void store4(float* p, const Slice& c, int t, bool ins
 }
 
 // ---- phases, each over items first, first + step, ... of a warp
+// N sums over the warps of a block, each warp's in its lane 0; thread 0 gets them. red: N * kObjectiveWarps values.
+template <int N, typename F>
+__device__ __forceinline__ void block_sum(F (&x)[N], F* red) {
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) red[k * kObjectiveWarps + (threadIdx.x >> 5)] = x[k];
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      x[k] = 0;
+#pragma unroll
+      for (int i = 0; i < kObjectiveWarps; ++i) x[k] += red[k * kObjectiveWarps + i];
+    }
+  }
+}
 template <bool WIDE>
-__device__ __forceinline__ void count_phase(const ObjectiveArgs& a, int first, int step, int lane) {
+__device__ __forceinline__ void count_phase(const ObjectiveArgs& a, int block, int blocks, int lane, long long* red) {
+  const int first = block * kObjectiveWarps + (threadIdx.x >> 5), step = blocks * kObjectiveWarps;
+  long long all[1] = {0};
   for (int item = first; item < a.S * a.parts; item += step) {
     const Slice c = slice_of(a, item);
     int n = 0;
     over_slice<WIDE>(a, c, lane, [&](int, uint32_t valid, bool) { n += __popc(valid); });
     n = warp_total(n);
     if (lane == 0) a.count[item] = n;
+    all[0] += n;
   }
+  block_sum(all, red);
+  if (threadIdx.x == 0) a.block_count[block] = all[0];
 }
 
 // e^q - 1 - q, and e^q - 1: near zero by the series, whose next term is below 2^-28 of the first; the function less q is off by q's rounding.
@@ -156,7 +182,9 @@ __device__ __forceinline__ void exp_beyond(float q, float& beyond, float& m1) {
 
 // total: all valid positions.
 template <bool WIDE>
-__device__ __forceinline__ void policy_phase(const ObjectiveArgs& a, int first, int step, int lane, long long total) {
+__device__ __forceinline__ void policy_phase(const ObjectiveArgs& a, int block, int blocks, int lane, long long total, double* red) {
+  const int first = block * kObjectiveWarps + (threadIdx.x >> 5), step = blocks * kObjectiveWarps;
+  double all[3] = {0.0, 0.0, 0.0};
   for (int item = first; item < a.S * a.parts; item += step) {
     const Slice c = slice_of(a, item);
     long long n = total;
@@ -204,11 +232,14 @@ __device__ __forceinline__ void policy_phase(const ObjectiveArgs& a, int first, 
     value = warp_total(value);
     kl = warp_total(kl);
     clipped = warp_total(clipped);
-    if (lane == 0) {
-      a.sum[3 * static_cast<size_t>(item)] = value * weight;
-      a.sum[3 * static_cast<size_t>(item) + 1] = kl * weight;
-      a.sum[3 * static_cast<size_t>(item) + 2] = clipped * weight;
-    }
+    all[0] += value * weight;
+    all[1] += kl * weight;
+    all[2] += clipped * weight;
+  }
+  block_sum(all, red);
+  if (threadIdx.x == 0) {
+#pragma unroll
+    for (int i = 0; i < 3; ++i) a.sum[3 * block + i] = all[i];
   }
 }
 
@@ -235,10 +266,10 @@ __device__ __forceinline__ void block_totals(int n, F (&x)[N], F* red, Get get) 
   }
 }
 // All valid positions (whole numbers: any order gives the same).
-__device__ __forceinline__ long long all_valid(const ObjectiveArgs& a, long long* red) {
+__device__ __forceinline__ long long all_valid(const ObjectiveArgs& a, int blocks, long long* red) {
   long long n[1];
   if (a.mask != nullptr) {
-    block_totals<1>(a.S * a.parts, n, red, [&](int i, long long (&x)[1]) { x[0] += a.count[i]; });
+    block_totals<1>(blocks, n, red, [&](int i, long long (&x)[1]) { x[0] += a.block_count[i]; });
   } else {
     block_totals<1>(a.S, n, red, [&](int s, long long (&x)[1]) {
       const Span c = span_of(a, s);
@@ -254,12 +285,12 @@ __device__ __forceinline__ bool any_refused(const ObjectiveArgs& a, long long* r
   if (n[0] > 0 && threadIdx.x == 0 && a.status != nullptr) atomicOr(a.status, kStatusBadOffset);
   return n[0] > 0;
 }
-__device__ __forceinline__ void policy_final(const ObjectiveArgs& a, double* red) {
+__device__ __forceinline__ void policy_final(const ObjectiveArgs& a, int blocks, double* red) {
   const bool refused = any_refused(a, reinterpret_cast<long long*>(red));
   double s[3];
-  block_totals<3>(a.S * a.parts, s, red, [&](int item, double (&x)[3]) {
+  block_totals<3>(blocks, s, red, [&](int block, double (&x)[3]) {
 #pragma unroll
-    for (int i = 0; i < 3; ++i) x[i] += a.sum[3 * static_cast<size_t>(item) + i];
+    for (int i = 0; i < 3; ++i) x[i] += a.sum[3 * block + i];
   });
   if (threadIdx.x == 0) {
     a.loss[0] = refused ? CUDART_NAN_F : static_cast<float>(s[0] + a.beta * s[1]);
@@ -324,57 +355,81 @@ __device__ __forceinline__ void spread_phase(const ObjectiveArgs& a, int first, 
   }
 }
 
-// ---- one cluster does the whole call
-template <bool WIDE>
-__global__ void __launch_bounds__(kObjectiveThreads) policy_cluster_kernel(const ObjectiveArgs a) {
-  __shared__ double red[3 * kObjectiveWarps];
-  grid_launch_dependents();
-  grid_dependency_wait();
-  const int rank = static_cast<int>(cluster_cta_rank()), lane = threadIdx.x & 31;
-  const int first = rank * kObjectiveWarps + (threadIdx.x >> 5), step = kObjectiveCtas * kObjectiveWarps;
-  if (a.mask != nullptr) {
-    count_phase<WIDE>(a, first, step, lane);
-    cluster_sync_all();
-  }
-  policy_phase<WIDE>(a, first, step, lane, a.by_sequence ? 0 : all_valid(a, reinterpret_cast<long long*>(red)));
-  cluster_sync_all();
-  if (rank == 0) policy_final(a, red);
+// ---- one cluster does the whole call; what its CTAs hand each other lies in the first one's shared memory
+struct ObjectiveShared {
+  double sum[kSmallItems], term[kSmallItems / 2];
+  long long block_count[kObjectiveCtas];
+  int count[kSmallItems];
+  float slope[kSmallItems / 2];
+};
+__device__ __forceinline__ void use_first_cta(ObjectiveArgs& a, ObjectiveShared* own) {
+  uint64_t at;
+  asm("mapa.u64 %0, %1, 0;" : "=l"(at) : "l"(reinterpret_cast<uint64_t>(own)));
+  ObjectiveShared* first = reinterpret_cast<ObjectiveShared*>(at);
+  a.sum = first->sum;
+  a.term = first->term;
+  a.block_count = first->block_count;
+  a.count = first->count;
+  a.slope = first->slope;
 }
 template <bool WIDE>
-__global__ void __launch_bounds__(kObjectiveThreads) preference_cluster_kernel(const ObjectiveArgs a) {
-  __shared__ double red[kObjectiveWarps];
+__global__ void __launch_bounds__(kObjectiveThreads) policy_cluster_kernel(ObjectiveArgs a) {
+  __shared__ double red[3 * kObjectiveWarps];
+  __shared__ ObjectiveShared shared;
+  use_first_cta(a, &shared);
+  const int rank = static_cast<int>(cluster_cta_rank()), lane = threadIdx.x & 31;
   grid_launch_dependents();
+  cluster_sync_all();                              // the first CTA is there
   grid_dependency_wait();
+  if (a.mask != nullptr) {
+    count_phase<WIDE>(a, rank, kObjectiveCtas, lane, reinterpret_cast<long long*>(red));
+    cluster_sync_all();
+  }
+  const long long total = a.by_sequence ? 0 : all_valid(a, kObjectiveCtas, reinterpret_cast<long long*>(red));
+  policy_phase<WIDE>(a, rank, kObjectiveCtas, lane, total, red);
+  cluster_sync_all();
+  if (rank == 0) policy_final(a, kObjectiveCtas, red);
+}
+template <bool WIDE>
+__global__ void __launch_bounds__(kObjectiveThreads) preference_cluster_kernel(ObjectiveArgs a) {
+  __shared__ double red[kObjectiveWarps];
+  __shared__ ObjectiveShared shared;
+  use_first_cta(a, &shared);
   const int rank = static_cast<int>(cluster_cta_rank()), lane = threadIdx.x & 31;
   const int first = rank * kObjectiveWarps + (threadIdx.x >> 5), step = kObjectiveCtas * kObjectiveWarps;
+  grid_launch_dependents();
+  cluster_sync_all();
+  grid_dependency_wait();
   ratio_phase<WIDE>(a, first, step, lane);
   cluster_sync_all();
   pairs_phase(a, first, step, lane);
   cluster_sync_all();
   spread_phase<WIDE>(a, first, step, lane);
   if (rank == 0) preference_final(a, red);
+  cluster_sync_all();                              // nobody reads the first CTA's any more
 }
 
 // ---- a launch for each phase
 template <bool WIDE>
 __global__ void __launch_bounds__(kObjectiveThreads) count_kernel(const ObjectiveArgs a) {
-  grid_launch_dependents();
-  grid_dependency_wait();
-  count_phase<WIDE>(a, blockIdx.x * kObjectiveWarps + (threadIdx.x >> 5), gridDim.x * kObjectiveWarps, threadIdx.x & 31);
-}
-template <bool WIDE>
-__global__ void __launch_bounds__(kObjectiveThreads) policy_kernel(const ObjectiveArgs a) {
   __shared__ long long red[kObjectiveWarps];
   grid_launch_dependents();
   grid_dependency_wait();
-  policy_phase<WIDE>(a, blockIdx.x * kObjectiveWarps + (threadIdx.x >> 5), gridDim.x * kObjectiveWarps, threadIdx.x & 31,
-                     a.by_sequence ? 0 : all_valid(a, red));
+  count_phase<WIDE>(a, blockIdx.x, gridDim.x, threadIdx.x & 31, red);
 }
-__global__ void __launch_bounds__(kObjectiveThreads) policy_final_kernel(const ObjectiveArgs a) {
+template <bool WIDE>
+__global__ void __launch_bounds__(kObjectiveThreads) policy_kernel(const ObjectiveArgs a) {
   __shared__ double red[3 * kObjectiveWarps];
   grid_launch_dependents();
   grid_dependency_wait();
-  policy_final(a, red);
+  const long long total = a.by_sequence ? 0 : all_valid(a, gridDim.x, reinterpret_cast<long long*>(red));
+  policy_phase<WIDE>(a, blockIdx.x, gridDim.x, threadIdx.x & 31, total, red);
+}
+__global__ void __launch_bounds__(kObjectiveThreads) policy_final_kernel(const ObjectiveArgs a, int blocks) {
+  __shared__ double red[3 * kObjectiveWarps];
+  grid_launch_dependents();
+  grid_dependency_wait();
+  policy_final(a, blocks, red);
 }
 template <bool WIDE>
 __global__ void __launch_bounds__(kObjectiveThreads) ratio_kernel(const ObjectiveArgs a) {

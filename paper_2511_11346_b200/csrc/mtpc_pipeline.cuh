@@ -40,7 +40,7 @@ __device__ __forceinline__ bool bounded_wait(uint32_t bar, uint32_t parity, Gemm
       if (ctl->abort) return false;
       if (global_timer_ns() - t0 > ctl->wait_limit_ns) {
         ctl->abort = 1;
-        atomicOr(status, kStatusTimeout);
+        if (status != nullptr) atomicOr(status, kStatusTimeout);
         return false;
       }
     }
@@ -67,7 +67,7 @@ __device__ __forceinline__ bool bounded_wait_all(uint32_t bar, uint32_t parity, 
     if (__all_sync(all, mbar_try_wait(bar, parity))) return true;
     if (__any_sync(all, global_timer_ns() - t0 > p.wait_limit_ns)) {
       ctl->abort = 1;
-      if (elect_one()) atomicOr(p.status, kStatusTimeout);
+      if (elect_one() && p.status != nullptr) atomicOr(p.status, kStatusTimeout);
       return false;
     }
   }
@@ -83,7 +83,7 @@ __device__ __forceinline__ bool first_wait(uint32_t bar, GemmControl* ctl, const
   while (!__all_sync(all, mbar_test_wait(bar, 0))) {
     if (__any_sync(all, global_timer_ns() - t0 > p.wait_limit_ns)) {
       ctl->abort = 1;
-      if (elect_one()) atomicOr(p.status, kStatusTimeout);
+      if (elect_one() && p.status != nullptr) atomicOr(p.status, kStatusTimeout);
       return false;
     }
   }

@@ -35,20 +35,26 @@ void launch_dropout(const DropoutArgs& a, bool vectors, cudaStream_t st) {
 
 // ---------------------------------------------------------------- losses
 constexpr int kMaxSequences = 1 << 20;
-constexpr int kSmallPositions = 1 << 16, kSmallItems = 2048;
+constexpr int kSmallPositions = 1 << 16;
 struct ObjectivePlan {
   int parts;
-  size_t off_count, off_sum, off_term, off_slope, total;
+  bool small;                           // one cluster does it, without a workspace
+  size_t off_count, off_blocks, off_sum, off_term, off_slope, total;
 };
-// Slices of about 512 positions (four of a lane's vectors), so that a million positions are 2000 warps; a small call's for the warps of its cluster.
+// Slices of about 256 positions (two of a lane's vectors), so that a million positions are 4000 warps; of a small call about 128, for the warps of its cluster.
 void plan_objective(int T, int S, ObjectivePlan* p) {
-  p->parts = std::max(1, std::min(ceil_div(T, static_cast<long long>(S) * 512), 1 << 14));
-  if (T <= kSmallPositions) p->parts = std::max(p->parts, std::min(ceil_div(kObjectiveCtas * kObjectiveWarps, S), std::max(1, ceil_div(T, static_cast<long long>(S) * 128))));
+  const int share = T <= kSmallPositions ? 128 : 256;
+  p->parts = std::max(1, std::min(ceil_div(T, static_cast<long long>(S) * share), 1 << 16));
+  if (T <= kSmallPositions) p->parts = std::max(1, std::min(p->parts, kSmallItems / S));
   const size_t items = static_cast<size_t>(S) * p->parts;
+  p->small = T <= kSmallPositions && items <= kSmallItems;
+  p->total = 0;
+  if (p->small) return;
   size_t off = 0;
   auto take = [&](size_t bytes) { size_t o = off; off += align_up(bytes); return o; };
   p->off_count = take(items * 4);
-  p->off_sum = take(items * 24);
+  p->off_blocks = take(kMostBlocks * 8);
+  p->off_sum = take(std::max<size_t>(items, 3 * kMostBlocks) * 8);
   p->off_term = take(static_cast<size_t>(S / 2 + 1) * 8);
   p->off_slope = take(static_cast<size_t>(S / 2 + 1) * 4);
   p->total = off;
@@ -62,26 +68,27 @@ bool a_share(float x) { return x >= 0.f && x <= 1.f; }      // (no NaN)
 void carve(const ObjectivePlan& p, void* workspace, ObjectiveArgs* a) {
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   a->parts = p.parts;
+  if (p.small) return;
   a->count = reinterpret_cast<int*>(ws + p.off_count);
+  a->block_count = reinterpret_cast<long long*>(ws + p.off_blocks);
   a->sum = reinterpret_cast<double*>(ws + p.off_sum);
   a->term = reinterpret_cast<double*>(ws + p.off_term);
   a->slope = reinterpret_cast<float*>(ws + p.off_slope);
 }
-bool small_call(const ObjectiveArgs& a) { return a.T <= kSmallPositions && static_cast<long long>(a.S) * a.parts <= kSmallItems; }
-int item_blocks(const ObjectiveArgs& a) { return std::min(ceil_div(static_cast<long long>(a.S) * a.parts, kObjectiveWarps), kSms * 4); }
+int item_blocks(const ObjectiveArgs& a) { return std::min(ceil_div(static_cast<long long>(a.S) * a.parts, kObjectiveWarps), kMostBlocks); }
 template <bool WIDE>
-void launch_policy(const ObjectiveArgs& a, cudaStream_t st) {
-  if (small_call(a)) {
+void launch_policy(const ObjectiveArgs& a, bool small, cudaStream_t st) {
+  if (small) {
     launch_clusters(policy_cluster_kernel<WIDE>, kObjectiveCtas, kObjectiveCtas, kObjectiveThreads, 0, st, true, a);
     return;
   }
   if (a.mask) launch_kernel(count_kernel<WIDE>, item_blocks(a), kObjectiveThreads, 0, st, true, a);
   launch_kernel(policy_kernel<WIDE>, item_blocks(a), kObjectiveThreads, 0, st, true, a);
-  launch_kernel(policy_final_kernel, 1, kObjectiveThreads, 0, st, true, a);
+  launch_kernel(policy_final_kernel, 1, kObjectiveThreads, 0, st, true, a, item_blocks(a));
 }
 template <bool WIDE>
-void launch_preference(const ObjectiveArgs& a, cudaStream_t st) {
-  if (small_call(a)) {
+void launch_preference(const ObjectiveArgs& a, bool small, cudaStream_t st) {
+  if (small) {
     launch_clusters(preference_cluster_kernel<WIDE>, kObjectiveCtas, kObjectiveCtas, kObjectiveThreads, 0, st, true, a);
     return;
   }
@@ -157,9 +164,9 @@ int mtpc_policy_loss(const float* logp, const float* old_logp, const float* ref_
                         static_cast<const void*>(advantage), static_cast<const void*>(offsets), static_cast<const void*>(out_loss),
                         static_cast<const void*>(out_stats), static_cast<const void*>(d_logp), static_cast<const void*>(out_status)})
     if (!aligned(q, 4)) return MTPC_ERR_SHAPE;
-  if (!workspace) return MTPC_ERR_NULL;
   ObjectivePlan p;
   plan_objective(T, S, &p);
+  if (p.total > 0 && !workspace) return MTPC_ERR_NULL;
   if (workspace_bytes < p.total || !aligned(workspace, kAlign)) return MTPC_ERR_WORKSPACE;
   if ((rc = check_device()) != MTPC_OK) return rc;
   ObjectiveArgs a;
@@ -186,8 +193,8 @@ int mtpc_policy_loss(const float* logp, const float* old_logp, const float* ref_
   carve(p, workspace, &a);
   const bool wide = aligned(logp, 16) && aligned(old_logp, 16) && aligned(a.ref, 16) && aligned(d_logp, 16) && aligned(mask, 4) &&
                     (!a.by_position || aligned(advantage, 16));
-  if (wide) launch_policy<true>(a, static_cast<cudaStream_t>(stream));
-  else launch_policy<false>(a, static_cast<cudaStream_t>(stream));
+  if (wide) launch_policy<true>(a, p.small, static_cast<cudaStream_t>(stream));
+  else launch_policy<false>(a, p.small, static_cast<cudaStream_t>(stream));
   return check_launch();
 }
 
@@ -202,9 +209,9 @@ int mtpc_preference_loss(const float* logp, const float* ref_logp, const uint8_t
                         static_cast<const void*>(out_loss), static_cast<const void*>(out_h), static_cast<const void*>(d_logp),
                         static_cast<const void*>(out_status)})
     if (!aligned(q, 4)) return MTPC_ERR_SHAPE;
-  if (!workspace) return MTPC_ERR_NULL;
   ObjectivePlan p;
   plan_objective(T, S, &p);
+  if (p.total > 0 && !workspace) return MTPC_ERR_NULL;
   if (workspace_bytes < p.total || !aligned(workspace, kAlign)) return MTPC_ERR_WORKSPACE;
   if ((rc = check_device()) != MTPC_OK) return rc;
   ObjectiveArgs a;
@@ -223,8 +230,8 @@ int mtpc_preference_loss(const float* logp, const float* ref_logp, const uint8_t
   a.status = out_status;
   carve(p, workspace, &a);
   const bool wide = aligned(logp, 16) && aligned(ref_logp, 16) && aligned(d_logp, 16) && aligned(mask, 4);
-  if (wide) launch_preference<true>(a, static_cast<cudaStream_t>(stream));
-  else launch_preference<false>(a, static_cast<cudaStream_t>(stream));
+  if (wide) launch_preference<true>(a, p.small, static_cast<cudaStream_t>(stream));
+  else launch_preference<false>(a, p.small, static_cast<cudaStream_t>(stream));
   return check_launch();
 }
 

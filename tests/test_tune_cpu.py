@@ -30,12 +30,12 @@ def preference(lp=P, ref=P, mask=None, off=P, T=64, S=4, beta=0.1, sm=0.0, loss=
     (dropout, dict(os=0), SHAPE), (dropout, dict(r=P, rs=-1), SHAPE), (dropout, dict(rng=ctypes.c_void_p(4100)), SHAPE), (dropout, dict(x=ODD, xd=F32), SHAPE),
     (dropout, dict(out=ODD, od=F32), SHAPE), (dropout, dict(r=ODD, od=F32), SHAPE),
     (policy, dict(lp=None), NULL), (policy, dict(old=None), NULL), (policy, dict(ref=None), NULL), (policy, dict(adv=None), NULL), (policy, dict(off=None), NULL),
-    (policy, dict(loss=None), NULL), (policy, dict(d=None), NULL), (policy, dict(ws=None), NULL), (policy, dict(wb=16), WORKSPACE), (policy, dict(ws=ODD), WORKSPACE),
+    (policy, dict(loss=None), NULL), (policy, dict(d=None), NULL), (policy, dict(ws=None, T=1 << 20), NULL), (policy, dict(wb=16, T=1 << 20), WORKSPACE), (policy, dict(ws=ODD), WORKSPACE),
     (policy, dict(T=-1), SHAPE), (policy, dict(S=0), SHAPE), (policy, dict(S=(1 << 20) + 1), UNSUPPORTED), (policy, dict(T=(1 << 30) + 1), UNSUPPORTED),
     (policy, dict(lo=-0.1), SHAPE), (policy, dict(hi=NAN), SHAPE), (policy, dict(hi=INF), SHAPE), (policy, dict(beta=-1.0), SHAPE), (policy, dict(beta=NAN), SHAPE),
     (policy, dict(lp=ODD), SHAPE), (policy, dict(d=ODD), SHAPE), (policy, dict(off=ODD), SHAPE), (policy, dict(stats=ODD), SHAPE), (policy, dict(status=ODD), SHAPE),
     (preference, dict(lp=None), NULL), (preference, dict(ref=None), NULL), (preference, dict(off=None), NULL), (preference, dict(loss=None), NULL),
-    (preference, dict(d=None), NULL), (preference, dict(ws=None), NULL), (preference, dict(wb=16), WORKSPACE), (preference, dict(S=3), SHAPE),
+    (preference, dict(d=None), NULL), (preference, dict(ws=None, T=1 << 20), NULL), (preference, dict(wb=16, T=1 << 20), WORKSPACE), (preference, dict(ws=ODD), WORKSPACE), (preference, dict(S=3), SHAPE),
     (preference, dict(S=0), SHAPE), (preference, dict(beta=-0.1), SHAPE), (preference, dict(sm=1.5), SHAPE), (preference, dict(sm=NAN), SHAPE),
     (preference, dict(h=ODD), SHAPE), (preference, dict(ref=ODD), SHAPE),
 ])
@@ -49,8 +49,8 @@ def test_what_is_allowed_reaches_the_check_for_a_device():
     if torch.cuda.is_available():
         pytest.skip("a device is present")
     assert dropout() == dropout(T=1, xs=-1, os=0) == dropout(x=ODD, out=ODD, p=0.0) == dropout(r=P, rs=0, od=F32) == CUDA
-    assert policy() == policy(ref=None, beta=0.0, stats=None) == policy(lo=5.0, mask=ODD) == policy(T=0, lp=None, old=None, ref=None, d=None) == CUDA
-    assert preference() == preference(h=None, sm=1.0) == preference(T=0, lp=None, ref=None, d=None) == CUDA
+    assert policy() == policy(ws=None, wb=0) == policy(ref=None, beta=0.0, stats=None) == policy(lo=5.0, mask=ODD) == policy(T=0, lp=None, old=None, ref=None, d=None) == CUDA
+    assert preference() == preference(ws=None, wb=0) == preference(h=None, sm=1.0) == preference(T=0, lp=None, ref=None, d=None) == CUDA
 
 
 def test_workspaces():
@@ -60,8 +60,8 @@ def test_workspaces():
     for T in (0, 1, 511, 65536, 65537, 1 << 20, 1 << 30):
         for S in (1, 2, 1000, 1 << 20):
             n = B.mtpc_objective_workspace_bytes(T, S)
-            assert n % 256 == 0 and n >= 28 * S
-    assert B.mtpc_objective_workspace_bytes(1 << 21, 256) < 1 << 20
+            assert n % 256 == 0 and (n >= 18 * S or (n == 0 and S <= 1000 and T <= 65536))
+    assert B.mtpc_objective_workspace_bytes(1 << 21, 256) < 1 << 20 and B.mtpc_objective_workspace_bytes(512, 8) == 0
 
 
 def test_tensors_that_do_not_fit_are_refused():
