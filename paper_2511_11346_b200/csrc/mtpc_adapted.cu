@@ -61,7 +61,7 @@ int pieces_of(int k) { return (k + kPieceRank - 1) / kPieceRank; }
 int chunks_of(int K) { return ceil_div(K, kChunkBlocks * kBlockK); }
 
 struct ForwardPlan {
-  size_t off_low, off_part, off_two, off_x, off_x_low, off_W, off_A, off_B, total;
+  size_t off_low, off_two, off_x, off_x_low, off_W, off_A, off_B, total;
 };
 void plan_forward(int T, int d, int m, int k, int S, bool copies, ForwardPlan* p) {
   size_t off = 0;
@@ -69,7 +69,6 @@ void plan_forward(int T, int d, int m, int k, int S, bool copies, ForwardPlan* p
   const size_t rows = T, dp = up8(d);
   const bool few = T <= kFewRows, own_low = static_cast<int64_t>(T) * k <= kOwnLow;
   p->off_low = take(few && !own_low ? rows * k * 4 : 0);
-  p->off_part = take(few ? 0 : rows * chunks_of(d) * rank16(k) * 4);
   p->off_two = take(few ? 0 : rows * pieces_of(k) * 128);
   p->off_x = take(copies ? rows * dp * 2 : 0);
   p->off_x_low = take(copies && !few ? rows * dp * 2 : 0);
@@ -93,7 +92,7 @@ int grad_splits(int tiles, int S, int blocks) {
 }
 struct BackwardPlan {
   int splits;
-  size_t off_part, off_two, off_low3, off_v3, off_present, off_grad, off_x, off_W, off_A, off_B, off_g, total;
+  size_t off_two, off_low3, off_v3, off_present, off_grad, off_x, off_W, off_A, off_B, off_g, total;
 };
 void plan_backward(int T, int d, int m, int k, int S, bool copies, BackwardPlan* p) {
   size_t off = 0;
@@ -101,7 +100,6 @@ void plan_backward(int T, int d, int m, int k, int S, bool copies, BackwardPlan*
   const size_t rows = T, dp = up8(d), k16 = rank16(k);
   const int blocks = ceil_div(T, 64), tiles = ceil_div(d, kBlockM) + ceil_div(m, kBlockM);
   p->splits = grad_splits(tiles, S, blocks);
-  p->off_part = take(rows * chunks_of(m) * k16 * 4);
   p->off_two = take(rows * pieces_of(k) * 128);
   p->off_low3 = take(rows * 3 * k16 * 2);
   p->off_v3 = take(rows * 3 * k16 * 2);
@@ -180,34 +178,32 @@ int stages_of(int stage_bytes, int ctas_per_sm = 1, int beside = 0) {
 }
 
 // ---------------------------------------------------------------- launches
-// low or v: rows [T, K] times the factors; parts of every chunk of K.
-int launch_low(const Rows& rows, const Rows& factors, bool mn, const int* which, int T, int K, int k, int S, float* part, unsigned* status, cudaStream_t st) {
-  LowParams p;
-  memset(&p, 0, sizeof(p));
-  int rc = map_rows(&p.tm_a, rows.p, T, K, rows.stride, kBlockM);
-  if (rc == MTPC_OK) rc = mn ? map_rows(&p.tm_f, factors.p, K, k, factors.stride, 64, S) : map_rows(&p.tm_f, factors.p, k, K, factors.stride, rank16(k), S);
-  if (rc != MTPC_OK) return rc;
+// low or v: rows [T, K] times the factors, if rows are given, and what else p asks for.
+int launch_low(LowParams& p, const Rows& rows, const Rows& factors, bool mn, const int* which, int T, int K, int k, int S, unsigned* status, cudaStream_t st) {
   p.which = which;
-  p.part = part;
   p.status = status;
   p.wait_limit_ns = kWaitLimitNs;
   p.T = T;
   p.S = S;
+  p.k = k;
   p.k16 = rank16(k);
-  p.kblocks = ceil_div(K, kBlockK);
-  p.chunks = chunks_of(K);
-  p.tiles = ceil_div(T, kBlockM);
+  p.pieces = pieces_of(k);
+  p.split = 1;
   p.stages = stages_of(kLowStageBytes, 2);
+  if (rows.p) {
+    int rc = map_rows(&p.tm_a, rows.p, T, K, rows.stride, kBlockM);
+    if (rc == MTPC_OK) rc = mn ? map_rows(&p.tm_f, factors.p, K, k, factors.stride, 64, S) : map_rows(&p.tm_f, factors.p, k, K, factors.stride, rank16(k), S);
+    if (rc != MTPC_OK) return rc;
+    p.kblocks = ceil_div(K, kBlockK);
+    p.chunks = chunks_of(K);
+    p.tiles = ceil_div(T, kBlockM);
+    while (p.split < 8 && p.split * 2 <= p.chunks && p.tiles * p.split <= kSms) p.split *= 2;
+  }
+  p.given_blocks = p.given ? ceil_div(static_cast<long long>(T) * (p.k16 / 4), kLowThreads * kGivenQuads) : 0;
+  p.present_blocks = p.present ? ceil_div(T, 32 * 64) : 0;
+  const int beside = ceil_div(p.given_blocks + p.present_blocks, p.split) * p.split;
   const size_t smem = kControl + static_cast<size_t>(p.stages) * kLowStageBytes;
-  launch_kernel(mn ? adaptor_low_kernel<true> : adaptor_low_kernel<false>, std::min(p.tiles * p.chunks, 2 * kSms), kLowThreads, smem, st, true, p);
-  return check_launch();
-}
-int launch_join(LowJoinParams& p, cudaStream_t st) {
-  const int blocks = ceil_div(static_cast<long long>(p.T) * (p.k16 / 4), kJoinThreads);
-  p.sum_blocks = p.part ? blocks : 0;
-  p.given_blocks = p.given ? blocks : 0;
-  const int present_blocks = p.present ? ceil_div(p.T, 32 * 64) : 0;
-  launch_kernel(adaptor_join_kernel, p.sum_blocks + p.given_blocks + present_blocks, kJoinThreads, p.present ? static_cast<size_t>(p.S) * 4 : 0, st, true, p);
+  launch_clusters(mn ? adaptor_low_kernel<true> : adaptor_low_kernel<false>, p.split, p.tiles * p.split + beside, kLowThreads, smem, st, true, p);
   return check_launch();
 }
 
@@ -370,24 +366,13 @@ int mtpc_adapted_projection(const void* x, int64_t x_stride, const void* x_low, 
   const Rows Ar = copy.rows(A, k, static_cast<int64_t>(S) * m, k, ws + plan.off_A), Br = copy.rows(B, d, static_cast<int64_t>(S) * k, d, ws + plan.off_B);
   const Rows lr = x_low == x && x_low_stride == x_stride ? xr : copy.rows(x_low, x_low_stride, T, d, ws + plan.off_x_low);
   copy.launch_now();
-  float* part = reinterpret_cast<float*>(ws + plan.off_part);
-  if ((rc = launch_low(lr, Br, false, row_adaptor, T, d, k, S, part, out_status, st)) != MTPC_OK) return rc;
-  LowJoinParams j;
-  memset(&j, 0, sizeof(j));
-  j.which = row_adaptor;
-  j.scale = scale;
-  j.part = part;
-  j.low = out_low;
-  j.two = reinterpret_cast<__nv_bfloat16*>(ws + plan.off_two);
-  j.status = out_status;
-  j.T = T;
-  j.S = S;
-  j.k = k;
-  j.k16 = rank16(k);
-  j.chunks = chunks_of(d);
-  j.pieces = pieces_of(k);
-  if ((rc = launch_join(j, st)) != MTPC_OK) return rc;
-  return launch_product(xr, Wr, j.two, Ar, false, row_adaptor, T, d, m, k, S, true, true, out, out_stride, out_status, st);
+  LowParams l;
+  memset(&l, 0, sizeof(l));
+  l.scale = scale;
+  l.low = out_low;
+  l.two = reinterpret_cast<__nv_bfloat16*>(ws + plan.off_two);
+  if ((rc = launch_low(l, lr, Br, false, row_adaptor, T, d, k, S, out_status, st)) != MTPC_OK) return rc;
+  return launch_product(xr, Wr, l.two, Ar, false, row_adaptor, T, d, m, k, S, true, true, out, out_stride, out_status, st);
 }
 
 int mtpc_adapted_projection_backward_workspace_bytes(int32_t T, int32_t d, int32_t m, int32_t k, int32_t S, int32_t aligned_rows, size_t* out_bytes) {
@@ -436,37 +421,24 @@ int mtpc_adapted_projection_backward(const void* x_low, int64_t x_low_stride, co
   const Rows xr = dB ? copy.rows(x_low, x_low_stride, T, d, ws + plan.off_x) : Rows{nullptr, 0};
   copy.launch_now();
 
-  LowJoinParams j;
-  memset(&j, 0, sizeof(j));
-  j.which = row_adaptor;
-  j.status = out_status;
-  j.T = T;
-  j.S = S;
-  j.k = k;
-  j.k16 = rank16(k);
-  j.pieces = pieces_of(k);
+  LowParams l;
+  memset(&l, 0, sizeof(l));
+  l.scale = scale;
   __nv_bfloat16* two = reinterpret_cast<__nv_bfloat16*>(ws + plan.off_two);
   __nv_bfloat16* low3 = reinterpret_cast<__nv_bfloat16*>(ws + plan.off_low3);
   __nv_bfloat16* v3 = reinterpret_cast<__nv_bfloat16*>(ws + plan.off_v3);
-  if (d_x || d_x_low || dB) {
-    j.part = reinterpret_cast<float*>(ws + plan.off_part);
-    if ((rc = launch_low(gr, Ar, true, row_adaptor, T, m, k, S, reinterpret_cast<float*>(ws + plan.off_part), out_status, st)) != MTPC_OK) return rc;
-    j.scale = scale;
-    j.two = d_x || d_x_low ? two : nullptr;
-    j.three = dB ? v3 : nullptr;
-    j.chunks = chunks_of(m);
-  }
+  if (d_x || d_x_low) l.two = two;
+  if (dB) l.three = v3;
   if (dA) {
-    j.given = low;
-    j.given_three = low3;
+    l.given = low;
+    l.given_three = low3;
   }
   if (dA || dB) {
-    j.present = reinterpret_cast<uint32_t*>(ws + plan.off_present);
-    j.whole = j.present + static_cast<size_t>(ceil_div(T, 32 * 64)) * S;
+    l.present = reinterpret_cast<uint32_t*>(ws + plan.off_present);
+    l.whole = l.present + static_cast<size_t>(ceil_div(T, 32 * 64)) * S;
   }
-  if (j.part || j.given) {
-    if ((rc = launch_join(j, st)) != MTPC_OK) return rc;
-  }
+  const bool sums = d_x || d_x_low || dB;
+  if ((sums || dA) && (rc = launch_low(l, sums ? gr : Rows{nullptr, 0}, Ar, true, row_adaptor, T, m, k, S, out_status, st)) != MTPC_OK) return rc;
   if (d_x && (rc = launch_product(gr, Wr, two, Br, true, row_adaptor, T, m, d, k, S, true, d_x_low == nullptr, d_x, d_x_stride, out_status, st)) != MTPC_OK) return rc;
   if (d_x_low && (rc = launch_product(gr, Rows{gr.p, gr.stride}, two, Br, true, row_adaptor, T, m, d, k, S, false, true, d_x_low, d_x_low_stride, out_status, st)) != MTPC_OK)
     return rc;
@@ -474,9 +446,9 @@ int mtpc_adapted_projection_backward(const void* x_low, int64_t x_low_stride, co
   GradParams p;
   memset(&p, 0, sizeof(p));
   p.which = row_adaptor;
-  p.present = j.present;
-  p.whole = j.whole;
-  p.after_join = !d_x && !d_x_low;
+  p.present = l.present;
+  p.whole = l.whole;
+  p.after_low = !d_x && !d_x_low;
   p.out[0] = dA;
   p.out[1] = dB;
   p.part = reinterpret_cast<float*>(ws + plan.off_grad);

@@ -3,10 +3,9 @@
 //   d_x[t] = W^T g[t] + B[i]^T v[t], v[t] = scale[i] A[i]^T g[t],    dA[i] = sum of g low^T, dB[i] = sum of v x'^T over the rows of i
 // x, W, A, B, g bf16; low, v, dA, dB fp32; out, d_x bf16.
 //
-// adaptor_low_kernel    low or v of many rows: K in chunks of 512, each its own accumulator. The tensor cores round every accumulation towards zero, so that
-//                       one accumulator over K = 4096 is 4e-6 off, chunks added up in fp32 4e-7.
-// adaptor_join_kernel   adds the chunks up, scales, and splits low or v into bf16 terms: two (16 bits) for the product with A or B whose result is rounded to
-//                       bf16, three (24 bits) for the fp32 gradients.
+// adaptor_low_kernel    low or v of many rows: K in chunks of 512, each its own accumulator, added up in fp32. The tensor cores round every accumulation towards
+//                       zero, so that one accumulator over K = 4096 is 4e-6 off, chunks 4e-7. The result is split into bf16 terms: two (16 bits) for the
+//                       product with A or B whose result is rounded to bf16, three (24 bits) for the fp32 gradients.
 // adapted_gemm_kernel   the shared product; the adaptors of a tile's rows follow as K blocks of their own.
 // low_rows_kernel, adapted_rows_kernel   the same of few rows (decoding), where W is read once by the whole device.
 // adaptor_grad_kernel, adaptor_grad_join_kernel   dA and dB.
@@ -96,6 +95,12 @@ __device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
   return x;
 }
 
+__device__ __forceinline__ float4 ld_cluster_v4(uint32_t addr) {
+  float4 x;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(addr) : "memory");
+  return x;
+}
+
 // ---- which adaptors a tile's rows have
 // Row t's adaptor; -1: none, or one that does not exist (its rows are refused by whoever writes results).
 __device__ __forceinline__ int adaptor_of(const int* which, int S, int t, int T) {
@@ -146,29 +151,104 @@ struct TileAdaptors {
 };
 
 // ---- low (or v) of many rows
+// A cluster has a tile of 128 rows; its CTAs share the chunks of K, add theirs up in registers and meet in shared memory, where each finishes its share of the rows:
+// sum, scale, low, its terms. Blocks behind the tiles' (if asked for) split given values into terms, and say which blocks of 64 rows have an adaptor's rows.
 struct LowParams {
   CUtensorMap tm_a;                     // rows [T, K]          box 64 x 128
   CUtensorMap tm_f;                     // factors: B [S, k, K] box 64 x k16 (K-major), or A [S, K, k] box 64 x 64 (MN-major)
   const int* which;
-  float* part;                          // [chunks][T][k16]
-  unsigned* status;
+  const float* scale;                   // [S] or NULL: ones
+  float* low;                           // [T, k] or NULL
+  __nv_bfloat16* two;                   // [T][pieces][64] or NULL
+  __nv_bfloat16* three;                 // [T][3][k16] or NULL
+  const float* given;                   // [T, k]
+  __nv_bfloat16* given_three;           // [T][3][k16]
+  uint32_t *present, *whole;            // bit b % 32 of [(b / 32) S + i]: block b has rows of i, and no others
+  unsigned* status;                     // or NULL
   uint64_t wait_limit_ns;
-  int T, S, k16;                        // k16: the rank, rounded up to 16
-  int kblocks, chunks, tiles, stages;
+  int T, S, k, k16, pieces;             // k16: the rank, rounded up to 16
+  int kblocks, chunks, tiles, split, stages;       // split: CTAs of a cluster; tiles 0: no sums are wanted
+  int given_blocks, present_blocks;
 };
 constexpr int kLowThreads = 192;
 constexpr int kLowStageBytes = kABytes + kMaxRank * kBlockK * 2;
 constexpr int kLowSlots = 4, kLowSlotCols = kMaxRank, kLowTmemCols = kLowSlots * kLowSlotCols;
+constexpr int kGivenQuads = 4;          // of a thread
+
+// x as a sum of bf16 values: the nearest, and the nearest to what is left (twice, where a third is wanted). A value that is not finite keeps its first.
+__device__ __forceinline__ void split_terms(float x, __nv_bfloat16& hi, __nv_bfloat16& mid, __nv_bfloat16& lo) {
+  hi = __float2bfloat16_rn(x);
+  const float r = isfinite(x) ? x - __bfloat162float(hi) : 0.f;
+  mid = __float2bfloat16_rn(r);
+  lo = __float2bfloat16_rn(r - __bfloat162float(mid));
+}
+// Four values of row t from rank j0 on (those past the rank are zeros) as terms.
+__device__ __forceinline__ void store_terms(const LowParams& p, int t, int j0, const float (&x)[4], __nv_bfloat16* two, __nv_bfloat16* three) {
+  __align__(8) __nv_bfloat16 h[4], m[4], l[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) split_terms(j0 + q < p.k ? x[q] : 0.f, h[q], m[q], l[q]);
+  const uint2 hv = *reinterpret_cast<const uint2*>(h), mv = *reinterpret_cast<const uint2*>(m), lv = *reinterpret_cast<const uint2*>(l);
+  if (two != nullptr) {
+    __nv_bfloat16* dst = two + (static_cast<size_t>(t) * p.pieces + j0 / kPieceRank) * 64 + j0 % kPieceRank;
+    *reinterpret_cast<uint2*>(dst) = hv;
+    *reinterpret_cast<uint2*>(dst + kPieceRank) = mv;
+  }
+  if (three != nullptr) {
+    __nv_bfloat16* dst = three + static_cast<size_t>(t) * 3 * p.k16 + j0;
+    *reinterpret_cast<uint2*>(dst) = hv;
+    *reinterpret_cast<uint2*>(dst + p.k16) = mv;
+    *reinterpret_cast<uint2*>(dst + 2 * p.k16) = lv;
+  }
+}
+__device__ __forceinline__ void given_terms(const LowParams& p, int block) {
+  const int quads = p.k16 / 4;
+#pragma unroll
+  for (int e = 0; e < kGivenQuads; ++e) {
+    const long long at = (static_cast<long long>(block) * kGivenQuads + e) * kLowThreads + threadIdx.x;
+    const int t = static_cast<int>(at / quads), j0 = static_cast<int>(at - static_cast<long long>(t) * quads) * 4;
+    if (t >= p.T) return;
+    const bool any = adaptor_of(p.which, p.S, t, p.T) >= 0;
+    float x[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) x[q] = any && j0 + q < p.k ? p.given[static_cast<size_t>(t) * p.k + j0 + q] : 0.f;
+    store_terms(p, t, j0, x, nullptr, p.given_three);
+  }
+}
+__device__ __forceinline__ void present_rows(const LowParams& p, int group, uint32_t* words) {       // words: S + 1
+  uint32_t* mixed = words + p.S;
+  for (int i = threadIdx.x; i <= p.S; i += kLowThreads) words[i] = 0;
+  __syncthreads();
+  for (int r = threadIdx.x; r < 32 * 64; r += kLowThreads) {
+    const long long t = static_cast<long long>(group) * (32 * 64) + r;
+    if (t >= p.T) continue;
+    const int i = adaptor_of(p.which, p.S, static_cast<int>(t), p.T), head = adaptor_of(p.which, p.S, static_cast<int>(t) - r % 64, p.T);
+    if (i >= 0) atomicOr(&words[i], 1u << (r / 64));
+    if (i != head) atomicOr(mixed, 1u << (r / 64));
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < p.S; i += kLowThreads) {
+    p.present[static_cast<size_t>(group) * p.S + i] = words[i];
+    p.whole[static_cast<size_t>(group) * p.S + i] = words[i] & ~*mixed;
+  }
+}
 
 template <bool F_MN>
 __global__ void __launch_bounds__(kLowThreads, 2) adaptor_low_kernel(const __grid_constant__ LowParams p) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw_addr = smem_u32(smem_raw);
   const uint32_t tiles_addr = (raw_addr + 1023u) & ~1023u;
+  if (static_cast<int>(blockIdx.x) >= p.tiles * p.split) {           // (whole clusters of such blocks)
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int block = blockIdx.x - p.tiles * p.split;
+    if (block < p.given_blocks) given_terms(p, block);
+    else if (block < p.given_blocks + p.present_blocks) present_rows(p, block - p.given_blocks, reinterpret_cast<uint32_t*>(smem_raw));
+    return;
+  }
   GemmControl* ctl = reinterpret_cast<GemmControl*>(smem_raw + (tiles_addr - raw_addr) + static_cast<size_t>(p.stages) * kLowStageBytes);
   const int warp = static_cast<int>(warp_uniform(threadIdx.x >> 5));
   const int lane = threadIdx.x & 31;
-  const int items = p.tiles * p.chunks;
+  const int tile = blockIdx.x / p.split, rank = blockIdx.x - tile * p.split, row0 = tile * kBlockM;
   if (threadIdx.x == 0) {
     for (int s = 0; s < p.stages; ++s) {
       mbar_init(smem_u32(&ctl->full[s]), 1);
@@ -194,27 +274,32 @@ __global__ void __launch_bounds__(kLowThreads, 2) adaptor_low_kernel(const __gri
   tc_fence_after();
   const uint32_t tmem_base = warp_uniform(ctl->tmem_base);
   grid_dependency_wait();
-  grid_launch_dependents();
+  grid_launch_dependents();             // (a gate: what is behind may read all but what is written here)
   const uint32_t full0 = smem_u32(&ctl->full[0]), empty0 = smem_u32(&ctl->empty[0]);
+  // sums [128][k16] of this CTA, over the stages once these have been multiplied; rows four floats apart from their neighbours' banks
+  float* sums = reinterpret_cast<float*>(smem_raw + (tiles_addr - raw_addr));
+  const int pitch = p.k16 + 4;
   TileAdaptors<4> ta;
+  ta.load(p.which, p.S, row0, p.T, lane);
+  const bool none = ta.none();
   int adaptor = 0;
   uint32_t off[4];
 
-  if (warp == 0) {
+  if (none) {
+  } else if (warp == 0) {
     const uint32_t lead = elect_one();
     const uint32_t f_bytes = F_MN ? kMnBoxBytes : static_cast<uint32_t>(p.k16) * (kBlockK * 2);
     uint32_t stage = 0, phase = 0, issued = 0;
     bool ok = true;
-    for (int item = blockIdx.x; item < items && ok; item += gridDim.x) {
-      const int tile = item / p.chunks, c = item - tile * p.chunks;
+    for (int c = rank; c < p.chunks && ok; c += p.split) {
       const int kb0 = c * kChunkBlocks, kb1 = min(p.kblocks, kb0 + kChunkBlocks);
-      ta.load(p.which, p.S, tile * kBlockM, p.T, lane);
-      while (ok && ta.next(adaptor, off)) {
+      TileAdaptors<4> each = ta;
+      while (ok && each.next(adaptor, off)) {
         for (int kb = kb0; kb < kb1; ++kb) {
           if (!bounded_wait_all(empty0 + 8 * stage, phase ^ 1u, ctl, p)) { ok = false; break; }
           const uint32_t full = full0 + 8 * stage, a_dst = tiles_addr + stage * kLowStageBytes;
           mbar_arrive_expect_tx(lead, full, kABytes + f_bytes);
-          tma_load_2d(lead, a_dst, &p.tm_a, full, kb * kBlockK, tile * kBlockM);
+          tma_load_2d(lead, a_dst, &p.tm_a, full, kb * kBlockK, row0);
           if (F_MN) tma_load_3d(lead, a_dst + kABytes, &p.tm_f, full, 0, kb * kBlockK, adaptor);
           else tma_load_3d(lead, a_dst + kABytes, &p.tm_f, full, kb * kBlockK, 0, adaptor);
           ++issued;
@@ -232,17 +317,14 @@ __global__ void __launch_bounds__(kLowThreads, 2) adaptor_low_kernel(const __gri
     constexpr uint32_t kStepF = F_MN ? 128u : 2u;
     const uint64_t a_desc0 = umma_smem_desc_sw128(tiles_addr);
     const uint64_t f_desc0 = F_MN ? umma_smem_desc_mn_sw128(tiles_addr + kABytes, kMnBoxBytes) : umma_smem_desc_sw128(tiles_addr + kABytes);
-    for (int item = blockIdx.x; item < items && ok; item += gridDim.x) {
-      const int tile = item / p.chunks, c = item - tile * p.chunks;
+    for (int c = rank; c < p.chunks && ok; c += p.split, ++use) {
       const int kb0 = c * kChunkBlocks, kb1 = min(p.kblocks, kb0 + kChunkBlocks);
-      ta.load(p.which, p.S, tile * kBlockM, p.T, lane);
-      if (ta.none()) continue;
       const uint32_t slot = use % kLowSlots;
       if (!bounded_wait_all(smem_u32(&ctl->tempty[slot]), ((use / kLowSlots) & 1u) ^ 1u, ctl, p)) break;
-      ++use;
       tc_fence_after();
       const uint32_t d_tmem = tmem_base + slot * kLowSlotCols;
-      while (ok && ta.next(adaptor, off)) {
+      TileAdaptors<4> each = ta;
+      while (ok && each.next(adaptor, off)) {
         for (int kb = kb0; kb < kb1; ++kb) {
           if (!bounded_wait_all(full0 + 8 * stage, phase, ctl, p)) { ok = false; break; }
           tc_fence_after();
@@ -261,136 +343,71 @@ __global__ void __launch_bounds__(kLowThreads, 2) adaptor_low_kernel(const __gri
   } else {
     const int quarter = warp & 3;
     const uint32_t lane_base = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16);
+    float acc[kMaxRank];
+#pragma unroll
+    for (int j = 0; j < kMaxRank; ++j) acc[j] = 0.f;
     uint32_t use = 0;
-    for (int item = blockIdx.x; item < items; item += gridDim.x) {
-      const int tile = item / p.chunks, c = item - tile * p.chunks;
-      ta.load(p.which, p.S, tile * kBlockM, p.T, lane);
-      if (ta.none()) continue;
+    for (int c = rank; c < p.chunks; c += p.split, ++use) {
       const uint32_t slot = use % kLowSlots;
       if (!bounded_wait_warp(smem_u32(&ctl->tfull[slot]), (use / kLowSlots) & 1u, ctl, p.status, lane)) break;
-      ++use;
       tc_fence_after();
-      const int row = tile * kBlockM + quarter * 32 + lane;
-      const bool mine = adaptor_of(p.which, p.S, row, p.T) >= 0;          // rows of none hold what was there before
-      float* dst = p.part + (static_cast<size_t>(c) * p.T + (mine ? row : 0)) * p.k16;
-      for (int b = 0; b < p.k16 / 16; ++b) {
+#pragma unroll
+      for (int b = 0; b < kMaxRank / 16; ++b) {
+        if (b * 16 >= p.k16) break;
         float x[16];
         tmem_ld16(lane_base + slot * kLowSlotCols + b * 16, x);
-        if (mine) {
-          st_global_v8(dst + b * 16, x);
-          st_global_v8(dst + b * 16 + 8, x + 8);
-        }
+#pragma unroll
+        for (int q = 0; q < 16; ++q) acc[b * 16 + q] += x[q];
       }
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&ctl->tempty[slot]));
     }
+    float4* dst = reinterpret_cast<float4*>(sums + (quarter * 32 + lane) * pitch);
+#pragma unroll
+    for (int j = 0; j < kMaxRank / 4; ++j) {
+      if (4 * j >= p.k16) break;
+      dst[j] = make_float4(acc[4 * j], acc[4 * j + 1], acc[4 * j + 2], acc[4 * j + 3]);
+    }
   }
   tc_fence_before();
   __syncthreads();
+  cluster_sync_all();                                                // the other CTAs' sums
+  const int quads = p.k16 / 4, rows = kBlockM / p.split;
+  for (int at = threadIdx.x; at < rows * quads; at += kLowThreads) {
+    const int r = at / quads, j0 = (at - r * quads) * 4, row = rank * rows + r, t = row0 + row;
+    if (t >= p.T) break;
+    const int i = adaptor_of(p.which, p.S, t, p.T);
+    float x[4] = {0.f, 0.f, 0.f, 0.f};
+    if (i >= 0) {
+      float4 y[8];
+      const uint32_t own = smem_u32(sums + row * pitch + j0);
+#pragma unroll
+      for (int c = 0; c < 8; ++c)
+        if (c < p.split) y[c] = ld_cluster_v4(cluster_map_shared(own, c));
+#pragma unroll
+      for (int c = 0; c < 8; ++c)
+        if (c < p.split) x[0] += y[c].x, x[1] += y[c].y, x[2] += y[c].z, x[3] += y[c].w;
+      const float s = p.scale == nullptr ? 1.f : p.scale[i];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) x[q] *= s;
+    }
+    const bool refused = adaptor_refused(p.which, p.S, t);
+    if (refused && p.status != nullptr && j0 == 0) atomicOr(p.status, kStatusBadAdaptor);
+    if (p.low != nullptr) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (j0 + q < p.k) p.low[static_cast<size_t>(t) * p.k + j0 + q] = refused ? CUDART_NAN_F : x[q];
+    }
+    store_terms(p, t, j0, x, p.two, p.three);
+  }
+  __syncthreads();
+  if (warp == 1) drain_after_abort<1>(ctl, true);
+  __syncthreads();
+  cluster_sync_all();                                                // nobody reads this CTA's sums any more
   if (warp == 1) {
-    drain_after_abort<1>(ctl, true);
     tc_fence_after();
     tmem_dealloc(tmem_base, kLowTmemCols);
-  }
-}
-
-// x as a sum of bf16 values: the nearest, and the nearest to what is left (twice, where a third is wanted). A value that is not finite keeps its first.
-__device__ __forceinline__ void split_terms(float x, __nv_bfloat16& hi, __nv_bfloat16& mid, __nv_bfloat16& lo) {
-  hi = __float2bfloat16_rn(x);
-  const float r = isfinite(x) ? x - __bfloat162float(hi) : 0.f;
-  mid = __float2bfloat16_rn(r);
-  lo = __float2bfloat16_rn(r - __bfloat162float(mid));
-}
-
-// Sums of chunks, scaled, as low or v and its terms; the terms of values that are given; and which blocks of 64 rows have an adaptor's rows. One launch: blocks
-// [0, sum_blocks), then given_blocks, then a block for every 32 blocks of rows.
-struct LowJoinParams {
-  const int* which;
-  const float* scale;                   // [S] or NULL: ones
-  const float* part;                    // [chunks][T][k16]
-  float* low;                           // [T, k] or NULL
-  __nv_bfloat16* two;                   // [T][pieces][64] or NULL
-  __nv_bfloat16* three;                 // [T][3][k16] or NULL
-  const float* given;                   // [T, k]
-  __nv_bfloat16* given_three;           // [T][3][k16]
-  uint32_t *present, *whole;            // bit b % 32 of [(b / 32) S + i]: block b has rows of i, and no others
-  unsigned* status;                     // or NULL
-  int T, S, k, k16, chunks, pieces;
-  int sum_blocks, given_blocks;
-};
-constexpr int kJoinThreads = 256;
-__device__ __forceinline__ void present_blocks(const LowJoinParams& p, int group, uint32_t* words) {
-  __shared__ uint32_t mixed;
-  for (int i = threadIdx.x; i < p.S; i += kJoinThreads) words[i] = 0;
-  if (threadIdx.x == 0) mixed = 0;
-  __syncthreads();
-  for (int r = threadIdx.x; r < 32 * 64; r += kJoinThreads) {
-    const long long t = static_cast<long long>(group) * (32 * 64) + r;
-    if (t >= p.T) continue;
-    const int i = adaptor_of(p.which, p.S, static_cast<int>(t), p.T), head = adaptor_of(p.which, p.S, static_cast<int>(t) - r % 64, p.T);
-    if (i >= 0) atomicOr(&words[i], 1u << (r / 64));
-    if (i != head) atomicOr(&mixed, 1u << (r / 64));
-  }
-  __syncthreads();
-  for (int i = threadIdx.x; i < p.S; i += kJoinThreads) {
-    p.present[static_cast<size_t>(group) * p.S + i] = words[i];
-    p.whole[static_cast<size_t>(group) * p.S + i] = words[i] & ~mixed;
-  }
-}
-__global__ void __launch_bounds__(kJoinThreads) adaptor_join_kernel(const LowJoinParams p) {
-  extern __shared__ uint32_t words[];
-  grid_launch_dependents();             // (no gate: what is behind waits before it reads what is written here)
-  grid_dependency_wait();
-  const int block = blockIdx.x;
-  if (block >= p.sum_blocks + p.given_blocks) {
-    present_blocks(p, block - p.sum_blocks - p.given_blocks, words);
-    return;
-  }
-  const bool given = block >= p.sum_blocks;
-  const long long at = static_cast<long long>(given ? block - p.sum_blocks : block) * kJoinThreads + threadIdx.x;
-  const int quads = p.k16 / 4;
-  const int t = static_cast<int>(at / quads), j0 = static_cast<int>(at - static_cast<long long>(t) * quads) * 4;
-  if (t >= p.T) return;
-  const int i = adaptor_of(p.which, p.S, t, p.T);
-  float x[4] = {0.f, 0.f, 0.f, 0.f};
-  if (given) {
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-      if (i >= 0 && j0 + q < p.k) x[q] = p.given[static_cast<size_t>(t) * p.k + j0 + q];
-  } else if (i >= 0) {
-#pragma unroll 8
-    for (int c = 0; c < p.chunks; ++c) {
-      const float4 y = *reinterpret_cast<const float4*>(p.part + (static_cast<size_t>(c) * p.T + t) * p.k16 + j0);
-      x[0] += y.x, x[1] += y.y, x[2] += y.z, x[3] += y.w;
-    }
-    const float s = p.scale == nullptr ? 1.f : p.scale[i];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) x[q] *= s;
-  }
-  const bool refused = adaptor_refused(p.which, p.S, t);
-  if (refused && p.status != nullptr && j0 == 0) atomicOr(p.status, kStatusBadAdaptor);
-  if (!given && p.low != nullptr) {
-    float* dst = p.low + static_cast<size_t>(t) * p.k + j0;
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-      if (j0 + q < p.k) dst[q] = refused ? CUDART_NAN_F : x[q];
-  }
-  __align__(8) __nv_bfloat16 h[4], m[4], l[4];
-#pragma unroll
-  for (int q = 0; q < 4; ++q) split_terms(j0 + q < p.k ? x[q] : 0.f, h[q], m[q], l[q]);
-  const uint2 hv = *reinterpret_cast<const uint2*>(h), mv = *reinterpret_cast<const uint2*>(m), lv = *reinterpret_cast<const uint2*>(l);
-  if (!given && p.two != nullptr) {
-    __nv_bfloat16* dst = p.two + (static_cast<size_t>(t) * p.pieces + j0 / kPieceRank) * 64 + j0 % kPieceRank;
-    *reinterpret_cast<uint2*>(dst) = hv;
-    *reinterpret_cast<uint2*>(dst + kPieceRank) = mv;
-  }
-  __nv_bfloat16* three = given ? p.given_three : p.three;
-  if (three != nullptr) {
-    __nv_bfloat16* dst = three + static_cast<size_t>(t) * 3 * p.k16 + j0;
-    *reinterpret_cast<uint2*>(dst) = hv;
-    *reinterpret_cast<uint2*>(dst + p.k16) = mv;
-    *reinterpret_cast<uint2*>(dst + 2 * p.k16) = lv;
   }
 }
 
@@ -503,8 +520,8 @@ __global__ void __launch_bounds__(kAdaptedThreads, 1) adapted_gemm_kernel(const 
   if (CTAS == 2) cluster_sync_all();   // the peer's barriers are initialised before anything arrives on them
   tc_fence_after();
   const uint32_t tmem_base = warp_uniform(ctl->tmem_base);
-  // Ahead of this kernel are adaptor_low_kernel, a gate, and adaptor_join_kernel, which is none: rows and W are there, the terms of low are waited for where they
-  // are read. This kernel is a gate again: what is behind it starts when the epilogue warps have waited.
+  // Ahead of this kernel is adaptor_low_kernel, a gate (or this kernel itself, of d_x): rows and W are there, the terms of low are waited for where they are read. It is a
+  // gate again: what is behind it starts when the epilogue warps have waited.
   TileAdaptors<kWords> ta;
   int adaptor = 0;
   uint32_t off[kWords];
@@ -1029,14 +1046,14 @@ struct GradParams {
   CUtensorMap tm_rows[2], tm_rows_each[2];       // [T, cols]    box 64 x 64, and 64 x 1
   CUtensorMap tm_terms[2], tm_terms_each[2];     // [T, 3 k16]   box 64 x 64, and 64 x 1
   const int* which;
-  const uint32_t *present, *whole;               // LowJoinParams
+  const uint32_t *present, *whole;               // LowParams
   float* out[2];                                 // dA [S, m, k], dB [S, k, d]; either may be NULL
   float* part;                                   // [splits][S][columns of both, whole tiles][k16], splits > 1
   unsigned* status;
   uint64_t wait_limit_ns;
   int T, S, k, cols[2], tiles[2];                // tiles of an absent product: 0
   int blocks, splits, stages, stage_bytes;
-  int after_join;
+  int after_low;
 };
 constexpr int kGradThreads = 192;
 
@@ -1118,8 +1135,8 @@ __global__ void __launch_bounds__(kGradThreads, 1) adaptor_grad_kernel(const __g
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = warp_uniform(ctl->tmem_base);
-  // The kernel ahead is a gate whatever was asked for, or the join itself (after_join): what the join wrote is there, and nothing here needs the product.
-  if (p.after_join) grid_dependency_wait();
+  // The kernel ahead is the product, a gate: what adaptor_low_kernel wrote is there, and nothing here needs the product. Or (after_low) that kernel itself.
+  if (p.after_low) grid_dependency_wait();
   grid_launch_dependents();
   const uint32_t full0 = smem_u32(&ctl->full[0]), empty0 = smem_u32(&ctl->empty[0]);
 

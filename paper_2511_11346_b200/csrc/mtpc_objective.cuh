@@ -7,13 +7,13 @@
 // Preference: sequences 2p and 2p + 1, h = beta (sum of logp - ref over the one's valid positions - over the other's),
 //   loss = mean of -(1 - s) log sigmoid(h) - s log sigmoid(-h),   slope = +- beta (s - sigmoid(-h)) / pairs.
 //
-// Differences of log-likelihoods are formed in fp64, where none is lost, and rounded for the exponentials; whether a ratio is clipped is decided on the fp64
-// difference, against the logarithms of the ends, since a position beside an end would else change sides by a rounding. All sums are fp64, in an
-// order that sizes fix.
+// Differences of log-likelihoods lose nothing: logp - old as two fp32 terms, of which whether a ratio is clipped is decided against the logarithms of the ends (in two
+// terms as well), since a position beside an end would else change sides by a rounding; those that a pair's sum adds up in fp64. Sums are fp64, the policy loss's of
+// four positions' fp32 ones, in an order that sizes fix.
 //
 // Work is dealt in items: a warp has one of P equal slices of one sequence, so that long sequences among short ones spread over the device and no
 // position has to look for its sequence. Weights need the counts of valid positions first, so the call goes over the data twice (the mask alone
-// for the counts; logp and ref for the sums of pairs). Few positions: all phases in one launch of one cluster, with its barrier between
+// for the counts, every warp over that of its own sequence where that is all it needs; logp and ref for the sums of pairs). Few positions: all phases in one launch of one cluster, with its barrier between
 // them (a chain of four kernels of 2 us each otherwise); many: a launch for each phase. Bound by launches, and by HBM from a million positions on.
 #pragma once
 #include <math_constants.h>
@@ -27,7 +27,7 @@ constexpr uint32_t kStatusBadOffset = 16u;
 constexpr int kObjectiveThreads = 512, kObjectiveWarps = kObjectiveThreads / 32;
 constexpr int kObjectiveCtas = 8;                  // of the cluster that does a small call alone
 constexpr int kSmallItems = 1024;                  // that such a call has at most
-constexpr int kMostBlocks = 148 * 4;               // of a launch for one phase
+constexpr int kMostBlocks = 148 * 2;               // of a launch for one phase: what the device holds at once
 
 struct ObjectiveArgs {
   const float *logp, *old, *ref, *advantage;       // ref: NULL without the KL term; advantage [S], or [T] with by_position (policy)
@@ -35,7 +35,8 @@ struct ObjectiveArgs {
   const int* offsets;                              // [S + 1]
   int T, S, parts;                                 // parts: slices of a sequence
   int by_sequence, by_position;
-  double log_low, log_high;                        // logarithms of the ends
+  int own_count;                                   // every warp counts the valid positions of its sequence itself
+  float log_low[2], log_high[2];                   // logarithms of the ends, in two terms
   float low, high;                                 // the ends: 1 - clip_low, 1 + clip_high
   double beta, smoothing;
   float *loss, *stats, *d_logp, *h;                // stats [3] or NULL; h [S / 2] or NULL
@@ -90,7 +91,6 @@ __device__ __forceinline__ F warp_total(F x) {
 // body(first position, four flags) for every group of four positions that a warp's lanes have of [begin, end): the flags say which are inside and valid.
 template <bool WIDE, typename Body>
 __device__ __forceinline__ void over_slice(const ObjectiveArgs& a, const Slice& c, int lane, Body body) {
-#pragma unroll 2
   for (int q = (c.begin >> 2) + lane; q * 4ll < c.end; q += 32) {
     const int t = q * 4;
     uint32_t valid = 0;
@@ -147,6 +147,26 @@ __device__ __forceinline__ void block_sum(F (&x)[N], F* red) {
     }
   }
 }
+// Bytes that are not zero of mask[begin, end), by a warp.
+__device__ __forceinline__ int count_mask(const uint8_t* mask, int begin, int end, int lane) {
+  int n = 0;
+  auto word = [](uint32_t w) { return __popc((w | ((w & 0x7f7f7f7fu) + 0x7f7f7f7fu)) & 0x80808080u); };
+  const uint8_t *from = mask + begin, *to = mask + end;
+  const uint8_t* first = reinterpret_cast<const uint8_t*>((reinterpret_cast<uintptr_t>(from) + 15) & ~static_cast<uintptr_t>(15));
+  const uint8_t* last = reinterpret_cast<const uint8_t*>(reinterpret_cast<uintptr_t>(to) & ~static_cast<uintptr_t>(15));
+  if (first >= last) {
+    for (const uint8_t* b = from + lane; b < to; b += 32) n += *b != 0;
+  } else {
+    if (from + lane < first) n += from[lane] != 0;
+#pragma unroll 4
+    for (const uint8_t* b = first + 16 * lane; b < last; b += 512) {
+      const uint4 v = *reinterpret_cast<const uint4*>(b);
+      n += word(v.x) + word(v.y) + word(v.z) + word(v.w);
+    }
+    if (last + lane < to) n += last[lane] != 0;
+  }
+  return warp_total(n);
+}
 template <bool WIDE>
 __device__ __forceinline__ void count_phase(const ObjectiveArgs& a, int block, int blocks, int lane, long long* red) {
   const int first = block * kObjectiveWarps + (threadIdx.x >> 5), step = blocks * kObjectiveWarps;
@@ -165,7 +185,6 @@ __device__ __forceinline__ void count_phase(const ObjectiveArgs& a, int block, i
 
 // e^q - 1 - q, and e^q - 1: near zero by the series, whose next term is below 2^-28 of the first; the function less q is off by q's rounding.
 __device__ __forceinline__ void exp_beyond(float q, float& beyond, float& m1) {
-  m1 = expm1f(q);
   if (fabsf(q) < 0.5f) {
     float s = 1.f / 40320.f;
     s = fmaf(s, q, 1.f / 5040.f);
@@ -175,9 +194,17 @@ __device__ __forceinline__ void exp_beyond(float q, float& beyond, float& m1) {
     s = fmaf(s, q, 1.f / 6.f);
     s = fmaf(s, q, 0.5f);
     beyond = q * q * s;
+    m1 = q + beyond;
   } else {
+    m1 = expm1f(q);
     beyond = m1 - q;
   }
+}
+// a - b as the nearest fp32 value and what it leaves (exactly, but for infinities): conversions to fp64 and back would be most of the kernel's time.
+__device__ __forceinline__ float difference(float a, float b, float& rest) {
+  const float d = __fsub_rn(a, b), back = __fadd_rn(d, b);
+  rest = __fsub_rn(__fsub_rn(a, back), __fsub_rn(b, __fsub_rn(back, d)));
+  return d;
 }
 
 // total: all valid positions.
@@ -190,10 +217,22 @@ __device__ __forceinline__ void policy_phase(const ObjectiveArgs& a, int block, 
     long long n = total;
     if (a.by_sequence) {
       const Span x = span_of(a, c.s);
-      int mine = a.mask == nullptr && lane == 0 ? x.end - x.begin : 0;
-      if (a.mask != nullptr)
-        for (int q = lane; q < a.parts; q += 32) mine += a.count[c.s * a.parts + q];
-      n = static_cast<long long>(warp_total(mine)) * a.S;
+      int here = x.end - x.begin;
+      if (a.own_count) {
+        // (the slice's values come from memory meanwhile, a line of 32 to a lane)
+        for (int t = (c.begin & ~31) + 32 * lane; t < c.end; t += 32 * 32) {
+          const int at = max(t, c.begin);
+          prefetch_l2(a.logp + at);
+          prefetch_l2(a.old + at);
+          if (a.ref != nullptr) prefetch_l2(a.ref + at);
+        }
+        here = count_mask(a.mask, x.begin, x.end, lane);
+      } else if (a.mask != nullptr) {
+        here = 0;
+        for (int q = lane; q < a.parts; q += 32) here += a.count[c.s * a.parts + q];
+        here = warp_total(here);
+      }
+      n = static_cast<long long>(here) * a.S;
     }
     const double weight = n > 0 ? 1.0 / static_cast<double>(n) : 0.0;
     const float w = static_cast<float>(weight), beta = static_cast<float>(a.beta);
@@ -202,7 +241,7 @@ __device__ __forceinline__ void policy_phase(const ObjectiveArgs& a, int block, 
     double value = 0.0, kl = 0.0;
     int clipped = 0;
     over_slice<WIDE>(a, c, lane, [&](int t, uint32_t valid, bool inside) {
-      float lp[4], old[4], ref[4], g[4];
+      float lp[4], old[4], ref[4], g[4], value4 = 0.f, kl4 = 0.f;
       load4<WIDE>(a.logp, t, inside, valid, lp);
       load4<WIDE>(a.old, t, inside, valid, old);
       if (a.ref != nullptr) load4<WIDE>(a.ref, t, inside, valid, ref);
@@ -210,23 +249,28 @@ __device__ __forceinline__ void policy_phase(const ObjectiveArgs& a, int block, 
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float adv = adv4[i];
-        const double diff = static_cast<double>(lp[i]) - static_cast<double>(old[i]);
-        const float r = expf(static_cast<float>(diff));
-        const bool up = adv > 0.f && diff > a.log_high, down = adv < 0.f && diff < a.log_low, out = up || down;
-        const float gain = adv == 0.f ? 0.f : (up ? a.high : down ? a.low : r) * adv;
+        float rest;
+        const float diff = difference(lp[i], old[i], rest), r = expf(diff);
+        // beyond the end that counts for this sign: (diff + rest) - logarithm, the first difference without rounding where it decides
+        const float end = adv > 0.f ? a.log_high[0] : a.log_low[0], end_rest = adv > 0.f ? a.log_high[1] : a.log_low[1];
+        const float over = fabsf(diff) < CUDART_INF_F ? (diff - end) + (rest - end_rest) : diff;
+        const bool out = adv > 0.f ? over > 0.f : adv < 0.f && over < 0.f;
+        const float gain = adv == 0.f ? 0.f : (out ? (adv > 0.f ? a.high : a.low) : r) * adv;
         float slope = out || adv == 0.f ? 0.f : -gain, beyond = 0.f, m1 = 0.f;
         if (a.ref != nullptr) {
-          exp_beyond(static_cast<float>(static_cast<double>(ref[i]) - static_cast<double>(lp[i])), beyond, m1);
+          exp_beyond(ref[i] - lp[i], beyond, m1);
           slope = fmaf(-beta, m1, slope);
         }
         const bool counts = valid >> i & 1;
         g[i] = counts ? w * slope : 0.f;
         if (counts) {
-          value -= static_cast<double>(gain);
-          kl += static_cast<double>(beyond);
+          value4 -= gain;
+          kl4 += beyond;
           clipped += out ? 1 : 0;
         }
       }
+      value += static_cast<double>(value4);
+      kl += static_cast<double>(kl4);
       store4<WIDE>(a.d_logp, c, t, inside, g);
     });
     value = warp_total(value);
@@ -381,7 +425,7 @@ __global__ void __launch_bounds__(kObjectiveThreads) policy_cluster_kernel(Objec
   grid_launch_dependents();
   cluster_sync_all();                              // the first CTA is there
   grid_dependency_wait();
-  if (a.mask != nullptr) {
+  if (a.mask != nullptr && !a.own_count) {
     count_phase<WIDE>(a, rank, kObjectiveCtas, lane, reinterpret_cast<long long*>(red));
     cluster_sync_all();
   }
@@ -418,7 +462,7 @@ __global__ void __launch_bounds__(kObjectiveThreads) count_kernel(const Objectiv
   count_phase<WIDE>(a, blockIdx.x, gridDim.x, threadIdx.x & 31, red);
 }
 template <bool WIDE>
-__global__ void __launch_bounds__(kObjectiveThreads) policy_kernel(const ObjectiveArgs a) {
+__global__ void __launch_bounds__(kObjectiveThreads, 2) policy_kernel(const ObjectiveArgs a) {
   __shared__ double red[3 * kObjectiveWarps];
   grid_launch_dependents();
   grid_dependency_wait();

@@ -36,16 +36,16 @@ void launch_dropout(const DropoutArgs& a, bool vectors, cudaStream_t st) {
 // ---------------------------------------------------------------- losses
 constexpr int kMaxSequences = 1 << 20;
 constexpr int kSmallPositions = 1 << 16;
+constexpr int kOwnCount = 1 << 14;      // mean length up to which a sequence's positions are counted by each of its warps: 16 vectors a lane
 struct ObjectivePlan {
   int parts;
   bool small;                           // one cluster does it, without a workspace
   size_t off_count, off_blocks, off_sum, off_term, off_slope, total;
 };
-// Slices of about 256 positions (two of a lane's vectors), so that a million positions are 4000 warps; of a small call about 128, for the warps of its cluster.
+// Slices for every warp that the device holds at once, of 128 positions (a vector of a lane) at least; of a small call for those of its cluster.
 void plan_objective(int T, int S, ObjectivePlan* p) {
-  const int share = T <= kSmallPositions ? 128 : 256;
-  p->parts = std::max(1, std::min(ceil_div(T, static_cast<long long>(S) * share), 1 << 16));
-  if (T <= kSmallPositions) p->parts = std::max(1, std::min(p->parts, kSmallItems / S));
+  const int most = T <= kSmallPositions ? kSmallItems : kMostBlocks * kObjectiveWarps;
+  p->parts = std::max(1, std::min(ceil_div(T, static_cast<long long>(S) * 128), most / S));
   const size_t items = static_cast<size_t>(S) * p->parts;
   p->small = T <= kSmallPositions && items <= kSmallItems;
   p->total = 0;
@@ -63,6 +63,10 @@ int check_sequences(int T, int S) {
   if (T < 0 || S < 1) return MTPC_ERR_SHAPE;
   if (T > kMaxRows || S > kMaxSequences) return MTPC_ERR_UNSUPPORTED;
   return MTPC_OK;
+}
+void two_terms(double x, float* y) {
+  y[0] = static_cast<float>(x);
+  y[1] = isinf(y[0]) ? 0.f : static_cast<float>(x - y[0]);
 }
 bool a_share(float x) { return x >= 0.f && x <= 1.f; }      // (no NaN)
 void carve(const ObjectivePlan& p, void* workspace, ObjectiveArgs* a) {
@@ -82,7 +86,7 @@ void launch_policy(const ObjectiveArgs& a, bool small, cudaStream_t st) {
     launch_clusters(policy_cluster_kernel<WIDE>, kObjectiveCtas, kObjectiveCtas, kObjectiveThreads, 0, st, true, a);
     return;
   }
-  if (a.mask) launch_kernel(count_kernel<WIDE>, item_blocks(a), kObjectiveThreads, 0, st, true, a);
+  if (a.mask && !a.own_count) launch_kernel(count_kernel<WIDE>, item_blocks(a), kObjectiveThreads, 0, st, true, a);
   launch_kernel(policy_kernel<WIDE>, item_blocks(a), kObjectiveThreads, 0, st, true, a);
   launch_kernel(policy_final_kernel, 1, kObjectiveThreads, 0, st, true, a, item_blocks(a));
 }
@@ -181,10 +185,11 @@ int mtpc_policy_loss(const float* logp, const float* old_logp, const float* ref_
   a.T = T;
   a.S = S;
   a.by_sequence = by_sequence != 0;
+  a.own_count = a.by_sequence && mask && T / S <= kOwnCount;
   a.low = static_cast<float>(1.0 - static_cast<double>(clip_low));
   a.high = static_cast<float>(1.0 + static_cast<double>(clip_high));
-  a.log_low = clip_low < 1.f ? log1p(-static_cast<double>(clip_low)) : -INFINITY;
-  a.log_high = log1p(static_cast<double>(clip_high));
+  two_terms(clip_low < 1.f ? log1p(-static_cast<double>(clip_low)) : -INFINITY, a.log_low);
+  two_terms(log1p(static_cast<double>(clip_high)), a.log_high);
   a.beta = beta;
   a.loss = out_loss;
   a.stats = out_stats;
