@@ -449,6 +449,7 @@ int mtpc_adapted_projection_backward(const void* x_low, int64_t x_low_stride, co
   p.present = l.present;
   p.whole = l.whole;
   p.after_low = !d_x && !d_x_low;
+  p.wide_a = k % 8 == 0 && aligned(dA, 32);
   p.out[0] = dA;
   p.out[1] = dB;
   p.part = reinterpret_cast<float*>(ws + plan.off_grad);
@@ -468,8 +469,7 @@ int mtpc_adapted_projection_backward(const void* x_low, int64_t x_low_stride, co
     if (!p.tiles[q]) continue;
     const Rows& r = q ? xr : gr;
     const __nv_bfloat16* terms = q ? v3 : low3;
-    if ((rc = map_rows(&p.tm_rows[q], r.p, T, p.cols[q], r.stride, 64)) != MTPC_OK || (rc = map_rows(&p.tm_rows_each[q], r.p, T, p.cols[q], r.stride, 1)) != MTPC_OK ||
-        (rc = map_rows(&p.tm_terms[q], terms, T, 3 * k16, 3 * k16, 64)) != MTPC_OK || (rc = map_rows(&p.tm_terms_each[q], terms, T, 3 * k16, 3 * k16, 1)) != MTPC_OK)
+    if ((rc = map_rows(&p.tm_rows[q], r.p, T, p.cols[q], r.stride, 64)) != MTPC_OK || (rc = map_rows(&p.tm_terms[q], terms, T, 3 * k16, 3 * k16, 64)) != MTPC_OK)
       return rc;
   }
   p.stage_bytes = kABytes + ceil_div(3 * k16, 64) * static_cast<int>(kMnBoxBytes);

@@ -52,17 +52,6 @@ __device__ __forceinline__ void tma_load_3d_pair(uint32_t lead, uint32_t dst_sme
       "l"(reinterpret_cast<uint64_t>(tm)), "r"(cluster_bar), "r"(x), "r"(y), "r"(z), "r"(lead)
       : "memory");
 }
-// Four rows of a matrix wherever they lie (rows past the last: zeros), one below the other. The map's box is one row high.
-__device__ __forceinline__ void tma_gather4(uint32_t lead, uint32_t dst_smem, const CUtensorMap* tm, uint32_t bar, int32_t x, const int32_t (&row)[4]) {
-  asm volatile(
-      "{\n"
-      ".reg .pred e;\n"
-      "setp.ne.b32 e, %8, 0;\n"
-      "@e cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];\n"
-      "}\n" ::"r"(dst_smem),
-      "l"(reinterpret_cast<uint64_t>(tm)), "r"(bar), "r"(x), "r"(row[0]), "r"(row[1]), "r"(row[2]), "r"(row[3]), "r"(lead)
-      : "memory");
-}
 // The MMA that leaves accumulator rows alone: bit l of off[w] is TMEM lane 32 w + l (pairs: words 4 to 7 are the peer's lanes).
 __device__ __forceinline__ void umma_bf16_rows(uint32_t lead, uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate,
                                                const uint32_t (&off)[4]) {
@@ -174,6 +163,8 @@ constexpr int kLowThreads = 192;
 constexpr int kLowStageBytes = kABytes + kMaxRank * kBlockK * 2;
 constexpr int kLowSlots = 4, kLowSlotCols = kMaxRank, kLowTmemCols = kLowSlots * kLowSlotCols;
 constexpr int kGivenQuads = 4;          // of a thread
+// Adaptors whose factors share a stage with a tile of the rows, so that the rows are read once for them (K-major factors; 300 rows of 64 requests: a pass for every four).
+__host__ __device__ constexpr int low_group(int k16, bool mn) { return mn ? 1 : kMaxRank / k16; }
 
 // x as a sum of bf16 values: the nearest, and the nearest to what is left (twice, where a third is wanted). A value that is not finite keeps its first.
 __device__ __forceinline__ void split_terms(float x, __nv_bfloat16& hi, __nv_bfloat16& mid, __nv_bfloat16& lo) {
@@ -284,24 +275,37 @@ __global__ void __launch_bounds__(kLowThreads, 2) adaptor_low_kernel(const __gri
   const bool none = ta.none();
   int adaptor = 0;
   uint32_t off[4];
+  const int group = low_group(p.k16, F_MN);
+  const uint32_t f_bytes = F_MN ? kMnBoxBytes : static_cast<uint32_t>(p.k16) * (kBlockK * 2);
 
   if (none) {
   } else if (warp == 0) {
     const uint32_t lead = elect_one();
-    const uint32_t f_bytes = F_MN ? kMnBoxBytes : static_cast<uint32_t>(p.k16) * (kBlockK * 2);
     uint32_t stage = 0, phase = 0, issued = 0;
     bool ok = true;
     for (int c = rank; c < p.chunks && ok; c += p.split) {
       const int kb0 = c * kChunkBlocks, kb1 = min(p.kblocks, kb0 + kChunkBlocks);
       TileAdaptors<4> each = ta;
-      while (ok && each.next(adaptor, off)) {
+      while (ok) {
+        int of[4], n = 0;
+        while (n < group && each.next(adaptor, off)) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            if (q == n) of[q] = adaptor;
+          ++n;
+        }
+        if (n == 0) break;
         for (int kb = kb0; kb < kb1; ++kb) {
           if (!bounded_wait_all(empty0 + 8 * stage, phase ^ 1u, ctl, p)) { ok = false; break; }
           const uint32_t full = full0 + 8 * stage, a_dst = tiles_addr + stage * kLowStageBytes;
-          mbar_arrive_expect_tx(lead, full, kABytes + f_bytes);
+          mbar_arrive_expect_tx(lead, full, kABytes + n * f_bytes);
           tma_load_2d(lead, a_dst, &p.tm_a, full, kb * kBlockK, row0);
-          if (F_MN) tma_load_3d(lead, a_dst + kABytes, &p.tm_f, full, 0, kb * kBlockK, adaptor);
-          else tma_load_3d(lead, a_dst + kABytes, &p.tm_f, full, kb * kBlockK, 0, adaptor);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            if (q >= n) break;
+            if (F_MN) tma_load_3d(lead, a_dst + kABytes, &p.tm_f, full, 0, kb * kBlockK, of[q]);
+            else tma_load_3d(lead, a_dst + kABytes + q * f_bytes, &p.tm_f, full, kb * kBlockK, 0, of[q]);
+          }
           ++issued;
           if (++stage == static_cast<uint32_t>(p.stages)) { stage = 0; phase ^= 1u; }
         }
@@ -324,14 +328,27 @@ __global__ void __launch_bounds__(kLowThreads, 2) adaptor_low_kernel(const __gri
       tc_fence_after();
       const uint32_t d_tmem = tmem_base + slot * kLowSlotCols;
       TileAdaptors<4> each = ta;
-      while (ok && each.next(adaptor, off)) {
+      while (ok) {
+        uint32_t offs[4][4];
+        int n = 0;
+        while (n < group && each.next(adaptor, off)) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            if (q == n) offs[q][0] = off[0], offs[q][1] = off[1], offs[q][2] = off[2], offs[q][3] = off[3];
+          ++n;
+        }
+        if (n == 0) break;
         for (int kb = kb0; kb < kb1; ++kb) {
           if (!bounded_wait_all(full0 + 8 * stage, phase, ctl, p)) { ok = false; break; }
           tc_fence_after();
           const uint64_t a_desc = a_desc0 + stage * (kLowStageBytes >> 4), f_desc = f_desc0 + stage * (kLowStageBytes >> 4);
 #pragma unroll
-          for (int kk = 0; kk < kBlockK / 16; ++kk)
-            umma_bf16_rows(lead, d_tmem, a_desc + 2 * kk, f_desc + kStepF * kk, idesc, (kb != kb0 || kk != 0) ? 1u : 0u, off);
+          for (int q = 0; q < 4; ++q) {
+            if (q >= n) break;
+#pragma unroll
+            for (int kk = 0; kk < kBlockK / 16; ++kk)
+              umma_bf16_rows(lead, d_tmem, a_desc + 2 * kk, f_desc + q * (f_bytes >> 4) + kStepF * kk, idesc, (kb != kb0 || kk != 0) ? 1u : 0u, offs[q]);
+          }
           umma_commit(lead, empty0 + 8 * stage);
           if (++stage == static_cast<uint32_t>(p.stages)) { stage = 0; phase ^= 1u; }
         }
@@ -1043,8 +1060,8 @@ __global__ void __launch_bounds__(kRowsThreads) adapted_rows_kernel(const __grid
 // dA (product 0: rows g, terms of low) and dB (product 1: rows x', terms of v): 128 columns of the rows are the MMA's M, the 3 k16 terms its N, rows its K. An item is
 // one tile of columns of one adaptor over one of `splits` runs of row blocks; every eight blocks the accumulators are added to fp32 registers.
 struct GradParams {
-  CUtensorMap tm_rows[2], tm_rows_each[2];       // [T, cols]    box 64 x 64, and 64 x 1
-  CUtensorMap tm_terms[2], tm_terms_each[2];     // [T, 3 k16]   box 64 x 64, and 64 x 1
+  CUtensorMap tm_rows[2];                        // [T, cols]    box 64 x 64
+  CUtensorMap tm_terms[2];                       // [T, 3 k16]   box 64 x 64
   const int* which;
   const uint32_t *present, *whole;               // LowParams
   float* out[2];                                 // dA [S, m, k], dB [S, k, d]; either may be NULL
@@ -1053,7 +1070,7 @@ struct GradParams {
   uint64_t wait_limit_ns;
   int T, S, k, cols[2], tiles[2];                // tiles of an absent product: 0
   int blocks, splits, stages, stage_bytes;
-  int after_low;
+  int after_low, wide_a;                         // wide_a: rows of dA are vectors of eight
 };
 constexpr int kGradThreads = 192;
 
@@ -1151,33 +1168,13 @@ __global__ void __launch_bounds__(kGradThreads, 1) adaptor_grad_kernel(const __g
       walk.start(p, g);
       while (walk.next(p, g)) {
         const int t0 = walk.block * 64;
-        const bool whole = walk.whole();
-        int at[4] = {0, 0, 0, 0};
-        if (!whole) {                   // lanes below 16 have four rows each; a row of another adaptor (or none) is read past the last: zeros
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const int t = t0 + 4 * (lane & 15) + q;
-            at[q] = adaptor_of(p.which, p.S, t, p.T) == g.adaptor ? t : p.T;
-          }
-        }
         if (!bounded_wait_all(empty0 + 8 * stage, phase ^ 1u, ctl, p)) { ok = false; break; }
         const uint32_t full = full0 + 8 * stage, dst = tiles_addr + stage * p.stage_bytes;
         mbar_arrive_expect_tx(lead, full, kABytes + kTermBoxes * kMnBoxBytes);
-        __syncwarp();
-        if (whole) {
 #pragma unroll
-          for (int q = 0; q < 2; ++q) tma_load_2d(lead, dst + q * kMnBoxBytes, rows, full, g.tile * kBlockM + q * 64, t0);
+        for (int q = 0; q < 2; ++q) tma_load_2d(lead, dst + q * kMnBoxBytes, rows, full, g.tile * kBlockM + q * 64, t0);
 #pragma unroll
-          for (int q = 0; q < kTermBoxes; ++q) tma_load_2d(lead, dst + kABytes + q * kMnBoxBytes, terms, full, q * 64, t0);
-        } else {
-          const uint32_t one = lane < 16 ? 1u : 0u;
-#pragma unroll
-          for (int q = 0; q < 2; ++q)
-            tma_gather4(one, dst + q * kMnBoxBytes + lane * 512, &p.tm_rows_each[g.product], full, g.tile * kBlockM + q * 64, at);
-#pragma unroll
-          for (int q = 0; q < kTermBoxes; ++q)
-            tma_gather4(one, dst + kABytes + q * kMnBoxBytes + lane * 512, &p.tm_terms_each[g.product], full, q * 64, at);
-        }
+        for (int q = 0; q < kTermBoxes; ++q) tma_load_2d(lead, dst + kABytes + q * kMnBoxBytes, terms, full, q * 64, t0);
         ++issued;
         if (++stage == static_cast<uint32_t>(p.stages)) { stage = 0; phase ^= 1u; }
       }
@@ -1203,7 +1200,33 @@ __global__ void __launch_bounds__(kGradThreads, 1) adaptor_grad_kernel(const __g
           if (!bounded_wait_all(smem_u32(&ctl->tempty[slot]), ((use / kSlots) & 1u) ^ 1u, ctl, p)) { ok = false; break; }
           ++use;
         }
+        const bool whole = walk.whole();
+        bool foreign[2] = {false, false};                            // rows lane and lane + 32 of the block
+        if (!whole) {
+#pragma unroll
+          for (int q = 0; q < 2; ++q) foreign[q] = adaptor_of(p.which, p.S, walk.block * 64 + 32 * q + lane, p.T) != g.adaptor;
+        }
         if (!bounded_wait_all(full0 + 8 * stage, phase, ctl, p)) { ok = false; break; }
+        if (!whole) {
+          // rows of other adaptors, which may hold anything, become zeros in both operands where they landed: a row is 128 bytes of every box
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            uint32_t rows = __ballot_sync(0xffffffffu, foreign[q]);
+            while (rows != 0) {                                      // four rows at a time, eight lanes each
+              uint32_t mine = rows;
+              for (int e = 0; e < lane / 8; ++e) mine &= mine - 1;
+              if (mine != 0) {
+                const uint32_t at = tiles_addr + stage * p.stage_bytes + (32 * q + __ffs(mine) - 1) * 128 + (lane & 7) * 16;
+#pragma unroll
+                for (int box = 0; box < 2 + kTermBoxes; ++box) st_shared_v4(at + box * kMnBoxBytes, 0, 0, 0, 0);
+              }
+#pragma unroll
+              for (int e = 0; e < 4; ++e) rows &= rows - 1;
+            }
+          }
+          fence_proxy_async_shared();
+          __syncwarp();
+        }
         tc_fence_after();
         const uint64_t a_desc = a_desc0 + stage * stage_step, b_desc = b_desc0 + stage * stage_step;
 #pragma unroll
@@ -1261,6 +1284,11 @@ __global__ void __launch_bounds__(kGradThreads, 1) adaptor_grad_kernel(const __g
         float* dst = p.part + ((static_cast<size_t>(g.split) * p.S + g.adaptor) * all + (g.product ? p.tiles[0] * kBlockM : 0) + col) * K16;
 #pragma unroll
         for (int j = 0; j < K16; j += 8) st_global_v8(dst + j, acc + j);
+      } else if (col < cols && g.product == 0 && p.wide_a) {
+        float* dst = p.out[0] + (static_cast<size_t>(g.adaptor) * cols + col) * p.k;
+#pragma unroll
+        for (int j = 0; j < K16; j += 8)
+          if (j < p.k) st_global_v8(dst + j, acc + j);
       } else if (col < cols) {
 #pragma unroll
         for (int j = 0; j < K16; ++j) {
