@@ -79,13 +79,13 @@ void plan_forward(int T, int d, int m, int k, int S, bool copies, ForwardPlan* p
 }
 
 // Runs of row blocks that the adaptors' gradients are cut into: what takes least, a run being its blocks and about four more for its start and end. An adaptor's
-// rows lie beside each other, so that up to S runs cut few adaptors' rows (n: runs that have rows).
+// rows lie beside each other, so that up to S runs cut few adaptors' rows (n: runs that have rows); adding the runs up takes a quarter of a block each.
 int grad_splits(int tiles, int S, int blocks) {
   int best = 1;
   double least = 0.0;
   for (int s = 1; s <= 32 && s <= std::max(1, blocks / 4); ++s) {
     const int n = std::max(s, S);
-    const double cost = static_cast<double>(ceil_div(static_cast<long long>(tiles) * n, kSms)) * (static_cast<double>(blocks) / n + 4.0);
+    const double cost = static_cast<double>(ceil_div(static_cast<long long>(tiles) * n, kSms)) * (static_cast<double>(blocks) / n + 4.0) + 0.25 * s;
     if (s == 1 || cost < least * 0.97) best = s, least = cost;
   }
   return best;
@@ -189,20 +189,24 @@ int launch_low(LowParams& p, const Rows& rows, const Rows& factors, bool mn, con
   p.k16 = rank16(k);
   p.pieces = pieces_of(k);
   p.split = 1;
-  p.stages = stages_of(kLowStageBytes, 2);
+  // K-major factors of several adaptors fit where one of the largest rank does; MN-major ones are boxes of 8 KB whatever the rank, so that more of them are worth their place
+  // where a tile has several requests (129 rows of eight: 45 -> 33 us for all gradients) and cost it where it has one (8192 of one: 16 -> 19).
+  const bool many = static_cast<int64_t>(S) * kBlockM > T;
+  p.group = mn ? (many ? 4 : 1) : kMaxRank / p.k16;
+  p.stage_bytes = kABytes + (mn ? p.group : 1) * static_cast<int>(kMnBoxBytes);
+  p.stages = stages_of(p.stage_bytes, p.stage_bytes > 32768 ? 1 : 2);
+  p.tiles = ceil_div(T, kBlockM);
   if (rows.p) {
     int rc = map_rows(&p.tm_a, rows.p, T, K, rows.stride, kBlockM);
     if (rc == MTPC_OK) rc = mn ? map_rows(&p.tm_f, factors.p, K, k, factors.stride, 64, S) : map_rows(&p.tm_f, factors.p, k, K, factors.stride, rank16(k), S);
     if (rc != MTPC_OK) return rc;
     p.kblocks = ceil_div(K, kBlockK);
     p.chunks = chunks_of(K);
-    p.tiles = ceil_div(T, kBlockM);
     while (p.split < 8 && p.split * 2 <= p.chunks && p.tiles * p.split <= kSms) p.split *= 2;
   }
-  p.given_blocks = p.given ? ceil_div(static_cast<long long>(T) * (p.k16 / 4), kLowThreads * kGivenQuads) : 0;
   p.present_blocks = p.present ? ceil_div(T, 32 * 64) : 0;
-  const int beside = ceil_div(p.given_blocks + p.present_blocks, p.split) * p.split;
-  const size_t smem = kControl + static_cast<size_t>(p.stages) * kLowStageBytes;
+  const int beside = ceil_div(p.present_blocks, p.split) * p.split;
+  const size_t smem = kControl + static_cast<size_t>(p.stages) * p.stage_bytes;
   launch_clusters(mn ? adaptor_low_kernel<true> : adaptor_low_kernel<false>, p.split, p.tiles * p.split + beside, kLowThreads, smem, st, true, p);
   return check_launch();
 }
@@ -473,8 +477,8 @@ int mtpc_adapted_projection_backward(const void* x_low, int64_t x_low_stride, co
       return rc;
   }
   p.stage_bytes = kABytes + ceil_div(3 * k16, 64) * static_cast<int>(kMnBoxBytes);
-  p.stages = stages_of(p.stage_bytes);
-  const size_t smem = kControl + static_cast<size_t>(p.stages) * p.stage_bytes;
+  p.stages = stages_of(p.stage_bytes, 1, kGradWords * 8);
+  const size_t smem = kControl + kGradWords * 8 + static_cast<size_t>(p.stages) * p.stage_bytes;
   auto* kernel = k16 == 16 ? adaptor_grad_kernel<16> : k16 == 32 ? adaptor_grad_kernel<32> : k16 == 48 ? adaptor_grad_kernel<48> : adaptor_grad_kernel<64>;
   const long long items = static_cast<long long>(p.tiles[0] + p.tiles[1]) * S * p.splits;
   launch_kernel(kernel, static_cast<int>(std::min<long long>(items, kSms)), kGradThreads, smem, st, true, p);

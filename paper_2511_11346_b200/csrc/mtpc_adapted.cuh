@@ -141,7 +141,7 @@ struct TileAdaptors {
 
 // ---- low (or v) of many rows
 // A cluster has a tile of 128 rows; its CTAs share the chunks of K, add theirs up in registers and meet in shared memory, where each finishes its share of the rows:
-// sum, scale, low, its terms. Blocks behind the tiles' (if asked for) split given values into terms, and say which blocks of 64 rows have an adaptor's rows.
+// sum, scale, low, its terms. For the gradients it splits given values into terms as well, and blocks behind the tiles' say which 64 rows have an adaptor's.
 struct LowParams {
   CUtensorMap tm_a;                     // rows [T, K]          box 64 x 128
   CUtensorMap tm_f;                     // factors: B [S, k, K] box 64 x k16 (K-major), or A [S, K, k] box 64 x 64 (MN-major)
@@ -156,16 +156,12 @@ struct LowParams {
   unsigned* status;                     // or NULL
   uint64_t wait_limit_ns;
   int T, S, k, k16, pieces;             // k16: the rank, rounded up to 16
-  int kblocks, chunks, tiles, split, stages;       // split: CTAs of a cluster; tiles 0: no sums are wanted
-  int given_blocks, present_blocks;
+  int kblocks, chunks, tiles, split, stages, stage_bytes;            // split: CTAs of a cluster; chunks 0: no sums are wanted
+  int group;                            // adaptors (at most four) whose factors share a stage with a tile of the rows: the rows are read once for them
+  int present_blocks;
 };
 constexpr int kLowThreads = 192;
-constexpr int kLowStageBytes = kABytes + kMaxRank * kBlockK * 2;
 constexpr int kLowSlots = 4, kLowSlotCols = kMaxRank, kLowTmemCols = kLowSlots * kLowSlotCols;
-constexpr int kGivenQuads = 4;          // of a thread
-// Adaptors whose factors share a stage with a tile of the rows, so that the rows are read once for them (K-major factors; 300 rows of 64 requests: a pass for every four).
-__host__ __device__ constexpr int low_group(int k16, bool mn) { return mn ? 1 : kMaxRank / k16; }
-
 // x as a sum of bf16 values: the nearest, and the nearest to what is left (twice, where a third is wanted). A value that is not finite keeps its first.
 __device__ __forceinline__ void split_terms(float x, __nv_bfloat16& hi, __nv_bfloat16& mid, __nv_bfloat16& lo) {
   hi = __float2bfloat16_rn(x);
@@ -191,13 +187,12 @@ __device__ __forceinline__ void store_terms(const LowParams& p, int t, int j0, c
     *reinterpret_cast<uint2*>(dst + 2 * p.k16) = lv;
   }
 }
-__device__ __forceinline__ void given_terms(const LowParams& p, int block) {
-  const int quads = p.k16 / 4;
-#pragma unroll
-  for (int e = 0; e < kGivenQuads; ++e) {
-    const long long at = (static_cast<long long>(block) * kGivenQuads + e) * kLowThreads + threadIdx.x;
-    const int t = static_cast<int>(at / quads), j0 = static_cast<int>(at - static_cast<long long>(t) * quads) * 4;
-    if (t >= p.T) return;
+// The terms of given values of rows [t0, t1), by the 128 threads of the epilogue.
+__device__ __forceinline__ void given_terms(const LowParams& p, int t0, int t1, int thread) {
+  const int quads = p.k16 / 4, all = (min(t1, p.T) - t0) * quads;
+#pragma unroll 4
+  for (int at = thread; at < all; at += 128) {
+    const int t = t0 + at / quads, j0 = at % quads * 4;
     const bool any = adaptor_of(p.which, p.S, t, p.T) >= 0;
     float x[4];
 #pragma unroll
@@ -232,11 +227,10 @@ __global__ void __launch_bounds__(kLowThreads, 2) adaptor_low_kernel(const __gri
     grid_dependency_wait();
     grid_launch_dependents();
     const int block = blockIdx.x - p.tiles * p.split;
-    if (block < p.given_blocks) given_terms(p, block);
-    else if (block < p.given_blocks + p.present_blocks) present_rows(p, block - p.given_blocks, reinterpret_cast<uint32_t*>(smem_raw));
+    if (block < p.present_blocks) present_rows(p, block, reinterpret_cast<uint32_t*>(smem_raw));
     return;
   }
-  GemmControl* ctl = reinterpret_cast<GemmControl*>(smem_raw + (tiles_addr - raw_addr) + static_cast<size_t>(p.stages) * kLowStageBytes);
+  GemmControl* ctl = reinterpret_cast<GemmControl*>(smem_raw + (tiles_addr - raw_addr) + static_cast<size_t>(p.stages) * p.stage_bytes);
   const int warp = static_cast<int>(warp_uniform(threadIdx.x >> 5));
   const int lane = threadIdx.x & 31;
   const int tile = blockIdx.x / p.split, rank = blockIdx.x - tile * p.split, row0 = tile * kBlockM;
@@ -253,8 +247,10 @@ __global__ void __launch_bounds__(kLowThreads, 2) adaptor_low_kernel(const __gri
     ctl->abort = 0;
     ctl->wait_limit_ns = p.wait_limit_ns;
     fence_mbar_init();
-    tma_prefetch_desc(&p.tm_a);
-    tma_prefetch_desc(&p.tm_f);
+    if (p.chunks > 0) {
+      tma_prefetch_desc(&p.tm_a);
+      tma_prefetch_desc(&p.tm_f);
+    }
   }
   if (warp == 1) {
     tmem_alloc(smem_u32(&ctl->tmem_base), kLowTmemCols);
@@ -275,10 +271,11 @@ __global__ void __launch_bounds__(kLowThreads, 2) adaptor_low_kernel(const __gri
   const bool none = ta.none();
   int adaptor = 0;
   uint32_t off[4];
-  const int group = low_group(p.k16, F_MN);
+  const int group = p.group;
   const uint32_t f_bytes = F_MN ? kMnBoxBytes : static_cast<uint32_t>(p.k16) * (kBlockK * 2);
 
-  if (none) {
+  if (warp >= 2 && p.given != nullptr) given_terms(p, row0 + rank * (kBlockM / p.split), row0 + (rank + 1) * (kBlockM / p.split), threadIdx.x - 64);
+  if (none || p.chunks == 0) {
   } else if (warp == 0) {
     const uint32_t lead = elect_one();
     uint32_t stage = 0, phase = 0, issued = 0;
@@ -297,13 +294,13 @@ __global__ void __launch_bounds__(kLowThreads, 2) adaptor_low_kernel(const __gri
         if (n == 0) break;
         for (int kb = kb0; kb < kb1; ++kb) {
           if (!bounded_wait_all(empty0 + 8 * stage, phase ^ 1u, ctl, p)) { ok = false; break; }
-          const uint32_t full = full0 + 8 * stage, a_dst = tiles_addr + stage * kLowStageBytes;
+          const uint32_t full = full0 + 8 * stage, a_dst = tiles_addr + stage * p.stage_bytes;
           mbar_arrive_expect_tx(lead, full, kABytes + n * f_bytes);
           tma_load_2d(lead, a_dst, &p.tm_a, full, kb * kBlockK, row0);
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             if (q >= n) break;
-            if (F_MN) tma_load_3d(lead, a_dst + kABytes, &p.tm_f, full, 0, kb * kBlockK, of[q]);
+            if (F_MN) tma_load_3d(lead, a_dst + kABytes + q * f_bytes, &p.tm_f, full, 0, kb * kBlockK, of[q]);
             else tma_load_3d(lead, a_dst + kABytes + q * f_bytes, &p.tm_f, full, kb * kBlockK, 0, of[q]);
           }
           ++issued;
@@ -341,7 +338,7 @@ __global__ void __launch_bounds__(kLowThreads, 2) adaptor_low_kernel(const __gri
         for (int kb = kb0; kb < kb1; ++kb) {
           if (!bounded_wait_all(full0 + 8 * stage, phase, ctl, p)) { ok = false; break; }
           tc_fence_after();
-          const uint64_t a_desc = a_desc0 + stage * (kLowStageBytes >> 4), f_desc = f_desc0 + stage * (kLowStageBytes >> 4);
+          const uint64_t a_desc = a_desc0 + stage * (p.stage_bytes >> 4), f_desc = f_desc0 + stage * (p.stage_bytes >> 4);
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             if (q >= n) break;
@@ -391,7 +388,7 @@ __global__ void __launch_bounds__(kLowThreads, 2) adaptor_low_kernel(const __gri
   __syncthreads();
   cluster_sync_all();                                                // the other CTAs' sums
   const int quads = p.k16 / 4, rows = kBlockM / p.split;
-  for (int at = threadIdx.x; at < rows * quads; at += kLowThreads) {
+  for (int at = threadIdx.x; at < (p.chunks > 0 ? rows * quads : 0); at += kLowThreads) {
     const int r = at / quads, j0 = (at - r * quads) * 4, row = rank * rows + r, t = row0 + row;
     if (t >= p.T) break;
     const int i = adaptor_of(p.which, p.S, t, p.T);
@@ -1073,6 +1070,7 @@ struct GradParams {
   int after_low, wide_a;                         // wide_a: rows of dA are vectors of eight
 };
 constexpr int kGradThreads = 192;
+constexpr int kGradWords = 1024;
 
 struct GradItem {
   int product, tile, adaptor, split;
@@ -1090,12 +1088,14 @@ __device__ __forceinline__ GradItem grad_item(const GradParams& p, int item) {
 }
 // The row blocks of an item that have rows of its adaptor, in order; a warp walks over them as a whole.
 struct BlockWalk {
+  const uint32_t *present, *whole;      // in shared memory, where they are few
   int block, end;
   uint32_t word, alone;
+  __device__ __forceinline__ BlockWalk(const uint32_t* present_, const uint32_t* whole_) : present(present_), whole(whole_) {}
   __device__ __forceinline__ void look(const GradParams& p, const GradItem& g, int b) {
     const size_t at = static_cast<size_t>(b >> 5) * p.S + g.adaptor;
-    word = p.present[at];
-    alone = p.whole[at];
+    word = present[at];
+    alone = whole[at];
   }
   __device__ __forceinline__ void start(const GradParams& p, const GradItem& g) {
     block = static_cast<int>(static_cast<long long>(g.split) * p.blocks / p.splits) - 1;
@@ -1116,7 +1116,7 @@ struct BlockWalk {
     }
   }
   // Whether all rows of the block are the adaptor's.
-  __device__ __forceinline__ bool whole() const { return alone >> (block & 31) & 1; }
+  __device__ __forceinline__ bool all() const { return alone >> (block & 31) & 1; }
 };
 
 template <int K16>
@@ -1155,6 +1155,18 @@ __global__ void __launch_bounds__(kGradThreads, 1) adaptor_grad_kernel(const __g
   // The kernel ahead is the product, a gate: what adaptor_low_kernel wrote is there, and nothing here needs the product. Or (after_low) that kernel itself.
   if (p.after_low) grid_dependency_wait();
   grid_launch_dependents();
+  const uint32_t *present = p.present, *whole_blocks = p.whole;
+  const int words = ((p.blocks + 31) >> 5) * p.S;
+  if (words <= kGradWords) {            // every role looks them up for every item
+    uint32_t* near = reinterpret_cast<uint32_t*>(ctl + 1);
+    for (int i = threadIdx.x; i < words; i += kGradThreads) {
+      near[i] = p.present[i];
+      near[kGradWords + i] = p.whole[i];
+    }
+    __syncthreads();
+    present = near;
+    whole_blocks = near + kGradWords;
+  }
   const uint32_t full0 = smem_u32(&ctl->full[0]), empty0 = smem_u32(&ctl->empty[0]);
 
   if (warp == 0) {
@@ -1164,7 +1176,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) adaptor_grad_kernel(const __g
     for (int item = blockIdx.x; item < items && ok; item += gridDim.x) {
       const GradItem g = grad_item(p, item);
       const CUtensorMap *rows = &p.tm_rows[g.product], *terms = &p.tm_terms[g.product];
-      BlockWalk walk;
+      BlockWalk walk(present, whole_blocks);
       walk.start(p, g);
       while (walk.next(p, g)) {
         const int t0 = walk.block * 64;
@@ -1190,7 +1202,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) adaptor_grad_kernel(const __g
     bool ok = true;
     for (int item = blockIdx.x; item < items && ok; item += gridDim.x) {
       const GradItem g = grad_item(p, item);
-      BlockWalk walk;
+      BlockWalk walk(present, whole_blocks);
       walk.start(p, g);
       int n = 0;                                                     // blocks in the open accumulator
       uint32_t slot = 0;
@@ -1200,7 +1212,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) adaptor_grad_kernel(const __g
           if (!bounded_wait_all(smem_u32(&ctl->tempty[slot]), ((use / kSlots) & 1u) ^ 1u, ctl, p)) { ok = false; break; }
           ++use;
         }
-        const bool whole = walk.whole();
+        const bool whole = walk.all();
         bool foreign[2] = {false, false};                            // rows lane and lane + 32 of the block
         if (!whole) {
 #pragma unroll
@@ -1211,18 +1223,12 @@ __global__ void __launch_bounds__(kGradThreads, 1) adaptor_grad_kernel(const __g
           // rows of other adaptors, which may hold anything, become zeros in both operands where they landed: a row is 128 bytes of every box
 #pragma unroll
           for (int q = 0; q < 2; ++q) {
-            uint32_t rows = __ballot_sync(0xffffffffu, foreign[q]);
-            while (rows != 0) {                                      // four rows at a time, eight lanes each
-              uint32_t mine = rows;
-              for (int e = 0; e < lane / 8; ++e) mine &= mine - 1;
-              if (mine != 0) {
-                const uint32_t at = tiles_addr + stage * p.stage_bytes + (32 * q + __ffs(mine) - 1) * 128 + (lane & 7) * 16;
+            if (!foreign[q]) continue;
+            const uint32_t row = tiles_addr + stage * p.stage_bytes + (32 * q + lane) * 128;
 #pragma unroll
-                for (int box = 0; box < 2 + kTermBoxes; ++box) st_shared_v4(at + box * kMnBoxBytes, 0, 0, 0, 0);
-              }
+            for (int c = 0; c < 8; ++c)                              // neighbours start at other banks
 #pragma unroll
-              for (int e = 0; e < 4; ++e) rows &= rows - 1;
-            }
+              for (int box = 0; box < 2 + kTermBoxes; ++box) st_shared_v4(row + box * kMnBoxBytes + ((c + lane) & 7) * 16, 0, 0, 0, 0);
           }
           fence_proxy_async_shared();
           __syncwarp();
@@ -1249,7 +1255,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) adaptor_grad_kernel(const __g
     bool ok = true;
     for (int item = blockIdx.x; item < items && ok; item += gridDim.x) {
       const GradItem g = grad_item(p, item);
-      BlockWalk walk;
+      BlockWalk walk(present, whole_blocks);
       walk.start(p, g);
       float acc[K16];
 #pragma unroll
@@ -1324,7 +1330,7 @@ __global__ void __launch_bounds__(256) adaptor_grad_join_kernel(const __grid_con
   const int i = static_cast<int>(row / all);
   int col = static_cast<int>(row - static_cast<size_t>(i) * all);
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
+#pragma unroll 8
   for (int q = 0; q < p.splits; ++q) {
     const float4 x = *reinterpret_cast<const float4*>(p.part + (static_cast<size_t>(q) * p.S * all + row) * k16 + j0);
     s.x += x.x, s.y += x.y, s.z += x.z, s.w += x.w;
