@@ -261,6 +261,20 @@ class DeviceHead:
                                                out["dT_static"])
         return out
 
+    def window_policy_backward(self, old_logp, ref_logp, advantage, offsets, clip_low=0.2, clip_high=0.2, beta=0.0, mask=None, by_sequence=False, hidden=None,
+                               targets=None):
+        """The clipped policy loss of the windows' log-likelihoods (positions of packed sequences) and its gradients -> the dicts of policy_loss and of
+        window_logprob_backward together."""
+        logp = self.window_logprob(hidden=hidden, targets=targets)
+        out = policy_loss(logp, old_logp, ref_logp, advantage, offsets, clip_low, clip_high, beta, mask=mask, by_sequence=by_sequence)
+        return dict(self.window_logprob_backward(out["d_logp"], hidden=hidden, targets=targets), **out)
+
+    def window_preference_backward(self, ref_logp, offsets, beta=0.1, smoothing=0.0, mask=None, hidden=None, targets=None):
+        """The same of the preference loss of pairs of sequences."""
+        logp = self.window_logprob(hidden=hidden, targets=targets)
+        out = preference_loss(logp, ref_logp, offsets, beta, smoothing, mask=mask)
+        return dict(self.window_logprob_backward(out["d_logp"], hidden=hidden, targets=targets), **out)
+
     def window_loss_backward(self, num_sequences, sequence_length, gamma, hidden=None, targets=None, out=None, max_norm=None):
         """-> dict(slot_loss [n], loss [1], dh, dW_emit, dW_sum, dT_static or None) as fp32 device tensors. out: the dict of an earlier call, whose
         buffers are written again. max_norm: the gradients of the head's parameters together are clipped to that norm, in place, and

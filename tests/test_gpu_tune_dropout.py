@@ -134,3 +134,18 @@ def test_calls_that_are_refused():
         with pytest.raises(B.MtpcError):
             call()
     B.mtpc_dropout(x[:0], out[:0], 0.5, rng)
+
+
+def test_places_beyond_32_bits():
+    n = 2 ** 31 + 4096 + 3
+    x = torch.ones(3, n // 3, dtype=torch.bfloat16, device="cuda")         # (a row has 2^30 elements at most)
+    out = torch.empty_like(x)
+    assert x.numel() == n
+    B.mtpc_dropout(x, out, 0.5, state(21, 2))
+    first = (n // 8 - 64)
+    draws = []
+    for block in range(first, -(-n // 8)):
+        words = tu.philox4x32([block & tu.MASK32, block >> 32, 2, 0], [21, 0])
+        draws += [part for w in words for part in (w & 0xFFFF, w >> 16)]
+    want = np.array(draws[:n - 8 * first]) >= 32768
+    assert np.array_equal(host(out.view(-1)[8 * first:]) != 0, want)
