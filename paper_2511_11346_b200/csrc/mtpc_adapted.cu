@@ -477,11 +477,11 @@ int mtpc_adapted_projection_backward(const void* x_low, int64_t x_low_stride, co
       return rc;
   }
   p.stage_bytes = kABytes + ceil_div(3 * k16, 64) * static_cast<int>(kMnBoxBytes);
-  p.stages = stages_of(p.stage_bytes, 1, kGradWords * 8);
+  p.stages = stages_of(p.stage_bytes, grad_ctas(k16), kGradWords * 8);
   const size_t smem = kControl + kGradWords * 8 + static_cast<size_t>(p.stages) * p.stage_bytes;
   auto* kernel = k16 == 16 ? adaptor_grad_kernel<16> : k16 == 32 ? adaptor_grad_kernel<32> : k16 == 48 ? adaptor_grad_kernel<48> : adaptor_grad_kernel<64>;
   const long long items = static_cast<long long>(p.tiles[0] + p.tiles[1]) * S * p.splits;
-  launch_kernel(kernel, static_cast<int>(std::min<long long>(items, kSms)), kGradThreads, smem, st, true, p);
+  launch_kernel(kernel, static_cast<int>(std::min<long long>(items, grad_ctas(k16) * kSms)), kGradThreads, smem, st, true, p);
   if (p.splits > 1) {
     const long long quads = static_cast<long long>(S) * (p.tiles[0] + p.tiles[1]) * kBlockM * (k16 / 4);
     launch_kernel(adaptor_grad_join_kernel, ceil_div(quads, 256), 256, 0, st, true, p, k16);

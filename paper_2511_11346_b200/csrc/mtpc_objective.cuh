@@ -360,24 +360,57 @@ __device__ __forceinline__ void ratio_phase(const ObjectiveArgs& a, int first, i
     if (lane == 0) a.sum[item] = sum;
   }
 }
-// Pairs first, first + step, ... of a warp.
+// h of pair p, by a warp: the difference of its sequences' sums.
+__device__ __forceinline__ double pair_h(const ObjectiveArgs& a, int p, int lane) {
+  double h = 0.0;
+  for (int q = lane; q < 2 * a.parts; q += 32) {
+    const double x = a.sum[static_cast<size_t>(2 * p) * a.parts + q];
+    h += q < a.parts ? x : -x;
+  }
+  return a.beta * warp_total(h);
+}
+// The pair's loss and the slope of its first sequence. e = exp(-|h|): log sigmoid(h) = min(h, 0) - log(1 + e).
+__device__ __forceinline__ double pair_loss(const ObjectiveArgs& a, double h) {
+  return log1p(exp(-fabs(h))) + (1.0 - a.smoothing) * fmax(-h, 0.0) + a.smoothing * fmax(h, 0.0);
+}
+__device__ __forceinline__ float pair_slope(const ObjectiveArgs& a, double h) {
+  const double e = exp(-fabs(h)), low = e / (1.0 + e), of_other = h > 0.0 ? low : 1.0 - low;      // sigmoid(-h)
+  return static_cast<float>(a.beta * (a.smoothing - of_other) / (a.S / 2));
+}
+// Pairs first, first + step, ... of a warp: h, slope and loss.
 __device__ __forceinline__ void pairs_phase(const ObjectiveArgs& a, int first, int step, int lane) {
-  const int pairs = a.S / 2;
-  for (int p = first; p < pairs; p += step) {
-    double h = 0.0;
-    for (int q = lane; q < 2 * a.parts; q += 32) {
-      const double x = a.sum[static_cast<size_t>(2 * p) * a.parts + q];
-      h += q < a.parts ? x : -x;
-    }
-    h = a.beta * warp_total(h);
-    const double e = exp(-fabs(h));
-    const double low = e / (1.0 + e), of_other = h > 0.0 ? low : 1.0 - low;      // sigmoid(-h)
+  for (int p = first; p < a.S / 2; p += step) {
+    const double h = pair_h(a, p, lane);
     if (lane == 0) {
-      a.term[p] = log1p(e) + (1.0 - a.smoothing) * fmax(-h, 0.0) + a.smoothing * fmax(h, 0.0);      // log sigmoid(h) = min(h, 0) - log1p(e)
-      a.slope[p] = static_cast<float>(a.beta * (a.smoothing - of_other) / pairs);
+      a.term[p] = pair_loss(a, h);
+      a.slope[p] = pair_slope(a, h);
       if (a.h != nullptr) a.h[p] = static_cast<float>(h);
     }
   }
+}
+// All pairs by one block: their sums a warp to a pair, four at once, then a thread to each pair's loss (one after the other by its warp, 128 pairs took 10 us).
+__device__ __forceinline__ void all_pairs(const ObjectiveArgs& a) {
+  const int pairs = a.S / 2, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (int base = warp * 4; base < pairs; base += 4 * kObjectiveWarps) {
+    double h[4] = {0.0, 0.0, 0.0, 0.0};
+    for (int q = lane; q < 2 * a.parts; q += 32) {
+      const double sign = q < a.parts ? 1.0 : -1.0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) h[i] += sign * a.sum[static_cast<size_t>(2 * min(base + i, pairs - 1)) * a.parts + q];
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) h[i] += __shfl_xor_sync(0xffffffffu, h[i], o);
+    if (lane < 4 && base + lane < pairs) a.term[base + lane] = a.beta * (lane == 0 ? h[0] : lane == 1 ? h[1] : lane == 2 ? h[2] : h[3]);
+  }
+  __syncthreads();
+  for (int p = threadIdx.x; p < pairs; p += kObjectiveThreads) {
+    const double h = a.term[p];
+    a.term[p] = pair_loss(a, h);
+    if (a.h != nullptr) a.h[p] = static_cast<float>(h);
+  }
+  __syncthreads();
 }
 __device__ __forceinline__ void preference_final(const ObjectiveArgs& a, double* red) {
   const bool refused = any_refused(a, reinterpret_cast<long long*>(red));
@@ -385,11 +418,13 @@ __device__ __forceinline__ void preference_final(const ObjectiveArgs& a, double*
   block_totals<1>(a.S / 2, s, red, [&](int p, double (&x)[1]) { x[0] += a.term[p]; });
   if (threadIdx.x == 0) a.loss[0] = refused ? CUDART_NAN_F : static_cast<float>(s[0] / (a.S / 2));
 }
+// own: every warp forms its pair's slope itself.
 template <bool WIDE>
-__device__ __forceinline__ void spread_phase(const ObjectiveArgs& a, int first, int step, int lane) {
+__device__ __forceinline__ void spread_phase(const ObjectiveArgs& a, int first, int step, int lane, bool own) {
   for (int item = first; item < a.S * a.parts; item += step) {
     const Slice c = slice_of(a, item);
-    const float slope = c.s & 1 ? -a.slope[c.s >> 1] : a.slope[c.s >> 1];
+    float slope = own ? pair_slope(a, pair_h(a, c.s >> 1, lane)) : a.slope[c.s >> 1];
+    if (c.s & 1) slope = -slope;
     over_slice<WIDE>(a, c, lane, [&](int t, uint32_t valid, bool inside) {
       float g[4];
 #pragma unroll
@@ -448,7 +483,7 @@ __global__ void __launch_bounds__(kObjectiveThreads) preference_cluster_kernel(O
   cluster_sync_all();
   pairs_phase(a, first, step, lane);
   cluster_sync_all();
-  spread_phase<WIDE>(a, first, step, lane);
+  spread_phase<WIDE>(a, first, step, lane, false);
   if (rank == 0) preference_final(a, red);
   cluster_sync_all();                              // nobody reads the first CTA's any more
 }
@@ -486,14 +521,18 @@ __global__ void __launch_bounds__(kObjectiveThreads) pairs_kernel(const Objectiv
   grid_dependency_wait();
   pairs_phase(a, blockIdx.x * kObjectiveWarps + (threadIdx.x >> 5), gridDim.x * kObjectiveWarps, threadIdx.x & 31);
 }
-// The last block adds up the loss.
+// The last block adds up the loss. own: without pairs_kernel ahead, every warp forms what it needs of the sums, the last block all pairs'.
 template <bool WIDE>
-__global__ void __launch_bounds__(kObjectiveThreads) spread_kernel(const ObjectiveArgs a) {
+__global__ void __launch_bounds__(kObjectiveThreads) spread_kernel(const ObjectiveArgs a, bool own) {
   __shared__ double red[kObjectiveWarps];
   grid_launch_dependents();
   grid_dependency_wait();
-  if (blockIdx.x + 1 == gridDim.x) preference_final(a, red);
-  else spread_phase<WIDE>(a, blockIdx.x * kObjectiveWarps + (threadIdx.x >> 5), (gridDim.x - 1) * kObjectiveWarps, threadIdx.x & 31);
+  if (blockIdx.x + 1 == gridDim.x) {
+    if (own) all_pairs(a);
+    preference_final(a, red);
+  } else {
+    spread_phase<WIDE>(a, blockIdx.x * kObjectiveWarps + (threadIdx.x >> 5), (gridDim.x - 1) * kObjectiveWarps, threadIdx.x & 31, own);
+  }
 }
 
 }  // namespace mtpc

@@ -36,6 +36,7 @@ void launch_dropout(const DropoutArgs& a, bool vectors, cudaStream_t st) {
 // ---------------------------------------------------------------- losses
 constexpr int kMaxSequences = 1 << 20;
 constexpr int kSmallPositions = 1 << 16;
+constexpr int kOwnParts = 64, kOwnPairs = 1024;
 constexpr int kOwnCount = 1 << 14;      // mean length up to which a sequence's positions are counted by each of its warps: 16 vectors a lane
 struct ObjectivePlan {
   int parts;
@@ -97,8 +98,10 @@ void launch_preference(const ObjectiveArgs& a, bool small, cudaStream_t st) {
     return;
   }
   launch_kernel(ratio_kernel<WIDE>, item_blocks(a), kObjectiveThreads, 0, st, true, a);
-  launch_kernel(pairs_kernel, std::min(ceil_div(a.S / 2, kObjectiveWarps), kSms * 4), kObjectiveThreads, 0, st, true, a);
-  launch_kernel(spread_kernel<WIDE>, item_blocks(a) + 1, kObjectiveThreads, 0, st, true, a);
+  // Where a pair's sums are few, whoever needs its slope forms it, and the last block has all of them for the loss in little time: one launch less.
+  const bool own = a.parts <= kOwnParts && a.S <= kOwnPairs;
+  if (!own) launch_kernel(pairs_kernel, std::min(ceil_div(a.S / 2, kObjectiveWarps), kSms * 4), kObjectiveThreads, 0, st, true, a);
+  launch_kernel(spread_kernel<WIDE>, item_blocks(a) + 1, kObjectiveThreads, 0, st, true, a, own);
 }
 
 }  // namespace
