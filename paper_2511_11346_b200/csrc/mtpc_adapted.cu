@@ -35,16 +35,16 @@ EncodeTiledFn encode_fn() {
   }();
   return fn;
 }
-// bf16 rows of `cols` adjacent elements, `pitch` apart, of `matrices` matrices one behind the other (0: a map of two axes): boxes of 64 columns x box_rows,
-// 128-byte swizzle, zeros outside.
-int map_rows(CUtensorMap* tm, const void* base, uint64_t rows, uint64_t cols, uint64_t pitch, uint32_t box_rows, uint64_t matrices = 0) {
+// bf16 rows of `cols` adjacent elements, `pitch` apart, of `matrices` matrices one behind the other (0: a map of two axes): boxes of box_cols (16, 32 or 64) columns x
+// box_rows, swizzled over the bytes of a box's row, zeros outside.
+int map_rows(CUtensorMap* tm, const void* base, uint64_t rows, uint64_t cols, uint64_t pitch, uint32_t box_rows, uint64_t matrices = 0, uint32_t box_cols = 64) {
   EncodeTiledFn fn = encode_fn();
   if (!fn) return MTPC_ERR_CUDA;
   const cuuint64_t dims[3] = {cols, rows, matrices}, strides[2] = {pitch * 2, rows * pitch * 2};
-  const cuuint32_t box[3] = {64, box_rows, 1}, each[3] = {1, 1, 1};
+  const cuuint32_t box[3] = {box_cols, box_rows, 1}, each[3] = {1, 1, 1};
+  const CUtensorMapSwizzle swizzle = box_cols == 16 ? CU_TENSOR_MAP_SWIZZLE_32B : box_cols == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B;
   const CUresult r = fn(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, matrices ? 3 : 2, const_cast<void*>(base), dims, strides, box, each,
-                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+                        CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? MTPC_OK : MTPC_ERR_CUDA;
 }
 
@@ -189,16 +189,13 @@ int launch_low(LowParams& p, const Rows& rows, const Rows& factors, bool mn, con
   p.k16 = rank16(k);
   p.pieces = pieces_of(k);
   p.split = 1;
-  // K-major factors of several adaptors fit where one of the largest rank does; MN-major ones are boxes of 8 KB whatever the rank, so that more of them are worth their place
-  // where a tile has several requests (129 rows of eight: 45 -> 33 us for all gradients) and cost it where it has one (8192 of one: 16 -> 19).
-  const bool many = static_cast<int64_t>(S) * kBlockM > T;
-  p.group = mn ? (many ? 4 : 1) : kMaxRank / p.k16;
-  p.stage_bytes = kABytes + (mn ? p.group : 1) * static_cast<int>(kMnBoxBytes);
-  p.stages = stages_of(p.stage_bytes, p.stage_bytes > 32768 ? 1 : 2);
+  p.group = mn ? 64 / factor_columns(p.k16) : kMaxRank / p.k16;
+  p.stage_bytes = kABytes + kMaxRank * kBlockK * 2;
+  p.stages = stages_of(p.stage_bytes, 2);
   p.tiles = ceil_div(T, kBlockM);
   if (rows.p) {
     int rc = map_rows(&p.tm_a, rows.p, T, K, rows.stride, kBlockM);
-    if (rc == MTPC_OK) rc = mn ? map_rows(&p.tm_f, factors.p, K, k, factors.stride, 64, S) : map_rows(&p.tm_f, factors.p, k, K, factors.stride, rank16(k), S);
+    if (rc == MTPC_OK) rc = mn ? map_rows(&p.tm_f, factors.p, K, k, factors.stride, 64, S, factor_columns(p.k16)) : map_rows(&p.tm_f, factors.p, k, K, factors.stride, rank16(k), S);
     if (rc != MTPC_OK) return rc;
     p.kblocks = ceil_div(K, kBlockK);
     p.chunks = chunks_of(K);

@@ -144,7 +144,7 @@ struct TileAdaptors {
 // sum, scale, low, its terms. For the gradients it splits given values into terms as well, and blocks behind the tiles' say which 64 rows have an adaptor's.
 struct LowParams {
   CUtensorMap tm_a;                     // rows [T, K]          box 64 x 128
-  CUtensorMap tm_f;                     // factors: B [S, k, K] box 64 x k16 (K-major), or A [S, K, k] box 64 x 64 (MN-major)
+  CUtensorMap tm_f;                     // factors: B [S, k, K] box 64 x k16 (K-major), or A [S, K, k] box factor_columns(k16) x 64 (MN-major)
   const int* which;
   const float* scale;                   // [S] or NULL: ones
   float* low;                           // [T, k] or NULL
@@ -162,6 +162,19 @@ struct LowParams {
 };
 constexpr int kLowThreads = 192;
 constexpr int kLowSlots = 4, kLowSlotCols = kMaxRank, kLowTmemCols = kLowSlots * kLowSlotCols;
+// MN-major factors lie in shared memory as 64 rows (of K) of 16, 32 or 64 columns, swizzled over the 32, 64 or 128 bytes that a row has: a quarter of what boxes of 64
+// columns would move for a rank of 16. Eight rows are 8 row-lengths apart, sixteen (an MMA's K) twice that.
+__host__ __device__ constexpr int factor_columns(int k16) { return k16 <= 32 ? k16 : 64; }
+__device__ __forceinline__ uint64_t umma_smem_desc_factor(uint32_t smem_addr, int columns) {
+  const uint64_t layout = columns == 16 ? 6 : columns == 32 ? 4 : 2;
+  uint64_t d = 0;
+  d |= static_cast<uint64_t>((smem_addr & 0x3FFFFu) >> 4);
+  d |= static_cast<uint64_t>(kMnBoxBytes >> 4) << 16;                  // (one box holds all columns: not used)
+  d |= static_cast<uint64_t>(columns) << 32;                           // eight rows of 2 columns bytes, in units of 16
+  d |= static_cast<uint64_t>(1) << 46;
+  d |= layout << 61;
+  return d;
+}
 // x as a sum of bf16 values: the nearest, and the nearest to what is left (twice, where a third is wanted). A value that is not finite keeps its first.
 __device__ __forceinline__ void split_terms(float x, __nv_bfloat16& hi, __nv_bfloat16& mid, __nv_bfloat16& lo) {
   hi = __float2bfloat16_rn(x);
@@ -272,7 +285,7 @@ __global__ void __launch_bounds__(kLowThreads, 2) adaptor_low_kernel(const __gri
   int adaptor = 0;
   uint32_t off[4];
   const int group = p.group;
-  const uint32_t f_bytes = F_MN ? kMnBoxBytes : static_cast<uint32_t>(p.k16) * (kBlockK * 2);
+  const uint32_t f_bytes = static_cast<uint32_t>(F_MN ? factor_columns(p.k16) : p.k16) * (kBlockK * 2);
 
   if (warp >= 2 && p.given != nullptr) given_terms(p, row0 + rank * (kBlockM / p.split), row0 + (rank + 1) * (kBlockM / p.split), threadIdx.x - 64);
   if (none || p.chunks == 0) {
@@ -315,9 +328,9 @@ __global__ void __launch_bounds__(kLowThreads, 2) adaptor_low_kernel(const __gri
     uint32_t stage = 0, phase = 0, use = 0;
     bool ok = true;
     const uint32_t idesc = umma_idesc_bf16(kBlockM, p.k16, false, F_MN);
-    constexpr uint32_t kStepF = F_MN ? 128u : 2u;
+    const uint32_t f_step = F_MN ? 2u * factor_columns(p.k16) : 2u;
     const uint64_t a_desc0 = umma_smem_desc_sw128(tiles_addr);
-    const uint64_t f_desc0 = F_MN ? umma_smem_desc_mn_sw128(tiles_addr + kABytes, kMnBoxBytes) : umma_smem_desc_sw128(tiles_addr + kABytes);
+    const uint64_t f_desc0 = F_MN ? umma_smem_desc_factor(tiles_addr + kABytes, factor_columns(p.k16)) : umma_smem_desc_sw128(tiles_addr + kABytes);
     for (int c = rank; c < p.chunks && ok; c += p.split, ++use) {
       const int kb0 = c * kChunkBlocks, kb1 = min(p.kblocks, kb0 + kChunkBlocks);
       const uint32_t slot = use % kLowSlots;
@@ -344,7 +357,7 @@ __global__ void __launch_bounds__(kLowThreads, 2) adaptor_low_kernel(const __gri
             if (q >= n) break;
 #pragma unroll
             for (int kk = 0; kk < kBlockK / 16; ++kk)
-              umma_bf16_rows(lead, d_tmem, a_desc + 2 * kk, f_desc + q * (f_bytes >> 4) + kStepF * kk, idesc, (kb != kb0 || kk != 0) ? 1u : 0u, offs[q]);
+              umma_bf16_rows(lead, d_tmem, a_desc + 2 * kk, f_desc + q * (f_bytes >> 4) + f_step * kk, idesc, (kb != kb0 || kk != 0) ? 1u : 0u, offs[q]);
           }
           umma_commit(lead, empty0 + 8 * stage);
           if (++stage == static_cast<uint32_t>(p.stages)) { stage = 0; phase ^= 1u; }
