@@ -11,7 +11,7 @@
 // adaptor_grad_kernel, adaptor_grad_join_kernel   dA and dB.
 //
 // Rows keep their order. A tile of 128 (256) rows has a K block for every adaptor that occurs in it, whose MMAs leave the accumulator rows of others alone
-// (the instruction's lane mask): no row is computed from another adaptor's weights, also not as zero times them, so that what one request's
+// (the instruction's lane mask): no row's result holds another adaptor's weights, also not as zero times them, so that what one request's
 // weights hold (infinities, NaN) reaches no other. Rows of a request that follow each other, as in prompts and training batches, give one to three
 // such blocks a tile; in the worst case, 128 adaptors in every tile, they are as many K blocks more.
 #pragma once
@@ -157,7 +157,8 @@ struct LowParams {
   uint64_t wait_limit_ns;
   int T, S, k, k16, pieces;             // k16: the rank, rounded up to 16
   int kblocks, chunks, tiles, split, stages, stage_bytes;            // split: CTAs of a cluster; chunks 0: no sums are wanted
-  int group;                            // adaptors (at most four) whose factors share a stage with a tile of the rows: the rows are read once for them
+  int group;                            // adaptors whose factors share a stage with a tile of the rows, 64 columns in all: one pass over the rows gives the products with all of them,
+                                        // and every row takes those of its own
   int present_blocks;
 };
 constexpr int kLowThreads = 192;
@@ -169,7 +170,7 @@ __device__ __forceinline__ uint64_t umma_smem_desc_factor(uint32_t smem_addr, in
   const uint64_t layout = columns == 16 ? 6 : columns == 32 ? 4 : 2;
   uint64_t d = 0;
   d |= static_cast<uint64_t>((smem_addr & 0x3FFFFu) >> 4);
-  d |= static_cast<uint64_t>(kMnBoxBytes >> 4) << 16;                  // (one box holds all columns: not used)
+  d |= static_cast<uint64_t>((columns * kBlockK * 2) >> 4) << 16;      // the next adaptor's box continues the columns
   d |= static_cast<uint64_t>(columns) << 32;                           // eight rows of 2 columns bytes, in units of 16
   d |= static_cast<uint64_t>(1) << 46;
   d |= layout << 61;
@@ -327,44 +328,32 @@ __global__ void __launch_bounds__(kLowThreads, 2) adaptor_low_kernel(const __gri
     const uint32_t lead = elect_one();
     uint32_t stage = 0, phase = 0, use = 0;
     bool ok = true;
-    const uint32_t idesc = umma_idesc_bf16(kBlockM, p.k16, false, F_MN);
     const uint32_t f_step = F_MN ? 2u * factor_columns(p.k16) : 2u;
     const uint64_t a_desc0 = umma_smem_desc_sw128(tiles_addr);
     const uint64_t f_desc0 = F_MN ? umma_smem_desc_factor(tiles_addr + kABytes, factor_columns(p.k16)) : umma_smem_desc_sw128(tiles_addr + kABytes);
-    for (int c = rank; c < p.chunks && ok; c += p.split, ++use) {
+    for (int c = rank; c < p.chunks && ok; c += p.split) {
       const int kb0 = c * kChunkBlocks, kb1 = min(p.kblocks, kb0 + kChunkBlocks);
-      const uint32_t slot = use % kLowSlots;
-      if (!bounded_wait_all(smem_u32(&ctl->tempty[slot]), ((use / kLowSlots) & 1u) ^ 1u, ctl, p)) break;
-      tc_fence_after();
-      const uint32_t d_tmem = tmem_base + slot * kLowSlotCols;
       TileAdaptors<4> each = ta;
       while (ok) {
-        uint32_t offs[4][4];
         int n = 0;
-        while (n < group && each.next(adaptor, off)) {
-#pragma unroll
-          for (int q = 0; q < 4; ++q)
-            if (q == n) offs[q][0] = off[0], offs[q][1] = off[1], offs[q][2] = off[2], offs[q][3] = off[3];
-          ++n;
-        }
+        while (n < group && each.next(adaptor, off)) ++n;
         if (n == 0) break;
+        const uint32_t slot = use % kLowSlots, idesc = umma_idesc_bf16(kBlockM, n * p.k16, false, F_MN);
+        if (!bounded_wait_all(smem_u32(&ctl->tempty[slot]), ((use / kLowSlots) & 1u) ^ 1u, ctl, p)) { ok = false; break; }
+        ++use;
+        tc_fence_after();
+        const uint32_t d_tmem = tmem_base + slot * kLowSlotCols;
         for (int kb = kb0; kb < kb1; ++kb) {
           if (!bounded_wait_all(full0 + 8 * stage, phase, ctl, p)) { ok = false; break; }
           tc_fence_after();
           const uint64_t a_desc = a_desc0 + stage * (p.stage_bytes >> 4), f_desc = f_desc0 + stage * (p.stage_bytes >> 4);
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            if (q >= n) break;
-#pragma unroll
-            for (int kk = 0; kk < kBlockK / 16; ++kk)
-              umma_bf16_rows(lead, d_tmem, a_desc + 2 * kk, f_desc + q * (f_bytes >> 4) + f_step * kk, idesc, (kb != kb0 || kk != 0) ? 1u : 0u, offs[q]);
-          }
+          for (int kk = 0; kk < kBlockK / 16; ++kk) umma_bf16(lead, d_tmem, a_desc + 2 * kk, f_desc + f_step * kk, idesc, (kb != kb0 || kk != 0) ? 1u : 0u);
           umma_commit(lead, empty0 + 8 * stage);
           if (++stage == static_cast<uint32_t>(p.stages)) { stage = 0; phase ^= 1u; }
         }
+        if (ok) umma_commit(lead, smem_u32(&ctl->tfull[slot]));
       }
-      if (!ok) break;
-      umma_commit(lead, smem_u32(&ctl->tfull[slot]));
     }
     __syncwarp();
   } else {
@@ -374,21 +363,38 @@ __global__ void __launch_bounds__(kLowThreads, 2) adaptor_low_kernel(const __gri
 #pragma unroll
     for (int j = 0; j < kMaxRank; ++j) acc[j] = 0.f;
     uint32_t use = 0;
-    for (int c = rank; c < p.chunks; c += p.split, ++use) {
-      const uint32_t slot = use % kLowSlots;
-      if (!bounded_wait_warp(smem_u32(&ctl->tfull[slot]), (use / kLowSlots) & 1u, ctl, p.status, lane)) break;
-      tc_fence_after();
+    bool ok = true;
+    for (int c = rank; c < p.chunks && ok; c += p.split) {
+      TileAdaptors<4> each = ta;
+      while (true) {
+        int n = 0, place = -1;                                       // which of the group's adaptors this thread's row has
+        while (n < group && each.next(adaptor, off)) {
+          uint32_t others = 0;
 #pragma unroll
-      for (int b = 0; b < kMaxRank / 16; ++b) {
-        if (b * 16 >= p.k16) break;
-        float x[16];
-        tmem_ld16(lane_base + slot * kLowSlotCols + b * 16, x);
+          for (int w = 0; w < 4; ++w)
+            if (w == quarter) others = off[w];
+          if (!(others >> lane & 1)) place = n;
+          ++n;
+        }
+        if (n == 0) break;
+        const uint32_t slot = use % kLowSlots;
+        if (!bounded_wait_warp(smem_u32(&ctl->tfull[slot]), (use / kLowSlots) & 1u, ctl, p.status, lane)) { ok = false; break; }
+        ++use;
+        tc_fence_after();
+        for (int q = 0; q < n; ++q) {
 #pragma unroll
-        for (int q = 0; q < 16; ++q) acc[b * 16 + q] += x[q];
+          for (int b = 0; b < kMaxRank / 16; ++b) {
+            if (b * 16 >= p.k16) break;
+            float x[16];
+            tmem_ld16(lane_base + slot * kLowSlotCols + q * p.k16 + b * 16, x);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[b * 16 + e] += place == q ? x[e] : 0.f;
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&ctl->tempty[slot]));
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&ctl->tempty[slot]));
     }
     float4* dst = reinterpret_cast<float4*>(sums + (quarter * 32 + lane) * pitch);
 #pragma unroll
