@@ -18,7 +18,10 @@ namespace {
 using namespace mtpc;
 
 constexpr int kSmemLimit = 232448;      // 227 KB of dynamic shared memory per CTA on sm_100
-constexpr int kFewRows = 128;
+// Rows that are dealt with each by itself (as the N of MMAs whose M are W's rows) rather than as tiles of 128. Each costs a little more time, in tiles every adaptor
+// that occurs does: 4096 x 4096, k = 16, us by rows / in tiles: one adaptor 32 rows 12.2 / 13.6, 64 rows 15.3 / 13.5, 128 rows 20.7 / 14.3; four 64 rows 15.5 / 14.3; 32 in
+// random order 32 rows 13.9 / 25.8, 128 rows 23.0 / 33.5.
+bool few_rows(int T, int S) { return T <= std::min(128, 32 + 8 * S); }
 constexpr int kMaxAdaptors = 4096, kMaxWidth = 1 << 17, kMaxBatch = 1 << 24;
 constexpr size_t kControl = 1024 + sizeof(GemmControl);
 constexpr int kRowsShared = sizeof(RowsShared) + 16;
@@ -67,7 +70,7 @@ void plan_forward(int T, int d, int m, int k, int S, bool copies, ForwardPlan* p
   size_t off = 0;
   auto take = [&](size_t bytes) { size_t o = off; off += align_up(bytes); return o; };
   const size_t rows = T, dp = up8(d);
-  const bool few = T <= kFewRows, own_low = static_cast<int64_t>(T) * k <= kOwnLow;
+  const bool few = few_rows(T, S), own_low = static_cast<int64_t>(T) * k <= kOwnLow;
   p->off_low = take(few && !own_low ? rows * k * 4 : 0);
   p->off_two = take(few ? 0 : rows * pieces_of(k) * 128);
   p->off_x = take(copies ? rows * dp * 2 : 0);
@@ -347,7 +350,7 @@ int mtpc_adapted_projection(const void* x, int64_t x_stride, const void* x_low, 
     if (!aligned(q, 2)) return MTPC_ERR_SHAPE;
   for (const void* q : {static_cast<const void*>(scale), static_cast<const void*>(row_adaptor), static_cast<const void*>(out_low), static_cast<const void*>(out_status)})
     if (!aligned(q, 4)) return MTPC_ERR_SHAPE;
-  const bool few = T <= kFewRows;
+  const bool few = few_rows(T, S);
   const bool copies = !mappable(x, x_stride, T, d) || !mappable(W, W_stride, m, d) ||
                       (!few && (!mappable(x_low, x_low_stride, T, d) || !mappable(A, k, 2, k) || !mappable(B, d, 2, d)));
   ForwardPlan plan;
