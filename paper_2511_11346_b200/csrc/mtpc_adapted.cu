@@ -248,11 +248,13 @@ int launch_product(const Rows& a, const Rows& b, const __nv_bfloat16* two, const
   p.pieces = adaptors ? pieces_of(k) : 0;
   p.kblocks = shared ? ceil_div(K, kBlockK) : 0;
   p.store = rows_allow(out, out_stride, 2, 16, T) ? 32 : rows_allow(out, out_stride, 2, 8, T) ? 16 : 2;
-  // Cycles that a K block of a tile takes and that its rest does, by the bytes that an SM gets from L2 and its MMAs' time, whichever is longer.
+  // Cycles that a K block of a tile takes and that its rest does, by the bytes that an SM gets from L2 and its MMAs' time, whichever is longer; rows that lie across lines of L2
+  // cost the smaller tiles, which read more, half as much again. 4096 x 4096, us for pairs / 128 / 64 columns: 256 rows 28 / 18 / 16, 512 27 / 19 / 25, 768 28 / 36 / 38.
+  const bool across = a.stride % 64 != 0 || b.stride % 64 != 0;
   const double kb = p.kblocks + 2.0 * p.pieces;
   const double pair = ceil_div(static_cast<long long>(ceil_div(T, 256)) * ceil_div(N, 256), kSms / 2) * (kb * 560 + 2000);
-  const double wide = ceil_div(static_cast<long long>(ceil_div(T, 128)) * ceil_div(N, 128), kSms) * (kb * 450 + 1500);
-  const double narrow = ceil_div(static_cast<long long>(ceil_div(T, 128)) * ceil_div(N, 64), kSms) * (kb * 350 + 1200);
+  const double wide = ceil_div(static_cast<long long>(ceil_div(T, 128)) * ceil_div(N, 128), kSms) * (kb * (across ? 700 : 450) + 1500);
+  const double narrow = ceil_div(static_cast<long long>(ceil_div(T, 128)) * ceil_div(N, 64), kSms) * (kb * (across ? 550 : 350) + 1200);
   if (pair <= wide && pair <= narrow)
     return b_mn ? launch_gemm<true, 256, 2>(p, a, b, two, f, K, st) : launch_gemm<false, 256, 2>(p, a, b, two, f, K, st);
   if (wide <= narrow) return b_mn ? launch_gemm<true, 128, 1>(p, a, b, two, f, K, st) : launch_gemm<false, 128, 1>(p, a, b, two, f, K, st);
