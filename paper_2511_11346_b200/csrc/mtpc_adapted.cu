@@ -83,12 +83,12 @@ void plan_forward(int T, int d, int m, int k, int S, bool copies, ForwardPlan* p
 
 // Runs of row blocks that the adaptors' gradients are cut into: what takes least, a run being its blocks and about four more for its start and end. An adaptor's
 // rows lie beside each other, so that up to S runs cut few adaptors' rows (n: runs that have rows); adding the runs up takes a quarter of a block each.
-int grad_splits(int tiles, int S, int blocks) {
+int grad_splits(int tiles, int S, int blocks, int k16) {
   int best = 1;
   double least = 0.0;
   for (int s = 1; s <= 32 && s <= std::max(1, blocks / 4); ++s) {
     const int n = std::max(s, S);
-    const double cost = static_cast<double>(ceil_div(static_cast<long long>(tiles) * n, kSms)) * (static_cast<double>(blocks) / n + 4.0) + 0.25 * s;
+    const double cost = static_cast<double>(ceil_div(static_cast<long long>(tiles) * n, kSms * grad_ctas(k16))) * (static_cast<double>(blocks) / n + 4.0) + 0.25 * s;
     if (s == 1 || cost < least * 0.97) best = s, least = cost;
   }
   return best;
@@ -102,7 +102,7 @@ void plan_backward(int T, int d, int m, int k, int S, bool copies, BackwardPlan*
   auto take = [&](size_t bytes) { size_t o = off; off += align_up(bytes); return o; };
   const size_t rows = T, dp = up8(d), k16 = rank16(k);
   const int blocks = ceil_div(T, 64), tiles = ceil_div(d, kBlockM) + ceil_div(m, kBlockM);
-  p->splits = grad_splits(tiles, S, blocks);
+  p->splits = grad_splits(tiles, S, blocks, static_cast<int>(k16));
   p->off_two = take(rows * pieces_of(k) * 128);
   p->off_low3 = take(rows * 3 * k16 * 2);
   p->off_v3 = take(rows * 3 * k16 * 2);

@@ -7,8 +7,8 @@
 // Preference: sequences 2p and 2p + 1, h = beta (sum of logp - ref over the one's valid positions - over the other's),
 //   loss = mean of -(1 - s) log sigmoid(h) - s log sigmoid(-h),   slope = +- beta (s - sigmoid(-h)) / pairs.
 //
-// Differences of log-likelihoods lose nothing: logp - old as two fp32 terms, of which whether a ratio is clipped is decided against the logarithms of the ends (in two
-// terms as well), since a position beside an end would else change sides by a rounding; those that a pair's sum adds up in fp64. Sums are fp64, the policy loss's of
+// Whether a ratio is clipped is decided on logp - old without loss, against the logarithms of the ends: where the rounded difference is beside an end, both are taken as
+// two fp32 terms, since a position there would else change sides by a rounding. The differences that a pair's sum adds up are fp64. Sums are fp64, the policy loss's of
 // four positions' fp32 ones, in an order that sizes fix.
 //
 // Work is dealt in items: a warp has one of P equal slices of one sequence, so that long sequences among short ones spread over the device and no
@@ -30,11 +30,11 @@ constexpr int kSmallItems = 1024;                  // that such a call has at mo
 constexpr int kMostBlocks = 148 * 2;               // of a launch for one phase: what the device holds at once
 
 struct ObjectiveArgs {
-  const float *logp, *old, *ref, *advantage;       // ref: NULL without the KL term; advantage [S], or [T] with by_position (policy)
+  const float *logp, *old, *ref, *advantage;       // ref: NULL without the KL term; advantage [S], or [T] with an advantage for every position (policy)
   const uint8_t* mask;                             // [T] or NULL
   const int* offsets;                              // [S + 1]
   int T, S, parts;                                 // parts: slices of a sequence
-  int by_sequence, by_position;
+  int by_sequence;
   int own_count;                                   // every warp counts the valid positions of its sequence itself
   float log_low[2], log_high[2];                   // logarithms of the ends, in two terms
   float low, high;                                 // the ends: 1 - clip_low, 1 + clip_high
@@ -147,25 +147,25 @@ __device__ __forceinline__ void block_sum(F (&x)[N], F* red) {
     }
   }
 }
-// Bytes that are not zero of mask[begin, end), by a warp.
-__device__ __forceinline__ int count_mask(const uint8_t* mask, int begin, int end, int lane) {
+// Bytes that are not zero of mask[begin, end): this one's of `lanes` threads.
+__device__ __forceinline__ int count_mask(const uint8_t* mask, int begin, int end, int lane, int lanes) {
   int n = 0;
   auto word = [](uint32_t w) { return __popc((w | ((w & 0x7f7f7f7fu) + 0x7f7f7f7fu)) & 0x80808080u); };
   const uint8_t *from = mask + begin, *to = mask + end;
   const uint8_t* first = reinterpret_cast<const uint8_t*>((reinterpret_cast<uintptr_t>(from) + 15) & ~static_cast<uintptr_t>(15));
   const uint8_t* last = reinterpret_cast<const uint8_t*>(reinterpret_cast<uintptr_t>(to) & ~static_cast<uintptr_t>(15));
   if (first >= last) {
-    for (const uint8_t* b = from + lane; b < to; b += 32) n += *b != 0;
+    for (const uint8_t* b = from + lane; b < to; b += lanes) n += *b != 0;
   } else {
     if (from + lane < first) n += from[lane] != 0;
 #pragma unroll 4
-    for (const uint8_t* b = first + 16 * lane; b < last; b += 512) {
+    for (const uint8_t* b = first + 16 * lane; b < last; b += 16 * lanes) {
       const uint4 v = *reinterpret_cast<const uint4*>(b);
       n += word(v.x) + word(v.y) + word(v.z) + word(v.w);
     }
     if (last + lane < to) n += last[lane] != 0;
   }
-  return warp_total(n);
+  return n;
 }
 template <bool WIDE>
 __device__ __forceinline__ void count_phase(const ObjectiveArgs& a, int block, int blocks, int lane, long long* red) {
@@ -200,33 +200,65 @@ __device__ __forceinline__ void exp_beyond(float q, float& beyond, float& m1) {
     beyond = m1 - q;
   }
 }
-// a - b as the nearest fp32 value and what it leaves (exactly, but for infinities): conversions to fp64 and back would be most of the kernel's time.
-__device__ __forceinline__ float difference(float a, float b, float& rest) {
-  const float d = __fsub_rn(a, b), back = __fadd_rn(d, b);
-  rest = __fsub_rn(__fsub_rn(a, back), __fsub_rn(b, __fsub_rn(back, d)));
-  return d;
+// What an advantage's sign says about clipping: the end that counts (its logarithm in two terms) and the value beyond it.
+struct ClipOf {
+  float adv, sign, end, end_rest, held;
+};
+__device__ __forceinline__ ClipOf clip_of(const ObjectiveArgs& a, float adv) {
+  const bool up = adv > 0.f;
+  return ClipOf{adv, up ? 1.f : adv < 0.f ? -1.f : 0.f, up ? a.log_high[0] : a.log_low[0], up ? a.log_high[1] : a.log_low[1], (up ? a.high : a.low) * adv};
+}
+// (logp - old) - the end's logarithm, where roundings would decide: the difference as the nearest fp32 value and what it leaves (exactly), less the two terms.
+__device__ __forceinline__ float beyond_end(float logp, float old, const ClipOf& side) {
+  const float d = __fsub_rn(logp, old), back = __fadd_rn(d, old);
+  const float rest = __fsub_rn(__fsub_rn(logp, back), __fsub_rn(old, __fsub_rn(back, d)));
+  return __fadd_rn(__fsub_rn(d, side.end), __fsub_rn(rest, side.end_rest));
 }
 
-// total: all valid positions.
-template <bool WIDE>
+// A slice's values on their way into L2 while its weight is formed, a line of 32 to a lane.
+__device__ __forceinline__ void prefetch_slice(const ObjectiveArgs& a, const Slice& c, int lane) {
+  for (int t = (c.begin & ~31) + 32 * lane; t < c.end; t += 32 * 32) {
+    const int at = max(t, c.begin);
+    prefetch_l2(a.logp + at);
+    prefetch_l2(a.old + at);
+    if (a.ref != nullptr) prefetch_l2(a.ref + at);
+  }
+}
+// total: all valid positions. EACH: an advantage for every position.
+template <bool WIDE, bool EACH>
 __device__ __forceinline__ void policy_phase(const ObjectiveArgs& a, int block, int blocks, int lane, long long total, double* red) {
-  const int first = block * kObjectiveWarps + (threadIdx.x >> 5), step = blocks * kObjectiveWarps;
+  const int items = a.S * a.parts;
   double all[3] = {0.0, 0.0, 0.0};
-  for (int item = first; item < a.S * a.parts; item += step) {
+  for (int base = block * kObjectiveWarps; base < items; base += blocks * kObjectiveWarps) {
+    const int item = base + (threadIdx.x >> 5);
+    int own = 0;
+    const bool together = a.own_count && a.parts >= kObjectiveWarps / 2;       // the block's warps share two or three sequences: counted by all of them
+    if (together) {
+      __shared__ int counted[4];
+      if (threadIdx.x < 4) counted[threadIdx.x] = 0;
+      if (item < items) prefetch_slice(a, slice_of(a, item), lane);
+      __syncthreads();
+      const int s0 = base / a.parts, s1 = (min(base + kObjectiveWarps, items) - 1) / a.parts;
+      for (int s = s0; s <= s1; ++s) {
+        const Span x = span_of(a, s);
+        const int n = warp_total(count_mask(a.mask, x.begin, x.end, threadIdx.x, kObjectiveThreads));
+        if (lane == 0 && n) atomicAdd(&counted[s - s0], n);
+      }
+      __syncthreads();
+      if (item < items) own = counted[item / a.parts - s0];
+      __syncthreads();
+    }
+    if (item >= items) continue;
     const Slice c = slice_of(a, item);
     long long n = total;
     if (a.by_sequence) {
       const Span x = span_of(a, c.s);
       int here = x.end - x.begin;
-      if (a.own_count) {
-        // (the slice's values come from memory meanwhile, a line of 32 to a lane)
-        for (int t = (c.begin & ~31) + 32 * lane; t < c.end; t += 32 * 32) {
-          const int at = max(t, c.begin);
-          prefetch_l2(a.logp + at);
-          prefetch_l2(a.old + at);
-          if (a.ref != nullptr) prefetch_l2(a.ref + at);
-        }
-        here = count_mask(a.mask, x.begin, x.end, lane);
+      if (together) {
+        here = own;
+      } else if (a.own_count) {
+        prefetch_slice(a, c, lane);
+        here = warp_total(count_mask(a.mask, x.begin, x.end, lane, 32));
       } else if (a.mask != nullptr) {
         here = 0;
         for (int q = lane; q < a.parts; q += 32) here += a.count[c.s * a.parts + q];
@@ -236,38 +268,34 @@ __device__ __forceinline__ void policy_phase(const ObjectiveArgs& a, int block, 
     }
     const double weight = n > 0 ? 1.0 / static_cast<double>(n) : 0.0;
     const float w = static_cast<float>(weight), beta = static_cast<float>(a.beta);
-    float adv4[4];
-    adv4[0] = adv4[1] = adv4[2] = adv4[3] = a.by_position ? 0.f : a.advantage[c.s];
+    const ClipOf one = clip_of(a, EACH ? 0.f : a.advantage[c.s]);
     double value = 0.0, kl = 0.0;
     int clipped = 0;
     over_slice<WIDE>(a, c, lane, [&](int t, uint32_t valid, bool inside) {
-      float lp[4], old[4], ref[4], g[4], value4 = 0.f, kl4 = 0.f;
+      float lp[4], old[4], ref[4], adv[4], g[4], value4 = 0.f, kl4 = 0.f;
       load4<WIDE>(a.logp, t, inside, valid, lp);
       load4<WIDE>(a.old, t, inside, valid, old);
       if (a.ref != nullptr) load4<WIDE>(a.ref, t, inside, valid, ref);
-      if (a.by_position) load4<WIDE>(a.advantage, t, inside, valid, adv4);
+      if (EACH) load4<WIDE>(a.advantage, t, inside, valid, adv);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float adv = adv4[i];
-        float rest;
-        const float diff = difference(lp[i], old[i], rest), r = expf(diff);
-        // beyond the end that counts for this sign: (diff + rest) - logarithm, the first difference without rounding where it decides
-        const float end = adv > 0.f ? a.log_high[0] : a.log_low[0], end_rest = adv > 0.f ? a.log_high[1] : a.log_low[1];
-        const float over = fabsf(diff) < CUDART_INF_F ? (diff - end) + (rest - end_rest) : diff;
-        const bool out = adv > 0.f ? over > 0.f : adv < 0.f && over < 0.f;
-        const float gain = adv == 0.f ? 0.f : (out ? (adv > 0.f ? a.high : a.low) : r) * adv;
-        float slope = out || adv == 0.f ? 0.f : -gain, beyond = 0.f, m1 = 0.f;
+        const ClipOf side = EACH ? clip_of(a, adv[i]) : one;
+        const float diff = lp[i] - old[i];
+        float over = diff - side.end;
+        if (fabsf(over) < fmaf(fabsf(diff), 1e-6f, 1e-6f)) over = beyond_end(lp[i], old[i], side);       // (both roundings are below 2^-23 of diff and end)
+        const bool out = side.sign * over > 0.f, counts = valid >> i & 1;
+        float gain = expf(diff) * side.adv;
+        if (out) gain = side.held;
+        if (side.adv == 0.f) gain = 0.f;
+        float slope = out ? 0.f : -gain, beyond = 0.f, m1 = 0.f;
         if (a.ref != nullptr) {
           exp_beyond(ref[i] - lp[i], beyond, m1);
           slope = fmaf(-beta, m1, slope);
         }
-        const bool counts = valid >> i & 1;
         g[i] = counts ? w * slope : 0.f;
-        if (counts) {
-          value4 -= gain;
-          kl4 += beyond;
-          clipped += out ? 1 : 0;
-        }
+        value4 -= counts ? gain : 0.f;
+        kl4 += counts ? beyond : 0.f;
+        clipped += counts && out ? 1 : 0;
       }
       value += static_cast<double>(value4);
       kl += static_cast<double>(kl4);
@@ -451,7 +479,7 @@ __device__ __forceinline__ void use_first_cta(ObjectiveArgs& a, ObjectiveShared*
   a.count = first->count;
   a.slope = first->slope;
 }
-template <bool WIDE>
+template <bool WIDE, bool EACH>
 __global__ void __launch_bounds__(kObjectiveThreads) policy_cluster_kernel(ObjectiveArgs a) {
   __shared__ double red[3 * kObjectiveWarps];
   __shared__ ObjectiveShared shared;
@@ -465,7 +493,7 @@ __global__ void __launch_bounds__(kObjectiveThreads) policy_cluster_kernel(Objec
     cluster_sync_all();
   }
   const long long total = a.by_sequence ? 0 : all_valid(a, kObjectiveCtas, reinterpret_cast<long long*>(red));
-  policy_phase<WIDE>(a, rank, kObjectiveCtas, lane, total, red);
+  policy_phase<WIDE, EACH>(a, rank, kObjectiveCtas, lane, total, red);
   cluster_sync_all();
   if (rank == 0) policy_final(a, kObjectiveCtas, red);
 }
@@ -496,13 +524,13 @@ __global__ void __launch_bounds__(kObjectiveThreads) count_kernel(const Objectiv
   grid_dependency_wait();
   count_phase<WIDE>(a, blockIdx.x, gridDim.x, threadIdx.x & 31, red);
 }
-template <bool WIDE>
+template <bool WIDE, bool EACH>
 __global__ void __launch_bounds__(kObjectiveThreads, 2) policy_kernel(const ObjectiveArgs a) {
   __shared__ double red[3 * kObjectiveWarps];
   grid_launch_dependents();
   grid_dependency_wait();
   const long long total = a.by_sequence ? 0 : all_valid(a, gridDim.x, reinterpret_cast<long long*>(red));
-  policy_phase<WIDE>(a, blockIdx.x, gridDim.x, threadIdx.x & 31, total, red);
+  policy_phase<WIDE, EACH>(a, blockIdx.x, gridDim.x, threadIdx.x & 31, total, red);
 }
 __global__ void __launch_bounds__(kObjectiveThreads) policy_final_kernel(const ObjectiveArgs a, int blocks) {
   __shared__ double red[3 * kObjectiveWarps];

@@ -81,14 +81,14 @@ void carve(const ObjectivePlan& p, void* workspace, ObjectiveArgs* a) {
   a->slope = reinterpret_cast<float*>(ws + p.off_slope);
 }
 int item_blocks(const ObjectiveArgs& a) { return std::min(ceil_div(static_cast<long long>(a.S) * a.parts, kObjectiveWarps), kMostBlocks); }
-template <bool WIDE>
+template <bool WIDE, bool EACH>
 void launch_policy(const ObjectiveArgs& a, bool small, cudaStream_t st) {
   if (small) {
-    launch_clusters(policy_cluster_kernel<WIDE>, kObjectiveCtas, kObjectiveCtas, kObjectiveThreads, 0, st, true, a);
+    launch_clusters(policy_cluster_kernel<WIDE, EACH>, kObjectiveCtas, kObjectiveCtas, kObjectiveThreads, 0, st, true, a);
     return;
   }
   if (a.mask && !a.own_count) launch_kernel(count_kernel<WIDE>, item_blocks(a), kObjectiveThreads, 0, st, true, a);
-  launch_kernel(policy_kernel<WIDE>, item_blocks(a), kObjectiveThreads, 0, st, true, a);
+  launch_kernel(policy_kernel<WIDE, EACH>, item_blocks(a), kObjectiveThreads, 0, st, true, a);
   launch_kernel(policy_final_kernel, 1, kObjectiveThreads, 0, st, true, a, item_blocks(a));
 }
 template <bool WIDE>
@@ -182,7 +182,6 @@ int mtpc_policy_loss(const float* logp, const float* old_logp, const float* ref_
   a.old = old_logp;
   a.ref = beta > 0.f ? ref_logp : nullptr;
   a.advantage = advantage;
-  a.by_position = advantage_by_position != 0;
   a.mask = mask;
   a.offsets = offsets;
   a.T = T;
@@ -199,10 +198,12 @@ int mtpc_policy_loss(const float* logp, const float* old_logp, const float* ref_
   a.d_logp = d_logp;
   a.status = out_status;
   carve(p, workspace, &a);
+  const bool each = advantage_by_position != 0;
   const bool wide = aligned(logp, 16) && aligned(old_logp, 16) && aligned(a.ref, 16) && aligned(d_logp, 16) && aligned(mask, 4) &&
-                    (!a.by_position || aligned(advantage, 16));
-  if (wide) launch_policy<true>(a, p.small, static_cast<cudaStream_t>(stream));
-  else launch_policy<false>(a, p.small, static_cast<cudaStream_t>(stream));
+                    (!each || aligned(advantage, 16));
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (each) wide ? launch_policy<true, true>(a, p.small, st) : launch_policy<false, true>(a, p.small, st);
+  else wide ? launch_policy<true, false>(a, p.small, st) : launch_policy<false, false>(a, p.small, st);
   return check_launch();
 }
 

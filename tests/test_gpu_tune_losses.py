@@ -174,6 +174,20 @@ def test_masked_positions_may_hold_anything_and_ends_are_sharp():
     d = torch.empty(2, device="cuda")
     B.mtpc_policy_loss(logp, torch.full((2,), -1.0, device="cuda"), None, a[:1], torch.tensor([0, 2], dtype=torch.int32, device="cuda"), 0.2, 0.2, 0.0, loss, d)
     assert d[0].item() == 0 and d[1].item() == -0.5 and loss.item() == -0.5
+    # with a negative advantage it is beyond the lower end: the end's value, clipped
+    stats = torch.empty(3, device="cuda")
+    B.mtpc_policy_loss(logp, torch.full((2,), -1.0, device="cuda"), None, a[1:], torch.tensor([0, 2], dtype=torch.int32, device="cuda"), 0.25, 0.25, 0.0, loss, d,
+                       out_stats=stats)
+    assert d[0].item() == 0 and d[1].item() == 0.5 and loss.item() == 0.875 and stats[2].item() == 0.5
+    # what an end at zero, or none, does: ratios of 1 are not beyond it, all others are; a clip_low of 1 or more never clips
+    two, zero = torch.full((2,), -1.0, device="cuda"), torch.tensor([0, 2], dtype=torch.int32, device="cuda")
+    for sign in (1.0, -1.0):
+        adv = torch.tensor([sign], device="cuda")
+        for step, clipped in ((0.0, 0.0), (2.0 ** -23, 1.0), (0.5, 1.0)):
+            B.mtpc_policy_loss(two + sign * step, two, None, adv, zero, 0.0, 0.0, 0.0, loss, d, out_stats=stats)
+            assert stats[2].item() == clipped and (d.abs() > 0).all() == (clipped == 0)
+    B.mtpc_policy_loss(two - 50, two, None, a[1:], zero, 1.0, 0.2, 0.0, loss, d, out_stats=stats)
+    assert stats[2].item() == 0 and loss.item() >= 0
 
 
 def test_offsets_that_are_refused_stay_within_the_buffers():
