@@ -387,12 +387,12 @@ _dtype_codes = None
 
 def _dtypes() -> dict:
     """What the calls look up in torch, once (an import statement in every call costs a tenth of a small one)."""
-    global _dtype_codes, _current_device, _raw_stream, _int32, _int64, _float32, _bfloat16, _bool, _uint8, _empty
+    global _dtype_codes, _current_device, _raw_stream, _int32, _int64, _float32, _bfloat16, _bool, _uint8, _raw_alloc, _raw_free
     if _dtype_codes is None:
         import torch
         _current_device, _int32, _float32 = torch._C._cuda_getDevice, torch.int32, torch.float32
         _int64, _bfloat16, _bool, _uint8 = torch.int64, torch.bfloat16, torch.bool, torch.uint8
-        _empty = torch.empty
+        _raw_alloc, _raw_free = torch._C._cuda_cudaCachingAllocator_raw_alloc, torch._C._cuda_cudaCachingAllocator_raw_delete
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
         _dtype_codes = {torch.float32: MTPC_F32, torch.bfloat16: MTPC_BF16}
     return _dtype_codes
@@ -480,15 +480,37 @@ def _flat(what: str, t, count: int, device: int, dtype) -> int:
     _refuse(what, f"{tuple(t.shape)} with strides {t.stride()} on {t.device} where {count} adjacent elements on device {device} are needed")
 
 
-def _workspace(what: str, workspace, need: int, device: int, stream):
-    """(address, bytes) of _scratch, and what keeps it alive; a call that needs none makes none."""
+def _call_with_workspace(what: str, function, device: int, stream, workspace, need: int, status: int, *args) -> None:
+    """_call of a function whose last arguments are a workspace, its size, a status word and the stream. workspace None: `need` bytes of torch's allocator for the call, given back
+    to it in the order of the stream (which it keeps apart per stream and per captured graph), without a tensor around them."""
+    if _current_device() != device:
+        import torch
+        with torch.cuda.device(device):
+            return _call_with_workspace(what, function, device, stream, workspace, need, status, *args)
+    raw = _raw_stream(device) if stream is None else _stream(stream, device)
     if need == 0:
-        return 0, 0, None
-    if workspace is None and stream is None:
-        ws = _empty(need, dtype=_uint8, device=device)
+        code = function(*args, 0, 0, status, raw)
+    elif workspace is not None:
+        if workspace.get_device() != device or not workspace.is_contiguous() or workspace.dtype is not _uint8:
+            _refuse(what, f"workspace of {workspace.dtype} on {workspace.device}")
+        code = function(*args, workspace.data_ptr(), workspace.numel(), status, raw)
     else:
-        ws = _scratch(what, workspace, need, device, stream)
-    return ws.data_ptr(), ws.numel(), ws
+        at = _raw_alloc(need, raw)
+        try:
+            code = function(*args, at, need, status, raw)
+        finally:
+            _raw_free(at)
+    if code != MTPC_OK:
+        raise MtpcError(code, what)
+
+
+def _like(what: str, name: str, t, shape: tuple, device: int) -> int:
+    """The address of an fp32 tensor of that shape and adjacent elements; 0 for None."""
+    if t is None:
+        return 0
+    if t.shape == shape and t.dtype is _float32 and t.get_device() == device and t.is_contiguous():
+        return t.data_ptr()
+    _refuse(what, f"{name} {tuple(t.shape)} of {t.dtype} on {t.device} where adjacent fp32 {tuple(shape)} on device {device} is needed")
 
 
 def mtpc_embed(tokens, table, out, scale: float = 1.0, out_status=None, stream=None) -> None:
@@ -594,16 +616,14 @@ def mtpc_adapted_projection(x, W, A, B, scale, row_adaptor, out, out_low=None, x
     S, k = _factors(what, A, B, m, d, dev)
     low_stride = 0 if x_low is None else _rows(what, x_low, T, d, dev, _bfloat16)
     out_stride = _rows(what, out, T, m, dev, _bfloat16)
-    if out_low is not None and (out_low.shape != (T, k) or out_low.dtype is not _float32 or not out_low.is_contiguous() or out_low.get_device() != dev):
-        _refuse(what, f"out_low {tuple(out_low.shape)} of {out_low.dtype}")
     x_at, W_at, A_at, B_at, low_at = x.data_ptr(), W.data_ptr(), A.data_ptr(), B.data_ptr(), 0 if x_low is None else x_low.data_ptr()
     # whether tensor maps address the operands as they lie
     plain = (x_at | W_at | A_at | B_at | low_at) % 16 == 0 and (d | k) % 8 == 0 and (T <= 1 or (stride % 8 == 0 and stride >= d)) and (
         m <= 1 or (W_stride % 8 == 0 and W_stride >= d)) and (x_low is None or T <= 1 or (low_stride % 8 == 0 and low_stride >= d))
-    ws_at, ws_bytes, ws = _workspace(what, workspace, _scratch_bytes("mtpc_adapted_projection_workspace_bytes", T, d, m, k, S, 1 if plain else 0), dev, stream)
-    _call(what, lib().mtpc_adapted_projection, dev, stream, x_at, stride, low_at, low_stride, W_at, W_stride, A_at, B_at, _flat(what, scale, S, dev, _float32),
-          _flat(what, row_adaptor, T, dev, _int32), T, d, m, k, S, out.data_ptr(), out_stride, _ptr(out_low), ws_at, ws_bytes,
-          _flat(what, out_status, 1, dev, _int32))
+    need = _scratch_bytes("mtpc_adapted_projection_workspace_bytes", T, d, m, k, S, 1 if plain else 0)
+    _call_with_workspace(what, lib().mtpc_adapted_projection, dev, stream, workspace, need, _flat(what, out_status, 1, dev, _int32), x_at, stride, low_at, low_stride,
+                         W_at, W_stride, A_at, B_at, _flat(what, scale, S, dev, _float32), _flat(what, row_adaptor, T, dev, _int32), T, d, m, k, S, out.data_ptr(),
+                         out_stride, _like(what, "out_low", out_low, (T, k), dev))
 
 
 def mtpc_adapted_projection_backward(x_low, W, A, B, scale, row_adaptor, low, d_out, d_x, dA=None, dB=None, d_x_low=None, workspace=None, out_status=None,
@@ -620,18 +640,15 @@ def mtpc_adapted_projection_backward(x_low, W, A, B, scale, row_adaptor, low, d_
     W_stride = _rows(what, W, m, d, dev, _bfloat16)
     S, k = _factors(what, A, B, m, d, dev)
     x_stride = 0 if x_low is None else _rows(what, x_low, T, d, dev, _bfloat16)
-    for name, t, shape in (("low", low, (T, k)), ("dA", dA, (S, m, k)), ("dB", dB, (S, k, d))):
-        if t is not None and (t.shape != shape or t.dtype is not _float32 or not t.is_contiguous() or t.get_device() != dev):
-            _refuse(what, f"{name} {tuple(t.shape)} of {t.dtype} where adjacent fp32 {shape} is needed")
     g_at, W_at, A_at, B_at, x_at = d_out.data_ptr(), W.data_ptr(), A.data_ptr(), B.data_ptr(), 0 if x_low is None else x_low.data_ptr()
     plain = (g_at | W_at | A_at | B_at | x_at) % 16 == 0 and (d | k) % 8 == 0 and (T <= 1 or (g_stride % 8 == 0 and g_stride >= m)) and (
         m <= 1 or (W_stride % 8 == 0 and W_stride >= d)) and (x_low is None or T <= 1 or (x_stride % 8 == 0 and x_stride >= d))
-    ws_at, ws_bytes, ws = _workspace(what, workspace, _scratch_bytes("mtpc_adapted_projection_backward_workspace_bytes", T, d, m, k, S, 1 if plain else 0), dev,
-                                     stream)
-    _call(what, lib().mtpc_adapted_projection_backward, dev, stream, x_at, x_stride, W_at, W_stride, A_at, B_at, _flat(what, scale, S, dev, _float32),
-          _flat(what, row_adaptor, T, dev, _int32), _ptr(low), T, d, m, k, S, g_at, g_stride, _ptr(d_x),
-          0 if d_x is None else _rows(what, d_x, T, d, dev, _bfloat16), _ptr(d_x_low), 0 if d_x_low is None else _rows(what, d_x_low, T, d, dev, _bfloat16),
-          _ptr(dA), _ptr(dB), ws_at, ws_bytes, _flat(what, out_status, 1, dev, _int32))
+    need = _scratch_bytes("mtpc_adapted_projection_backward_workspace_bytes", T, d, m, k, S, 1 if plain else 0)
+    dx_stride = 0 if d_x is None else _rows(what, d_x, T, d, dev, _bfloat16)
+    dl_stride = 0 if d_x_low is None else _rows(what, d_x_low, T, d, dev, _bfloat16)
+    _call_with_workspace(what, lib().mtpc_adapted_projection_backward, dev, stream, workspace, need, _flat(what, out_status, 1, dev, _int32), x_at, x_stride, W_at, W_stride,
+                         A_at, B_at, _flat(what, scale, S, dev, _float32), _flat(what, row_adaptor, T, dev, _int32), _like(what, "low", low, (T, k), dev), T, d, m, k, S,
+                         g_at, g_stride, _ptr(d_x), dx_stride, _ptr(d_x_low), dl_stride, _like(what, "dA", dA, A.shape, dev), _like(what, "dB", dB, B.shape, dev))
 
 
 def mtpc_dropout(x, out, p: float, rng, offset: int = 0, residual=None, stream=None) -> None:
@@ -668,12 +685,11 @@ def mtpc_policy_loss(logp, old_logp, ref_logp, advantage, offsets, clip_low: flo
     _dtypes()
     what = "mtpc_policy_loss"
     T, S, dev, mask_at = _positions(what, logp, offsets, mask)
-    ws_at, ws_bytes, ws = _workspace(what, workspace, _scratch_bytes("mtpc_objective_workspace_bytes", T, S), dev, stream)
-    _call(what, lib().mtpc_policy_loss, dev, stream, _flat(what, logp, T, dev, _float32), _flat(what, old_logp, T, dev, _float32),
-          _flat(what, ref_logp, T, dev, _float32), _flat(what, advantage, T if by_position else S, dev, _float32), 1 if by_position else 0, mask_at,
-          _flat(what, offsets, S + 1, dev, _int32), T, S, clip_low, clip_high, beta, 1 if by_sequence else 0, _flat(what, out_loss, 1, dev, _float32),
-          _flat(what, out_stats, 3, dev, _float32), _flat(what, d_logp, T, dev, _float32), ws_at, ws_bytes,
-          _flat(what, out_status, 1, dev, _int32))
+    _call_with_workspace(what, lib().mtpc_policy_loss, dev, stream, workspace, _scratch_bytes("mtpc_objective_workspace_bytes", T, S),
+                         _flat(what, out_status, 1, dev, _int32), _flat(what, logp, T, dev, _float32), _flat(what, old_logp, T, dev, _float32),
+                         _flat(what, ref_logp, T, dev, _float32), _flat(what, advantage, T if by_position else S, dev, _float32), 1 if by_position else 0, mask_at,
+                         _flat(what, offsets, S + 1, dev, _int32), T, S, clip_low, clip_high, beta, 1 if by_sequence else 0,
+                         _flat(what, out_loss, 1, dev, _float32), _flat(what, out_stats, 3, dev, _float32), _flat(what, d_logp, T, dev, _float32))
 
 
 def mtpc_preference_loss(logp, ref_logp, offsets, beta: float, out_loss, d_logp, mask=None, smoothing: float = 0.0, out_h=None, workspace=None,
@@ -683,11 +699,10 @@ def mtpc_preference_loss(logp, ref_logp, offsets, beta: float, out_loss, d_logp,
     _dtypes()
     what = "mtpc_preference_loss"
     T, S, dev, mask_at = _positions(what, logp, offsets, mask)
-    ws_at, ws_bytes, ws = _workspace(what, workspace, _scratch_bytes("mtpc_objective_workspace_bytes", T, S), dev, stream)
-    _call(what, lib().mtpc_preference_loss, dev, stream, _flat(what, logp, T, dev, _float32), _flat(what, ref_logp, T, dev, _float32), mask_at,
-          _flat(what, offsets, S + 1, dev, _int32), T, S, beta, smoothing, _flat(what, out_loss, 1, dev, _float32),
-          _flat(what, out_h, S // 2, dev, _float32), _flat(what, d_logp, T, dev, _float32), ws_at, ws_bytes,
-          _flat(what, out_status, 1, dev, _int32))
+    _call_with_workspace(what, lib().mtpc_preference_loss, dev, stream, workspace, _scratch_bytes("mtpc_objective_workspace_bytes", T, S),
+                         _flat(what, out_status, 1, dev, _int32), _flat(what, logp, T, dev, _float32), _flat(what, ref_logp, T, dev, _float32), mask_at,
+                         _flat(what, offsets, S + 1, dev, _int32), T, S, beta, smoothing, _flat(what, out_loss, 1, dev, _float32),
+                         _flat(what, out_h, S // 2, dev, _float32), _flat(what, d_logp, T, dev, _float32))
 
 
 class GradientList:
