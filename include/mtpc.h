@@ -562,7 +562,7 @@ int mtpc_destroy_gradient_list(mtpc_gradient_list* list);
  *   out  dev [T, m] bf16, not overlapping an input;  out_low dev [T, k] fp32, adjacent, or NULL: low, which the gradient of A needs (0 without adaptor).
  *   workspace dev, 256-byte aligned, >= mtpc_adapted_projection_workspace_bytes(T, d, m, k, S, aligned_rows) (0 bytes: it may be NULL). aligned_rows != 0: every operand starts on 16
  *        bytes, with strides, k and d that are multiples of eight elements and strides >= d; 0: any, of which the call makes copies.
- *   out_status as for mtpc_embed.
+ *   out_status as for mtpc_embed; MTPC_STATUS_TIMEOUT as for a head: the call's outputs are invalid.
  * Products accumulate in fp32; low is held to 16 bits or more for its product with A, and out is rounded once.
  * 0 <= T <= 2^24, 1 <= d, m <= 2^17, 1 <= k <= 64, 1 <= S <= 4096, S k max(d, m) <= 2^34 (MTPC_ERR_UNSUPPORTED beyond).
  */
@@ -578,7 +578,7 @@ int mtpc_adapted_projection(const void* x, int64_t x_stride, const void* x_low, 
  *   x_low  dev [T, d] bf16: what the adaptors read (x, where the forward call had no x_low); needed for dB.   low: the forward call's out_low; for dA.
  *   d_out  dev [T, m] bf16 (the norm's gradient in front of the head writes that type);  d_x dev [T, d] bf16.
  *   d_x_low dev [T, d] bf16 or NULL: takes B[i]^T v[t] apart from d_x (for the gradient of the dropout in front of the adaptors, whose call adds it to d_x).
- *   dA dev [S, m, k] fp32, dB dev [S, k, d] fp32, adjacent, overwritten.
+ *   dA dev [S, m, k] fp32, dB dev [S, k, d] fp32, adjacent, overwritten. No output may overlap an input or another output.
  *   Rows with an adaptor >= S: as above, in d_x (d_x_low, where that is given). Other arguments and limits as above; aligned_rows speaks of d_out and m too.
  */
 int mtpc_adapted_projection_backward_workspace_bytes(int32_t T, int32_t d, int32_t m, int32_t k, int32_t S, int32_t aligned_rows, size_t* out_bytes);

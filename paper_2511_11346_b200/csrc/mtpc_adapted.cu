@@ -214,8 +214,11 @@ int launch_low(LowParams& p, const Rows& rows, const Rows& factors, bool mn, con
 template <bool B_MN, int TN, int CTAS>
 int launch_gemm(AdaptedParams& p, const Rows& a, const Rows& b, const __nv_bfloat16* two, const Rows& f, int K, cudaStream_t st) {
   constexpr int kBCols = TN / CTAS;
-  int rc = map_rows(&p.tm_a, a.p, p.T, K, a.stride, kBlockM);
-  if (rc == MTPC_OK) rc = B_MN ? map_rows(&p.tm_b, b.p, K, p.N, b.stride, 64) : map_rows(&p.tm_b, b.p, p.N, K, b.stride, kBCols);
+  int rc = MTPC_OK;
+  if (p.kblocks > 0) {
+    rc = map_rows(&p.tm_a, a.p, p.T, K, a.stride, kBlockM);
+    if (rc == MTPC_OK) rc = B_MN ? map_rows(&p.tm_b, b.p, K, p.N, b.stride, 64) : map_rows(&p.tm_b, b.p, p.N, K, b.stride, kBCols);
+  }
   if (rc == MTPC_OK && p.pieces > 0) {
     rc = map_rows(&p.tm_u, two, p.T, p.pieces * 64, p.pieces * 64, kBlockM);
     if (rc == MTPC_OK) rc = B_MN ? map_rows(&p.tm_f, f.p, p.k, p.N, f.stride, 64, p.S) : map_rows(&p.tm_f, f.p, p.N, p.k, f.stride, kBCols, p.S);
@@ -446,7 +449,7 @@ int mtpc_adapted_projection_backward(const void* x_low, int64_t x_low_stride, co
   const bool sums = d_x || d_x_low || dB;
   if ((sums || dA) && (rc = launch_low(l, sums ? gr : Rows{nullptr, 0}, Ar, true, row_adaptor, T, m, k, S, out_status, st)) != MTPC_OK) return rc;
   if (d_x && (rc = launch_product(gr, Wr, two, Br, true, row_adaptor, T, m, d, k, S, true, d_x_low == nullptr, d_x, d_x_stride, out_status, st)) != MTPC_OK) return rc;
-  if (d_x_low && (rc = launch_product(gr, Rows{gr.p, gr.stride}, two, Br, true, row_adaptor, T, m, d, k, S, false, true, d_x_low, d_x_low_stride, out_status, st)) != MTPC_OK)
+  if (d_x_low && (rc = launch_product(gr, Rows{nullptr, 0}, two, Br, true, row_adaptor, T, m, d, k, S, false, true, d_x_low, d_x_low_stride, out_status, st)) != MTPC_OK)
     return rc;
   if (!dA && !dB) return MTPC_OK;
   GradParams p;

@@ -534,10 +534,14 @@ __global__ void __launch_bounds__(kAdaptedThreads, 1) adapted_gemm_kernel(const 
     ctl->abort = 0;
     ctl->wait_limit_ns = p.wait_limit_ns;
     fence_mbar_init();
-    tma_prefetch_desc(&p.tm_a);
-    tma_prefetch_desc(&p.tm_b);
-    tma_prefetch_desc(&p.tm_u);
-    tma_prefetch_desc(&p.tm_f);
+    if (p.kblocks > 0) {
+      tma_prefetch_desc(&p.tm_a);
+      tma_prefetch_desc(&p.tm_b);
+    }
+    if (p.pieces > 0) {
+      tma_prefetch_desc(&p.tm_u);
+      tma_prefetch_desc(&p.tm_f);
+    }
   }
   if (warp == 1) {
     if (CTAS == 2) {

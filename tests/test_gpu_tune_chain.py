@@ -155,3 +155,47 @@ def test_decoding_steps_eager_and_from_a_graph():
     B.mtpc_adapted_projection(x, W, A, Bf, None, torch.full_like(task, -1), plain)
     assert torch.equal(plain[task < 0], y[task < 0]) and not torch.equal(plain[task >= 0], y[task >= 0])
     dh.close()
+
+
+def test_the_first_calls_of_a_process_may_be_captured():
+    """(in a process of its own: nothing has run before)"""
+    import subprocess
+    import sys
+    code = """
+import torch
+from paper_2511_11346_b200 import binding as B
+bf = torch.bfloat16
+g = torch.Generator(device="cuda").manual_seed(1)
+new = lambda *s: torch.randn(s, device="cuda", generator=g).to(bf)
+W, A, Bf, rng = new(96, 64), new(2, 96, 16), new(2, 16, 64), torch.tensor([1, 2], device="cuda")
+sets = []
+for T in (1, 20, 300):
+    sets.append((new(T, 64), new(T, 96), (torch.arange(T, device="cuda") % 3 - 1).int(), torch.zeros(T, 96, device="cuda", dtype=bf), torch.zeros(T, 16, device="cuda"),
+                 torch.zeros(T, 64, device="cuda", dtype=bf), torch.zeros(2, 96, 16, device="cuda"), torch.zeros(2, 16, 64, device="cuda")))
+logp, offsets = -torch.rand(70000, device="cuda", generator=g), torch.tensor([0, 30, 500, 600, 700, 70000, 70000], dtype=torch.int32, device="cuda")
+losses, grads = torch.zeros(4, device="cuda"), torch.zeros(4, 70000, device="cuda")
+
+def calls():
+    for x, d_out, which, out, low, d_x, dA, dB in sets:
+        B.mtpc_adapted_projection(x, W, A, Bf, None, which, out, out_low=low)
+        B.mtpc_adapted_projection_backward(x, W, A, Bf, None, which, low, d_out, d_x, dA, dB)
+        B.mtpc_dropout(d_x, d_x, 0.5, rng)
+    for i, n in enumerate((700, 70000)):
+        of = offsets if n == 70000 else offsets[:5]
+        B.mtpc_policy_loss(logp[:n], logp[:n] - 0.1, None, torch.ones(of.numel() - 1, device="cuda"), of, 0.2, 0.2, 0.0, losses[2 * i:2 * i + 1], grads[2 * i][:n])
+        B.mtpc_preference_loss(logp[:n], logp[:n] * 0.9, of, 0.1, losses[2 * i + 1:2 * i + 2], grads[2 * i + 1][:n])
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    calls()
+graph.replay()
+torch.cuda.synchronize()
+first = [t.clone() for s in sets for t in s[3:]] + [losses.clone(), grads.clone()]
+calls()
+torch.cuda.synchronize()
+assert all(torch.equal(a, b) for a, b in zip(first, [t for s in sets for t in s[3:]] + [losses, grads]))
+# the one row of the first set has no adaptor: its low, dA and dB are zeros by definition
+assert [bool(t.any()) for t in first] == [True, False, True, False, False] + [True] * 12
+"""
+    done = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0, done.stderr[-2000:]
