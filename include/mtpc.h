@@ -558,7 +558,8 @@ int mtpc_destroy_gradient_list(mtpc_gradient_list* list);
  *   W    dev [m, d] bf16;  A dev [S, m, k], B dev [S, k, d] bf16, adjacent;  scale dev [S] fp32 or NULL (ones).
  *   row_adaptor dev [T] int32, or NULL: adaptor 0 for all rows. An adaptor >= S gives a row of NaN and MTPC_STATUS_BAD_ADAPTOR. Rows of one
  *        adaptor are fastest beside each other, as those of a request are; any order works. What one adaptor's factors hold does not
- *        reach rows of another, infinities and NaN included.
+ *        reach rows of another, infinities and NaN included. (In the row of an infinity itself, or in its adaptor's gradients, a result that is not finite may be
+ *        NaN instead of an infinity: products are sums of a few.)
  *   out  dev [T, m] bf16, not overlapping an input;  out_low dev [T, k] fp32, adjacent, or NULL: low, which the gradient of A needs (0 without adaptor).
  *   workspace dev, 256-byte aligned, >= mtpc_adapted_projection_workspace_bytes(T, d, m, k, S, aligned_rows) (0 bytes: it may be NULL). aligned_rows != 0: every operand starts on 16
  *        bytes, with strides, k and d that are multiples of eight elements and strides >= d; 0: any, of which the call makes copies.
@@ -608,7 +609,7 @@ int mtpc_dropout(const void* x, int64_t x_stride, int32_t x_dtype, const void* r
  *   logp, old_logp, ref_logp dev [T] fp32;  d_logp dev [T] fp32, overwritten at the positions of sequences (0 where the mask is 0) and left as it
  *           was outside of them; not overlapping an input.
  *   offsets dev int32 [S + 1], not decreasing, within [0, T]; otherwise MTPC_STATUS_BAD_OFFSET is or-ed into out_status (dev uint32 or NULL), the loss is NaN,
- *           and what d_logp holds is not defined. A sequence may be empty.
+ *           what d_logp holds within [0, T) is not defined, and the call may take as long as its sequences are together. A sequence may be empty.
  *   mask    dev [T] bytes or NULL: positions with 0 count nowhere, whatever their values are (infinities and NaN too).
  *   workspace dev, 256-byte aligned, >= mtpc_objective_workspace_bytes(T, S); small calls need none (0 bytes: it may be NULL).
  * 0 <= T <= 2^30, 1 <= S <= 2^20 (MTPC_ERR_UNSUPPORTED beyond). Differences of log-likelihoods are formed without loss, sums are fp64.
