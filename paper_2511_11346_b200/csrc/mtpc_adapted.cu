@@ -18,10 +18,11 @@ namespace {
 using namespace mtpc;
 
 constexpr int kSmemLimit = 232448;      // 227 KB of dynamic shared memory per CTA on sm_100
-// Rows that are dealt with each by itself (as the N of MMAs whose M are W's rows) rather than as tiles of 128. Each costs a little more time, in tiles every adaptor
-// that occurs does: 4096 x 4096, k = 16, us by rows / in tiles: one adaptor 32 rows 12.2 / 13.6, 64 rows 15.3 / 13.5, 128 rows 20.7 / 14.3; four 64 rows 15.5 / 14.3; 32 in
-// random order 32 rows 13.9 / 25.8, 128 rows 23.0 / 33.5.
-bool few_rows(int T, int S) { return T <= std::min(128, 32 + 8 * S); }
+// Rows that are dealt with each by itself (as the N of MMAs whose M are W's rows) rather than as tiles of 128. There every row costs time by its rank, in tiles every adaptor
+// that occurs does. 4096 x 4096, rows in random order, us by rows / in tiles: k = 16, one adaptor 32 rows 12.3 / 14.1, 64 rows 14.5 / 14.3, 128 rows 18.8 / 14.5; four 64 rows
+// 14.6 / 14.8, 128 rows 18.9 / 15.1; 32 adaptors 128 rows 19.7 / 33.5; k = 64, one adaptor 16 rows 14.2 / 14.0, four 32 rows 19.0 / 20.0, 64 rows 25.4 / 19.8, 32 adaptors
+// 128 rows 49.8 / 84.7.
+bool few_rows(int T, int k, int S) { return T <= std::min(128, 640 / std::max(k, 8) + 8 * S); }
 constexpr int kMaxAdaptors = 4096, kMaxWidth = 1 << 17, kMaxBatch = 1 << 24;
 constexpr size_t kControl = 1024 + sizeof(GemmControl);
 constexpr int kRowsShared = sizeof(RowsShared) + 16;
@@ -70,7 +71,7 @@ void plan_forward(int T, int d, int m, int k, int S, bool copies, ForwardPlan* p
   size_t off = 0;
   auto take = [&](size_t bytes) { size_t o = off; off += align_up(bytes); return o; };
   const size_t rows = T, dp = up8(d);
-  const bool few = few_rows(T, S), own_low = static_cast<int64_t>(T) * k <= kOwnLow;
+  const bool few = few_rows(T, k, S), own_low = static_cast<int64_t>(T) * k <= kOwnLow;
   p->off_low = take(few && !own_low ? rows * k * 4 : 0);
   p->off_two = take(few ? 0 : rows * pieces_of(k) * 128);
   p->off_x = take(copies ? rows * dp * 2 : 0);
@@ -163,10 +164,11 @@ int allow_shared_memory() {
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return MTPC_ERR_CUDA;
   if (__atomic_load_n(&g_allowed[dev], __ATOMIC_ACQUIRE)) return MTPC_OK;
   const auto allow = [](auto* kernel, int bytes) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess; };
-  bool ok = allow(adaptor_low_kernel<false>, kSmemLimit) && allow(adaptor_low_kernel<true>, kSmemLimit) && allow(adapted_rows_kernel<1, false>, kSmemLimit);
-  ok = ok && allow(adapted_rows_kernel<1, true>, kSmemLimit) && allow(adapted_rows_kernel<2, true>, kSmemLimit);
-  ok = ok && allow(adapted_rows_kernel<4, true>, kSmemLimit) && allow(adapted_rows_kernel<8, true>, kSmemLimit);
-  ok = ok && allow(adapted_rows_kernel<2, false>, kSmemLimit) && allow(adapted_rows_kernel<4, false>, kSmemLimit) && allow(adapted_rows_kernel<8, false>, kSmemLimit);
+  bool ok = allow(adaptor_low_kernel<false>, kSmemLimit) && allow(adaptor_low_kernel<true>, kSmemLimit);
+  const auto allow_rows = [&](auto* s1, auto* s2, auto* s4, auto* s8) { ok = ok && allow(s1, kSmemLimit) && allow(s2, kSmemLimit) && allow(s4, kSmemLimit) && allow(s8, kSmemLimit); };
+  allow_rows(adapted_rows_kernel<1, true, 4>, adapted_rows_kernel<2, true, 4>, adapted_rows_kernel<4, true, 4>, adapted_rows_kernel<8, true, 4>);
+  allow_rows(adapted_rows_kernel<1, false, 4>, adapted_rows_kernel<2, false, 4>, adapted_rows_kernel<4, false, 4>, adapted_rows_kernel<8, false, 4>);
+  allow_rows(adapted_rows_kernel<1, false, 8>, adapted_rows_kernel<2, false, 8>, adapted_rows_kernel<4, false, 8>, adapted_rows_kernel<8, false, 8>);
   ok = ok && allow(adapted_gemm_kernel<false, 256, 2>, kSmemLimit) && allow(adapted_gemm_kernel<true, 256, 2>, kSmemLimit);
   ok = ok && allow(adapted_gemm_kernel<false, 128, 1>, kSmemLimit) && allow(adapted_gemm_kernel<true, 128, 1>, kSmemLimit);
   ok = ok && allow(adapted_gemm_kernel<false, 64, 1>, kSmemLimit) && allow(adapted_gemm_kernel<true, 64, 1>, kSmemLimit);
@@ -302,25 +304,24 @@ int launch_few_rows(const Rows& x, const Rows& W, const void* x_low, int64_t x_l
   p.k = k;
   p.kblocks = ceil_div(d, kBlockK);
   const int tiles = ceil_div(m, kBlockM);
-  // K is cut until the CTAs are as many as the device holds at once, two on an SM; behind low_rows_kernel and for few rows no further than into four (4096 x 4096, k = 16,
-  // two / four / eight parts, us: 5 rows 10.7 / 10.6 / 14, 16 rows 12.3 / 11.5 / 12.9, 64 rows 24 / 18.5 / 17.5; one row by itself 17.5 / 13.2 / 10.3).
-  const int most = own_low || T > 32 ? 8 : 4;
+  // K is cut into up to four parts until the CTAs are as many as the device holds at once, two on an SM; one row by itself and more than 32 into eight, the latter where each
+  // still has an SM of its own (4096 x 4096, k = 16, two / four / eight parts, us: one row 17.5 / 13.2 / 10.3, 16 rows 12.3 / 11.5 / 13.4, 64 rows 19.0 / 14.3 / 17.4; 1024 rows
+  // of W: 64 rows 13.0 / 7.9 / 7.5).
   int split = 1;
-  while (split < most && split * 2 <= p.kblocks && tiles * split <= kSms) split *= 2;
+  while (split < (own_low || T > 32 ? 8 : 4) && split * 2 <= p.kblocks && tiles * split * (split < 4 || own_low ? 1 : 2) <= kSms) split *= 2;
   p.stage_bytes = kABytes + p.tokens * kBlockK * 2;
-  p.stages = stages_of(p.stage_bytes, 2, kRowsShared);
-  p.wide = k % 8 == 0 && aligned(A, 16) && (own_low || aligned(low, 16));
+  const int shared = kRowsShared + (own_low ? 0 : ceil_div(T, split) * k * 4);       // (32 KB at most: two stages are left of the longest, and hold the sums)
+  p.stages = stages_of(p.stage_bytes, 2, shared);
+  p.wide = k % 8 == 0 && aligned(A, 16);
+  p.store4 = rows_allow(out, out_stride, 2, 4, T);
   p.own = l;
   p.own.low = user_low;
-  const size_t smem = kControl + kRowsShared + static_cast<size_t>(p.stages) * p.stage_bytes;
-  auto* kernel = own_low ? (split == 8   ? adapted_rows_kernel<8, true>
-                            : split == 4 ? adapted_rows_kernel<4, true>
-                            : split == 2 ? adapted_rows_kernel<2, true>
-                                         : adapted_rows_kernel<1, true>)
-                         : (split == 8   ? adapted_rows_kernel<8, false>
-                            : split == 4 ? adapted_rows_kernel<4, false>
-                            : split == 2 ? adapted_rows_kernel<2, false>
-                                         : adapted_rows_kernel<1, false>);
+  const size_t smem = kControl + shared + static_cast<size_t>(p.stages) * p.stage_bytes;
+  const bool many = ceil_div(T, 2 * split) > 4;           // rows of a thread
+  const auto pick = [&](auto* s1, auto* s2, auto* s4, auto* s8) { return split == 8 ? s8 : split == 4 ? s4 : split == 2 ? s2 : s1; };
+  auto* kernel = own_low ? pick(adapted_rows_kernel<1, true, 4>, adapted_rows_kernel<2, true, 4>, adapted_rows_kernel<4, true, 4>, adapted_rows_kernel<8, true, 4>)
+                 : many  ? pick(adapted_rows_kernel<1, false, 8>, adapted_rows_kernel<2, false, 8>, adapted_rows_kernel<4, false, 8>, adapted_rows_kernel<8, false, 8>)
+                         : pick(adapted_rows_kernel<1, false, 4>, adapted_rows_kernel<2, false, 4>, adapted_rows_kernel<4, false, 4>, adapted_rows_kernel<8, false, 4>);
   launch_clusters(kernel, split, tiles * split, kRowsThreads, smem, st, true, p);
   return check_launch();
 }
@@ -355,7 +356,7 @@ int mtpc_adapted_projection(const void* x, int64_t x_stride, const void* x_low, 
     if (!aligned(q, 2)) return MTPC_ERR_SHAPE;
   for (const void* q : {static_cast<const void*>(scale), static_cast<const void*>(row_adaptor), static_cast<const void*>(out_low), static_cast<const void*>(out_status)})
     if (!aligned(q, 4)) return MTPC_ERR_SHAPE;
-  const bool few = few_rows(T, S);
+  const bool few = few_rows(T, k, S);
   const bool copies = !mappable(x, x_stride, T, d) || !mappable(W, W_stride, m, d) ||
                       (!few && (!mappable(x_low, x_low_stride, T, d) || !mappable(A, k, 2, k) || !mappable(B, d, 2, d)));
   ForwardPlan plan;

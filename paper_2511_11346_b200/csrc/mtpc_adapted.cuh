@@ -797,9 +797,10 @@ __global__ void __launch_bounds__(128) low_rows_kernel(const LowRowsParams p) {
   }
 }
 
-// out of few rows: W's rows are the MMA's M (128 of them a cluster), the tokens its N. The CTAs of a cluster share K; their sums meet in shared memory, every CTA
-// adds up its share of the tokens and the adaptors' part. W, which is all but a few of the bytes, is asked into L2 while the kernels ahead still run.
-// A few rank values in all (T k <= kOwnLow): every cluster forms low itself, each CTA over its share of K, one launch less.
+// out of few rows: W's rows are the MMA's M (128 of them a cluster), the tokens its N. The CTAs of a cluster share K; each has every SPLIT-th token, forms its adaptors'
+// part, adds it to its own sums, and adds the cluster's sums of its tokens up, which meet in shared memory.
+// A few rank values in all (T k <= kOwnLow): every cluster forms low itself, each CTA over its share of K, one launch less; W, which is all but a few of the bytes, is asked
+// into L2 while the kernels ahead still run.
 struct RowsParams {
   CUtensorMap tm_w;                     // W [N, K]   box 64 x 128
   CUtensorMap tm_x;                     // x [T, K]   box 64 x tokens
@@ -812,7 +813,8 @@ struct RowsParams {
   uint64_t wait_limit_ns;
   int T, S, N, k, tokens;               // tokens: T rounded up to 16
   int kblocks, stages, stage_bytes;
-  int wide;                             // rows of A and of low are vectors of eight elements
+  int wide;                             // rows of A are vectors of eight elements
+  int store4;                           // rows of out allow stores of four elements
   // where low is formed here
   LowRowsParams own;                    // low: NULL or where it is wanted
 };
@@ -821,43 +823,57 @@ struct RowsShared {
   float part[kOwnLow], low[kOwnLow];
 };
 constexpr int kRowsThreads = 320;
-constexpr int kRowsAhead = 8;                     // rows of a thread whose adaptors' part is formed while W is on its way
-// The adaptors' part of column n of rows t, t + step, t + 2 step, t + 3 step (those that exist): begin() asks for A, finish() needs low.
+// The adaptors' part of column n of ROWS rows t, t + step, t + 2 step, ... (those that exist): begin() asks for A, finish() needs low, whose rows are low_step apart in
+// shared memory.
+template <int ROWS>
 struct RowsAdaptors {
-  int i[4];
-  Raw<__nv_bfloat16, 8> a[4][2];        // the first sixteen of A's row, where rows are vectors
-  __device__ __forceinline__ void begin(const RowsParams& p, int step, int t, int n) {
+  int i[ROWS];
+  Raw<__nv_bfloat16, 8> a[ROWS][2];     // sixteen of A's row, where rows are vectors
+  __device__ __forceinline__ const __nv_bfloat16* row(const RowsParams& p, int q, int n) const { return p.A + (static_cast<size_t>(i[q]) * p.N + n) * p.k; }
+  __device__ __forceinline__ void load(const RowsParams& p, int n, int j) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) i[q] = n < p.N ? adaptor_of(p.which, p.S, t + q * step, p.T) : -1;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
+    for (int q = 0; q < ROWS; ++q) {
       if (i[q] < 0) continue;
-      const __nv_bfloat16* row = p.A + (static_cast<size_t>(i[q]) * p.N + n) * p.k;
-      if (p.wide) {
-        a[q][0].load(row);
-        if (p.k > 8) a[q][1].load(row + 8);
-      }
-      if (!p.wide || p.k > 16) prefetch_l2(row + p.k - 1);
+      a[q][0].load(row(p, q, n) + j);
+      if (p.k > j + 8) a[q][1].load(row(p, q, n) + j + 8);
     }
   }
-  __device__ __forceinline__ void finish(const RowsParams& p, const float* low_rows, int step, int t, int n, float* y) {
+  __device__ __forceinline__ void begin(const RowsParams& p, int step, int t, int n) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      y[q] = 0.f;
-      if (i[q] < 0) continue;
-      const __nv_bfloat16* row = p.A + (static_cast<size_t>(i[q]) * p.N + n) * p.k;
-      const float* low = low_rows + static_cast<size_t>(t + q * step) * p.k;
-      if (p.wide) {
-        for (int j = 0; j < p.k; j += 8) {
-          const float4 l0 = reinterpret_cast<const float4*>(low + j)[0], l1 = reinterpret_cast<const float4*>(low + j)[1];
-          Raw<__nv_bfloat16, 8> v = j == 0 ? a[q][0] : a[q][1];
-          if (j >= 16) v.load(row + j);
-          const float l[8] = {l0.x, l0.y, l0.z, l0.w, l1.x, l1.y, l1.z, l1.w};
+    for (int q = 0; q < ROWS; ++q) i[q] = n < p.N ? adaptor_of(p.which, p.S, t + q * step, p.T) : -1;
+    if (p.wide) load(p, n, 0);
+    if (!p.wide || p.k > 16) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) y[q] = fmaf(v.value(e), l[e], y[q]);
+      for (int q = 0; q < ROWS; ++q)
+        if (i[q] >= 0) prefetch_l2(row(p, q, n) + p.k - 1);
+    }
+  }
+  __device__ __forceinline__ void finish(const RowsParams& p, const float* low_row, int low_step, int n, float* y) {
+#pragma unroll
+    for (int q = 0; q < ROWS; ++q) y[q] = 0.f;
+    if (p.wide) {
+      for (int j = 0; j < p.k; j += 16) {
+        if (j > 0) load(p, n, j);
+#pragma unroll
+        for (int q = 0; q < ROWS; ++q) {
+          if (i[q] < 0) continue;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            if (j + 8 * h >= p.k) break;
+            const float4* low = reinterpret_cast<const float4*>(low_row + q * low_step + j + 8 * h);
+            const float4 l0 = low[0], l1 = low[1];
+            const float l[8] = {l0.x, l0.y, l0.z, l0.w, l1.x, l1.y, l1.z, l1.w};
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[q] = fmaf(a[q][h].value(e), l[e], y[q]);
+          }
         }
-      } else {
-        for (int j = 0; j < p.k; ++j) y[q] = fmaf(to_f32(row[j]), low[j], y[q]);
+      }
+    } else {
+#pragma unroll
+      for (int q = 0; q < ROWS; ++q) {
+        if (i[q] < 0) continue;
+        const __nv_bfloat16* at = row(p, q, n);
+        for (int j = 0; j < p.k; ++j) y[q] = fmaf(to_f32(at[j]), low_row[q * low_step + j], y[q]);
       }
     }
   }
@@ -902,13 +918,16 @@ __device__ __forceinline__ void own_low_parts(const LowRowsParams& p, int c0, in
 }
 __device__ __forceinline__ void rows_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }      // warps 2 to 9
 
-template <int SPLIT, bool OWN_LOW>
-__global__ void __launch_bounds__(kRowsThreads) adapted_rows_kernel(const __grid_constant__ RowsParams p) {
+// AHEAD: rows of a thread whose adaptors' part is formed while W is on its way (all loads in flight together: eight rows a thread, 4096 x 4096, 64 rows 15.1 -> 14.3 us against
+// twice four; one or two, 1024 x 1024, 16 rows 5.5 -> 5.9).
+template <int SPLIT, bool OWN_LOW, int AHEAD>
+__global__ void __launch_bounds__(kRowsThreads, 2) adapted_rows_kernel(const __grid_constant__ RowsParams p) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw_addr = smem_u32(smem_raw);
   const uint32_t tiles_addr = (raw_addr + 1023u) & ~1023u;
   GemmControl* ctl = reinterpret_cast<GemmControl*>(smem_raw + (tiles_addr - raw_addr) + static_cast<size_t>(p.stages) * p.stage_bytes);
   RowsShared* shared = reinterpret_cast<RowsShared*>((reinterpret_cast<uintptr_t>(ctl + 1) + 15) & ~static_cast<uintptr_t>(15));
+  float* lows = reinterpret_cast<float*>(shared + 1);                // of this CTA's tokens [T / SPLIT][k] (without OWN_LOW)
   const int warp = static_cast<int>(warp_uniform(threadIdx.x >> 5));
   const int lane = threadIdx.x & 31;
   const int rank = static_cast<int>(blockIdx.x % SPLIT), tile = blockIdx.x / SPLIT;
@@ -936,7 +955,7 @@ __global__ void __launch_bounds__(kRowsThreads) adapted_rows_kernel(const __grid
   tc_fence_after();
   const uint32_t tmem_base = warp_uniform(ctl->tmem_base);
   const uint32_t full0 = smem_u32(&ctl->full[0]), empty0 = smem_u32(&ctl->empty[0]);
-  float part[kRowsAhead];               // the adaptors' part of this CTA's rows
+  float part[AHEAD];                    // the adaptors' part of this CTA's rows
   // sums [tokens][128] fp32, over the stages once these have been multiplied
   float* sums = reinterpret_cast<float*>(smem_raw + (tiles_addr - raw_addr));
 
@@ -990,17 +1009,21 @@ __global__ void __launch_bounds__(kRowsThreads) adapted_rows_kernel(const __grid
       }
       own_low_parts(p.own, kb0 * kBlockK, min(kb1 * kBlockK, p.own.d), warp - 2, lane, shared->part);
     } else {
-      RowsAdaptors ra;
+      RowsAdaptors<AHEAD> ra;
       ra.begin(p, 2 * SPLIT, first, n);
+      for (int t = first + AHEAD * 2 * SPLIT; t < p.T; t += 2 * SPLIT) {
+        const int i = adaptor_of(p.which, p.S, t, p.T);
+        if (i >= 0 && n < p.N) prefetch_l2(p.A + (static_cast<size_t>(i) * p.N + n) * p.k);
+      }
       grid_dependency_wait();
       grid_launch_dependents();
-      ra.finish(p, p.low, 2 * SPLIT, first, n, part);
-#pragma unroll
-      for (int q = 4; q < kRowsAhead; q += 4) {
-        if (first + q * 2 * SPLIT >= p.T) break;
-        ra.begin(p, 2 * SPLIT, first + q * 2 * SPLIT, n);
-        ra.finish(p, p.low, 2 * SPLIT, first + q * 2 * SPLIT, n, part + q);
+      const int values = (p.T - rank + SPLIT - 1) / SPLIT * p.k;
+      for (int e = threadIdx.x - 64; e < values; e += 256) {
+        const int j = e / p.k;
+        lows[e] = p.low[static_cast<size_t>(rank + SPLIT * j) * p.k + (e - j * p.k)];
       }
+      rows_sync();
+      ra.finish(p, lows + sub * p.k, 2 * p.k, n, part);
     }
     if (bounded_wait_warp(smem_u32(&ctl->tfull[0]), 0, ctl, p.status, lane)) {
       tc_fence_after();
@@ -1012,38 +1035,54 @@ __global__ void __launch_bounds__(kRowsThreads) adapted_rows_kernel(const __grid
       }
     }
     tc_fence_before();
+    if (!OWN_LOW) {
+      rows_sync();                                                   // this CTA's sums are there: its tokens' parts are added to them
+      float* mine = sums + quarter * 32 + lane;
+#pragma unroll
+      for (int q = 0; q < AHEAD; ++q)
+        if (first + q * 2 * SPLIT < p.T) mine[(first + q * 2 * SPLIT) * kBlockM] += part[q];
+      for (int q = AHEAD; first + q * 2 * SPLIT < p.T; q += AHEAD) {
+        RowsAdaptors<AHEAD> ra;
+        ra.begin(p, 2 * SPLIT, first + q * 2 * SPLIT, n);
+        ra.finish(p, lows + (sub + 2 * q) * p.k, 2 * p.k, n, part);
+#pragma unroll
+        for (int e = 0; e < AHEAD; ++e)
+          if (first + (q + e) * 2 * SPLIT < p.T) mine[(first + (q + e) * 2 * SPLIT) * kBlockM] += part[e];
+      }
+    }
   }
   __syncthreads();
   cluster_sync_all();                                                // the other CTAs' sums
-  if (warp >= 2) {
+  if (OWN_LOW && warp >= 2) {
     const int m = (warp & 3) * 32 + lane, n = tile * kBlockM + m, first = rank + SPLIT * ((warp - 2) >> 2);
     const uint32_t own = smem_u32(sums) + 4u * m;
-    if (OWN_LOW) {
-      const int id = threadIdx.x - 64;
-      if (id < p.T * p.k) {
-        float v[SPLIT], all = 0.f;
+    const int id = threadIdx.x - 64;
+    if (id < p.T * p.k) {
+      float v[SPLIT], all = 0.f;
 #pragma unroll
-        for (int r = 0; r < SPLIT; ++r) v[r] = ld_cluster_f32(cluster_map_shared(smem_u32(shared->part + id), r));
+      for (int r = 0; r < SPLIT; ++r) v[r] = ld_cluster_f32(cluster_map_shared(smem_u32(shared->part + id), r));
 #pragma unroll
-        for (int r = 0; r < SPLIT; ++r) all += v[r];
-        const int t = id / p.k, i = adaptor_of(p.which, p.S, t, p.T);
-        const bool refused = adaptor_refused(p.which, p.S, t);
-        all = i < 0 ? 0.f : all * (p.own.scale == nullptr ? 1.f : p.own.scale[i]);
-        shared->low[id] = all;
-        if (blockIdx.x == 0) {
-          if (p.own.low != nullptr) p.own.low[id] = refused ? CUDART_NAN_F : all;
-          if (refused && p.own.status != nullptr) atomicOr(p.own.status, kStatusBadAdaptor);
-        }
+      for (int r = 0; r < SPLIT; ++r) all += v[r];
+      const int t = id / p.k, i = adaptor_of(p.which, p.S, t, p.T);
+      const bool refused = adaptor_refused(p.which, p.S, t);
+      all = i < 0 ? 0.f : all * (p.own.scale == nullptr ? 1.f : p.own.scale[i]);
+      shared->low[id] = all;
+      if (blockIdx.x == 0) {
+        if (p.own.low != nullptr) p.own.low[id] = refused ? CUDART_NAN_F : all;
+        if (refused && p.own.status != nullptr) atomicOr(p.own.status, kStatusBadAdaptor);
       }
-      rows_sync();
     }
-    auto finish = [&](int t, const float* y) {                        // four rows: all loads in flight together
-      float sum[4][SPLIT];
+    rows_sync();
+    for (int t = first; t < p.T; t += 8 * SPLIT) {
+      float y[4], sum[4][SPLIT];
+      RowsAdaptors<4> ra;
+      ra.begin(p, 2 * SPLIT, t, n);
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
+      for (int q = 0; q < 4; ++q)                                    // four rows: all loads in flight together
 #pragma unroll
         for (int r = 0; r < SPLIT; ++r)
           sum[q][r] = t + q * 2 * SPLIT < p.T ? ld_cluster_f32(cluster_map_shared(own + 4u * kBlockM * (t + q * 2 * SPLIT), r)) : 0.f;
+      ra.finish(p, shared->low + t * p.k, 2 * SPLIT * p.k, n, y);
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const int at = t + q * 2 * SPLIT;
@@ -1053,16 +1092,31 @@ __global__ void __launch_bounds__(kRowsThreads) adapted_rows_kernel(const __grid
         for (int r = 0; r < SPLIT; ++r) all += sum[q][r];
         p.out[at * p.out_stride + n] = __float2bfloat16_rn(adaptor_refused(p.which, p.S, at) ? CUDART_NAN_F : all);
       }
-    };
+    }
+  } else if (warp >= 2) {
+    // a warp to a token, four columns to a lane
+#pragma unroll 2
+    for (int t = rank + SPLIT * (warp - 2); t < p.T; t += SPLIT * 8) {
+      const uint32_t own = smem_u32(sums + t * kBlockM + 4 * lane);
+      float4 v[SPLIT];
 #pragma unroll
-    for (int q = 0; q < (OWN_LOW ? 0 : kRowsAhead); q += 4)
-      if (first + q * 2 * SPLIT < p.T) finish(first + q * 2 * SPLIT, part + q);
-    for (int t = first + (OWN_LOW ? 0 : kRowsAhead * 2 * SPLIT); t < p.T; t += 8 * SPLIT) {
-      float more[4];
-      RowsAdaptors ra;
-      ra.begin(p, 2 * SPLIT, t, n);
-      ra.finish(p, OWN_LOW ? shared->low : p.low, 2 * SPLIT, t, n, more);
-      finish(t, more);
+      for (int r = 0; r < SPLIT; ++r) v[r] = ld_cluster_v4(cluster_map_shared(own, r));
+      float x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int r = 0; r < SPLIT; ++r) x[0] += v[r].x, x[1] += v[r].y, x[2] += v[r].z, x[3] += v[r].w;
+      const bool refused = adaptor_refused(p.which, p.S, t);
+      __align__(8) __nv_bfloat16 y[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) y[q] = __float2bfloat16_rn(refused ? CUDART_NAN_F : x[q]);
+      const int n = tile * kBlockM + 4 * lane;
+      __nv_bfloat16* dst = p.out + t * p.out_stride + n;
+      if (p.store4 && n + 4 <= p.N) {
+        *reinterpret_cast<uint2*>(dst) = *reinterpret_cast<const uint2*>(y);
+      } else {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          if (n + q < p.N) dst[q] = y[q];
+      }
     }
   }
   tc_fence_before();
