@@ -62,7 +62,6 @@ int check_sizes(int T, int d, int m, int k, int S) {
 int up8(int x) { return (x + 7) / 8 * 8; }
 int rank16(int k) { return (k + 15) / 16 * 16; }
 int pieces_of(int k) { return (k + kPieceRank - 1) / kPieceRank; }
-int chunks_of(int K) { return ceil_div(K, kChunkBlocks * kBlockK); }
 
 struct ForwardPlan {
   size_t off_low, off_two, off_x, off_x_low, off_W, off_A, off_B, total;
@@ -184,7 +183,9 @@ int stages_of(int stage_bytes, int ctas_per_sm = 1, int beside = 0) {
 
 // ---------------------------------------------------------------- launches
 // low or v: rows [T, K] times the factors, if rows are given, and what else p asks for.
-int launch_low(LowParams& p, const Rows& rows, const Rows& factors, bool mn, const int* which, int T, int K, int k, int S, unsigned* status, cudaStream_t st) {
+// product_ctas: those of the product behind it, or 0.
+int launch_low(LowParams& p, const Rows& rows, const Rows& factors, bool mn, const int* which, int T, int K, int k, int S, int product_ctas, unsigned* status,
+               cudaStream_t st) {
   p.which = which;
   p.status = status;
   p.wait_limit_ns = kWaitLimitNs;
@@ -203,8 +204,15 @@ int launch_low(LowParams& p, const Rows& rows, const Rows& factors, bool mn, con
     if (rc == MTPC_OK) rc = mn ? map_rows(&p.tm_f, factors.p, K, k, factors.stride, 64, S, factor_columns(p.k16)) : map_rows(&p.tm_f, factors.p, k, K, factors.stride, rank16(k), S);
     if (rc != MTPC_OK) return rc;
     p.kblocks = ceil_div(K, kBlockK);
-    p.chunks = chunks_of(K);
-    while (p.split < 8 && p.split * 2 <= p.chunks && p.tiles * p.split <= kSms) p.split *= 2;
+    // CTAs that share a tile's K: four (two to eight, K = 4096, us: 8192 rows 191 / 183 / 183, 2005 rows to 4096 columns 35.3 / 32.3 / 36.0 at rank 64), since clusters of eight
+    // find few places, but for three tiles and less (129 rows 28.6 / 19.7 / 15.9). Where the product's last round leaves SMs free, and one pass over the rows gives low, no more
+    // than those: the product starts beside them (gradients of 1024 x 4096, 4096 columns 33.9 / 40.4 / 39.0).
+    const int spare = product_ctas == 0 ? kSms : (kSms - product_ctas % kSms) % kSms;
+    int most = p.tiles <= 3 ? 8 : 4;
+    if (p.group >= 4 && p.tiles * 2 <= spare) most = std::min(most, spare / p.tiles);
+    while (p.split * 2 <= most && p.split * 4 <= p.kblocks && p.tiles * p.split <= kSms) p.split *= 2;
+    p.chunk_blocks = std::min(kChunkBlocks, ceil_div(p.kblocks, p.split));
+    p.chunks = ceil_div(p.kblocks, p.chunk_blocks);
   }
   p.present_blocks = p.present ? ceil_div(T, 32 * 64) : 0;
   const int beside = ceil_div(p.present_blocks, p.split) * p.split;
@@ -236,7 +244,22 @@ int launch_gemm(AdaptedParams& p, const Rows& a, const Rows& b, const __nv_bfloa
   launch_clusters(adapted_gemm_kernel<B_MN, TN, CTAS>, CTAS, workers * CTAS, kAdaptedThreads, smem, st, true, p);
   return check_launch();
 }
-// rows [T, K] times W (N rows of K, or with b_mn K rows of N), plus two terms of low times the factors; kblocks 0: these alone.
+// The tiles of a product of T rows and N columns over kb K blocks: their columns, and the CTAs that a tile has.
+struct ProductTile {
+  int columns, ctas, count;             // count: of tiles
+};
+// Cycles that a K block of a tile takes and that its rest does, by the bytes that an SM gets from L2 and its MMAs' time, whichever is longer; rows that lie across lines of L2
+// cost the smaller tiles, which read more, half as much again. 4096 x 4096, us for pairs / 128 / 64 columns: 256 rows 28 / 18 / 16, 512 27 / 19 / 25, 768 28 / 36 / 38.
+ProductTile product_tile(int T, int N, int kb, const Rows& a, const Rows& b) {
+  const bool across = a.stride % 64 != 0 || b.stride % 64 != 0;
+  const int pairs = ceil_div(T, 256) * ceil_div(N, 256), wides = ceil_div(T, 128) * ceil_div(N, 128), narrows = ceil_div(T, 128) * ceil_div(N, 64);
+  const double pair = ceil_div(pairs, kSms / 2) * (kb * 560.0 + 2000), wide = ceil_div(wides, kSms) * (kb * (across ? 700.0 : 450.0) + 1500);
+  const double narrow = ceil_div(narrows, kSms) * (kb * (across ? 550.0 : 350.0) + 1200);
+  if (pair <= wide && pair <= narrow) return ProductTile{256, 2, pairs};
+  return wide <= narrow ? ProductTile{128, 1, wides} : ProductTile{64, 1, narrows};
+}
+int k_blocks(int K, bool shared, int k, bool adaptors) { return (shared ? ceil_div(K, kBlockK) : 0) + (adaptors ? 2 * pieces_of(k) : 0); }
+// rows [T, K] times W (N rows of K, or with b_mn K rows of N), plus two terms of low times the factors; shared false: these alone.
 int launch_product(const Rows& a, const Rows& b, const __nv_bfloat16* two, const Rows& f, bool b_mn, const int* which, int T, int K, int N, int k, int S,
                    bool shared, bool adaptors, void* out, int64_t out_stride, unsigned* status, cudaStream_t st) {
   AdaptedParams p;
@@ -253,16 +276,9 @@ int launch_product(const Rows& a, const Rows& b, const __nv_bfloat16* two, const
   p.pieces = adaptors ? pieces_of(k) : 0;
   p.kblocks = shared ? ceil_div(K, kBlockK) : 0;
   p.store = rows_allow(out, out_stride, 2, 16, T) ? 32 : rows_allow(out, out_stride, 2, 8, T) ? 16 : 2;
-  // Cycles that a K block of a tile takes and that its rest does, by the bytes that an SM gets from L2 and its MMAs' time, whichever is longer; rows that lie across lines of L2
-  // cost the smaller tiles, which read more, half as much again. 4096 x 4096, us for pairs / 128 / 64 columns: 256 rows 28 / 18 / 16, 512 27 / 19 / 25, 768 28 / 36 / 38.
-  const bool across = a.stride % 64 != 0 || b.stride % 64 != 0;
-  const double kb = p.kblocks + 2.0 * p.pieces;
-  const double pair = ceil_div(static_cast<long long>(ceil_div(T, 256)) * ceil_div(N, 256), kSms / 2) * (kb * 560 + 2000);
-  const double wide = ceil_div(static_cast<long long>(ceil_div(T, 128)) * ceil_div(N, 128), kSms) * (kb * (across ? 700 : 450) + 1500);
-  const double narrow = ceil_div(static_cast<long long>(ceil_div(T, 128)) * ceil_div(N, 64), kSms) * (kb * (across ? 550 : 350) + 1200);
-  if (pair <= wide && pair <= narrow)
-    return b_mn ? launch_gemm<true, 256, 2>(p, a, b, two, f, K, st) : launch_gemm<false, 256, 2>(p, a, b, two, f, K, st);
-  if (wide <= narrow) return b_mn ? launch_gemm<true, 128, 1>(p, a, b, two, f, K, st) : launch_gemm<false, 128, 1>(p, a, b, two, f, K, st);
+  const int columns = product_tile(T, N, k_blocks(K, shared, k, adaptors), a, b).columns;
+  if (columns == 256) return b_mn ? launch_gemm<true, 256, 2>(p, a, b, two, f, K, st) : launch_gemm<false, 256, 2>(p, a, b, two, f, K, st);
+  if (columns == 128) return b_mn ? launch_gemm<true, 128, 1>(p, a, b, two, f, K, st) : launch_gemm<false, 128, 1>(p, a, b, two, f, K, st);
   return b_mn ? launch_gemm<true, 64, 1>(p, a, b, two, f, K, st) : launch_gemm<false, 64, 1>(p, a, b, two, f, K, st);
 }
 
@@ -381,7 +397,8 @@ int mtpc_adapted_projection(const void* x, int64_t x_stride, const void* x_low, 
   l.scale = scale;
   l.low = out_low;
   l.two = reinterpret_cast<__nv_bfloat16*>(ws + plan.off_two);
-  if ((rc = launch_low(l, lr, Br, false, row_adaptor, T, d, k, S, out_status, st)) != MTPC_OK) return rc;
+  const ProductTile tile = product_tile(T, m, k_blocks(d, true, k, true), xr, Wr);
+  if ((rc = launch_low(l, lr, Br, false, row_adaptor, T, d, k, S, tile.count * tile.ctas, out_status, st)) != MTPC_OK) return rc;
   return launch_product(xr, Wr, l.two, Ar, false, row_adaptor, T, d, m, k, S, true, true, out, out_stride, out_status, st);
 }
 
@@ -448,7 +465,9 @@ int mtpc_adapted_projection_backward(const void* x_low, int64_t x_low_stride, co
     l.whole = l.present + static_cast<size_t>(ceil_div(T, 32 * 64)) * S;
   }
   const bool sums = d_x || d_x_low || dB;
-  if ((sums || dA) && (rc = launch_low(l, sums ? gr : Rows{nullptr, 0}, Ar, true, row_adaptor, T, m, k, S, out_status, st)) != MTPC_OK) return rc;
+  const ProductTile tile = d_x ? product_tile(T, d, k_blocks(m, true, k, d_x_low == nullptr), gr, Wr) : ProductTile{0, 0, 0};
+  if ((sums || dA) && (rc = launch_low(l, sums ? gr : Rows{nullptr, 0}, Ar, true, row_adaptor, T, m, k, S, tile.count * tile.ctas, out_status, st)) != MTPC_OK)
+    return rc;
   if (d_x && (rc = launch_product(gr, Wr, two, Br, true, row_adaptor, T, m, d, k, S, true, d_x_low == nullptr, d_x, d_x_stride, out_status, st)) != MTPC_OK) return rc;
   if (d_x_low && (rc = launch_product(gr, Rows{nullptr, 0}, two, Br, true, row_adaptor, T, m, d, k, S, false, true, d_x_low, d_x_low_stride, out_status, st)) != MTPC_OK)
     return rc;

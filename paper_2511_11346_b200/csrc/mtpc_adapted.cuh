@@ -27,7 +27,7 @@ namespace mtpc {
 constexpr uint32_t kStatusBadAdaptor = 32u;
 constexpr int kMaxRank = 64;
 constexpr int kPieceRank = 32;                     // rank columns of one K block: their high terms, then their low ones
-constexpr int kChunkBlocks = 8;                    // K blocks of one accumulator where fp32 is returned
+constexpr int kChunkBlocks = 8;                    // K blocks of one accumulator at most where fp32 is returned
 
 // ---- instructions
 // 3-D tiled loads: x innermost (a multiple of 16 bytes), then row, then matrix.
@@ -156,7 +156,7 @@ struct LowParams {
   unsigned* status;                     // or NULL
   uint64_t wait_limit_ns;
   int T, S, k, k16, pieces;             // k16: the rank, rounded up to 16
-  int kblocks, chunks, tiles, split, stages, stage_bytes;            // split: CTAs of a cluster; chunks 0: no sums are wanted
+  int kblocks, chunk_blocks, chunks, tiles, split, stages, stage_bytes;              // split: CTAs of a cluster; chunks 0: no sums are wanted
   int group;                            // adaptors whose factors share a stage with a tile of the rows, 64 columns in all: one pass over the rows gives the products with all of them,
                                         // and every row takes those of its own
   int present_blocks;
@@ -295,7 +295,7 @@ __global__ void __launch_bounds__(kLowThreads, 2) adaptor_low_kernel(const __gri
     uint32_t stage = 0, phase = 0, issued = 0;
     bool ok = true;
     for (int c = rank; c < p.chunks && ok; c += p.split) {
-      const int kb0 = c * kChunkBlocks, kb1 = min(p.kblocks, kb0 + kChunkBlocks);
+      const int kb0 = c * p.chunk_blocks, kb1 = min(p.kblocks, kb0 + p.chunk_blocks);
       TileAdaptors<4> each = ta;
       while (ok) {
         int of[4], n = 0;
@@ -332,7 +332,7 @@ __global__ void __launch_bounds__(kLowThreads, 2) adaptor_low_kernel(const __gri
     const uint64_t a_desc0 = umma_smem_desc_sw128(tiles_addr);
     const uint64_t f_desc0 = F_MN ? umma_smem_desc_factor(tiles_addr + kABytes, factor_columns(p.k16)) : umma_smem_desc_sw128(tiles_addr + kABytes);
     for (int c = rank; c < p.chunks && ok; c += p.split) {
-      const int kb0 = c * kChunkBlocks, kb1 = min(p.kblocks, kb0 + kChunkBlocks);
+      const int kb0 = c * p.chunk_blocks, kb1 = min(p.kblocks, kb0 + p.chunk_blocks);
       TileAdaptors<4> each = ta;
       while (ok) {
         int n = 0;
