@@ -81,14 +81,17 @@ void plan_forward(int T, int d, int m, int k, int S, bool copies, ForwardPlan* p
   p->total = off;
 }
 
-// Runs of row blocks that the adaptors' gradients are cut into: what takes least, a run being its blocks and about four more for its start and end. An adaptor's
-// rows lie beside each other, so that up to S runs cut few adaptors' rows (n: runs that have rows); adding the runs up takes a quarter of a block each.
+// Runs of row blocks that the adaptors' gradients are cut into: what takes least, in us: 0.45 a block, a run being its blocks and about four more for its start and end; 3 for
+// the launch that adds the runs up, 0.12 a run, and their parts' bytes, which are written and read (8192 rows, 4096 to 1024 columns, k = 64, eight adaptors: one run 90 us, eleven,
+// which share the work more evenly, 140). An adaptor's rows lie beside each other, so that up to S runs cut few adaptors' rows (n: runs that have rows).
 int grad_splits(int tiles, int S, int blocks, int k16) {
   int best = 1;
   double least = 0.0;
+  const double parts = static_cast<double>(S) * tiles * (kBlockM * 4 * 2) * k16 / 5e6;
   for (int s = 1; s <= 32 && s <= std::max(1, blocks / 4); ++s) {
     const int n = std::max(s, S);
-    const double cost = static_cast<double>(ceil_div(static_cast<long long>(tiles) * n, kSms * grad_ctas(k16))) * (static_cast<double>(blocks) / n + 4.0) + 0.25 * s;
+    const double cost =
+        ceil_div(static_cast<long long>(tiles) * n, kSms * grad_ctas(k16)) * (static_cast<double>(blocks) / n + 4.0) * 0.45 + (s > 1 ? 3.0 + s * (0.12 + parts) : 0.0);
     if (s == 1 || cost < least * 0.97) best = s, least = cost;
   }
   return best;
