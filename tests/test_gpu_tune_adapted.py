@@ -316,3 +316,24 @@ def test_calls_that_are_refused():
     wide = torch.zeros(1, 65, 64, device="cuda").bfloat16(), torch.zeros(1, 48, 65, device="cuda").bfloat16()
     with pytest.raises(B.MtpcError):
         f(x, W, wide[1], wide[0], None, None, out)
+
+
+@pytest.mark.parametrize("T", [2, 9, 33, 70, 128])
+@pytest.mark.parametrize("d,m,k,S", [(64, 300, 64, 16), (40, 19100, 3, 16), (200, 9700, 16, 20), (300, 1100, 24, 16), (1024, 136, 64, 16), (2000, 130, 9, 12)])
+def test_few_rows_in_every_cluster_size(T, d, m, k, S):
+    x, W, A, Bf, scale, which, g = make(T, d, m, k, S, "mixed", T + m)
+    out, low = check_forward(x, W, A, Bf, scale, which, pad=T % 3)
+    # rows by themselves and rows of a longer batch (tiles) agree within their errors, and a row does not depend on the others
+    alone = torch.empty(T, m, dtype=x.dtype, device="cuda")
+    for t in range(0, T, 31):
+        B.mtpc_adapted_projection(x[t:t + 1], W, A, Bf, scale, which[t:t + 1], alone[t:t + 1])
+        assert (alone[t].double() - out[t].double()).abs().max().item() <= 0.05 * out[t].double().abs().max().item() + 1e-3
+
+
+@pytest.mark.parametrize("T,d,m,k,S", [(300, 576, 576, 16, 3), (300, 1088, 72, 40, 2), (700, 300, 330, 16, 4), (520, 2112, 64, 8, 2), (140, 2500, 1100, 64, 3)])
+def test_low_of_chunks_of_every_length(T, d, m, k, S):
+    x, W, A, Bf, scale, which, g = make(T, d, m, k, S, "runs", T + d)
+    _, low = check_forward(x, W, A, Bf, scale, which)
+    d_out = (torch.randn(T, m, device="cuda", generator=g) * 0.1).bfloat16()
+    check_backward(x, W, A, Bf, scale, which, low, d_out)
+    check_backward(x, W, A, Bf, scale, which, low, d_out, apart=True)
