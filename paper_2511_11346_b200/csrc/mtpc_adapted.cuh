@@ -3,7 +3,7 @@
 //   d_x[t] = W^T g[t] + B[i]^T v[t], v[t] = scale[i] A[i]^T g[t],    dA[i] = sum of g low^T, dB[i] = sum of v x'^T over the rows of i
 // x, W, A, B, g bf16; low, v, dA, dB fp32; out, d_x bf16.
 //
-// adaptor_low_kernel    low or v of many rows: K in chunks of 512, each its own accumulator, added up in fp32. The tensor cores round every accumulation towards
+// adaptor_low_kernel    low or v of many rows: K in chunks of 512 at most, each its own accumulator, added up in fp32. The tensor cores round every accumulation towards
 //                       zero, so that one accumulator over K = 4096 is 4e-6 off, chunks 4e-7. The result is split into bf16 terms: two (16 bits) for the
 //                       product with A or B whose result is rounded to bf16, three (24 bits) for the fp32 gradients.
 // adapted_gemm_kernel   the shared product; the adaptors of a tile's rows follow as K blocks of their own.
@@ -142,6 +142,7 @@ struct TileAdaptors {
 // ---- low (or v) of many rows
 // A cluster has a tile of 128 rows; its CTAs share the chunks of K, add theirs up in registers and meet in shared memory, where each finishes its share of the rows:
 // sum, scale, low, its terms. For the gradients it splits given values into terms as well, and blocks behind the tiles' say which 64 rows have an adaptor's.
+// Bound by the rows' bytes where there are many (8192 x 4096, k = 16: 15.4 us, 10 of them HBM's), by its chain of latencies where there are few (512 rows 6.3).
 struct LowParams {
   CUtensorMap tm_a;                     // rows [T, K]          box 64 x 128
   CUtensorMap tm_f;                     // factors: B [S, k, K] box 64 x k16 (K-major), or A [S, K, k] box factor_columns(k16) x 64 (MN-major)
@@ -445,6 +446,7 @@ __global__ void __launch_bounds__(kLowThreads, 2) adaptor_low_kernel(const __gri
 }
 
 // ---- the shared product and the adaptors' part
+// Bound by the tensor pipe: 8192 x 4096 x 4096, k = 16, eight adaptors 172 us with the pipe 88 % busy; 2005 rows in one round of 64 pairs 26 us (at the peak rate 20).
 struct AdaptedParams {
   CUtensorMap tm_a;                     // rows [T, K]              box 64 x 128
   CUtensorMap tm_b;                     // W [N, K] box 64 x (TN / CTAS), or [K, N] box 64 x 64 (MN-major)
@@ -741,7 +743,8 @@ __global__ void __launch_bounds__(kAdaptedThreads, 1) adapted_gemm_kernel(const 
 }
 
 // ---- few rows
-// low of few rows: a block has four of a row's rank values, its warps a quarter of d each.
+// low of few rows: a block has four of a row's rank values, its warps a quarter of d each. Bound by latency: 64 rows, d = 4096, k = 16, 32 adaptors 5 us, of which 1.4 are
+// the dot products.
 struct LowRowsParams {
   const __nv_bfloat16 *x, *B;
   int64_t x_stride;
@@ -1132,7 +1135,8 @@ __global__ void __launch_bounds__(kRowsThreads, 2) adapted_rows_kernel(const __g
 
 // ---- gradients of the adaptors
 // dA (product 0: rows g, terms of low) and dB (product 1: rows x', terms of v): 128 columns of the rows are the MMA's M, the 3 k16 terms its N, rows its K. An item is
-// one tile of columns of one adaptor over one of `splits` runs of row blocks; every eight blocks the accumulators are added to fp32 registers.
+// one tile of columns of one adaptor over one of `splits` runs of row blocks; every eight blocks the accumulators are added to fp32 registers. Bound by the rows' bytes:
+// 8192 rows, 4096 + 4096 columns, k = 16: 26 us for 136 MB.
 struct GradParams {
   CUtensorMap tm_rows[2];                        // [T, cols]    box 64 x 64
   CUtensorMap tm_terms[2];                       // [T, 3 k16]   box 64 x 64
@@ -1394,7 +1398,7 @@ __global__ void __launch_bounds__(kGradThreads, grad_ctas(K16)) adaptor_grad_ker
   }
 }
 
-// Adds the splits' parts up, in order: a thread has one column's rank values four at a time.
+// Adds the splits' parts up, in order: a thread has one column's rank values four at a time. (Four runs of 64 tiles of 128 columns, k = 16: 6 us, a launch's latency.)
 __global__ void __launch_bounds__(256) adaptor_grad_join_kernel(const __grid_constant__ GradParams p, int k16) {
   grid_dependency_wait();
   grid_launch_dependents();
@@ -1426,7 +1430,7 @@ __global__ void __launch_bounds__(256) adaptor_grad_join_kernel(const __grid_con
   }
 }
 
-// ---- rows that the tensor maps cannot address (an address or pitch that is no multiple of 16 bytes), copied to ones that they can
+// ---- rows that the tensor maps cannot address (an address or pitch that is no multiple of 16 bytes), copied to ones that they can (2005 and 2003 rows of 1001: 7 us)
 struct CopyRows {
   const __nv_bfloat16* src;
   __nv_bfloat16* dst;

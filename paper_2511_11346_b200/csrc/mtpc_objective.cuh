@@ -14,7 +14,8 @@
 // Work is dealt in items: a warp has one of P equal slices of one sequence, so that long sequences among short ones spread over the device and no
 // position has to look for its sequence. Weights need the counts of valid positions first, so the call goes over the data twice (the mask alone
 // for the counts, every warp over that of its own sequence where that is all it needs; logp and ref for the sums of pairs). Few positions: all phases in one launch of one cluster, with its barrier between
-// them (a chain of four kernels of 2 us each otherwise); many: a launch for each phase. Bound by launches, and by HBM from a million positions on.
+// them (a chain of four kernels of 2 us each otherwise); many: a launch for each phase. Bound by launches and their chains of loads: 1.6 million masked positions 15 us (policy) and 12 (preference) in a
+// graph, of which the bytes are 4 and 3; a few hundred positions 8, mostly the host's.
 #pragma once
 #include <math_constants.h>
 #include <stdint.h>
