@@ -14,7 +14,7 @@
 // Work is dealt in items: a warp has one of P equal slices of one sequence, so that long sequences among short ones spread over the device and no
 // position has to look for its sequence. Weights need the counts of valid positions first, so the call goes over the data twice (the mask alone
 // for the counts, every warp over that of its own sequence where that is all it needs; logp and ref for the sums of pairs). Few positions: all phases in one launch of one cluster, with its barrier between
-// them (a chain of four kernels of 2 us each otherwise); many: a launch for each phase. Bound by launches and their chains of loads: 1.6 million masked positions 15 us (policy) and 12 (preference) in a
+// them (a chain of four kernels of 2 us each otherwise); many: a launch for each phase. Bound by launches and their chains of loads: 1.6 million masked positions 13.5 us (policy) and 11.4 (preference) in a
 // graph, of which the bytes are 4 and 3; a few hundred positions 8, mostly the host's.
 #pragma once
 #include <math_constants.h>
@@ -63,7 +63,8 @@ __device__ __forceinline__ Span span_of(const ObjectiveArgs& a, int s) {
   x.end = max(x.begin, min(max(hi, 0), a.T));
   return x;
 }
-// Item `item`: slice `item % parts` of sequence `item / parts`, cut at multiples of four positions.
+// Item `item`: slice `item % parts` of sequence `item / parts`, cut at multiples of four positions (equal steps: a 64-bit division for either end was a third of a warp's
+// instructions).
 struct Slice {
   int s, begin, end;
 };
@@ -72,13 +73,10 @@ __device__ __forceinline__ Slice slice_of(const ObjectiveArgs& a, int item) {
   c.s = item / a.parts;
   const int part = item - c.s * a.parts;
   const Span x = span_of(a, c.s);
-  auto cut = [&](int q) {
-    if (q == 0) return x.begin;
-    if (q == a.parts) return x.end;
-    return max(x.begin, (x.begin + static_cast<int>(static_cast<long long>(x.end - x.begin) * q / a.parts)) & ~3);
-  };
-  c.begin = cut(part);
-  c.end = cut(part + 1);
+  const int base = x.begin & ~3, step = ((x.end - base + a.parts - 1) / a.parts + 3) & ~3;       // (parts * step: below 2^30 + 8 * 4736)
+  c.begin = min(x.end, max(x.begin, base + part * step));
+  c.end = min(x.end, base + (part + 1) * step);
+  c.end = max(c.begin, c.end);
   return c;
 }
 
@@ -184,21 +182,32 @@ __device__ __forceinline__ void count_phase(const ObjectiveArgs& a, int block, i
   if (threadIdx.x == 0) a.block_count[block] = all[0];
 }
 
-// e^q - 1 - q, and e^q - 1: near zero by the series, whose next term is below 2^-28 of the first; the function less q is off by q's rounding.
-__device__ __forceinline__ void exp_beyond(float q, float& beyond, float& m1) {
-  if (fabsf(q) < 0.5f) {
+// e^q - 1 - q, and e^q - 1, of four: near zero by the series, whose next term is below 2^-28 of the first; the function less q is off by q's rounding.
+__device__ __forceinline__ void exp_beyond(const float (&q)[4], float (&beyond)[4], float (&m1)[4]) {
+  bool far = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
     float s = 1.f / 40320.f;
-    s = fmaf(s, q, 1.f / 5040.f);
-    s = fmaf(s, q, 1.f / 720.f);
-    s = fmaf(s, q, 1.f / 120.f);
-    s = fmaf(s, q, 1.f / 24.f);
-    s = fmaf(s, q, 1.f / 6.f);
-    s = fmaf(s, q, 0.5f);
-    beyond = q * q * s;
-    m1 = q + beyond;
-  } else {
-    m1 = expm1f(q);
-    beyond = m1 - q;
+    s = fmaf(s, q[i], 1.f / 5040.f);
+    s = fmaf(s, q[i], 1.f / 720.f);
+    s = fmaf(s, q[i], 1.f / 120.f);
+    s = fmaf(s, q[i], 1.f / 24.f);
+    s = fmaf(s, q[i], 1.f / 6.f);
+    s = fmaf(s, q[i], 0.5f);
+    beyond[i] = q[i] * q[i] * s;
+    m1[i] = q[i] + beyond[i];
+    far |= fabsf(q[i]) >= 0.5f;
+  }
+  if (far) {
+#pragma unroll 1
+    for (int i = 0; i < 4; ++i) {
+      const float x = i < 2 ? (i == 0 ? q[0] : q[1]) : (i == 2 ? q[2] : q[3]);
+      if (fabsf(x) < 0.5f) continue;
+      const float y = expm1f(x);
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (k == i) m1[k] = y, beyond[k] = y - x;
+    }
   }
 }
 // What an advantage's sign says about clipping: the end that counts (its logarithm in two terms) and the value beyond it.
@@ -232,12 +241,13 @@ __device__ __forceinline__ void policy_phase(const ObjectiveArgs& a, int block, 
   double all[3] = {0.0, 0.0, 0.0};
   for (int base = block * kObjectiveWarps; base < items; base += blocks * kObjectiveWarps) {
     const int item = base + (threadIdx.x >> 5);
+    const Slice c = slice_of(a, min(item, items - 1));
     int own = 0;
     const bool together = a.own_count && a.parts >= kObjectiveWarps / 2;       // the block's warps share two or three sequences: counted by all of them
     if (together) {
       __shared__ int counted[4];
       if (threadIdx.x < 4) counted[threadIdx.x] = 0;
-      if (item < items) prefetch_slice(a, slice_of(a, item), lane);
+      if (item < items) prefetch_slice(a, c, lane);
       __syncthreads();
       const int s0 = base / a.parts, s1 = (min(base + kObjectiveWarps, items) - 1) / a.parts;
       for (int s = s0; s <= s1; ++s) {
@@ -246,11 +256,10 @@ __device__ __forceinline__ void policy_phase(const ObjectiveArgs& a, int block, 
         if (lane == 0 && n) atomicAdd(&counted[s - s0], n);
       }
       __syncthreads();
-      if (item < items) own = counted[item / a.parts - s0];
+      if (item < items) own = counted[c.s - s0];
       __syncthreads();
     }
     if (item >= items) continue;
-    const Slice c = slice_of(a, item);
     long long n = total;
     if (a.by_sequence) {
       const Span x = span_of(a, c.s);
@@ -278,24 +287,36 @@ __device__ __forceinline__ void policy_phase(const ObjectiveArgs& a, int block, 
       load4<WIDE>(a.old, t, inside, valid, old);
       if (a.ref != nullptr) load4<WIDE>(a.ref, t, inside, valid, ref);
       if (EACH) load4<WIDE>(a.advantage, t, inside, valid, adv);
+      float diff[4], over[4], beyond[4] = {0.f, 0.f, 0.f, 0.f}, m1[4] = {0.f, 0.f, 0.f, 0.f};
+      bool near = false;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const ClipOf side = EACH ? clip_of(a, adv[i]) : one;
-        const float diff = lp[i] - old[i];
-        float over = diff - side.end;
-        if (fabsf(over) < fmaf(fabsf(diff), 1e-6f, 1e-6f)) over = beyond_end(lp[i], old[i], side);       // (both roundings are below 2^-23 of diff and end)
-        const bool out = side.sign * over > 0.f, counts = valid >> i & 1;
-        float gain = expf(diff) * side.adv;
+        diff[i] = lp[i] - old[i];
+        over[i] = diff[i] - side.end;
+        near |= fabsf(over[i]) < fmaf(fabsf(diff[i]), 1e-6f, 1e-6f);                  // (both roundings are below 2^-23 of diff and end)
+      }
+      if (near) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (fabsf(over[i]) < fmaf(fabsf(diff[i]), 1e-6f, 1e-6f)) over[i] = beyond_end(lp[i], old[i], EACH ? clip_of(a, adv[i]) : one);
+      }
+      if (a.ref != nullptr) {
+        const float q[4] = {ref[0] - lp[0], ref[1] - lp[1], ref[2] - lp[2], ref[3] - lp[3]};
+        exp_beyond(q, beyond, m1);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const ClipOf side = EACH ? clip_of(a, adv[i]) : one;
+        const bool out = side.sign * over[i] > 0.f, counts = valid >> i & 1;
+        float gain = expf(diff[i]) * side.adv;
         if (out) gain = side.held;
         if (side.adv == 0.f) gain = 0.f;
-        float slope = out ? 0.f : -gain, beyond = 0.f, m1 = 0.f;
-        if (a.ref != nullptr) {
-          exp_beyond(ref[i] - lp[i], beyond, m1);
-          slope = fmaf(-beta, m1, slope);
-        }
+        float slope = out ? 0.f : -gain;
+        if (a.ref != nullptr) slope = fmaf(-beta, m1[i], slope);
         g[i] = counts ? w * slope : 0.f;
         value4 -= counts ? gain : 0.f;
-        kl4 += counts ? beyond : 0.f;
+        kl4 += counts ? beyond[i] : 0.f;
         clipped += counts && out ? 1 : 0;
       }
       value += static_cast<double>(value4);
