@@ -180,6 +180,8 @@ int allow_shared_memory() {
   __atomic_store_n(&g_allowed[dev], 1, __ATOMIC_RELEASE);
   return MTPC_OK;
 }
+// Stages fill an SM's shared memory, or half of it for kernels that take 256 columns of tensor memory at most: whatever CTAs meet on an SM, of calls on several streams too, have
+// 512 columns together, so that none in a cluster waits for columns that another one holds.
 int stages_of(int stage_bytes, int ctas_per_sm = 1, int beside = 0) {
   return std::min(kMaxStages, static_cast<int>((kSmemLimit / ctas_per_sm - (ctas_per_sm > 1 ? 1024 : 0) - kControl - beside) / stage_bytes));
 }
