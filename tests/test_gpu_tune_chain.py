@@ -199,3 +199,28 @@ assert [bool(t.any()) for t in first] == [True, False, True, False, False] + [Tr
 """
     done = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
     assert done.returncode == 0, done.stderr[-2000:]
+
+
+def test_calls_on_three_streams_at_once():
+    """Few rows, tiles and gradients beside each other, again and again: every call gives what it gives alone."""
+    g = torch.Generator(device="cuda").manual_seed(8)
+    new = lambda *s: torch.randn(s, device="cuda", generator=g).bfloat16()  # noqa: E731
+    d, m, S = 1024, 768, 4
+    jobs = []
+    for T, k in ((1, 16), (40, 64), (700, 16), (1500, 64)):
+        x, W, A, Bf, d_out = new(T, d), new(m, d), new(S, m, k), new(S, k, d), new(T, m)
+        which = (torch.arange(T, device="cuda") % (S + 1) - 1).int()
+        low = torch.randn(T, k, device="cuda", generator=g)
+
+        def job(x=x, W=W, A=A, Bf=Bf, d_out=d_out, which=which, low=low):
+            out, kept = R.adapted_projection(x, W, A, Bf, None, which)
+            return [out, kept, *(t for t in R.adapted_projection_backward(x, W, A, Bf, low, d_out, None, which).values() if t is not None)]
+        jobs.append((job, job()))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    got = []
+    for i in range(48):
+        with torch.cuda.stream(streams[i % 3]):
+            got.append((i % 4, jobs[i % 4][0]()))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for which, results in got for a, b in zip(results, jobs[which][1]))
