@@ -622,7 +622,8 @@ int mtpc_dropout(const void* x, int64_t x_stride, int32_t x_dtype, const void* r
  *   clip_low, clip_high, beta >= 0 and finite.
  *
  * mtpc_preference_loss: sequences 2p (preferred) and 2p + 1 are a pair, S even. h = beta (sum of logp - ref_logp over the one's valid positions - over
- * the other's); the loss is the mean over the pairs of -(1 - smoothing) log sigmoid(h) - smoothing log sigmoid(-h).
+ * the other's); the loss is the mean over the pairs of -(1 - smoothing) log sigmoid(h) - smoothing log sigmoid(-h). A term whose factor (beta, smoothing, 1 - smoothing) is
+ * zero counts nothing, also where a log-likelihood is -infinity: with smoothing 0 a rejected sequence that has such a window costs its pair nothing.
  *   out_loss dev [1]; out_h dev [S / 2] or NULL.  beta >= 0 and finite, 0 <= smoothing <= 1.
  */
 int mtpc_objective_workspace_bytes(int32_t T, int32_t S, size_t* out_bytes);

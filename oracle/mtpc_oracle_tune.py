@@ -77,10 +77,11 @@ def preference_loss(logp, ref, offsets, beta, smoothing=0.0, mask=None):
         ratio.append(math.fsum([float(logp[t]) for t in at] + [-float(ref[t]) for t in at]))
     grad, hs, loss = np.full(len(logp), np.nan), [], 0.0
     log_sigmoid = lambda x: -math.log1p(math.exp(-x)) if x > -30 else x - math.log1p(math.exp(x))  # noqa: E731
+    of = lambda share, x: share * x if share else 0.0  # noqa: E731  (a factor of zero takes its term away, also one without a bound)
     for p in range(S // 2):
-        h = beta * (ratio[2 * p] - ratio[2 * p + 1])
+        h = of(beta, ratio[2 * p] - ratio[2 * p + 1])
         hs.append(h)
-        loss -= ((1 - smoothing) * log_sigmoid(h) + smoothing * log_sigmoid(-h)) / (S // 2)
+        loss -= (of(1 - smoothing, log_sigmoid(h)) + of(smoothing, log_sigmoid(-h))) / (S // 2)
         slope = beta * (smoothing - math.exp(log_sigmoid(-h))) / (S // 2)
         for s, sign in ((2 * p, 1), (2 * p + 1, -1)):
             for t in range(offsets[s], offsets[s + 1]):

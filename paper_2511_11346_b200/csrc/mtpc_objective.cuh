@@ -410,6 +410,8 @@ __device__ __forceinline__ void ratio_phase(const ObjectiveArgs& a, int first, i
     if (lane == 0) a.sum[item] = sum;
   }
 }
+// A factor of zero takes its term away, also where that has no bound (a window without probability).
+__device__ __forceinline__ double of_share(double share, double x) { return share > 0.0 ? share * x : 0.0; }
 // h of pair p, by a warp: the difference of its sequences' sums.
 __device__ __forceinline__ double pair_h(const ObjectiveArgs& a, int p, int lane) {
   double h = 0.0;
@@ -417,11 +419,11 @@ __device__ __forceinline__ double pair_h(const ObjectiveArgs& a, int p, int lane
     const double x = a.sum[static_cast<size_t>(2 * p) * a.parts + q];
     h += q < a.parts ? x : -x;
   }
-  return a.beta * warp_total(h);
+  return of_share(a.beta, warp_total(h));
 }
 // The pair's loss and the slope of its first sequence. e = exp(-|h|): log sigmoid(h) = min(h, 0) - log(1 + e).
 __device__ __forceinline__ double pair_loss(const ObjectiveArgs& a, double h) {
-  return log1p(exp(-fabs(h))) + (1.0 - a.smoothing) * fmax(-h, 0.0) + a.smoothing * fmax(h, 0.0);
+  return log1p(exp(-fabs(h))) + of_share(1.0 - a.smoothing, fmax(-h, 0.0)) + of_share(a.smoothing, fmax(h, 0.0));
 }
 __device__ __forceinline__ float pair_slope(const ObjectiveArgs& a, double h) {
   const double e = exp(-fabs(h)), low = e / (1.0 + e), of_other = h > 0.0 ? low : 1.0 - low;      // sigmoid(-h)
@@ -452,7 +454,7 @@ __device__ __forceinline__ void all_pairs(const ObjectiveArgs& a) {
     for (int o = 16; o > 0; o >>= 1)
 #pragma unroll
       for (int i = 0; i < 4; ++i) h[i] += __shfl_xor_sync(0xffffffffu, h[i], o);
-    if (lane < 4 && base + lane < pairs) a.term[base + lane] = a.beta * (lane == 0 ? h[0] : lane == 1 ? h[1] : lane == 2 ? h[2] : h[3]);
+    if (lane < 4 && base + lane < pairs) a.term[base + lane] = of_share(a.beta, lane == 0 ? h[0] : lane == 1 ? h[1] : lane == 2 ? h[2] : h[3]);
   }
   __syncthreads();
   for (int p = threadIdx.x; p < pairs; p += kObjectiveThreads) {
