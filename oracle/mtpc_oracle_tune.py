@@ -60,7 +60,7 @@ def policy_loss(logp, old, ref, advantage, offsets, clip_low, clip_high, beta, m
             first = -min(r * a, held * a)
             clipped = held * a < r * a
             q = float(ref[t]) - float(logp[t]) if beta else 0.0
-            kl = math.expm1(q) - q
+            kl = math.expm1(q) - q if q < math.inf else q
             stats += w * np.array([first, kl, float(clipped)])
             size += w * (abs(first) + beta * kl)
             grad[t] = w * ((0.0 if clipped else -r * a) - beta * math.expm1(q))

@@ -206,7 +206,7 @@ __device__ __forceinline__ void exp_beyond(const float (&q)[4], float (&beyond)[
       const float y = expm1f(x);
 #pragma unroll
       for (int k = 0; k < 4; ++k)
-        if (k == i) m1[k] = y, beyond[k] = y - x;
+        if (k == i) m1[k] = y, beyond[k] = y < CUDART_INF_F ? y - x : y;       // (of infinity: itself)
     }
   }
 }

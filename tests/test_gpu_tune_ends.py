@@ -55,3 +55,30 @@ def test_preference_of_windows_without_probability(lengths):
     # both have one: nothing can be said of the pair
     loss, h, d = preference(lengths, [1, lengths[0] + 1])
     assert math.isnan(loss) and math.isnan(h[0].item()) and not h[1:].any()
+
+
+def policy(logp, old, ref, advantage, offsets, beta, low=0.2, high=0.2, by_position=False):
+    d, loss, stats = torch.full_like(logp, 9.0), torch.empty(1, device="cuda"), torch.empty(3, device="cuda")
+    B.mtpc_policy_loss(logp, old, ref, advantage, offsets, low, high, beta, loss, d, out_stats=stats, by_position=by_position)
+    return d, loss.item(), stats
+
+
+@pytest.mark.parametrize("T", [16, 70000])
+def test_kl_term_of_windows_without_probability(T):
+    """q = ref - logp without a bound: e^q - 1 - q is infinite whichever way, and its slope beta (1 - e^q) what it tends to."""
+    one, offsets, a = torch.full((T,), -1.0, device="cuda"), packed([T // 2, T - T // 2]), torch.ones(2, device="cuda")
+    holes = [1, T // 2 + 2, T - 1]
+    bad = one.clone()
+    bad[holes] = -INF
+    keep = torch.ones(T, dtype=torch.bool, device="cuda")
+    keep[holes] = False
+    d, loss, stats = policy(bad, one, one, a, offsets, 0.5)                       # the policy gives a window no probability, the reference does: q = inf
+    assert loss == INF and stats[1].item() == INF and (d[holes] == -INF).all() and math.isfinite(stats[0].item())
+    assert torch.equal(d[keep], torch.full_like(d[keep], -1.0 / T))
+    d, loss, stats = policy(one, one, bad, a, offsets, 0.5)                       # the other way about: q = -inf, e^q = 0
+    assert loss == INF and stats[1].item() == INF and (d[holes] == (0.5 - 1.0) / T).all() and torch.equal(d[keep], torch.full_like(d[keep], -1.0 / T))
+    # so large that only e^q overflows fp32
+    far = one.clone()
+    far[holes] = -1001.0
+    d, loss, stats = policy(far, one, one, a, offsets, 0.5)
+    assert loss == INF and (d[holes] == -INF).all() and not torch.isnan(stats).any()

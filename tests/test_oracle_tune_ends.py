@@ -16,3 +16,12 @@ def test_preference_of_windows_without_probability():
         assert not grad[:4].any() or want == math.inf
     loss, h, grad = tu.preference_loss(x, ref, [0, 2, 4, 6, 8], 0.0)
     assert loss == math.log(2) and not h.any() and not grad.any()
+
+
+def test_kl_term_of_windows_without_probability():
+    one, bad = np.full(4, -1.0), np.array([-1.0, -math.inf, -1.0, -1.0])
+    with np.errstate(all="raise"):
+        loss, stats, grad, _ = tu.policy_loss(bad, one, one, [1.0, 1.0], [0, 2, 4], 0.2, 0.2, 0.5)
+        assert loss == stats[1] == math.inf and stats[0] == -0.75 and grad[1] == -math.inf and (np.delete(grad, 1) == -0.25).all()
+        loss, stats, grad, _ = tu.policy_loss(one, one, bad, [1.0, 1.0], [0, 2, 4], 0.2, 0.2, 0.5)
+        assert loss == stats[1] == math.inf and stats[0] == -1 and grad[1] == -0.125
