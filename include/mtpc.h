@@ -580,7 +580,7 @@ int mtpc_adapted_projection(const void* x, int64_t x_stride, const void* x_low, 
  *   d_out  dev [T, m] bf16 (the norm's gradient in front of the head writes that type);  d_x dev [T, d] bf16.
  *   d_x_low dev [T, d] bf16 or NULL: takes B[i]^T v[t] apart from d_x (for the gradient of the dropout in front of the adaptors, whose call adds it to d_x).
  *   dA dev [S, m, k] fp32, dB dev [S, k, d] fp32, adjacent, overwritten. No output may overlap an input or another output.
- *   Rows with an adaptor >= S: as above, in d_x (d_x_low, where that is given). Other arguments and limits as above; aligned_rows speaks of d_out and m too.
+ *   Rows with an adaptor >= S: as above, in d_x (d_x_low, where that is given); reported by every call that has an output. Other arguments and limits as above; aligned_rows speaks of d_out and m too.
  */
 int mtpc_adapted_projection_backward_workspace_bytes(int32_t T, int32_t d, int32_t m, int32_t k, int32_t S, int32_t aligned_rows, size_t* out_bytes);
 int mtpc_adapted_projection_backward(const void* x_low, int64_t x_low_stride, const void* W, int64_t W_stride, const void* A, const void* B,

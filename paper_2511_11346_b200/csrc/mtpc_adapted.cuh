@@ -209,6 +209,8 @@ __device__ __forceinline__ void given_terms(const LowParams& p, int t0, int t1, 
   for (int at = thread; at < all; at += 128) {
     const int t = t0 + at / quads, j0 = at % quads * 4;
     const bool any = adaptor_of(p.which, p.S, t, p.T) >= 0;
+    // without sums nothing else looks at every row
+    if (p.chunks == 0 && j0 == 0 && p.status != nullptr && adaptor_refused(p.which, p.S, t)) atomicOr(p.status, kStatusBadAdaptor);
     float x[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) x[q] = any && j0 + q < p.k ? p.given[static_cast<size_t>(t) * p.k + j0 + q] : 0.f;
