@@ -609,7 +609,7 @@ int mtpc_dropout(const void* x, int64_t x_stride, int32_t x_dtype, const void* r
  *   logp, old_logp, ref_logp dev [T] fp32;  d_logp dev [T] fp32, overwritten at the positions of sequences (0 where the mask is 0) and left as it
  *           was outside of them; not overlapping an input.
  *   offsets dev int32 [S + 1], not decreasing, within [0, T]; otherwise MTPC_STATUS_BAD_OFFSET is or-ed into out_status (dev uint32 or NULL), the loss is NaN,
- *           what d_logp holds within [0, T) is not defined, and the call may take as long as its sequences are together. A sequence may be empty.
+ *           what d_logp holds within [0, T) is not defined, and the call may take as long as one with min(S, 4736) T positions. A sequence may be empty.
  *   mask    dev [T] bytes or NULL: positions with 0 count nowhere, whatever their values are (infinities and NaN too).
  *   workspace dev, 256-byte aligned, >= mtpc_objective_workspace_bytes(T, S); small calls need none (0 bytes: it may be NULL).
  * 0 <= T <= 2^30, 1 <= S <= 2^20 (MTPC_ERR_UNSUPPORTED beyond). Differences of log-likelihoods are formed without loss, sums are fp64.

@@ -63,16 +63,31 @@ __device__ __forceinline__ Span span_of(const ObjectiveArgs& a, int s) {
   x.end = max(x.begin, min(max(hi, 0), a.T));
   return x;
 }
+// The sequences that a warp takes, in order: none begins before the end of the one ahead, whatever the offsets say. (Refused ones may name all positions for every
+// sequence, S T of them together; so a warp has T at most.)
+struct Taken {
+  int s, from, end;                                // the last sequence, where it may begin, where it ends
+  __device__ __forceinline__ Taken() : s(-1), from(0), end(0) {}
+  __device__ __forceinline__ Span span(const ObjectiveArgs& a, int next) {
+    Span x = span_of(a, next);
+    if (next != s) from = max(from, end), s = next;
+    x.begin = max(x.begin, from);
+    x.end = max(x.end, x.begin);
+    end = x.end;
+    return x;
+  }
+};
 // Item `item`: slice `item % parts` of sequence `item / parts`, cut at multiples of four positions (equal steps: a 64-bit division for either end was a third of a warp's
 // instructions).
 struct Slice {
   int s, begin, end;
+  Span of;                                         // its sequence
 };
-__device__ __forceinline__ Slice slice_of(const ObjectiveArgs& a, int item) {
+__device__ __forceinline__ Slice slice_of(const ObjectiveArgs& a, int item, Taken& taken) {
   Slice c;
   c.s = item / a.parts;
   const int part = item - c.s * a.parts;
-  const Span x = span_of(a, c.s);
+  const Span x = c.of = taken.span(a, c.s);
   const int base = x.begin & ~3, step = ((x.end - base + a.parts - 1) / a.parts + 3) & ~3;       // (parts * step: below 2^30 + 8 * 4736)
   c.begin = min(x.end, max(x.begin, base + part * step));
   c.end = min(x.end, base + (part + 1) * step);
@@ -170,8 +185,9 @@ template <bool WIDE>
 __device__ __forceinline__ void count_phase(const ObjectiveArgs& a, int block, int blocks, int lane, long long* red) {
   const int first = block * kObjectiveWarps + (threadIdx.x >> 5), step = blocks * kObjectiveWarps;
   long long all[1] = {0};
+  Taken taken;
   for (int item = first; item < a.S * a.parts; item += step) {
-    const Slice c = slice_of(a, item);
+    const Slice c = slice_of(a, item, taken);
     int n = 0;
     over_slice<WIDE>(a, c, lane, [&](int, uint32_t valid, bool) { n += __popc(valid); });
     n = warp_total(n);
@@ -239,9 +255,10 @@ template <bool WIDE, bool EACH>
 __device__ __forceinline__ void policy_phase(const ObjectiveArgs& a, int block, int blocks, int lane, long long total, double* red) {
   const int items = a.S * a.parts;
   double all[3] = {0.0, 0.0, 0.0};
+  Taken taken;
   for (int base = block * kObjectiveWarps; base < items; base += blocks * kObjectiveWarps) {
     const int item = base + (threadIdx.x >> 5);
-    const Slice c = slice_of(a, min(item, items - 1));
+    const Slice c = slice_of(a, min(item, items - 1), taken);
     int own = 0;
     const bool together = a.own_count && a.parts >= kObjectiveWarps / 2;       // the block's warps share two or three sequences: counted by all of them
     if (together) {
@@ -262,13 +279,12 @@ __device__ __forceinline__ void policy_phase(const ObjectiveArgs& a, int block, 
     if (item >= items) continue;
     long long n = total;
     if (a.by_sequence) {
-      const Span x = span_of(a, c.s);
-      int here = x.end - x.begin;
+      int here = c.of.end - c.of.begin;
       if (together) {
         here = own;
       } else if (a.own_count) {
         prefetch_slice(a, c, lane);
-        here = warp_total(count_mask(a.mask, x.begin, x.end, lane, 32));
+        here = warp_total(count_mask(a.mask, c.of.begin, c.of.end, lane, 32));
       } else if (a.mask != nullptr) {
         here = 0;
         for (int q = lane; q < a.parts; q += 32) here += a.count[c.s * a.parts + q];
@@ -395,8 +411,9 @@ __device__ __forceinline__ void policy_final(const ObjectiveArgs& a, int blocks,
 
 template <bool WIDE>
 __device__ __forceinline__ void ratio_phase(const ObjectiveArgs& a, int first, int step, int lane) {
+  Taken taken;
   for (int item = first; item < a.S * a.parts; item += step) {
-    const Slice c = slice_of(a, item);
+    const Slice c = slice_of(a, item, taken);
     double sum = 0.0;
     over_slice<WIDE>(a, c, lane, [&](int t, uint32_t valid, bool inside) {
       float lp[4], ref[4];
@@ -473,8 +490,9 @@ __device__ __forceinline__ void preference_final(const ObjectiveArgs& a, double*
 // own: every warp forms its pair's slope itself.
 template <bool WIDE>
 __device__ __forceinline__ void spread_phase(const ObjectiveArgs& a, int first, int step, int lane, bool own) {
+  Taken taken;
   for (int item = first; item < a.S * a.parts; item += step) {
-    const Slice c = slice_of(a, item);
+    const Slice c = slice_of(a, item, taken);
     float slope = own ? pair_slope(a, pair_h(a, c.s >> 1, lane)) : a.slope[c.s >> 1];
     if (c.s & 1) slope = -slope;
     over_slice<WIDE>(a, c, lane, [&](int t, uint32_t valid, bool inside) {
