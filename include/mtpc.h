@@ -612,7 +612,8 @@ int mtpc_dropout(const void* x, int64_t x_stride, int32_t x_dtype, const void* r
  *           what d_logp holds within [0, T) is not defined, and the call may take as long as one with min(S, 4736) T positions. A sequence may be empty.
  *   mask    dev [T] bytes or NULL: positions with 0 count nowhere, whatever their values are (infinities and NaN too).
  *   workspace dev, 256-byte aligned, >= mtpc_objective_workspace_bytes(T, S); small calls need none (0 bytes: it may be NULL).
- * 0 <= T <= 2^30, 1 <= S <= 2^20 (MTPC_ERR_UNSUPPORTED beyond). Differences of log-likelihoods are formed without loss, sums are fp64.
+ * 0 <= T <= 2^30, 1 <= S <= 2^20 (MTPC_ERR_UNSUPPORTED beyond). Differences of log-likelihoods are formed without loss, sums are fp64; the policy loss's
+ * exponentials and products of a position are fp32 (a ratio, or e^q, that fp32 does not hold is infinite).
  *
  * mtpc_policy_loss: the average over the valid positions (by_sequence != 0: over every sequence's valid positions and then over the S sequences, those
  * without any among them with 0) of -min(r a, clip(r, 1 - clip_low, 1 + clip_high) a) + beta (exp(q) - q - 1), r = exp(logp - old_logp),

@@ -7,15 +7,15 @@
 // Preference: sequences 2p and 2p + 1, h = beta (sum of logp - ref over the one's valid positions - over the other's),
 //   loss = mean of -(1 - s) log sigmoid(h) - s log sigmoid(-h),   slope = +- beta (s - sigmoid(-h)) / pairs.
 //
-// Whether a ratio is clipped is decided on logp - old without loss, against the logarithms of the ends: where the rounded difference is beside an end, both are taken as
-// two fp32 terms, since a position there would else change sides by a rounding. The differences that a pair's sum adds up are fp64. Sums are fp64, the policy loss's of
-// four positions' fp32 ones, in an order that sizes fix.
+// Differences of log-likelihoods lose nothing: the policy loss takes them as two fp32 terms, the nearest value and what it leaves, and e^(d + rest) as e^d (1 + rest); the sums of pairs
+// take them in fp64. Whether a ratio is clipped is decided on both terms, against the logarithms of the ends in two terms as well, since a position beside an end would else
+// change sides by a rounding. What a position comes to (ratios, products, slopes) is fp32; sums are fp64, in an order that sizes fix.
 //
 // Work is dealt in items: a warp has one of P equal slices of one sequence, so that long sequences among short ones spread over the device and no
 // position has to look for its sequence. Weights need the counts of valid positions first, so the call goes over the data twice (the mask alone
 // for the counts, every warp over that of its own sequence where that is all it needs; logp and ref for the sums of pairs). Few positions: all phases in one launch of one cluster, with its barrier between
-// them (a chain of four kernels of 2 us each otherwise); many: a launch for each phase. Bound by launches and their chains of loads: 1.6 million masked positions 13.5 us (policy) and 11.4 (preference) in a
-// graph, of which the bytes are 4 and 3; a few hundred positions 8, mostly the host's.
+// them (a chain of four kernels of 2 us each otherwise); many: a launch for each phase. Bound by launches and their chains of loads: 1.6 million masked positions 16.0 us (policy; with differences and
+// sums of four in fp32 alone 14.5) and 12.0 (preference), of which the bytes are 4 and 3; a few hundred positions 8, mostly the host's.
 #pragma once
 #include <math_constants.h>
 #include <stdint.h>
@@ -198,6 +198,13 @@ __device__ __forceinline__ void count_phase(const ObjectiveArgs& a, int block, i
   if (threadIdx.x == 0) a.block_count[block] = all[0];
 }
 
+// x - y in two terms: the nearest fp32 value, and what it leaves (exactly).
+__device__ __forceinline__ float difference_rest(float x, float y, float d) {
+  const float back = __fadd_rn(d, y);
+  return __fsub_rn(__fsub_rn(x, back), __fsub_rn(y, __fsub_rn(back, d)));
+}
+// Whether an exponential of the difference takes the rest into account: up to where fp32 ends, so that no infinity is multiplied by it.
+__device__ __forceinline__ bool rest_counts(float d) { return fabsf(d) < 88.f; }
 // e^q - 1 - q, and e^q - 1, of four: near zero by the series, whose next term is below 2^-28 of the first; the function less q is off by q's rounding.
 __device__ __forceinline__ void exp_beyond(const float (&q)[4], float (&beyond)[4], float (&m1)[4]) {
   bool far = false;
@@ -234,12 +241,8 @@ __device__ __forceinline__ ClipOf clip_of(const ObjectiveArgs& a, float adv) {
   const bool up = adv > 0.f;
   return ClipOf{adv, up ? 1.f : adv < 0.f ? -1.f : 0.f, up ? a.log_high[0] : a.log_low[0], up ? a.log_high[1] : a.log_low[1], (up ? a.high : a.low) * adv};
 }
-// (logp - old) - the end's logarithm, where roundings would decide: the difference as the nearest fp32 value and what it leaves (exactly), less the two terms.
-__device__ __forceinline__ float beyond_end(float logp, float old, const ClipOf& side) {
-  const float d = __fsub_rn(logp, old), back = __fadd_rn(d, old);
-  const float rest = __fsub_rn(__fsub_rn(logp, back), __fsub_rn(old, __fsub_rn(back, d)));
-  return __fadd_rn(__fsub_rn(d, side.end), __fsub_rn(rest, side.end_rest));
-}
+// (logp - old) - the end's logarithm, where roundings would decide: both in two terms.
+__device__ __forceinline__ float beyond_end(float d, float rest, const ClipOf& side) { return __fadd_rn(__fsub_rn(d, side.end), __fsub_rn(rest, side.end_rest)); }
 
 // A slice's values on their way into L2 while its weight is formed, a line of 32 to a lane.
 __device__ __forceinline__ void prefetch_slice(const ObjectiveArgs& a, const Slice& c, int lane) {
@@ -298,45 +301,52 @@ __device__ __forceinline__ void policy_phase(const ObjectiveArgs& a, int block, 
     double value = 0.0, kl = 0.0;
     int clipped = 0;
     over_slice<WIDE>(a, c, lane, [&](int t, uint32_t valid, bool inside) {
-      float lp[4], old[4], ref[4], adv[4], g[4], value4 = 0.f, kl4 = 0.f;
+      float lp[4], old[4], ref[4], adv[4], g[4];
       load4<WIDE>(a.logp, t, inside, valid, lp);
       load4<WIDE>(a.old, t, inside, valid, old);
       if (a.ref != nullptr) load4<WIDE>(a.ref, t, inside, valid, ref);
       if (EACH) load4<WIDE>(a.advantage, t, inside, valid, adv);
-      float diff[4], over[4], beyond[4] = {0.f, 0.f, 0.f, 0.f}, m1[4] = {0.f, 0.f, 0.f, 0.f};
+      float diff[4], rest[4], over[4], beyond[4] = {0.f, 0.f, 0.f, 0.f}, m1[4] = {0.f, 0.f, 0.f, 0.f};
       bool near = false;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const ClipOf side = EACH ? clip_of(a, adv[i]) : one;
-        diff[i] = lp[i] - old[i];
+        diff[i] = __fsub_rn(lp[i], old[i]);
+        rest[i] = difference_rest(lp[i], old[i], diff[i]);
         over[i] = diff[i] - side.end;
         near |= fabsf(over[i]) < fmaf(fabsf(diff[i]), 1e-6f, 1e-6f);                  // (both roundings are below 2^-23 of diff and end)
       }
       if (near) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (fabsf(over[i]) < fmaf(fabsf(diff[i]), 1e-6f, 1e-6f)) over[i] = beyond_end(lp[i], old[i], EACH ? clip_of(a, adv[i]) : one);
+          if (fabsf(over[i]) < fmaf(fabsf(diff[i]), 1e-6f, 1e-6f)) over[i] = beyond_end(diff[i], rest[i], EACH ? clip_of(a, adv[i]) : one);
       }
       if (a.ref != nullptr) {
-        const float q[4] = {ref[0] - lp[0], ref[1] - lp[1], ref[2] - lp[2], ref[3] - lp[3]};
+        const float q[4] = {__fsub_rn(ref[0], lp[0]), __fsub_rn(ref[1], lp[1]), __fsub_rn(ref[2], lp[2]), __fsub_rn(ref[3], lp[3])};
         exp_beyond(q, beyond, m1);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float more = difference_rest(ref[i], lp[i], q[i]);
+          if (!rest_counts(q[i])) continue;
+          beyond[i] = fmaf(more, m1[i], beyond[i]);
+          m1[i] = fmaf(more, 1.f + m1[i], m1[i]);
+        }
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const ClipOf side = EACH ? clip_of(a, adv[i]) : one;
         const bool out = side.sign * over[i] > 0.f, counts = valid >> i & 1;
-        float gain = expf(diff[i]) * side.adv;
+        const float ratio = expf(diff[i]);
+        float gain = (rest_counts(diff[i]) ? fmaf(ratio, rest[i], ratio) : ratio) * side.adv;
         if (out) gain = side.held;
         if (side.adv == 0.f) gain = 0.f;
         float slope = out ? 0.f : -gain;
         if (a.ref != nullptr) slope = fmaf(-beta, m1[i], slope);
         g[i] = counts ? w * slope : 0.f;
-        value4 -= counts ? gain : 0.f;
-        kl4 += counts ? beyond[i] : 0.f;
+        value -= static_cast<double>(counts ? gain : 0.f);
+        kl += static_cast<double>(counts ? beyond[i] : 0.f);
         clipped += counts && out ? 1 : 0;
       }
-      value += static_cast<double>(value4);
-      kl += static_cast<double>(kl4);
       store4<WIDE>(a.d_logp, c, t, inside, g);
     });
     value = warp_total(value);

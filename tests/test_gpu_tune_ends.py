@@ -82,3 +82,30 @@ def test_kl_term_of_windows_without_probability(T):
     far[holes] = -1001.0
     d, loss, stats = policy(far, one, one, a, offsets, 0.5)
     assert loss == INF and (d[holes] == -INF).all() and not torch.isnan(stats).any()
+
+
+@pytest.mark.parametrize("T", [64, 70000])
+def test_differences_of_log_likelihoods_lose_nothing(T):
+    """Log-likelihoods whose difference does not fit fp32: rounded, it would move a ratio by up to |diff| u = 80 u (u = 2^-24). Without: expf and expm1f are within
+    2 units in the last place (4 u), the rest of the difference, the product with the advantage, the weight and its product u each: 8 u; e^q - 1 - q one more."""
+    u = 2.0 ** -24
+    g = torch.Generator(device="cuda").manual_seed(T)
+    near, far = -torch.rand(T, device="cuda", generator=g), -50 - 30 * torch.rand(T, device="cuda", generator=g)
+    offsets = packed([T // 2, T - T // 2])
+    d, loss, stats = policy(near, far, None, torch.full((2,), -1.0, device="cuda"), offsets, 0.0)       # a ratio above the upper end counts where the advantage is negative
+    want = torch.exp(near.double() - far.double()) / T
+    assert ((d.double() - want).abs() <= 8 * u * want).all() and (want > d.double()).any() and (want < d.double()).any()
+    assert abs(loss - float(want.sum())) <= 8 * u * float(want.sum()) and stats[2].item() == 0
+    d, loss, stats = policy(far, far, near, torch.zeros(2, device="cuda"), offsets, 1.0)                # the KL term alone
+    q = near.double() - far.double()
+    assert ((d.double() + torch.expm1(q) / T).abs() <= 9 * u * torch.expm1(q) / T).all()
+    want = float((torch.expm1(q) - q).sum()) / T
+    assert abs(loss - want) <= 9 * u * want
+
+
+@pytest.mark.parametrize("T", [64, 70000])
+def test_sums_of_terms_that_cancel(T):
+    """Terms of 2^25 and 1 whose large ones cancel: exact in fp64, lost where fp32 adds them up. Ratios are 1 here, the terms the advantages with their signs turned."""
+    logp, a = torch.full((T,), -3.0, device="cuda"), torch.tensor([2.0 ** 25, 1.0, -2.0 ** 25, 1.0], device="cuda").repeat(T // 4)
+    d, loss, stats = policy(logp, logp, None, a, packed([T]), 0.0, by_position=True)
+    assert loss == -0.5 and stats[0].item() == -0.5 and torch.allclose(d * T, -a, rtol=2.0 ** -23, atol=0)
