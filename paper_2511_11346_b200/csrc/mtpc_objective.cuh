@@ -210,7 +210,8 @@ __device__ __forceinline__ void exp_beyond(const float (&q)[4], float (&beyond)[
   bool far = false;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    float s = 1.f / 40320.f;
+    float s = 1.f / 362880.f;
+    s = fmaf(s, q[i], 1.f / 40320.f);
     s = fmaf(s, q[i], 1.f / 5040.f);
     s = fmaf(s, q[i], 1.f / 720.f);
     s = fmaf(s, q[i], 1.f / 120.f);

@@ -109,3 +109,17 @@ def test_sums_of_terms_that_cancel(T):
     logp, a = torch.full((T,), -3.0, device="cuda"), torch.tensor([2.0 ** 25, 1.0, -2.0 ** 25, 1.0], device="cuda").repeat(T // 4)
     d, loss, stats = policy(logp, logp, None, a, packed([T]), 0.0, by_position=True)
     assert loss == -0.5 and stats[0].item() == -0.5 and torch.allclose(d * T, -a, rtol=2.0 ** -23, atol=0)
+
+
+@pytest.mark.parametrize("lo,hi", [(0.499, 0.4999999), (-0.4999999, -0.499), (0.48, 0.4999)])
+def test_series_of_the_kl_term(lo, hi):
+    """What the series of e^q - 1 - q leaves out at its end, |q| = 1/2: 2 q^8 / 10! = 2^-28.8 of q^2 / 2 (with one coefficient less 2^-24.5). A value's own roundings hide that; here
+    the terms' mean is less an advantage that is nearly it, so that the loss is what they are off together: the roundings of 2^17 different q (within 3 u each, u = 2^-24, of either
+    sign) average out to below u / 100, those of the coefficients (u / 2 of 1/6 and the ones behind it, of 1/2 nothing) stay below u q / 6 + u q^2 / 12 < u / 8. 2^-26 is a quarter of u."""
+    T = 1 << 17
+    logp = -(lo + (hi - lo) * torch.rand(T, device="cuda", dtype=torch.float64, generator=torch.Generator(device="cuda").manual_seed(3))).float()
+    q = -logp.double()
+    want = float((torch.expm1(q) - q).mean())
+    a = torch.tensor([want], dtype=torch.float32, device="cuda")
+    _, loss, _ = policy(logp, logp, torch.zeros(T, device="cuda"), a, packed([T]), 1.0)
+    assert abs(loss - (want - a.double().item())) <= 2.0 ** -26 * want
