@@ -400,6 +400,12 @@ int mtpc_launch_count(mtpc_head* head, uint64_t* out_count);
 int mtpc_debug_set_wait_limit_ns(mtpc_head* head, uint64_t limit_ns);
 
 /*
+ * Test hook: the same for the adapted projection and its gradients (below), which have no head: of all calls of the process from then on, until it is set again.
+ * Their calls report an expired wait in out_status alone.
+ */
+int mtpc_debug_set_adapted_wait_limit_ns(uint64_t limit_ns);
+
+/*
  * Test and measurement hook (no passage of the paper): which build of the projection kernel this head launches.
  * 0 (default): chosen per launch; 1: every CTA works alone (tcgen05 cta_group::1); 2: clusters of two CTAs share every
  * MMA (cta_group::2), MTPC_ERR_UNSUPPORTED if the device cannot hold such a cluster. The results are the same numbers

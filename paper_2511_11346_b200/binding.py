@@ -32,7 +32,7 @@ EXPORTS = [
     "mtpc_residual_rmsnorm", "mtpc_residual_rmsnorm_backward", "mtpc_residual_rmsnorm_backward_workspace_bytes",
     "mtpc_gradient_list_workspace_bytes", "mtpc_create_gradient_list", "mtpc_clip_gradients", "mtpc_destroy_gradient_list",
     "mtpc_adapted_projection_workspace_bytes", "mtpc_adapted_projection", "mtpc_adapted_projection_backward_workspace_bytes",
-    "mtpc_adapted_projection_backward", "mtpc_dropout", "mtpc_objective_workspace_bytes", "mtpc_policy_loss", "mtpc_preference_loss",
+    "mtpc_adapted_projection_backward", "mtpc_debug_set_adapted_wait_limit_ns", "mtpc_dropout", "mtpc_objective_workspace_bytes", "mtpc_policy_loss", "mtpc_preference_loss",
 ]
 STATIC_SCRATCH_BYTES = 16 << 20
 ERR_STATIC_SCRATCH = -7
@@ -118,6 +118,7 @@ def lib() -> ctypes.CDLL:
     L.mtpc_adapted_projection_backward_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, i32, ctypes.POINTER(sz)]
     L.mtpc_adapted_projection_backward.argtypes = [vp, i64, vp, i64, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, vp, vp, sz, vp,
                                                    vp]
+    L.mtpc_debug_set_adapted_wait_limit_ns.argtypes = [ctypes.c_uint64]
     L.mtpc_dropout.argtypes = [vp, i64, i32, vp, i64, i32, i32, f32, vp, i64, vp, i64, i32, vp]
     L.mtpc_objective_workspace_bytes.argtypes = [i32, i32, ctypes.POINTER(sz)]
     L.mtpc_policy_loss.argtypes = [vp, vp, vp, vp, i32, vp, vp, i32, i32, f32, f32, f32, i32, vp, vp, vp, vp, sz, vp, vp]
@@ -649,6 +650,11 @@ def mtpc_adapted_projection_backward(x_low, W, A, B, scale, row_adaptor, low, d_
     _call_with_workspace(what, lib().mtpc_adapted_projection_backward, dev, stream, workspace, need, _flat(what, out_status, 1, dev, _int32), x_at, x_stride, W_at, W_stride,
                          A_at, B_at, _flat(what, scale, S, dev, _float32), _flat(what, row_adaptor, T, dev, _int32), _like(what, "low", low, (T, k), dev), T, d, m, k, S,
                          g_at, g_stride, _ptr(d_x), dx_stride, _ptr(d_x_low), dl_stride, _like(what, "dA", dA, A.shape, dev), _like(what, "dB", dB, B.shape, dev))
+
+
+def mtpc_debug_set_adapted_wait_limit_ns(limit_ns: int) -> None:
+    """Test hook: time limit of the pipeline waits of the adapted projection and its gradients, of all later calls of the process (0: the default of 1 s)."""
+    _check(lib().mtpc_debug_set_adapted_wait_limit_ns(int(limit_ns)), "mtpc_debug_set_adapted_wait_limit_ns")
 
 
 def mtpc_dropout(x, out, p: float, rng, offset: int = 0, residual=None, stream=None) -> None:

@@ -6,6 +6,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <atomic>
 #include <initializer_list>
 
 #include "../../include/mtpc.h"
@@ -26,6 +27,7 @@ bool few_rows(int T, int k, int S) { return T <= std::min(128, 640 / std::max(k,
 constexpr int kMaxAdaptors = 4096, kMaxWidth = 1 << 17, kMaxBatch = 1 << 24;
 constexpr size_t kControl = 1024 + sizeof(GemmControl);
 constexpr int kRowsShared = sizeof(RowsShared) + 16;
+std::atomic<uint64_t> g_wait_limit_ns{kWaitLimitNs};      // of every pipeline wait (a test may shorten it)
 
 // ---------------------------------------------------------------- tensor maps
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
@@ -193,7 +195,7 @@ int launch_low(LowParams& p, const Rows& rows, const Rows& factors, bool mn, con
                cudaStream_t st) {
   p.which = which;
   p.status = status;
-  p.wait_limit_ns = kWaitLimitNs;
+  p.wait_limit_ns = g_wait_limit_ns.load(std::memory_order_relaxed);
   p.T = T;
   p.S = S;
   p.k = k;
@@ -273,7 +275,7 @@ int launch_product(const Rows& a, const Rows& b, const __nv_bfloat16* two, const
   p.out = static_cast<__nv_bfloat16*>(out);
   p.out_stride = out_stride;
   p.status = status;
-  p.wait_limit_ns = kWaitLimitNs;
+  p.wait_limit_ns = g_wait_limit_ns.load(std::memory_order_relaxed);
   p.T = T;
   p.S = S;
   p.N = N;
@@ -318,7 +320,7 @@ int launch_few_rows(const Rows& x, const Rows& W, const void* x_low, int64_t x_l
   p.out = static_cast<__nv_bfloat16*>(out);
   p.out_stride = out_stride;
   p.status = status;
-  p.wait_limit_ns = kWaitLimitNs;
+  p.wait_limit_ns = g_wait_limit_ns.load(std::memory_order_relaxed);
   p.T = T;
   p.S = S;
   p.N = m;
@@ -350,6 +352,11 @@ int launch_few_rows(const Rows& x, const Rows& W, const void* x_low, int64_t x_l
 }  // namespace
 
 extern "C" {
+
+int mtpc_debug_set_adapted_wait_limit_ns(uint64_t limit_ns) {
+  g_wait_limit_ns.store(limit_ns == 0 ? kWaitLimitNs : limit_ns, std::memory_order_relaxed);
+  return MTPC_OK;
+}
 
 int mtpc_adapted_projection_workspace_bytes(int32_t T, int32_t d, int32_t m, int32_t k, int32_t S, int32_t aligned_rows, size_t* out_bytes) {
   if (!out_bytes) return MTPC_ERR_NULL;
@@ -488,7 +495,7 @@ int mtpc_adapted_projection_backward(const void* x_low, int64_t x_low_stride, co
   p.out[1] = dB;
   p.part = reinterpret_cast<float*>(ws + plan.off_grad);
   p.status = out_status;
-  p.wait_limit_ns = kWaitLimitNs;
+  p.wait_limit_ns = g_wait_limit_ns.load(std::memory_order_relaxed);
   p.T = T;
   p.S = S;
   p.k = k;

@@ -330,7 +330,7 @@ __global__ void __launch_bounds__(kLowThreads, 2) adaptor_low_kernel(const __gri
   } else if (warp == 1) {
     const uint32_t lead = elect_one();
     uint32_t stage = 0, phase = 0, use = 0;
-    bool ok = true;
+    bool ok = rank >= p.chunks || first_wait(full0, ctl, p);
     const uint32_t f_step = F_MN ? 2u * factor_columns(p.k16) : 2u;
     const uint64_t a_desc0 = umma_smem_desc_sw128(tiles_addr);
     const uint64_t f_desc0 = F_MN ? umma_smem_desc_factor(tiles_addr + kABytes, factor_columns(p.k16)) : umma_smem_desc_sw128(tiles_addr + kABytes);
@@ -633,7 +633,7 @@ __global__ void __launch_bounds__(kAdaptedThreads, 1) adapted_gemm_kernel(const 
     if (cta_rank == 0) {
       const uint32_t lead = elect_one();
       uint32_t stage = 0, phase = 0, use = 0;
-      bool ok = true;
+      bool ok = first_item >= items || p.kblocks == 0 || first_wait(smem_u32(&ctl->full[0]), ctl, p);
       const uint32_t idesc = umma_idesc_bf16(kBlockM * CTAS, TN, false, B_MN);
       constexpr uint32_t kStepB = B_MN ? 128u : 2u;
       const uint64_t a_desc0 = umma_smem_desc_sw128(tiles_addr);
@@ -989,8 +989,8 @@ __global__ void __launch_bounds__(kRowsThreads, 2) adapted_rows_kernel(const __g
     const uint32_t idesc = umma_idesc_bf16(kBlockM, p.tokens);
     const uint64_t a_desc0 = umma_smem_desc_sw128(tiles_addr), b_desc0 = umma_smem_desc_sw128(tiles_addr + kABytes);
     uint32_t stage = 0, phase = 0;
-    bool ok = true;
-    for (int kb = kb0; kb < kb1; ++kb) {
+    bool ok = first_wait(full0, ctl, p);
+    for (int kb = kb0; kb < kb1 && ok; ++kb) {
       if (!bounded_wait_all(full0 + 8 * stage, phase, ctl, p)) { ok = false; break; }
       tc_fence_after();
       const uint64_t a_desc = a_desc0 + stage * (p.stage_bytes >> 4), b_desc = b_desc0 + stage * (p.stage_bytes >> 4);
@@ -1295,6 +1295,7 @@ __global__ void __launch_bounds__(kGradThreads, grad_ctas(K16)) adaptor_grad_ker
         if (n == 0) {
           slot = use % kSlots;
           if (!bounded_wait_all(smem_u32(&ctl->tempty[slot]), ((use / kSlots) & 1u) ^ 1u, ctl, p)) { ok = false; break; }
+          if (use == 0 && !first_wait(full0, ctl, p)) { ok = false; break; }
           ++use;
         }
         const bool whole = walk.all();
