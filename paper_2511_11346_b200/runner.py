@@ -80,24 +80,25 @@ def residual_rmsnorm_backward(total, weight, d_hidden, d_total=None, eps: float 
     return d_x, d_weight
 
 
-def adapted_projection(x, W, A, B_, scale=None, row_adaptor=None, x_low=None, keep_low=True):
+def adapted_projection(x, W, A, B_, scale=None, row_adaptor=None, x_low=None, keep_low=True, out_status=None):
     """Device bf16 tensors x [T, d], W [m, d] and the adaptors' factors A [S, m, k], B_ [S, k, d] -> (out [T, m], low [T, k] fp32 or None): W x and, for rows
-    with an adaptor, A low, low = scale B_ x (or B_ x_low)."""
+    with an adaptor, A low, low = scale B_ x (or B_ x_low). out_status: int32 [1], into which the status bits are or-ed (a wait that expired shows nowhere else)."""
     import torch
     out = torch.empty((x.shape[0], W.shape[0]), dtype=x.dtype, device=x.device)
     low = torch.empty((x.shape[0], A.shape[2]), dtype=torch.float32, device=x.device) if keep_low else None
-    B.mtpc_adapted_projection(x, W, A, B_, scale, row_adaptor, out, out_low=low, x_low=x_low)
+    B.mtpc_adapted_projection(x, W, A, B_, scale, row_adaptor, out, out_low=low, x_low=x_low, out_status=out_status)
     return out, low
 
 
-def adapted_projection_backward(x, W, A, B_, low, d_out, scale=None, row_adaptor=None, x_low=None):
-    """-> dict(d_x, dA, dB, d_x_low): gradients of adapted_projection from d_out [T, m] bf16; with x_low, d_x_low is its gradient (None otherwise)."""
+def adapted_projection_backward(x, W, A, B_, low, d_out, scale=None, row_adaptor=None, x_low=None, out_status=None):
+    """-> dict(d_x, dA, dB, d_x_low): gradients of adapted_projection from d_out [T, m] bf16; with x_low, d_x_low is its gradient (None otherwise).
+    out_status as above."""
     import torch
     f32 = dict(dtype=torch.float32, device=x.device)
     out = dict(d_x=torch.empty(x.shape, dtype=x.dtype, device=x.device), dA=torch.empty(A.shape, **f32), dB=torch.empty(B_.shape, **f32),
                d_x_low=None if x_low is None else torch.empty(x.shape, dtype=x.dtype, device=x.device))
     B.mtpc_adapted_projection_backward(x if x_low is None else x_low, W, A, B_, scale, row_adaptor, low, d_out, out["d_x"], out["dA"], out["dB"],
-                                       d_x_low=out["d_x_low"])
+                                       d_x_low=out["d_x_low"], out_status=out_status)
     return out
 
 

@@ -82,3 +82,31 @@ def test_captured_calls_keep_the_limit_that_they_were_captured_with(limit):
         torch.cuda.synchronize()
         assert status.item() == bits
     assert torch.equal(out, want)
+
+
+def test_the_allocating_forms_say_so_too(limit):
+    from paper_2511_11346_b200 import runner as R
+    T, d, m, k = 200, 256, 136, 16
+    new = lambda *s: torch.randn(s, device="cuda").bfloat16()  # noqa: E731
+    x, W, A, Bf, d_out = new(T, d), new(m, d), new(2, m, k), new(2, k, d), new(T, m)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+
+    def forward():
+        return R.adapted_projection(x, W, A, Bf, out_status=status)
+    low = forward()[1]
+
+    def backward():
+        return R.adapted_projection_backward(x, W, A, Bf, low, d_out, x_low=x, out_status=status)
+    backward()
+    assert status.item() == 0
+    for call in (forward, backward):
+        limit(50)
+        call()
+        assert status.item() == B.STATUS_TIMEOUT
+        status.zero_()
+        limit(0)
+        call()
+        assert status.item() == 0
+    none = torch.full((T,), 2, dtype=torch.int32, device="cuda")
+    R.adapted_projection(x, W, A, Bf, row_adaptor=none, out_status=status)
+    assert status.item() == B.STATUS_BAD_ADAPTOR
