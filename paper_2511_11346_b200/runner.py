@@ -263,11 +263,11 @@ class DeviceHead:
         return out
 
     def window_policy_backward(self, old_logp, ref_logp, advantage, offsets, clip_low=0.2, clip_high=0.2, beta=0.0, mask=None, by_sequence=False, hidden=None,
-                               targets=None):
+                               targets=None, by_position=False):
         """The clipped policy loss of the windows' log-likelihoods (positions of packed sequences) and its gradients -> the dicts of policy_loss and of
-        window_logprob_backward together."""
+        window_logprob_backward together. by_position: an advantage for every position."""
         logp = self.window_logprob(hidden=hidden, targets=targets)
-        out = policy_loss(logp, old_logp, ref_logp, advantage, offsets, clip_low, clip_high, beta, mask=mask, by_sequence=by_sequence)
+        out = policy_loss(logp, old_logp, ref_logp, advantage, offsets, clip_low, clip_high, beta, mask=mask, by_sequence=by_sequence, by_position=by_position)
         return dict(self.window_logprob_backward(out["d_logp"], hidden=hidden, targets=targets), **out)
 
     def window_preference_backward(self, ref_logp, offsets, beta=0.1, smoothing=0.0, mask=None, hidden=None, targets=None):
