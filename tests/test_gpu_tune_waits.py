@@ -46,10 +46,14 @@ def test_calls_give_up_and_recover(T, d, m, k, S, limit):
     assert status.item() == 0
     for call, right in zip(calls, want):
         limit(50)
-        got = call()
-        torch.cuda.synchronize()                              # the kernels returned; the context is alive
-        # one step of K is one copy, which may have landed before its wait begins (the waiting warp's instructions come from memory too): no wait expires then
-        assert status.item() == B.STATUS_TIMEOUT or (d <= 64 and status.item() == 0 and equal(got, right))
+        for _ in range(20):
+            # a copy may have landed before its wait begins, since the waiting warp's instructions come from memory too the first time: no wait expires then
+            got = call()
+            torch.cuda.synchronize()                          # the kernels returned; the context is alive
+            if status.item() != 0:
+                break
+            assert equal(got, right)
+        assert status.item() == B.STATUS_TIMEOUT
         status.zero_()
         limit(0)
         assert equal(call(), right) and status.item() == 0
@@ -78,7 +82,8 @@ def test_captured_calls_keep_the_limit_that_they_were_captured_with(limit):
     limit(0)
     for graph, bits in zip(graphs, (B.STATUS_TIMEOUT, 0)):
         status.zero_()
-        graph.replay()
+        for _ in range(20):
+            graph.replay()
         torch.cuda.synchronize()
         assert status.item() == bits
     assert torch.equal(out, want)
@@ -101,7 +106,8 @@ def test_the_allocating_forms_say_so_too(limit):
     assert status.item() == 0
     for call in (forward, backward):
         limit(50)
-        call()
+        for _ in range(20):
+            call()
         assert status.item() == B.STATUS_TIMEOUT
         status.zero_()
         limit(0)
