@@ -20,9 +20,11 @@ using namespace mtpc;
 
 constexpr int kSmemLimit = 232448;      // 227 KB of dynamic shared memory per CTA on sm_100
 // Rows that are dealt with each by itself (as the N of MMAs whose M are W's rows) rather than as tiles of 128. There every row costs time by its rank, in tiles every adaptor
-// that occurs does. 4096 x 4096, rows in random order, us by rows / in tiles: k = 16, one adaptor 32 rows 12.3 / 14.1, 64 rows 14.5 / 14.3, 128 rows 18.8 / 14.5; four 64 rows
-// 14.6 / 14.8, 128 rows 18.9 / 15.1; 32 adaptors 128 rows 19.7 / 33.5; k = 64, one adaptor 16 rows 14.2 / 14.0, four 32 rows 19.0 / 20.0, 64 rows 25.4 / 19.8, 32 adaptors
-// 128 rows 49.8 / 84.7.
+// that occurs does. 4096 x 4096, rows in random order, graph replays, us by rows / in tiles: k = 16, one adaptor 64 rows 10.1 / 12.1, 96 rows 13.4 / 12.2; eight 96 rows 13.5, 128
+// rows 15.7 / 13.9; 32 adaptors 128 rows 16.0 / 28.1 (129 rows); k = 64, one 16 rows 10.3, 32 rows 13.9 / 12.2; four 32 rows 14.9, 48 rows 19.5 / 14.7; eight 64 rows 24.2, 96
+// rows 37.7 / 21.2; 32 adaptors 128 rows 44.5 / 60.8 (129 rows).
+// S counts the adaptors that there are, since which of them occur is known on the device alone. Where fewer do, tiles would be faster: 128 rows of one of 64 adaptors 15.7 / 12.4
+// (k = 16), 41.6 / 12.6 (k = 64).
 bool few_rows(int T, int k, int S) { return T <= std::min(128, 640 / std::max(k, 8) + 8 * S); }
 constexpr int kMaxAdaptors = 4096, kMaxWidth = 1 << 17, kMaxBatch = 1 << 24;
 constexpr size_t kControl = 1024 + sizeof(GemmControl);
@@ -329,9 +331,10 @@ int launch_few_rows(const Rows& x, const Rows& W, const void* x_low, int64_t x_l
   const int tiles = ceil_div(m, kBlockM);
   // K is cut into up to four parts until the CTAs are as many as the device holds at once, two on an SM; one row by itself and more than 32 into eight, the latter where each
   // still has an SM of its own (4096 x 4096, k = 16, two / four / eight parts, us: one row 17.5 / 13.2 / 10.3, 16 rows 12.3 / 11.5 / 13.4, 64 rows 19.0 / 14.3 / 17.4; 1024 rows
-  // of W: 64 rows 13.0 / 7.9 / 7.5).
+  // of W: 64 rows 13.0 / 7.9 / 7.5), or where reading their adaptors' factors, for which more CTAs have more loads in flight, takes longer than that costs (four / eight parts:
+  // k = 32, 64 rows 14.2 / 16.0, 128 rows 33.4 / 24.1; k = 48, 48 rows 18.6 / 14.8; k = 64, 64 rows 39.2 / 24.5, 128 rows 75.4 / 44.4).
   int split = 1;
-  while (split < (own_low || T > 32 ? 8 : 4) && split * 2 <= p.kblocks && tiles * split * (split < 4 || own_low ? 1 : 2) <= kSms) split *= 2;
+  while (split < (own_low || T > 32 ? 8 : 4) && split * 2 <= p.kblocks && tiles * split * (split < 4 || own_low || T * k > 2048 ? 1 : 2) <= kSms) split *= 2;
   p.stage_bytes = kABytes + p.tokens * kBlockK * 2;
   const int shared = kRowsShared + (own_low ? 0 : ceil_div(T, split) * k * 4);       // (32 KB at most: two stages are left of the longest, and hold the sums)
   p.stages = stages_of(p.stage_bytes, 2, shared);
@@ -340,7 +343,7 @@ int launch_few_rows(const Rows& x, const Rows& W, const void* x_low, int64_t x_l
   p.own = l;
   p.own.low = user_low;
   const size_t smem = kControl + shared + static_cast<size_t>(p.stages) * p.stage_bytes;
-  const bool many = ceil_div(T, 2 * split) > 4;           // rows of a thread
+  const bool many = ceil_div(T, 2 * split) > 4 && k <= 16;           // rows of a thread; behind sixteen of rank their loads are not ahead (128 rows, k = 64: 49.2 / 44.4 us)
   const auto pick = [&](auto* s1, auto* s2, auto* s4, auto* s8) { return split == 8 ? s8 : split == 4 ? s4 : split == 2 ? s2 : s1; };
   auto* kernel = own_low ? pick(adapted_rows_kernel<1, true, 4>, adapted_rows_kernel<2, true, 4>, adapted_rows_kernel<4, true, 4>, adapted_rows_kernel<8, true, 4>)
                  : many  ? pick(adapted_rows_kernel<1, false, 8>, adapted_rows_kernel<2, false, 8>, adapted_rows_kernel<4, false, 8>, adapted_rows_kernel<8, false, 8>)
