@@ -20,7 +20,7 @@ using namespace mtpc;
 
 constexpr int kSmemLimit = 232448;      // 227 KB of dynamic shared memory per CTA on sm_100
 // Rows that are dealt with each by itself (as the N of MMAs whose M are W's rows) rather than as tiles of 128. There every row costs time by its rank, in tiles every adaptor
-// that occurs does. 4096 x 4096, rows in random order, graph replays, us by rows / in tiles: k = 16, one adaptor 64 rows 10.1 / 12.1, 96 rows 13.4 / 12.2; eight 96 rows 13.5, 128
+// that occurs does. 4096 x 4096, rows in random order, graph replays with the operands in L2, us by rows / in tiles: k = 16, one adaptor 64 rows 10.1 / 12.1, 96 rows 13.4 / 12.2; eight 96 rows 13.5, 128
 // rows 15.7 / 13.9; 32 adaptors 128 rows 16.0 / 28.1 (129 rows); k = 64, one 16 rows 10.3, 32 rows 13.9 / 12.2; four 32 rows 14.9, 48 rows 19.5 / 14.7; eight 64 rows 24.2, 96
 // rows 37.7 / 21.2; 32 adaptors 128 rows 44.5 / 60.8 (129 rows).
 // S counts the adaptors that there are, since which of them occur is known on the device alone. Where fewer do, tiles would be faster: 128 rows of one of 64 adaptors 15.7 / 12.4
@@ -331,7 +331,7 @@ int launch_few_rows(const Rows& x, const Rows& W, const void* x_low, int64_t x_l
   const int tiles = ceil_div(m, kBlockM);
   // K is cut into up to four parts until the CTAs are as many as the device holds at once, two on an SM; one row by itself and more than 32 into eight, the latter where each
   // still has an SM of its own (4096 x 4096, k = 16, two / four / eight parts, us: one row 17.5 / 13.2 / 10.3, 16 rows 12.3 / 11.5 / 13.4, 64 rows 19.0 / 14.3 / 17.4; 1024 rows
-  // of W: 64 rows 13.0 / 7.9 / 7.5), or where reading their adaptors' factors, for which more CTAs have more loads in flight, takes longer than that costs (four / eight parts:
+  // of W: 64 rows 13.0 / 7.9 / 7.5), or where reading their adaptors' factors, for which more CTAs have more loads in flight, takes longer than that costs (four / eight parts, operands in L2:
   // k = 32, 64 rows 14.2 / 16.0, 128 rows 33.4 / 24.1; k = 48, 48 rows 18.6 / 14.8; k = 64, 64 rows 39.2 / 24.5, 128 rows 75.4 / 44.4).
   int split = 1;
   while (split < (own_low || T > 32 ? 8 : 4) && split * 2 <= p.kblocks && tiles * split * (split < 4 || own_low || T * k > 2048 ? 1 : 2) <= kSms) split *= 2;

@@ -11,8 +11,9 @@
 // take them in fp64. Whether a ratio is clipped is decided on both terms, against the logarithms of the ends in two terms as well, since a position beside an end would else
 // change sides by a rounding. What a position comes to (ratios, products, slopes) is fp32; sums are fp64, in an order that sizes fix.
 //
-// Work is dealt in items: a warp has one of P equal slices of one sequence, so that long sequences among short ones spread over the device and no
-// position has to look for its sequence. Weights need the counts of valid positions first, so the call goes over the data twice (the mask alone
+// Work is dealt in items: a warp has one of P equal slices of one sequence, so that no position has to look for its sequence. P is the same for all sequences, 4736 / S at most
+// (the warps that the device holds), so lengths that differ leave warps idle: 1.6 million positions in 256 sequences alike 15 us (masked, policy), with all but 255 x 128 of them
+// in one sequence, which 18 warps then have, 760. Weights need the counts of valid positions first, so the call goes over the data twice (the mask alone
 // for the counts, every warp over that of its own sequence where that is all it needs; logp and ref for the sums of pairs). Few positions: all phases in one launch of one cluster, with its barrier between
 // them (a chain of four kernels of 2 us each otherwise); many: a launch for each phase. Bound by launches and their chains of loads: 1.6 million masked positions 16.0 us (policy; with differences and
 // sums of four in fp32 alone 14.5) and 12.0 (preference), of which the bytes are 4 and 3; a few hundred positions 8, mostly the host's.

@@ -37,7 +37,7 @@ void launch_dropout(const DropoutArgs& a, bool vectors, cudaStream_t st) {
 constexpr int kMaxSequences = 1 << 20;
 constexpr int kSmallPositions = 1 << 16;
 constexpr int kOwnParts = 64, kOwnPairs = 1024;
-constexpr int kOwnCount = 1 << 14;      // mean length up to which a sequence's positions are counted by each of its warps: 16 vectors a lane
+constexpr int kOwnCount = 1 << 14;      // mean length up to which a sequence's positions are counted by each of its warps: 32 vectors of 16 bytes a lane
 struct ObjectivePlan {
   int parts;
   bool small;                           // one cluster does it, without a workspace
