@@ -1,5 +1,5 @@
 """The losses of sequences in the forms that long batches take, against the same in vectors of fp64 (u = 2^-24). The warps' slices of a sequence, here `parts_of`, decide the form.
-policy: expf is within 2 units in the last place (4 u), a difference of log-likelihoods rounded to fp32 within |diff| u <= 2 u here, the product with the advantage, the weight and its
+policy: expf is within 2 units in the last place (4 u), what rounding leaves of a difference of log-likelihoods is taken in within u, the product with the advantage, the weight and its
 product u each; the KL term's e^q - 1 as much of |e^q - 1| + |q|, e^q - 1 - q within 12 u of e^q: 12 u of the terms' magnitudes, as in the test of short batches. preference: fp64, rounded once."""
 import numpy as np
 import pytest
